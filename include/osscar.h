@@ -58,7 +58,7 @@ typedef enum {
   OSSCAR_ESTATE = 5  /* call order violated, or the context is poisoned by an earlier failure */
 } osscar_status;
 
-typedef enum { OSSCAR_F32 = 0, OSSCAR_BF16 = 1 } osscar_dtype;
+typedef enum { OSSCAR_F32 = 0, OSSCAR_BF16 = 1, OSSCAR_I8 = 2 /* activations of osscar_int_product only */ } osscar_dtype;
 
 /* Problem description (Section 3: d1 x m weights, p groups of q rows; Section 4.1: keep k = p - p'). */
 typedef struct {
@@ -314,6 +314,87 @@ int32_t osscar_debug_tile_schedule(int64_t d1, int32_t* out_host, int32_t capaci
 osscar_status osscar_gram_static(const void* X_dev, int64_t n, int64_t ldx, int32_t x_dtype, const void* W_dev, int64_t ldw,
                                  int32_t w_dtype, int64_t d1, int64_t m, double lambda_abs, double lambda_rel, float* H_dev,
                                  float* G_dev, double* scalars_dev, void* hip_stream);
+
+/* ----------------------------------------------------------------------------------------------------------------------
+ * Running, serving, scoring and training a pruned layer.  These calls take no context.  Everything is enqueued on
+ * hip_stream (a hipStream_t, NULL = default stream) and may be captured into a graph; no call waits for it, allocates or keeps
+ * anything.  A workspace is device memory of the size that the query beside the call names, at a 256-byte boundary, with any
+ * contents; two calls may use the same one if they are ordered.  Buffers of one call must not overlap unless said.  dtypes are
+ * OSSCAR_F32 or OSSCAR_BF16 unless said.  No size may exceed 2^30.  After a failure osscar_last_error(NULL) describes it (per host thread).
+ * ---------------------------------------------------------------------------------------------------------------------- */
+
+/* Gated feed-forward layer (the other common form of the layers whose neurons Section 3 prunes; its output is the X of the
+ * down projection's Gram, osscar_gram):
+ *   g = X Wg,  u = X Wu,  H = act(g) * u  (element by element),   X n x d, Wg and Wu d x f, H n x f.
+ * Sums are float32 (float32 operands: as three bf16 pieces each, which leaves the error of a float32 product); H is rounded once. */
+enum { OSSCAR_ACT_SILU = 0, OSSCAR_ACT_GELU = 1 /* 0.5 g (1 + erf(g / sqrt 2)) */, OSSCAR_ACT_GELU_TANH = 2, OSSCAR_ACT_RELU = 3 };
+typedef struct {
+  int64_t n, d, f;    /* tokens (n = 0: nothing to do), inputs, neurons */
+  int64_t ldx;        /* leading dimension of X */
+  int64_t ldw;        /* leading dimension of Wg and Wu */
+  int64_t ldh;        /* leading dimension of H and dH */
+  int32_t dtype;      /* of X, Wg, Wu, H, dH, dX */
+  int32_t act;
+  int32_t rows_out;   /* 0: Wg, Wu are d x f in memory (as W of this interface); nonzero: f x d, a neuron's weights side by side */
+  int32_t unaligned;  /* nonzero: X, Wg or Wu may begin at any element; zero: at a 16-byte boundary (bf16) */
+} osscar_gated_desc;
+/* Workspace of a forward (backward = 0) or backward call; 0 if the description is invalid.  Small, unless rows are copied: float32
+ * operands, and bf16 operands whose rows do not begin at 16-byte boundaries or are not a multiple of 8 long. */
+size_t osscar_gated_workspace_bytes(const osscar_gated_desc* desc, int32_t backward);
+/* G_dev, U_dev (both or neither): dense n x f float32 outputs, g and u for osscar_gated_backward. */
+osscar_status osscar_gated_forward(const osscar_gated_desc* desc, const void* X_dev, const void* Wg_dev, const void* Wu_dev, void* H_dev,
+                                   float* G_dev, float* U_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+/* Gradients, given dH (n x f, leading dimension ldh):  dg = dH u act'(g), du = dH act(g) (both rounded to the dtype before the
+ * products), dX = dg Wg^T + du Wu^T, dWg = X^T dg, dWu = X^T du.  G_dev, U_dev: what forward left there, or NULL: g and u are computed
+ * again.  dX_dev (may be NULL): leading dimension lddx.  dWg_dev, dWu_dev (both or neither): layout of Wg, leading dimension lddw, dtype
+ * dw_dtype; they are written, not added to.  act' is 0 at the corner of ReLU. */
+osscar_status osscar_gated_backward(const osscar_gated_desc* desc, const void* X_dev, const void* Wg_dev, const void* Wu_dev, const void* dH_dev,
+                                    const float* G_dev, const float* U_dev, void* dX_dev, int64_t lddx, void* dWg_dev, void* dWu_dev, int64_t lddw,
+                                    int32_t dw_dtype, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* Products in 8-bit integers, for serving kept rows: with a scale per token and one per output channel
+ *   s_i = max_k |X_ik| / 127,  q_ik = X_ik / s_i to the nearest integer (halves to even),  Y_ij = s_i w_j sum_k q_ik Wq_jk + bias_j.
+ * The sum is exact (int32; d1 <= OSSCAR_INT_MAX_DIM).  A row of zeros has scale 0 and gives bias; a row with an infinity or NaN gives NaN, and
+ * so does a channel.
+ * osscar_int_weights: W_dev is d1 x m (rows_out = 0) or m x d1 (nonzero) in memory, leading dimension ldw; Wq_dev is m x d1 with leading
+ * dimension ldq (a multiple of 16, at a 16-byte boundary; zeros from column d1 on), w_scale_dev m float32.
+ * osscar_int_rows: the same of the n rows of X, for several products with the same X. */
+#define OSSCAR_INT_MAX_DIM 131071
+osscar_status osscar_int_weights(const void* W_dev, int64_t d1, int64_t m, int64_t ldw, int32_t w_dtype, int32_t rows_out, int8_t* Wq_dev, int64_t ldq,
+                                 float* w_scale_dev, void* hip_stream);
+osscar_status osscar_int_rows(const void* X_dev, int64_t n, int64_t d1, int64_t ldx, int32_t x_dtype, int8_t* Xq_dev, int64_t ldq, float* x_scale_dev,
+                              void* hip_stream);
+/* Workspace of osscar_int_product; 0 if the sizes are invalid. */
+size_t osscar_int_workspace_bytes(int64_t n, int64_t d1, int64_t m);
+/* x_dtype OSSCAR_F32 or OSSCAR_BF16: X is quantised here, x_scale_dev must be NULL; OSSCAR_I8: X_dev is Xq with x_scale_dev (n float32).
+ * Wq_dev as osscar_int_weights leaves it (what lies in a row from column d1 on does not matter).  bias_dev: m float32, or NULL.  Y_dev: n x m,
+ * leading dimension ldy, dtype y_dtype. */
+osscar_status osscar_int_product(const void* X_dev, int64_t n, int64_t d1, int64_t ldx, int32_t x_dtype, const float* x_scale_dev, const int8_t* Wq_dev,
+                                 int64_t ldq, const float* w_scale_dev, int64_t m, const float* bias_dev, void* Y_dev, int64_t ldy, int32_t y_dtype,
+                                 void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* What a model answers with, from its logits (n x vocab, leading dimension ld, the paper's perplexities are the exponential of the mean of -logp;
+ * Section 5): with z = scale * logits and scale > 0,
+ *   logp_i = z_{i,t_i} - lse_i,  entropy_i = -sum_v p_iv log p_iv,  lse_i = log sum_v exp z_iv,
+ * and the `top` (<= OSSCAR_TOP_MAX, <= vocab) largest logits of each row, largest first, equal ones by index, NaN before all others.
+ * targets_dev: n int64; negative: the row has no target, logp_i = 0; vocab or more: logp_i = NaN.
+ * logp_dev, entropy_dev: n float32 (entropy may be NULL).  lse_dev: n x 2 float32 (may be NULL), the largest logit m of the row and
+ * log sum_v exp(scale (l_v - m)): lse_i = scale m + that, in two parts for osscar_logprobs_backward.  top_index_dev, top_logp_dev: n x top int64 and float32
+ * (ignored with top = 0).  A logit of minus infinity has probability 0.  A row of nothing else has lse minus infinity, entropy 0, and logp minus infinity
+ * for its target and its alternatives; a row with NaN or plus infinity has NaN. */
+#define OSSCAR_TOP_MAX 64
+size_t osscar_logprobs_workspace_bytes(int64_t n, int64_t vocab, int32_t top);
+osscar_status osscar_logprobs(const void* logits_dev, int64_t n, int64_t vocab, int64_t ld, int32_t dtype, const int64_t* targets_dev, float scale,
+                              int32_t top, float* logp_dev, float* entropy_dev, float* lse_dev, int64_t* top_index_dev, float* top_logp_dev,
+                              void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+/* Gradient of sum_i (dlogp_i logp_i + dentropy_i entropy_i + sum_j dtop_ij top_logp_ij) with respect to the logits:
+ *   scale [ dlogp (1{v = t} - p_v) - dentropy p_v (log p_v + entropy) + sum_j dtop_j (1{v = top_index_j} - p_v) ].
+ * Any of dlogp_dev, dentropy_dev and dtop_dev may be NULL; entropy_dev goes with dentropy_dev, top_index_dev with dtop_dev.  A row without a target ignores
+ * dlogp_i; a target of vocab or more makes the row NaN; a row of minus infinities alone has gradient 0.  dlogits_dev: leading dimension ldd, dtype as
+ * logits; it may be logits_dev itself (with ldd = ld). */
+osscar_status osscar_logprobs_backward(const void* logits_dev, int64_t n, int64_t vocab, int64_t ld, int32_t dtype, const int64_t* targets_dev, float scale,
+                                       const float* lse_dev, const float* dlogp_dev, const float* entropy_dev, const float* dentropy_dev, int32_t top,
+                                       const int64_t* top_index_dev, const float* dtop_dev, void* dlogits_dev, int64_t ldd, void* hip_stream);
 
 /* Description of the last failure: of a context, or (ctx == NULL) of the last failed call on this host thread that takes
  * no context. */

@@ -9,7 +9,8 @@ from typing import Tuple, Optional, Sequence
 import numpy as np
 import torch
 
-OSSCAR_F32, OSSCAR_BF16 = 0, 1
+OSSCAR_F32, OSSCAR_BF16, OSSCAR_I8 = 0, 1, 2
+OSSCAR_ACT_SILU, OSSCAR_ACT_GELU, OSSCAR_ACT_GELU_TANH, OSSCAR_ACT_RELU = 0, 1, 2, 3
 OSSCAR_INIT_MAGNITUDE, OSSCAR_INIT_GIVEN = 0, 1
 OSSCAR_SEARCH_ALWAYS_ACCEPT = 1
 OSSCAR_SEARCH_EAGER = 2
@@ -26,7 +27,10 @@ EXPORTED_SYMBOLS = ["osscar_workspace_bytes", "osscar_create", "osscar_destroy",
                     "osscar_init_support", "osscar_init_greedy", "osscar_local_search", "osscar_block_search", "osscar_apply_swap", "osscar_backsolve",
                     "osscar_get_tensor", "osscar_get_scalars", "osscar_get_timers", "osscar_get_counters", "osscar_debug_tile_schedule",
                     "osscar_debug_gemm_log", "osscar_debug_gemm_log_read", "osscar_debug_int_products", "osscar_debug_refined_inverse", "osscar_debug_side_stream",
-                    "osscar_gram_static", "osscar_last_error"]
+                    "osscar_gram_static", "osscar_last_error",
+                    "osscar_gated_workspace_bytes", "osscar_gated_forward", "osscar_gated_backward",
+                    "osscar_int_weights", "osscar_int_rows", "osscar_int_workspace_bytes", "osscar_int_product",
+                    "osscar_logprobs_workspace_bytes", "osscar_logprobs", "osscar_logprobs_backward"]
 
 
 class OsscarError(RuntimeError):
@@ -39,6 +43,11 @@ class _Desc(C.Structure):
     _fields_ = [("d1", C.c_int64), ("m", C.c_int64), ("p", C.c_int32), ("q", C.c_int32), ("k", C.c_int32),
                 ("max_swaps", C.c_int32), ("x_dtype", C.c_int32), ("w_dtype", C.c_int32), ("from_dense", C.c_int32),
                 ("target_output", C.c_int32)]
+
+
+class _GatedDesc(C.Structure):
+    _fields_ = [("n", C.c_int64), ("d", C.c_int64), ("f", C.c_int64), ("ldx", C.c_int64), ("ldw", C.c_int64), ("ldh", C.c_int64),
+                ("dtype", C.c_int32), ("act", C.c_int32), ("rows_out", C.c_int32), ("unaligned", C.c_int32)]
 
 
 class _SearchResult(C.Structure):
@@ -92,10 +101,23 @@ def load_library():
     lib.osscar_gram_static.argtypes = [vp, i64, i64, i32, vp, i64, i32, i64, i64, dbl, dbl, vp, vp, vp, vp]
     lib.osscar_debug_tile_schedule.restype = C.c_int32
     lib.osscar_debug_tile_schedule.argtypes = [i64, C.POINTER(i32), i32]
+    for name in ("osscar_gated_workspace_bytes", "osscar_int_workspace_bytes", "osscar_logprobs_workspace_bytes"):
+        getattr(lib, name).restype = C.c_size_t
+    gd, f32 = C.POINTER(_GatedDesc), C.c_float
+    lib.osscar_gated_workspace_bytes.argtypes = [gd, i32]
+    lib.osscar_gated_forward.argtypes = [gd, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.osscar_gated_backward.argtypes = [gd, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp, i64, i32, vp, C.c_size_t, vp]
+    lib.osscar_int_weights.argtypes = [vp, i64, i64, i64, i32, i32, vp, i64, vp, vp]
+    lib.osscar_int_rows.argtypes = [vp, i64, i64, i64, i32, vp, i64, vp, vp]
+    lib.osscar_int_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.osscar_int_product.argtypes = [vp, i64, i64, i64, i32, vp, vp, i64, vp, i64, vp, vp, i64, i32, vp, C.c_size_t, vp]
+    lib.osscar_logprobs_workspace_bytes.argtypes = [i64, i64, i32]
+    lib.osscar_logprobs.argtypes = [vp, i64, i64, i64, i32, vp, f32, i32, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.osscar_logprobs_backward.argtypes = [vp, i64, i64, i64, i32, vp, f32, vp, vp, vp, vp, i32, vp, vp, vp, i64, vp]
     lib.osscar_last_error.restype = C.c_char_p
     lib.osscar_last_error.argtypes = [vp]
     for name in EXPORTED_SYMBOLS:
-        if name not in ("osscar_workspace_bytes", "osscar_last_error", "osscar_debug_tile_schedule", "osscar_debug_gemm_log_read"):
+        if not name.endswith("workspace_bytes") and name not in ("osscar_last_error", "osscar_debug_tile_schedule", "osscar_debug_gemm_log_read"):
             getattr(lib, name).restype = C.c_int
     _LIB = lib
     return lib

@@ -1,0 +1,392 @@
+// Gated feed-forward: g = X Wg, u = X Wu, h = a(g) u with a one of SiLU, GELU (two forms), ReLU; its backward pass
+//     dg = dh u a'(g), du = dh a(g);   dX = dg Wg^T + du Wu^T, dWg = X^T dg, dWu = X^T du.
+// h is the X that the Gram of the layer's down projection takes.
+#include "ops.h"
+#include "tile.h"
+
+using namespace osscar;
+using namespace osscar::tile;
+
+namespace {
+
+// ---- activations -----------------------------------------------------------------------------
+// logistic function; e^-x past float32's range gives 0
+__device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }
+constexpr float ROOT_HALF = 0.70710678118654752f, TWO_ROOT_2_PI = 1.5957691216057308f, ROOT_2PI_INV = 0.39894228040143268f;
+
+template <int ACT>
+__device__ __forceinline__ float act_value(float g) {
+  if (ACT == OSSCAR_ACT_SILU) return g * logistic(g);
+  if (ACT == OSSCAR_ACT_GELU) return 0.5f * g * (1.f + erff(g * ROOT_HALF));
+  if (ACT == OSSCAR_ACT_GELU_TANH) return g * logistic(TWO_ROOT_2_PI * (g + 0.044715f * g * g * g));      // (1 + tanh(w / 2)) / 2 is the logistic function of w
+  return g > 0.f ? g : (g == g ? 0.f : g);      // NaN stays
+}
+template <int ACT>
+__device__ __forceinline__ void act_slope(float g, float& a, float& da) {
+  if (ACT == OSSCAR_ACT_SILU) {
+    const float s = logistic(g);
+    a = g * s;
+    da = s + a * (1.f - s);
+  } else if (ACT == OSSCAR_ACT_GELU) {
+    const float c = 0.5f * (1.f + erff(g * ROOT_HALF));
+    a = g * c;
+    da = c + g * __expf(-0.5f * g * g) * ROOT_2PI_INV;
+  } else if (ACT == OSSCAR_ACT_GELU_TANH) {
+    const float s = logistic(TWO_ROOT_2_PI * (g + 0.044715f * g * g * g));
+    a = g * s;
+    da = s + a * (1.f - s) * TWO_ROOT_2_PI * (1.f + 3.f * 0.044715f * g * g);
+  } else {
+    a = act_value<OSSCAR_ACT_RELU>(g);
+    da = g > 0.f ? 1.f : (g == g ? 0.f : g);
+  }
+}
+// f(integral_constant) for the activation of a call
+template <class F>
+__device__ __forceinline__ void with_act(int act, F f) {
+  switch (act) {
+    case OSSCAR_ACT_SILU: f(std::integral_constant<int, OSSCAR_ACT_SILU>()); break;
+    case OSSCAR_ACT_GELU: f(std::integral_constant<int, OSSCAR_ACT_GELU>()); break;
+    case OSSCAR_ACT_GELU_TANH: f(std::integral_constant<int, OSSCAR_ACT_GELU_TANH>()); break;
+    default: f(std::integral_constant<int, OSSCAR_ACT_RELU>());
+  }
+}
+
+// ---- float32 as three bf16 -------------------------------------------------------------------
+// x = p0 + p1 + p2, each the nearest bf16 of what is left: 24 bits.  What bf16 cannot hold as a finite number (infinities, NaN, the last
+// float32 values) goes into p0 alone, as it is or, if finite, cut off.
+__device__ __forceinline__ void cut3(float x, uint16_t (&p)[3]) {
+  uint16_t b = bf16_nearest(x);
+  if ((b & 0x7F80) == 0x7F80) {
+    const uint32_t u = __float_as_uint(x);
+    if ((u & 0x7F800000u) == 0x7F800000u) { p[0] = b; p[1] = p[2] = 0; return; }
+    b = (uint16_t)(u >> 16);
+  }
+  p[0] = b;
+  const float r = x - bf16_value(b);
+  p[1] = bf16_nearest(r);
+  p[2] = bf16_nearest(r - bf16_value(p[1]));
+}
+// C neighbouring values as `pieces` bf16 each, in arrays `step` elements apart; columns from `most` on become zeros up to `width`
+template <int C>
+__device__ __forceinline__ void put_pieces(uint16_t* p, int64_t step, int pieces, const float (&v)[C], int most, int width) {
+#pragma unroll
+  for (int c = 0; c < C; c += 8) {
+    if (c >= width) break;      // (width is a multiple of eight)
+    u16x8 w[3];
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      const float x = c + e < most ? v[c + e] : 0.f;
+      if (pieces == 1) {
+        w[0][e] = bf16_nearest(x);
+      } else {
+        uint16_t t[3];
+        cut3(x, t);
+        w[0][e] = t[0]; w[1][e] = t[1]; w[2][e] = t[2];
+      }
+    }
+    *reinterpret_cast<u16x8*>(p + c) = w[0];
+    if (pieces > 1) {
+      *reinterpret_cast<u16x8*>(p + step + c) = w[1];
+      *reinterpret_cast<u16x8*>(p + 2 * step + c) = w[2];
+    }
+  }
+}
+// A matrix as `pieces` matrices of bf16 whose rows are `ld` long (a multiple of eight, zeros past cols).  Eight columns per thread; bound by
+// its reads and writes.
+__global__ __launch_bounds__(256) void gated_pieces_kernel(const void* __restrict__ src, int f32, int64_t rows, int cols, int64_t lds_, uint16_t* __restrict__ dst,
+                                                           int64_t ld, int64_t step, int pieces) {
+  const int packs = (int)(ld / 8);
+  for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < rows * packs; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / packs;
+    const int c = (int)(i - r * packs) * 8;
+    float v[8];
+    get_values(src, r * lds_ + c, f32, v, cols - c);
+    put_pieces(dst + r * ld + c, step, pieces, v, cols - c, 8);
+  }
+}
+
+// ---- epilogues -------------------------------------------------------------------------------
+struct GatedOut {      // h, and g and u as they are where the caller keeps them for the backward pass
+  void* H; int64_t ldh; int f32, act; float *G, *U;
+  template <int C>
+  __device__ __forceinline__ void put(int m, int n, const float (&v)[2][C], int, int N) const {
+    float h[C];
+    with_act(act, [&](auto a) {
+#pragma unroll
+      for (int c = 0; c < C; c++) h[c] = act_value<decltype(a)::value>(v[0][c]) * v[1][c];
+    });
+    if (f32) put_f32(reinterpret_cast<float*>(H) + (int64_t)m * ldh + n, h, N - n);
+    else put_bf16(reinterpret_cast<uint16_t*>(H) + (int64_t)m * ldh + n, h, N - n);
+    if (G) {
+      put_f32(G + (int64_t)m * N + n, v[0], N - n);
+      put_f32(U + (int64_t)m * N + n, v[1], N - n);
+    }
+  }
+};
+// dg and du, rounded to bf16 (they are operands of the next products, as h is of the next layer) or in three pieces
+struct GradPlace { uint16_t *dg, *du; int64_t ld, step; int pieces; };
+template <int C>
+__device__ __forceinline__ void put_grad(const GradPlace& o, int act, int64_t row, int n, int N, const float (&g)[C], const float (&u)[C], const float (&dh)[C]) {
+  float dg[C], du[C];
+  with_act(act, [&](auto a) {
+#pragma unroll
+    for (int c = 0; c < C; c++) {
+      float av, da;
+      act_slope<decltype(a)::value>(g[c], av, da);
+      dg[c] = dh[c] * u[c] * da;
+      du[c] = dh[c] * av;
+    }
+  });
+  const int64_t at = row * o.ld + n;
+  put_pieces(o.dg + at, o.step, o.pieces, dg, N - n, (int)o.ld - n);
+  put_pieces(o.du + at, o.step, o.pieces, du, N - n, (int)o.ld - n);
+}
+struct GatedGrad {
+  const void* dH; int64_t lddh; int f32, act; GradPlace o;
+  template <int C>
+  __device__ __forceinline__ void put(int m, int n, const float (&v)[2][C], int, int N) const {
+    float dh[C];
+    get_values(dH, (int64_t)m * lddh + n, f32, dh, N - n);
+    put_grad(o, act, m, n, N, v[0], v[1], dh);
+  }
+};
+struct PlainOut {
+  void* out; int64_t ld; int f32;
+  template <int C>
+  __device__ __forceinline__ void put(int m, int n, const float (&v)[1][C], int, int N) const {
+    if (f32) put_f32(reinterpret_cast<float*>(out) + (int64_t)m * ld + n, v[0], N - n);
+    else put_bf16(reinterpret_cast<uint16_t*>(out) + (int64_t)m * ld + n, v[0], N - n);
+  }
+};
+// dg and du from kept g and u.  Bound by its 14 bytes per element (bf16).
+__global__ __launch_bounds__(256) void gated_grad_kernel(const void* __restrict__ dH, int64_t lddh, int f32, int act, const float* __restrict__ G,
+                                                         const float* __restrict__ U, int64_t rows, int f, GradPlace o) {
+  const int packs = (int)(o.ld / 8);
+  for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < rows * packs; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / packs;
+    const int n = (int)(i - r * packs) * 8;
+    float g[8], u[8], dh[8];
+    get_values(G, r * f + n, 1, g, f - n);
+    get_values(U, r * f + n, 1, u, f - n);
+    get_values(dH, r * lddh + n, f32, dh, f - n);
+    put_grad(o, act, r, n, f, g, u, dh);
+  }
+}
+
+// up to two products of the same sizes in one launch
+template <int NB, class Epi> struct Pair { Product<NB> p[2]; Epi e[2]; };
+template <int AM, int BMODE, class S, class Epi>
+__global__ __launch_bounds__(S::WAVES * 64, 1) void gated_product_kernel(const Pair<S::NB, Epi> q) {
+  product_tile<false, AM, BMODE, S>(q.p[blockIdx.y], q.e[blockIdx.y]);
+}
+
+// ---- shapes ----------------------------------------------------------------------------------
+typedef Shape<2, 4, 8, 2, 2> Big2;       // 256 x (128 + 128), eight waves
+typedef Shape<2, 2, 4, 2, 2> Small2;     // 128 x (64 + 64), four waves
+typedef Shape<2, 4, 8, 4, 1> Big1;       // 256 x 256
+typedef Shape<2, 2, 4, 4, 1> Small1;     // 128 x 128
+constexpr int FILL = 192;                // workgroups of the big shape from which on it is taken: three quarters of the compute units
+
+template <class S, int NB>
+int64_t tiles(const Product<NB>& p) { return ((int64_t)p.M + S::BM - 1) / S::BM * (((int64_t)p.N + S::BN - 1) / S::BN); }
+
+template <int AM, int BMODE, class SB, class SS, class Epi>
+void launch_product(const Pair<SB::NB, Epi>& q, int count, hipStream_t s) {
+  const int64_t big = tiles<SB>(q.p[0]);
+  if (big * count >= FILL)
+    hipLaunchKernelGGL((gated_product_kernel<AM, BMODE, SB, Epi>), dim3((unsigned)big, count), dim3(SB::WAVES * 64), 0, s, q);
+  else
+    hipLaunchKernelGGL((gated_product_kernel<AM, BMODE, SS, Epi>), dim3((unsigned)tiles<SS>(q.p[0]), count), dim3(SS::WAVES * 64), 0, s, q);
+}
+
+// ---- operands --------------------------------------------------------------------------------
+inline int64_t up8(int64_t v) { return (v + 7) / 8 * 8; }
+inline unsigned pieces_grid(int64_t rows, int64_t ld) {
+  const int64_t n = (rows * (ld / 8) + 255) / 256;
+  return (unsigned)(n < 1 ? 1 : (n > 8192 ? 8192 : n));
+}
+// A matrix of a call as the products take it: in place, or as pieces in the workspace.
+struct Source {
+  const void* p; int64_t rows, cols, ld; bool copied; int pieces; char* at; int64_t ldp;
+  Operand operand() const {      // piece 0 in p[0], ...
+    Operand o{};
+    for (int t = 0; t < pieces; t++) o.p[t] = copied ? at + (size_t)t * rows * ldp * 2 : reinterpret_cast<const char*>(p);
+    o.ldb = (copied ? ldp : ld) * 2; o.rows = (int)rows; o.cols = (int)(copied ? ldp : cols);
+    return o;
+  }
+  void make(int f32, hipStream_t s) const {
+    if (copied && rows > 0)
+      hipLaunchKernelGGL(gated_pieces_kernel, dim3(pieces_grid(rows, ldp)), dim3(256), 0, s, p, f32, rows, (int)cols, ld, reinterpret_cast<uint16_t*>(at), ldp,
+                         rows * ldp, pieces);
+  }
+};
+// `loose`: some buffer of the call does not begin at a 16-byte boundary
+Source source(Carve& c, const void* p, int64_t rows, int64_t cols, int64_t ld, int32_t dtype, bool loose) {
+  Source s{p, rows, cols, ld, false, dtype == OSSCAR_F32 ? 3 : 1, nullptr, up8(cols)};
+  s.copied = dtype == OSSCAR_F32 || loose || !operand_fits(nullptr, ld, cols, 2);
+  if (s.copied) s.at = c.take((size_t)s.pieces * rows * s.ldp * 2);
+  return s;
+}
+// The segments of sum_t A_t B_t: pieces of weight 2^-16 and more, the smallest products first.
+constexpr int PAIRS3[6][2] = {{2, 0}, {1, 1}, {0, 2}, {1, 0}, {0, 1}, {0, 0}};
+template <int NB>
+void add_segments(Product<NB>& q, const Operand& a, const Operand (&b)[NB], int pieces) {
+  const int first = q.nseg;
+  q.a.ldb = a.ldb; q.a.rows = a.rows; q.a.cols = a.cols;
+  for (int z = 0; z < NB; z++) { q.b[z].ldb = b[z].ldb; q.b[z].rows = b[z].rows; q.b[z].cols = b[z].cols; }
+  for (int t = 0; t < (pieces == 1 ? 1 : 6); t++) {
+    const int x = pieces == 1 ? 0 : PAIRS3[t][0], y = pieces == 1 ? 0 : PAIRS3[t][1];
+    q.a.p[first + t] = a.p[x];
+    for (int z = 0; z < NB; z++) q.b[z].p[first + t] = b[z].p[y];
+    q.nseg++;
+  }
+}
+
+struct Buffers {
+  Source x, wg, wu;
+  uint16_t *dg, *du; int64_t ldg;
+};
+Buffers buffers(Carve& c, const osscar_gated_desc& q, const void* X, const void* Wg, const void* Wu, int backward) {
+  Buffers b{};
+  const int64_t wr = q.rows_out ? q.f : q.d, wc = q.rows_out ? q.d : q.f;
+  b.x = source(c, X, q.n, q.d, q.ldx, q.dtype, q.unaligned != 0);
+  b.wg = source(c, Wg, wr, wc, q.ldw, q.dtype, q.unaligned != 0);
+  b.wu = source(c, Wu, wr, wc, q.ldw, q.dtype, q.unaligned != 0);
+  if (backward) {
+    b.ldg = up8(q.f);
+    const size_t bytes = (size_t)(q.dtype == OSSCAR_F32 ? 3 : 1) * q.n * b.ldg * 2;
+    b.dg = reinterpret_cast<uint16_t*>(c.take(bytes));
+    b.du = reinterpret_cast<uint16_t*>(c.take(bytes));
+  }
+  return b;
+}
+const char* bad_desc(const osscar_gated_desc* q) {
+  if (!q) return "osscar_gated: NULL description";
+  if (!a_size(q->n, 0) || !a_size(q->d, 1) || !a_size(q->f, 1)) return "osscar_gated: n >= 0, d and f must be positive, none above 2^30";
+  if (!real_dtype(q->dtype)) return "osscar_gated: unknown dtype";
+  if (q->act < OSSCAR_ACT_SILU || q->act > OSSCAR_ACT_RELU) return "osscar_gated: unknown activation";
+  if (q->ldx < q->d || q->ldw < (q->rows_out ? q->d : q->f) || q->ldh < q->f) return "osscar_gated: leading dimension below the row length";
+  return nullptr;
+}
+bool loose(const void* p) { return ((uintptr_t)p & 15) != 0; }
+// what both calls check of their buffers; nullptr if there is nothing to refuse
+const char* bad_buffers(const osscar_gated_desc& q, const void* X, const void* Wg, const void* Wu, const void* H, const void* G, const void* U, const void* ws) {
+  if (!Wg || !Wu || (q.n > 0 && (!X || !H))) return "osscar_gated: NULL pointer";
+  if ((G == nullptr) != (U == nullptr) && q.n > 0) return "osscar_gated: G and U are given together or not at all";
+  const uintptr_t es = q.dtype == OSSCAR_F32 ? 4 : 2;
+  if ((uintptr_t)X % es || (uintptr_t)Wg % es || (uintptr_t)Wu % es || (uintptr_t)H % es || (uintptr_t)G % 4 || (uintptr_t)U % 4)
+    return "osscar_gated: a buffer is not aligned to its elements";
+  if (q.dtype == OSSCAR_BF16 && !q.unaligned && (loose(X) || loose(Wg) || loose(Wu)))
+    return "osscar_gated: X, Wg or Wu does not begin at a 16-byte boundary (set unaligned in the description)";
+  if ((uintptr_t)ws & 255) return "osscar_gated: the workspace must begin at a 256-byte boundary";
+  return nullptr;
+}
+template <int NB>
+bool countable(const Product<NB>& p) { return tiles<Small1>(p) <= 0x3FFFFFFF; }
+
+// X Wg, X Wu with epilogue e
+template <class Epi>
+osscar_status projections(const osscar_gated_desc& q, const Buffers& b, const Epi& e, hipStream_t s) {
+  Pair<2, Epi> two{};
+  Product<2>& p = two.p[0];
+  two.e[0] = e;
+  p.M = (int)q.n; p.N = (int)q.f; p.k = (int)q.d;
+  const Operand w[2] = {b.wg.operand(), b.wu.operand()};
+  add_segments(p, b.x.operand(), w, b.x.pieces);
+  if (!countable(p)) return refuse_call(OSSCAR_EINVAL, "osscar_gated: n times f is too large for one call");
+  if (q.rows_out) launch_product<OP_K, OP_K, Big2, Small2>(two, 1, s);
+  else launch_product<OP_K, OP_T, Big2, Small2>(two, 1, s);
+  return OSSCAR_OK;
+}
+
+}  // namespace
+
+extern "C" size_t osscar_gated_workspace_bytes(const osscar_gated_desc* desc, int32_t backward) {
+  if (bad_desc(desc)) return 0;
+  Carve c(nullptr);
+  buffers(c, *desc, nullptr, nullptr, nullptr, backward);
+  return c.used + 256;      // (never 0: that says that the description is invalid)
+}
+
+extern "C" osscar_status osscar_gated_forward(const osscar_gated_desc* desc, const void* X_dev, const void* Wg_dev, const void* Wu_dev, void* H_dev,
+                                              float* G_dev, float* U_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  const char* bad = bad_desc(desc);
+  if (!bad) bad = bad_buffers(*desc, X_dev, Wg_dev, Wu_dev, H_dev, G_dev, U_dev, workspace_dev);
+  if (bad) return refuse_call(OSSCAR_EINVAL, bad);
+  const osscar_gated_desc& q = *desc;
+  Carve c(workspace_dev);
+  const Buffers b = buffers(c, q, X_dev, Wg_dev, Wu_dev, 0);
+  if (c.used > workspace_bytes || (c.used > 0 && !workspace_dev)) return refuse_call(OSSCAR_ENOMEM, "osscar_gated_forward: workspace too small");
+  if (q.n == 0) return OSSCAR_OK;
+  hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
+  const int f32 = q.dtype == OSSCAR_F32;
+  b.x.make(f32, s); b.wg.make(f32, s); b.wu.make(f32, s);
+  const GatedOut e{H_dev, q.ldh, f32, q.act, G_dev, U_dev};
+  const osscar_status st = projections(q, b, e, s);
+  return st != OSSCAR_OK ? st : launched("osscar_gated_forward");
+}
+
+extern "C" osscar_status osscar_gated_backward(const osscar_gated_desc* desc, const void* X_dev, const void* Wg_dev, const void* Wu_dev, const void* dH_dev,
+                                               const float* G_dev, const float* U_dev, void* dX_dev, int64_t lddx, void* dWg_dev, void* dWu_dev, int64_t lddw,
+                                               int32_t dw_dtype, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  const char* bad = bad_desc(desc);
+  if (!bad) bad = bad_buffers(*desc, X_dev, Wg_dev, Wu_dev, dH_dev, G_dev, U_dev, workspace_dev);
+  if (!bad && (!real_dtype(dw_dtype) || (dWg_dev == nullptr) != (dWu_dev == nullptr))) bad = "osscar_gated_backward: unknown dtype, or one of dWg and dWu alone";
+  if (!bad && ((dX_dev && lddx < desc->d) || (dWg_dev && lddw < (desc->rows_out ? desc->d : desc->f))))
+    bad = "osscar_gated_backward: leading dimension below the row length";
+  if (!bad && ((uintptr_t)dX_dev % (desc->dtype == OSSCAR_F32 ? 4 : 2) || (uintptr_t)dWg_dev % (dw_dtype == OSSCAR_F32 ? 4 : 2) || (uintptr_t)dWu_dev % (dw_dtype == OSSCAR_F32 ? 4 : 2)))
+    bad = "osscar_gated_backward: a buffer is not aligned to its elements";
+  if (bad) return refuse_call(OSSCAR_EINVAL, bad);
+  const osscar_gated_desc& q = *desc;
+  Carve c(workspace_dev);
+  const Buffers b = buffers(c, q, X_dev, Wg_dev, Wu_dev, 1);
+  if (c.used > workspace_bytes || (c.used > 0 && !workspace_dev)) return refuse_call(OSSCAR_ENOMEM, "osscar_gated_backward: workspace too small");
+  hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
+  const int f32 = q.dtype == OSSCAR_F32, pieces = b.x.pieces;
+  const GradPlace place{b.dg, b.du, b.ldg, q.n * b.ldg, pieces};
+  if (q.n > 0) {
+    if (!G_dev || dWg_dev) b.x.make(f32, s);
+    if (!G_dev || dX_dev) { b.wg.make(f32, s); b.wu.make(f32, s); }
+    if (G_dev) {
+      hipLaunchKernelGGL(gated_grad_kernel, dim3(pieces_grid(q.n, b.ldg)), dim3(256), 0, s, dH_dev, q.ldh, f32, q.act, G_dev, U_dev, q.n, (int)q.f, place);
+    } else {
+      const GatedGrad e{dH_dev, q.ldh, f32, q.act, place};
+      const osscar_status st = projections(q, b, e, s);
+      if (st != OSSCAR_OK) return st;
+    }
+  }
+  // dg and du as operands: n rows of ldg bf16, zeros past f
+  Operand dg{}, du{};
+  for (int t = 0; t < pieces; t++) {
+    dg.p[t] = reinterpret_cast<const char*>(b.dg + t * place.step);
+    du.p[t] = reinterpret_cast<const char*>(b.du + t * place.step);
+  }
+  dg.ldb = du.ldb = b.ldg * 2; dg.rows = du.rows = (int)q.n; dg.cols = du.cols = (int)b.ldg;
+  if (dX_dev && q.n > 0) {
+    Pair<1, PlainOut> two{};
+    Product<1>& p = two.p[0];
+    p.M = (int)q.n; p.N = (int)q.d; p.k = (int)q.f;
+    const Operand wg[1] = {b.wg.operand()}, wu[1] = {b.wu.operand()};
+    add_segments(p, dg, wg, pieces);
+    add_segments(p, du, wu, pieces);
+    if (!countable(p)) return refuse_call(OSSCAR_EINVAL, "osscar_gated_backward: n times d is too large for one call");
+    two.e[0] = PlainOut{dX_dev, lddx, f32};
+    if (q.rows_out) launch_product<OP_K, OP_T, Big1, Small1>(two, 1, s);
+    else launch_product<OP_K, OP_K, Big1, Small1>(two, 1, s);
+  }
+  if (dWg_dev) {      // both weights in one launch
+    Pair<1, PlainOut> two{};
+    Product<1>* p = two.p;
+    const Operand x = b.x.operand(), *dd[2] = {&dg, &du};
+    for (int z = 0; z < 2; z++) {
+      const Operand bs[1] = {q.rows_out ? x : *dd[z]};
+      add_segments(p[z], q.rows_out ? *dd[z] : x, bs, pieces);
+      p[z].M = (int)(q.rows_out ? q.f : q.d); p[z].N = (int)(q.rows_out ? q.d : q.f); p[z].k = (int)q.n;
+    }
+    if (!countable(p[0])) return refuse_call(OSSCAR_EINVAL, "osscar_gated_backward: d times f is too large for one call");
+    two.e[0] = PlainOut{dWg_dev, lddw, dw_dtype == OSSCAR_F32};
+    two.e[1] = PlainOut{dWu_dev, lddw, dw_dtype == OSSCAR_F32};
+    launch_product<OP_T, OP_T, Big1, Small1>(two, 2, s);
+  }
+  return launched("osscar_gated_backward");
+}

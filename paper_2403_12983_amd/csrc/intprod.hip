@@ -1,0 +1,213 @@
+// Products in 8-bit integers with a scale per token and per output channel, and the quantisation of both sides.
+#include "ops.h"
+#include "tile.h"
+
+using namespace osscar;
+using namespace osscar::tile;
+
+namespace {
+
+// The scale of a maximum (given as the bits of a non-negative float, which order as the floats do, NaN above all), and a value in it.
+__device__ __forceinline__ float scale_of(uint32_t most) { return __uint_as_float(most) / 127.f; }
+__device__ __forceinline__ float usable(float s) { return s > 0.f && s < INFINITY ? s : 0.f; }      // else all digits are 0, and s itself makes the result NaN
+__device__ __forceinline__ int digit(float x, float s) { return s > 0.f ? (int)fminf(fmaxf(rintf(x / s), -127.f), 127.f) : 0; }
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+typedef int8_t s8x8 __attribute__((ext_vector_type(8)));
+
+// One row per workgroup, read twice (the second time from cache); eight values per thread and step.  Bound by reading X and writing Xq.
+__global__ __launch_bounds__(256) void int_rows_kernel(const void* __restrict__ X, int f32, int d1, int64_t ldx, int8_t* __restrict__ Xq, int64_t ldq,
+                                                       float* __restrict__ scale) {
+  __shared__ uint32_t sh[4];
+  const int64_t row = blockIdx.x;
+  uint32_t most = 0;
+  for (int k = threadIdx.x * 8; k < d1; k += 2048) {
+    float v[8];
+    get_values(X, row * ldx + k, f32, v, d1 - k);
+#pragma unroll
+    for (int e = 0; e < 8; e++) most = max(most, magnitude(v[e]));
+  }
+  for (int o = 32; o > 0; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = most;
+  __syncthreads();
+  most = max(max(sh[0], sh[1]), max(sh[2], sh[3]));
+  const float s = scale_of(most), u = usable(s);
+  if (threadIdx.x == 0) scale[row] = s;
+  for (int k = threadIdx.x * 8; k < ldq; k += 2048) {
+    float v[8];
+    get_values(X, row * ldx + k, f32, v, d1 - k);
+    s8x8 w;
+#pragma unroll
+    for (int e = 0; e < 8; e++) w[e] = (int8_t)(k + e < d1 ? digit(v[e], u) : 0);
+    *reinterpret_cast<s8x8*>(Xq + row * ldq + k) = w;
+  }
+}
+// copies digits to rows of ldq, zeros past d1
+__global__ __launch_bounds__(256) void int_copy_kernel(const int8_t* __restrict__ X, int64_t n, int d1, int64_t ldx, int8_t* __restrict__ Xq, int64_t ldq) {
+  for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < n * ldq; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / ldq;
+    const int k = (int)(i - r * ldq);
+    Xq[i] = k < d1 ? X[r * ldx + k] : (int8_t)0;
+  }
+}
+// Columns of W (d1 x m): the maxima, 64 rows per workgroup and 256 columns, joined by an atomic maximum (the order does not matter)
+__global__ void int_zero_kernel(uint32_t* p, int n) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < n) p[i] = 0u;
+}
+__global__ __launch_bounds__(256) void int_column_max_kernel(const void* __restrict__ W, int f32, int d1, int m, int64_t ldw, uint32_t* __restrict__ most) {
+  const int j = blockIdx.x * 256 + threadIdx.x, k0 = blockIdx.y * 64, k1 = min(d1, k0 + 64);
+  if (j >= m) return;
+  uint32_t v = 0;
+  for (int k = k0; k < k1; k++) {
+    const int64_t at = (int64_t)k * ldw + j;
+    v = max(v, magnitude(f32 ? reinterpret_cast<const float*>(W)[at] : bf16_value(reinterpret_cast<const uint16_t*>(W)[at])));
+  }
+  atomicMax(most + j, v);
+}
+__global__ void int_scales_kernel(uint32_t* p, int n) {      // maxima become scales
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < n) p[i] = __float_as_uint(scale_of(p[i]));
+}
+// 64 x 64 blocks turned over in LDS
+__global__ __launch_bounds__(256) void int_columns_kernel(const void* __restrict__ W, int f32, int d1, int m, int64_t ldw, const float* __restrict__ scale,
+                                                          int8_t* __restrict__ Wq, int64_t ldq) {
+  __shared__ int8_t T[64][68];
+  const int k0 = blockIdx.x * 64, j0 = blockIdx.y * 64, c = threadIdx.x & 63, r = threadIdx.x >> 6;
+  const float u = j0 + c < m ? usable(scale[j0 + c]) : 0.f;
+  for (int k = r; k < 64; k += 4) {
+    float x = 0.f;
+    if (k0 + k < d1 && j0 + c < m) {
+      const int64_t at = (int64_t)(k0 + k) * ldw + j0 + c;
+      x = f32 ? reinterpret_cast<const float*>(W)[at] : bf16_value(reinterpret_cast<const uint16_t*>(W)[at]);
+    }
+    T[c][k] = (int8_t)digit(x, u);
+  }
+  __syncthreads();
+  for (int j = r; j < 64; j += 4)
+    if (j0 + j < m && k0 + c < ldq) Wq[(int64_t)(j0 + j) * ldq + k0 + c] = T[j][c];
+}
+
+struct IntOut {
+  const float *xs, *ws, *bias; void* Y; int64_t ldy; int f32;
+  template <int C>
+  __device__ __forceinline__ void put(int m, int n, const int (&v)[1][C], int, int N) const {
+    const float s = xs[m];
+    float y[C];
+#pragma unroll
+    for (int c = 0; c < C; c++) {
+      const int j = min(n + c, N - 1);
+      y[c] = (float)v[0][c] * s * ws[j];
+      if (bias) y[c] += bias[j];
+    }
+    if (f32) put_f32(reinterpret_cast<float*>(Y) + (int64_t)m * ldy + n, y, N - n);
+    else put_bf16(reinterpret_cast<uint16_t*>(Y) + (int64_t)m * ldy + n, y, N - n);
+  }
+};
+typedef Shape<2, 4, 8, 4, 1> Big;        // 256 x 256, eight waves
+typedef Shape<2, 2, 4, 4, 1> Small;      // 128 x 128, four waves
+constexpr int FILL = 192;
+
+template <class S>
+__global__ __launch_bounds__(S::WAVES * 64, 1) void int_product_kernel(const Product<1> p, const IntOut e) {
+  product_tile<true, OP_K, OP_K, S>(p, e);
+}
+
+inline int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
+template <class S>
+int64_t tiles(int64_t n, int64_t m) { return (n + S::BM - 1) / S::BM * ((m + S::BN - 1) / S::BN); }
+bool bad_sizes(int64_t n, int64_t d1, int64_t m) { return !a_size(n, 0) || !a_size(m, 1) || d1 < 1 || d1 > OSSCAR_INT_MAX_DIM || tiles<Small>(n, m) > 0x3FFFFFFF; }
+bool bad_digits(const void* q, int64_t ldq, int64_t d1) { return !q || (uintptr_t)q % 16 || ldq % 16 || ldq < d1 || ldq > MAX_LD_BYTES; }
+
+void quantise_rows(const void* X, int64_t n, int64_t d1, int64_t ldx, int f32, int8_t* Xq, int64_t ldq, float* scale, hipStream_t s) {
+  hipLaunchKernelGGL(int_rows_kernel, dim3((unsigned)n), dim3(256), 0, s, X, f32, (int)d1, ldx, Xq, ldq, scale);
+}
+
+}  // namespace
+
+extern "C" osscar_status osscar_int_rows(const void* X_dev, int64_t n, int64_t d1, int64_t ldx, int32_t x_dtype, int8_t* Xq_dev, int64_t ldq, float* x_scale_dev,
+                                         void* hip_stream) {
+  if (bad_sizes(n, d1, 1)) return refuse_call(OSSCAR_EINVAL, "osscar_int_rows: n >= 0 and 1 <= d1 <= OSSCAR_INT_MAX_DIM");
+  if (!real_dtype(x_dtype)) return refuse_call(OSSCAR_EINVAL, "osscar_int_rows: unknown dtype");
+  if (n == 0) return OSSCAR_OK;
+  if (!X_dev || ldx < d1 || !x_scale_dev || (uintptr_t)X_dev % (x_dtype == OSSCAR_F32 ? 4 : 2)) return refuse_call(OSSCAR_EINVAL, "osscar_int_rows: NULL or misaligned pointer, or leading dimension below the row length");
+  if (bad_digits(Xq_dev, ldq, d1)) return refuse_call(OSSCAR_EINVAL, "osscar_int_rows: Xq begins at a 16-byte boundary and ldq is a multiple of 16");
+  quantise_rows(X_dev, n, d1, ldx, x_dtype == OSSCAR_F32, Xq_dev, ldq, x_scale_dev, reinterpret_cast<hipStream_t>(hip_stream));
+  return launched("osscar_int_rows");
+}
+
+extern "C" osscar_status osscar_int_weights(const void* W_dev, int64_t d1, int64_t m, int64_t ldw, int32_t w_dtype, int32_t rows_out, int8_t* Wq_dev, int64_t ldq,
+                                            float* w_scale_dev, void* hip_stream) {
+  if (bad_sizes(0, d1, m)) return refuse_call(OSSCAR_EINVAL, "osscar_int_weights: m must be positive and 1 <= d1 <= OSSCAR_INT_MAX_DIM");
+  if (!real_dtype(w_dtype)) return refuse_call(OSSCAR_EINVAL, "osscar_int_weights: unknown dtype");
+  if (!W_dev || !w_scale_dev || ldw < (rows_out ? d1 : m) || (uintptr_t)W_dev % (w_dtype == OSSCAR_F32 ? 4 : 2))
+    return refuse_call(OSSCAR_EINVAL, "osscar_int_weights: NULL or misaligned pointer, or leading dimension below the row length");
+  if (bad_digits(Wq_dev, ldq, d1)) return refuse_call(OSSCAR_EINVAL, "osscar_int_weights: Wq begins at a 16-byte boundary and ldq is a multiple of 16");
+  hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
+  const int f32 = w_dtype == OSSCAR_F32;
+  if (rows_out) {
+    quantise_rows(W_dev, m, d1, ldw, f32, Wq_dev, ldq, w_scale_dev, s);
+  } else {
+    uint32_t* most = reinterpret_cast<uint32_t*>(w_scale_dev);
+    const unsigned mb = (unsigned)((m + 255) / 256);
+    hipLaunchKernelGGL(int_zero_kernel, dim3(mb), dim3(256), 0, s, most, (int)m);
+    hipLaunchKernelGGL(int_column_max_kernel, dim3(mb, (unsigned)((d1 + 63) / 64)), dim3(256), 0, s, W_dev, f32, (int)d1, (int)m, ldw, most);
+    hipLaunchKernelGGL(int_scales_kernel, dim3(mb), dim3(256), 0, s, most, (int)m);
+    for (int64_t j0 = 0; j0 < m; j0 += (int64_t)64 * 65535) {      // (the grid's second dimension ends at 65535)
+      const int64_t part = m - j0 < (int64_t)64 * 65535 ? m - j0 : (int64_t)64 * 65535;
+      hipLaunchKernelGGL(int_columns_kernel, dim3((unsigned)((ldq + 63) / 64), (unsigned)((part + 63) / 64)), dim3(256), 0, s,
+                         reinterpret_cast<const char*>(W_dev) + j0 * (f32 ? 4 : 2), f32, (int)d1, (int)part, ldw, w_scale_dev + j0, Wq_dev + j0 * ldq, ldq);
+    }
+  }
+  return launched("osscar_int_weights");
+}
+
+extern "C" size_t osscar_int_workspace_bytes(int64_t n, int64_t d1, int64_t m) {
+  if (bad_sizes(n, d1, m)) return 0;
+  Carve c(nullptr);
+  c.take((size_t)n * up16(d1));
+  c.take((size_t)n * 4);
+  return c.used + 256;
+}
+
+extern "C" osscar_status osscar_int_product(const void* X_dev, int64_t n, int64_t d1, int64_t ldx, int32_t x_dtype, const float* x_scale_dev, const int8_t* Wq_dev,
+                                            int64_t ldq, const float* w_scale_dev, int64_t m, const float* bias_dev, void* Y_dev, int64_t ldy, int32_t y_dtype,
+                                            void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  if (bad_sizes(n, d1, m)) return refuse_call(OSSCAR_EINVAL, "osscar_int_product: n >= 0, m must be positive and 1 <= d1 <= OSSCAR_INT_MAX_DIM");
+  if ((!real_dtype(x_dtype) && x_dtype != OSSCAR_I8) || !real_dtype(y_dtype)) return refuse_call(OSSCAR_EINVAL, "osscar_int_product: unknown dtype");
+  if (n == 0) return OSSCAR_OK;
+  const bool given = x_dtype == OSSCAR_I8;
+  if (!X_dev || !w_scale_dev || !Y_dev || ldx < d1 || ldy < m || given != (x_scale_dev != nullptr))
+    return refuse_call(OSSCAR_EINVAL, "osscar_int_product: NULL pointer, leading dimension below the row length, or x_scale not exactly with 8-bit X");
+  if (!given && (uintptr_t)X_dev % (x_dtype == OSSCAR_F32 ? 4 : 2)) return refuse_call(OSSCAR_EINVAL, "osscar_int_product: X is not aligned to its elements");
+  if ((uintptr_t)Y_dev % (y_dtype == OSSCAR_F32 ? 4 : 2)) return refuse_call(OSSCAR_EINVAL, "osscar_int_product: Y is not aligned to its elements");
+  if (bad_digits(Wq_dev, ldq, d1)) return refuse_call(OSSCAR_EINVAL, "osscar_int_product: Wq begins at a 16-byte boundary and ldq is a multiple of 16");
+  if ((uintptr_t)workspace_dev & 255) return refuse_call(OSSCAR_EINVAL, "osscar_int_product: the workspace must begin at a 256-byte boundary");
+  hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
+  const int8_t* xq = reinterpret_cast<const int8_t*>(X_dev);
+  const float* xs = x_scale_dev;
+  int64_t ldxq = ldx;
+  if (!given || !operand_fits(X_dev, ldx, d1, 1)) {
+    Carve c(workspace_dev);
+    ldxq = up16(d1);
+    int8_t* q = reinterpret_cast<int8_t*>(c.take((size_t)n * ldxq));
+    float* sc = reinterpret_cast<float*>(c.take((size_t)n * 4));
+    if (!workspace_dev || c.used > workspace_bytes) return refuse_call(OSSCAR_ENOMEM, "osscar_int_product: workspace too small");
+    if (given) {
+      const int64_t g = (n * ldxq + 255) / 256;
+      hipLaunchKernelGGL(int_copy_kernel, dim3((unsigned)(g > 8192 ? 8192 : g)), dim3(256), 0, s, xq, n, (int)d1, ldx, q, ldxq);
+    } else {
+      quantise_rows(X_dev, n, d1, ldx, x_dtype == OSSCAR_F32, q, ldxq, sc, s);
+      xs = sc;
+    }
+    xq = q;
+  }
+  Product<1> p{};
+  p.a.p[0] = reinterpret_cast<const char*>(xq); p.a.ldb = ldxq; p.a.rows = (int)n; p.a.cols = (int)up16(d1);
+  p.b[0].p[0] = reinterpret_cast<const char*>(Wq_dev); p.b[0].ldb = ldq; p.b[0].rows = (int)m; p.b[0].cols = (int)up16(d1);
+  p.nseg = 1; p.k = (int)d1; p.M = (int)n; p.N = (int)m;
+  const IntOut e{xs, w_scale_dev, bias_dev, Y_dev, ldy, y_dtype == OSSCAR_F32};
+  if (tiles<Big>(n, m) >= FILL) hipLaunchKernelGGL(int_product_kernel<Big>, dim3((unsigned)tiles<Big>(n, m)), dim3(Big::WAVES * 64), 0, s, p, e);
+  else hipLaunchKernelGGL(int_product_kernel<Small>, dim3((unsigned)tiles<Small>(n, m)), dim3(Small::WAVES * 64), 0, s, p, e);
+  return launched("osscar_int_product");
+}
