@@ -181,9 +181,9 @@ __global__ __launch_bounds__(S::WAVES * 64, 1) void gated_product_kernel(const P
 }
 
 // ---- shapes ----------------------------------------------------------------------------------
-typedef Shape<2, 4, 8, 2, 2> Big2;       // 256 x (128 + 128), eight waves
+typedef Shape<2, 2, 8, 4, 2> Big2;       // 256 x (128 + 128), four waves
 typedef Shape<2, 2, 4, 2, 2> Small2;     // 128 x (64 + 64), four waves
-typedef Shape<2, 4, 8, 4, 1> Big1;       // 256 x 256
+typedef Shape<2, 2, 8, 8, 1> Big1;       // 256 x 256
 typedef Shape<2, 2, 4, 4, 1> Small1;     // 128 x 128
 constexpr int FILL = 192;                // workgroups of the big shape from which on it is taken: three quarters of the compute units
 

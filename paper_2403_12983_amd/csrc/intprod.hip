@@ -104,7 +104,7 @@ struct IntOut {
     else put_bf16(reinterpret_cast<uint16_t*>(Y) + (int64_t)m * ldy + n, y, N - n);
   }
 };
-typedef Shape<2, 4, 8, 4, 1> Big;        // 256 x 256, eight waves
+typedef Shape<2, 2, 8, 8, 1> Big;        // 256 x 256, four waves
 typedef Shape<2, 2, 4, 4, 1> Small;      // 128 x 128, four waves
 constexpr int FILL = 192;
 

@@ -22,12 +22,11 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef short v8s __attribute__((ext_vector_type(8)));
-typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) void lds_void;
 
 enum { OP_K = 0, OP_T = 1 };
 constexpr int SEGS = 12;                        // two products of float32 operands
-constexpr int STEP_BYTES = 128;                 // contraction per stage and row: 64 bf16 or 128 int8
+constexpr int STEP_BYTES = 128;                 // contraction per stage and row: 64 bf16 or 128 int8, two matrix-core operands
 constexpr int64_t MAX_LD_BYTES = 1 << 22;       // 256 rows stay below the 2^30 bytes that an offset may take
 
 struct Operand {
@@ -40,19 +39,38 @@ inline bool operand_fits(const void* p, int64_t ld, int64_t cols, int es) {
   return ((uintptr_t)p & 15) == 0 && (ld * es) % 16 == 0 && (cols * es) % 16 == 0 && ld * es <= MAX_LD_BYTES;
 }
 
+// vmcnt <= N; lgkmcnt = 0, then the barrier: builtins, which the compiler takes into account where it places waits of its own
+template <int N>
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14)); }
+__device__ __forceinline__ void stage_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// D = A B + D with the sums in the accumulation registers.  Written out so that the sums stay where they are: the compiler's own form gives D
+// other registers than it reads, which four tiles' worth of copies per product pay for where 256 registers of sums are all there are.
+// Of the two shapes of the instruction the 16 x 16 one moves less between registers per operation: on random operands, where the chip's power
+// sets its clock, 2.1 PFLOP/s alone against 1.8.
 template <bool I8> struct Num;
 template <> struct Num<false> {
   typedef v4f acc; typedef float val;
   static constexpr int ES = 2;
-  static __device__ __forceinline__ acc mma(v4i a, v4i b, acc c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
-  }
+  static __device__ __forceinline__ void mma(v4i a, v4i b, acc& c) { asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
 };
 template <> struct Num<true> {
   typedef v4i acc; typedef int val;
   static constexpr int ES = 1;
-  static __device__ __forceinline__ acc mma(v4i a, v4i b, acc c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ void mma(v4i a, v4i b, acc& c) { asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
 };
+// The matrix core has written the sums when this has passed (16 cycles cover its longest result).
+__device__ __forceinline__ void sums_written() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
 
 // The shape of a workgroup: WM x WN waves, each of FM x (NB FN) tiles of 16 x 16.  NB: matrices on the B side whose columns a wave takes
 // alike (gate and up projection), FN tiles of each.
@@ -62,67 +80,75 @@ struct Shape {
 };
 
 // One side's way into LDS and out of it.  EXT: rows of the result that the workgroup takes of it; PER: tiles of 16 per wave.  A-side tiles
-// lie one behind the other.  On the B side (PERM) lane group g holds PER x 4 neighbouring columns: tile j, matrix-core row i is column
-// (i / 4) 4 PER + 4 j + i % 4 of the wave's, so that a lane's results are 4 PER neighbours in memory.
-// Packets are permuted inside an LDS row so that the lanes of one access meet all banks once.
+// lie one behind the other.  Lane group g (16 lanes) of the matrix core's result holds rows 4 g + b of a tile, b < 4; on the B side (PERM) that row of
+// tile t is column 32 (t / 2) + 8 g + 4 (t % 2) + b of the wave's: a lane holds eight neighbours of a pair of tiles, and the four groups together 32, 64
+// bytes of bf16, which a write to memory takes as one (with 32 or 64 neighbours in one lane, four times the writes: 7 % of a product of
+// contraction 2048).
+// Packets are permuted inside an LDS row so that the lanes of one access meet the banks evenly.
 template <int MODE, int ES, int EXT, int PER, bool PERM, int WAVES>
 struct Side {
   static constexpr int ROW = MODE == OP_K ? STEP_BYTES : EXT * ES;      // bytes of an LDS row
   static constexpr int PK = ROW / 16;                                   // its packets
   static constexpr int BYTES = EXT * STEP_BYTES;
   static constexpr int NJ = BYTES / 1024 / WAVES;                       // loads of a wave per stage
+  static constexpr int READS = MODE == OP_K ? 1 : 2;                    // reads of LDS per operand
   static_assert(BYTES % (1024 * WAVES) == 0, "every wave issues the same number of loads");
   static constexpr int RPI = 64 / PK;                                   // LDS rows per load
   static __device__ __forceinline__ int swizzle(int row) {
-    if (MODE == OP_K) return PERM ? (row & 3) | (((row / (4 * PER)) & 1) << 2) : row & 7;
-    if (!PERM) return (((row & 3) | (((row >> 3) & 1) << 2)) << 1) & (PK - 1);
-    if (PK == 8) return ((row >> 1) & 1) << 2;
-    return PER >= 4 ? (row & 1) | ((row & 2) << 2) : (row & 3) << 2;
+    if (MODE == OP_K) return PERM ? ((row >> 1) & 1) | (((row >> 3) & 3) << 1) : (row >> 1) & 7;
+    if (PERM) return PK == 8 ? (row & 2) << 1 : (row & 3) << 2;
+    return (((row & 3) | (((row >> 3) & 1) << 2)) << 1) & (PK - 1);
   }
-  int voff[NJ], vcol[NJ];      // byte offset of the lane's packet from the stage's corner; first element of it along the row
-  int seg_row0;                // result rows before the workgroup's
+  // Load j of a wave begins at LDS row (wave + WAVES j) RPI: its lanes' packets are permuted like those of load j % NV
+  static constexpr int NV = MODE == OP_T && !PERM && NJ > 1 ? 2 : 1;
+  static_assert(WAVES == 4, "");
+  int voff[NV], vcol[MODE == OP_K ? NV : 1];      // byte offset of the lane's packet from the load's corner; first element of it along the row
+  int seg_row0;                                   // result rows before the workgroup's
   __device__ __forceinline__ void open(const Operand& o, int row0, int wave, int lane) {
     seg_row0 = row0;
 #pragma unroll
-    for (int j = 0; j < NJ; j++) {
+    for (int j = 0; j < NV; j++) {
       const int r = (wave + WAVES * j) * RPI + lane / PK, c = (lane % PK) ^ swizzle(r);
-      vcol[j] = c * (16 / ES);
       voff[j] = (lane / PK) * (int)o.ldb + c * 16;
-      if (MODE == OP_T && row0 + vcol[j] >= o.cols) voff[j] = 0x7FFFFFF0;
+      if (MODE == OP_K) vcol[j] = c * (16 / ES);
+      else if (row0 + c * (16 / ES) >= o.cols) voff[j] = 0x7FFFFFF0;
     }
   }
-  // requests the stage that begins at k of segment seg
-  __device__ __forceinline__ void load(const Operand& o, int seg, int k, char* lds, int wave) const {
+  // the requests of the stage that begins at k of segment seg; zeros if there is none
+  struct Stage { __amdgpu_buffer_rsrc_t rs; int v[NV]; };
+  __device__ __forceinline__ void stage(const Operand& o, int seg, int k, bool there, Stage& st) const {
     const int r0 = MODE == OP_K ? seg_row0 : k, c0 = MODE == OP_K ? k : seg_row0;
     const int64_t at = (int64_t)r0 * o.ldb + (int64_t)c0 * ES;
     int64_t left = (int64_t)(o.rows - r0 - 1) * o.ldb + (int64_t)(o.cols - c0) * ES;      // bytes from here to the end of the operand
-    left = left < 0 || r0 >= o.rows || c0 >= o.cols ? 0 : (left > 0x7FFFFFF0 ? 0x7FFFFFF0 : left);
-    __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)(o.p[seg] + at), 0, (int)left, 0x00020000);
-    const bool tail = MODE == OP_K && k + STEP_BYTES / ES > o.cols;
+    left = !there || left < 0 || r0 >= o.rows || c0 >= o.cols ? 0 : (left > 0x7FFFFFF0 ? 0x7FFFFFF0 : left);
+    st.rs = __builtin_amdgcn_make_buffer_rsrc((void*)(o.p[seg] + at), 0, (int)left, 0x00020000);
 #pragma unroll
-    for (int j = 0; j < NJ; j++) {
-      const int i = wave + WAVES * j;
-      const int v = tail && k + vcol[j] >= o.cols ? 0x7FFFFFF0 : voff[j];
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(lds + i * 1024), 16, v, i * RPI * (int)o.ldb, 0, 0);
-    }
+    for (int j = 0; j < NV; j++) st.v[j] = MODE == OP_K && k + vcol[MODE == OP_K ? j : 0] >= o.cols ? 0x7FFFFFF0 : voff[j];
   }
-  // the wave's PER operands of half stage `sub`, wpos: its place among the waves along this side
-  int raddr[MODE == OP_K ? 1 : PER];
+  __device__ __forceinline__ void load(const Operand& o, const Stage& st, int j, char* lds, int wave) const {
+    const int i = wave + WAVES * j;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(st.rs, (lds_void*)(lds + i * 1024), 16, st.v[j % NV], i * RPI * (int)o.ldb, 0, 0);
+  }
+  // the wave's operands of a stage: tile t < PER, half `sub` of the contraction; wpos: the wave's place among those along this side
+  int raddr[MODE == OP_K ? 2 : PER];
   __device__ __forceinline__ void open_read(int wpos, int lane) {
-    const int i = lane & 15, g = lane >> 4;
+    const int i = lane & 15, g = lane >> 4, first = wpos * PER * 16;
     if (MODE == OP_K) {
-      const int row = wpos * PER * 16 + (PERM ? (i >> 2) * 4 * PER + (i & 3) : i);
-      raddr[0] = row * ROW + ((g ^ swizzle(row)) * 16);
+      const int row = first + (PERM ? (i >> 2) * 8 + (i & 3) : i);
+#pragma unroll
+      for (int sub = 0; sub < 2; sub++) raddr[sub] = row * ROW + (((sub * 4 + g) ^ swizzle(row)) * 16);
     } else {
+      // sixteen lanes read four rows k of four quads of neighbouring elements each and get a column of them
+      const int k = g * 8 + (i >> 2), q = i & 3;      // the quad that this lane fetches
 #pragma unroll
       for (int t = 0; t < PER; t++) {
-        const int col = wpos * PER * 16 + (PERM ? (i & 3) * 4 * PER + t * 4 : t * 16 + (i & 3) * 4), k = g * 8 + (i >> 2);
+        const int col = first + (PERM ? (t >> 1) * 32 + q * 8 + (t & 1) * 4 : t * 16 + q * 4);
         raddr[t] = k * ROW + (((col >> 3) ^ swizzle(k)) * 16) + ((col >> 2) & 1) * 8;
       }
     }
   }
   __device__ __forceinline__ v4i read(const char* lds, int t, int sub) const {
-    if (MODE == OP_K) return *reinterpret_cast<const v4i*>(lds + (raddr[0] ^ (sub * 64)) + t * (PERM ? 4 : 16) * ROW);
+    if (MODE == OP_K) return *reinterpret_cast<const v4i*>(lds + raddr[MODE == OP_K ? sub : 0] + (PERM ? (t >> 1) * 32 + (t & 1) * 4 : t * 16) * ROW);
     typedef __attribute__((address_space(3))) v4s lds_v4s;
     const char* q = lds + raddr[MODE == OP_K ? 0 : t] + sub * 32 * ROW;
     const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)q), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(q + 4 * ROW));
@@ -148,14 +174,15 @@ __device__ __forceinline__ void tile_of(int b, int tiles_m, int tiles_n, int& tm
   tn = in / rows;
 }
 
-// Epi: __device__ void put(int m, int n, const val (&v)[NB][4 * FN], int M, int N), 4 FN neighbouring columns of row m from n on; m < M, but columns may pass N.
+// Epi: __device__ void put(int m, int n, const val (&v)[NB][8], int M, int N), eight neighbouring columns of row m from n on; m < M and n < N, but columns may
+// pass N.
 template <bool I8, int AM, int BMODE, class S, class Epi>
 __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi& epi) {
   typedef Num<I8> T;
   constexpr int ES = T::ES, KS = STEP_BYTES / ES;
   typedef Side<AM, ES, S::BM, S::FM, false, S::WAVES> SA;
   typedef Side<BMODE, ES, S::BN, S::FN, true, S::WAVES> SB;
-  // Two stages, each in arrays of its own: with one array the compiler waits before every read of LDS for all requests under way.
+  // An array per stage: with one array the compiler waits before every read of LDS for all requests under way.
   __shared__ __align__(1024) char a0[SA::BYTES], a1[SA::BYTES], b0[S::NB][SB::BYTES], b1[S::NB][SB::BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN;
   int tm, tn;
@@ -175,55 +202,87 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
       for (int j = 0; j < S::FN; j++)
 #pragma unroll
         for (int r = 0; r < 4; r++) acc[i][z][j][r] = 0;
-  int seg = 0, k = 0;      // of the next stage to be requested
-  const int per = (q.k + KS - 1) / KS, total = per * q.nseg;
-  auto request = [&](char* a, char (*b)[SB::BYTES]) {
-    sa.load(q.a, seg, k, a, wave);
+  const int per = (q.k + KS - 1) / KS, total = per * q.nseg;      // stages of a segment, of all
+  // Workgroups begin at stages of their own, so that rows whose distance is a power of two do not all ask one memory channel at a time (contraction 2048: 7 %;
+  // int8, 14336: 5 %).
+  const int k0 = (per > 0 ? (tm + tn) % per : 0) * KS;
+  int seg = 0, k = k0;      // of the next stage to be requested
+  constexpr int NL = SA::NJ + S::NB * SB::NJ;      // loads of a wave per stage
+  typename SA::Stage qa;
+  typename SB::Stage qb[S::NB];
+  auto next_stage = [&]() {
+    const bool there = seg < q.nseg;
+    const int at = there ? seg : 0;
+    sa.stage(q.a, at, k, there, qa);
 #pragma unroll
-    for (int z = 0; z < S::NB; z++) sb.load(q.b[z], seg, k, b[z], wave);
+    for (int z = 0; z < S::NB; z++) sb.stage(q.b[z], at, k, there, qb[z]);
     k += KS;
-    if (k >= q.k) { k = 0; seg++; }
+    if (k >= q.k) k = 0;
+    if (k == k0) seg++;
   };
-  auto multiply = [&](const char* a, const char (*b)[SB::BYTES]) {
+  auto request = [&](int l, char* a, char (*b)[SB::BYTES]) {      // load l < NL of a stage
+    if (l < SA::NJ) sa.load(q.a, qa, l, a, wave);
+    else sb.load(q.b[(l - SA::NJ) / SB::NJ], qb[(l - SA::NJ) / SB::NJ], (l - SA::NJ) % SB::NJ, b[(l - SA::NJ) / SB::NJ], wave);
+  };
+  constexpr int NF = S::NB * S::FN + S::FM, NM = S::FM * S::NB * S::FN;      // operands and products of half a stage
+  v4i fa[2][S::FM], fb[2][S::NB][S::FN];
+  auto read = [&](int set, int l, const char* a, const char (*b)[SB::BYTES]) {      // operand l < NF of half `set` of a stage, into register set `set`
+    if (l < S::NB * S::FN) fb[set][l / S::FN][l % S::FN] = sb.read(b[l / S::FN], l % S::FN, set);
+    else fa[set][l - S::NB * S::FN] = sa.read(a, l - S::NB * S::FN, set);
+  };
+  // Half `set` is multiplied; meanwhile half 1 - set of (ra, rb) is read and, for set = 1, the stage prepared in qa, qb requested into (la, lb), evenly spread.
+  auto half = [&](int set, const char* ra, const char (*rb)[SB::BYTES], char* la, char (*lb)[SB::BYTES]) {
 #pragma unroll
-    for (int sub = 0; sub < 2; sub++) {
-      v4i fa[S::FM], fb[S::NB][S::FN];
+    for (int n = 0; n < NM; n++) {
 #pragma unroll
-      for (int z = 0; z < S::NB; z++)
+      for (int l = n * NF / NM; l < (n + 1) * NF / NM; l++) read(1 - set, l, ra, rb);
+      if (set == 1) {
 #pragma unroll
-        for (int j = 0; j < S::FN; j++) fb[z][j] = sb.read(b[z], j, sub);
-#pragma unroll
-      for (int i = 0; i < S::FM; i++) fa[i] = sa.read(a, i, sub);
-#pragma unroll
-      for (int i = 0; i < S::FM; i++)
-#pragma unroll
-        for (int z = 0; z < S::NB; z++)
-#pragma unroll
-          for (int j = 0; j < S::FN; j++) acc[i][z][j] = T::mma(fb[z][j], fa[i], acc[i][z][j]);      // rows of the result tile: columns n
+        for (int l = n * NL / NM; l < (n + 1) * NL / NM; l++) request(l, la, lb);
+      }
+      T::mma(fb[set][(n / S::FN) % S::NB][n % S::FN], fa[set][n / (S::NB * S::FN)], acc[n / (S::NB * S::FN)][(n / S::FN) % S::NB][n % S::FN]);      // rows of the result tile: columns n
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
-  request(a0, b0);
-  for (int st = 0; st < total; st += 2) {
-    __syncthreads();      // the stage has landed (every wave waits for its requests) and the other one's readers are done
-    if (st + 1 < total) request(a1, b1);
-    multiply(a0, b0);
-    if (st + 1 >= total) break;
-    __syncthreads();
-    if (st + 2 < total) request(a0, b0);
-    multiply(a1, b1);
+  // The first half of a stage is in registers when its turn comes.  While it is multiplied the second half is read; then every wave has read all
+  // of the stage, which the barrier establishes together with the arrival of the next one, its buffer takes the stage after that, and
+  // the next stage's first half is read while the second half is multiplied.
+#define OSSCAR_TILE_STAGE(a_, b_, an_, bn_) \
+  half(0, a_, b_, nullptr, nullptr);        \
+  next_stage();                             \
+  wait_loads<0>();                          \
+  stage_barrier();                          \
+  half(1, an_, bn_, a_, b_);
+  next_stage();
+#pragma unroll
+  for (int l = 0; l < NL; l++) request(l, a0, b0);
+  next_stage();
+#pragma unroll
+  for (int l = 0; l < NL; l++) request(l, a1, b1);
+  wait_loads<NL>();
+  stage_barrier();
+#pragma unroll
+  for (int l = 0; l < NF; l++) read(0, l, a0, b0);
+  for (int st = 0; st < total; st += 2) {      // (stages past the last one are zeros)
+    OSSCAR_TILE_STAGE(a0, b0, a1, b1)
+    OSSCAR_TILE_STAGE(a1, b1, a0, b0)
   }
+#undef OSSCAR_TILE_STAGE
+  sums_written();
   const int i = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int f = 0; f < S::FM; f++) {
-    const int m = tm * S::BM + (wm * S::FM + f) * 16 + i, n = tn * S::BN + wn * S::FN * 16 + g * 4 * S::FN;
-    typename T::val v[S::NB][4 * S::FN];
+    const int m = tm * S::BM + (wm * S::FM + f) * 16 + i;
 #pragma unroll
-    for (int z = 0; z < S::NB; z++)
+    for (int t = 0; t < S::FN; t += 2) {
+      const int n = tn * S::BN + wn * S::FN * 16 + t * 16 + g * 8;
+      typename T::val v[S::NB][8];
 #pragma unroll
-      for (int j = 0; j < S::FN; j++)
+      for (int z = 0; z < S::NB; z++)
 #pragma unroll
-        for (int r = 0; r < 4; r++) v[z][4 * j + r] = acc[f][z][j][r];
-    if (m < q.M && n < q.N) epi.put(m, n, v, q.M, q.N);
+        for (int e = 0; e < 8; e++) v[z][e] = acc[f][z][t + e / 4][e % 4];
+      if (m < q.M && n < q.N) epi.put(m, n, v, q.M, q.N);
+    }
   }
 }
 
