@@ -90,18 +90,20 @@ __global__ __launch_bounds__(256) void int_columns_kernel(const void* __restrict
 
 struct IntOut {
   const float *xs, *ws, *bias; void* Y; int64_t ldy; int f32;
-  template <int C>
-  __device__ __forceinline__ void put(int m, int n, const int (&v)[1][C], int, int N) const {
-    const float s = xs[m];
-    float y[C];
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+    f([&](int m, int n, const int (&v)[1][8], int N) {
+      const float s = xs[m];
+      float y[8];
 #pragma unroll
-    for (int c = 0; c < C; c++) {
-      const int j = min(n + c, N - 1);
-      y[c] = (float)v[0][c] * s * ws[j];
-      if (bias) y[c] += bias[j];
-    }
-    if (f32) put_f32(reinterpret_cast<float*>(Y) + (int64_t)m * ldy + n, y, N - n);
-    else put_bf16(reinterpret_cast<uint16_t*>(Y) + (int64_t)m * ldy + n, y, N - n);
+      for (int c = 0; c < 8; c++) {
+        const int j = min(n + c, N - 1);
+        y[c] = (float)v[0][c] * s * ws[j];
+        if (bias) y[c] += bias[j];
+      }
+      if (f32) put_f32(reinterpret_cast<float*>(Y) + (int64_t)m * ldy + n, y, N - n);
+      else put_bf16(reinterpret_cast<uint16_t*>(Y) + (int64_t)m * ldy + n, y, N - n);
+    });
   }
 };
 typedef Shape<2, 2, 8, 8, 1> Big;        // 256 x 256, four waves

@@ -114,16 +114,27 @@ struct Side {
       else if (row0 + c * (16 / ES) >= o.cols) voff[j] = 0x7FFFFFF0;
     }
   }
-  // the requests of the stage that begins at k of segment seg; zeros if there is none
-  struct Stage { __amdgpu_buffer_rsrc_t rs; int v[NV]; };
-  __device__ __forceinline__ void stage(const Operand& o, int seg, int k, bool there, Stage& st) const {
-    const int r0 = MODE == OP_K ? seg_row0 : k, c0 = MODE == OP_K ? k : seg_row0;
-    const int64_t at = (int64_t)r0 * o.ldb + (int64_t)c0 * ES;
-    int64_t left = (int64_t)(o.rows - r0 - 1) * o.ldb + (int64_t)(o.cols - c0) * ES;      // bytes from here to the end of the operand
-    left = !there || left < 0 || r0 >= o.rows || c0 >= o.cols ? 0 : (left > 0x7FFFFFF0 ? 0x7FFFFFF0 : left);
-    st.rs = __builtin_amdgcn_make_buffer_rsrc((void*)(o.p[seg] + at), 0, (int)left, 0x00020000);
+  // Where the requests of a stage begin, kept from stage to stage so that a new one costs few scalar instructions: a wave has no time to spare
+  // for them between two matrix instructions.  OP_K: the corner of the segment, the stage's k is in the offsets; OP_T: the stage's row.
+  struct Stage { const char* cur; int num; __amdgpu_buffer_rsrc_t rs; int v[NV]; };
+  __device__ __forceinline__ void place(const Operand& o, const char* p, int k, bool there, Stage& st) const {
+    st.cur = p + (MODE == OP_K ? (int64_t)seg_row0 * o.ldb : (int64_t)k * o.ldb + (int64_t)seg_row0 * ES);
+    if (MODE == OP_K) {      // bytes from there to the end of the operand; zeros if there is no such segment
+      const int64_t left = (int64_t)(o.rows - seg_row0 - 1) * o.ldb + (int64_t)o.cols * ES;
+      st.num = !there || seg_row0 >= o.rows ? 0 : (left > 0x7FFFFFF0 ? 0x7FFFFFF0 : (int)left);
+    }
+  }
+  __device__ __forceinline__ void advance(const Operand& o, Stage& st) const {
+    if (MODE == OP_T) st.cur += o.ldb * (STEP_BYTES / ES);
+  }
+  __device__ __forceinline__ void prepare(const Operand& o, int k, bool there, Stage& st) const {
+    if (MODE == OP_T) {      // rows of the stage that exist; columns that do not have offsets past any end
+      const int n = o.rows - k;
+      st.num = !there || n <= 0 ? 0 : (n >= STEP_BYTES / ES ? 0x7FFFFFF0 : (n - 1) * (int)o.ldb + (o.cols - seg_row0) * ES);
+    }
+    st.rs = __builtin_amdgcn_make_buffer_rsrc((void*)st.cur, 0, st.num, 0x00020000);
 #pragma unroll
-    for (int j = 0; j < NV; j++) st.v[j] = MODE == OP_K && k + vcol[MODE == OP_K ? j : 0] >= o.cols ? 0x7FFFFFF0 : voff[j];
+    for (int j = 0; j < NV; j++) st.v[j] = MODE == OP_T ? voff[j] : (k + vcol[MODE == OP_K ? j : 0] >= o.cols ? 0x7FFFFFF0 : voff[j] + k * ES);
   }
   __device__ __forceinline__ void load(const Operand& o, const Stage& st, int j, char* lds, int wave) const {
     const int i = wave + WAVES * j;
@@ -174,8 +185,7 @@ __device__ __forceinline__ void tile_of(int b, int tiles_m, int tiles_n, int& tm
   tn = in / rows;
 }
 
-// Epi: __device__ void put(int m, int n, const val (&v)[NB][8], int M, int N), eight neighbouring columns of row m from n on; m < M and n < N, but columns may
-// pass N.
+// Epi::each(f) calls f(put) once, put(m, n, val (&v)[NB][8], N): eight neighbouring columns of row m from n on; n < N, but columns may pass N.
 template <bool I8, int AM, int BMODE, class S, class Epi>
 __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi& epi) {
   typedef Num<I8> T;
@@ -206,23 +216,35 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
   // Workgroups begin at stages of their own, so that rows whose distance is a power of two do not all ask one memory channel at a time (contraction 2048: 7 %;
   // int8, 14336: 5 %).
   const int k0 = (per > 0 ? (tm + tn) % per : 0) * KS;
-  int seg = 0, k = k0;      // of the next stage to be requested
+  int seg = 0, k = k0;      // of the stage that is prepared
+  bool there = true;
   constexpr int NL = SA::NJ + S::NB * SB::NJ;      // loads of a wave per stage
   typename SA::Stage qa;
   typename SB::Stage qb[S::NB];
-  auto next_stage = [&]() {
-    const bool there = seg < q.nseg;
+  auto place = [&]() {
+    there = seg < q.nseg;
     const int at = there ? seg : 0;
-    sa.stage(q.a, at, k, there, qa);
+    sa.place(q.a, q.a.p[at], k, there, qa);
 #pragma unroll
-    for (int z = 0; z < S::NB; z++) sb.stage(q.b[z], at, k, there, qb[z]);
+    for (int z = 0; z < S::NB; z++) sb.place(q.b[0], q.b[z].p[at], k, there, qb[z]);
+  };
+  auto step = [&]() {      // to the next stage
+    bool anew = false;
     k += KS;
-    if (k >= q.k) k = 0;
-    if (k == k0) seg++;
+    if (k >= q.k) { k = 0; anew = true; }
+    if (k == k0) { seg++; anew = true; }
+    if (anew) { place(); return; }
+    sa.advance(q.a, qa);
+#pragma unroll
+    for (int z = 0; z < S::NB; z++) sb.advance(q.b[0], qb[z]);
+  };
+  auto prepare = [&](int part) {      // 0: A, 1 + z: B
+    if (part == 0) sa.prepare(q.a, k, there, qa);
+    else sb.prepare(q.b[0], k, there, qb[part - 1]);
   };
   auto request = [&](int l, char* a, char (*b)[SB::BYTES]) {      // load l < NL of a stage
     if (l < SA::NJ) sa.load(q.a, qa, l, a, wave);
-    else sb.load(q.b[(l - SA::NJ) / SB::NJ], qb[(l - SA::NJ) / SB::NJ], (l - SA::NJ) % SB::NJ, b[(l - SA::NJ) / SB::NJ], wave);
+    else sb.load(q.b[0], qb[(l - SA::NJ) / SB::NJ], (l - SA::NJ) % SB::NJ, b[(l - SA::NJ) / SB::NJ], wave);
   };
   constexpr int NF = S::NB * S::FN + S::FM, NM = S::FM * S::NB * S::FN;      // operands and products of half a stage
   v4i fa[2][S::FM], fb[2][S::NB][S::FN];
@@ -230,7 +252,8 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
     if (l < S::NB * S::FN) fb[set][l / S::FN][l % S::FN] = sb.read(b[l / S::FN], l % S::FN, set);
     else fa[set][l - S::NB * S::FN] = sa.read(a, l - S::NB * S::FN, set);
   };
-  // Half `set` is multiplied; meanwhile half 1 - set of (ra, rb) is read and, for set = 1, the stage prepared in qa, qb requested into (la, lb), evenly spread.
+  // Half `set` is multiplied; meanwhile half 1 - set of (ra, rb) is read and, for set = 1, the stage prepared in qa, qb requested into (la, lb), evenly spread;
+  // for set = 0 that stage is prepared.
   auto half = [&](int set, const char* ra, const char (*rb)[SB::BYTES], char* la, char (*lb)[SB::BYTES]) {
 #pragma unroll
     for (int n = 0; n < NM; n++) {
@@ -239,6 +262,11 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
       if (set == 1) {
 #pragma unroll
         for (int l = n * NL / NM; l < (n + 1) * NL / NM; l++) request(l, la, lb);
+      } else {
+        if (n == NM / 8) step();
+#pragma unroll
+        for (int part = 0; part <= S::NB; part++)
+          if (n == (part + 2) * NM / 8) prepare(part);
       }
       T::mma(fb[set][(n / S::FN) % S::NB][n % S::FN], fa[set][n / (S::NB * S::FN)], acc[n / (S::NB * S::FN)][(n / S::FN) % S::NB][n % S::FN]);      // rows of the result tile: columns n
       __builtin_amdgcn_sched_barrier(0);
@@ -249,14 +277,17 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
   // the next stage's first half is read while the second half is multiplied.
 #define OSSCAR_TILE_STAGE(a_, b_, an_, bn_) \
   half(0, a_, b_, nullptr, nullptr);        \
-  next_stage();                             \
   wait_loads<0>();                          \
   stage_barrier();                          \
   half(1, an_, bn_, a_, b_);
-  next_stage();
+  place();
+#pragma unroll
+  for (int part = 0; part <= S::NB; part++) prepare(part);
 #pragma unroll
   for (int l = 0; l < NL; l++) request(l, a0, b0);
-  next_stage();
+  step();
+#pragma unroll
+  for (int part = 0; part <= S::NB; part++) prepare(part);
 #pragma unroll
   for (int l = 0; l < NL; l++) request(l, a1, b1);
   wait_loads<NL>();
@@ -270,20 +301,22 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
 #undef OSSCAR_TILE_STAGE
   sums_written();
   const int i = lane & 15, g = lane >> 4;
+  epi.each([&](auto put) {
 #pragma unroll
-  for (int f = 0; f < S::FM; f++) {
-    const int m = tm * S::BM + (wm * S::FM + f) * 16 + i;
+    for (int f = 0; f < S::FM; f++) {
+      const int m = tm * S::BM + (wm * S::FM + f) * 16 + i;
 #pragma unroll
-    for (int t = 0; t < S::FN; t += 2) {
-      const int n = tn * S::BN + wn * S::FN * 16 + t * 16 + g * 8;
-      typename T::val v[S::NB][8];
+      for (int t = 0; t < S::FN; t += 2) {
+        const int n = tn * S::BN + wn * S::FN * 16 + t * 16 + g * 8;
+        typename T::val v[S::NB][8];
 #pragma unroll
-      for (int z = 0; z < S::NB; z++)
+        for (int z = 0; z < S::NB; z++)
 #pragma unroll
-        for (int e = 0; e < 8; e++) v[z][e] = acc[f][z][t + e / 4][e % 4];
-      if (m < q.M && n < q.N) epi.put(m, n, v, q.M, q.N);
+          for (int e = 0; e < 8; e++) v[z][e] = acc[f][z][t + e / 4][e % 4];
+        if (m < q.M && n < q.N) put(m, n, v, q.N);
+      }
     }
-  }
+  });
 }
 
 }  // namespace tile

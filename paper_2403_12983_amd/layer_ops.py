@@ -146,7 +146,7 @@ def osscar_gated_backward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, d
         if need_w:
             shape = (f, d) if desc.rows_out else (d, f)
             dWg, dWu = torch.empty(shape, dtype=dw_dtype, device=device), torch.empty(shape, dtype=dw_dtype, device=device)
-        size = lib.osscar_gated_workspace_bytes(C.byref(desc), 1)
+        size = lib.osscar_gated_workspace_bytes(C.byref(desc), 1 if G is not None else 2)
         ws = _workspace(size, device)
         status = lib.osscar_gated_backward(C.byref(desc), xp, gp, up, dH.data_ptr(), G.data_ptr() if G is not None else None,
                                            U.data_ptr() if U is not None else None, dX.data_ptr() if need_x else None, d,
