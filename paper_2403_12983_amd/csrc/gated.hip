@@ -2,6 +2,7 @@
 //     dg = dh u a'(g), du = dh a(g);   dX = dg Wg^T + du Wu^T, dWg = X^T dg, dWu = X^T du.
 // h is the X that the Gram of the layer's down projection takes.
 #include "ops.h"
+#include "thin.h"
 #include "tile.h"
 
 using namespace osscar;
@@ -140,9 +141,28 @@ struct GatedOut {      // h, and g and u as they are where the caller keeps them
       });
     });
   }
+  template <class F>
+  __device__ __forceinline__ void one(F f) const {
+    with_act(H ? act : OSSCAR_ACT_RELU, [&](auto a) {
+      f([&](int m, int n, const float (&v)[2], int N) {
+        if (H) {
+          const float h = act_value<decltype(a)::value>(v[0]) * v[1];
+          if (f32) reinterpret_cast<float*>(H)[(int64_t)m * ldh + n] = h;
+          else reinterpret_cast<uint16_t*>(H)[(int64_t)m * ldh + n] = bf16_nearest(h);
+        }
+        if (G) { G[(int64_t)m * N + n] = v[0]; U[(int64_t)m * N + n] = v[1]; }
+      });
+    });
+  }
 };
 // dg and du, rounded to bf16 (they are operands of the next products, as h is of the next layer) or in three pieces
 struct GradPlace { uint16_t *dg, *du; int64_t ld, step; int pieces; };
+template <int LAYOUT, int KIND, int RT>
+__global__ __launch_bounds__((thin::Wave<LAYOUT, KIND, 2, RT>::WAVES) * 64, 1) void gated_thin_kernel(const thin::Product<2> p, const GatedOut e) {
+  thin::product<LAYOUT, KIND, 2, RT>(p, e);
+}
+__global__ __launch_bounds__(256) void gated_join_kernel(const thin::Product<2> p, const GatedOut e) { thin::join<2, float>(p, e); }
+
 struct PlainOut {
   void* out; int64_t ld; int f32;
   template <class F>
@@ -253,9 +273,17 @@ struct Buffers {
   Source x, wg, wu;
   uint16_t *dg, *du; int64_t ldg;
   float *g, *u;      // computed again
+  int parts; char* sums;      // few rows: of the contraction, and their sums
 };
+bool few(const osscar_gated_desc& q) { return q.n <= thin::ROWS; }
 Buffers buffers(Carve& c, const osscar_gated_desc& q, const void* X, const void* Wg, const void* Wu, int backward, bool kept) {
   Buffers b{};
+  if (few(q) && !kept) {
+    b.parts = q.rows_out ? (q.dtype == OSSCAR_F32 ? thin::parts_of<OP_K, thin::F32>(q.f, q.d) : thin::parts_of<OP_K, thin::BF16>(q.f, q.d))
+                         : (q.dtype == OSSCAR_F32 ? thin::parts_of<OP_T, thin::F32>(q.f, q.d) : thin::parts_of<OP_T, thin::BF16>(q.f, q.d));
+    if (b.parts > 1) b.sums = c.take((size_t)b.parts * 2 * q.n * q.f * 4);
+    if (!backward) return b;
+  }
   const int64_t wr = q.rows_out ? q.f : q.d, wc = q.rows_out ? q.d : q.f;
   b.x = source(c, X, q.n, q.d, q.ldx, q.dtype, q.unaligned != 0);
   b.wg = source(c, Wg, wr, wc, q.ldw, q.dtype, q.unaligned != 0);
@@ -297,7 +325,23 @@ template <int NB>
 bool countable(const Product<NB>& p) { return tiles<Small1>(p) <= 0x3FFFFFFF; }
 
 // X Wg, X Wu with epilogue e
-osscar_status projections(const osscar_gated_desc& q, const Buffers& b, const GatedOut& e, hipStream_t s) {
+template <int LAYOUT, int KIND>
+void thin_projections(const thin::Product<2>& p, const GatedOut& e, hipStream_t s) {
+  const dim3 grid(thin::blocks_of<LAYOUT, KIND>(p.N), (unsigned)p.parts), block(thin::Wave<LAYOUT, KIND, 2, 1>::WAVES * 64);
+  if (p.M <= 16) hipLaunchKernelGGL((gated_thin_kernel<LAYOUT, KIND, 1>), grid, block, 0, s, p, e);
+  else hipLaunchKernelGGL((gated_thin_kernel<LAYOUT, KIND, 2>), grid, block, 0, s, p, e);
+  const int64_t n = ((int64_t)p.M * p.N + 255) / 256;
+  if (p.parts > 1) hipLaunchKernelGGL(gated_join_kernel, dim3((unsigned)(n > 4096 ? 4096 : n)), dim3(256), 0, s, p, e);
+}
+osscar_status projections(const osscar_gated_desc& q, const Buffers& b, const void* X, const void* Wg, const void* Wu, const GatedOut& e, hipStream_t s) {
+  if (few(q)) {
+    const int es = q.dtype == OSSCAR_F32 ? 4 : 2;
+    const thin::Product<2> p{reinterpret_cast<const char*>(X), {reinterpret_cast<const char*>(Wg), reinterpret_cast<const char*>(Wu)}, q.ldx * es, q.ldw * es,
+                             (int)q.n, (int)q.f, (int)q.d, b.parts, b.sums};
+    if (q.rows_out) q.dtype == OSSCAR_F32 ? thin_projections<OP_K, thin::F32>(p, e, s) : thin_projections<OP_K, thin::BF16>(p, e, s);
+    else q.dtype == OSSCAR_F32 ? thin_projections<OP_T, thin::F32>(p, e, s) : thin_projections<OP_T, thin::BF16>(p, e, s);
+    return OSSCAR_OK;
+  }
   Pair<2, GatedOut> two{};
   Product<2>& p = two.p[0];
   two.e[0] = e;
@@ -326,14 +370,14 @@ extern "C" osscar_status osscar_gated_forward(const osscar_gated_desc* desc, con
   if (bad) return refuse_call(OSSCAR_EINVAL, bad);
   const osscar_gated_desc& q = *desc;
   Carve c(workspace_dev);
-  const Buffers b = buffers(c, q, X_dev, Wg_dev, Wu_dev, 0, true);
+  const Buffers b = buffers(c, q, X_dev, Wg_dev, Wu_dev, 0, false);
   if (c.used > workspace_bytes || (c.used > 0 && !workspace_dev)) return refuse_call(OSSCAR_ENOMEM, "osscar_gated_forward: workspace too small");
   if (q.n == 0) return OSSCAR_OK;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   const int f32 = q.dtype == OSSCAR_F32;
-  b.x.make(f32, s); b.wg.make(f32, s); b.wu.make(f32, s);
+  if (!few(q)) { b.x.make(f32, s); b.wg.make(f32, s); b.wu.make(f32, s); }
   const GatedOut e{H_dev, q.ldh, f32, q.act, G_dev, U_dev};
-  const osscar_status st = projections(q, b, e, s);
+  const osscar_status st = projections(q, b, X_dev, Wg_dev, Wu_dev, e, s);
   return st != OSSCAR_OK ? st : launched("osscar_gated_forward");
 }
 
@@ -360,7 +404,7 @@ extern "C" osscar_status osscar_gated_backward(const osscar_gated_desc* desc, co
     if (!G_dev || dX_dev) { b.wg.make(f32, s); b.wu.make(f32, s); }
     const float *G = G_dev, *U = U_dev;
     if (!G) {
-      const osscar_status st = projections(q, b, GatedOut{nullptr, 0, f32, q.act, b.g, b.u}, s);
+      const osscar_status st = projections(q, b, X_dev, Wg_dev, Wu_dev, GatedOut{nullptr, 0, f32, q.act, b.g, b.u}, s);
       if (st != OSSCAR_OK) return st;
       G = b.g; U = b.u;
     }

@@ -1,5 +1,6 @@
 // Products in 8-bit integers with a scale per token and per output channel, and the quantisation of both sides.
 #include "ops.h"
+#include "thin.h"
 #include "tile.h"
 
 using namespace osscar;
@@ -105,6 +106,15 @@ struct IntOut {
       else put_bf16(reinterpret_cast<uint16_t*>(Y) + (int64_t)m * ldy + n, y, N - n);
     });
   }
+  template <class F>
+  __device__ __forceinline__ void one(F f) const {
+    f([&](int m, int n, const int (&v)[1], int) {
+      float y = (float)v[0] * xs[m] * ws[n];
+      if (bias) y += bias[n];
+      if (f32) reinterpret_cast<float*>(Y)[(int64_t)m * ldy + n] = y;
+      else reinterpret_cast<uint16_t*>(Y)[(int64_t)m * ldy + n] = bf16_nearest(y);
+    });
+  }
 };
 typedef Shape<2, 2, 8, 8, 1> Big;        // 256 x 256, four waves
 typedef Shape<2, 2, 4, 4, 1> Small;      // 128 x 128, four waves
@@ -114,6 +124,12 @@ template <class S>
 __global__ __launch_bounds__(S::WAVES * 64, 1) void int_product_kernel(const Product<1> p, const IntOut e) {
   product_tile<true, OP_K, OP_K, S>(p, e);
 }
+
+template <int RT>
+__global__ __launch_bounds__((thin::Wave<OP_K, thin::I8, 1, RT>::WAVES) * 64, 1) void int_thin_kernel(const thin::Product<1> p, const IntOut e) {
+  thin::product<OP_K, thin::I8, 1, RT>(p, e);
+}
+__global__ __launch_bounds__(256) void int_join_kernel(const thin::Product<1> p, const IntOut e) { thin::join<1, int>(p, e); }
 
 inline int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
 template <class S>
@@ -169,6 +185,7 @@ extern "C" size_t osscar_int_workspace_bytes(int64_t n, int64_t d1, int64_t m) {
   Carve c(nullptr);
   c.take((size_t)n * up16(d1));
   c.take((size_t)n * 4);
+  if (n <= thin::ROWS) c.take((size_t)thin::parts_of<OP_K, thin::I8>(m, d1) * n * m * 4);
   return c.used + 256;
 }
 
@@ -189,8 +206,9 @@ extern "C" osscar_status osscar_int_product(const void* X_dev, int64_t n, int64_
   const int8_t* xq = reinterpret_cast<const int8_t*>(X_dev);
   const float* xs = x_scale_dev;
   int64_t ldxq = ldx;
-  if (!given || !operand_fits(X_dev, ldx, d1, 1)) {
-    Carve c(workspace_dev);
+  const bool few = n <= thin::ROWS;
+  Carve c(workspace_dev);
+  if (!given || (!few && !operand_fits(X_dev, ldx, d1, 1))) {
     ldxq = up16(d1);
     int8_t* q = reinterpret_cast<int8_t*>(c.take((size_t)n * ldxq));
     float* sc = reinterpret_cast<float*>(c.take((size_t)n * 4));
@@ -204,11 +222,24 @@ extern "C" osscar_status osscar_int_product(const void* X_dev, int64_t n, int64_
     }
     xq = q;
   }
+  const IntOut e{xs, w_scale_dev, bias_dev, Y_dev, ldy, y_dtype == OSSCAR_F32};
+  if (few) {
+    thin::Product<1> t{reinterpret_cast<const char*>(xq), {reinterpret_cast<const char*>(Wq_dev)}, ldxq, ldq, (int)n, (int)m, (int)d1, thin::parts_of<OP_K, thin::I8>(m, d1), nullptr};
+    if (t.parts > 1) {
+      t.sums = c.take((size_t)t.parts * n * m * 4);
+      if (!workspace_dev || c.used > workspace_bytes) return refuse_call(OSSCAR_ENOMEM, "osscar_int_product: workspace too small");
+    }
+    const dim3 grid(thin::blocks_of<OP_K, thin::I8>(m), (unsigned)t.parts), block(thin::Wave<OP_K, thin::I8, 1, 1>::WAVES * 64);
+    if (n <= 16) hipLaunchKernelGGL(int_thin_kernel<1>, grid, block, 0, s, t, e);
+    else hipLaunchKernelGGL(int_thin_kernel<2>, grid, block, 0, s, t, e);
+    const int64_t g = (n * m + 255) / 256;
+    if (t.parts > 1) hipLaunchKernelGGL(int_join_kernel, dim3((unsigned)(g > 4096 ? 4096 : g)), dim3(256), 0, s, t, e);
+    return launched("osscar_int_product");
+  }
   Product<1> p{};
   p.a.p[0] = reinterpret_cast<const char*>(xq); p.a.ldb = ldxq; p.a.rows = (int)n; p.a.cols = (int)up16(d1);
   p.b[0].p[0] = reinterpret_cast<const char*>(Wq_dev); p.b[0].ldb = ldq; p.b[0].rows = (int)m; p.b[0].cols = (int)up16(d1);
   p.nseg = 1; p.k = (int)d1; p.M = (int)n; p.N = (int)m;
-  const IntOut e{xs, w_scale_dev, bias_dev, Y_dev, ldy, y_dtype == OSSCAR_F32};
   if (tiles<Big>(n, m) >= FILL) hipLaunchKernelGGL(int_product_kernel<Big>, dim3((unsigned)tiles<Big>(n, m)), dim3(Big::WAVES * 64), 0, s, p, e);
   else hipLaunchKernelGGL(int_product_kernel<Small>, dim3((unsigned)tiles<Small>(n, m)), dim3(Small::WAVES * 64), 0, s, p, e);
   return launched("osscar_int_product");

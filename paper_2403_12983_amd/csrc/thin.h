@@ -1,0 +1,299 @@
+// The products of tile.h for few rows (single tokens and small batches): C[m][n] = sum_k A[m][k] B[n][k] with at most 32 rows m.  Bound by reading B once,
+// so B goes from memory to registers and from there to the matrix core, past LDS: no barrier stands between a wave's loads, and any alignment will do.
+//
+// OP_K (a column's elements side by side): a workgroup takes 16 columns, its waves take the contraction in turns of four matrix-core operands.
+// OP_T (a row of B, one k, side by side): a wave takes 64 columns; lane l reads four neighbouring columns of the eight (float32: four) rows k that the
+// matrix core wants of its lane group and turns the block over in registers, half an instruction per element, so that tile j of the wave is columns
+// 4 i + j.  The waves of a workgroup take the contraction in turns; where the column blocks do not fill the chip, it is also cut into parts of a
+// workgroup each, whose sums a second launch adds in order.
+#pragma once
+#include "ops.h"
+#include "tile.h"
+
+namespace osscar {
+namespace thin {
+
+using tile::OP_K;
+using tile::OP_T;
+using tile::v4f;
+using tile::v4i;
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+
+constexpr int ROWS = 32;           // rows of A, at most
+enum { BF16 = 0, F32 = 1, I8 = 2 };
+
+// Packet: 16 bytes of one row or column.  ELEMS of them; a matrix-core step contracts STEP elements, OPS instructions.
+template <int KIND> struct Num;
+template <> struct Num<BF16> {
+  typedef v4f acc; typedef float val; typedef uint16_t el;
+  static constexpr int ELEMS = 8, STEP = 32;
+  static __device__ __forceinline__ void mma(v4i b, v4i a, acc& c) {
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, b), __builtin_bit_cast(v8bf, a), c, 0, 0, 0);
+  }
+};
+template <> struct Num<F32> {      // lane group g contracts k = 4 g + e in instruction e
+  typedef v4f acc; typedef float val; typedef uint32_t el;
+  static constexpr int ELEMS = 4, STEP = 16;
+  static __device__ __forceinline__ void mma(v4i b, v4i a, acc& c) {
+#pragma unroll
+    for (int e = 0; e < 4; e++) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__int_as_float(b[e]), __int_as_float(a[e]), c, 0, 0, 0);
+  }
+};
+template <> struct Num<I8> {
+  typedef v4i acc; typedef int val; typedef uint8_t el;
+  static constexpr int ELEMS = 16, STEP = 64;
+  static __device__ __forceinline__ void mma(v4i b, v4i a, acc& c) { c = __builtin_amdgcn_mfma_i32_16x16x64_i8(b, a, c, 0, 0, 0); }
+};
+
+typedef v4i v4i_any __attribute__((aligned(1)));
+// The packet at element k of a row of `K` elements; zeros past its end
+template <int KIND>
+__device__ __forceinline__ v4i packet(const char* row, int k, int K) {
+  typedef typename Num<KIND>::el el;
+  constexpr int E = Num<KIND>::ELEMS;
+  const el* p = reinterpret_cast<const el*>(row) + k;
+  if (k + E <= K) return *reinterpret_cast<const v4i_any*>(p);
+  el w[E];
+#pragma unroll
+  for (int e = 0; e < E; e++) {
+    w[e] = 0;
+    if (k + e < K) w[e] = p[e];
+  }
+  return __builtin_bit_cast(v4i, w);
+}
+
+template <int NB>
+struct Product {
+  const char *a, *b[NB];
+  int64_t lda, ldb;          // bytes
+  int M, N, K;
+  int parts;                 // of the contraction, a workgroup each (blockIdx.y)
+  void* sums;                // parts > 1: [part][matrix][m][n], 4 bytes each
+};
+
+template <int LAYOUT, int KIND, int NB, int RT> struct Wave;
+// OP_K
+template <int KIND, int NB, int RT>
+struct Wave<OP_K, KIND, NB, RT> {
+  typedef Num<KIND> T;
+  static constexpr int COLS = 16, TILES = 1, WAVES = 8, TURN = 4 * T::STEP;
+  static __device__ __forceinline__ int column(int, int i) { return i; }
+  const char *rb[NB], *ra[RT];
+  int koff;
+  __device__ __forceinline__ void open(const Product<NB>& q, int n0, int lane) {
+    const int i = lane & 15;
+    koff = (lane >> 4) * T::ELEMS;
+#pragma unroll
+    for (int z = 0; z < NB; z++) rb[z] = q.b[z] + (int64_t)min(n0 + i, q.N - 1) * q.ldb;      // (past the end: the last one again, not used)
+#pragma unroll
+    for (int r = 0; r < RT; r++) ra[r] = q.a + (int64_t)min(r * 16 + i, q.M - 1) * q.lda;
+  }
+  struct Regs { v4i b[NB][4], a[RT][4]; };
+  __device__ __forceinline__ void load(const Product<NB>& q, int k0, Regs& w) const {
+    if (k0 + TURN <= q.K) {
+#pragma unroll
+      for (int u = 0; u < 4; u++) {
+        const int64_t at = (int64_t)(k0 + u * T::STEP + koff) * sizeof(typename T::el);
+#pragma unroll
+        for (int z = 0; z < NB; z++) w.b[z][u] = *reinterpret_cast<const v4i_any*>(rb[z] + at);
+#pragma unroll
+        for (int r = 0; r < RT; r++) w.a[r][u] = *reinterpret_cast<const v4i_any*>(ra[r] + at);
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; u++) {
+        const int k = k0 + u * T::STEP + koff;
+#pragma unroll
+        for (int z = 0; z < NB; z++) w.b[z][u] = packet<KIND>(rb[z], k, q.K);
+#pragma unroll
+        for (int r = 0; r < RT; r++) w.a[r][u] = packet<KIND>(ra[r], k, q.K);
+      }
+    }
+  }
+  __device__ __forceinline__ void multiply(const Regs& w, typename T::acc (&acc)[RT][NB][TILES]) const {
+#pragma unroll
+    for (int u = 0; u < 4; u++)
+#pragma unroll
+      for (int z = 0; z < NB; z++)
+#pragma unroll
+        for (int r = 0; r < RT; r++) T::mma(w.b[z][u], w.a[r][u], acc[r][z][0]);
+  }
+};
+// OP_T: four columns of E rows k per lane (64 columns a wave: a memory line of bf16; with eight per lane the sums of two row tiles do not fit the registers)
+template <int KIND, int NB, int RT>
+struct Wave<OP_T, KIND, NB, RT> {
+  typedef Num<KIND> T;
+  typedef typename T::el el;
+  static constexpr int E = T::ELEMS, WIDTH = 4, DWORDS = WIDTH * sizeof(el) / 4, COLS = 16 * WIDTH, TILES = WIDTH, WAVES = 4, TURN = T::STEP;
+  typedef int vec __attribute__((ext_vector_type(DWORDS)));
+  typedef vec vec_any __attribute__((aligned(1)));
+  static __device__ __forceinline__ int column(int t, int i) { return i * WIDTH + t; }
+  const char *cb[NB], *ra[RT];
+  int koff, left;      // columns of the lane's packet that exist
+  __device__ __forceinline__ void open(const Product<NB>& q, int n0, int lane) {
+    const int i = lane & 15, n = n0 + i * WIDTH;
+    koff = (lane >> 4) * E;
+    left = min(WIDTH, q.N - n);
+#pragma unroll
+    for (int z = 0; z < NB; z++) cb[z] = q.b[z] + (int64_t)min(n, q.N - 1) * sizeof(el);
+#pragma unroll
+    for (int r = 0; r < RT; r++) ra[r] = q.a + (int64_t)min(r * 16 + i, q.M - 1) * q.lda;
+  }
+  struct Regs { vec b[NB][E]; v4i a[RT]; };
+  __device__ __forceinline__ void load(const Product<NB>& q, int k0, Regs& w) const {
+    const int k = k0 + koff;
+    if (k0 + TURN <= q.K) {
+#pragma unroll
+      for (int r = 0; r < RT; r++) w.a[r] = *reinterpret_cast<const v4i_any*>(ra[r] + (int64_t)k * sizeof(el));
+    } else {
+#pragma unroll
+      for (int r = 0; r < RT; r++) w.a[r] = packet<KIND>(ra[r], k, q.K);
+    }
+    if (k0 + TURN <= q.K && left == WIDTH) {
+#pragma unroll
+      for (int z = 0; z < NB; z++)
+#pragma unroll
+        for (int e = 0; e < E; e++) w.b[z][e] = *reinterpret_cast<const vec_any*>(cb[z] + (int64_t)(k + e) * q.ldb);
+    } else {
+#pragma unroll
+      for (int z = 0; z < NB; z++)
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+          const el* p = reinterpret_cast<const el*>(cb[z] + (int64_t)min(k + e, q.K - 1) * q.ldb);
+          el x[WIDTH];
+#pragma unroll
+          for (int c = 0; c < WIDTH; c++) {
+            x[c] = 0;
+            if (c < left && k + e < q.K) x[c] = p[c];
+          }
+          w.b[z][e] = __builtin_bit_cast(vec, x);
+        }
+    }
+  }
+  __device__ __forceinline__ void multiply(const Regs& w, typename T::acc (&acc)[RT][NB][TILES]) const {
+#pragma unroll
+    for (int z = 0; z < NB; z++)
+#pragma unroll
+      for (int t = 0; t < TILES; t++) {
+        v4i b;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          if (KIND == F32) b[e] = w.b[z][e][t % DWORDS];
+          else b[e] = (int)__builtin_amdgcn_perm((unsigned)w.b[z][(2 * e + 1) % E][(t / 2) % DWORDS], (unsigned)w.b[z][(2 * e) % E][(t / 2) % DWORDS], t & 1 ? 0x07060302u : 0x05040100u);
+        }
+#pragma unroll
+        for (int r = 0; r < RT; r++) T::mma(b, w.a[r], acc[r][z][t]);
+      }
+  }
+};
+
+// Epi::one(f) calls f(put) once, put(m, n, val (&v)[NB])
+template <int LAYOUT, int KIND, int NB, int RT, class Epi>
+__device__ __forceinline__ void product(const Product<NB>& q, const Epi& epi) {
+  typedef Wave<LAYOUT, KIND, NB, RT> W;
+  typedef typename W::T T;
+  typedef typename T::val val;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n0 = blockIdx.x * W::COLS;
+  W w;
+  w.open(q, n0, lane);
+  typename T::acc acc[RT][NB][W::TILES];
+#pragma unroll
+  for (int r = 0; r < RT; r++)
+#pragma unroll
+    for (int z = 0; z < NB; z++)
+#pragma unroll
+      for (int t = 0; t < W::TILES; t++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) acc[r][z][t][e] = 0;
+  // turns of this part, one wave after the other; the next turn's loads are on their way while one is multiplied
+  const int turns = (q.K + W::TURN - 1) / W::TURN, per = (turns + q.parts - 1) / q.parts;
+  const int first = blockIdx.y * per + wave, last = min(turns, (int)(blockIdx.y + 1) * per);
+  if (first < last) {
+    typename W::Regs x[2];
+    w.load(q, first * W::TURN, x[0]);
+    for (int t = first; t < last; t += 2 * W::WAVES) {
+      if (t + W::WAVES < last) w.load(q, (t + W::WAVES) * W::TURN, x[1]);
+      w.multiply(x[0], acc);
+      if (t + W::WAVES >= last) break;
+      if (t + 2 * W::WAVES < last) w.load(q, (t + 2 * W::WAVES) * W::TURN, x[0]);
+      w.multiply(x[1], acc);
+    }
+  }
+  // the waves' sums, added in order: [wave][row tile][matrix][column][16 rows + 1]
+  constexpr int PER = W::TILES * 16 * 17, ALL = RT * NB * PER;
+  __shared__ val sums[W::WAVES / 2][ALL];
+  const int g = lane >> 4, i = lane & 15;
+  auto each = [&](auto f) {      // f(place, value): the new value
+    if (i >= q.M && RT == 1) return;
+#pragma unroll
+    for (int r = 0; r < RT; r++)
+#pragma unroll
+      for (int z = 0; z < NB; z++)
+#pragma unroll
+        for (int t = 0; t < W::TILES; t++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) acc[r][z][t][e] = f((r * NB + z) * PER + W::column(t, g * 4 + e) * 17 + i, acc[r][z][t][e]);
+  };
+#pragma unroll
+  for (int half = W::WAVES / 2; half > 0; half /= 2) {
+    if (wave >= half && wave < 2 * half) each([&](int at, val v) { return sums[wave - half][at] = v; });
+    __syncthreads();
+    if (wave < half) each([&](int at, val v) { return v + sums[wave][at]; });
+    __syncthreads();
+  }
+  if (wave == 0) each([&](int at, val v) { return sums[0][at] = v; });
+  __syncthreads();
+  const int rows = q.M, cols = min(W::COLS, q.N - n0);
+  if (q.parts > 1) {
+    val* out = reinterpret_cast<val*>(q.sums) + (int64_t)blockIdx.y * NB * q.M * q.N;
+    for (int j = threadIdx.x; j < NB * rows * W::COLS; j += W::WAVES * 64) {
+      const int c = j % W::COLS, m = j / W::COLS % rows, z = j / W::COLS / rows;
+      if (c < cols) out[((int64_t)z * q.M + m) * q.N + n0 + c] = sums[0][((m >> 4) * NB + z) * PER + c * 17 + (m & 15)];
+    }
+    return;
+  }
+  epi.one([&](auto put) {
+    for (int j = threadIdx.x; j < rows * W::COLS; j += W::WAVES * 64) {
+      const int c = j % W::COLS, m = j / W::COLS;
+      if (c >= cols) continue;
+      val v[NB];
+#pragma unroll
+      for (int z = 0; z < NB; z++) v[z] = sums[0][((m >> 4) * NB + z) * PER + c * 17 + (m & 15)];
+      put(m, n0 + c, v, q.N);
+    }
+  });
+}
+// Adds the parts' sums in order and goes on with them.
+template <int NB, class V, class Epi>
+__device__ __forceinline__ void join(const Product<NB>& q, const Epi& epi) {
+  const V* s = reinterpret_cast<const V*>(q.sums);
+  epi.one([&](auto put) {
+    for (int64_t j = blockIdx.x * (int64_t)256 + threadIdx.x; j < (int64_t)q.M * q.N; j += (int64_t)gridDim.x * 256) {
+      V v[NB];
+#pragma unroll
+      for (int z = 0; z < NB; z++) {
+        V t = 0;
+        for (int p = 0; p < q.parts; p++) t += s[((int64_t)p * NB + z) * q.M * q.N + j];
+        v[z] = t;
+      }
+      put((int)(j / q.N), (int)(j % q.N), v, q.N);
+    }
+  });
+}
+// Workgroups of a product, and the parts of its contraction: enough for `want` workgroups, of at least four turns for each wave.
+template <int LAYOUT, int KIND>
+int parts_of(int64_t N, int64_t K) {
+  typedef Wave<LAYOUT, KIND, 1, 1> W;
+  const int64_t blocks = (N + W::COLS - 1) / W::COLS, turns = (K + W::TURN - 1) / W::TURN;
+  const int64_t want = LAYOUT == OP_K ? 128 : 512, most = turns / (W::WAVES * 2);
+  int64_t parts = want / blocks;
+  if (parts > most) parts = most;
+  if (parts > 16) parts = 16;
+  return parts < 1 ? 1 : (int)parts;
+}
+template <int LAYOUT, int KIND>
+unsigned blocks_of(int64_t N) { return (unsigned)((N + Wave<LAYOUT, KIND, 1, 1>::COLS - 1) / Wave<LAYOUT, KIND, 1, 1>::COLS); }
+
+}  // namespace thin
+}  // namespace osscar
