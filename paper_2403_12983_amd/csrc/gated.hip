@@ -157,9 +157,9 @@ struct GatedOut {      // h, and g and u as they are where the caller keeps them
 };
 // dg and du, rounded to bf16 (they are operands of the next products, as h is of the next layer) or in three pieces
 struct GradPlace { uint16_t *dg, *du; int64_t ld, step; int pieces; };
-template <int LAYOUT, int KIND, int RT>
-__global__ __launch_bounds__((thin::Wave<LAYOUT, KIND, 2, RT>::WAVES) * 64, 1) void gated_thin_kernel(const thin::Product<2> p, const GatedOut e) {
-  thin::product<LAYOUT, KIND, 2, RT>(p, e);
+template <int LAYOUT, int KIND, int RT, bool WIDE>
+__global__ __launch_bounds__((thin::Wave<LAYOUT, KIND, 2, RT, WIDE>::WAVES) * 64, 1) void gated_thin_kernel(const thin::Product<2> p, const GatedOut e) {
+  thin::product<LAYOUT, KIND, 2, RT, WIDE>(p, e);
 }
 __global__ __launch_bounds__(256) void gated_join_kernel(const thin::Product<2> p, const GatedOut e) { thin::join<2, float>(p, e); }
 
@@ -273,15 +273,15 @@ struct Buffers {
   Source x, wg, wu;
   uint16_t *dg, *du; int64_t ldg;
   float *g, *u;      // computed again
-  int parts; char* sums;      // few rows: of the contraction, and their sums
+  thin::Deal few; char* sums;      // few rows: how they are dealt out, and the sums of the parts
 };
 bool few(const osscar_gated_desc& q) { return q.n <= thin::ROWS; }
 Buffers buffers(Carve& c, const osscar_gated_desc& q, const void* X, const void* Wg, const void* Wu, int backward, bool kept) {
   Buffers b{};
   if (few(q) && !kept) {
-    b.parts = q.rows_out ? (q.dtype == OSSCAR_F32 ? thin::parts_of<OP_K, thin::F32>(q.f, q.d) : thin::parts_of<OP_K, thin::BF16>(q.f, q.d))
-                         : (q.dtype == OSSCAR_F32 ? thin::parts_of<OP_T, thin::F32>(q.f, q.d) : thin::parts_of<OP_T, thin::BF16>(q.f, q.d));
-    if (b.parts > 1) b.sums = c.take((size_t)b.parts * 2 * q.n * q.f * 4);
+    b.few = q.rows_out ? (q.dtype == OSSCAR_F32 ? thin::deal<OP_K, thin::F32>(q.n, q.f, q.d) : thin::deal<OP_K, thin::BF16>(q.n, q.f, q.d))
+                       : (q.dtype == OSSCAR_F32 ? thin::deal<OP_T, thin::F32>(q.n, q.f, q.d) : thin::deal<OP_T, thin::BF16>(q.n, q.f, q.d));
+    if (b.few.parts > 1) b.sums = c.take((size_t)b.few.parts * 2 * q.n * q.f * 4);
     if (!backward) return b;
   }
   const int64_t wr = q.rows_out ? q.f : q.d, wc = q.rows_out ? q.d : q.f;
@@ -325,21 +325,27 @@ template <int NB>
 bool countable(const Product<NB>& p) { return tiles<Small1>(p) <= 0x3FFFFFFF; }
 
 // X Wg, X Wu with epilogue e
-template <int LAYOUT, int KIND>
-void thin_projections(const thin::Product<2>& p, const GatedOut& e, hipStream_t s) {
-  const dim3 grid(thin::blocks_of<LAYOUT, KIND>(p.N), (unsigned)p.parts), block(thin::Wave<LAYOUT, KIND, 2, 1>::WAVES * 64);
-  if (p.M <= 16) hipLaunchKernelGGL((gated_thin_kernel<LAYOUT, KIND, 1>), grid, block, 0, s, p, e);
-  else hipLaunchKernelGGL((gated_thin_kernel<LAYOUT, KIND, 2>), grid, block, 0, s, p, e);
+template <int LAYOUT, int KIND, bool WIDE>
+void thin_launch(const thin::Product<2>& p, const thin::Deal& d, const GatedOut& e, hipStream_t s) {
+  const dim3 grid(d.blocks, (unsigned)d.parts), block(thin::Wave<LAYOUT, KIND, 2, 1, WIDE>::WAVES * 64);
+  if (p.M <= 16) hipLaunchKernelGGL((gated_thin_kernel<LAYOUT, KIND, 1, WIDE>), grid, block, 0, s, p, e);
+  else hipLaunchKernelGGL((gated_thin_kernel<LAYOUT, KIND, 2, WIDE>), grid, block, 0, s, p, e);
   const int64_t n = ((int64_t)p.M * p.N + 255) / 256;
-  if (p.parts > 1) hipLaunchKernelGGL(gated_join_kernel, dim3((unsigned)(n > 4096 ? 4096 : n)), dim3(256), 0, s, p, e);
+  if (d.parts > 1) hipLaunchKernelGGL(gated_join_kernel, dim3((unsigned)(n > 4096 ? 4096 : n)), dim3(256), 0, s, p, e);
+}
+template <int KIND>
+void thin_projections(const thin::Product<2>& p, bool rows_out, const thin::Deal& d, const GatedOut& e, hipStream_t s) {
+  if (!rows_out) thin_launch<OP_T, KIND, false>(p, d, e, s);
+  else if (d.wide) thin_launch<OP_K, KIND, true>(p, d, e, s);
+  else thin_launch<OP_K, KIND, false>(p, d, e, s);
 }
 osscar_status projections(const osscar_gated_desc& q, const Buffers& b, const void* X, const void* Wg, const void* Wu, const GatedOut& e, hipStream_t s) {
   if (few(q)) {
     const int es = q.dtype == OSSCAR_F32 ? 4 : 2;
     const thin::Product<2> p{reinterpret_cast<const char*>(X), {reinterpret_cast<const char*>(Wg), reinterpret_cast<const char*>(Wu)}, q.ldx * es, q.ldw * es,
-                             (int)q.n, (int)q.f, (int)q.d, b.parts, b.sums};
-    if (q.rows_out) q.dtype == OSSCAR_F32 ? thin_projections<OP_K, thin::F32>(p, e, s) : thin_projections<OP_K, thin::BF16>(p, e, s);
-    else q.dtype == OSSCAR_F32 ? thin_projections<OP_T, thin::F32>(p, e, s) : thin_projections<OP_T, thin::BF16>(p, e, s);
+                             (int)q.n, (int)q.f, (int)q.d, b.few.parts, b.sums};
+    if (q.dtype == OSSCAR_F32) thin_projections<thin::F32>(p, q.rows_out != 0, b.few, e, s);
+    else thin_projections<thin::BF16>(p, q.rows_out != 0, b.few, e, s);
     return OSSCAR_OK;
   }
   Pair<2, GatedOut> two{};

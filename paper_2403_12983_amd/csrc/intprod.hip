@@ -16,13 +16,15 @@ __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(
 
 typedef int8_t s8x8 __attribute__((ext_vector_type(8)));
 
-// One row per workgroup, read twice (the second time from cache); eight values per thread and step.  Bound by reading X and writing Xq.
-__global__ __launch_bounds__(256) void int_rows_kernel(const void* __restrict__ X, int f32, int d1, int64_t ldx, int8_t* __restrict__ Xq, int64_t ldq,
+// One row per workgroup of T threads, read twice (the second time from cache); eight values per thread and step.  Bound by reading X and writing Xq;
+// few rows: by the latency of the steps, so that they get 1024 threads each.
+template <int T>
+__global__ __launch_bounds__(T) void int_rows_kernel(const void* __restrict__ X, int f32, int d1, int64_t ldx, int8_t* __restrict__ Xq, int64_t ldq,
                                                        float* __restrict__ scale) {
-  __shared__ uint32_t sh[4];
+  __shared__ uint32_t sh[T / 64];
   const int64_t row = blockIdx.x;
   uint32_t most = 0;
-  for (int k = threadIdx.x * 8; k < d1; k += 2048) {
+  for (int k = threadIdx.x * 8; k < d1; k += T * 8) {
     float v[8];
     get_values(X, row * ldx + k, f32, v, d1 - k);
 #pragma unroll
@@ -31,10 +33,11 @@ __global__ __launch_bounds__(256) void int_rows_kernel(const void* __restrict__ 
   for (int o = 32; o > 0; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = most;
   __syncthreads();
-  most = max(max(sh[0], sh[1]), max(sh[2], sh[3]));
+#pragma unroll
+  for (int w = 0; w < T / 64; w++) most = max(most, sh[w]);
   const float s = scale_of(most), u = usable(s);
   if (threadIdx.x == 0) scale[row] = s;
-  for (int k = threadIdx.x * 8; k < ldq; k += 2048) {
+  for (int k = threadIdx.x * 8; k < ldq; k += T * 8) {
     float v[8];
     get_values(X, row * ldx + k, f32, v, d1 - k);
     s8x8 w;
@@ -125,9 +128,9 @@ __global__ __launch_bounds__(S::WAVES * 64, 1) void int_product_kernel(const Pro
   product_tile<true, OP_K, OP_K, S>(p, e);
 }
 
-template <int RT>
-__global__ __launch_bounds__((thin::Wave<OP_K, thin::I8, 1, RT>::WAVES) * 64, 1) void int_thin_kernel(const thin::Product<1> p, const IntOut e) {
-  thin::product<OP_K, thin::I8, 1, RT>(p, e);
+template <int RT, bool WIDE>
+__global__ __launch_bounds__((thin::Wave<OP_K, thin::I8, 1, RT, WIDE>::WAVES) * 64, 1) void int_thin_kernel(const thin::Product<1> p, const IntOut e) {
+  thin::product<OP_K, thin::I8, 1, RT, WIDE>(p, e);
 }
 __global__ __launch_bounds__(256) void int_join_kernel(const thin::Product<1> p, const IntOut e) { thin::join<1, int>(p, e); }
 
@@ -138,7 +141,8 @@ bool bad_sizes(int64_t n, int64_t d1, int64_t m) { return !a_size(n, 0) || !a_si
 bool bad_digits(const void* q, int64_t ldq, int64_t d1) { return !q || (uintptr_t)q % 16 || ldq % 16 || ldq < d1 || ldq > MAX_LD_BYTES; }
 
 void quantise_rows(const void* X, int64_t n, int64_t d1, int64_t ldx, int f32, int8_t* Xq, int64_t ldq, float* scale, hipStream_t s) {
-  hipLaunchKernelGGL(int_rows_kernel, dim3((unsigned)n), dim3(256), 0, s, X, f32, (int)d1, ldx, Xq, ldq, scale);
+  if (n <= 256) hipLaunchKernelGGL(int_rows_kernel<1024>, dim3((unsigned)n), dim3(1024), 0, s, X, f32, (int)d1, ldx, Xq, ldq, scale);
+  else hipLaunchKernelGGL(int_rows_kernel<256>, dim3((unsigned)n), dim3(256), 0, s, X, f32, (int)d1, ldx, Xq, ldq, scale);
 }
 
 }  // namespace
@@ -185,7 +189,7 @@ extern "C" size_t osscar_int_workspace_bytes(int64_t n, int64_t d1, int64_t m) {
   Carve c(nullptr);
   c.take((size_t)n * up16(d1));
   c.take((size_t)n * 4);
-  if (n <= thin::ROWS) c.take((size_t)thin::parts_of<OP_K, thin::I8>(m, d1) * n * m * 4);
+  if (n <= thin::ROWS) c.take((size_t)thin::deal<OP_K, thin::I8>(n, m, d1).parts * n * m * 4);
   return c.used + 256;
 }
 
@@ -224,14 +228,17 @@ extern "C" osscar_status osscar_int_product(const void* X_dev, int64_t n, int64_
   }
   const IntOut e{xs, w_scale_dev, bias_dev, Y_dev, ldy, y_dtype == OSSCAR_F32};
   if (few) {
-    thin::Product<1> t{reinterpret_cast<const char*>(xq), {reinterpret_cast<const char*>(Wq_dev)}, ldxq, ldq, (int)n, (int)m, (int)d1, thin::parts_of<OP_K, thin::I8>(m, d1), nullptr};
+    const thin::Deal d = thin::deal<OP_K, thin::I8>(n, m, d1);
+    thin::Product<1> t{reinterpret_cast<const char*>(xq), {reinterpret_cast<const char*>(Wq_dev)}, ldxq, ldq, (int)n, (int)m, (int)d1, d.parts, nullptr};
     if (t.parts > 1) {
       t.sums = c.take((size_t)t.parts * n * m * 4);
       if (!workspace_dev || c.used > workspace_bytes) return refuse_call(OSSCAR_ENOMEM, "osscar_int_product: workspace too small");
     }
-    const dim3 grid(thin::blocks_of<OP_K, thin::I8>(m), (unsigned)t.parts), block(thin::Wave<OP_K, thin::I8, 1, 1>::WAVES * 64);
-    if (n <= 16) hipLaunchKernelGGL(int_thin_kernel<1>, grid, block, 0, s, t, e);
-    else hipLaunchKernelGGL(int_thin_kernel<2>, grid, block, 0, s, t, e);
+    const dim3 grid(d.blocks, (unsigned)d.parts), block(512);
+    if (n <= 16 && d.wide) hipLaunchKernelGGL((int_thin_kernel<1, true>), grid, block, 0, s, t, e);
+    else if (n <= 16) hipLaunchKernelGGL((int_thin_kernel<1, false>), grid, block, 0, s, t, e);
+    else if (d.wide) hipLaunchKernelGGL((int_thin_kernel<2, true>), grid, block, 0, s, t, e);
+    else hipLaunchKernelGGL((int_thin_kernel<2, false>), grid, block, 0, s, t, e);
     const int64_t g = (n * m + 255) / 256;
     if (t.parts > 1) hipLaunchKernelGGL(int_join_kernel, dim3((unsigned)(g > 4096 ? 4096 : g)), dim3(256), 0, s, t, e);
     return launched("osscar_int_product");

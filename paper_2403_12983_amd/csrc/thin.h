@@ -20,6 +20,7 @@ using tile::v4i;
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 
 constexpr int ROWS = 32;           // rows of A, at most
+constexpr int WIDE_FROM = 6144;    // columns from which on 32 of them a workgroup fill three quarters of the compute units
 enum { BF16 = 0, F32 = 1, I8 = 2 };
 
 // Packet: 16 bytes of one row or column.  ELEMS of them; a matrix-core step contracts STEP elements, OPS instructions.
@@ -71,40 +72,48 @@ struct Product {
   void* sums;                // parts > 1: [part][matrix][m][n], 4 bytes each
 };
 
-template <int LAYOUT, int KIND, int NB, int RT> struct Wave;
+// WIDE: OP_K with 32 columns a wave and turns of two operands, so that the rows of A are read half as often (7168 x 14336, 16 rows: 109 us without);
+// taken where the chip is full with it.
+template <int LAYOUT, int KIND, int NB, int RT, bool WIDE> struct Wave;
 // OP_K
-template <int KIND, int NB, int RT>
-struct Wave<OP_K, KIND, NB, RT> {
+template <int KIND, int NB, int RT, bool WIDE>
+struct Wave<OP_K, KIND, NB, RT, WIDE> {
   typedef Num<KIND> T;
-  static constexpr int COLS = 16, TILES = 1, WAVES = 8, TURN = 4 * T::STEP;
-  static __device__ __forceinline__ int column(int, int i) { return i; }
-  const char *rb[NB], *ra[RT];
+  static constexpr int TILES = WIDE ? 2 : 1, U = WIDE ? 2 : 4, COLS = 16 * TILES, WAVES = 8, TURN = U * T::STEP;
+  static __device__ __forceinline__ int column(int t, int i) { return t * 16 + i; }
+  const char *rb[NB][TILES], *ra[RT];
   int koff;
   __device__ __forceinline__ void open(const Product<NB>& q, int n0, int lane) {
     const int i = lane & 15;
     koff = (lane >> 4) * T::ELEMS;
 #pragma unroll
-    for (int z = 0; z < NB; z++) rb[z] = q.b[z] + (int64_t)min(n0 + i, q.N - 1) * q.ldb;      // (past the end: the last one again, not used)
+    for (int z = 0; z < NB; z++)
+#pragma unroll
+      for (int t = 0; t < TILES; t++) rb[z][t] = q.b[z] + (int64_t)min(n0 + t * 16 + i, q.N - 1) * q.ldb;      // (past the end: the last one again, not used)
 #pragma unroll
     for (int r = 0; r < RT; r++) ra[r] = q.a + (int64_t)min(r * 16 + i, q.M - 1) * q.lda;
   }
-  struct Regs { v4i b[NB][4], a[RT][4]; };
+  struct Regs { v4i b[NB][TILES][U], a[RT][U]; };
   __device__ __forceinline__ void load(const Product<NB>& q, int k0, Regs& w) const {
     if (k0 + TURN <= q.K) {
 #pragma unroll
-      for (int u = 0; u < 4; u++) {
+      for (int u = 0; u < U; u++) {
         const int64_t at = (int64_t)(k0 + u * T::STEP + koff) * sizeof(typename T::el);
 #pragma unroll
-        for (int z = 0; z < NB; z++) w.b[z][u] = *reinterpret_cast<const v4i_any*>(rb[z] + at);
+        for (int z = 0; z < NB; z++)
+#pragma unroll
+          for (int t = 0; t < TILES; t++) w.b[z][t][u] = *reinterpret_cast<const v4i_any*>(rb[z][t] + at);
 #pragma unroll
         for (int r = 0; r < RT; r++) w.a[r][u] = *reinterpret_cast<const v4i_any*>(ra[r] + at);
       }
     } else {
 #pragma unroll
-      for (int u = 0; u < 4; u++) {
+      for (int u = 0; u < U; u++) {
         const int k = k0 + u * T::STEP + koff;
 #pragma unroll
-        for (int z = 0; z < NB; z++) w.b[z][u] = packet<KIND>(rb[z], k, q.K);
+        for (int z = 0; z < NB; z++)
+#pragma unroll
+          for (int t = 0; t < TILES; t++) w.b[z][t][u] = packet<KIND>(rb[z][t], k, q.K);
 #pragma unroll
         for (int r = 0; r < RT; r++) w.a[r][u] = packet<KIND>(ra[r], k, q.K);
       }
@@ -112,16 +121,18 @@ struct Wave<OP_K, KIND, NB, RT> {
   }
   __device__ __forceinline__ void multiply(const Regs& w, typename T::acc (&acc)[RT][NB][TILES]) const {
 #pragma unroll
-    for (int u = 0; u < 4; u++)
+    for (int u = 0; u < U; u++)
 #pragma unroll
       for (int z = 0; z < NB; z++)
 #pragma unroll
-        for (int r = 0; r < RT; r++) T::mma(w.b[z][u], w.a[r][u], acc[r][z][0]);
+        for (int t = 0; t < TILES; t++)
+#pragma unroll
+          for (int r = 0; r < RT; r++) T::mma(w.b[z][t][u], w.a[r][u], acc[r][z][t]);
   }
 };
 // OP_T: four columns of E rows k per lane (64 columns a wave: a memory line of bf16; with eight per lane the sums of two row tiles do not fit the registers)
 template <int KIND, int NB, int RT>
-struct Wave<OP_T, KIND, NB, RT> {
+struct Wave<OP_T, KIND, NB, RT, false> {
   typedef Num<KIND> T;
   typedef typename T::el el;
   static constexpr int E = T::ELEMS, WIDTH = 4, DWORDS = WIDTH * sizeof(el) / 4, COLS = 16 * WIDTH, TILES = WIDTH, WAVES = 4, TURN = T::STEP;
@@ -188,9 +199,9 @@ struct Wave<OP_T, KIND, NB, RT> {
 };
 
 // Epi::one(f) calls f(put) once, put(m, n, val (&v)[NB])
-template <int LAYOUT, int KIND, int NB, int RT, class Epi>
+template <int LAYOUT, int KIND, int NB, int RT, bool WIDE, class Epi>
 __device__ __forceinline__ void product(const Product<NB>& q, const Epi& epi) {
-  typedef Wave<LAYOUT, KIND, NB, RT> W;
+  typedef Wave<LAYOUT, KIND, NB, RT, WIDE> W;
   typedef typename W::T T;
   typedef typename T::val val;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -281,19 +292,21 @@ __device__ __forceinline__ void join(const Product<NB>& q, const Epi& epi) {
     }
   });
 }
-// Workgroups of a product, and the parts of its contraction: enough for `want` workgroups, of at least four turns for each wave.
+// How a product is dealt out: column blocks, wide or not, and parts of the contraction, enough for about two workgroups of four waves (OP_T) or half a
+// workgroup of eight (OP_K) per compute unit, each wave with at least two turns.
+struct Deal { unsigned blocks; int parts; bool wide; };
 template <int LAYOUT, int KIND>
-int parts_of(int64_t N, int64_t K) {
-  typedef Wave<LAYOUT, KIND, 1, 1> W;
-  const int64_t blocks = (N + W::COLS - 1) / W::COLS, turns = (K + W::TURN - 1) / W::TURN;
-  const int64_t want = LAYOUT == OP_K ? 128 : 512, most = turns / (W::WAVES * 2);
-  int64_t parts = want / blocks;
+Deal deal(int64_t M, int64_t N, int64_t K) {
+  typedef Wave<LAYOUT, KIND, 1, 1, false> W;
+  Deal d{(unsigned)((N + W::COLS - 1) / W::COLS), 1, LAYOUT == OP_K && M > 1 && N >= WIDE_FROM};
+  if (d.wide) { d.blocks = (unsigned)((N + 31) / 32); return d; }
+  const int64_t turns = (K + W::TURN - 1) / W::TURN, want = LAYOUT == OP_K ? 128 : 512, most = turns / (W::WAVES * 2);
+  int64_t parts = want / d.blocks;
   if (parts > most) parts = most;
   if (parts > 16) parts = 16;
-  return parts < 1 ? 1 : (int)parts;
+  d.parts = parts < 1 ? 1 : (int)parts;
+  return d;
 }
-template <int LAYOUT, int KIND>
-unsigned blocks_of(int64_t N) { return (unsigned)((N + Wave<LAYOUT, KIND, 1, 1>::COLS - 1) / Wave<LAYOUT, KIND, 1, 1>::COLS); }
 
 }  // namespace thin
 }  // namespace osscar

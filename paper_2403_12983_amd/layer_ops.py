@@ -46,10 +46,10 @@ def _ld(t: torch.Tensor, what: str) -> int:
     return s0
 
 
-def _on(device: torch.device, **tensors: Optional[torch.Tensor]):
+def _on(index: int, **tensors: Optional[torch.Tensor]):
     for name, t in tensors.items():
-        if t is not None and t.device != device:
-            _refuse(f"{name} is on {t.device}, expected {device}")
+        if t is not None and t.get_device() != index:
+            _refuse(f"{name} is on {t.device}, expected cuda:{index}")
 
 
 def _vector(t: torch.Tensor, n: int, dtype: torch.dtype, what: str) -> int:
@@ -59,16 +59,30 @@ def _vector(t: torch.Tensor, n: int, dtype: torch.dtype, what: str) -> int:
 
 
 def _begin(t: torch.Tensor, stream: Optional[torch.cuda.Stream]):
-    """(library, stream handle, contexts in which outputs are made and the call is issued)"""
-    if not t.is_cuda:
+    """(library, index of the GPU, stream handle, context in which outputs are made and the call is issued)"""
+    index = t.get_device()
+    if index < 0:
         _refuse("tensors must be on a GPU")
     if stream is None:
-        if t.device.index == torch.cuda.current_device():
-            return load_library(), torch.cuda.current_stream().cuda_stream, _NO_CONTEXT
-        return load_library(), torch.cuda.current_stream(t.device).cuda_stream, torch.cuda.device(t.device)
-    if stream.device != t.device:
-        _refuse(f"the stream is on {stream.device}, expected {t.device}")
-    return load_library(), stream.cuda_stream, torch.cuda.stream(stream)
+        context = _NO_CONTEXT if index == _current_device() else torch.cuda.device(index)
+        return load_library(), index, _current_stream(index), context
+    if stream.device.index != index:
+        _refuse(f"the stream is on {stream.device}, expected cuda:{index}")
+    return load_library(), index, stream.cuda_stream, torch.cuda.stream(stream)
+
+
+def _current_device() -> int:
+    return torch.cuda.current_device()
+
+
+def _current_stream(index: int) -> int:
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+# The handle without a Stream object around it, where this torch has it: a call of a single token is bound by what the host does.
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", _current_device)
+_EMPTY = torch.empty
 
 
 def _done(lib, status: int):
@@ -77,9 +91,13 @@ def _done(lib, status: int):
 
 
 def _workspace(size: int, device: torch.device):
+    """(tensor that holds it or None, its address, its size); the queries add 256 bytes to what is needed, so that 0 says invalid."""
     if size == 0:
         _refuse("invalid sizes")
-    return torch.empty(size, dtype=torch.uint8, device=device)
+    if size <= 256:
+        return None, None, 0
+    ws = _EMPTY(size, dtype=torch.uint8, device=device)
+    return ws, ws.data_ptr(), size
 
 
 def _gated(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, act: int) -> Tuple[_GatedDesc, int, int, int]:
@@ -88,7 +106,9 @@ def _gated(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, act: int) -> Tup
         _refuse("X is n x d, Wg and Wu are d x f")
     if Wg.dtype != X.dtype or Wu.dtype != X.dtype:
         _refuse("X, Wg and Wu have one dtype")
-    _on(X.device, Wg=Wg, Wu=Wu)
+    at = X.get_device()
+    if Wg.get_device() != at or Wu.get_device() != at:
+        _refuse("X, Wg and Wu are on one GPU")
     n, d = X.shape
     f = Wg.shape[1]
     if Wg.stride() != Wu.stride():
@@ -103,18 +123,18 @@ def osscar_gated_forward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, ac
                          stream: Optional[torch.cuda.Stream] = None):
     """H = act(X Wg) * (X Wu).  X: n x d, Wg, Wu: d x f, all float32 or all bfloat16.  save: returns (H, G, U) with the float32 projections
     that osscar_gated_backward takes, else H."""
-    lib, handle, context = _begin(X, stream)
+    lib, index, handle, context = _begin(X, stream)
     desc, xp, gp, up = _gated(X, Wg, Wu, act)
     n, f, device = desc.n, desc.f, X.device
     with context:
-        H = torch.empty(n, f, dtype=X.dtype, device=device)
+        H = _EMPTY(n, f, dtype=X.dtype, device=device)
         G = U = None
         if save:
-            G, U = torch.empty(n, f, dtype=torch.float32, device=device), torch.empty(n, f, dtype=torch.float32, device=device)
+            G, U = _EMPTY(n, f, dtype=torch.float32, device=device), _EMPTY(n, f, dtype=torch.float32, device=device)
         size = lib.osscar_gated_workspace_bytes(C.byref(desc), 0)
-        ws = _workspace(size, device)
+        ws, wp, size = _workspace(size, device)
         status = lib.osscar_gated_forward(C.byref(desc), xp, gp, up, H.data_ptr(), G.data_ptr() if save else None, U.data_ptr() if save else None,
-                                          ws.data_ptr(), size, handle)
+                                          wp, size, handle)
     _done(lib, status)
     return (H, G, U) if save else H
 
@@ -124,7 +144,7 @@ def osscar_gated_backward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, d
                           dw_dtype: Optional[torch.dtype] = None, stream: Optional[torch.cuda.Stream] = None):
     """(dX, dWg, dWu) of osscar_gated_forward for the gradient dH of H; None for what is not needed.  G, U: from forward's save=True (else they
     are computed again).  The weights' gradients lie in memory as the weights do; dw_dtype: float32 or bfloat16, by default the weights'."""
-    lib, handle, context = _begin(X, stream)
+    lib, index, handle, context = _begin(X, stream)
     desc, xp, gp, up = _gated(X, Wg, Wu, act)
     n, d, f, device = desc.n, desc.d, desc.f, X.device
     if dH.shape != (n, f) or dH.dtype != X.dtype:
@@ -134,23 +154,23 @@ def osscar_gated_backward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, d
     for name, t in (("G", G), ("U", U)):
         if t is not None and (t.shape != (n, f) or t.dtype != torch.float32 or not t.is_contiguous()):
             _refuse(f"{name} must be a contiguous float32 matrix, n x f")
-    _on(device, dH=dH, G=G, U=U)
+    _on(index, dH=dH, G=G, U=U)
     desc.ldh = _ld(dH, "dH")
     dw_dtype = X.dtype if dw_dtype is None else dw_dtype
     if dw_dtype not in _CODES:
         _refuse(f"dw_dtype {dw_dtype} is neither float32 nor bfloat16")
     with context:
-        dX = torch.empty(n, d, dtype=X.dtype, device=device) if need_x else None
+        dX = _EMPTY(n, d, dtype=X.dtype, device=device) if need_x else None
         dWg = dWu = None
         lddw = d if desc.rows_out else f
         if need_w:
             shape = (f, d) if desc.rows_out else (d, f)
-            dWg, dWu = torch.empty(shape, dtype=dw_dtype, device=device), torch.empty(shape, dtype=dw_dtype, device=device)
+            dWg, dWu = _EMPTY(shape, dtype=dw_dtype, device=device), _EMPTY(shape, dtype=dw_dtype, device=device)
         size = lib.osscar_gated_workspace_bytes(C.byref(desc), 1 if G is not None else 2)
-        ws = _workspace(size, device)
+        ws, wp, size = _workspace(size, device)
         status = lib.osscar_gated_backward(C.byref(desc), xp, gp, up, dH.data_ptr(), G.data_ptr() if G is not None else None,
                                            U.data_ptr() if U is not None else None, dX.data_ptr() if need_x else None, d,
-                                           dWg.data_ptr() if need_w else None, dWu.data_ptr() if need_w else None, lddw, _CODES[dw_dtype], ws.data_ptr(),
+                                           dWg.data_ptr() if need_w else None, dWu.data_ptr() if need_w else None, lddw, _CODES[dw_dtype], wp,
                                            size, handle)
     _done(lib, status)
     if need_w and desc.rows_out:
@@ -161,7 +181,7 @@ def osscar_gated_backward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, d
 def osscar_int_weights(W: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(Wq, w_scale) of W (d1 x m, either layout in memory): Wq is m x ld int8, ld = d1 rounded up to 16, zeros from column d1 on; channel j of W is
     w_scale[j] * Wq[j, :d1] to the nearest."""
-    lib, handle, context = _begin(W, stream)
+    lib, index, handle, context = _begin(W, stream)
     code = _code(W, "W")
     if W.dim() != 2:
         _refuse("W must be a matrix")
@@ -170,7 +190,7 @@ def osscar_int_weights(W: torch.Tensor, stream: Optional[torch.cuda.Stream] = No
     ldw = _ld(W.t() if rows_out else W, "W")
     ldq = -(-d1 // 16) * 16
     with context:
-        Wq, scale = torch.empty(m, ldq, dtype=torch.int8, device=W.device), torch.empty(m, dtype=torch.float32, device=W.device)
+        Wq, scale = _EMPTY(m, ldq, dtype=torch.int8, device=W.device), _EMPTY(m, dtype=torch.float32, device=W.device)
         status = lib.osscar_int_weights(W.data_ptr(), d1, m, ldw, code, rows_out, Wq.data_ptr(), ldq, scale.data_ptr(), handle)
     _done(lib, status)
     return Wq, scale
@@ -178,12 +198,12 @@ def osscar_int_weights(W: torch.Tensor, stream: Optional[torch.cuda.Stream] = No
 
 def osscar_int_rows(X: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(Xq, x_scale) of the rows of X (n x d1), for several products with the same X: Xq is n x d1 int8 (a view of rows padded to 16)."""
-    lib, handle, context = _begin(X, stream)
+    lib, index, handle, context = _begin(X, stream)
     code, ldx = _code(X, "X"), _ld(X, "X")
     n, d1 = X.shape
     ldq = -(-d1 // 16) * 16
     with context:
-        Xq, scale = torch.empty(n, ldq, dtype=torch.int8, device=X.device), torch.empty(n, dtype=torch.float32, device=X.device)
+        Xq, scale = _EMPTY(n, ldq, dtype=torch.int8, device=X.device), _EMPTY(n, dtype=torch.float32, device=X.device)
         status = lib.osscar_int_rows(X.data_ptr(), n, d1, ldx, code, Xq.data_ptr(), ldq, scale.data_ptr(), handle)
     _done(lib, status)
     return Xq[:, :d1], scale
@@ -193,7 +213,7 @@ def osscar_int_product(X: torch.Tensor, Wq: torch.Tensor, w_scale: torch.Tensor,
                        x_scale: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.bfloat16,
                        stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Y = (X quantised row by row) times the weights of osscar_int_weights, n x m.  X: float32 or bfloat16, or int8 with x_scale (osscar_int_rows)."""
-    lib, handle, context = _begin(X, stream)
+    lib, index, handle, context = _begin(X, stream)
     if X.dim() != 2 or Wq.dim() != 2 or Wq.dtype != torch.int8:
         _refuse("X is a matrix, Wq an int8 matrix")
     n, d1 = X.shape
@@ -206,17 +226,17 @@ def osscar_int_product(X: torch.Tensor, Wq: torch.Tensor, w_scale: torch.Tensor,
     if out_dtype not in _CODES:
         _refuse(f"out_dtype {out_dtype} is neither float32 nor bfloat16")
     device = X.device
-    _on(device, Wq=Wq, w_scale=w_scale, bias=bias, x_scale=x_scale)
+    _on(index, Wq=Wq, w_scale=w_scale, bias=bias, x_scale=x_scale)
     wsp = _vector(w_scale, m, torch.float32, "w_scale")
     bp = _vector(bias, m, torch.float32, "bias") if bias is not None else None
     xsp = _vector(x_scale, n, torch.float32, "x_scale") if x_scale is not None else None
     ldx, ldq = _ld(X, "X"), _ld(Wq, "Wq")
     with context:
-        Y = torch.empty(n, m, dtype=out_dtype, device=device)
+        Y = _EMPTY(n, m, dtype=out_dtype, device=device)
         size = lib.osscar_int_workspace_bytes(n, d1, m)
-        ws = _workspace(size, device)
+        ws, wp, size = _workspace(size, device)
         status = lib.osscar_int_product(X.data_ptr(), n, d1, ldx, code, xsp, Wq.data_ptr(), ldq, wsp, m, bp, Y.data_ptr(), m, _CODES[out_dtype],
-                                        ws.data_ptr(), size, handle)
+                                        wp, size, handle)
     _done(lib, status)
     return Y
 
@@ -234,23 +254,23 @@ def osscar_logprobs(logits: torch.Tensor, targets: torch.Tensor, top: int = 0, s
                     stream: Optional[torch.cuda.Stream] = None) -> LogProbs:
     """Log probability of targets[i] under softmax(scale * logits[i]), the entropy, and the `top` largest logits of every row with their log
     probabilities.  targets: int64, negative where a row has none."""
-    lib, handle, context = _begin(logits, stream)
+    lib, index, handle, context = _begin(logits, stream)
     code, ld = _code(logits, "logits"), _ld(logits, "logits")
     n, vocab = logits.shape
     device = logits.device
-    _on(device, targets=targets)
+    _on(index, targets=targets)
     tp = _vector(targets, n, torch.int64, "targets")
     with context:
-        out = torch.empty(4, n, dtype=torch.float32, device=device)      # logp, entropy, lse
-        index = torch.empty(n, top, dtype=torch.int64, device=device) if top > 0 else None
-        top_logp = torch.empty(n, top, dtype=torch.float32, device=device) if top > 0 else None
+        out = _EMPTY(4, n, dtype=torch.float32, device=device)      # logp, entropy, lse
+        top_index = _EMPTY(n, top, dtype=torch.int64, device=device) if top > 0 else None
+        top_logp = _EMPTY(n, top, dtype=torch.float32, device=device) if top > 0 else None
         size = lib.osscar_logprobs_workspace_bytes(n, vocab, top)
-        ws = _workspace(size, device)
+        ws, wp, size = _workspace(size, device)
         base = out.data_ptr()
         status = lib.osscar_logprobs(logits.data_ptr(), n, vocab, ld, code, tp, scale, top, base, base + 4 * n, base + 8 * n,
-                                     index.data_ptr() if top > 0 else None, top_logp.data_ptr() if top > 0 else None, ws.data_ptr(), size, handle)
+                                     top_index.data_ptr() if top > 0 else None, top_logp.data_ptr() if top > 0 else None, wp, size, handle)
     _done(lib, status)
-    return LogProbs(out[0], out[1], out[2:].view(n, 2), index, top_logp)
+    return LogProbs(out[0], out[1], out[2:].view(n, 2), top_index, top_logp)
 
 
 def osscar_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, dlogp: Optional[torch.Tensor] = None,
@@ -259,11 +279,11 @@ def osscar_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, lse: t
                              out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Gradient of the logits from those of logp, entropy and top_logp (any may be None).  lse, entropy, top_index: what osscar_logprobs returned
     for these logits and this scale.  out: where to put it, `logits` itself included."""
-    lib, handle, context = _begin(logits, stream)
+    lib, index, handle, context = _begin(logits, stream)
     code, ld = _code(logits, "logits"), _ld(logits, "logits")
     n, vocab = logits.shape
     device = logits.device
-    _on(device, targets=targets, lse=lse, dlogp=dlogp, entropy=entropy, dentropy=dentropy, top_index=top_index, dtop=dtop, out=out)
+    _on(index, targets=targets, lse=lse, dlogp=dlogp, entropy=entropy, dentropy=dentropy, top_index=top_index, dtop=dtop, out=out)
     if lse.shape != (n, 2) or lse.dtype != torch.float32 or not lse.is_contiguous():
         _refuse("lse must be the n x 2 float32 tensor of osscar_logprobs")
     if (dtop is None) != (top_index is None) or (dentropy is not None and entropy is None):
@@ -280,7 +300,7 @@ def osscar_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, lse: t
     rows = [None if t is None else _vector(t, n, torch.float32, name) for name, t in (("dlogp", dlogp), ("entropy", entropy), ("dentropy", dentropy))]
     with context:
         if out is None:
-            out = torch.empty(n, vocab, dtype=logits.dtype, device=device)
+            out = _EMPTY(n, vocab, dtype=logits.dtype, device=device)
         status = lib.osscar_logprobs_backward(logits.data_ptr(), n, vocab, ld, code, tp, scale, lse.data_ptr(), rows[0], rows[1], rows[2], top,
                                               top_index.data_ptr() if top > 0 else None, dtop.data_ptr() if top > 0 else None, out.data_ptr(), _ld(out, "out"),
                                               handle)
