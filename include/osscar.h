@@ -339,8 +339,7 @@ typedef struct {
   int32_t unaligned;  /* nonzero: X, Wg or Wu may begin at any element; zero: at a 16-byte boundary (bf16) */
 } osscar_gated_desc;
 /* Workspace of a forward call (backward = 0), of a backward call with G and U (1) or without (2); 0 if the description is invalid.  A
- * forward call takes next to nothing, unless rows are copied: float32 operands, and bf16 operands whose rows do not begin at 16-byte boundaries or are not a
- * multiple of 8 long. */
+ * forward call takes next to nothing, unless rows are copied: bf16 operands whose rows do not begin at 16-byte boundaries or are not a multiple of 8 long. */
 size_t osscar_gated_workspace_bytes(const osscar_gated_desc* desc, int32_t backward);
 /* G_dev, U_dev (both or neither): dense n x f float32 outputs, g and u for osscar_gated_backward. */
 osscar_status osscar_gated_forward(const osscar_gated_desc* desc, const void* X_dev, const void* Wg_dev, const void* Wu_dev, void* H_dev,

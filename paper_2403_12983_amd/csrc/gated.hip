@@ -2,6 +2,7 @@
 //     dg = dh u a'(g), du = dh a(g);   dX = dg Wg^T + du Wu^T, dWg = X^T dg, dWu = X^T du.
 // h is the X that the Gram of the layer's down projection takes.
 #include "ops.h"
+#include "split.h"
 #include "thin.h"
 #include "tile.h"
 
@@ -66,57 +67,24 @@ __device__ __forceinline__ void with_act(int act, F f) {
   }
 }
 
-// ---- float32 as three bf16 -------------------------------------------------------------------
-// x = p0 + p1 + p2, each the nearest bf16 of what is left: 24 bits.  What bf16 cannot hold as a finite number (infinities, NaN, the last
-// float32 values) goes into p0 alone, as it is or, if finite, cut off.
-__device__ __forceinline__ void cut3(float x, uint16_t (&p)[3]) {
-  uint16_t b = bf16_nearest(x);
-  if ((b & 0x7F80) == 0x7F80) {
-    const uint32_t u = __float_as_uint(x);
-    if ((u & 0x7F800000u) == 0x7F800000u) { p[0] = b; p[1] = p[2] = 0; return; }
-    b = (uint16_t)(u >> 16);
-  }
-  p[0] = b;
-  const float r = x - bf16_value(b);
-  p[1] = bf16_nearest(r);
-  p[2] = bf16_nearest(r - bf16_value(p[1]));
-}
-// C neighbouring values as `pieces` bf16 each, in arrays `step` elements apart; columns from `most` on become zeros up to `width`
-template <int C>
-__device__ __forceinline__ void put_pieces(uint16_t* p, int64_t step, int pieces, const float (&v)[C], int most, int width) {
-#pragma unroll
-  for (int c = 0; c < C; c += 8) {
-    if (c >= width) break;      // (width is a multiple of eight)
-    u16x8 w[3];
-#pragma unroll
-    for (int e = 0; e < 8; e++) {
-      const float x = c + e < most ? v[c + e] : 0.f;
-      if (pieces == 1) {
-        w[0][e] = bf16_nearest(x);
-      } else {
-        uint16_t t[3];
-        cut3(x, t);
-        w[0][e] = t[0]; w[1][e] = t[1]; w[2][e] = t[2];
-      }
-    }
-    *reinterpret_cast<u16x8*>(p + c) = w[0];
-    if (pieces > 1) {
-      *reinterpret_cast<u16x8*>(p + step + c) = w[1];
-      *reinterpret_cast<u16x8*>(p + 2 * step + c) = w[2];
-    }
-  }
-}
-// A matrix as `pieces` matrices of bf16 whose rows are `ld` long (a multiple of eight, zeros past cols).  Eight columns per thread; bound by
-// its reads and writes.
-__global__ __launch_bounds__(256) void gated_pieces_kernel(const void* __restrict__ src, int f32, int64_t rows, int cols, int64_t lds_, uint16_t* __restrict__ dst,
-                                                           int64_t ld, int64_t step, int pieces) {
+// ---- copies ----------------------------------------------------------------------------------
+// A bf16 matrix with rows of `ld` (a multiple of eight), zeros past cols.  Eight columns per thread; bound by its reads and writes.
+__global__ __launch_bounds__(256) void gated_copy_kernel(const uint16_t* __restrict__ src, int64_t rows, int cols, int64_t lds_, uint16_t* __restrict__ dst, int64_t ld) {
   const int packs = (int)(ld / 8);
   for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < rows * packs; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / packs;
     const int c = (int)(i - r * packs) * 8;
-    float v[8];
-    get_values(src, r * lds_ + c, f32, v, cols - c);
-    put_pieces(dst + r * ld + c, step, pieces, v, cols - c, 8);
+    u16x8 w;
+    if (c + 8 <= cols) {
+      w = *reinterpret_cast<const u16x8_any*>(src + r * lds_ + c);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        w[e] = 0;
+        if (c + e < cols) w[e] = src[r * lds_ + c + e];
+      }
+    }
+    *reinterpret_cast<u16x8*>(dst + r * ld + c) = w;
   }
 }
 
@@ -155,13 +123,13 @@ struct GatedOut {      // h, and g and u as they are where the caller keeps them
     });
   }
 };
-// dg and du, rounded to bf16 (they are operands of the next products, as h is of the next layer) or in three pieces
-struct GradPlace { uint16_t *dg, *du; int64_t ld, step; int pieces; };
 template <int LAYOUT, int KIND, int RT, bool WIDE>
 __global__ __launch_bounds__((thin::Wave<LAYOUT, KIND, 2, RT, WIDE>::WAVES) * 64, 1) void gated_thin_kernel(const thin::Product<2> p, const GatedOut e) {
   thin::product<LAYOUT, KIND, 2, RT, WIDE>(p, e);
 }
-__global__ __launch_bounds__(256) void gated_join_kernel(const thin::Product<2> p, const GatedOut e) { thin::join<2, float>(p, e); }
+__global__ __launch_bounds__(256) void gated_join_kernel(const float* __restrict__ sums, int parts, int M, int N, const GatedOut e) {
+  tile::join<2>(sums, parts, M, N, e);
+}
 
 struct PlainOut {
   void* out; int64_t ld; int f32;
@@ -172,31 +140,46 @@ struct PlainOut {
       else put_bf16(reinterpret_cast<uint16_t*>(out) + (int64_t)m * ld + n, v[0], N - n);
     });
   }
+  template <class F>
+  __device__ __forceinline__ void one(F f) const {
+    f([&](int m, int n, const float (&v)[1], int) {
+      if (f32) reinterpret_cast<float*>(out)[(int64_t)m * ld + n] = v[0];
+      else reinterpret_cast<uint16_t*>(out)[(int64_t)m * ld + n] = bf16_nearest(v[0]);
+    });
+  }
 };
-// dg and du from kept g and u.  Bound by its 14 bytes per element (bf16).
-__global__ __launch_bounds__(256) void gated_grad_kernel(const void* __restrict__ dH, int64_t lddh, int f32, int act, const float* __restrict__ G,
-                                                         const float* __restrict__ U, int64_t rows, int f, GradPlace o) {
-  const int packs = (int)(o.ld / 8);
+// dg and du from kept g and u, in the type of the products that take them: bf16 rounds them once more, as h is rounded for the next layer.  Rows of
+// `ld`, a multiple of eight, zeros past f.  Bound by its 14 (float32: 20) bytes per element.
+template <bool F32>
+__global__ __launch_bounds__(256) void gated_grad_kernel(const void* __restrict__ dH, int64_t lddh, int act, const float* __restrict__ G,
+                                                         const float* __restrict__ U, int64_t rows, int f, void* __restrict__ out_g, void* __restrict__ out_u, int64_t ld) {
+  const int packs = (int)(ld / 8);
   for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < rows * packs; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / packs;
     const int n = (int)(i - r * packs) * 8;
     float g[8], u[8], dh[8];
     get_values(G, r * f + n, 1, g, f - n);
     get_values(U, r * f + n, 1, u, f - n);
-    get_values(dH, r * lddh + n, f32, dh, f - n);
+    get_values(dH, r * lddh + n, F32, dh, f - n);
     float dg[8], du[8];
     with_act(act, [&](auto a) {
 #pragma unroll
       for (int c = 0; c < 8; c++) {
         float av, da;
         act_slope<decltype(a)::value>(g[c], av, da);
-        dg[c] = dh[c] * u[c] * da;
-        du[c] = dh[c] * av;
+        const bool in = n + c < f;
+        dg[c] = in ? dh[c] * u[c] * da : 0.f;
+        du[c] = in ? dh[c] * av : 0.f;
       }
     });
-    const int64_t at = r * o.ld + n;
-    put_pieces(o.dg + at, o.step, o.pieces, dg, f - n, 8);
-    put_pieces(o.du + at, o.step, o.pieces, du, f - n, 8);
+    const int64_t at = r * ld + n;
+    if (F32) {
+      put_f32(reinterpret_cast<float*>(out_g) + at, dg, 8);
+      put_f32(reinterpret_cast<float*>(out_u) + at, du, 8);
+    } else {
+      put_bf16(reinterpret_cast<uint16_t*>(out_g) + at, dg, 8);
+      put_bf16(reinterpret_cast<uint16_t*>(out_u) + at, du, 8);
+    }
   }
 }
 
@@ -204,95 +187,120 @@ __global__ __launch_bounds__(256) void gated_grad_kernel(const void* __restrict_
 template <int NB, class Epi> struct Pair { Product<NB> p[2]; Epi e[2]; };
 template <int AM, int BMODE, class S, class Epi>
 __global__ __launch_bounds__(S::WAVES * 64, 1) void gated_product_kernel(const Pair<S::NB, Epi> q) {
-  product_tile<false, AM, BMODE, S>(q.p[blockIdx.y], q.e[blockIdx.y]);
+  tile::product_tile<false, AM, BMODE, S>(q.p[blockIdx.y], q.e[blockIdx.y]);
+}
+template <int AM, int BMODE, class S, class Epi>      // float32
+__global__ __launch_bounds__(S::WAVES * 64, 2) void gated_split_kernel(const Pair<S::NB, Epi> q) {
+  split::product_tile<AM, BMODE, S>(q.p[blockIdx.y], q.e[blockIdx.y]);
 }
 
 // ---- shapes ----------------------------------------------------------------------------------
-typedef Shape<2, 2, 8, 4, 2> Big2;       // 256 x (128 + 128), four waves
-typedef Shape<2, 2, 4, 2, 2> Small2;     // 128 x (64 + 64), four waves
-typedef Shape<2, 2, 8, 8, 1> Big1;       // 256 x 256
-typedef Shape<2, 2, 4, 4, 1> Small1;     // 128 x 128
-constexpr int FILL = 192;                // workgroups of the big shape from which on it is taken: three quarters of the compute units
-
-template <class S, int NB>
-int64_t tiles(const Product<NB>& p) { return ((int64_t)p.M + S::BM - 1) / S::BM * (((int64_t)p.N + S::BN - 1) / S::BN); }
-
+typedef Shape<2, 2, 8, 4, 2, false> Big2;       // 256 x (128 + 128), four waves
+typedef Shape<2, 2, 4, 2, 2, true> Small2;     // 128 x (64 + 64), four waves
+typedef Shape<2, 2, 8, 8, 1, false> Big1;       // 256 x 256
+typedef Shape<2, 2, 4, 4, 1, true> Small1;     // 128 x 128
+__global__ __launch_bounds__(256) void plain_join_kernel(const float* __restrict__ sums, int parts, int M, int N, const PlainOut e) {
+  tile::join<1>(sums, parts, M, N, e);
+}
+void launch_join(const Product<2>& p, const GatedOut& e, hipStream_t s) {
+  hipLaunchKernelGGL(gated_join_kernel, dim3(join_grid(p.M, p.N)), dim3(256), 0, s, reinterpret_cast<const float*>(p.sums), p.parts, p.M, p.N, e);
+}
+void launch_join(const Product<1>& p, const PlainOut& e, hipStream_t s) {
+  hipLaunchKernelGGL(plain_join_kernel, dim3(join_grid(p.M, p.N)), dim3(256), 0, s, reinterpret_cast<const float*>(p.sums), p.parts, p.M, p.N, e);
+}
+// `count` products of one launch; sums: sums_bytes() of them
 template <int AM, int BMODE, class SB, class SS, class Epi>
-void launch_product(const Pair<SB::NB, Epi>& q, int count, hipStream_t s) {
-  const int64_t big = tiles<SB>(q.p[0]);
-  if (big * count >= FILL)
-    hipLaunchKernelGGL((gated_product_kernel<AM, BMODE, SB, Epi>), dim3((unsigned)big, count), dim3(SB::WAVES * 64), 0, s, q);
-  else
-    hipLaunchKernelGGL((gated_product_kernel<AM, BMODE, SS, Epi>), dim3((unsigned)tiles<SS>(q.p[0]), count), dim3(SS::WAVES * 64), 0, s, q);
+void launch_product(Pair<SB::NB, Epi>& q, int count, bool f32, const Deal& d, char* sums, hipStream_t s) {
+  for (int c = 0; c < count; c++) {
+    q.p[c].parts = d.parts;
+    q.p[c].sums = sums + (size_t)c * sums_bytes(d, SB::NB, 1, q.p[c].M, q.p[c].N);
+  }
+  const dim3 grid(d.tiles, count, d.parts);
+  if (f32) hipLaunchKernelGGL((gated_split_kernel<AM, BMODE, SS, Epi>), grid, dim3(SS::WAVES * 64), 0, s, q);
+  else if (d.big) hipLaunchKernelGGL((gated_product_kernel<AM, BMODE, SB, Epi>), grid, dim3(SB::WAVES * 64), 0, s, q);
+  else hipLaunchKernelGGL((gated_product_kernel<AM, BMODE, SS, Epi>), grid, dim3(SS::WAVES * 64), 0, s, q);
+  for (int c = 0; c < count && d.parts > 1; c++) launch_join(q.p[c], q.e[c], s);
 }
 
 // ---- operands --------------------------------------------------------------------------------
 inline int64_t up8(int64_t v) { return (v + 7) / 8 * 8; }
-inline unsigned pieces_grid(int64_t rows, int64_t ld) {
+inline unsigned packs_grid(int64_t rows, int64_t ld) {
   const int64_t n = (rows * (ld / 8) + 255) / 256;
   return (unsigned)(n < 1 ? 1 : (n > 8192 ? 8192 : n));
 }
-// A matrix of a call as the products take it: in place, or as pieces in the workspace.
+// A matrix of a call as the products take it: in place, or (bf16 at other alignments) copied to the workspace.
 struct Source {
-  const void* p; int64_t rows, cols, ld; bool copied; int pieces; char* at; int64_t ldp;
-  Operand operand() const {      // piece 0 in p[0], ...
+  const void* p; int64_t rows, cols, ld; int es; bool copied; char* at;
+  Operand operand() const {
     Operand o{};
-    for (int t = 0; t < pieces; t++) o.p[t] = copied ? at + (size_t)t * rows * ldp * 2 : reinterpret_cast<const char*>(p);
-    o.ldb = (copied ? ldp : ld) * 2; o.rows = (int)rows; o.cols = (int)(copied ? ldp : cols);
+    o.p[0] = copied ? at : reinterpret_cast<const char*>(p);
+    o.ldb = (copied ? up8(cols) : ld) * es; o.rows = (int)rows; o.cols = (int)(copied ? up8(cols) : cols);
     return o;
   }
-  void make(int f32, hipStream_t s) const {
+  void make(hipStream_t s) const {
     if (copied && rows > 0)
-      hipLaunchKernelGGL(gated_pieces_kernel, dim3(pieces_grid(rows, ldp)), dim3(256), 0, s, p, f32, rows, (int)cols, ld, reinterpret_cast<uint16_t*>(at), ldp,
-                         rows * ldp, pieces);
+      hipLaunchKernelGGL(gated_copy_kernel, dim3(packs_grid(rows, up8(cols))), dim3(256), 0, s, reinterpret_cast<const uint16_t*>(p), rows, (int)cols, ld,
+                         reinterpret_cast<uint16_t*>(at), up8(cols));
   }
 };
 // `loose`: some buffer of the call does not begin at a 16-byte boundary
 Source source(Carve& c, const void* p, int64_t rows, int64_t cols, int64_t ld, int32_t dtype, bool loose) {
-  Source s{p, rows, cols, ld, false, dtype == OSSCAR_F32 ? 3 : 1, nullptr, up8(cols)};
-  s.copied = dtype == OSSCAR_F32 || loose || !operand_fits(nullptr, ld, cols, 2);
-  if (s.copied) s.at = c.take((size_t)s.pieces * rows * s.ldp * 2);
+  Source s{p, rows, cols, ld, dtype == OSSCAR_F32 ? 4 : 2, false, nullptr};
+  s.copied = dtype == OSSCAR_BF16 && (loose || !operand_fits(nullptr, ld, cols, 2));
+  if (s.copied) s.at = c.take((size_t)rows * up8(cols) * 2);
   return s;
 }
-// The segments of sum_t A_t B_t: pieces of weight 2^-16 and more, the smallest products first.
-constexpr int PAIRS3[6][2] = {{2, 0}, {1, 1}, {0, 2}, {1, 0}, {0, 1}, {0, 0}};
 template <int NB>
-void add_segments(Product<NB>& q, const Operand& a, const Operand (&b)[NB], int pieces) {
-  const int first = q.nseg;
+void add_segment(Product<NB>& q, const Operand& a, const Operand (&b)[NB]) {
   q.a.ldb = a.ldb; q.a.rows = a.rows; q.a.cols = a.cols;
-  for (int z = 0; z < NB; z++) { q.b[z].ldb = b[z].ldb; q.b[z].rows = b[z].rows; q.b[z].cols = b[z].cols; }
-  for (int t = 0; t < (pieces == 1 ? 1 : 6); t++) {
-    const int x = pieces == 1 ? 0 : PAIRS3[t][0], y = pieces == 1 ? 0 : PAIRS3[t][1];
-    q.a.p[first + t] = a.p[x];
-    for (int z = 0; z < NB; z++) q.b[z].p[first + t] = b[z].p[y];
-    q.nseg++;
+  q.a.p[q.nseg] = a.p[0];
+  for (int z = 0; z < NB; z++) {
+    q.b[z].ldb = b[z].ldb; q.b[z].rows = b[z].rows; q.b[z].cols = b[z].cols;
+    q.b[z].p[q.nseg] = b[z].p[0];
   }
+  q.nseg++;
 }
 
 struct Buffers {
   Source x, wg, wu;
-  uint16_t *dg, *du; int64_t ldg;
+  char *dg, *du; int64_t ldg;
   float *g, *u;      // computed again
-  thin::Deal few; char* sums;      // few rows: how they are dealt out, and the sums of the parts
+  thin::Deal few;        // how the products are dealt out: few rows' projections, others', dX, both weights' gradients
+  Deal proj, dx, dw;
+  char* sums;            // of parts, one product after the other
 };
 bool few(const osscar_gated_desc& q) { return q.n <= thin::ROWS; }
 Buffers buffers(Carve& c, const osscar_gated_desc& q, const void* X, const void* Wg, const void* Wu, int backward, bool kept) {
   Buffers b{};
-  if (few(q) && !kept) {
-    b.few = q.rows_out ? (q.dtype == OSSCAR_F32 ? thin::deal<OP_K, thin::F32>(q.n, q.f, q.d) : thin::deal<OP_K, thin::BF16>(q.n, q.f, q.d))
-                       : (q.dtype == OSSCAR_F32 ? thin::deal<OP_T, thin::F32>(q.n, q.f, q.d) : thin::deal<OP_T, thin::BF16>(q.n, q.f, q.d));
-    if (b.few.parts > 1) b.sums = c.take((size_t)b.few.parts * 2 * q.n * q.f * 4);
-    if (!backward) return b;
+  const bool f32 = q.dtype == OSSCAR_F32;
+  const int ks = f32 ? split::KS : STEP_BYTES / 2;
+  size_t sums = 0;
+  if (!kept && few(q)) {
+    b.few = q.rows_out ? (f32 ? thin::deal<OP_K, thin::F32>(q.n, q.f, q.d) : thin::deal<OP_K, thin::BF16>(q.n, q.f, q.d))
+                       : (f32 ? thin::deal<OP_T, thin::F32>(q.n, q.f, q.d) : thin::deal<OP_T, thin::BF16>(q.n, q.f, q.d));
+    if (b.few.parts > 1) sums = (size_t)b.few.parts * 2 * q.n * q.f * 4;
+  } else if (!kept) {
+    b.proj = deal<Big2, Small2>(q.n, q.f, (q.d + ks - 1) / ks, 1, f32);
+    sums = sums_bytes(b.proj, 2, 1, q.n, q.f);
   }
+  if (backward) {
+    b.dx = deal<Big1, Small1>(q.n, q.d, (q.f + ks - 1) / ks * 2, 1, f32);
+    b.dw = deal<Big1, Small1>(q.rows_out ? q.f : q.d, q.rows_out ? q.d : q.f, (q.n + ks - 1) / ks, 2, f32);
+    const size_t x = sums_bytes(b.dx, 1, 1, q.n, q.d), w = sums_bytes(b.dw, 1, 2, q.d, q.f);
+    sums = sums > x ? sums : x;
+    sums = sums > w ? sums : w;
+  }
+  b.sums = c.take(sums);
+  if (!backward && few(q)) return b;
   const int64_t wr = q.rows_out ? q.f : q.d, wc = q.rows_out ? q.d : q.f;
   b.x = source(c, X, q.n, q.d, q.ldx, q.dtype, q.unaligned != 0);
   b.wg = source(c, Wg, wr, wc, q.ldw, q.dtype, q.unaligned != 0);
   b.wu = source(c, Wu, wr, wc, q.ldw, q.dtype, q.unaligned != 0);
   if (backward) {
     b.ldg = up8(q.f);
-    const size_t bytes = (size_t)(q.dtype == OSSCAR_F32 ? 3 : 1) * q.n * b.ldg * 2;
-    b.dg = reinterpret_cast<uint16_t*>(c.take(bytes));
-    b.du = reinterpret_cast<uint16_t*>(c.take(bytes));
+    const size_t bytes = (size_t)q.n * b.ldg * (q.dtype == OSSCAR_F32 ? 4 : 2);
+    b.dg = c.take(bytes);
+    b.du = c.take(bytes);
     if (!kept) {
       b.g = reinterpret_cast<float*>(c.take((size_t)q.n * q.f * 4));
       b.u = reinterpret_cast<float*>(c.take((size_t)q.n * q.f * 4));
@@ -300,9 +308,12 @@ Buffers buffers(Carve& c, const osscar_gated_desc& q, const void* X, const void*
   }
   return b;
 }
+int64_t up_tiles(int64_t v) { return (v + 63) / 64; }
 const char* bad_desc(const osscar_gated_desc* q) {
   if (!q) return "osscar_gated: NULL description";
   if (!a_size(q->n, 0) || !a_size(q->d, 1) || !a_size(q->f, 1)) return "osscar_gated: n >= 0, d and f must be positive, none above 2^30";
+  if (up_tiles(q->n) * up_tiles(q->f) > 0x3FFFFFFF || up_tiles(q->n) * up_tiles(q->d) > 0x3FFFFFFF || up_tiles(q->d) * up_tiles(q->f) > 0x3FFFFFFF)
+    return "osscar_gated: the products of the sizes are too large for one call";
   if (!real_dtype(q->dtype)) return "osscar_gated: unknown dtype";
   if (q->act < OSSCAR_ACT_SILU || q->act > OSSCAR_ACT_RELU) return "osscar_gated: unknown activation";
   if (q->ldx < q->d || q->ldw < (q->rows_out ? q->d : q->f) || q->ldh < q->f) return "osscar_gated: leading dimension below the row length";
@@ -321,8 +332,6 @@ const char* bad_buffers(const osscar_gated_desc& q, const void* X, const void* W
   if ((uintptr_t)ws & 255) return "osscar_gated: the workspace must begin at a 256-byte boundary";
   return nullptr;
 }
-template <int NB>
-bool countable(const Product<NB>& p) { return tiles<Small1>(p) <= 0x3FFFFFFF; }
 
 // X Wg, X Wu with epilogue e
 template <int LAYOUT, int KIND, bool WIDE>
@@ -330,8 +339,8 @@ void thin_launch(const thin::Product<2>& p, const thin::Deal& d, const GatedOut&
   const dim3 grid(d.blocks, (unsigned)d.parts), block(thin::Wave<LAYOUT, KIND, 2, 1, WIDE>::WAVES * 64);
   if (p.M <= 16) hipLaunchKernelGGL((gated_thin_kernel<LAYOUT, KIND, 1, WIDE>), grid, block, 0, s, p, e);
   else hipLaunchKernelGGL((gated_thin_kernel<LAYOUT, KIND, 2, WIDE>), grid, block, 0, s, p, e);
-  const int64_t n = ((int64_t)p.M * p.N + 255) / 256;
-  if (d.parts > 1) hipLaunchKernelGGL(gated_join_kernel, dim3((unsigned)(n > 4096 ? 4096 : n)), dim3(256), 0, s, p, e);
+  if (d.parts > 1)
+    hipLaunchKernelGGL(gated_join_kernel, dim3(join_grid(p.M, p.N)), dim3(256), 0, s, reinterpret_cast<const float*>(p.sums), d.parts, p.M, p.N, e);
 }
 template <int KIND>
 void thin_projections(const thin::Product<2>& p, bool rows_out, const thin::Deal& d, const GatedOut& e, hipStream_t s) {
@@ -353,10 +362,9 @@ osscar_status projections(const osscar_gated_desc& q, const Buffers& b, const vo
   two.e[0] = e;
   p.M = (int)q.n; p.N = (int)q.f; p.k = (int)q.d;
   const Operand w[2] = {b.wg.operand(), b.wu.operand()};
-  add_segments(p, b.x.operand(), w, b.x.pieces);
-  if (!countable(p)) return refuse_call(OSSCAR_EINVAL, "osscar_gated: n times f is too large for one call");
-  if (q.rows_out) launch_product<OP_K, OP_K, Big2, Small2>(two, 1, s);
-  else launch_product<OP_K, OP_T, Big2, Small2>(two, 1, s);
+  add_segment(p, b.x.operand(), w);
+  if (q.rows_out) launch_product<OP_K, OP_K, Big2, Small2>(two, 1, e.f32, b.proj, b.sums, s);
+  else launch_product<OP_K, OP_T, Big2, Small2>(two, 1, e.f32, b.proj, b.sums, s);
   return OSSCAR_OK;
 }
 
@@ -381,7 +389,7 @@ extern "C" osscar_status osscar_gated_forward(const osscar_gated_desc* desc, con
   if (q.n == 0) return OSSCAR_OK;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   const int f32 = q.dtype == OSSCAR_F32;
-  if (!few(q)) { b.x.make(f32, s); b.wg.make(f32, s); b.wu.make(f32, s); }
+  if (!few(q)) { b.x.make(s); b.wg.make(s); b.wu.make(s); }
   const GatedOut e{H_dev, q.ldh, f32, q.act, G_dev, U_dev};
   const osscar_status st = projections(q, b, X_dev, Wg_dev, Wu_dev, e, s);
   return st != OSSCAR_OK ? st : launched("osscar_gated_forward");
@@ -403,37 +411,34 @@ extern "C" osscar_status osscar_gated_backward(const osscar_gated_desc* desc, co
   const Buffers b = buffers(c, q, X_dev, Wg_dev, Wu_dev, 1, G_dev != nullptr);
   if (c.used > workspace_bytes || (c.used > 0 && !workspace_dev)) return refuse_call(OSSCAR_ENOMEM, "osscar_gated_backward: workspace too small");
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
-  const int f32 = q.dtype == OSSCAR_F32, pieces = b.x.pieces;
-  const GradPlace place{b.dg, b.du, b.ldg, q.n * b.ldg, pieces};
+  const int f32 = q.dtype == OSSCAR_F32;
   if (q.n > 0) {
-    if (!G_dev || dWg_dev) b.x.make(f32, s);
-    if (!G_dev || dX_dev) { b.wg.make(f32, s); b.wu.make(f32, s); }
+    if (!G_dev || dWg_dev) b.x.make(s);
+    if (!G_dev || dX_dev) { b.wg.make(s); b.wu.make(s); }
     const float *G = G_dev, *U = U_dev;
     if (!G) {
       const osscar_status st = projections(q, b, X_dev, Wg_dev, Wu_dev, GatedOut{nullptr, 0, f32, q.act, b.g, b.u}, s);
       if (st != OSSCAR_OK) return st;
       G = b.g; U = b.u;
     }
-    hipLaunchKernelGGL(gated_grad_kernel, dim3(pieces_grid(q.n, b.ldg)), dim3(256), 0, s, dH_dev, q.ldh, f32, q.act, G, U, q.n, (int)q.f, place);
+    const dim3 grid(packs_grid(q.n, b.ldg));
+    if (f32) hipLaunchKernelGGL(gated_grad_kernel<true>, grid, dim3(256), 0, s, dH_dev, q.ldh, q.act, G, U, q.n, (int)q.f, b.dg, b.du, b.ldg);
+    else hipLaunchKernelGGL(gated_grad_kernel<false>, grid, dim3(256), 0, s, dH_dev, q.ldh, q.act, G, U, q.n, (int)q.f, b.dg, b.du, b.ldg);
   }
-  // dg and du as operands: n rows of ldg bf16, zeros past f
+  // dg and du as operands: n rows of ldg, zeros past f
   Operand dg{}, du{};
-  for (int t = 0; t < pieces; t++) {
-    dg.p[t] = reinterpret_cast<const char*>(b.dg + t * place.step);
-    du.p[t] = reinterpret_cast<const char*>(b.du + t * place.step);
-  }
-  dg.ldb = du.ldb = b.ldg * 2; dg.rows = du.rows = (int)q.n; dg.cols = du.cols = (int)b.ldg;
+  dg.p[0] = b.dg; du.p[0] = b.du;
+  dg.ldb = du.ldb = b.ldg * (f32 ? 4 : 2); dg.rows = du.rows = (int)q.n; dg.cols = du.cols = (int)b.ldg;
   if (dX_dev && q.n > 0) {
     Pair<1, PlainOut> two{};
     Product<1>& p = two.p[0];
     p.M = (int)q.n; p.N = (int)q.d; p.k = (int)q.f;
     const Operand wg[1] = {b.wg.operand()}, wu[1] = {b.wu.operand()};
-    add_segments(p, dg, wg, pieces);
-    add_segments(p, du, wu, pieces);
-    if (!countable(p)) return refuse_call(OSSCAR_EINVAL, "osscar_gated_backward: n times d is too large for one call");
-    two.e[0] = PlainOut{dX_dev, lddx, f32};
-    if (q.rows_out) launch_product<OP_K, OP_T, Big1, Small1>(two, 1, s);
-    else launch_product<OP_K, OP_K, Big1, Small1>(two, 1, s);
+    add_segment(p, dg, wg);
+    add_segment(p, du, wu);
+      two.e[0] = PlainOut{dX_dev, lddx, f32};
+    if (q.rows_out) launch_product<OP_K, OP_T, Big1, Small1>(two, 1, f32, b.dx, b.sums, s);
+    else launch_product<OP_K, OP_K, Big1, Small1>(two, 1, f32, b.dx, b.sums, s);
   }
   if (dWg_dev) {      // both weights in one launch
     Pair<1, PlainOut> two{};
@@ -441,13 +446,12 @@ extern "C" osscar_status osscar_gated_backward(const osscar_gated_desc* desc, co
     const Operand x = b.x.operand(), *dd[2] = {&dg, &du};
     for (int z = 0; z < 2; z++) {
       const Operand bs[1] = {q.rows_out ? x : *dd[z]};
-      add_segments(p[z], q.rows_out ? *dd[z] : x, bs, pieces);
+      add_segment(p[z], q.rows_out ? *dd[z] : x, bs);
       p[z].M = (int)(q.rows_out ? q.f : q.d); p[z].N = (int)(q.rows_out ? q.d : q.f); p[z].k = (int)q.n;
     }
-    if (!countable(p[0])) return refuse_call(OSSCAR_EINVAL, "osscar_gated_backward: d times f is too large for one call");
     two.e[0] = PlainOut{dWg_dev, lddw, dw_dtype == OSSCAR_F32};
     two.e[1] = PlainOut{dWu_dev, lddw, dw_dtype == OSSCAR_F32};
-    launch_product<OP_T, OP_T, Big1, Small1>(two, 2, s);
+    launch_product<OP_T, OP_T, Big1, Small1>(two, 2, f32, b.dw, b.sums, s);
   }
   return launched("osscar_gated_backward");
 }

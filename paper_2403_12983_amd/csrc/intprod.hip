@@ -119,9 +119,8 @@ struct IntOut {
     });
   }
 };
-typedef Shape<2, 2, 8, 8, 1> Big;        // 256 x 256, four waves
-typedef Shape<2, 2, 4, 4, 1> Small;      // 128 x 128, four waves
-constexpr int FILL = 192;
+typedef Shape<2, 2, 8, 8, 1, false> Big;        // 256 x 256, four waves
+typedef Shape<2, 2, 4, 4, 1, true> Small;      // 128 x 128, four waves
 
 template <class S>
 __global__ __launch_bounds__(S::WAVES * 64, 1) void int_product_kernel(const Product<1> p, const IntOut e) {
@@ -132,11 +131,14 @@ template <int RT, bool WIDE>
 __global__ __launch_bounds__((thin::Wave<OP_K, thin::I8, 1, RT, WIDE>::WAVES) * 64, 1) void int_thin_kernel(const thin::Product<1> p, const IntOut e) {
   thin::product<OP_K, thin::I8, 1, RT, WIDE>(p, e);
 }
-__global__ __launch_bounds__(256) void int_join_kernel(const thin::Product<1> p, const IntOut e) { thin::join<1, int>(p, e); }
+__global__ __launch_bounds__(256) void int_join_kernel(const int* __restrict__ sums, int parts, int M, int N, const IntOut e) {
+  tile::join<1>(sums, parts, M, N, e);
+}
 
 inline int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
 template <class S>
 int64_t tiles(int64_t n, int64_t m) { return (n + S::BM - 1) / S::BM * ((m + S::BN - 1) / S::BN); }
+Deal deal_of(int64_t n, int64_t d1, int64_t m) { return deal<Big, Small>(n, m, (d1 + STEP_BYTES - 1) / STEP_BYTES, 1, false); }
 bool bad_sizes(int64_t n, int64_t d1, int64_t m) { return !a_size(n, 0) || !a_size(m, 1) || d1 < 1 || d1 > OSSCAR_INT_MAX_DIM || tiles<Small>(n, m) > 0x3FFFFFFF; }
 bool bad_digits(const void* q, int64_t ldq, int64_t d1) { return !q || (uintptr_t)q % 16 || ldq % 16 || ldq < d1 || ldq > MAX_LD_BYTES; }
 
@@ -189,7 +191,7 @@ extern "C" size_t osscar_int_workspace_bytes(int64_t n, int64_t d1, int64_t m) {
   Carve c(nullptr);
   c.take((size_t)n * up16(d1));
   c.take((size_t)n * 4);
-  if (n <= thin::ROWS) c.take((size_t)thin::deal<OP_K, thin::I8>(n, m, d1).parts * n * m * 4);
+  c.take(n <= thin::ROWS ? (size_t)thin::deal<OP_K, thin::I8>(n, m, d1).parts * n * m * 4 : sums_bytes(deal_of(n, d1, m), 1, 1, n, m));
   return c.used + 256;
 }
 
@@ -239,15 +241,24 @@ extern "C" osscar_status osscar_int_product(const void* X_dev, int64_t n, int64_
     else if (n <= 16) hipLaunchKernelGGL((int_thin_kernel<1, false>), grid, block, 0, s, t, e);
     else if (d.wide) hipLaunchKernelGGL((int_thin_kernel<2, true>), grid, block, 0, s, t, e);
     else hipLaunchKernelGGL((int_thin_kernel<2, false>), grid, block, 0, s, t, e);
-    const int64_t g = (n * m + 255) / 256;
-    if (t.parts > 1) hipLaunchKernelGGL(int_join_kernel, dim3((unsigned)(g > 4096 ? 4096 : g)), dim3(256), 0, s, t, e);
+    if (t.parts > 1)
+      hipLaunchKernelGGL(int_join_kernel, dim3(join_grid(n, m)), dim3(256), 0, s, reinterpret_cast<const int*>(t.sums), t.parts, (int)n, (int)m, e);
     return launched("osscar_int_product");
   }
   Product<1> p{};
   p.a.p[0] = reinterpret_cast<const char*>(xq); p.a.ldb = ldxq; p.a.rows = (int)n; p.a.cols = (int)up16(d1);
   p.b[0].p[0] = reinterpret_cast<const char*>(Wq_dev); p.b[0].ldb = ldq; p.b[0].rows = (int)m; p.b[0].cols = (int)up16(d1);
   p.nseg = 1; p.k = (int)d1; p.M = (int)n; p.N = (int)m;
-  if (tiles<Big>(n, m) >= FILL) hipLaunchKernelGGL(int_product_kernel<Big>, dim3((unsigned)tiles<Big>(n, m)), dim3(Big::WAVES * 64), 0, s, p, e);
-  else hipLaunchKernelGGL(int_product_kernel<Small>, dim3((unsigned)tiles<Small>(n, m)), dim3(Small::WAVES * 64), 0, s, p, e);
+  const Deal d = deal_of(n, d1, m);
+  p.parts = d.parts;
+  if (d.parts > 1) {
+    p.sums = c.take(sums_bytes(d, 1, 1, n, m));
+    if (!workspace_dev || c.used > workspace_bytes) return refuse_call(OSSCAR_ENOMEM, "osscar_int_product: workspace too small");
+  }
+  const dim3 grid(d.tiles, 1, d.parts);
+  if (d.big) hipLaunchKernelGGL(int_product_kernel<Big>, grid, dim3(Big::WAVES * 64), 0, s, p, e);
+  else hipLaunchKernelGGL(int_product_kernel<Small>, grid, dim3(Small::WAVES * 64), 0, s, p, e);
+  if (d.parts > 1)
+    hipLaunchKernelGGL(int_join_kernel, dim3(join_grid(n, m)), dim3(256), 0, s, reinterpret_cast<const int*>(p.sums), d.parts, (int)n, (int)m, e);
   return launched("osscar_int_product");
 }

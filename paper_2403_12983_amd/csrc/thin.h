@@ -275,23 +275,6 @@ __device__ __forceinline__ void product(const Product<NB>& q, const Epi& epi) {
     }
   });
 }
-// Adds the parts' sums in order and goes on with them.
-template <int NB, class V, class Epi>
-__device__ __forceinline__ void join(const Product<NB>& q, const Epi& epi) {
-  const V* s = reinterpret_cast<const V*>(q.sums);
-  epi.one([&](auto put) {
-    for (int64_t j = blockIdx.x * (int64_t)256 + threadIdx.x; j < (int64_t)q.M * q.N; j += (int64_t)gridDim.x * 256) {
-      V v[NB];
-#pragma unroll
-      for (int z = 0; z < NB; z++) {
-        V t = 0;
-        for (int p = 0; p < q.parts; p++) t += s[((int64_t)p * NB + z) * q.M * q.N + j];
-        v[z] = t;
-      }
-      put((int)(j / q.N), (int)(j % q.N), v, q.N);
-    }
-  });
-}
 // How a product is dealt out: column blocks, wide or not, and parts of the contraction, enough for about two workgroups of four waves (OP_T) or half a
 // workgroup of eight (OP_K) per compute unit, each wave with at least two turns.
 struct Deal { unsigned blocks; int parts; bool wide; };

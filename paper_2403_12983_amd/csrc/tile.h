@@ -5,15 +5,13 @@
 // rows of the result side by side).  Both go from global memory straight into LDS in packets of 16 bytes.  OP_K operands are read
 // from there a packet per lane, OP_T operands through the transposing read of four 16-bit elements (ds_read_b64_tr_b16), so that no
 // pass over an operand is needed for any of the three products of a layer's forward and backward pass.
-// A segment is one pair of operands of the same shapes; several are summed: the two products of dX, and the six products of bf16 pieces that
-// make a float32 product (x = x1 + x2 + x3 of 8 bits each; all products of weight 2^-16 and more).
+// A segment is one pair of operands of the same shapes; two are summed for dX.
 //
 // Every packet is read through a buffer descriptor that ends where the operand ends, and a lane whose packet lies beyond the end of a
 // row gets an offset past that end: what is outside an operand reads as zero.  Rows and packets begin at 16-byte boundaries and the
 // contiguous length is a multiple of a packet; the callers copy operands of other alignments first.
 #pragma once
-#include <hip/hip_runtime.h>
-#include <stdint.h>
+#include "ops.h"
 
 namespace osscar {
 namespace tile {
@@ -25,7 +23,7 @@ typedef short v8s __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) void lds_void;
 
 enum { OP_K = 0, OP_T = 1 };
-constexpr int SEGS = 12;                        // two products of float32 operands
+constexpr int SEGS = 2;                         // the two products of dX
 constexpr int STEP_BYTES = 128;                 // contraction per stage and row: 64 bf16 or 128 int8, two matrix-core operands
 constexpr int64_t MAX_LD_BYTES = 1 << 22;       // 256 rows stay below the 2^30 bytes that an offset may take
 
@@ -74,8 +72,10 @@ __device__ __forceinline__ void sums_written() {
 
 // The shape of a workgroup: WM x WN waves, each of FM x (NB FN) tiles of 16 x 16.  NB: matrices on the B side whose columns a wave takes
 // alike (gate and up projection), FN tiles of each.
-template <int WM_, int WN_, int FM_, int FN_, int NB_>
+// CUT: its products may be dealt out in parts.
+template <int WM_, int WN_, int FM_, int FN_, int NB_, bool CUT_>
 struct Shape {
+  static constexpr bool CUT = CUT_;
   static constexpr int WM = WM_, WN = WN_, FM = FM_, FN = FN_, NB = NB_, WAVES = WM * WN, BM = WM * FM * 16, BN = WN * FN * 16;
 };
 
@@ -117,11 +117,11 @@ struct Side {
   // Where the requests of a stage begin, kept from stage to stage so that a new one costs few scalar instructions: a wave has no time to spare
   // for them between two matrix instructions.  OP_K: the corner of the segment, the stage's k is in the offsets; OP_T: the stage's row.
   struct Stage { const char* cur; int num; __amdgpu_buffer_rsrc_t rs; int v[NV]; };
-  __device__ __forceinline__ void place(const Operand& o, const char* p, int k, bool there, Stage& st) const {
+  __device__ __forceinline__ void place(const Operand& o, const char* p, int k, Stage& st) const {
     st.cur = p + (MODE == OP_K ? (int64_t)seg_row0 * o.ldb : (int64_t)k * o.ldb + (int64_t)seg_row0 * ES);
-    if (MODE == OP_K) {      // bytes from there to the end of the operand; zeros if there is no such segment
+    if (MODE == OP_K) {      // bytes from there to the end of the operand
       const int64_t left = (int64_t)(o.rows - seg_row0 - 1) * o.ldb + (int64_t)o.cols * ES;
-      st.num = !there || seg_row0 >= o.rows ? 0 : (left > 0x7FFFFFF0 ? 0x7FFFFFF0 : (int)left);
+      st.num = seg_row0 >= o.rows ? 0 : (left > 0x7FFFFFF0 ? 0x7FFFFFF0 : (int)left);
     }
   }
   __device__ __forceinline__ void advance(const Operand& o, Stage& st) const {
@@ -130,9 +130,9 @@ struct Side {
   __device__ __forceinline__ void prepare(const Operand& o, int k, bool there, Stage& st) const {
     if (MODE == OP_T) {      // rows of the stage that exist; columns that do not have offsets past any end
       const int n = o.rows - k;
-      st.num = !there || n <= 0 ? 0 : (n >= STEP_BYTES / ES ? 0x7FFFFFF0 : (n - 1) * (int)o.ldb + (o.cols - seg_row0) * ES);
+      st.num = n <= 0 ? 0 : (n >= STEP_BYTES / ES ? 0x7FFFFFF0 : (n - 1) * (int)o.ldb + (o.cols - seg_row0) * ES);
     }
-    st.rs = __builtin_amdgcn_make_buffer_rsrc((void*)st.cur, 0, st.num, 0x00020000);
+    st.rs = __builtin_amdgcn_make_buffer_rsrc((void*)st.cur, 0, there ? st.num : 0, 0x00020000);      // (zeros if there is no such stage)
 #pragma unroll
     for (int j = 0; j < NV; j++) st.v[j] = MODE == OP_T ? voff[j] : (k + vcol[MODE == OP_K ? j : 0] >= o.cols ? 0x7FFFFFF0 : voff[j] + k * ES);
   }
@@ -172,7 +172,36 @@ struct Product {
   Operand a, b[NB];
   int nseg, k;               // segments, contraction of each in elements
   int M, N;
+  int parts;                 // of the stages, a workgroup each (blockIdx.z), where the tiles alone do not fill the chip
+  void* sums;                // parts > 1: [part][matrix][m][n], 4 bytes each, for join()
 };
+__device__ __forceinline__ void put_sums(float* p, const float (&v)[8], int most) { put_f32(p, v, most); }
+__device__ __forceinline__ void put_sums(int* p, const int (&v)[8], int most) {
+  float f[8];
+#pragma unroll
+  for (int e = 0; e < 8; e++) f[e] = __int_as_float(v[e]);
+  put_f32(reinterpret_cast<float*>(p), f, most);
+}
+// Adds the parts' sums in order and goes on with them.  Epi::one(f) calls f(put) once, put(m, n, V (&v)[NB], N).
+template <int NB, class V, class Epi>
+__device__ __forceinline__ void join(const V* sums, int parts, int M, int N, const Epi& epi) {
+  epi.one([&](auto put) {
+    for (int64_t j = blockIdx.x * (int64_t)256 + threadIdx.x; j < (int64_t)M * N; j += (int64_t)gridDim.x * 256) {
+      V v[NB];
+#pragma unroll
+      for (int z = 0; z < NB; z++) {
+        V t = 0;
+        for (int p = 0; p < parts; p++) t += sums[((int64_t)p * NB + z) * M * N + j];
+        v[z] = t;
+      }
+      put((int)(j / N), (int)(j % N), v, N);
+    }
+  });
+}
+inline unsigned join_grid(int64_t M, int64_t N) {
+  const int64_t n = (M * N + 255) / 256;
+  return (unsigned)(n > 4096 ? 4096 : n);
+}
 
 // Workgroup b runs on XCD b % 8: every XCD gets a contiguous range of the tiles, which go down eight rows of tiles before the next column, so
 // that what an XCD works on together shares operands in its L2.
@@ -212,24 +241,26 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
       for (int j = 0; j < S::FN; j++)
 #pragma unroll
         for (int r = 0; r < 4; r++) acc[i][z][j][r] = 0;
-  const int per = (q.k + KS - 1) / KS, total = per * q.nseg;      // stages of a segment, of all
+  const int parts = S::CUT ? q.parts : 1;
+  const int per = (q.k + KS - 1) / KS, all = per * q.nseg, span = (all + parts - 1) / parts;      // stages of a segment, of all, of a part
+  const int begin = S::CUT ? min(all, (int)blockIdx.z * span) : 0, total = min(all - begin, span);
   // Workgroups begin at stages of their own, so that rows whose distance is a power of two do not all ask one memory channel at a time (contraction 2048: 7 %;
   // int8, 14336: 5 %).
-  const int k0 = (per > 0 ? (tm + tn) % per : 0) * KS;
-  int seg = 0, k = k0;      // of the stage that is prepared
-  bool there = true;
+  const int k0 = per > 0 && parts == 1 ? (tm + tn) % per * KS : 0;
+  int seg = per > 0 ? begin / per : 0, k = per > 0 && parts > 1 ? begin % per * KS : k0;      // of the stage that is prepared
+  int left = total;                                                                             // stages from there on
   constexpr int NL = SA::NJ + S::NB * SB::NJ;      // loads of a wave per stage
   typename SA::Stage qa;
   typename SB::Stage qb[S::NB];
   auto place = [&]() {
-    there = seg < q.nseg;
-    const int at = there ? seg : 0;
-    sa.place(q.a, q.a.p[at], k, there, qa);
+    const int at = seg < q.nseg ? seg : 0;
+    sa.place(q.a, q.a.p[at], k, qa);
 #pragma unroll
-    for (int z = 0; z < S::NB; z++) sb.place(q.b[0], q.b[z].p[at], k, there, qb[z]);
+    for (int z = 0; z < S::NB; z++) sb.place(q.b[0], q.b[z].p[at], k, qb[z]);
   };
   auto step = [&]() {      // to the next stage
     bool anew = false;
+    left--;
     k += KS;
     if (k >= q.k) { k = 0; anew = true; }
     if (k == k0) { seg++; anew = true; }
@@ -239,8 +270,8 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
     for (int z = 0; z < S::NB; z++) sb.advance(q.b[0], qb[z]);
   };
   auto prepare = [&](int part) {      // 0: A, 1 + z: B
-    if (part == 0) sa.prepare(q.a, k, there, qa);
-    else sb.prepare(q.b[0], k, there, qb[part - 1]);
+    if (part == 0) sa.prepare(q.a, k, left > 0, qa);
+    else sb.prepare(q.b[0], k, left > 0, qb[part - 1]);
   };
   auto request = [&](int l, char* a, char (*b)[SB::BYTES]) {      // load l < NL of a stage
     if (l < SA::NJ) sa.load(q.a, qa, l, a, wave);
@@ -301,7 +332,7 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
 #undef OSSCAR_TILE_STAGE
   sums_written();
   const int i = lane & 15, g = lane >> 4;
-  epi.each([&](auto put) {
+  auto each = [&](auto put) {
 #pragma unroll
     for (int f = 0; f < S::FM; f++) {
       const int m = tm * S::BM + (wm * S::FM + f) * 16 + i;
@@ -316,8 +347,32 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
         if (m < q.M && n < q.N) put(m, n, v, q.N);
       }
     }
-  });
+  };
+  if (parts == 1) {
+    epi.each(each);
+  } else {
+    typename T::val* sums = reinterpret_cast<typename T::val*>(q.sums) + (int64_t)blockIdx.z * S::NB * q.M * q.N;
+    each([&](int m, int n, const typename T::val (&v)[S::NB][8], int N) {
+#pragma unroll
+      for (int z = 0; z < S::NB; z++) put_sums(sums + ((int64_t)z * q.M + m) * N + n, v[z], N - n);
+    });
+  }
 }
+
+// How a product is dealt out: the big shape where its tiles fill three quarters of the compute units, else the small one, the contraction cut into parts
+// where its tiles are fewer than two per compute unit, each of at least eight stages.
+constexpr int FILL = 192;
+struct Deal { bool big; int parts; unsigned tiles; };
+template <class SB, class SS>
+Deal deal(int64_t M, int64_t N, int64_t stages, int count, bool never_big) {
+  const int64_t big = (M + SB::BM - 1) / SB::BM * ((N + SB::BN - 1) / SB::BN), small = (M + SS::BM - 1) / SS::BM * ((N + SS::BN - 1) / SS::BN);
+  if (!never_big && big * count >= FILL) return Deal{true, 1, (unsigned)big};
+  int64_t parts = 512 / (small * count);
+  if (parts > stages / 8) parts = stages / 8;
+  if (parts > 32) parts = 32;
+  return Deal{false, parts < 1 ? 1 : (int)parts, (unsigned)small};
+}
+inline size_t sums_bytes(const Deal& d, int nb, int count, int64_t M, int64_t N) { return d.parts > 1 ? (size_t)d.parts * nb * count * M * N * 4 : 0; }
 
 }  // namespace tile
 }  // namespace osscar
