@@ -68,23 +68,25 @@ __device__ __forceinline__ void with_act(int act, F f) {
 }
 
 // ---- copies ----------------------------------------------------------------------------------
-// A bf16 matrix with rows of `ld` (a multiple of eight), zeros past cols.  Eight columns per thread; bound by its reads and writes.
-__global__ __launch_bounds__(256) void gated_copy_kernel(const uint16_t* __restrict__ src, int64_t rows, int cols, int64_t lds_, uint16_t* __restrict__ dst, int64_t ld) {
-  const int packs = (int)(ld / 8);
-  for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < rows * packs; i += (int64_t)gridDim.x * 256) {
+// Up to three bf16 matrices (blockIdx.y) with rows of `ld` (a multiple of eight), zeros past cols.  Eight columns per thread; bound by its reads and writes.
+struct Copies { struct { const uint16_t* src; int64_t rows, lds; int cols; uint16_t* dst; int64_t ld; } m[3]; };
+__global__ __launch_bounds__(256) void gated_copy_kernel(const Copies q) {
+  const auto& m = q.m[blockIdx.y];
+  const int packs = (int)(m.ld / 8);
+  for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < m.rows * packs; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / packs;
     const int c = (int)(i - r * packs) * 8;
     u16x8 w;
-    if (c + 8 <= cols) {
-      w = *reinterpret_cast<const u16x8_any*>(src + r * lds_ + c);
+    if (c + 8 <= m.cols) {
+      w = *reinterpret_cast<const u16x8_any*>(m.src + r * m.lds + c);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; e++) {
         w[e] = 0;
-        if (c + e < cols) w[e] = src[r * lds_ + c + e];
+        if (c + e < m.cols) w[e] = m.src[r * m.lds + c + e];
       }
     }
-    *reinterpret_cast<u16x8*>(dst + r * ld + c) = w;
+    *reinterpret_cast<u16x8*>(m.dst + r * m.ld + c) = w;
   }
 }
 
@@ -237,12 +239,23 @@ struct Source {
     o.ldb = (copied ? up8(cols) : ld) * es; o.rows = (int)rows; o.cols = (int)(copied ? up8(cols) : cols);
     return o;
   }
-  void make(hipStream_t s) const {
-    if (copied && rows > 0)
-      hipLaunchKernelGGL(gated_copy_kernel, dim3(packs_grid(rows, up8(cols))), dim3(256), 0, s, reinterpret_cast<const uint16_t*>(p), rows, (int)cols, ld,
-                         reinterpret_cast<uint16_t*>(at), up8(cols));
-  }
 };
+// Makes the copies that these need, in one launch.
+void make_copies(const Source* const (&from)[3], hipStream_t s) {
+  Copies q{};
+  int n = 0;
+  unsigned grid = 1;
+  for (const Source* f : from)
+    if (f && f->copied && f->rows > 0) {
+      const int64_t ld = up8(f->cols);
+      q.m[n].src = reinterpret_cast<const uint16_t*>(f->p); q.m[n].rows = f->rows; q.m[n].lds = f->ld; q.m[n].cols = (int)f->cols;
+      q.m[n].dst = reinterpret_cast<uint16_t*>(f->at); q.m[n].ld = ld;
+      const unsigned need = packs_grid(f->rows, ld);
+      grid = grid > need ? grid : need;
+      n++;
+    }
+  if (n > 0) hipLaunchKernelGGL(gated_copy_kernel, dim3(grid, n), dim3(256), 0, s, q);
+}
 // `loose`: some buffer of the call does not begin at a 16-byte boundary
 Source source(Carve& c, const void* p, int64_t rows, int64_t cols, int64_t ld, int32_t dtype, bool loose) {
   Source s{p, rows, cols, ld, dtype == OSSCAR_F32 ? 4 : 2, false, nullptr};
@@ -269,15 +282,15 @@ struct Buffers {
   Deal proj, dx, dw;
   char* sums;            // of parts, one product after the other
 };
-bool few(const osscar_gated_desc& q) { return q.n <= thin::ROWS; }
+// The products of few rows (thin.h says where)
+bool few(const osscar_gated_desc& q) { return q.dtype == OSSCAR_F32 ? q.n <= 32 : q.rows_out && q.n <= 16 && q.d * q.f <= (1 << 24); }
 Buffers buffers(Carve& c, const osscar_gated_desc& q, const void* X, const void* Wg, const void* Wu, int backward, bool kept) {
   Buffers b{};
   const bool f32 = q.dtype == OSSCAR_F32;
   const int ks = f32 ? split::KS : STEP_BYTES / 2;
   size_t sums = 0;
   if (!kept && few(q)) {
-    b.few = q.rows_out ? (f32 ? thin::deal<OP_K, thin::F32>(q.n, q.f, q.d) : thin::deal<OP_K, thin::BF16>(q.n, q.f, q.d))
-                       : (f32 ? thin::deal<OP_T, thin::F32>(q.n, q.f, q.d) : thin::deal<OP_T, thin::BF16>(q.n, q.f, q.d));
+    b.few = !f32 ? thin::deal<OP_K, thin::BF16>(q.n, q.f, q.d) : q.rows_out ? thin::deal<OP_K, thin::F32>(q.n, q.f, q.d) : thin::deal<OP_T, thin::F32>(q.n, q.f, q.d);
     if (b.few.parts > 1) sums = (size_t)b.few.parts * 2 * q.n * q.f * 4;
   } else if (!kept) {
     b.proj = deal<Big2, Small2>(q.n, q.f, (q.d + ks - 1) / ks, 1, f32);
@@ -333,28 +346,26 @@ const char* bad_buffers(const osscar_gated_desc& q, const void* X, const void* W
   return nullptr;
 }
 
-// X Wg, X Wu with epilogue e
-template <int LAYOUT, int KIND, bool WIDE>
+template <int LAYOUT, int KIND, int RT, bool WIDE>
 void thin_launch(const thin::Product<2>& p, const thin::Deal& d, const GatedOut& e, hipStream_t s) {
-  const dim3 grid(d.blocks, (unsigned)d.parts), block(thin::Wave<LAYOUT, KIND, 2, 1, WIDE>::WAVES * 64);
-  if (p.M <= 16) hipLaunchKernelGGL((gated_thin_kernel<LAYOUT, KIND, 1, WIDE>), grid, block, 0, s, p, e);
-  else hipLaunchKernelGGL((gated_thin_kernel<LAYOUT, KIND, 2, WIDE>), grid, block, 0, s, p, e);
+  hipLaunchKernelGGL((gated_thin_kernel<LAYOUT, KIND, RT, WIDE>), dim3(d.blocks, (unsigned)d.parts), dim3(thin::Wave<LAYOUT, KIND, 2, RT, WIDE>::WAVES * 64), 0, s, p, e);
+}
+void thin_projections(const thin::Product<2>& p, bool f32, bool rows_out, const thin::Deal& d, const GatedOut& e, hipStream_t s) {
+  const bool one = p.M <= 16;
+  if (!f32) thin_launch<OP_K, thin::BF16, 1, false>(p, d, e, s);
+  else if (!rows_out) one ? thin_launch<OP_T, thin::F32, 1, false>(p, d, e, s) : thin_launch<OP_T, thin::F32, 2, false>(p, d, e, s);
+  else if (d.wide) one ? thin_launch<OP_K, thin::F32, 1, true>(p, d, e, s) : thin_launch<OP_K, thin::F32, 2, true>(p, d, e, s);
+  else one ? thin_launch<OP_K, thin::F32, 1, false>(p, d, e, s) : thin_launch<OP_K, thin::F32, 2, false>(p, d, e, s);
   if (d.parts > 1)
     hipLaunchKernelGGL(gated_join_kernel, dim3(join_grid(p.M, p.N)), dim3(256), 0, s, reinterpret_cast<const float*>(p.sums), d.parts, p.M, p.N, e);
 }
-template <int KIND>
-void thin_projections(const thin::Product<2>& p, bool rows_out, const thin::Deal& d, const GatedOut& e, hipStream_t s) {
-  if (!rows_out) thin_launch<OP_T, KIND, false>(p, d, e, s);
-  else if (d.wide) thin_launch<OP_K, KIND, true>(p, d, e, s);
-  else thin_launch<OP_K, KIND, false>(p, d, e, s);
-}
+// X Wg, X Wu with epilogue e
 osscar_status projections(const osscar_gated_desc& q, const Buffers& b, const void* X, const void* Wg, const void* Wu, const GatedOut& e, hipStream_t s) {
   if (few(q)) {
     const int es = q.dtype == OSSCAR_F32 ? 4 : 2;
     const thin::Product<2> p{reinterpret_cast<const char*>(X), {reinterpret_cast<const char*>(Wg), reinterpret_cast<const char*>(Wu)}, q.ldx * es, q.ldw * es,
                              (int)q.n, (int)q.f, (int)q.d, b.few.parts, b.sums};
-    if (q.dtype == OSSCAR_F32) thin_projections<thin::F32>(p, q.rows_out != 0, b.few, e, s);
-    else thin_projections<thin::BF16>(p, q.rows_out != 0, b.few, e, s);
+    thin_projections(p, q.dtype == OSSCAR_F32, q.rows_out != 0, b.few, e, s);
     return OSSCAR_OK;
   }
   Pair<2, GatedOut> two{};
@@ -389,7 +400,7 @@ extern "C" osscar_status osscar_gated_forward(const osscar_gated_desc* desc, con
   if (q.n == 0) return OSSCAR_OK;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   const int f32 = q.dtype == OSSCAR_F32;
-  if (!few(q)) { b.x.make(s); b.wg.make(s); b.wu.make(s); }
+  if (!few(q)) make_copies({&b.x, &b.wg, &b.wu}, s);
   const GatedOut e{H_dev, q.ldh, f32, q.act, G_dev, U_dev};
   const osscar_status st = projections(q, b, X_dev, Wg_dev, Wu_dev, e, s);
   return st != OSSCAR_OK ? st : launched("osscar_gated_forward");
@@ -413,8 +424,8 @@ extern "C" osscar_status osscar_gated_backward(const osscar_gated_desc* desc, co
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   const int f32 = q.dtype == OSSCAR_F32;
   if (q.n > 0) {
-    if (!G_dev || dWg_dev) b.x.make(s);
-    if (!G_dev || dX_dev) { b.wg.make(s); b.wu.make(s); }
+    const bool x = !G_dev || dWg_dev, w = !G_dev || dX_dev;
+    make_copies({x ? &b.x : nullptr, w ? &b.wg : nullptr, w ? &b.wu : nullptr}, s);
     const float *G = G_dev, *U = U_dev;
     if (!G) {
       const osscar_status st = projections(q, b, X_dev, Wg_dev, Wu_dev, GatedOut{nullptr, 0, f32, q.act, b.g, b.u}, s);

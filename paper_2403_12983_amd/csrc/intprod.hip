@@ -127,9 +127,9 @@ __global__ __launch_bounds__(S::WAVES * 64, 1) void int_product_kernel(const Pro
   product_tile<true, OP_K, OP_K, S>(p, e);
 }
 
-template <int RT, bool WIDE>
-__global__ __launch_bounds__((thin::Wave<OP_K, thin::I8, 1, RT, WIDE>::WAVES) * 64, 1) void int_thin_kernel(const thin::Product<1> p, const IntOut e) {
-  thin::product<OP_K, thin::I8, 1, RT, WIDE>(p, e);
+template <bool WIDE>
+__global__ __launch_bounds__((thin::Wave<OP_K, thin::I8, 1, 1, WIDE>::WAVES) * 64, 1) void int_thin_kernel(const thin::Product<1> p, const IntOut e) {
+  thin::product<OP_K, thin::I8, 1, 1, WIDE>(p, e);
 }
 __global__ __launch_bounds__(256) void int_join_kernel(const int* __restrict__ sums, int parts, int M, int N, const IntOut e) {
   tile::join<1>(sums, parts, M, N, e);
@@ -139,6 +139,7 @@ inline int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
 template <class S>
 int64_t tiles(int64_t n, int64_t m) { return (n + S::BM - 1) / S::BM * ((m + S::BN - 1) / S::BN); }
 Deal deal_of(int64_t n, int64_t d1, int64_t m) { return deal<Big, Small>(n, m, (d1 + STEP_BYTES - 1) / STEP_BYTES, 1, false); }
+bool few_rows(int64_t n) { return n <= 16; }      // (thin.h says why)
 bool bad_sizes(int64_t n, int64_t d1, int64_t m) { return !a_size(n, 0) || !a_size(m, 1) || d1 < 1 || d1 > OSSCAR_INT_MAX_DIM || tiles<Small>(n, m) > 0x3FFFFFFF; }
 bool bad_digits(const void* q, int64_t ldq, int64_t d1) { return !q || (uintptr_t)q % 16 || ldq % 16 || ldq < d1 || ldq > MAX_LD_BYTES; }
 
@@ -191,7 +192,7 @@ extern "C" size_t osscar_int_workspace_bytes(int64_t n, int64_t d1, int64_t m) {
   Carve c(nullptr);
   c.take((size_t)n * up16(d1));
   c.take((size_t)n * 4);
-  c.take(n <= thin::ROWS ? (size_t)thin::deal<OP_K, thin::I8>(n, m, d1).parts * n * m * 4 : sums_bytes(deal_of(n, d1, m), 1, 1, n, m));
+  c.take(few_rows(n) ? (size_t)thin::deal<OP_K, thin::I8>(n, m, d1).parts * n * m * 4 : sums_bytes(deal_of(n, d1, m), 1, 1, n, m));
   return c.used + 256;
 }
 
@@ -212,7 +213,7 @@ extern "C" osscar_status osscar_int_product(const void* X_dev, int64_t n, int64_
   const int8_t* xq = reinterpret_cast<const int8_t*>(X_dev);
   const float* xs = x_scale_dev;
   int64_t ldxq = ldx;
-  const bool few = n <= thin::ROWS;
+  const bool few = few_rows(n);
   Carve c(workspace_dev);
   if (!given || (!few && !operand_fits(X_dev, ldx, d1, 1))) {
     ldxq = up16(d1);
@@ -237,10 +238,8 @@ extern "C" osscar_status osscar_int_product(const void* X_dev, int64_t n, int64_
       if (!workspace_dev || c.used > workspace_bytes) return refuse_call(OSSCAR_ENOMEM, "osscar_int_product: workspace too small");
     }
     const dim3 grid(d.blocks, (unsigned)d.parts), block(512);
-    if (n <= 16 && d.wide) hipLaunchKernelGGL((int_thin_kernel<1, true>), grid, block, 0, s, t, e);
-    else if (n <= 16) hipLaunchKernelGGL((int_thin_kernel<1, false>), grid, block, 0, s, t, e);
-    else if (d.wide) hipLaunchKernelGGL((int_thin_kernel<2, true>), grid, block, 0, s, t, e);
-    else hipLaunchKernelGGL((int_thin_kernel<2, false>), grid, block, 0, s, t, e);
+    if (d.wide) hipLaunchKernelGGL(int_thin_kernel<true>, grid, block, 0, s, t, e);
+    else hipLaunchKernelGGL(int_thin_kernel<false>, grid, block, 0, s, t, e);
     if (t.parts > 1)
       hipLaunchKernelGGL(int_join_kernel, dim3(join_grid(n, m)), dim3(256), 0, s, reinterpret_cast<const int*>(t.sums), t.parts, (int)n, (int)m, e);
     return launched("osscar_int_product");

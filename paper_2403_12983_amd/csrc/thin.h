@@ -2,10 +2,11 @@
 // so B goes from memory to registers and from there to the matrix core, past LDS: no barrier stands between a wave's loads, and any alignment will do.
 //
 // OP_K (a column's elements side by side): a workgroup takes 16 columns, its waves take the contraction in turns of four matrix-core operands.
-// OP_T (a row of B, one k, side by side): a wave takes 64 columns; lane l reads four neighbouring columns of the eight (float32: four) rows k that the
-// matrix core wants of its lane group and turns the block over in registers, half an instruction per element, so that tile j of the wave is columns
-// 4 i + j.  The waves of a workgroup take the contraction in turns; where the column blocks do not fill the chip, it is also cut into parts of a
+// OP_T (a row of B, one k, side by side; float32): a wave takes 64 columns.  The waves of a workgroup take the contraction in turns; where the column blocks do not fill the chip, it is also cut into parts of a
 // workgroup each, whose sums a second launch adds in order.
+// Taken where it beats the tiles, which read B as fast from 64 or 128 of their rows used (both sides measured): float32 up to 32 rows (the float32 instruction
+// has no pieces to make; 7168 x 14336, 16 rows 152 us, 33 rows in tiles 375), bf16 OP_K up to 16 rows of small matrices (2048 x 5461 13 us, tiles in two launches 15;
+// 7168 x 14336 82 and 75), int8 up to 16 rows (14336 x 7168 21 and 26; 24 rows 27 and 27).
 #pragma once
 #include "ops.h"
 #include "tile.h"
@@ -19,7 +20,6 @@ using tile::v4f;
 using tile::v4i;
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 
-constexpr int ROWS = 32;           // rows of A, at most
 constexpr int WIDE_FROM = 6144;    // columns from which on 32 of them a workgroup fill three quarters of the compute units
 enum { BF16 = 0, F32 = 1, I8 = 2 };
 
@@ -72,7 +72,7 @@ struct Product {
   void* sums;                // parts > 1: [part][matrix][m][n], 4 bytes each
 };
 
-// WIDE: OP_K with 32 columns a wave and turns of two operands, so that the rows of A are read half as often (7168 x 14336, 16 rows: 109 us without);
+// WIDE: OP_K with 32 columns a wave and turns of two operands, so that the rows of A are read half as often (14336 x 7168 int8, 16 rows: 28 us without, 23 with);
 // taken where the chip is full with it.
 template <int LAYOUT, int KIND, int NB, int RT, bool WIDE> struct Wave;
 // OP_K
@@ -130,54 +130,50 @@ struct Wave<OP_K, KIND, NB, RT, WIDE> {
           for (int r = 0; r < RT; r++) T::mma(w.b[z][t][u], w.a[r][u], acc[r][z][t]);
   }
 };
-// OP_T: four columns of E rows k per lane (64 columns a wave: a memory line of bf16; with eight per lane the sums of two row tiles do not fit the registers)
-template <int KIND, int NB, int RT>
-struct Wave<OP_T, KIND, NB, RT, false> {
-  typedef Num<KIND> T;
-  typedef typename T::el el;
-  static constexpr int E = T::ELEMS, WIDTH = 4, DWORDS = WIDTH * sizeof(el) / 4, COLS = 16 * WIDTH, TILES = WIDTH, WAVES = 4, TURN = T::STEP;
-  typedef int vec __attribute__((ext_vector_type(DWORDS)));
-  typedef vec vec_any __attribute__((aligned(1)));
-  static __device__ __forceinline__ int column(int t, int i) { return i * WIDTH + t; }
+// OP_T (float32): four columns of four rows k per lane, 64 columns a wave; the instruction that contracts k = 4 g + e of tile t takes column t of row e
+// as it is.
+template <int NB, int RT>
+struct Wave<OP_T, F32, NB, RT, false> {
+  typedef Num<F32> T;
+  static constexpr int E = 4, COLS = 64, TILES = 4, WAVES = 4, TURN = T::STEP;
+  static __device__ __forceinline__ int column(int t, int i) { return i * 4 + t; }
   const char *cb[NB], *ra[RT];
   int koff, left;      // columns of the lane's packet that exist
   __device__ __forceinline__ void open(const Product<NB>& q, int n0, int lane) {
-    const int i = lane & 15, n = n0 + i * WIDTH;
+    const int i = lane & 15, n = n0 + i * 4;
     koff = (lane >> 4) * E;
-    left = min(WIDTH, q.N - n);
+    left = min(4, q.N - n);
 #pragma unroll
-    for (int z = 0; z < NB; z++) cb[z] = q.b[z] + (int64_t)min(n, q.N - 1) * sizeof(el);
+    for (int z = 0; z < NB; z++) cb[z] = q.b[z] + (int64_t)min(n, q.N - 1) * 4;
 #pragma unroll
     for (int r = 0; r < RT; r++) ra[r] = q.a + (int64_t)min(r * 16 + i, q.M - 1) * q.lda;
   }
-  struct Regs { vec b[NB][E]; v4i a[RT]; };
+  struct Regs { v4i b[NB][E], a[RT]; };
   __device__ __forceinline__ void load(const Product<NB>& q, int k0, Regs& w) const {
     const int k = k0 + koff;
     if (k0 + TURN <= q.K) {
 #pragma unroll
-      for (int r = 0; r < RT; r++) w.a[r] = *reinterpret_cast<const v4i_any*>(ra[r] + (int64_t)k * sizeof(el));
+      for (int r = 0; r < RT; r++) w.a[r] = *reinterpret_cast<const v4i_any*>(ra[r] + (int64_t)k * 4);
     } else {
 #pragma unroll
-      for (int r = 0; r < RT; r++) w.a[r] = packet<KIND>(ra[r], k, q.K);
+      for (int r = 0; r < RT; r++) w.a[r] = packet<F32>(ra[r], k, q.K);
     }
-    if (k0 + TURN <= q.K && left == WIDTH) {
+    if (k0 + TURN <= q.K && left == 4) {
 #pragma unroll
       for (int z = 0; z < NB; z++)
 #pragma unroll
-        for (int e = 0; e < E; e++) w.b[z][e] = *reinterpret_cast<const vec_any*>(cb[z] + (int64_t)(k + e) * q.ldb);
+        for (int e = 0; e < E; e++) w.b[z][e] = *reinterpret_cast<const v4i_any*>(cb[z] + (int64_t)(k + e) * q.ldb);
     } else {
 #pragma unroll
       for (int z = 0; z < NB; z++)
 #pragma unroll
         for (int e = 0; e < E; e++) {
-          const el* p = reinterpret_cast<const el*>(cb[z] + (int64_t)min(k + e, q.K - 1) * q.ldb);
-          el x[WIDTH];
+          const int* p = reinterpret_cast<const int*>(cb[z] + (int64_t)min(k + e, q.K - 1) * q.ldb);
 #pragma unroll
-          for (int c = 0; c < WIDTH; c++) {
-            x[c] = 0;
-            if (c < left && k + e < q.K) x[c] = p[c];
+          for (int c = 0; c < 4; c++) {
+            w.b[z][e][c] = 0;
+            if (c < left && k + e < q.K) w.b[z][e][c] = p[c];
           }
-          w.b[z][e] = __builtin_bit_cast(vec, x);
         }
     }
   }
@@ -186,12 +182,7 @@ struct Wave<OP_T, KIND, NB, RT, false> {
     for (int z = 0; z < NB; z++)
 #pragma unroll
       for (int t = 0; t < TILES; t++) {
-        v4i b;
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-          if (KIND == F32) b[e] = w.b[z][e][t % DWORDS];
-          else b[e] = (int)__builtin_amdgcn_perm((unsigned)w.b[z][(2 * e + 1) % E][(t / 2) % DWORDS], (unsigned)w.b[z][(2 * e) % E][(t / 2) % DWORDS], t & 1 ? 0x07060302u : 0x05040100u);
-        }
+        const v4i b{w.b[z][0][t], w.b[z][1][t], w.b[z][2][t], w.b[z][3][t]};
 #pragma unroll
         for (int r = 0; r < RT; r++) T::mma(b, w.a[r], acc[r][z][t]);
       }
@@ -281,7 +272,7 @@ struct Deal { unsigned blocks; int parts; bool wide; };
 template <int LAYOUT, int KIND>
 Deal deal(int64_t M, int64_t N, int64_t K) {
   typedef Wave<LAYOUT, KIND, 1, 1, false> W;
-  Deal d{(unsigned)((N + W::COLS - 1) / W::COLS), 1, LAYOUT == OP_K && M > 1 && N >= WIDE_FROM};
+  Deal d{(unsigned)((N + W::COLS - 1) / W::COLS), 1, LAYOUT == OP_K && KIND != BF16 && M > 1 && N >= WIDE_FROM};
   if (d.wide) { d.blocks = (unsigned)((N + 31) / 32); return d; }
   const int64_t turns = (K + W::TURN - 1) / W::TURN, want = LAYOUT == OP_K ? 128 : 512, most = turns / (W::WAVES * 2);
   int64_t parts = want / d.blocks;
