@@ -50,7 +50,7 @@ __device__ __forceinline__ void act_slope(float g, float& a, float& da) {
   } else if (ACT == OSSCAR_ACT_GELU_TANH) {
     const float s = logistic(TWO_ROOT_2_PI * (g + 0.044715f * g * g * g));
     a = g * s;
-    da = s + a * (1.f - s) * TWO_ROOT_2_PI * (1.f + 3.f * 0.044715f * g * g);
+    da = s + a * (1.f - s) * TWO_ROOT_2_PI * (1.f + 3.f * 0.044715f * fminf(g * g, 1e30f));      // (no infinity to multiply the 0 with)
   } else {
     a = act_value<OSSCAR_ACT_RELU>(g);
     da = g > 0.f ? 1.f : (g == g ? 0.f : g);

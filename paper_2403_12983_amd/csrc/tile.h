@@ -367,6 +367,7 @@ template <class SB, class SS>
 Deal deal(int64_t M, int64_t N, int64_t stages, int count, bool never_big) {
   const int64_t big = (M + SB::BM - 1) / SB::BM * ((N + SB::BN - 1) / SB::BN), small = (M + SS::BM - 1) / SS::BM * ((N + SS::BN - 1) / SS::BN);
   if (!never_big && big * count >= FILL) return Deal{true, 1, (unsigned)big};
+  if (small == 0) return Deal{false, 1, 0};
   int64_t parts = 512 / (small * count);
   if (parts > stages / 8) parts = stages / 8;
   if (parts > 32) parts = 32;

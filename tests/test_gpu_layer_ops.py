@@ -1,0 +1,569 @@
+"""Gated feed-forward, 8-bit integer products and log probabilities against plain float64 implementations of their definitions.
+
+Tolerances.  u = 2^-8 is the largest relative error of rounding to bf16's eight bits, e = 2^-24 that of float32's 24.  A float32 sum of K products is off by a random walk of
+about e sqrt(K) of its size; the tests allow e (4 + 2 sqrt(K)) in the 2-norm.  A bf16 result adds u of itself, elementwise, and
+what is rounded to bf16 between two products (dg, du) adds u of the sum of the absolute products, elementwise."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U, E = 2.0 ** -8, 2.0 ** -24
+ACTS = ("SILU", "GELU", "GELU_TANH", "RELU")
+
+
+@pytest.fixture(scope="module")
+def osscar():
+    import paper_2403_12983_amd as pkg
+    pkg.load_library()
+    return pkg
+
+
+def _act(pkg, name):
+    return getattr(pkg, "OSSCAR_ACT_" + name)
+
+
+def _gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def _randn(g, *shape, scale=1.0, dtype=torch.float32):
+    return (torch.randn(*shape, generator=g, device=DEV) * scale).to(dtype)
+
+
+def _act64(g, name):
+    """value and slope"""
+    if name == "SILU":
+        s = torch.sigmoid(g)
+        return g * s, s * (1 + g * (1 - s))
+    if name == "GELU":
+        c = 0.5 * torch.special.erfc(-g / math.sqrt(2))
+        return g * c, c + g * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+    if name == "GELU_TANH":
+        a = math.sqrt(2 / math.pi)
+        t = torch.tanh(a * (g + 0.044715 * g ** 3))
+        return 0.5 * g * (1 + t), 0.5 * (1 + t) + 0.5 * g * (1 - t * t) * a * (1 + 3 * 0.044715 * g * g)
+    return torch.clamp_min(g, 0), (g > 0).double()
+
+
+def _near(got, want, size, rounding, K, what):
+    """|got - want| <= rounding (of the result) elementwise + a random walk over K products of absolute sum `size`, in the 2-norm over rows"""
+    got, want = got.double(), want.double()
+    assert torch.equal(torch.isfinite(got), torch.isfinite(want)), what
+    err = (got - want).abs()
+    walk = E * (4 + 2 * math.sqrt(K))
+    excess = torch.clamp_min(err - rounding, 0)
+    assert torch.linalg.norm(excess).item() <= walk * torch.linalg.norm(size).item() + 1e-30, (what, torch.linalg.norm(excess).item(), walk * torch.linalg.norm(size).item())
+    assert excess.max().item() <= 8 * walk * size.max().item() + 1e-30, what      # no single element stands out
+
+
+def _weights(g, d, f, dtype, rows):
+    w = [_randn(g, *((f, d) if rows == "out" else (d, f)), scale=1.2 / math.sqrt(d), dtype=dtype) for _ in range(2)]
+    return [x.t() for x in w] if rows == "out" else w
+
+
+def _forward64(X, Wg, Wu, name):
+    X, Wg, Wu = X.double(), Wg.double().contiguous(), Wu.double().contiguous()
+    g, u = X @ Wg, X @ Wu
+    a, da = _act64(g, name)
+    # what an error of g and u of their absolute sums does to h (all slopes are below 1.2)
+    size = 1.2 * (X.abs() @ Wg.abs()) * u.abs() + (X.abs() @ Wu.abs()) * a.abs() + 16 * (a * u).abs()
+    return g, u, a, da, a * u, size
+
+
+def _check_gated(osscar, n, d, f, dtype, rows, name, seed=0, X=None, W=None):
+    g = _gen(seed)
+    X = _randn(g, n, d, dtype=dtype) if X is None else X
+    Wg, Wu = _weights(g, d, f, dtype, rows) if W is None else W
+    act = _act(osscar, name)
+    rounding = U if dtype == torch.bfloat16 else 0.0
+    G64, U64, a, da, h, size = _forward64(X, Wg, Wu, name)
+    H, G, Up = osscar.osscar_gated_forward(X, Wg, Wu, act, save=True)
+    assert H.dtype == dtype and H.shape == (n, f)
+    _near(H, h, size, rounding * h.abs(), d, "H")
+    Xd, Wgd, Wud = X.double(), Wg.double().contiguous(), Wu.double().contiguous()
+    _near(G, G64, Xd.abs() @ Wgd.abs(), 0.0, d, "G")
+    _near(Up, U64, Xd.abs() @ Wud.abs(), 0.0, d, "U")
+    assert torch.equal(H, osscar.osscar_gated_forward(X, Wg, Wu, act))      # the same without keeping, and the same bits again
+    # gradients
+    dH = _randn(g, n, f, dtype=dtype)
+    dh = dH.double()
+    dg, du = dh * U64 * da, dh * a
+    Wgt, Wut, Xt = Wgd.t().contiguous(), Wud.t().contiguous(), Xd.t().contiguous()
+    want = (dg @ Wgt + du @ Wut, Xt @ dg, Xt @ du)
+    mass = (dg.abs() @ Wgt.abs() + du.abs() @ Wut.abs(), Xt.abs() @ dg.abs(), Xt.abs() @ du.abs())
+    # errors of g and u reach dg and du: at most as much again as sums of d products (slopes and their slopes are below 2)
+    dgs, dus = 2 * dh.abs() * (U64.abs() + 1) * (Xd.abs() @ Wgd.abs() + Xd.abs() @ Wud.abs() + 1), 2 * dh.abs() * (Xd.abs() @ Wgd.abs() + 1)
+    more = (dgs @ Wgt.abs() + dus @ Wut.abs(), Xt.abs() @ dgs, Xt.abs() @ dus)
+    for kept in (True, False):
+        got = osscar.osscar_gated_backward(X, Wg, Wu, dH, act, **(dict(G=G, U=Up) if kept else {}))
+        for x, w, m, s, K, what in zip(got, want, mass, more, (2 * f, n, n), ("dX", "dWg", "dWu")):
+            assert x.dtype == dtype and x.shape == w.shape
+            _near(x, w, m + s, rounding * (w.abs() * (1 + U) + m), K + d, what)
+        assert (got[1].t() if rows == "out" else got[1]).is_contiguous()      # laid out as the weights are
+    return got
+
+
+GATED = [(1, 1, 1), (1, 64, 64), (1, 2048, 300), (2, 72, 40), (16, 136, 513), (17, 200, 264), (31, 1000, 17), (33, 33, 129), (64, 512, 96), (129, 257, 301), (300, 512, 777),
+         (513, 65, 1030)]
+
+
+@pytest.mark.parametrize("rows", ["in", "out"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,d,f", GATED)
+def test_gated_forward_and_backward(osscar, n, d, f, dtype, rows):
+    name = ACTS[(n + d + f + (rows == "out")) % 4]
+    _check_gated(osscar, n, d, f, dtype, rows, name, seed=n + d)
+
+
+@pytest.mark.parametrize("name", ACTS)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_gated_activations(osscar, dtype, name):
+    _check_gated(osscar, 40, 96, 136, dtype, "in", name, seed=7)
+
+
+@pytest.mark.parametrize("dtype,rows", [(torch.bfloat16, "in"), (torch.bfloat16, "out"), (torch.float32, "in")])
+@pytest.mark.parametrize("n,d,f", [(2100, 328, 3000), (3600, 3600, 136), (136, 3600, 2600)])
+def test_gated_large_tiles(osscar, n, d, f, dtype, rows):
+    """enough tiles for the 256-row shape in the projections, in dX, in dWg and dWu; ragged at every edge"""
+    _check_gated(osscar, n, d, f, dtype, rows, "SILU", seed=3)
+
+
+@pytest.mark.parametrize("name", ACTS)
+def test_gated_activation_over_its_range(osscar, name):
+    """H of single products: g runs over the range of float32, u = 1"""
+    v = torch.cat([torch.linspace(-30, 30, 4001), torch.tensor([0.0, -0.0, 1e-30, -1e-30, 88.0, -88.0, 104.0, -104.0, 3e38, -3e38, 1e4, -1e4])]).to(DEV)
+    X = torch.stack([v, torch.ones_like(v)], 1).contiguous()
+    Wg, Wu = torch.tensor([[1.0], [0.0]], device=DEV), torch.tensor([[0.0], [1.0]], device=DEV)
+    H, G, U_ = osscar.osscar_gated_forward(X, Wg, Wu, _act(osscar, name), save=True)
+    x = v.double()
+    a, da = _act64(x, name)
+    a, da = torch.nan_to_num(a), torch.nan_to_num(da)      # (the definition's own overflows, where the value is 0 or x and the slope 0 or 1)
+    big = x.abs() > 40
+    a, da = torch.where(big, torch.clamp_min(x, 0), a), torch.where(big, (x > 0).double(), da)
+    # 24 e relative where the tail is not below float32's range; 1e-6 of x elsewhere (erfc's fit is 7e-7 of the tail, which is below x)
+    assert ((H[:, 0].double() - a).abs() <= 1e-6 * x.abs() + 1e-37).all(), name
+    dX, _, _ = osscar.osscar_gated_backward(X, Wg, Wu, torch.ones(len(v), 1, device=DEV), _act(osscar, name), G=G, U=U_, need_w=False)
+    got = dX[:, 0].double()
+    corner = (x == 0) & (name == "RELU")
+    assert (((got - da).abs() <= 2e-6 * (1 + x.abs().clamp_max(30))) | corner).all(), name
+    if name == "RELU":
+        assert (got[x == 0] == 0).all()
+
+
+def test_gated_gradients_equal_differences(osscar):
+    g = _gen(11)
+    n, d, f = 9, 20, 14
+    X = _randn(g, n, d)
+    Wg, Wu = _weights(g, d, f, torch.float32, "in")
+    R = _randn(g, n, f)
+    D = [_randn(g, *t.shape).double() for t in (X, Wg, Wu)]
+    for name in ("SILU", "GELU", "GELU_TANH"):
+        got = osscar.osscar_gated_backward(X, Wg, Wu, R, _act(osscar, name))
+        for k, (t, direction) in enumerate(zip((X, Wg, Wu), D)):
+            def loss(step):
+                args = [X.double(), Wg.double(), Wu.double()]
+                args[k] = args[k] + step * direction
+                return (_forward64(*args, name)[4] * R.double()).sum().item()
+            diff = (loss(1e-5) - loss(-1e-5)) / 2e-5
+            mine = (got[k].double() * direction).sum().item()
+            assert abs(mine - diff) <= 2e-5 * got[k].double().norm().item() * direction.norm().item(), (name, k)
+
+
+def test_gated_views_alignment_and_poison(osscar):
+    """Operands inside larger buffers of NaN, at odd starts and leading dimensions: nothing outside reaches a result"""
+    g = _gen(5)
+    for dtype in (torch.bfloat16, torch.float32):
+        for n, d, f in ((5, 72, 40), (40, 72, 200), (70, 65, 131), (300, 136, 264)):
+            for lead, first in ((8, 0), (3, 1), (5, 3)):
+                def inside(rows, cols, scale):
+                    buf = torch.full((rows + 2, cols + lead), float("nan"), dtype=dtype, device=DEV).reshape(-1)[first:]
+                    view = torch.as_strided(buf, (rows, cols), (cols + lead, 1), buf.storage_offset() + cols + lead)
+                    view.copy_(_randn(g, rows, cols, scale=scale, dtype=dtype))
+                    return view
+                X = inside(n, d, 1.0)
+                for rows in ("in", "out"):
+                    W = [inside(f, d, 0.1).t() if rows == "out" else inside(d, f, 0.1) for _ in range(2)]
+                    _check_gated(osscar, n, d, f, dtype, rows, "SILU", seed=n, X=X, W=W)
+
+
+def test_gated_special_values(osscar):
+    """float32 operands that bf16 pieces cannot hold, an infinity in one row, a NaN in one neuron's weights: only they are touched"""
+    g = _gen(9)
+    for n in (3, 40):
+        X, (Wg, Wu) = _randn(g, n, 64), _weights(g, 64, 24, torch.float32, "in")
+        X[1, 5], Wu[7, 3] = float("inf"), float("nan")
+        H = osscar.osscar_gated_forward(X, Wg, Wu, osscar.OSSCAR_ACT_RELU)
+        want = torch.clamp_min(X.double() @ Wg.double(), 0) * (X.double() @ Wu.double())
+        bad = ~torch.isfinite(H)
+        assert bad[:, 3].all() and bad[1].any()
+        keep = torch.ones_like(bad)
+        keep[1], keep[:, 3] = False, False
+        assert torch.allclose(H[keep].double(), want[keep], rtol=1e-4, atol=1e-4)
+        big = torch.zeros(n, 64, device=DEV)
+        big[:, 0] = 3.4e38
+        Wg1, Wu1 = torch.zeros(64, 8, device=DEV), torch.zeros(64, 8, device=DEV)
+        Wg1[0], Wu1[0] = 1e-30, 1e-37
+        H = osscar.osscar_gated_forward(big, Wg1, Wu1, osscar.OSSCAR_ACT_RELU)
+        assert torch.allclose(H.double(), torch.full_like(H, 1.0).double() * (3.4e38 * 1e-30) * (3.4e38 * 1e-37), rtol=1e-2)
+
+
+def test_gated_empty_and_partial_requests(osscar):
+    g = _gen(1)
+    Wg, Wu = _weights(g, 48, 56, torch.bfloat16, "in")
+    X = torch.empty(0, 48, dtype=torch.bfloat16, device=DEV)
+    assert osscar.osscar_gated_forward(X, Wg, Wu).shape == (0, 56)
+    dX, dWg, dWu = osscar.osscar_gated_backward(X, Wg, Wu, torch.empty(0, 56, dtype=torch.bfloat16, device=DEV))
+    assert dX.shape == (0, 48) and (dWg == 0).all() and (dWu == 0).all()
+    X, dH = _randn(g, 100, 48, dtype=torch.bfloat16), _randn(g, 100, 56, dtype=torch.bfloat16)
+    full = osscar.osscar_gated_backward(X, Wg, Wu, dH)
+    assert osscar.osscar_gated_backward(X, Wg, Wu, dH, need_x=False)[0] is None
+    assert torch.equal(osscar.osscar_gated_backward(X, Wg, Wu, dH, need_w=False)[0], full[0])
+    f32 = osscar.osscar_gated_backward(X, Wg, Wu, dH, dw_dtype=torch.float32)
+    assert f32[1].dtype == torch.float32 and torch.equal(f32[1].to(torch.bfloat16), full[1])
+
+
+def test_gated_offsets_past_32_bits(osscar):
+    n, d, f = 66000, 32768, 8      # X is 4.3 GB
+    X = torch.zeros(n, d, dtype=torch.bfloat16, device=DEV)
+    g = _gen(2)
+    X[-3:] = _randn(g, 3, d, dtype=torch.bfloat16)
+    Wg, Wu = _weights(g, d, f, torch.bfloat16, "in")
+    H = osscar.osscar_gated_forward(X, Wg, Wu)
+    want = _forward64(X[-3:], Wg, Wu, "SILU")
+    _near(H[-3:], want[4], want[5], U * want[4].abs(), d, "H")
+    assert (H[:-3] == 0).all()
+    dH = torch.zeros(n, f, dtype=torch.bfloat16, device=DEV)
+    dH[-3:] = 1.0
+    dX, dWg, dWu = osscar.osscar_gated_backward(X, Wg, Wu, dH)
+    du = want[2]
+    w = X[-3:].double().t().contiguous() @ du
+    m = X[-3:].double().abs().t().contiguous() @ du.abs()
+    _near(dWu, w, 64 * m + 1e-3, U * (w.abs() * (1 + U) + m), n, "dWu")
+    assert (dX[:-3] == 0).all() and dX[-3:].abs().sum() > 0
+
+
+# ---- 8-bit integer products ------------------------------------------------------------------
+def _quantise(x):
+    """float32 scale and digits, by the definition (numpy divides as IEEE says)"""
+    x = x.float().cpu().numpy()
+    s = np.abs(x).max(1) / np.float32(127)
+    q = np.zeros(x.shape, dtype=np.float32)
+    np.divide(x, s[:, None], out=q, where=(s > 0)[:, None])
+    return torch.from_numpy(np.clip(np.rint(q), -127, 127).astype(np.int8)).to(DEV), torch.from_numpy(s).to(DEV)
+
+
+def _check_int(osscar, X, Wq, ws, bias, out_dtype, x_scale=None):
+    d1 = X.shape[1]
+    q, s = (X, x_scale) if x_scale is not None else _quantise(X)
+    Y = osscar.osscar_int_product(X, Wq, ws, bias=bias, x_scale=x_scale, out_dtype=out_dtype)
+    core = (q.double() @ Wq[:, :d1].double().t().contiguous()) * s.double()[:, None] * ws.double()      # (whole numbers below 2^53)
+    want = core + (bias.double() if bias is not None else 0)
+    tol = 4 * E * (core.abs() + want.abs()) + (U * want.abs() if out_dtype == torch.bfloat16 else 0)
+    assert Y.dtype == out_dtype and ((Y.double() - want).abs() <= tol + 1e-37).all()
+    return Y
+
+
+INTS = [(1, 1, 1), (1, 64, 16), (1, 5461, 1365), (3, 40, 72), (16, 1030, 6200), (17, 130, 33), (64, 16, 129), (130, 200, 264), (257, 333, 301), (1000, 4096, 136)]
+
+
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,d1,m", INTS)
+def test_int_product(osscar, n, d1, m, dtype, bias):
+    g = _gen(n + d1)
+    X = _randn(g, n, d1, dtype=dtype) * torch.exp(_randn(g, d1)).to(dtype)
+    W = _randn(g, d1, m, scale=0.02)
+    Wq, ws = osscar.osscar_int_weights(W)
+    q, s = _quantise(W.t().contiguous())
+    assert torch.equal(Wq[:, :d1], q) and (Wq[:, d1:] == 0).all() and torch.equal(ws, s) and Wq.shape[1] % 16 == 0
+    Wq2, ws2 = osscar.osscar_int_weights(W.t().contiguous().t())      # the other layout in memory
+    assert torch.equal(Wq, Wq2) and torch.equal(ws, ws2)
+    b = _randn(g, m) if bias else None
+    for out in (torch.bfloat16, torch.float32):
+        Y = _check_int(osscar, X, Wq, ws, b, out)
+        Xq, xs = osscar.osscar_int_rows(X)
+        assert torch.equal(Xq, _quantise(X)[0]) and torch.equal(xs, _quantise(X)[1])
+        assert torch.equal(osscar.osscar_int_product(Xq, Wq, ws, bias=b, x_scale=xs, out_dtype=out), Y)
+        assert torch.equal(osscar.osscar_int_product(Xq.contiguous(), Wq, ws, bias=b, x_scale=xs, out_dtype=out), Y)      # rows of any length
+
+
+def test_int_product_large_tiles_and_full_range(osscar):
+    """the 256-row shape; digits of -128 and 127 alone; garbage behind a weight row"""
+    g = _gen(4)
+    n, d1, m = 2100, 1000, 6200
+    Xq = torch.randint(-128, 128, (n, d1), generator=g, device=DEV, dtype=torch.int32).to(torch.int8)
+    Wq = torch.randint(-128, 128, (m, 1008), generator=g, device=DEV, dtype=torch.int32).to(torch.int8)
+    ws, xs = torch.rand(m, generator=g, device=DEV), torch.rand(n, generator=g, device=DEV)
+    _check_int(osscar, Xq, Wq, ws, None, torch.float32, x_scale=xs)
+    K = 131056      # the longest contraction, every product at its largest: 2^31 - 245760
+    one = torch.full((1, K), -128, dtype=torch.int8, device=DEV)
+    for n in (1, 40):
+        Y = osscar.osscar_int_product(one.expand(n, K).contiguous(), one, torch.ones(1, device=DEV), x_scale=torch.ones(n, device=DEV), out_dtype=torch.float32)
+        assert (Y == float(K * 16384)).all()
+
+
+def test_int_special_rows(osscar):
+    """a row of zeros, rows with an infinity and a NaN, tiny rows; channels likewise"""
+    g = _gen(6)
+    for n in (6, 40):
+        X = _randn(g, n, 70)
+        X[0], X[1, 3], X[2, 69] = 0, float("inf"), float("nan")
+        X[3] *= 1e-38
+        W = _randn(g, 70, 20)
+        W[:, 4], W[3, 5] = 0, float("nan")
+        Wq, ws = osscar.osscar_int_weights(W)
+        assert torch.isnan(ws[5]) and (Wq[5] == 0).all() and ws[4] == 0
+        bias = _randn(g, 20)
+        Y = osscar.osscar_int_product(X, Wq, ws, bias=bias, out_dtype=torch.float32)
+        fine = [c for c in range(20) if c != 5]
+        assert torch.equal(Y[0][fine], bias[fine]) and torch.isnan(Y[1]).all() and torch.isnan(Y[2]).all() and torch.isnan(Y[:, 5]).all()
+        assert torch.equal(Y[3:, 4], bias[4].expand(n - 3))
+        rest = _check_int(osscar, X[4:], Wq[:4], ws[:4], bias[:4], torch.float32)
+        assert torch.equal(rest, Y[4:, :4])
+
+
+# ---- log probabilities -----------------------------------------------------------------------
+def _logprobs64(L, t, scale):
+    z = L.double() * scale
+    lp = torch.log_softmax(z, 1)
+    p = lp.exp()
+    entropy = -torch.where(p > 0, p * lp, torch.zeros_like(p)).sum(1)
+    ok = t >= 0
+    logp = torch.zeros(len(t), dtype=torch.float64, device=DEV)
+    logp[ok] = lp[torch.arange(len(t), device=DEV)[ok], t[ok]]
+    return lp, p, entropy, logp
+
+
+def _check_logprobs(osscar, L, t, top, scale=1.0):
+    lp, p, entropy, logp = _logprobs64(L, t, scale)
+    r = osscar.osscar_logprobs(L, t, top, scale)
+    # differences of scaled logits carry 2 e of their size, the sum of the exponentials and its logarithm about 1e-6
+    bound = lambda v: 2e-6 * (1 + v.abs() / 2)  # noqa: E731
+    fine = torch.isfinite(logp)
+    assert torch.equal(torch.isfinite(r.logp), fine) and ((r.logp.double() - logp)[fine].abs() <= bound(logp[fine])).all()
+    assert ((r.entropy.double() - entropy).abs() <= 5e-6 * (1 + entropy)).all()
+    lse = torch.logsumexp(L.double() * scale, 1)
+    assert (((r.lse[:, 0].double() * scale + r.lse[:, 1].double()) - lse).abs() <= 2e-6 * (1 + lse.abs())).all()
+    if top:
+        order = torch.sort(L.float() + 0.0, dim=1, descending=True, stable=True).indices[:, :top]
+        assert torch.equal(r.top_index, order)
+        want = torch.gather(lp, 1, order)
+        fine = torch.isfinite(want)
+        assert torch.equal(torch.isfinite(r.top_logp), fine) and ((r.top_logp.double() - want)[fine].abs() <= bound(want[fine])).all()
+    return r, lp, p, entropy
+
+
+SCORES = [(1, 1, 1), (1, 5, 5), (3, 70, 64), (2, 4096, 8), (1, 131072, 20), (5, 8191, 1), (5, 8193, 33), (40, 3001, 9), (17, 40000, 5), (700, 9000, 8), (513, 2050, 0)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,v,top", SCORES)
+def test_logprobs_and_gradient(osscar, n, v, top, dtype):
+    g = _gen(n + v)
+    L = _randn(g, n, v, scale=2.5, dtype=dtype)
+    t = torch.randint(0, v, (n,), generator=g, device=DEV)
+    t[::3] = -1
+    if v > 10:
+        L[:, v - 3:] = -math.inf
+    scale = 1.0 if n % 2 else 0.7
+    r, lp, p, entropy = _check_logprobs(osscar, L, t, top, scale)
+    dlogp, dent = _randn(g, n), _randn(g, n)
+    dtop = _randn(g, n, top) if top else None
+    hot = torch.zeros(n, v, dtype=torch.float64, device=DEV)
+    ok = t >= 0
+    hot[torch.arange(n, device=DEV)[ok], t[ok]] = 1.0
+    w = torch.where(ok, dlogp, torch.zeros_like(dlogp)).double()[:, None]
+    own = w * hot
+    size = w.abs() * (hot + p)
+    total = w.clone()
+    if top:
+        own = own.scatter_add(1, r.top_index, dtop.double())
+        size = size + torch.zeros_like(hot).scatter_add(1, r.top_index, dtop.double().abs()) + p * dtop.double().abs().sum(1, keepdim=True)
+        total = total + dtop.double().sum(1, keepdim=True)
+    plogp = torch.where(p > 0, p * lp, torch.zeros_like(p))
+    want = scale * (own - p * total - dent.double()[:, None] * (plogp + p * entropy[:, None]))
+    size = scale * (size + dent.double().abs()[:, None] * (plogp.abs() + p * (1 + entropy[:, None])))
+    got = osscar.osscar_logprobs_backward(L, t, r.lse, dlogp, entropy=r.entropy, dentropy=dent, top_index=r.top_index, dtop=dtop, scale=scale)
+    tol = 8e-6 * (1 + torch.where(p > 0, lp.abs(), torch.zeros_like(lp))) * size + (U * want.abs() if dtype == torch.bfloat16 else 0)
+    assert ((got.double() - want).abs() <= tol + 1e-30).all()
+    # each part alone, and in place
+    only = osscar.osscar_logprobs_backward(L, t, r.lse, dlogp, scale=scale)
+    want1 = scale * w * (hot - p)
+    assert ((only.double() - want1).abs() <= 8e-6 * scale * (1 + torch.where(p > 0, lp.abs(), torch.zeros_like(lp))) * w.abs() * (hot + p) + (U * want1.abs() if dtype == torch.bfloat16 else 0) + 1e-30).all()
+    L2 = L.clone()
+    same = osscar.osscar_logprobs_backward(L2, t, r.lse, dlogp, entropy=r.entropy, dentropy=dent, top_index=r.top_index, dtop=dtop, scale=scale, out=L2)
+    assert same.data_ptr() == L2.data_ptr() and torch.equal(same, got)
+
+
+@pytest.mark.parametrize("kind", ["ties", "constant", "lowest", "few finite", "ascending", "zeros of both signs", "large", "descending"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_logprobs_awkward_rows(osscar, kind, dtype):
+    g = _gen(8)
+    for n, v in ((3, 70), (2, 8192), (2, 8200), (700, 9000), (1, 70000)):
+        if kind == "ties":
+            L = torch.randint(-2, 3, (n, v), generator=g, device=DEV).to(dtype)
+        elif kind == "constant":
+            L = torch.full((n, v), 3.0, device=DEV, dtype=dtype)
+        elif kind == "lowest":
+            L = torch.full((n, v), torch.finfo(dtype).min, device=DEV, dtype=dtype)
+        elif kind == "few finite":
+            L = torch.full((n, v), -math.inf, device=DEV, dtype=dtype)
+            L.scatter_(1, torch.randint(0, v, (n, 3), generator=g, device=DEV), _randn(g, n, 3, dtype=dtype))
+        elif kind in ("ascending", "descending"):
+            L = (torch.arange(v, device=DEV).float() / v * (20 if kind == "ascending" else -20)).to(dtype).expand(n, v).contiguous()
+        elif kind == "zeros of both signs":
+            L = torch.where(torch.rand(n, v, generator=g, device=DEV) < 0.5, -0.0, 0.0).to(dtype)
+        else:
+            L = _randn(g, n, v, scale=1e4, dtype=dtype)
+        t = torch.randint(0, v, (n,), generator=g, device=DEV)
+        for top in (1, 8, 33, 64):
+            _check_logprobs(osscar, L, t, top, 1.0 if top != 8 else 0.37)
+
+
+def test_logprobs_empty_rows_and_values_that_are_no_numbers(osscar):
+    for v, n in ((50, 4), (9000, 4), (70000, 4), (300, 600)):
+        L = torch.zeros(n, v, device=DEV)
+        L[0] = -math.inf                                   # nothing is left
+        L[1, 7], L[2, 3], L[2, 9] = math.nan, math.inf, math.nan
+        t = torch.full((n,), 5, device=DEV)
+        t[3] = v                                           # outside the vocabulary
+        r = osscar.osscar_logprobs(L, t, 3)
+        assert r.entropy[0] == 0 and r.logp[0] == -math.inf and (r.top_logp[0] == -math.inf).all() and r.top_index[0].tolist() == [0, 1, 2]
+        assert torch.isnan(r.logp[1:4]).all() and torch.isnan(r.entropy[1:3]).all()
+        assert r.top_index[1].tolist() == [7, 0, 1] and r.top_index[2].tolist() == [9, 3, 0]
+        assert abs(r.entropy[3].item() - math.log(v)) < 1e-5
+        d = osscar.osscar_logprobs_backward(L, t, r.lse, torch.ones(n, device=DEV), entropy=r.entropy, dentropy=torch.ones(n, device=DEV))
+        assert (d[0] == 0).all() and torch.isnan(d[1]).all() and torch.isnan(d[2]).all() and torch.isnan(d[3]).all()
+        t[:] = -1                                          # no targets: what dlogp holds does not matter
+        d = osscar.osscar_logprobs_backward(L, t, r.lse, torch.full((n,), math.nan, device=DEV))
+        assert (d[3] == 0).all() and (d[0] == 0).all()
+    assert osscar.osscar_logprobs(torch.empty(0, 9, device=DEV), torch.empty(0, dtype=torch.int64, device=DEV), 2).top_index.shape == (0, 2)
+
+
+def test_logprobs_strides_alignment_and_offsets_past_32_bits(osscar):
+    g = _gen(3)
+    for dtype in (torch.bfloat16, torch.float32):
+        buf = torch.full((12 * 1100 + 5,), math.nan, dtype=dtype, device=DEV)
+        L = torch.as_strided(buf, (12, 1001), (1100, 1), 3)
+        L.copy_(_randn(g, 12, 1001, dtype=dtype))
+        t = torch.randint(0, 1001, (12,), generator=g, device=DEV)
+        r, lp, p, _ = _check_logprobs(osscar, L, t, 7)
+        d = torch.ones(12, device=DEV)
+        out = torch.full((12, 1100), 7.0, dtype=dtype, device=DEV)
+        osscar.osscar_logprobs_backward(L, t, r.lse, d, out=out[:, 1:1002])
+        assert (out[:, 0] == 7).all() and (out[:, 1002:] == 7).all()
+        assert torch.equal(out[:, 1:1002], osscar.osscar_logprobs_backward(L.clone(), t, r.lse, d))
+    n, v = 33000, 70000
+    L = torch.zeros(n, v, dtype=torch.bfloat16, device=DEV)
+    L[-2:] = _randn(g, 2, v, dtype=torch.bfloat16)
+    t = torch.randint(0, v, (n,), generator=g, device=DEV)
+    r = osscar.osscar_logprobs(L, t, 4)
+    _, _, entropy, logp = _logprobs64(L[-2:], t[-2:], 1.0)
+    assert ((r.logp[-2:].double() - logp).abs() <= 2e-6 * (1 + logp.abs() / 2)).all() and ((r.entropy[-2:].double() - entropy).abs() <= 1e-4).all()
+    assert torch.equal(r.top_index[:5], torch.arange(4, device=DEV).expand(5, 4)) and torch.equal(r.top_index[-2:], torch.sort(L[-2:].float(), dim=1, descending=True, stable=True).indices[:, :4])
+    del r
+    g1 = osscar.osscar_logprobs_backward(L, t, osscar.osscar_logprobs(L, t).lse, torch.ones(n, device=DEV), out=L)
+    assert g1[-1].double().sum().abs() < 0.05 and g1[-1, t[-1]] > 0.5
+
+
+def test_logprobs_gradient_equals_differences(osscar):
+    g = _gen(12)
+    n, v = 4, 30
+    L = _randn(g, n, v)
+    t = torch.randint(0, v, (n,), generator=g, device=DEV)
+    a, b, c = _randn(g, n), _randn(g, n), _randn(g, n, 3)
+    r = osscar.osscar_logprobs(L, t, 3)
+    got = osscar.osscar_logprobs_backward(L, t, r.lse, a, entropy=r.entropy, dentropy=b, top_index=r.top_index, dtop=c)
+    D = _randn(g, n, v).double()
+
+    def loss(step):
+        lp, _, entropy, logp = _logprobs64(L.double() + step * D, t, 1.0)
+        return (a.double() * logp + b.double() * entropy + (c.double() * torch.gather(lp, 1, r.top_index)).sum(1)).sum().item()
+    diff = (loss(1e-5) - loss(-1e-5)) / 2e-5
+    assert abs((got.double() * D).sum().item() - diff) <= 2e-5 * got.double().norm().item() * D.norm().item()
+
+
+# ---- streams, graphs, refusals ---------------------------------------------------------------
+def _all(osscar, X, Wg, Wu, Wq, ws, t):
+    H, G, U_ = osscar.osscar_gated_forward(X, Wg, Wu, save=True)
+    Y = osscar.osscar_int_product(H, Wq, ws, out_dtype=torch.float32)
+    r = osscar.osscar_logprobs(Y, t, 4)
+    dY = osscar.osscar_logprobs_backward(Y, t, r.lse, torch.ones_like(r.logp), entropy=r.entropy, dentropy=torch.ones_like(r.logp))
+    dH = dY[:, :H.shape[1]].to(H.dtype).contiguous()
+    return [H, Y, r.logp, r.entropy, r.top_index, r.top_logp, dY, *osscar.osscar_gated_backward(X, Wg, Wu, dH, G=G, U=U_)]
+
+
+@pytest.mark.parametrize("n", [1, 20, 200])
+def test_on_another_stream_and_in_a_graph(osscar, n):
+    g = _gen(n)
+    d, f, v = 136, 264, 1000
+    X = _randn(g, n, d, dtype=torch.bfloat16)
+    Wg, Wu = _weights(g, d, f, torch.bfloat16, "in")
+    Wq, ws = osscar.osscar_int_weights(_randn(g, f, v, scale=0.1))
+    t = torch.randint(0, v, (n,), generator=g, device=DEV)
+    want = _all(osscar, X, Wg, Wu, Wq, ws, t)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    H = osscar.osscar_gated_forward(X, Wg, Wu, stream=side)
+    Y = osscar.osscar_int_product(H, Wq, ws, out_dtype=torch.float32, stream=side)
+    r = osscar.osscar_logprobs(Y, t, 4, stream=side)
+    side.synchronize()
+    assert torch.equal(H, want[0]) and torch.equal(Y, want[1]) and torch.equal(r.top_index, want[4])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = _all(osscar, X, Wg, Wu, Wq, ws, t)
+    for k in range(4):
+        X.copy_(_randn(g, n, d, dtype=torch.bfloat16))
+        eager = _all(osscar, X, Wg, Wu, Wq, ws, t)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, eager):
+            assert torch.equal(a, b), k
+
+
+def test_refusals_of_the_binding(osscar):
+    from paper_2403_12983_amd import OsscarError
+    bf = dict(dtype=torch.bfloat16, device=DEV)
+    X, W = torch.zeros(4, 16, **bf), torch.zeros(16, 24, **bf)
+    bad = [
+        lambda: osscar.osscar_gated_forward(X.cpu(), W, W),
+        lambda: osscar.osscar_gated_forward(X, W.cpu(), W.cpu()),
+        lambda: osscar.osscar_gated_forward(X.half(), W.half(), W.half()),
+        lambda: osscar.osscar_gated_forward(X, W.float(), W.float()),
+        lambda: osscar.osscar_gated_forward(X, W[:8], W[:8]),
+        lambda: osscar.osscar_gated_forward(X, W, W[:, :8]),
+        lambda: osscar.osscar_gated_forward(X, W, W.t().contiguous().t()),
+        lambda: osscar.osscar_gated_forward(X[:, ::2], W[:8], W[:8]),
+        lambda: osscar.osscar_gated_forward(X[:1].expand(4, 16), W, W),
+        lambda: osscar.osscar_gated_forward(X, W, W, 9),
+        lambda: osscar.osscar_gated_backward(X, W, W, torch.zeros(4, 16, **bf)),
+        lambda: osscar.osscar_gated_backward(X, W, W, torch.zeros(4, 24, **bf), G=torch.zeros(4, 24, device=DEV)),
+        lambda: osscar.osscar_gated_backward(X, W, W, torch.zeros(4, 24, **bf), dw_dtype=torch.float16),
+        lambda: osscar.osscar_int_product(X, torch.zeros(8, 16, device=DEV), torch.zeros(8, device=DEV)),
+        lambda: osscar.osscar_int_product(X, torch.zeros(8, 15, dtype=torch.int8, device=DEV), torch.zeros(8, device=DEV)),
+        lambda: osscar.osscar_int_product(X, torch.zeros(8, 17, dtype=torch.int8, device=DEV), torch.zeros(8, device=DEV)),
+        lambda: osscar.osscar_int_product(X, torch.zeros(8, 16, dtype=torch.int8, device=DEV), torch.zeros(7, device=DEV)),
+        lambda: osscar.osscar_int_product(X, torch.zeros(8, 16, dtype=torch.int8, device=DEV), torch.zeros(8, device=DEV), x_scale=torch.zeros(4, device=DEV)),
+        lambda: osscar.osscar_int_product(X.to(torch.int8), torch.zeros(8, 16, dtype=torch.int8, device=DEV), torch.zeros(8, device=DEV)),
+        lambda: osscar.osscar_int_weights(W.double()),
+        lambda: osscar.osscar_logprobs(X, torch.zeros(4, dtype=torch.int32, device=DEV)),
+        lambda: osscar.osscar_logprobs(X, torch.zeros(3, dtype=torch.int64, device=DEV)),
+        lambda: osscar.osscar_logprobs(X, torch.zeros(4, dtype=torch.int64, device=DEV), 17),
+        lambda: osscar.osscar_logprobs(X, torch.zeros(4, dtype=torch.int64, device=DEV), -1),
+        lambda: osscar.osscar_logprobs(X, torch.zeros(4, dtype=torch.int64, device=DEV), scale=0.0),
+        lambda: osscar.osscar_logprobs(X, torch.zeros(4, dtype=torch.int64, device=DEV), scale=math.nan),
+        lambda: osscar.osscar_logprobs_backward(X, torch.zeros(4, dtype=torch.int64, device=DEV), torch.zeros(4, device=DEV)),
+        lambda: osscar.osscar_logprobs_backward(X, torch.zeros(4, dtype=torch.int64, device=DEV), torch.zeros(4, 2, device=DEV), dentropy=torch.zeros(4, device=DEV)),
+        lambda: osscar.osscar_logprobs_backward(X, torch.zeros(4, dtype=torch.int64, device=DEV), torch.zeros(4, 2, device=DEV), dtop=torch.zeros(4, 2, device=DEV)),
+    ]
+    for k, call in enumerate(bad):
+        with pytest.raises(OsscarError) as e:
+            call()
+        assert e.value.status == 1, k
