@@ -63,12 +63,15 @@ template <> struct Num<true> {
   static constexpr int ES = 1;
   static __device__ __forceinline__ void mma(v4i a, v4i b, acc& c) { asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
 };
-// The matrix core has written the sums when this has passed (16 cycles cover its longest result).
+// The matrix core has written the sums when this has passed (16 wait states cover its longest result).  The compiler does not see matrix instructions there,
+// and without settled() it reads sums before the wait, and all 256 of them at once, which it then moves about between registers and memory.
 __device__ __forceinline__ void sums_written() {
   __builtin_amdgcn_sched_barrier(0);
   asm volatile("s_nop 15" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
 }
+template <class V>
+__device__ __forceinline__ void settled(V& c) { asm volatile("" : "+a"(c)); }
 
 // The shape of a workgroup: WM x WN waves, each of FM x (NB FN) tiles of 16 x 16.  NB: matrices on the B side whose columns a wave takes
 // alike (gate and up projection), FN tiles of each.
@@ -339,6 +342,8 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
 #pragma unroll
       for (int t = 0; t < S::FN; t += 2) {
         const int n = tn * S::BN + wn * S::FN * 16 + t * 16 + g * 8;
+#pragma unroll
+        for (int z = 0; z < S::NB; z++) { settled(acc[f][z][t]); settled(acc[f][z][t + 1]); }
         typename T::val v[S::NB][8];
 #pragma unroll
         for (int z = 0; z < S::NB; z++)

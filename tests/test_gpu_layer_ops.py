@@ -134,6 +134,14 @@ def test_gated_large_tiles(osscar, n, d, f, dtype, rows):
     _check_gated(osscar, n, d, f, dtype, rows, "SILU", seed=3)
 
 
+@pytest.mark.parametrize("rows", ["in", "out"])
+@pytest.mark.parametrize("n,d,f", [(2100, 333, 3001), (3600, 3601, 137), (137, 3601, 2603), (5, 1553, 9130)])
+def test_gated_large_tiles_with_columns_left_over(osscar, n, d, f, rows):
+    """the same with one to seven columns in the last group of eight: every row of them is written (a lane's sums were once read too early there)"""
+    for name in ("SILU", "RELU"):
+        _check_gated(osscar, n, d, f, torch.bfloat16, rows, name, seed=4)
+
+
 @pytest.mark.parametrize("name", ACTS)
 def test_gated_activation_over_its_range(osscar, name):
     """H of single products: g runs over the range of float32, u = 1"""
@@ -306,6 +314,15 @@ def test_int_product_large_tiles_and_full_range(osscar):
     for n in (1, 40):
         Y = osscar.osscar_int_product(one.expand(n, K).contiguous(), one, torch.ones(1, device=DEV), x_scale=torch.ones(n, device=DEV), out_dtype=torch.float32)
         assert (Y == float(K * 16384)).all()
+
+
+@pytest.mark.parametrize("m", [6145, 6203, 6207])
+def test_int_product_large_tiles_with_columns_left_over(osscar, m):
+    g = _gen(m)
+    X, W = _randn(g, 2050, 300, dtype=torch.bfloat16), _randn(g, 300, m)
+    Wq, ws = osscar.osscar_int_weights(W)
+    for out in (torch.bfloat16, torch.float32):
+        _check_int(osscar, X, Wq, ws, _randn(g, m), out)
 
 
 def test_int_special_rows(osscar):
