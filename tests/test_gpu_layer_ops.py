@@ -142,6 +142,20 @@ def test_gated_large_tiles_with_columns_left_over(osscar, n, d, f, rows):
         _check_gated(osscar, n, d, f, torch.bfloat16, rows, name, seed=4)
 
 
+@pytest.mark.parametrize("rows", ["in", "out"])
+def test_gated_float32_projection_near_zero(osscar, rows):
+    """RELU's slope turns on the sign of g: its error is that of a sum with one rounding to the sum's size in 32 of the contraction.  A rounding is off by at most e of the
+    value (0.4 e in the mean square), d / 32 of them at sqrt(1/2) of the last size make 0.28 e sqrt(d / 32); six per stage at sqrt(32 / d) of it make
+    e sqrt(6); a quarter more is allowed."""
+    n, d, f = 4096, 2688, 367
+    g = _gen(21)
+    X, (Wg, Wu) = _randn(g, n, d), _weights(g, d, f, torch.float32, rows)
+    _, G, Up = osscar.osscar_gated_forward(X, Wg, Wu, osscar.OSSCAR_ACT_RELU, save=True)
+    for got, W in ((G, Wg), (Up, Wu)):
+        want = X.double() @ W.double().contiguous()
+        assert ((got.double() - want).norm() / want.norm()).item() <= 1.25 * E * (math.sqrt(6) + 0.28 * math.sqrt(d / 32))
+
+
 @pytest.mark.parametrize("name", ACTS)
 def test_gated_activation_over_its_range(osscar, name):
     """H of single products: g runs over the range of float32, u = 1"""
