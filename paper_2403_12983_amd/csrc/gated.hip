@@ -283,7 +283,9 @@ struct Buffers {
   char* sums;            // of parts, one product after the other
 };
 // The products of few rows (thin.h says where)
-bool few(const osscar_gated_desc& q) { return q.dtype == OSSCAR_F32 ? q.n <= 32 : q.rows_out && q.n <= 16 && q.d * q.f <= (1 << 24); }
+bool few(const osscar_gated_desc& q) {
+  return q.dtype == OSSCAR_F32 ? q.n <= 32 : q.rows_out && q.n <= 16 && (q.d * q.f <= (1 << 24) || q.unaligned || !operand_fits(nullptr, q.ldw, q.d, 2));
+}
 Buffers buffers(Carve& c, const osscar_gated_desc& q, const void* X, const void* Wg, const void* Wu, int backward, bool kept) {
   Buffers b{};
   const bool f32 = q.dtype == OSSCAR_F32;
