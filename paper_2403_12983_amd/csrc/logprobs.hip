@@ -132,6 +132,7 @@ __device__ __forceinline__ void choose(const uint64_t* ranks, int n, int k, F pu
   for (int i = threadIdx.x; i < n; i += T) {
     const uint64_t r = ranks[i];
     int above = 0;
+#pragma unroll 8
     for (int j = 0; j < n; j++) above += ranks[j] > r;
     if (above < k) put(above, r);
   }
@@ -295,7 +296,8 @@ __global__ __launch_bounds__(T) void logprobs_kernel(const void* __restrict__ lo
 // The parts of a row put together, a row per workgroup.
 __global__ __launch_bounds__(T) void logprobs_join_kernel(const void* __restrict__ logits, int f32, int vocab, int64_t ld, int parts, Row out,
                                                           const Stat* __restrict__ part_stat, const uint64_t* __restrict__ part_rank) {
-  __shared__ uint64_t ranks[JOIN];
+  __shared__ uint64_t ranks[JOIN], best[JOIN];
+  __shared__ int count;
   const int64_t row = blockIdx.x, base = row * ld;
   const float c2 = out.scale * LOG2E;
   const int lane = threadIdx.x & 63;
@@ -305,11 +307,22 @@ __global__ __launch_bounds__(T) void logprobs_join_kernel(const void* __restrict
   for (int o = 32; o > 0; o >>= 1) join(s, Stat{__shfl_xor(s.m, o, 64), __shfl_xor(s.S, o, 64), __shfl_xor(s.A, o, 64)}, c2);
   if (threadIdx.x == 0) put_row(out, row, s, g, c2);
   if (out.top == 0) return;
-  const int n = parts * out.top;
+  // A part's alternatives come in order.  With c parts whose m-th is not below some rank, c m >= top are not, and what is below it is out: about half the parts
+  // give a rank that few others reach.
+  const int n = parts * out.top, m = min(out.top, (2 * out.top + parts - 1) / parts), c = (out.top + m - 1) / m;
   for (int i = threadIdx.x; i < n; i += T) ranks[i] = part_rank[row * n + i];
+  if (threadIdx.x == 0) count = 0;
   __syncthreads();
-  choose(ranks, n, out.top, [&](int j, uint64_t r) {
-    if (r == 0) return;
+  const uint64_t mine = lane < parts ? ranks[lane * out.top + m - 1] : 0;
+  int above = 0;
+#pragma unroll 8
+  for (int j = 0; j < parts; j++) above += ranks[j * out.top + m - 1] > mine;
+  const uint64_t at = __ballot(above == c - 1 && lane < parts);      // (no lane: short parts, whose missing ones are 0)
+  const uint64_t bound = at ? (uint64_t)__shfl((unsigned long long)mine, __ffsll((unsigned long long)at) - 1, 64) : 0;
+  for (int i = threadIdx.x; i < n; i += T)
+    if (ranks[i] > 0 && ranks[i] >= bound) best[atomicAdd(&count, 1)] = ranks[i];
+  __syncthreads();
+  choose(best, count, out.top, [&](int j, uint64_t r) {
     out.top_index[row * out.top + j] = index_of(r);
     out.top_logp[row * out.top + j] = logp_of(s, logit_of(r), c2);
   });

@@ -261,16 +261,17 @@ def osscar_logprobs(logits: torch.Tensor, targets: torch.Tensor, top: int = 0, s
     _on(index, targets=targets)
     tp = _vector(targets, n, torch.int64, "targets")
     with context:
-        out = _EMPTY(4, n, dtype=torch.float32, device=device)      # logp, entropy, lse
+        out, lse = _EMPTY(2, n, dtype=torch.float32, device=device), _EMPTY(n, 2, dtype=torch.float32, device=device)      # logp and entropy
         top_index = _EMPTY(n, top, dtype=torch.int64, device=device) if top > 0 else None
         top_logp = _EMPTY(n, top, dtype=torch.float32, device=device) if top > 0 else None
         size = lib.osscar_logprobs_workspace_bytes(n, vocab, top)
         ws, wp, size = _workspace(size, device)
         base = out.data_ptr()
-        status = lib.osscar_logprobs(logits.data_ptr(), n, vocab, ld, code, tp, scale, top, base, base + 4 * n, base + 8 * n,
+        status = lib.osscar_logprobs(logits.data_ptr(), n, vocab, ld, code, tp, scale, top, base, base + 4 * n, lse.data_ptr(),
                                      top_index.data_ptr() if top > 0 else None, top_logp.data_ptr() if top > 0 else None, wp, size, handle)
     _done(lib, status)
-    return LogProbs(out[0], out[1], out[2:].view(n, 2), top_index, top_logp)
+    logp, entropy = out.unbind()
+    return LogProbs(logp, entropy, lse, top_index, top_logp)
 
 
 def osscar_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, dlogp: Optional[torch.Tensor] = None,
