@@ -142,13 +142,6 @@ struct PlainOut {
       else put_bf16(reinterpret_cast<uint16_t*>(out) + (int64_t)m * ld + n, v[0], N - n);
     });
   }
-  template <class F>
-  __device__ __forceinline__ void one(F f) const {
-    f([&](int m, int n, const float (&v)[1], int) {
-      if (f32) reinterpret_cast<float*>(out)[(int64_t)m * ld + n] = v[0];
-      else reinterpret_cast<uint16_t*>(out)[(int64_t)m * ld + n] = bf16_nearest(v[0]);
-    });
-  }
 };
 // dg and du from kept g and u, in the type of the products that take them: bf16 rounds them once more, as h is rounded for the next layer.  Rows of
 // `ld`, a multiple of eight, zeros past f.  Bound by its 14 (float32: 20) bytes per element.
@@ -201,27 +194,23 @@ typedef Shape<2, 2, 8, 4, 2, false> Big2;       // 256 x (128 + 128), four waves
 typedef Shape<2, 2, 4, 2, 2, true> Small2;     // 128 x (64 + 64), four waves
 typedef Shape<2, 2, 8, 8, 1, false> Big1;       // 256 x 256
 typedef Shape<2, 2, 4, 4, 1, true> Small1;     // 128 x 128
-__global__ __launch_bounds__(256) void plain_join_kernel(const float* __restrict__ sums, int parts, int M, int N, const PlainOut e) {
-  tile::join<1>(sums, parts, M, N, e);
+template <class S, class Epi>
+__global__ __launch_bounds__(256) void gated_join_tiles_kernel(const Pair<S::NB, Epi> q) {
+  tile::join_tiles<S, float>(q.p[blockIdx.y], q.e[blockIdx.y]);
 }
-void launch_join(const Product<2>& p, const GatedOut& e, hipStream_t s) {
-  hipLaunchKernelGGL(gated_join_kernel, dim3(join_grid(p.M, p.N)), dim3(256), 0, s, reinterpret_cast<const float*>(p.sums), p.parts, p.M, p.N, e);
-}
-void launch_join(const Product<1>& p, const PlainOut& e, hipStream_t s) {
-  hipLaunchKernelGGL(plain_join_kernel, dim3(join_grid(p.M, p.N)), dim3(256), 0, s, reinterpret_cast<const float*>(p.sums), p.parts, p.M, p.N, e);
-}
-// `count` products of one launch; sums: sums_bytes() of them
+// `count` products of one launch; sums: d.sums for each
 template <int AM, int BMODE, class SB, class SS, class Epi>
 void launch_product(Pair<SB::NB, Epi>& q, int count, bool f32, const Deal& d, char* sums, hipStream_t s) {
   for (int c = 0; c < count; c++) {
+    q.p[c].whole = d.whole;
     q.p[c].parts = d.parts;
-    q.p[c].sums = sums + (size_t)c * sums_bytes(d, SB::NB, 1, q.p[c].M, q.p[c].N);
+    q.p[c].sums = sums + c * d.sums;
   }
-  const dim3 grid(d.tiles, count, d.parts);
+  const dim3 grid(d.blocks, count);
   if (f32) hipLaunchKernelGGL((gated_split_kernel<AM, BMODE, SS, Epi>), grid, dim3(SS::WAVES * 64), 0, s, q);
   else if (d.big) hipLaunchKernelGGL((gated_product_kernel<AM, BMODE, SB, Epi>), grid, dim3(SB::WAVES * 64), 0, s, q);
   else hipLaunchKernelGGL((gated_product_kernel<AM, BMODE, SS, Epi>), grid, dim3(SS::WAVES * 64), 0, s, q);
-  for (int c = 0; c < count && d.parts > 1; c++) launch_join(q.p[c], q.e[c], s);
+  if (d.parts > 1) hipLaunchKernelGGL((gated_join_tiles_kernel<SS, Epi>), dim3((unsigned)d.join, count), dim3(256), 0, s, q);
 }
 
 // ---- operands --------------------------------------------------------------------------------
@@ -296,14 +285,13 @@ Buffers buffers(Carve& c, const osscar_gated_desc& q, const void* X, const void*
     if (b.few.parts > 1) sums = (size_t)b.few.parts * 2 * q.n * q.f * 4;
   } else if (!kept) {
     b.proj = deal<Big2, Small2>(q.n, q.f, (q.d + ks - 1) / ks, 1, f32);
-    sums = sums_bytes(b.proj, 2, 1, q.n, q.f);
+    sums = b.proj.sums;
   }
   if (backward) {
     b.dx = deal<Big1, Small1>(q.n, q.d, (q.f + ks - 1) / ks * 2, 1, f32);
     b.dw = deal<Big1, Small1>(q.rows_out ? q.f : q.d, q.rows_out ? q.d : q.f, (q.n + ks - 1) / ks, 2, f32);
-    const size_t x = sums_bytes(b.dx, 1, 1, q.n, q.d), w = sums_bytes(b.dw, 1, 2, q.d, q.f);
-    sums = sums > x ? sums : x;
-    sums = sums > w ? sums : w;
+    sums = sums > b.dx.sums ? sums : b.dx.sums;
+    sums = sums > 2 * b.dw.sums ? sums : 2 * b.dw.sums;
   }
   b.sums = c.take(sums);
   if (!backward && few(q)) return b;

@@ -135,6 +135,8 @@ __global__ __launch_bounds__(256) void int_join_kernel(const int* __restrict__ s
   tile::join<1>(sums, parts, M, N, e);
 }
 
+__global__ __launch_bounds__(256) void int_join_tiles_kernel(const Product<1> p, const IntOut e) { tile::join_tiles<Small, int>(p, e); }
+
 inline int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
 template <class S>
 int64_t tiles(int64_t n, int64_t m) { return (n + S::BM - 1) / S::BM * ((m + S::BN - 1) / S::BN); }
@@ -192,7 +194,7 @@ extern "C" size_t osscar_int_workspace_bytes(int64_t n, int64_t d1, int64_t m) {
   Carve c(nullptr);
   c.take((size_t)n * up16(d1));
   c.take((size_t)n * 4);
-  c.take(few_rows(n) ? (size_t)thin::deal<OP_K, thin::I8>(n, m, d1).parts * n * m * 4 : sums_bytes(deal_of(n, d1, m), 1, 1, n, m));
+  c.take(few_rows(n) ? (size_t)thin::deal<OP_K, thin::I8>(n, m, d1).parts * n * m * 4 : deal_of(n, d1, m).sums);
   return c.used + 256;
 }
 
@@ -249,15 +251,15 @@ extern "C" osscar_status osscar_int_product(const void* X_dev, int64_t n, int64_
   p.b[0].p[0] = reinterpret_cast<const char*>(Wq_dev); p.b[0].ldb = ldq; p.b[0].rows = (int)m; p.b[0].cols = (int)up16(d1);
   p.nseg = 1; p.k = (int)d1; p.M = (int)n; p.N = (int)m;
   const Deal d = deal_of(n, d1, m);
+  p.whole = d.whole;
   p.parts = d.parts;
   if (d.parts > 1) {
-    p.sums = c.take(sums_bytes(d, 1, 1, n, m));
+    p.sums = c.take(d.sums);
     if (!workspace_dev || c.used > workspace_bytes) return refuse_call(OSSCAR_ENOMEM, "osscar_int_product: workspace too small");
   }
-  const dim3 grid(d.tiles, 1, d.parts);
+  const dim3 grid(d.blocks);
   if (d.big) hipLaunchKernelGGL(int_product_kernel<Big>, grid, dim3(Big::WAVES * 64), 0, s, p, e);
   else hipLaunchKernelGGL(int_product_kernel<Small>, grid, dim3(Small::WAVES * 64), 0, s, p, e);
-  if (d.parts > 1)
-    hipLaunchKernelGGL(int_join_kernel, dim3(join_grid(n, m)), dim3(256), 0, s, reinterpret_cast<const int*>(p.sums), d.parts, (int)n, (int)m, e);
+  if (d.parts > 1) hipLaunchKernelGGL(int_join_tiles_kernel, dim3((unsigned)d.join), dim3(256), 0, s, p, e);
   return launched("osscar_int_product");
 }

@@ -144,8 +144,10 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
   typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
   __shared__ __align__(1024) char la[3][SA::BYTES], lb[S::NB][3][SB::BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN;
+  const int tiles_m = (q.M + S::BM - 1) / S::BM, tiles_n = (q.N + S::BN - 1) / S::BN;
+  const tile::Share share = tile::share_of(blockIdx.x, tiles_m * tiles_n, q.whole, q.parts);
   int tm, tn;
-  tile::tile_of(blockIdx.x, (q.M + S::BM - 1) / S::BM, (q.N + S::BN - 1) / S::BN, tm, tn);
+  tile::tile_of(share.t, tiles_m, tiles_n, tm, tn);
   SA sa;
   SB sb[S::NB];
   sa.open();
@@ -162,8 +164,8 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
 #pragma unroll
         for (int r = 0; r < 4; r++) acc[i][z][j][r] = 0;
   float xa[2][SA::NJ][8], xb[2][S::NB][SB::NJ][8];      // two stages under way
-  const int per = (q.k + KS - 1) / KS, all = per * q.nseg, span = (all + q.parts - 1) / q.parts;      // stages of a segment, of all, of a part
-  const int begin = min(all, (int)blockIdx.z * span), total = min(all - begin, span);
+  const int per = (q.k + KS - 1) / KS, all = per * q.nseg, span = (all + share.parts - 1) / share.parts;      // stages of a segment, of all, of a part
+  const int begin = min(all, share.part * span), total = min(all - begin, span);
   int seg = per > 0 ? begin / per : 0, k = per > 0 ? begin % per * KS : 0;
   bool anew = true;
   auto load = [&](int set) {      // the next stage
@@ -247,13 +249,13 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
       }
     }
   };
-  if (q.parts == 1) {
+  if (share.parts == 1) {
     epi.each(each);
   } else {
-    float* sums = reinterpret_cast<float*>(q.sums) + (int64_t)blockIdx.z * S::NB * q.M * q.N;
-    each([&](int m, int n, const float (&v)[S::NB][8], int N) {
+    float* sums = reinterpret_cast<float*>(q.sums) + (int64_t)share.slot * S::NB * S::BM * S::BN;
+    each([&](int m, int n, const float (&v)[S::NB][8], int) {
 #pragma unroll
-      for (int z = 0; z < S::NB; z++) put_f32(sums + ((int64_t)z * q.M + m) * N + n, v[z], N - n);
+      for (int z = 0; z < S::NB; z++) tile::put_sums(sums + (z * S::BM + m - tm * S::BM) * S::BN + n - tn * S::BN, v[z]);
     });
   }
 }

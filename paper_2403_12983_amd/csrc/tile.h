@@ -175,17 +175,22 @@ struct Product {
   Operand a, b[NB];
   int nseg, k;               // segments, contraction of each in elements
   int M, N;
-  int parts;                 // of the stages, a workgroup each (blockIdx.z), where the tiles alone do not fill the chip
-  void* sums;                // parts > 1: [part][matrix][m][n], 4 bytes each, for join()
+  int whole, parts;          // tiles from `whole` on have their stages dealt out in parts, a workgroup each
+  void* sums;                // of those: [part][tile][matrix][row][column], 4 bytes each, for join_tiles()
 };
-__device__ __forceinline__ void put_sums(float* p, const float (&v)[8], int most) { put_f32(p, v, most); }
-__device__ __forceinline__ void put_sums(int* p, const int (&v)[8], int most) {
-  float f[8];
-#pragma unroll
-  for (int e = 0; e < 8; e++) f[e] = __int_as_float(v[e]);
-  put_f32(reinterpret_cast<float*>(p), f, most);
+// What workgroup b does: part `part` of `parts` of tile t, whose sums are the slot-th of all parts'
+struct Share { int t, part, parts, slot; };
+__device__ __forceinline__ Share share_of(int b, int tiles, int whole, int parts) {
+  if (b < whole) return Share{b, 0, 1, 0};
+  const int j = b - whole, rest = tiles - whole;
+  return Share{whole + j % rest, j / rest, parts, j};
 }
-// Adds the parts' sums in order and goes on with them.  Epi::one(f) calls f(put) once, put(m, n, V (&v)[NB], N).
+__device__ __forceinline__ void put_sums(float* p, const float (&v)[8]) { put_f32(p, v, 8); }
+__device__ __forceinline__ void put_sums(int* p, const int (&v)[8]) {
+  *reinterpret_cast<v4i*>(p) = v4i{v[0], v[1], v[2], v[3]};
+  *reinterpret_cast<v4i*>(p + 4) = v4i{v[4], v[5], v[6], v[7]};
+}
+// Adds the parts' sums [part][matrix][m][n] in order and goes on with them.  Epi::one(f) calls f(put) once, put(m, n, V (&v)[NB], N).
 template <int NB, class V, class Epi>
 __device__ __forceinline__ void join(const V* sums, int parts, int M, int N, const Epi& epi) {
   epi.one([&](auto put) {
@@ -227,8 +232,10 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
   // An array per stage: with one array the compiler waits before every read of LDS for all requests under way.
   __shared__ __align__(1024) char a0[SA::BYTES], a1[SA::BYTES], b0[S::NB][SB::BYTES], b1[S::NB][SB::BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN;
+  const int tiles_m = (q.M + S::BM - 1) / S::BM, tiles_n = (q.N + S::BN - 1) / S::BN;
+  const Share share = S::CUT ? share_of(blockIdx.x, tiles_m * tiles_n, q.whole, q.parts) : Share{(int)blockIdx.x, 0, 1, 0};
   int tm, tn;
-  tile_of(blockIdx.x, (q.M + S::BM - 1) / S::BM, (q.N + S::BN - 1) / S::BN, tm, tn);
+  tile_of(share.t, tiles_m, tiles_n, tm, tn);
   SA sa;
   SB sb;
   sa.open(q.a, tm * S::BM, wave, lane);
@@ -244,9 +251,9 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
       for (int j = 0; j < S::FN; j++)
 #pragma unroll
         for (int r = 0; r < 4; r++) acc[i][z][j][r] = 0;
-  const int parts = S::CUT ? q.parts : 1;
+  const int parts = share.parts;
   const int per = (q.k + KS - 1) / KS, all = per * q.nseg, span = (all + parts - 1) / parts;      // stages of a segment, of all, of a part
-  const int begin = S::CUT ? min(all, (int)blockIdx.z * span) : 0, total = min(all - begin, span);
+  const int begin = S::CUT ? min(all, share.part * span) : 0, total = min(all - begin, span);
   // Workgroups begin at stages of their own, so that rows whose distance is a power of two do not all ask one memory channel at a time (contraction 2048: 7 %;
   // int8, 14336: 5 %).
   const int k0 = per > 0 && parts == 1 ? (tm + tn) % per * KS : 0;
@@ -356,29 +363,68 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
   if (parts == 1) {
     epi.each(each);
   } else {
-    typename T::val* sums = reinterpret_cast<typename T::val*>(q.sums) + (int64_t)blockIdx.z * S::NB * q.M * q.N;
-    each([&](int m, int n, const typename T::val (&v)[S::NB][8], int N) {
+    typename T::val* sums = reinterpret_cast<typename T::val*>(q.sums) + (int64_t)share.slot * S::NB * S::BM * S::BN;
+    each([&](int m, int n, const typename T::val (&v)[S::NB][8], int) {
 #pragma unroll
-      for (int z = 0; z < S::NB; z++) put_sums(sums + ((int64_t)z * q.M + m) * N + n, v[z], N - n);
+      for (int z = 0; z < S::NB; z++) put_sums(sums + (z * S::BM + m - tm * S::BM) * S::BN + n - tn * S::BN, v[z]);
     });
   }
 }
 
-// How a product is dealt out: the big shape where its tiles fill three quarters of the compute units, else the small one, the contraction cut into parts
-// where its tiles are fewer than two per compute unit, each of at least eight stages.
-constexpr int FILL = 192;
-struct Deal { bool big; int parts; unsigned tiles; };
-template <class SB, class SS>
-Deal deal(int64_t M, int64_t N, int64_t stages, int count, bool never_big) {
-  const int64_t big = (M + SB::BM - 1) / SB::BM * ((N + SB::BN - 1) / SB::BN), small = (M + SS::BM - 1) / SS::BM * ((N + SS::BN - 1) / SS::BN);
-  if (!never_big && big * count >= FILL) return Deal{true, 1, (unsigned)big};
-  if (small == 0) return Deal{false, 1, 0};
-  int64_t parts = 512 / (small * count);
-  if (parts > stages / 8) parts = stages / 8;
-  if (parts > 32) parts = 32;
-  return Deal{false, parts < 1 ? 1 : (int)parts, (unsigned)small};
+// Adds the sums of the tiles that were dealt out in parts, in order, and goes on with them, eight columns a thread; a workgroup takes 2048 elements of a tile.
+template <class S, class V, class Epi>
+__device__ __forceinline__ void join_tiles(const Product<S::NB>& q, const Epi& epi) {
+  constexpr int PER = S::BM * S::BN / 2048;
+  typedef V v4 __attribute__((ext_vector_type(4)));
+  const int tiles_m = (q.M + S::BM - 1) / S::BM, tiles_n = (q.N + S::BN - 1) / S::BN, rest = tiles_m * tiles_n - q.whole;
+  const int t = blockIdx.x / PER, i = blockIdx.x % PER * 256 + threadIdx.x, row = i / (S::BN / 8), col = i % (S::BN / 8) * 8;
+  int tm, tn;
+  tile_of(q.whole + t, tiles_m, tiles_n, tm, tn);
+  const int m = tm * S::BM + row, n = tn * S::BN + col;
+  if (m >= q.M || n >= q.N) return;
+  epi.each([&](auto put) {
+    V v[S::NB][8];
+#pragma unroll
+    for (int z = 0; z < S::NB; z++) {
+#pragma unroll
+      for (int e = 0; e < 8; e++) v[z][e] = 0;
+      for (int p = 0; p < q.parts; p++) {
+        const v4* w = reinterpret_cast<const v4*>(reinterpret_cast<const V*>(q.sums) + (((int64_t)p * rest + t) * S::NB + z) * (S::BM * S::BN) + row * S::BN + col);
+        const v4 a = w[0], b = w[1];
+#pragma unroll
+        for (int e = 0; e < 4; e++) { v[z][e] += a[e]; v[z][4 + e] += b[e]; }
+      }
+    }
+    put(m, n, v, q.N);
+  });
 }
-inline size_t sums_bytes(const Deal& d, int nb, int count, int64_t M, int64_t N) { return d.parts > 1 ? (size_t)d.parts * nb * count * M * N * 4 : 0; }
+
+// How a product of `stages` stages is dealt out, one of `count` in a launch.  The chip takes 256 big tiles at a time or 512 small ones, a big one, four times a small one,
+// in BIG times its time (8192 x 8192 x 8192 bf16: 1500 TFLOP/s and 1200).  Small tiles past the last full 512 would keep part of the chip busy for
+// as long as the rest: their stages are dealt out in parts of at least eight, where that makes up for the sums' way through memory (as long as about JOIN stages).
+// What takes fewer of these units is taken.
+constexpr double BIG = 1.6;
+struct Deal { bool big; int whole, parts; unsigned blocks; size_t sums, join; };      // sums: bytes of a product's; join: workgroups that add them
+template <class SB, class SS>
+Deal deal(int64_t M, int64_t N, int64_t stages, int count, bool f32) {
+  const int64_t big = (M + SB::BM - 1) / SB::BM * ((N + SB::BN - 1) / SB::BN), small = (M + SS::BM - 1) / SS::BM * ((N + SS::BN - 1) / SS::BN);
+  if (small == 0) return Deal{false, 0, 1, 0, 0, 0};
+  const int64_t slots = 512 / count, rest = small % slots;
+  int64_t whole = small - rest, parts = 1;
+  const double JOIN = f32 ? 3 : 8, alone = 2 * rest > slots ? 1 : 0.65;      // (a workgroup alone on its compute unit takes less time than one of two)
+  double last = rest > 0 ? alone : 0;
+  if (rest > 0) {
+    parts = slots / rest;
+    if (parts > stages / 8) parts = stages / 8;
+    if (parts > 32) parts = 32;
+    const double cut = parts > 1 ? 1. / parts + JOIN / stages : 1;
+    if (parts < 2 || (whole > 0 && cut >= alone)) parts = 1;
+    else last = cut;
+  }
+  if (!f32 && (big * count + 255) / 256 * BIG <= small / slots + last) return Deal{true, (int)big, 1, (unsigned)big, 0, 0};
+  if (parts == 1) return Deal{false, (int)small, 1, (unsigned)small, 0, 0};
+  return Deal{false, (int)whole, (int)parts, (unsigned)(whole + rest * parts), (size_t)rest * parts * SS::NB * SS::BM * SS::BN * 4, (size_t)rest * (SS::BM * SS::BN / 2048)};
+}
 
 }  // namespace tile
 }  // namespace osscar
