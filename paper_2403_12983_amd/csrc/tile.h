@@ -401,25 +401,28 @@ __device__ __forceinline__ void join_tiles(const Product<S::NB>& q, const Epi& e
 
 // How a product of `stages` stages is dealt out, one of `count` in a launch.  The chip takes 256 big tiles at a time or 512 small ones, a big one, four times a small one,
 // in BIG times its time (8192 x 8192 x 8192 bf16: 1500 TFLOP/s and 1200).  Small tiles past the last full 512 would keep part of the chip busy for
-// as long as the rest: their stages are dealt out in parts of at least eight, where that makes up for the sums' way through memory (as long as about JOIN stages).
-// What takes fewer of these units is taken.
+// as long as the rest: their stages are dealt out in parts of at least eight, so many that they fill it once, twice or three times, where that makes up for the
+// launch that adds the sums and their way through memory (as long as about LAUNCH stages, and SUMS for 512 tiles' sums).  What takes fewer of these units is taken.
 constexpr double BIG = 1.6;
 struct Deal { bool big; int whole, parts; unsigned blocks; size_t sums, join; };      // sums: bytes of a product's; join: workgroups that add them
 template <class SB, class SS>
 Deal deal(int64_t M, int64_t N, int64_t stages, int count, bool f32) {
   const int64_t big = (M + SB::BM - 1) / SB::BM * ((N + SB::BN - 1) / SB::BN), small = (M + SS::BM - 1) / SS::BM * ((N + SS::BN - 1) / SS::BN);
   if (small == 0) return Deal{false, 0, 1, 0, 0, 0};
-  const int64_t slots = 512 / count, rest = small % slots;
-  int64_t whole = small - rest, parts = 1;
-  const double JOIN = f32 ? 3 : 8, alone = 2 * rest > slots ? 1 : 0.65;      // (a workgroup alone on its compute unit takes less time than one of two)
-  double last = rest > 0 ? alone : 0;
-  if (rest > 0) {
-    parts = slots / rest;
-    if (parts > stages / 8) parts = stages / 8;
-    if (parts > 32) parts = 32;
-    const double cut = parts > 1 ? 1. / parts + JOIN / stages : 1;
-    if (parts < 2 || (whole > 0 && cut >= alone)) parts = 1;
-    else last = cut;
+  const int64_t slots = 512 / count, rest = small % slots, whole = small - rest;
+  const double LAUNCH = f32 ? 1 : 2, SUMS = f32 ? 2.5 : 15;
+  auto rounds = [&](int64_t n) {      // (a workgroup alone on its compute unit takes less time than one of two)
+    const int64_t over = n % slots;
+    return n / slots + (2 * over > slots ? 1 : over > 0 ? 0.75 : 0);
+  };
+  double last = rounds(rest);
+  int64_t parts = 1;
+  for (int r = 1; r <= 3 && rest > 0; r++) {
+    int64_t p = r * slots / rest;
+    if (p > stages / 8) p = stages / 8;
+    if (p > 32) p = 32;
+    const double cut = p > 1 ? rounds(rest * p) / p + (LAUNCH + SUMS * rest * p / slots) / stages : 2;
+    if (cut < last) { last = cut; parts = p; }
   }
   if (!f32 && (big * count + 255) / 256 * BIG <= small / slots + last) return Deal{true, (int)big, 1, (unsigned)big, 0, 0};
   if (parts == 1) return Deal{false, (int)small, 1, (unsigned)small, 0, 0};
