@@ -190,10 +190,10 @@ __global__ __launch_bounds__(S::WAVES * 64, 2) void gated_split_kernel(const Pai
 }
 
 // ---- shapes ----------------------------------------------------------------------------------
-typedef Shape<2, 2, 8, 4, 2, false> Big2;       // 256 x (128 + 128), four waves
-typedef Shape<2, 2, 4, 2, 2, true> Small2;     // 128 x (64 + 64), four waves
-typedef Shape<2, 2, 8, 8, 1, false> Big1;       // 256 x 256
-typedef Shape<2, 2, 4, 4, 1, true> Small1;     // 128 x 128
+typedef Shape<2, 2, 8, 4, 2> Big2;       // 256 x (128 + 128), four waves
+typedef Shape<2, 2, 4, 2, 2> Small2;     // 128 x (64 + 64), four waves
+typedef Shape<2, 2, 8, 8, 1> Big1;       // 256 x 256
+typedef Shape<2, 2, 4, 4, 1> Small1;     // 128 x 128
 template <class S, class Epi>
 __global__ __launch_bounds__(256) void gated_join_tiles_kernel(const Pair<S::NB, Epi> q) {
   tile::join_tiles<S, float>(q.p[blockIdx.y], q.e[blockIdx.y]);
@@ -210,7 +210,9 @@ void launch_product(Pair<SB::NB, Epi>& q, int count, bool f32, const Deal& d, ch
   if (f32) hipLaunchKernelGGL((gated_split_kernel<AM, BMODE, SS, Epi>), grid, dim3(SS::WAVES * 64), 0, s, q);
   else if (d.big) hipLaunchKernelGGL((gated_product_kernel<AM, BMODE, SB, Epi>), grid, dim3(SB::WAVES * 64), 0, s, q);
   else hipLaunchKernelGGL((gated_product_kernel<AM, BMODE, SS, Epi>), grid, dim3(SS::WAVES * 64), 0, s, q);
-  if (d.parts > 1) hipLaunchKernelGGL((gated_join_tiles_kernel<SS, Epi>), dim3((unsigned)d.join, count), dim3(256), 0, s, q);
+  const dim3 join((unsigned)d.join, count);
+  if (d.parts > 1 && d.big) hipLaunchKernelGGL((gated_join_tiles_kernel<SB, Epi>), join, dim3(256), 0, s, q);
+  else if (d.parts > 1) hipLaunchKernelGGL((gated_join_tiles_kernel<SS, Epi>), join, dim3(256), 0, s, q);
 }
 
 // ---- operands --------------------------------------------------------------------------------

@@ -119,8 +119,8 @@ struct IntOut {
     });
   }
 };
-typedef Shape<2, 2, 8, 8, 1, false> Big;        // 256 x 256, four waves
-typedef Shape<2, 2, 4, 4, 1, true> Small;      // 128 x 128, four waves
+typedef Shape<2, 2, 8, 8, 1> Big;        // 256 x 256, four waves
+typedef Shape<2, 2, 4, 4, 1> Small;      // 128 x 128, four waves
 
 template <class S>
 __global__ __launch_bounds__(S::WAVES * 64, 1) void int_product_kernel(const Product<1> p, const IntOut e) {
@@ -135,7 +135,8 @@ __global__ __launch_bounds__(256) void int_join_kernel(const int* __restrict__ s
   tile::join<1>(sums, parts, M, N, e);
 }
 
-__global__ __launch_bounds__(256) void int_join_tiles_kernel(const Product<1> p, const IntOut e) { tile::join_tiles<Small, int>(p, e); }
+template <class S>
+__global__ __launch_bounds__(256) void int_join_tiles_kernel(const Product<1> p, const IntOut e) { tile::join_tiles<S, int>(p, e); }
 
 inline int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
 template <class S>
@@ -260,6 +261,7 @@ extern "C" osscar_status osscar_int_product(const void* X_dev, int64_t n, int64_
   const dim3 grid(d.blocks);
   if (d.big) hipLaunchKernelGGL(int_product_kernel<Big>, grid, dim3(Big::WAVES * 64), 0, s, p, e);
   else hipLaunchKernelGGL(int_product_kernel<Small>, grid, dim3(Small::WAVES * 64), 0, s, p, e);
-  if (d.parts > 1) hipLaunchKernelGGL(int_join_tiles_kernel, dim3((unsigned)d.join), dim3(256), 0, s, p, e);
+  if (d.parts > 1 && d.big) hipLaunchKernelGGL(int_join_tiles_kernel<Big>, dim3((unsigned)d.join), dim3(256), 0, s, p, e);
+  else if (d.parts > 1) hipLaunchKernelGGL(int_join_tiles_kernel<Small>, dim3((unsigned)d.join), dim3(256), 0, s, p, e);
   return launched("osscar_int_product");
 }

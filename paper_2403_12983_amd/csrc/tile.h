@@ -75,10 +75,8 @@ __device__ __forceinline__ void settled(V& c) { asm volatile("" : "+a"(c)); }
 
 // The shape of a workgroup: WM x WN waves, each of FM x (NB FN) tiles of 16 x 16.  NB: matrices on the B side whose columns a wave takes
 // alike (gate and up projection), FN tiles of each.
-// CUT: its products may be dealt out in parts.
-template <int WM_, int WN_, int FM_, int FN_, int NB_, bool CUT_>
+template <int WM_, int WN_, int FM_, int FN_, int NB_>
 struct Shape {
-  static constexpr bool CUT = CUT_;
   static constexpr int WM = WM_, WN = WN_, FM = FM_, FN = FN_, NB = NB_, WAVES = WM * WN, BM = WM * FM * 16, BN = WN * FN * 16;
 };
 
@@ -233,7 +231,7 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
   __shared__ __align__(1024) char a0[SA::BYTES], a1[SA::BYTES], b0[S::NB][SB::BYTES], b1[S::NB][SB::BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN;
   const int tiles_m = (q.M + S::BM - 1) / S::BM, tiles_n = (q.N + S::BN - 1) / S::BN;
-  const Share share = S::CUT ? share_of(blockIdx.x, tiles_m * tiles_n, q.whole, q.parts) : Share{(int)blockIdx.x, 0, 1, 0};
+  const Share share = share_of(blockIdx.x, tiles_m * tiles_n, q.whole, q.parts);
   int tm, tn;
   tile_of(share.t, tiles_m, tiles_n, tm, tn);
   SA sa;
@@ -253,7 +251,7 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
         for (int r = 0; r < 4; r++) acc[i][z][j][r] = 0;
   const int parts = share.parts;
   const int per = (q.k + KS - 1) / KS, all = per * q.nseg, span = (all + parts - 1) / parts;      // stages of a segment, of all, of a part
-  const int begin = S::CUT ? min(all, share.part * span) : 0, total = min(all - begin, span);
+  const int begin = min(all, share.part * span), total = min(all - begin, span);
   // Workgroups begin at stages of their own, so that rows whose distance is a power of two do not all ask one memory channel at a time (contraction 2048: 7 %;
   // int8, 14336: 5 %).
   const int k0 = per > 0 && parts == 1 ? (tm + tn) % per * KS : 0;
@@ -400,33 +398,36 @@ __device__ __forceinline__ void join_tiles(const Product<S::NB>& q, const Epi& e
 }
 
 // How a product of `stages` stages is dealt out, one of `count` in a launch.  The chip takes 256 big tiles at a time or 512 small ones, a big one, four times a small one,
-// in BIG times its time (8192 x 8192 x 8192 bf16: 1500 TFLOP/s and 1200).  Small tiles past the last full 512 would keep part of the chip busy for
-// as long as the rest: their stages are dealt out in parts of at least eight, so many that they fill it once, twice or three times, where that makes up for the
-// launch that adds the sums and their way through memory (as long as about LAUNCH stages, and SUMS for 512 tiles' sums).  What takes fewer of these units is taken.
+// in BIG times its time (8192 x 8192 x 8192 bf16: 1500 TFLOP/s and 1200).  Tiles past the last full 256 or 512 would keep part of the chip busy for as
+// long as all: their stages are dealt out in parts of at least eight, so many that they fill it once, twice or three times, where that makes up for
+// the launch that adds the sums and their way through memory (as long as about `launch` stages, and `sums` for a chip full of tiles).  The shape that takes less time
+// is taken.
 constexpr double BIG = 1.6;
-struct Deal { bool big; int whole, parts; unsigned blocks; size_t sums, join; };      // sums: bytes of a product's; join: workgroups that add them
-template <class SB, class SS>
-Deal deal(int64_t M, int64_t N, int64_t stages, int count, bool f32) {
-  const int64_t big = (M + SB::BM - 1) / SB::BM * ((N + SB::BN - 1) / SB::BN), small = (M + SS::BM - 1) / SS::BM * ((N + SS::BN - 1) / SS::BN);
-  if (small == 0) return Deal{false, 0, 1, 0, 0, 0};
-  const int64_t slots = 512 / count, rest = small % slots, whole = small - rest;
-  const double LAUNCH = f32 ? 1 : 2, SUMS = f32 ? 2.5 : 15;
-  auto rounds = [&](int64_t n) {      // (a workgroup alone on its compute unit takes less time than one of two)
-    const int64_t over = n % slots;
-    return n / slots + (2 * over > slots ? 1 : over > 0 ? 0.75 : 0);
-  };
-  double last = rounds(rest);
-  int64_t parts = 1;
+struct Plan { double time; int64_t whole, parts, blocks; };      // time: rounds of the chip
+inline Plan plan(int64_t tiles, int64_t slots, int64_t stages, double alone, double launch, double sums) {
+  const int64_t rest = tiles % slots;
+  auto rounds = [&](int64_t n) { return n / slots + (2 * (n % slots) > slots ? 1 : n % slots > 0 ? alone : 0); };
+  Plan best{rounds(tiles), tiles, 1, tiles};
   for (int r = 1; r <= 3 && rest > 0; r++) {
     int64_t p = r * slots / rest;
     if (p > stages / 8) p = stages / 8;
     if (p > 32) p = 32;
-    const double cut = p > 1 ? rounds(rest * p) / p + (LAUNCH + SUMS * rest * p / slots) / stages : 2;
-    if (cut < last) { last = cut; parts = p; }
+    if (p < 2) continue;
+    const double time = tiles / slots + rounds(rest * p) / p + (launch + sums * rest * p / slots) / stages;
+    if (time < best.time) best = Plan{time, tiles - rest, p, tiles - rest + rest * p};
   }
-  if (!f32 && (big * count + 255) / 256 * BIG <= small / slots + last) return Deal{true, (int)big, 1, (unsigned)big, 0, 0};
-  if (parts == 1) return Deal{false, (int)small, 1, (unsigned)small, 0, 0};
-  return Deal{false, (int)whole, (int)parts, (unsigned)(whole + rest * parts), (size_t)rest * parts * SS::NB * SS::BM * SS::BN * 4, (size_t)rest * (SS::BM * SS::BN / 2048)};
+  return best;
+}
+struct Deal { bool big; int whole, parts; unsigned blocks; size_t sums, join; };      // sums: bytes of a product's; join: workgroups that add them
+template <class SB, class SS>
+Deal deal(int64_t M, int64_t N, int64_t stages, int count, bool f32) {
+  const int64_t big = (M + SB::BM - 1) / SB::BM * ((N + SB::BN - 1) / SB::BN), small = (M + SS::BM - 1) / SS::BM * ((N + SS::BN - 1) / SS::BN);
+  // (a small tile alone on its compute unit takes less time than one of two)
+  const Plan s = plan(small, 512 / count, stages, 0.75, f32 ? 1 : 2, f32 ? 2.5 : 15), b = f32 ? s : plan(big, 256 / count, stages, 1, 1.2, 18);
+  const bool take = !f32 && b.time * BIG <= s.time;
+  const Plan& p = take ? b : s;
+  const int64_t rest = p.parts > 1 ? (take ? big : small) - p.whole : 0, area = take ? SB::BM * SB::BN : SS::BM * SS::BN;
+  return Deal{take, (int)p.whole, (int)p.parts, (unsigned)p.blocks, (size_t)(rest * p.parts * SS::NB * area * 4), (size_t)(rest * (area / 2048))};
 }
 
 }  // namespace tile
