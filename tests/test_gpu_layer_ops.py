@@ -156,6 +156,13 @@ def test_gated_float32_projection_near_zero(osscar, rows):
         assert ((got.double() - want).norm() / want.norm()).item() <= 1.25 * E * (math.sqrt(6) + 0.28 * math.sqrt(d / 32))
 
 
+@pytest.mark.parametrize("dtype,rows", [(torch.bfloat16, "in"), (torch.bfloat16, "out"), (torch.float32, "out")])
+@pytest.mark.parametrize("n,d,f", [(2300, 4100, 4100), (1100, 2700, 1900)])
+def test_gated_tiles_past_a_full_chip(osscar, n, d, f, dtype, rows):
+    """more tiles of either shape than the chip takes at a time: the last ones in parts"""
+    _check_gated(osscar, n, d, f, dtype, rows, ACTS[(n + d) % 3], seed=n + f)
+
+
 @pytest.mark.parametrize("name", ACTS)
 def test_gated_activation_over_its_range(osscar, name):
     """H of single products: g runs over the range of float32, u = 1"""
@@ -335,6 +342,16 @@ def test_int_product_large_tiles_with_columns_left_over(osscar, m):
     g = _gen(m)
     X, W = _randn(g, 2050, 300, dtype=torch.bfloat16), _randn(g, 300, m)
     Wq, ws = osscar.osscar_int_weights(W)
+    for out in (torch.bfloat16, torch.float32):
+        _check_int(osscar, X, Wq, ws, _randn(g, m), out)
+
+
+@pytest.mark.parametrize("n,d1,m", [(2300, 8200, 8190), (1400, 3000, 6407)])
+def test_int_product_tiles_past_a_full_chip(osscar, n, d1, m):
+    """more tiles of either shape than the chip takes at a time: the last ones in parts"""
+    g = _gen(n)
+    X = _randn(g, n, d1, dtype=torch.bfloat16)
+    Wq, ws = osscar.osscar_int_weights(_randn(g, d1, m))
     for out in (torch.bfloat16, torch.float32):
         _check_int(osscar, X, Wq, ws, _randn(g, m), out)
 
