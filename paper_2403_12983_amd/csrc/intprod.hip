@@ -1,4 +1,6 @@
-// Products in 8-bit integers with a scale per token and per output channel, and the quantisation of both sides.
+// Products in 8-bit integers with a scale per token and per output channel, and the quantisation of both sides: s_i = max_k |x_ik| / 127, q_ik = rint(x_ik / s_i),
+// y_ij = s_i w_j sum_k q_ik Q_jk (+ b_j), the sums exact in int32.  14336 x 7168 with given digits: one row 19 us (5.4 TB/s, thin.h), 64 rows 30 us, 8192 rows 0.65 ms
+// (2.6 POP/s, tile.h; the library's largest product 2.5).
 #include "ops.h"
 #include "thin.h"
 #include "tile.h"
@@ -17,7 +19,9 @@ __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(
 typedef int8_t s8x8 __attribute__((ext_vector_type(8)));
 
 // One row per workgroup of T threads, read twice (the second time from cache); eight values per thread and step.  Bound by reading X and writing Xq;
-// few rows: by the latency of the steps, so that they get 1024 threads each.
+// few rows: by the latency of the steps, so that they get 1024 threads each.  x (1 / s) is within 3 2^-24 127 = 2.3e-5 of the rounded quotient x / s, so that
+// both have the same nearest integer unless one lies closer than that to a half; only there, and where 1 / s might be no normal number, is
+// divided (everywhere: 97 us for 8192 x 14336 bf16; so 91, 3.9 TB/s).
 template <int T>
 __global__ __launch_bounds__(T) void int_rows_kernel(const void* __restrict__ X, int f32, int d1, int64_t ldx, int8_t* __restrict__ Xq, int64_t ldq,
                                                        float* __restrict__ scale) {
@@ -35,14 +39,23 @@ __global__ __launch_bounds__(T) void int_rows_kernel(const void* __restrict__ X,
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < T / 64; w++) most = max(most, sh[w]);
-  const float s = scale_of(most), u = usable(s);
+  const float s = scale_of(most), u = usable(s), r = 1.f / u;
+  const bool quick = u > 1e-30f && u < 1e30f;
   if (threadIdx.x == 0) scale[row] = s;
   for (int k = threadIdx.x * 8; k < ldq; k += T * 8) {
     float v[8];
-    get_values(X, row * ldx + k, f32, v, d1 - k);
+    get_values(X, row * ldx + k, f32, v, d1 - k);      // (zeros past d1)
     s8x8 w;
+    float far = quick ? 0.f : 1.f;
 #pragma unroll
-    for (int e = 0; e < 8; e++) w[e] = (int8_t)(k + e < d1 ? digit(v[e], u) : 0);
+    for (int e = 0; e < 8; e++) {
+      const float y = v[e] * r, q = rintf(y);
+      far = fmaxf(far, fabsf(y - q));
+      w[e] = (int8_t)q;
+    }
+    if (far > 0.49996f)
+#pragma unroll
+      for (int e = 0; e < 8; e++) w[e] = (int8_t)(k + e < d1 ? digit(v[e], u) : 0);
     *reinterpret_cast<s8x8*>(Xq + row * ldq + k) = w;
   }
 }

@@ -145,7 +145,7 @@ __device__ __forceinline__ void choose(const uint64_t* ranks, int n, int k, F pu
 // random logits, whatever the row's length; a step where no thread has one costs a comparison per 32 logits.  At the end the k best packets are
 // chosen by counting, read again, and the k best logits in them chosen likewise.  Where the list is too short (ever larger logits), or with NaN and infinity,
 // the part is read k times more.
-// Bound by reading the logits; per logit about 10 slots of the vector unit, four of them the exponential.
+// Bound by reading the logits (4096 x 50304 bf16, five alternatives: 89 us, 4.6 TB/s; float32 6.0 TB/s); per logit about 10 slots of the vector unit, four of them the exponential.
 template <bool F32>
 __global__ __launch_bounds__(T) void logprobs_kernel(const void* __restrict__ logits, int vocab, int64_t ld, int span, Row out, Stat* part_stat, uint64_t* part_rank) {
   __shared__ Stat st[T / 64];
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(T) void logprobs_kernel(const void* __restrict__ lo
   __syncthreads();
   choose(cand, count2, k, put);
 }
-// The parts of a row put together, a row per workgroup.
+// The parts of a row put together, a row per workgroup: 4 x 131072 float32 13 us for both launches with eight alternatives, 22 us with 64, 8 us without.
 __global__ __launch_bounds__(T) void logprobs_join_kernel(const void* __restrict__ logits, int f32, int vocab, int64_t ld, int parts, Row out,
                                                           const Stat* __restrict__ part_stat, const uint64_t* __restrict__ part_rank) {
   __shared__ uint64_t ranks[JOIN], best[JOIN];
@@ -338,7 +338,7 @@ int parts_of(int64_t n, int64_t vocab, int32_t top) {
 }
 
 // Gradient.  A workgroup takes CHUNK columns of a row; the few columns that have a term of their own (target, alternatives) are computed by a
-// thread each from logits read before the others are written.
+// thread each from logits read before the others are written.  Bound by reading and writing: 8192 x 32000 bf16 187 us, 5.6 TB/s.
 constexpr int CHUNK = T * 8 * 4;
 __global__ __launch_bounds__(T) void logprobs_backward_kernel(const void* logits, int f32, int vocab, int64_t ld, const int64_t* __restrict__ targets, float scale,
                                                               const float* __restrict__ lse, const float* __restrict__ dlogp, const float* __restrict__ entropy,
