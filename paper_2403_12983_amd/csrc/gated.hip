@@ -195,12 +195,14 @@ typedef Shape<2, 2, 8, 4, 2> Big2;       // 256 x (128 + 128), four waves
 typedef Shape<2, 2, 4, 2, 2> Small2;     // 128 x (64 + 64), four waves
 typedef Shape<2, 2, 8, 8, 1> Big1;       // 256 x 256
 typedef Shape<2, 2, 4, 4, 1> Small1;     // 128 x 128
+typedef Shape<1, 4, 4, 2, 2> Flat2;      // 64 x (128 + 128)
+typedef Shape<1, 4, 4, 4, 1> Flat1;      // 64 x 256
 template <class S, class Epi>
 __global__ __launch_bounds__(256) void gated_join_tiles_kernel(const Pair<S::NB, Epi> q) {
   tile::join_tiles<S, float>(q.p[blockIdx.y], q.e[blockIdx.y]);
 }
 // `count` products of one launch; sums: d.sums for each
-template <int AM, int BMODE, class SB, class SS, class Epi>
+template <int AM, int BMODE, class SB, class SS, class SF, class Epi>
 void launch_product(Pair<SB::NB, Epi>& q, int count, bool f32, const Deal& d, char* sums, hipStream_t s) {
   for (int c = 0; c < count; c++) {
     q.p[c].whole = d.whole;
@@ -208,12 +210,16 @@ void launch_product(Pair<SB::NB, Epi>& q, int count, bool f32, const Deal& d, ch
     q.p[c].sums = sums + c * d.sums;
   }
   const dim3 grid(d.blocks, count);
-  if (f32) hipLaunchKernelGGL((gated_split_kernel<AM, BMODE, SS, Epi>), grid, dim3(SS::WAVES * 64), 0, s, q);
-  else if (d.big) hipLaunchKernelGGL((gated_product_kernel<AM, BMODE, SB, Epi>), grid, dim3(SB::WAVES * 64), 0, s, q);
-  else hipLaunchKernelGGL((gated_product_kernel<AM, BMODE, SS, Epi>), grid, dim3(SS::WAVES * 64), 0, s, q);
+  if constexpr (AM == OP_K)
+    if (d.pick == FLAT) hipLaunchKernelGGL((gated_split_kernel<AM, BMODE, SF, Epi>), grid, dim3(SF::WAVES * 64), 0, s, q);
+  if (d.pick == SMALL && f32) hipLaunchKernelGGL((gated_split_kernel<AM, BMODE, SS, Epi>), grid, dim3(SS::WAVES * 64), 0, s, q);
+  else if (d.pick == BIG_TILE) hipLaunchKernelGGL((gated_product_kernel<AM, BMODE, SB, Epi>), grid, dim3(SB::WAVES * 64), 0, s, q);
+  else if (d.pick == SMALL) hipLaunchKernelGGL((gated_product_kernel<AM, BMODE, SS, Epi>), grid, dim3(SS::WAVES * 64), 0, s, q);
   const dim3 join((unsigned)d.join, count);
-  if (d.parts > 1 && d.big) hipLaunchKernelGGL((gated_join_tiles_kernel<SB, Epi>), join, dim3(256), 0, s, q);
-  else if (d.parts > 1) hipLaunchKernelGGL((gated_join_tiles_kernel<SS, Epi>), join, dim3(256), 0, s, q);
+  if (d.parts < 2) return;
+  if (d.pick == FLAT) hipLaunchKernelGGL((gated_join_tiles_kernel<SF, Epi>), join, dim3(256), 0, s, q);
+  else if (d.pick == BIG_TILE) hipLaunchKernelGGL((gated_join_tiles_kernel<SB, Epi>), join, dim3(256), 0, s, q);
+  else hipLaunchKernelGGL((gated_join_tiles_kernel<SS, Epi>), join, dim3(256), 0, s, q);
 }
 
 // ---- operands --------------------------------------------------------------------------------
@@ -276,7 +282,8 @@ struct Buffers {
 };
 // The products of few rows (thin.h says where)
 bool few(const osscar_gated_desc& q) {
-  return q.dtype == OSSCAR_F32 ? q.n <= 32 : q.rows_out && q.n <= 16 && (q.d * q.f <= (1 << 24) || q.unaligned || !operand_fits(nullptr, q.ldw, q.d, 2));
+  if (q.dtype == OSSCAR_F32) return q.n <= 16 || (q.n <= 32 && q.d * q.f <= (1 << 25));
+  return q.rows_out && q.n <= 16 && (q.d * q.f <= (1 << 24) || q.unaligned || !operand_fits(nullptr, q.ldw, q.d, 2));
 }
 Buffers buffers(Carve& c, const osscar_gated_desc& q, const void* X, const void* Wg, const void* Wu, int backward, bool kept) {
   Buffers b{};
@@ -287,12 +294,14 @@ Buffers buffers(Carve& c, const osscar_gated_desc& q, const void* X, const void*
     b.few = !f32 ? thin::deal<OP_K, thin::BF16>(q.n, q.f, q.d) : q.rows_out ? thin::deal<OP_K, thin::F32>(q.n, q.f, q.d) : thin::deal<OP_T, thin::F32>(q.n, q.f, q.d);
     if (b.few.parts > 1) sums = (size_t)b.few.parts * 2 * q.n * q.f * 4;
   } else if (!kept) {
-    b.proj = deal<Big2, Small2>(q.n, q.f, (q.d + ks - 1) / ks, 1, f32);
+    const int64_t stages = (q.d + ks - 1) / ks;
+    b.proj = f32 ? deal_split<Flat2, Small2>(q.n, q.f, stages, 1, true) : deal<Big2, Small2>(q.n, q.f, stages, 1);
     sums = b.proj.sums;
   }
   if (backward) {
-    b.dx = deal<Big1, Small1>(q.n, q.d, (q.f + ks - 1) / ks * 2, 1, f32);
-    b.dw = deal<Big1, Small1>(q.rows_out ? q.f : q.d, q.rows_out ? q.d : q.f, (q.n + ks - 1) / ks, 2, f32);
+    const int64_t sx = (q.f + ks - 1) / ks * 2, sw = (q.n + ks - 1) / ks, M = q.rows_out ? q.f : q.d, N = q.rows_out ? q.d : q.f;
+    b.dx = f32 ? deal_split<Flat1, Small1>(q.n, q.d, sx, 1, true) : deal<Big1, Small1>(q.n, q.d, sx, 1);
+    b.dw = f32 ? deal_split<Flat1, Small1>(M, N, sw, 2, false) : deal<Big1, Small1>(M, N, sw, 2);
     sums = sums > b.dx.sums ? sums : b.dx.sums;
     sums = sums > 2 * b.dw.sums ? sums : 2 * b.dw.sums;
   }
@@ -353,13 +362,13 @@ void thin_projections(const thin::Product<2>& p, bool f32, bool rows_out, const 
     hipLaunchKernelGGL(gated_join_kernel, dim3(join_grid(p.M, p.N)), dim3(256), 0, s, reinterpret_cast<const float*>(p.sums), d.parts, p.M, p.N, e);
 }
 // X Wg, X Wu with epilogue e
-osscar_status projections(const osscar_gated_desc& q, const Buffers& b, const void* X, const void* Wg, const void* Wu, const GatedOut& e, hipStream_t s) {
+void projections(const osscar_gated_desc& q, const Buffers& b, const void* X, const void* Wg, const void* Wu, const GatedOut& e, hipStream_t s) {
   if (few(q)) {
     const int es = q.dtype == OSSCAR_F32 ? 4 : 2;
     const thin::Product<2> p{reinterpret_cast<const char*>(X), {reinterpret_cast<const char*>(Wg), reinterpret_cast<const char*>(Wu)}, q.ldx * es, q.ldw * es,
                              (int)q.n, (int)q.f, (int)q.d, b.few.parts, b.sums};
     thin_projections(p, q.dtype == OSSCAR_F32, q.rows_out != 0, b.few, e, s);
-    return OSSCAR_OK;
+    return;
   }
   Pair<2, GatedOut> two{};
   Product<2>& p = two.p[0];
@@ -367,9 +376,8 @@ osscar_status projections(const osscar_gated_desc& q, const Buffers& b, const vo
   p.M = (int)q.n; p.N = (int)q.f; p.k = (int)q.d;
   const Operand w[2] = {b.wg.operand(), b.wu.operand()};
   add_segment(p, b.x.operand(), w);
-  if (q.rows_out) launch_product<OP_K, OP_K, Big2, Small2>(two, 1, e.f32, b.proj, b.sums, s);
-  else launch_product<OP_K, OP_T, Big2, Small2>(two, 1, e.f32, b.proj, b.sums, s);
-  return OSSCAR_OK;
+  if (q.rows_out) launch_product<OP_K, OP_K, Big2, Small2, Flat2>(two, 1, e.f32, b.proj, b.sums, s);
+  else launch_product<OP_K, OP_T, Big2, Small2, Flat2>(two, 1, e.f32, b.proj, b.sums, s);
 }
 
 }  // namespace
@@ -395,8 +403,8 @@ extern "C" osscar_status osscar_gated_forward(const osscar_gated_desc* desc, con
   const int f32 = q.dtype == OSSCAR_F32;
   if (!few(q)) make_copies({&b.x, &b.wg, &b.wu}, s);
   const GatedOut e{H_dev, q.ldh, f32, q.act, G_dev, U_dev};
-  const osscar_status st = projections(q, b, X_dev, Wg_dev, Wu_dev, e, s);
-  return st != OSSCAR_OK ? st : launched("osscar_gated_forward");
+  projections(q, b, X_dev, Wg_dev, Wu_dev, e, s);
+  return launched();
 }
 
 extern "C" osscar_status osscar_gated_backward(const osscar_gated_desc* desc, const void* X_dev, const void* Wg_dev, const void* Wu_dev, const void* dH_dev,
@@ -421,8 +429,7 @@ extern "C" osscar_status osscar_gated_backward(const osscar_gated_desc* desc, co
     make_copies({x ? &b.x : nullptr, w ? &b.wg : nullptr, w ? &b.wu : nullptr}, s);
     const float *G = G_dev, *U = U_dev;
     if (!G) {
-      const osscar_status st = projections(q, b, X_dev, Wg_dev, Wu_dev, GatedOut{nullptr, 0, f32, q.act, b.g, b.u}, s);
-      if (st != OSSCAR_OK) return st;
+      projections(q, b, X_dev, Wg_dev, Wu_dev, GatedOut{nullptr, 0, f32, q.act, b.g, b.u}, s);
       G = b.g; U = b.u;
     }
     const dim3 grid(packs_grid(q.n, b.ldg));
@@ -441,8 +448,8 @@ extern "C" osscar_status osscar_gated_backward(const osscar_gated_desc* desc, co
     add_segment(p, dg, wg);
     add_segment(p, du, wu);
       two.e[0] = PlainOut{dX_dev, lddx, f32};
-    if (q.rows_out) launch_product<OP_K, OP_T, Big1, Small1>(two, 1, f32, b.dx, b.sums, s);
-    else launch_product<OP_K, OP_K, Big1, Small1>(two, 1, f32, b.dx, b.sums, s);
+    if (q.rows_out) launch_product<OP_K, OP_T, Big1, Small1, Flat1>(two, 1, f32, b.dx, b.sums, s);
+    else launch_product<OP_K, OP_K, Big1, Small1, Flat1>(two, 1, f32, b.dx, b.sums, s);
   }
   if (dWg_dev) {      // both weights in one launch
     Pair<1, PlainOut> two{};
@@ -455,7 +462,7 @@ extern "C" osscar_status osscar_gated_backward(const osscar_gated_desc* desc, co
     }
     two.e[0] = PlainOut{dWg_dev, lddw, dw_dtype == OSSCAR_F32};
     two.e[1] = PlainOut{dWu_dev, lddw, dw_dtype == OSSCAR_F32};
-    launch_product<OP_T, OP_T, Big1, Small1>(two, 2, f32, b.dw, b.sums, s);
+    launch_product<OP_T, OP_T, Big1, Small1, Flat1>(two, 2, f32, b.dw, b.sums, s);
   }
-  return launched("osscar_gated_backward");
+  return launched();
 }

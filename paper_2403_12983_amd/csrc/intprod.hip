@@ -154,7 +154,7 @@ __global__ __launch_bounds__(256) void int_join_tiles_kernel(const Product<1> p,
 inline int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
 template <class S>
 int64_t tiles(int64_t n, int64_t m) { return (n + S::BM - 1) / S::BM * ((m + S::BN - 1) / S::BN); }
-Deal deal_of(int64_t n, int64_t d1, int64_t m) { return deal<Big, Small>(n, m, (d1 + STEP_BYTES - 1) / STEP_BYTES, 1, false); }
+Deal deal_of(int64_t n, int64_t d1, int64_t m) { return deal<Big, Small>(n, m, (d1 + STEP_BYTES - 1) / STEP_BYTES, 1); }
 bool few_rows(int64_t n) { return n <= 16; }      // (thin.h says why)
 bool bad_sizes(int64_t n, int64_t d1, int64_t m) { return !a_size(n, 0) || !a_size(m, 1) || d1 < 1 || d1 > OSSCAR_INT_MAX_DIM || tiles<Small>(n, m) > 0x3FFFFFFF; }
 bool bad_digits(const void* q, int64_t ldq, int64_t d1) { return !q || (uintptr_t)q % 16 || ldq % 16 || ldq < d1 || ldq > MAX_LD_BYTES; }
@@ -174,7 +174,7 @@ extern "C" osscar_status osscar_int_rows(const void* X_dev, int64_t n, int64_t d
   if (!X_dev || ldx < d1 || !x_scale_dev || (uintptr_t)X_dev % (x_dtype == OSSCAR_F32 ? 4 : 2)) return refuse_call(OSSCAR_EINVAL, "osscar_int_rows: NULL or misaligned pointer, or leading dimension below the row length");
   if (bad_digits(Xq_dev, ldq, d1)) return refuse_call(OSSCAR_EINVAL, "osscar_int_rows: Xq begins at a 16-byte boundary and ldq is a multiple of 16");
   quantise_rows(X_dev, n, d1, ldx, x_dtype == OSSCAR_F32, Xq_dev, ldq, x_scale_dev, reinterpret_cast<hipStream_t>(hip_stream));
-  return launched("osscar_int_rows");
+  return launched();
 }
 
 extern "C" osscar_status osscar_int_weights(const void* W_dev, int64_t d1, int64_t m, int64_t ldw, int32_t w_dtype, int32_t rows_out, int8_t* Wq_dev, int64_t ldq,
@@ -200,7 +200,7 @@ extern "C" osscar_status osscar_int_weights(const void* W_dev, int64_t d1, int64
                          reinterpret_cast<const char*>(W_dev) + j0 * (f32 ? 4 : 2), f32, (int)d1, (int)part, ldw, w_scale_dev + j0, Wq_dev + j0 * ldq, ldq);
     }
   }
-  return launched("osscar_int_weights");
+  return launched();
 }
 
 extern "C" size_t osscar_int_workspace_bytes(int64_t n, int64_t d1, int64_t m) {
@@ -258,7 +258,7 @@ extern "C" osscar_status osscar_int_product(const void* X_dev, int64_t n, int64_
     else hipLaunchKernelGGL(int_thin_kernel<false>, grid, block, 0, s, t, e);
     if (t.parts > 1)
       hipLaunchKernelGGL(int_join_kernel, dim3(join_grid(n, m)), dim3(256), 0, s, reinterpret_cast<const int*>(t.sums), t.parts, (int)n, (int)m, e);
-    return launched("osscar_int_product");
+    return launched();
   }
   Product<1> p{};
   p.a.p[0] = reinterpret_cast<const char*>(xq); p.a.ldb = ldxq; p.a.rows = (int)n; p.a.cols = (int)up16(d1);
@@ -272,9 +272,9 @@ extern "C" osscar_status osscar_int_product(const void* X_dev, int64_t n, int64_
     if (!workspace_dev || c.used > workspace_bytes) return refuse_call(OSSCAR_ENOMEM, "osscar_int_product: workspace too small");
   }
   const dim3 grid(d.blocks);
-  if (d.big) hipLaunchKernelGGL(int_product_kernel<Big>, grid, dim3(Big::WAVES * 64), 0, s, p, e);
+  if (d.pick == BIG_TILE) hipLaunchKernelGGL(int_product_kernel<Big>, grid, dim3(Big::WAVES * 64), 0, s, p, e);
   else hipLaunchKernelGGL(int_product_kernel<Small>, grid, dim3(Small::WAVES * 64), 0, s, p, e);
-  if (d.parts > 1 && d.big) hipLaunchKernelGGL(int_join_tiles_kernel<Big>, dim3((unsigned)d.join), dim3(256), 0, s, p, e);
+  if (d.parts > 1 && d.pick == BIG_TILE) hipLaunchKernelGGL(int_join_tiles_kernel<Big>, dim3((unsigned)d.join), dim3(256), 0, s, p, e);
   else if (d.parts > 1) hipLaunchKernelGGL(int_join_tiles_kernel<Small>, dim3((unsigned)d.join), dim3(256), 0, s, p, e);
-  return launched("osscar_int_product");
+  return launched();
 }

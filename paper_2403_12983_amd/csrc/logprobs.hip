@@ -431,7 +431,7 @@ extern "C" osscar_status osscar_logprobs(const void* logits_dev, int64_t n, int6
   if (f32) hipLaunchKernelGGL(logprobs_kernel<true>, grid, dim3(T), 0, s, logits_dev, (int)vocab, ld, span, out, stat, rank);
   else hipLaunchKernelGGL(logprobs_kernel<false>, grid, dim3(T), 0, s, logits_dev, (int)vocab, ld, span, out, stat, rank);
   if (parts > 1) hipLaunchKernelGGL(logprobs_join_kernel, dim3((unsigned)n), dim3(T), 0, s, logits_dev, f32, (int)vocab, ld, parts, out, stat, rank);
-  return launched("osscar_logprobs");
+  return launched();
 }
 
 extern "C" osscar_status osscar_logprobs_backward(const void* logits_dev, int64_t n, int64_t vocab, int64_t ld, int32_t dtype, const int64_t* targets_dev, float scale,
@@ -453,5 +453,5 @@ extern "C" osscar_status osscar_logprobs_backward(const void* logits_dev, int64_
                        dlogp_dev ? dlogp_dev + r : nullptr, entropy_dev ? entropy_dev + r : nullptr, dentropy_dev ? dentropy_dev + r : nullptr, top,
                        top > 0 ? top_index_dev + r * top : nullptr, top > 0 ? dtop_dev + r * top : nullptr, reinterpret_cast<char*>(dlogits_dev) + r * ldd * es, ldd);
   }
-  return launched("osscar_logprobs_backward");
+  return launched();
 }

@@ -6,10 +6,9 @@
 namespace osscar {
 
 inline osscar_status refuse_call(osscar_status st, const char* msg) { set_contextless_error(msg); return st; }
-inline osscar_status launched(const char* what) {
+inline osscar_status launched() {
   const hipError_t e = hipGetLastError();
   if (e == hipSuccess) return OSSCAR_OK;
-  (void)what;
   return refuse_call(OSSCAR_EHIP, hipGetErrorString(e));
 }
 inline bool real_dtype(int32_t t) { return t == OSSCAR_F32 || t == OSSCAR_BF16; }

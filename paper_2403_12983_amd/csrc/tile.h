@@ -421,16 +421,29 @@ inline Plan plan(int64_t tiles, int64_t slots, int64_t stages, double alone, dou
   }
   return best;
 }
-struct Deal { bool big; int whole, parts; unsigned blocks; size_t sums, join; };      // sums: bytes of a product's; join: workgroups that add them
+enum Pick { SMALL, BIG_TILE, FLAT };
+struct Deal { Pick pick; int whole, parts; unsigned blocks; size_t sums, join; };      // sums: bytes of a product's; join: workgroups that add them
+template <class S>
+Deal deal_of_plan(Pick pick, int64_t tiles, const Plan& p) {
+  const int64_t rest = p.parts > 1 ? tiles - p.whole : 0, area = S::BM * S::BN;
+  return Deal{pick, (int)p.whole, (int)p.parts, (unsigned)p.blocks, (size_t)(rest * p.parts * S::NB * area * 4), (size_t)(rest * (area / 2048))};
+}
+template <class S> int64_t tiles_of(int64_t M, int64_t N) { return (M + S::BM - 1) / S::BM * ((N + S::BN - 1) / S::BN); }
 template <class SB, class SS>
-Deal deal(int64_t M, int64_t N, int64_t stages, int count, bool f32) {
-  const int64_t big = (M + SB::BM - 1) / SB::BM * ((N + SB::BN - 1) / SB::BN), small = (M + SS::BM - 1) / SS::BM * ((N + SS::BN - 1) / SS::BN);
+Deal deal(int64_t M, int64_t N, int64_t stages, int count) {
+  const int64_t big = tiles_of<SB>(M, N), small = tiles_of<SS>(M, N);
   // (a small tile alone on its compute unit takes less time than one of two)
-  const Plan s = plan(small, 512 / count, stages, 0.75, f32 ? 1 : 2, f32 ? 2.5 : 15), b = f32 ? s : plan(big, 256 / count, stages, 1, 1.2, 18);
-  const bool take = !f32 && b.time * BIG <= s.time;
-  const Plan& p = take ? b : s;
-  const int64_t rest = p.parts > 1 ? (take ? big : small) - p.whole : 0, area = take ? SB::BM * SB::BN : SS::BM * SS::BN;
-  return Deal{take, (int)p.whole, (int)p.parts, (unsigned)p.blocks, (size_t)(rest * p.parts * SS::NB * area * 4), (size_t)(rest * (area / 2048))};
+  const Plan s = plan(small, 512 / count, stages, 0.75, 2, 15), b = plan(big, 256 / count, stages, 1, 1.2, 18);
+  return b.time * BIG <= s.time ? deal_of_plan<SB>(BIG_TILE, big, b) : deal_of_plan<SS>(SMALL, small, s);
+}
+// float32 (split.h): flat tiles, 64 rows instead of 128 and twice the columns, more of which are cut per product.  7168 x 14336, 64 rows 340 us in tiles of 128 rows and 230 in flat
+// ones, 150 rows 700 and 560; tiles of either count (100 rows) 335 and 375.
+constexpr double FLAT_TIME = 1.1;
+template <class SF, class SS>
+Deal deal_split(int64_t M, int64_t N, int64_t stages, int count, bool flat_too) {
+  const int64_t flat = tiles_of<SF>(M, N), small = tiles_of<SS>(M, N);
+  const Plan s = plan(small, 512 / count, stages, 0.75, 1, 2.5), f = plan(flat, 512 / count, stages, 0.75, 1, 2.5);
+  return flat_too && f.time * FLAT_TIME < s.time ? deal_of_plan<SF>(FLAT, flat, f) : deal_of_plan<SS>(SMALL, small, s);
 }
 
 }  // namespace tile
