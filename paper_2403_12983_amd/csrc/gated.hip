@@ -197,9 +197,15 @@ typedef Shape<2, 2, 8, 8, 1> Big1;       // 256 x 256
 typedef Shape<2, 2, 4, 4, 1> Small1;     // 128 x 128
 typedef Shape<1, 4, 4, 2, 2> Flat2;      // 64 x (128 + 128)
 typedef Shape<1, 4, 4, 4, 1> Flat1;      // 64 x 256
-template <class S, class Epi>
+template <class S, int G, class Epi>
 __global__ __launch_bounds__(256) void gated_join_tiles_kernel(const Pair<S::NB, Epi> q) {
-  tile::join_tiles<S, float>(q.p[blockIdx.y], q.e[blockIdx.y]);
+  tile::join_tiles<S, float, G>(q.p[blockIdx.y], q.e[blockIdx.y]);
+}
+template <class S, class Epi>
+void launch_join(const Pair<S::NB, Epi>& q, int count, const Deal& d, hipStream_t s) {
+  const dim3 grid((unsigned)d.join, count);
+  if (d.parts >= JOIN_GROUPS_FROM) hipLaunchKernelGGL((gated_join_tiles_kernel<S, 4, Epi>), grid, dim3(256), 0, s, q);
+  else hipLaunchKernelGGL((gated_join_tiles_kernel<S, 1, Epi>), grid, dim3(256), 0, s, q);
 }
 // `count` products of one launch; sums: d.sums for each
 template <int AM, int BMODE, class SB, class SS, class SF, class Epi>
@@ -215,11 +221,10 @@ void launch_product(Pair<SB::NB, Epi>& q, int count, bool f32, const Deal& d, ch
   if (d.pick == SMALL && f32) hipLaunchKernelGGL((gated_split_kernel<AM, BMODE, SS, Epi>), grid, dim3(SS::WAVES * 64), 0, s, q);
   else if (d.pick == BIG_TILE) hipLaunchKernelGGL((gated_product_kernel<AM, BMODE, SB, Epi>), grid, dim3(SB::WAVES * 64), 0, s, q);
   else if (d.pick == SMALL) hipLaunchKernelGGL((gated_product_kernel<AM, BMODE, SS, Epi>), grid, dim3(SS::WAVES * 64), 0, s, q);
-  const dim3 join((unsigned)d.join, count);
   if (d.parts < 2) return;
-  if (d.pick == FLAT) hipLaunchKernelGGL((gated_join_tiles_kernel<SF, Epi>), join, dim3(256), 0, s, q);
-  else if (d.pick == BIG_TILE) hipLaunchKernelGGL((gated_join_tiles_kernel<SB, Epi>), join, dim3(256), 0, s, q);
-  else hipLaunchKernelGGL((gated_join_tiles_kernel<SS, Epi>), join, dim3(256), 0, s, q);
+  if (d.pick == FLAT) launch_join<SF>(q, count, d, s);
+  else if (d.pick == BIG_TILE) launch_join<SB>(q, count, d, s);
+  else launch_join<SS>(q, count, d, s);
 }
 
 // ---- operands --------------------------------------------------------------------------------

@@ -148,8 +148,13 @@ __global__ __launch_bounds__(256) void int_join_kernel(const int* __restrict__ s
   tile::join<1>(sums, parts, M, N, e);
 }
 
+template <class S, int G>
+__global__ __launch_bounds__(256) void int_join_tiles_kernel(const Product<1> p, const IntOut e) { tile::join_tiles<S, int, G>(p, e); }
 template <class S>
-__global__ __launch_bounds__(256) void int_join_tiles_kernel(const Product<1> p, const IntOut e) { tile::join_tiles<S, int>(p, e); }
+void launch_join(const Product<1>& p, const IntOut& e, const Deal& d, hipStream_t s) {
+  if (d.parts >= JOIN_GROUPS_FROM) hipLaunchKernelGGL((int_join_tiles_kernel<S, 4>), dim3((unsigned)d.join), dim3(256), 0, s, p, e);
+  else hipLaunchKernelGGL((int_join_tiles_kernel<S, 1>), dim3((unsigned)d.join), dim3(256), 0, s, p, e);
+}
 
 inline int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
 template <class S>
@@ -274,7 +279,6 @@ extern "C" osscar_status osscar_int_product(const void* X_dev, int64_t n, int64_
   const dim3 grid(d.blocks);
   if (d.pick == BIG_TILE) hipLaunchKernelGGL(int_product_kernel<Big>, grid, dim3(Big::WAVES * 64), 0, s, p, e);
   else hipLaunchKernelGGL(int_product_kernel<Small>, grid, dim3(Small::WAVES * 64), 0, s, p, e);
-  if (d.parts > 1 && d.pick == BIG_TILE) hipLaunchKernelGGL(int_join_tiles_kernel<Big>, dim3((unsigned)d.join), dim3(256), 0, s, p, e);
-  else if (d.parts > 1) hipLaunchKernelGGL(int_join_tiles_kernel<Small>, dim3((unsigned)d.join), dim3(256), 0, s, p, e);
+  if (d.parts > 1) d.pick == BIG_TILE ? launch_join<Big>(p, e, d, s) : launch_join<Small>(p, e, d, s);
   return launched();
 }

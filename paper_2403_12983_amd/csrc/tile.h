@@ -372,32 +372,46 @@ __device__ __forceinline__ void product_tile(const Product<S::NB>& q, const Epi&
   }
 }
 
-// Adds the sums of the tiles that were dealt out in parts, in order, and goes on with them, eight columns a thread; a workgroup takes 2048 elements of a tile.
-template <class S, class V, class Epi>
+// Adds the sums of the tiles that were dealt out in parts and goes on with them, eight columns a thread: G groups of threads take the parts in turn, and their sums
+// are added in order.  Where there are many parts one thread would wait for all of them one after the other (32 parts of five tiles 21 us, in four groups 4.8).
+constexpr int JOIN_GROUPS_FROM = 8;      // parts
+template <class S, class V, int G, class Epi>
 __device__ __forceinline__ void join_tiles(const Product<S::NB>& q, const Epi& epi) {
-  constexpr int PER = S::BM * S::BN / 2048;
+  constexpr int L = 256 / G, PER = S::BM * S::BN / (8 * L);      // threads of a group; workgroups of a tile
   typedef V v4 __attribute__((ext_vector_type(4)));
   const int tiles_m = (q.M + S::BM - 1) / S::BM, tiles_n = (q.N + S::BN - 1) / S::BN, rest = tiles_m * tiles_n - q.whole;
-  const int t = blockIdx.x / PER, i = blockIdx.x % PER * 256 + threadIdx.x, row = i / (S::BN / 8), col = i % (S::BN / 8) * 8;
+  const int t = blockIdx.x / PER, group = threadIdx.x / L, mine = threadIdx.x % L, i = blockIdx.x % PER * L + mine, row = i / (S::BN / 8), col = i % (S::BN / 8) * 8;
   int tm, tn;
   tile_of(q.whole + t, tiles_m, tiles_n, tm, tn);
   const int m = tm * S::BM + row, n = tn * S::BN + col;
-  if (m >= q.M || n >= q.N) return;
-  epi.each([&](auto put) {
-    V v[S::NB][8];
+  const bool in = m < q.M && n < q.N;
+  V v[S::NB][8];
+#pragma unroll
+  for (int z = 0; z < S::NB; z++)
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[z][e] = 0;
+  for (int p = group; p < q.parts && in; p += G) {
 #pragma unroll
     for (int z = 0; z < S::NB; z++) {
+      const v4* w = reinterpret_cast<const v4*>(reinterpret_cast<const V*>(q.sums) + (((int64_t)p * rest + t) * S::NB + z) * (S::BM * S::BN) + row * S::BN + col);
+      const v4 a = w[0], b = w[1];
 #pragma unroll
-      for (int e = 0; e < 8; e++) v[z][e] = 0;
-      for (int p = 0; p < q.parts; p++) {
-        const v4* w = reinterpret_cast<const v4*>(reinterpret_cast<const V*>(q.sums) + (((int64_t)p * rest + t) * S::NB + z) * (S::BM * S::BN) + row * S::BN + col);
-        const v4 a = w[0], b = w[1];
-#pragma unroll
-        for (int e = 0; e < 4; e++) { v[z][e] += a[e]; v[z][4 + e] += b[e]; }
-      }
+      for (int e = 0; e < 4; e++) { v[z][e] += a[e]; v[z][4 + e] += b[e]; }
     }
-    put(m, n, v, q.N);
-  });
+  }
+  if constexpr (G > 1) {
+    __shared__ V sh[G - 1][S::NB * 8][L];
+    if (group > 0)
+#pragma unroll
+      for (int e = 0; e < S::NB * 8; e++) sh[group - 1][e][mine] = v[e / 8][e % 8];
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int g = 0; g < G - 1; g++)
+#pragma unroll
+      for (int e = 0; e < S::NB * 8; e++) v[e / 8][e % 8] += sh[g][e][mine];
+  }
+  if (in) epi.each([&](auto put) { put(m, n, v, q.N); });
 }
 
 // How a product of `stages` stages is dealt out, one of `count` in a launch.  The chip takes 256 big tiles at a time or 512 small ones, a big one, four times a small one,
@@ -407,13 +421,13 @@ __device__ __forceinline__ void join_tiles(const Product<S::NB>& q, const Epi& e
 // is taken.
 constexpr double BIG = 1.6;
 struct Plan { double time; int64_t whole, parts, blocks; };      // time: rounds of the chip
-inline Plan plan(int64_t tiles, int64_t slots, int64_t stages, double alone, double launch, double sums) {
+inline Plan plan(int64_t tiles, int64_t slots, int64_t stages, int64_t least, double alone, double launch, double sums) {
   const int64_t rest = tiles % slots;
   auto rounds = [&](int64_t n) { return n / slots + (2 * (n % slots) > slots ? 1 : n % slots > 0 ? alone : 0); };
   Plan best{rounds(tiles), tiles, 1, tiles};
   for (int r = 1; r <= 3 && rest > 0; r++) {
     int64_t p = r * slots / rest;
-    if (p > stages / 8) p = stages / 8;
+    if (p > stages / least) p = stages / least;
     if (p > 32) p = 32;
     if (p < 2) continue;
     const double time = tiles / slots + rounds(rest * p) / p + (launch + sums * rest * p / slots) / stages;
@@ -426,14 +440,14 @@ struct Deal { Pick pick; int whole, parts; unsigned blocks; size_t sums, join; }
 template <class S>
 Deal deal_of_plan(Pick pick, int64_t tiles, const Plan& p) {
   const int64_t rest = p.parts > 1 ? tiles - p.whole : 0, area = S::BM * S::BN;
-  return Deal{pick, (int)p.whole, (int)p.parts, (unsigned)p.blocks, (size_t)(rest * p.parts * S::NB * area * 4), (size_t)(rest * (area / 2048))};
+  return Deal{pick, (int)p.whole, (int)p.parts, (unsigned)p.blocks, (size_t)(rest * p.parts * S::NB * area * 4), (size_t)(rest * (area / 2048) * (p.parts >= JOIN_GROUPS_FROM ? 4 : 1))};
 }
 template <class S> int64_t tiles_of(int64_t M, int64_t N) { return (M + S::BM - 1) / S::BM * ((N + S::BN - 1) / S::BN); }
 template <class SB, class SS>
 Deal deal(int64_t M, int64_t N, int64_t stages, int count) {
   const int64_t big = tiles_of<SB>(M, N), small = tiles_of<SS>(M, N);
   // (a small tile alone on its compute unit takes less time than one of two)
-  const Plan s = plan(small, 512 / count, stages, 0.75, 2, 15), b = plan(big, 256 / count, stages, 1, 1.2, 18);
+  const Plan s = plan(small, 512 / count, stages, 8, 0.75, 2, 15), b = plan(big, 256 / count, stages, 8, 1, 1.2, 18);
   return b.time * BIG <= s.time ? deal_of_plan<SB>(BIG_TILE, big, b) : deal_of_plan<SS>(SMALL, small, s);
 }
 // float32 (split.h): flat tiles, 64 rows instead of 128 and twice the columns, more of which are cut per product.  7168 x 14336, 64 rows 340 us in tiles of 128 rows and 230 in flat
@@ -442,7 +456,7 @@ constexpr double FLAT_TIME = 1.1;
 template <class SF, class SS>
 Deal deal_split(int64_t M, int64_t N, int64_t stages, int count, bool flat_too) {
   const int64_t flat = tiles_of<SF>(M, N), small = tiles_of<SS>(M, N);
-  const Plan s = plan(small, 512 / count, stages, 0.75, 1, 2.5), f = plan(flat, 512 / count, stages, 0.75, 1, 2.5);
+  const Plan s = plan(small, 512 / count, stages, 3, 0.75, 1, 2.5), f = plan(flat, 512 / count, stages, 3, 0.75, 1, 2.5);
   return flat_too && f.time * FLAT_TIME < s.time ? deal_of_plan<SF>(FLAT, flat, f) : deal_of_plan<SS>(SMALL, small, s);
 }
 
