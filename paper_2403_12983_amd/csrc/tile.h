@@ -416,7 +416,7 @@ __device__ __forceinline__ void join_tiles(const Product<S::NB>& q, const Epi& e
 
 // How a product of `stages` stages is dealt out, one of `count` in a launch.  The chip takes 256 big tiles at a time or 512 small ones, a big one, four times a small one,
 // in BIG times its time (8192 x 8192 x 8192 bf16: 1500 TFLOP/s and 1200).  Tiles past the last full 256 or 512 would keep part of the chip busy for as
-// long as all: their stages are dealt out in parts of at least eight, so many that they fill it once, twice or three times, where that makes up for
+// long as all: their stages are dealt out in parts of at least `least` (eight; float32, whose stages take three times as long, three), so many that they fill it once, twice or three times, where that makes up for
 // the launch that adds the sums and their way through memory (as long as about `launch` stages, and `sums` for a chip full of tiles).  The shape that takes less time
 // is taken.
 constexpr double BIG = 1.6;
