@@ -163,6 +163,14 @@ def test_gated_tiles_past_a_full_chip(osscar, n, d, f, dtype, rows):
     _check_gated(osscar, n, d, f, dtype, rows, ACTS[(n + d) % 3], seed=n + f)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows", ["in", "out"])
+@pytest.mark.parametrize("n,d,f", [(40, 700, 9001), (64, 3003, 4100), (150, 1500, 5000), (33, 4000, 601), (34, 6001, 70), (20, 1365, 3001)])
+def test_gated_few_rows_of_wide_and_long_layers(osscar, n, d, f, rows, dtype):
+    """tiles of 64 rows, many parts of the contraction, small matrices past 16 rows"""
+    _check_gated(osscar, n, d, f, dtype, rows, ACTS[(n + f) % 3], seed=n + d)
+
+
 @pytest.mark.parametrize("name", ACTS)
 def test_gated_activation_over_its_range(osscar, name):
     """H of single products: g runs over the range of float32, u = 1"""
