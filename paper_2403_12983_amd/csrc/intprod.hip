@@ -18,19 +18,15 @@ __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(
 
 typedef int8_t s8x8 __attribute__((ext_vector_type(8)));
 
-// One row per workgroup of T threads, read twice (the second time from cache); eight values per thread and step.  Bound by reading X and writing Xq;
-// few rows: by the latency of the steps, so that they get 1024 threads each.  x (1 / s) is within 3 2^-24 127 = 2.3e-5 of the rounded quotient x / s, so that
+// One row by T threads: its digits, zeros from d1 to ldq, and its scale; sh: T / 64 words.  x (1 / s) is within 3 2^-24 127 = 2.3e-5 of the rounded quotient x / s, so that
 // both have the same nearest integer unless one lies closer than that to a half; only there, and where 1 / s might be no normal number, is
 // divided (everywhere: 97 us for 8192 x 14336 bf16; so 91, 3.9 TB/s).
 template <int T>
-__global__ __launch_bounds__(T) void int_rows_kernel(const void* __restrict__ X, int f32, int d1, int64_t ldx, int8_t* __restrict__ Xq, int64_t ldq,
-                                                       float* __restrict__ scale) {
-  __shared__ uint32_t sh[T / 64];
-  const int64_t row = blockIdx.x;
+__device__ __forceinline__ float row_digits(const void* __restrict__ X, int64_t at, int f32, int d1, int8_t* __restrict__ q8, int ldq, uint32_t* sh) {
   uint32_t most = 0;
   for (int k = threadIdx.x * 8; k < d1; k += T * 8) {
     float v[8];
-    get_values(X, row * ldx + k, f32, v, d1 - k);
+    get_values(X, at + k, f32, v, d1 - k);
 #pragma unroll
     for (int e = 0; e < 8; e++) most = max(most, magnitude(v[e]));
   }
@@ -41,10 +37,9 @@ __global__ __launch_bounds__(T) void int_rows_kernel(const void* __restrict__ X,
   for (int w = 0; w < T / 64; w++) most = max(most, sh[w]);
   const float s = scale_of(most), u = usable(s), r = 1.f / u;
   const bool quick = u > 1e-30f && u < 1e30f;
-  if (threadIdx.x == 0) scale[row] = s;
   for (int k = threadIdx.x * 8; k < ldq; k += T * 8) {
     float v[8];
-    get_values(X, row * ldx + k, f32, v, d1 - k);      // (zeros past d1)
+    get_values(X, at + k, f32, v, d1 - k);      // (zeros past d1)
     s8x8 w;
     float far = quick ? 0.f : 1.f;
 #pragma unroll
@@ -56,8 +51,19 @@ __global__ __launch_bounds__(T) void int_rows_kernel(const void* __restrict__ X,
     if (far > 0.49996f)
 #pragma unroll
       for (int e = 0; e < 8; e++) w[e] = (int8_t)(k + e < d1 ? digit(v[e], u) : 0);
-    *reinterpret_cast<s8x8*>(Xq + row * ldq + k) = w;
+    *reinterpret_cast<s8x8*>(q8 + k) = w;
   }
+  return s;
+}
+// One row per workgroup, read twice (the second time from cache).  Bound by reading X and writing Xq; few rows: by the latency of the steps, so that they get 1024
+// threads each.
+template <int T>
+__global__ __launch_bounds__(T) void int_rows_kernel(const void* __restrict__ X, int f32, int d1, int64_t ldx, int8_t* __restrict__ Xq, int64_t ldq,
+                                                       float* __restrict__ scale) {
+  __shared__ uint32_t sh[T / 64];
+  const int64_t row = blockIdx.x;
+  const float s = row_digits<T>(X, row * ldx, f32, d1, Xq + row * ldq, (int)ldq, sh);
+  if (threadIdx.x == 0) scale[row] = s;
 }
 // copies digits to rows of ldq, zeros past d1
 __global__ __launch_bounds__(256) void int_copy_kernel(const int8_t* __restrict__ X, int64_t n, int d1, int64_t ldx, int8_t* __restrict__ Xq, int64_t ldq) {
@@ -143,6 +149,25 @@ __global__ __launch_bounds__(S::WAVES * 64, 1) void int_product_kernel(const Pro
 template <bool WIDE>
 __global__ __launch_bounds__((thin::Wave<OP_K, thin::I8, 1, 1, WIDE>::WAVES) * 64, 1) void int_thin_kernel(const thin::Product<1> p, const IntOut e) {
   thin::product<OP_K, thin::I8, 1, 1, WIDE>(p, e);
+}
+// The same for one row that is not digits yet: every workgroup makes them for itself, in LDS; scale: where the first one leaves the scale for a join.  Taken for rows of
+// up to TOKEN_DIM and no more than two workgroups per compute unit, where it costs less than a launch before (14336 x 7168 21.8 us and 24.5, 2048 x 2048 9.9 and 13.2; 32768 x 4096
+// 39 and 35, 7168 x 14336 in 896 workgroups 25 and 23; two rows 26 and 23).
+constexpr int TOKEN_DIM = 16384, TOKEN_BLOCKS = 512;
+__global__ __launch_bounds__(512, 1) void int_token_kernel(const void* __restrict__ X, int f32, int ldq, float* __restrict__ scale, thin::Product<1> p, IntOut e) {
+  static_assert(thin::Wave<OP_K, thin::I8, 1, 1, false>::WAVES == 8, "");
+  __shared__ __align__(16) int8_t digits[TOKEN_DIM];
+  __shared__ float own;
+  __shared__ uint32_t sh[8];
+  const float s = row_digits<512>(X, 0, f32, p.K, digits, ldq, sh);
+  if (threadIdx.x == 0) {
+    own = s;
+    if (blockIdx.x == 0 && blockIdx.y == 0) *scale = s;
+  }
+  __syncthreads();
+  p.a = reinterpret_cast<const char*>(digits);
+  e.xs = &own;
+  thin::product<OP_K, thin::I8, 1, 1, false>(p, e);
 }
 __global__ __launch_bounds__(256) void int_join_kernel(const int* __restrict__ sums, int parts, int M, int N, const IntOut e) {
   tile::join<1>(sums, parts, M, N, e);
@@ -236,7 +261,13 @@ extern "C" osscar_status osscar_int_product(const void* X_dev, int64_t n, int64_
   int64_t ldxq = ldx;
   const bool few = few_rows(n);
   Carve c(workspace_dev);
-  if (!given || (!few && !operand_fits(X_dev, ldx, d1, 1))) {
+  const thin::Deal thin_deal = thin::deal<OP_K, thin::I8>(n, m, d1);
+  const bool token = !given && n == 1 && d1 <= TOKEN_DIM && (int64_t)thin_deal.blocks * thin_deal.parts <= TOKEN_BLOCKS;
+  float* scales = nullptr;      // made here
+  if (token) {
+    xs = scales = reinterpret_cast<float*>(c.take(4));
+    if (!workspace_dev || c.used > workspace_bytes) return refuse_call(OSSCAR_ENOMEM, "osscar_int_product: workspace too small");
+  } else if (!given || (!few && !operand_fits(X_dev, ldx, d1, 1))) {
     ldxq = up16(d1);
     int8_t* q = reinterpret_cast<int8_t*>(c.take((size_t)n * ldxq));
     float* sc = reinterpret_cast<float*>(c.take((size_t)n * 4));
@@ -252,14 +283,15 @@ extern "C" osscar_status osscar_int_product(const void* X_dev, int64_t n, int64_
   }
   const IntOut e{xs, w_scale_dev, bias_dev, Y_dev, ldy, y_dtype == OSSCAR_F32};
   if (few) {
-    const thin::Deal d = thin::deal<OP_K, thin::I8>(n, m, d1);
+    const thin::Deal& d = thin_deal;
     thin::Product<1> t{reinterpret_cast<const char*>(xq), {reinterpret_cast<const char*>(Wq_dev)}, ldxq, ldq, (int)n, (int)m, (int)d1, d.parts, nullptr};
     if (t.parts > 1) {
       t.sums = c.take((size_t)t.parts * n * m * 4);
       if (!workspace_dev || c.used > workspace_bytes) return refuse_call(OSSCAR_ENOMEM, "osscar_int_product: workspace too small");
     }
     const dim3 grid(d.blocks, (unsigned)d.parts), block(512);
-    if (d.wide) hipLaunchKernelGGL(int_thin_kernel<true>, grid, block, 0, s, t, e);
+    if (token) hipLaunchKernelGGL(int_token_kernel, grid, block, 0, s, X_dev, x_dtype == OSSCAR_F32, (int)up16(d1), scales, t, e);
+    else if (d.wide) hipLaunchKernelGGL(int_thin_kernel<true>, grid, block, 0, s, t, e);
     else hipLaunchKernelGGL(int_thin_kernel<false>, grid, block, 0, s, t, e);
     if (t.parts > 1)
       hipLaunchKernelGGL(int_join_kernel, dim3(join_grid(n, m)), dim3(256), 0, s, reinterpret_cast<const int*>(t.sums), t.parts, (int)n, (int)m, e);

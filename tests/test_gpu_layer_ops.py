@@ -364,6 +364,26 @@ def test_int_product_tiles_past_a_full_chip(osscar, n, d1, m):
         _check_int(osscar, X, Wq, ws, _randn(g, m), out)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d1,m", [(1, 1), (15, 40), (2048, 2048), (5461, 1365), (16384, 300), (16385, 300), (16000, 8191), (700, 8193)])
+def test_int_product_of_one_row_equals_its_digits(osscar, d1, m, dtype):
+    """a token's digits are the same wherever they are made; both sides of the sizes that decide it; a row of zeros, an infinity, NaN and the smallest numbers"""
+    g = _gen(d1 + m)
+    Wq, ws = osscar.osscar_int_weights(_randn(g, d1, m))
+    for special in (None, 0.0, math.inf, math.nan, 1e-38):
+        X = _randn(g, 1, d1, dtype=dtype)
+        if special == 0.0:
+            X.zero_()
+        elif special is not None:
+            X[0, d1 // 2:] = special
+        Xq, xs = osscar.osscar_int_rows(X)
+        want = osscar.osscar_int_product(Xq, Wq, ws, x_scale=xs, out_dtype=torch.float32)
+        got = osscar.osscar_int_product(X, Wq, ws, out_dtype=torch.float32)
+        assert torch.equal(torch.nan_to_num(got, nan=7.0), torch.nan_to_num(want, nan=7.0)) and torch.equal(got.isnan(), want.isnan())
+        if special is None:
+            _check_int(osscar, X, Wq, ws, _randn(g, m), torch.bfloat16)
+
+
 def test_int_special_rows(osscar):
     """a row of zeros, rows with an infinity and a NaN, tiny rows; channels likewise"""
     g = _gen(6)
