@@ -18,7 +18,8 @@ __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(
 
 typedef int8_t s8x8 __attribute__((ext_vector_type(8)));
 
-// One row by T threads: its digits, zeros from d1 to ldq, and its scale; sh: T / 64 words.  x (1 / s) is within 3 2^-24 127 = 2.3e-5 of the rounded quotient x / s, so that
+// One row by T threads: its digits, zeros from d1 to ldq, and its scale; sh: T / 64 words.  x (1 / s) is within 3 2^-24 127 = 2.3e-5 of the rounded quotient x / s,
+// so that
 // both have the same nearest integer unless one lies closer than that to a half; only there, and where 1 / s might be no normal number, is
 // divided (everywhere: 97 us for 8192 x 14336 bf16; so 91, 3.9 TB/s).
 template <int T>
@@ -151,7 +152,8 @@ __global__ __launch_bounds__((thin::Wave<OP_K, thin::I8, 1, 1, WIDE>::WAVES) * 6
   thin::product<OP_K, thin::I8, 1, 1, WIDE>(p, e);
 }
 // The same for one row that is not digits yet: every workgroup makes them for itself, in LDS; scale: where the first one leaves the scale for a join.  Taken for rows of
-// up to TOKEN_DIM and no more than two workgroups per compute unit, where it costs less than a launch before (14336 x 7168 21.8 us and 24.5, 2048 x 2048 9.9 and 13.2; 32768 x 4096
+// up to TOKEN_DIM and no more than two workgroups per compute unit, where it costs less than a launch before (14336 x 7168 21.8 us and 24.5, 2048 x 2048 9.9 and
+// 13.2; 32768 x 4096
 // 39 and 35, 7168 x 14336 in 896 workgroups 25 and 23; two rows 26 and 23).
 constexpr int TOKEN_DIM = 16384, TOKEN_BLOCKS = 512;
 __global__ __launch_bounds__(512, 1) void int_token_kernel(const void* __restrict__ X, int f32, int ldq, float* __restrict__ scale, thin::Product<1> p, IntOut e) {

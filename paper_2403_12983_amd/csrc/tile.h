@@ -414,9 +414,11 @@ __device__ __forceinline__ void join_tiles(const Product<S::NB>& q, const Epi& e
   if (in) epi.each([&](auto put) { put(m, n, v, q.N); });
 }
 
-// How a product of `stages` stages is dealt out, one of `count` in a launch.  The chip takes 256 big tiles at a time or 512 small ones, a big one, four times a small one,
+// How a product of `stages` stages is dealt out, one of `count` in a launch.  The chip takes 256 big tiles at a time or 512 small ones, a big one, four times a
+// small one,
 // in BIG times its time (8192 x 8192 x 8192 bf16: 1500 TFLOP/s and 1200).  Tiles past the last full 256 or 512 would keep part of the chip busy for as
-// long as all: their stages are dealt out in parts of at least `least` (eight; float32, whose stages take three times as long, three), so many that they fill it once, twice or three times, where that makes up for
+// long as all: their stages are dealt out in parts of at least `least` (eight; float32, whose stages take three times as long, three), so many that they fill it
+// once, twice or three times, where that makes up for
 // the launch that adds the sums and their way through memory (as long as about `launch` stages, and `sums` for a chip full of tiles).  The shape that takes less time
 // is taken.
 constexpr double BIG = 1.6;
@@ -450,7 +452,8 @@ Deal deal(int64_t M, int64_t N, int64_t stages, int count) {
   const Plan s = plan(small, 512 / count, stages, 8, 0.75, 2, 15), b = plan(big, 256 / count, stages, 8, 1, 1.2, 18);
   return b.time * BIG <= s.time ? deal_of_plan<SB>(BIG_TILE, big, b) : deal_of_plan<SS>(SMALL, small, s);
 }
-// float32 (split.h): flat tiles, 64 rows instead of 128 and twice the columns, more of which are cut per product.  7168 x 14336, 64 rows 340 us in tiles of 128 rows and 230 in flat
+// float32 (split.h): flat tiles, 64 rows instead of 128 and twice the columns, more of which are cut per product.  7168 x 14336, 64 rows 340 us in tiles of 128
+// rows and 230 in flat
 // ones, 150 rows 700 and 560; tiles of either count (100 rows) 335 and 375.
 constexpr double FLAT_TIME = 1.1;
 template <class SF, class SS>
