@@ -13,10 +13,11 @@ constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.69314718055994531f;
 
 // Running state of a row's softmax: the largest logit m so far (raw, at least -FLT_MAX), S = sum 2^y and A = sum -y 2^y with
 // y = c2 l - m2 <= 0, c2 = scale log2(e), m2 = c2 m rounded.  log sum exp = ln2 (m2 + log2 S) and entropy = ln2 (log2 S + A / S): sums of terms of one sign.
-// The rounding of m2 cancels, since every y has the same one.  A row of minus infinities leaves S = 0; NaN and plus infinity make S NaN.
-// Where c2 m might overflow (a row masked with the type's lowest value alone, or with minus infinity), y = c2 (l - m).
+// The rounding of m2 cancels, since every y has the same one, as long as it is small: 2^y of the largest logit is two to the power of that rounding, at most 2^-5
+// while |m2| < 2^20 (float32's 24 bits).  Beyond (rows masked with a large constant or with minus infinity, logits of such a size) y = c2 (l - m), rounded
+// to its own size.  A row of minus infinities leaves S = 0; NaN and plus infinity make S NaN.
 struct Stat { float m, S, A; };
-__device__ __forceinline__ bool plain(float m, float c2) { return fabsf(m) * c2 < 1e37f; }
+__device__ __forceinline__ bool plain(float m, float c2) { return fabsf(m) * c2 < 0x1p20f; }
 __device__ __forceinline__ float offset_of(float m, float c2) { return plain(m, c2) ? m * c2 : 0.f; }
 __device__ __forceinline__ float power_of(float l, float m, float c2) { return plain(m, c2) ? fmaf(l, c2, -(m * c2)) : (l - m) * c2; }
 // c2 m - m2: y = c2 (l - m) + this

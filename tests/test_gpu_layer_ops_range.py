@@ -1,0 +1,111 @@
+"""The layer operators at the ends of their ranges, against float64 definitions: masks by large constants, scales far from 1, gradients that are whole numbers and
+have to be met exactly, the most rows and the longest rows that a call takes."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def osscar():
+    import paper_2403_12983_amd as pkg
+    pkg.load_library()
+    return pkg
+
+
+def _gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def _randn(g, *shape, scale=1.0, dtype=torch.float32):
+    return (torch.randn(*shape, generator=g, device=DEV) * scale).to(dtype)
+
+
+def _check_logprobs(osscar, L, t, top, scale=1.0):
+    """logp, entropy, lse, alternatives and the gradient of all three.  A difference of scaled logits is off by 2 e = 2^-23 of its size, the sum of the exponentials and its
+    logarithm by about 1e-6 together; the gradient by a few e times (1 + |log p|) of the terms it is made of, and half a unit of bf16's eight bits where it is
+    rounded to them."""
+    n, v = L.shape
+    z = L.double() * scale
+    lp = torch.log_softmax(z, 1)
+    p = lp.exp()
+    plogp = torch.where(p > 0, p * lp, torch.zeros_like(p))
+    entropy = -plogp.sum(1)
+    logp = lp.gather(1, t[:, None])[:, 0]
+    r = osscar.osscar_logprobs(L, t, top, scale)
+    bound = lambda x: 2e-6 * (1 + x.abs() / 2)  # noqa: E731
+    fine = torch.isfinite(logp)
+    assert torch.equal(torch.isfinite(r.logp), fine) and ((r.logp.double() - logp)[fine].abs() <= bound(logp[fine])).all()
+    assert ((r.entropy.double() - entropy).abs() <= 5e-6 * (1 + entropy)).all()
+    lse = torch.logsumexp(z, 1)
+    assert (((r.lse[:, 0].double() * scale + r.lse[:, 1].double()) - lse).abs() <= 2e-6 * (1 + lse.abs())).all()
+    if top:
+        order = torch.sort(L.float() + 0.0, dim=1, descending=True, stable=True).indices[:, :top]
+        assert torch.equal(r.top_index, order)
+        want = torch.gather(lp, 1, order)
+        fine = torch.isfinite(want)
+        assert torch.equal(torch.isfinite(r.top_logp), fine) and ((r.top_logp.double() - want)[fine].abs() <= bound(want[fine])).all()
+    g = _gen(n + v)
+    a, b = _randn(g, n), _randn(g, n)
+    c = _randn(g, n, top) if top else None
+    hot = torch.zeros_like(p).scatter_(1, t[:, None], 1.0)
+    own, total, size = a.double()[:, None] * hot, a.double()[:, None], a.double().abs()[:, None] * (hot + p)
+    if top:
+        own = own.scatter_add(1, r.top_index, c.double())
+        total = total + c.double().sum(1, keepdim=True)
+        size = size + torch.zeros_like(hot).scatter_add(1, r.top_index, c.double().abs()) + p * c.double().abs().sum(1, keepdim=True)
+    want = scale * (own - p * total - b.double()[:, None] * (plogp + p * entropy[:, None]))
+    size = scale * (size + b.double().abs()[:, None] * (plogp.abs() + p * (1 + entropy[:, None])))
+    got = osscar.osscar_logprobs_backward(L, t, r.lse, a, entropy=r.entropy, dentropy=b, top_index=r.top_index, dtop=c, scale=scale)
+    tol = 8e-6 * (1 + torch.where(p > 0, lp.abs(), torch.zeros_like(lp))) * size + (2.0 ** -8 * want.abs() if L.dtype == torch.bfloat16 else 0)
+    assert ((got.double() - want).abs() <= tol + 1e-30).all()
+
+
+MASKS = [-1e9, -1e10, -1e12, -1e20, -1e30]
+
+
+@pytest.mark.parametrize("mask", MASKS)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,v", [(3, 70), (2, 8200), (40, 20000), (600, 9000), (2, 131072)])
+def test_logprobs_of_rows_masked_with_a_constant(osscar, n, v, dtype, mask):
+    """a large finite number where others write minus infinity: over whole packets, whole steps, all of a row, all but one"""
+    g = _gen(v)
+    for pattern in ("blocks of 8", "blocks of 64", "first half", "last half", "all", "all but one"):
+        at = torch.arange(v, device=DEV)
+        if pattern.startswith("blocks"):
+            size = int(pattern.split()[-1])
+            out = (torch.rand(n, -(-v // size), generator=g, device=DEV) < 0.5).repeat_interleave(size, 1)[:, :v]
+        elif pattern.endswith("half"):
+            out = (at < v // 2 if pattern[0] == "f" else at >= v // 2).expand(n, v)
+        else:
+            out = torch.ones(n, v, dtype=torch.bool, device=DEV)
+            if pattern == "all but one":
+                out.scatter_(1, torch.randint(0, v, (n, 1), generator=g, device=DEV), False)
+        L = torch.where(out, torch.full((), mask, device=DEV), _randn(g, n, v, scale=2.5)).to(dtype)
+        t = torch.randint(0, v, (n,), generator=g, device=DEV)
+        for top, scale in ((0, 1.0), (5, 0.01), (33, 1.0)):
+            _check_logprobs(osscar, L, t, top, scale)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("size", [1e6, 1e8, 1e10, 1e20, 1e30])
+def test_logprobs_of_large_logits(osscar, size, dtype):
+    """equal ones and normal ones of that size, of either sign"""
+    g = _gen(17)
+    for n, v in ((3, 70), (2, 8200), (700, 9000), (2, 70000)):
+        t = torch.randint(0, v, (n,), generator=g, device=DEV)
+        for L in (torch.full((n, v), size, device=DEV), _randn(g, n, v, scale=size)):
+            _check_logprobs(osscar, L.to(dtype), t, 5)
+
+
+@pytest.mark.parametrize("scale", [0.01, 1e-3, 1e-10])
+def test_logprobs_rows_of_the_lowest_value_at_small_scales(osscar, scale):
+    """every logit the lowest float32: as likely as the others, however small the scale"""
+    for n, v in ((3, 70), (700, 9000), (2, 70000)):
+        L = torch.full((n, v), torch.finfo(torch.float32).min, device=DEV)
+        _check_logprobs(osscar, L, torch.randint(0, v, (n,), generator=_gen(v), device=DEV), 5, scale)
