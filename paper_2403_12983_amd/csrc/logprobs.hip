@@ -162,7 +162,7 @@ __global__ __launch_bounds__(T) void logprobs_kernel(const void* __restrict__ lo
   Given g{-1, 0.f};
   if (tid == 0 && !part_stat) g = given(out, logits, F32, vocab, base, row);
   Stat s{-FLT_MAX, 0.f, 0.f};
-  float m2 = 0.f, bound = INFINITY;
+  float m2 = offset_of(s.m, c2), bound = INFINITY;
   if (tid == 0) count = count2 = 0;
   auto from_row = [&](int v0, int v1, auto put) {      // the k largest of [v0, v1) one by one, by thread 0
     uint64_t last = ~0ull;

@@ -109,3 +109,13 @@ def test_logprobs_rows_of_the_lowest_value_at_small_scales(osscar, scale):
     for n, v in ((3, 70), (700, 9000), (2, 70000)):
         L = torch.full((n, v), torch.finfo(torch.float32).min, device=DEV)
         _check_logprobs(osscar, L, torch.randint(0, v, (n,), generator=_gen(v), device=DEV), 5, scale)
+
+
+def test_logprobs_rows_of_the_lowest_value_at_the_smallest_scales(osscar):
+    """so small that the lowest float32 times the scale is an ordinary number: a row of it is the start of the running maximum"""
+    for scale in (1e-34, 1e-36, 1e-38):
+        for n, v in ((3, 70), (700, 9000), (2, 70000)):
+            L = torch.full((n, v), torch.finfo(torch.float32).min, device=DEV)
+            _check_logprobs(osscar, L, torch.randint(0, v, (n,), generator=_gen(v), device=DEV), 5, scale)
+            L[:, ::7] = 0.0
+            _check_logprobs(osscar, L, torch.randint(0, v, (n,), generator=_gen(v), device=DEV), 5, scale)
