@@ -391,8 +391,8 @@ osscar_status osscar_logprobs(const void* logits_dev, int64_t n, int64_t vocab, 
 /* Gradient of sum_i (dlogp_i logp_i + dentropy_i entropy_i + sum_j dtop_ij top_logp_ij) with respect to the logits:
  *   scale [ dlogp (1{v = t} - p_v) - dentropy p_v (log p_v + entropy) + sum_j dtop_j (1{v = top_index_j} - p_v) ].
  * Any of dlogp_dev, dentropy_dev and dtop_dev may be NULL; entropy_dev goes with dentropy_dev, top_index_dev with dtop_dev.  A row without a target ignores
- * dlogp_i; a target of vocab or more makes the row NaN; a row of minus infinities alone has gradient 0.  dlogits_dev: leading dimension ldd, dtype as
- * logits; it may be logits_dev itself (with ldd = ld). */
+ * dlogp_i; with dlogp_dev a target of vocab or more makes the row NaN; a row of minus infinities alone has gradient 0 whatever its target.  dlogits_dev: leading
+ * dimension ldd, dtype as logits; it may be logits_dev itself (with ldd = ld). */
 osscar_status osscar_logprobs_backward(const void* logits_dev, int64_t n, int64_t vocab, int64_t ld, int32_t dtype, const int64_t* targets_dev, float scale,
                                        const float* lse_dev, const float* dlogp_dev, const float* entropy_dev, const float* dentropy_dev, int32_t top,
                                        const int64_t* top_index_dev, const float* dtop_dev, void* dlogits_dev, int64_t ldd, void* hip_stream);

@@ -357,7 +357,7 @@ __global__ __launch_bounds__(T) void logprobs_backward_kernel(const void* logits
   const bool empty = lnS == -INFINITY;
   auto grad = [&](float l, float own) {
     const float lp = scale * (l - m) - lnS, p = __expf(lp);
-    const float x = p == 0.f ? 0.f : -p * (w + dh * (lp + H));
+    const float x = -p * (w + (p == 0.f ? 0.f : dh * (lp + H)));      // (w of no number makes the whole row so)
     return empty ? 0.f : scale * (x + own);
   };
   // this thread's special column: the target (thread 0) or an alternative

@@ -119,3 +119,20 @@ def test_logprobs_rows_of_the_lowest_value_at_the_smallest_scales(osscar):
             _check_logprobs(osscar, L, torch.randint(0, v, (n,), generator=_gen(v), device=DEV), 5, scale)
             L[:, ::7] = 0.0
             _check_logprobs(osscar, L, torch.randint(0, v, (n,), generator=_gen(v), device=DEV), 5, scale)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_logprobs_gradient_of_a_target_outside_the_vocabulary(osscar, dtype):
+    """the whole row is NaN, the columns of probability zero among them; no other row is touched; without dlogp the target does not matter"""
+    n, v = 4, 9000
+    L = _randn(_gen(1), n, v, dtype=dtype)
+    L[:, 100:200] = -math.inf
+    t = torch.tensor([5, v, v + 7, -1], device=DEV)
+    r = osscar.osscar_logprobs(L, t)
+    one = torch.ones(n, device=DEV)
+    d = osscar.osscar_logprobs_backward(L, t, r.lse, one)
+    assert d[1:3].isnan().all() and torch.isfinite(d[0]).all() and (d[0, 100:200] == 0).all() and (d[3] == 0).all()
+    d = osscar.osscar_logprobs_backward(L, t, r.lse, None, entropy=r.entropy, dentropy=one)
+    assert torch.isfinite(d).all()
+    d = osscar.osscar_logprobs_backward(L, t, r.lse, torch.full((n,), math.nan, device=DEV))
+    assert d[:3].isnan().all() and (d[3] == 0).all()
