@@ -429,9 +429,16 @@ extern "C" osscar_status osscar_logprobs(const void* logits_dev, int64_t n, int6
     rank = reinterpret_cast<uint64_t*>(c.take((size_t)n * parts * top * 8));
     if (!workspace_dev || c.used > workspace_bytes) return refuse_call(OSSCAR_ENOMEM, "osscar_logprobs: workspace too small");
   }
-  const dim3 grid((unsigned)n, (unsigned)parts);
-  if (f32) hipLaunchKernelGGL(logprobs_kernel<true>, grid, dim3(T), 0, s, logits_dev, (int)vocab, ld, span, out, stat, rank);
-  else hipLaunchKernelGGL(logprobs_kernel<false>, grid, dim3(T), 0, s, logits_dev, (int)vocab, ld, span, out, stat, rank);
+  constexpr int64_t LAUNCH = 1 << 23;      // rows: a launch has fewer than 2^32 threads along a dimension (many rows are in one part)
+  const size_t es = f32 ? 4 : 2;
+  for (int64_t r = 0; r < n; r += LAUNCH) {
+    const dim3 grid((unsigned)(n - r < LAUNCH ? n - r : LAUNCH), (unsigned)parts);
+    const void* from = reinterpret_cast<const char*>(logits_dev) + r * ld * es;
+    const Row to{targets_dev + r, scale, top, logp_dev + r, entropy_dev ? entropy_dev + r : nullptr, lse_dev ? lse_dev + 2 * r : nullptr,
+                 top > 0 ? top_index_dev + r * top : nullptr, top > 0 ? top_logp_dev + r * top : nullptr};
+    if (f32) hipLaunchKernelGGL(logprobs_kernel<true>, grid, dim3(T), 0, s, from, (int)vocab, ld, span, to, stat, rank);
+    else hipLaunchKernelGGL(logprobs_kernel<false>, grid, dim3(T), 0, s, from, (int)vocab, ld, span, to, stat, rank);
+  }
   if (parts > 1) hipLaunchKernelGGL(logprobs_join_kernel, dim3((unsigned)n), dim3(T), 0, s, logits_dev, f32, (int)vocab, ld, parts, out, stat, rank);
   return launched();
 }

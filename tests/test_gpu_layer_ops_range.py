@@ -136,3 +136,22 @@ def test_logprobs_gradient_of_a_target_outside_the_vocabulary(osscar, dtype):
     assert torch.isfinite(d).all()
     d = osscar.osscar_logprobs_backward(L, t, r.lse, torch.full((n,), math.nan, device=DEV))
     assert d[:3].isnan().all() and (d[3] == 0).all()
+
+
+MANY = (1 << 24) + 5      # rows of a workgroup each, 256 threads: more than 2^32 of them
+
+
+def test_logprobs_of_more_rows_than_a_launch_takes(osscar):
+    g = _gen(4)
+    L = _randn(g, MANY, 3, dtype=torch.bfloat16)
+    t = torch.randint(0, 3, (MANY,), generator=g, device=DEV)
+    r = osscar.osscar_logprobs(L, t, 1)
+    lp = torch.log_softmax(L.float(), 1)
+    assert ((r.logp - lp.gather(1, t[:, None])[:, 0]).abs() <= 1e-5).all()      # (both float32)
+    assert ((r.entropy + (lp * lp.exp()).sum(1)).abs() <= 1e-5).all() and ((r.lse.sum(1) - torch.logsumexp(L.float(), 1)).abs() <= 1e-5).all()
+    best = L.float().max(1)
+    first = torch.where(L[:, 0] == best.values.to(L.dtype), 0, torch.where(L[:, 1] == best.values.to(L.dtype), 1, 2))
+    assert torch.equal(r.top_index[:, 0], first) and ((r.top_logp[:, 0] - lp.max(1).values).abs() <= 1e-5).all()
+    d = osscar.osscar_logprobs_backward(L, t, r.lse, torch.ones(MANY, device=DEV))
+    want = torch.zeros_like(lp).scatter_(1, t[:, None], 1.0) - lp.exp()
+    assert ((d.float() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-5).all()
