@@ -192,8 +192,14 @@ bool bad_sizes(int64_t n, int64_t d1, int64_t m) { return !a_size(n, 0) || !a_si
 bool bad_digits(const void* q, int64_t ldq, int64_t d1) { return !q || (uintptr_t)q % 16 || ldq % 16 || ldq < d1 || ldq > MAX_LD_BYTES; }
 
 void quantise_rows(const void* X, int64_t n, int64_t d1, int64_t ldx, int f32, int8_t* Xq, int64_t ldq, float* scale, hipStream_t s) {
-  if (n <= 256) hipLaunchKernelGGL(int_rows_kernel<1024>, dim3((unsigned)n), dim3(1024), 0, s, X, f32, (int)d1, ldx, Xq, ldq, scale);
-  else hipLaunchKernelGGL(int_rows_kernel<256>, dim3((unsigned)n), dim3(256), 0, s, X, f32, (int)d1, ldx, Xq, ldq, scale);
+  if (n <= 256) {
+    hipLaunchKernelGGL(int_rows_kernel<1024>, dim3((unsigned)n), dim3(1024), 0, s, X, f32, (int)d1, ldx, Xq, ldq, scale);
+    return;
+  }
+  constexpr int64_t LAUNCH = 1 << 23;      // rows: a launch has fewer than 2^32 threads along a dimension
+  for (int64_t r = 0; r < n; r += LAUNCH)
+    hipLaunchKernelGGL(int_rows_kernel<256>, dim3((unsigned)(n - r < LAUNCH ? n - r : LAUNCH)), dim3(256), 0, s, reinterpret_cast<const char*>(X) + r * ldx * (f32 ? 4 : 2), f32, (int)d1, ldx,
+                       Xq + r * ldq, ldq, scale + r);
 }
 
 }  // namespace

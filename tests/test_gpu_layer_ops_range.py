@@ -2,6 +2,7 @@
 have to be met exactly, the most rows and the longest rows that a call takes."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -155,3 +156,23 @@ def test_logprobs_of_more_rows_than_a_launch_takes(osscar):
     d = osscar.osscar_logprobs_backward(L, t, r.lse, torch.ones(MANY, device=DEV))
     want = torch.zeros_like(lp).scatter_(1, t[:, None], 1.0) - lp.exp()
     assert ((d.float() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-5).all()
+
+
+def test_int_rows_and_channels_beyond_what_a_launch_takes(osscar):
+    """a row of one number x has the scale |x| / 127 and the digit 127 or -127; so has a channel"""
+    g = _gen(5)
+    X = _randn(g, MANY, 1)
+    X[X.abs() < 1e-3] = 1e-3
+    sign = torch.where(X[:, 0] > 0, 127, -127)
+    scale = X[:, 0].abs().double() / 127
+    q, s = osscar.osscar_int_rows(X)
+    assert torch.equal(q[:, 0].int(), sign.int()) and ((s.double() - scale).abs() <= 2.0 ** -24 * scale).all()
+    wq, ws = osscar.osscar_int_weights(X.t())      # 1 x MANY, a channel's number beside the next
+    assert torch.equal(wq[:, 0].int(), sign.int()) and torch.equal(ws, s)
+    two = torch.stack([X[:, 0], X[:, 0] / 2], 1)      # MANY x 2 in memory, a channel's numbers side by side
+    wq, ws = osscar.osscar_int_weights(two.t())
+    half = np.rint(two[:, 1].cpu().numpy() / s.cpu().numpy())      # (63.5 but for the quotient's rounding: 63 or 64)
+    assert torch.equal(wq[:, 0].int(), sign.int()) and torch.equal(ws, s) and np.array_equal(wq[:, 1].cpu().numpy(), half) and (wq[:, 2:] == 0).all()
+    one, s1 = osscar.osscar_int_weights(torch.ones(1, 1, device=DEV))
+    Y = osscar.osscar_int_product(X, one, s1, out_dtype=torch.float32)
+    assert ((Y - X).abs() <= 4 * 2.0 ** -24 * X.abs()).all()
