@@ -320,7 +320,8 @@ osscar_status osscar_gram_static(const void* X_dev, int64_t n, int64_t ldx, int3
  * hip_stream (a hipStream_t, NULL = default stream) and may be captured into a graph; no call waits for it, allocates or keeps
  * anything.  A workspace is device memory of the size that the query beside the call names, at a 256-byte boundary, with any
  * contents; two calls may use the same one if they are ordered.  Buffers of one call must not overlap unless said.  dtypes are
- * OSSCAR_F32 or OSSCAR_BF16 unless said.  No size may exceed 2^30.  After a failure osscar_last_error(NULL) describes it (per host thread).
+ * OSSCAR_F32 or OSSCAR_BF16 unless said.  No size may exceed 2^30, and a product's result no launch (16 rows or fewer: 2^27 columns, at least).  After a failure
+ * osscar_last_error(NULL) describes it (per host thread).
  * ---------------------------------------------------------------------------------------------------------------------- */
 
 /* Gated feed-forward layer (the other common form of the layers whose neurons Section 3 prunes; its output is the X of the

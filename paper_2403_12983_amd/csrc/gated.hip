@@ -285,7 +285,11 @@ struct Buffers {
   thin::Deal few;        // how the products are dealt out: few rows' projections, others', dX, both weights' gradients
   Deal proj, dx, dw;
   char* sums;            // of parts, one product after the other
+  bool launchable() const {
+    return osscar::launchable(few.blocks, few.threads) && osscar::launchable(proj.blocks, 256) && osscar::launchable(dx.blocks, 256) && osscar::launchable(dw.blocks, 256);
+  }
 };
+const char TOO_LARGE[] = "osscar_gated: the products of the sizes are too large for one call";
 // The products of few rows (thin.h says where)
 bool few(const osscar_gated_desc& q) {
   if (q.dtype == OSSCAR_F32) return q.n <= 16 || (q.n <= 32 && q.d * q.f <= (1 << 25));
@@ -299,6 +303,7 @@ Buffers buffers(Carve& c, const osscar_gated_desc& q, const void* X, const void*
   if (!kept && few(q)) {
     b.few = !f32 ? thin::deal<OP_K, thin::BF16>(q.n, q.f, q.d) : q.rows_out ? thin::deal<OP_K, thin::F32>(q.n, q.f, q.d) : thin::deal<OP_T, thin::F32>(q.n, q.f, q.d);
     if (b.few.parts > 1) sums = (size_t)b.few.parts * 2 * q.n * q.f * 4;
+    if (q.n == 0) b.few.blocks = 0;
   } else if (!kept) {
     const int64_t stages = (q.d + ks - 1) / ks;
     b.proj = f32 ? deal_split<Flat2, Small2>(q.n, q.f, stages, 1, true) : deal<Big2, Small2>(q.n, q.f, stages, 1);
@@ -334,7 +339,7 @@ const char* bad_desc(const osscar_gated_desc* q) {
   if (!q) return "osscar_gated: NULL description";
   if (!a_size(q->n, 0) || !a_size(q->d, 1) || !a_size(q->f, 1)) return "osscar_gated: n >= 0, d and f must be positive, none above 2^30";
   if (up_tiles(q->n) * up_tiles(q->f) > 0x3FFFFFFF || up_tiles(q->n) * up_tiles(q->d) > 0x3FFFFFFF || up_tiles(q->d) * up_tiles(q->f) > 0x3FFFFFFF)
-    return "osscar_gated: the products of the sizes are too large for one call";
+    return TOO_LARGE;
   if (!real_dtype(q->dtype)) return "osscar_gated: unknown dtype";
   if (q->act < OSSCAR_ACT_SILU || q->act > OSSCAR_ACT_RELU) return "osscar_gated: unknown activation";
   if (q->ldx < q->d || q->ldw < (q->rows_out ? q->d : q->f) || q->ldh < q->f) return "osscar_gated: leading dimension below the row length";
@@ -391,7 +396,7 @@ void projections(const osscar_gated_desc& q, const Buffers& b, const void* X, co
 extern "C" size_t osscar_gated_workspace_bytes(const osscar_gated_desc* desc, int32_t backward) {
   if (bad_desc(desc)) return 0;
   Carve c(nullptr);
-  buffers(c, *desc, nullptr, nullptr, nullptr, backward != 0, backward == 1);
+  if (!buffers(c, *desc, nullptr, nullptr, nullptr, backward != 0, backward == 1).launchable()) return 0;
   return c.used + 256;      // (never 0: that says that the description is invalid)
 }
 
@@ -403,6 +408,7 @@ extern "C" osscar_status osscar_gated_forward(const osscar_gated_desc* desc, con
   const osscar_gated_desc& q = *desc;
   Carve c(workspace_dev);
   const Buffers b = buffers(c, q, X_dev, Wg_dev, Wu_dev, 0, false);
+  if (!b.launchable()) return refuse_call(OSSCAR_EINVAL, TOO_LARGE);
   if (c.used > workspace_bytes || (c.used > 0 && !workspace_dev)) return refuse_call(OSSCAR_ENOMEM, "osscar_gated_forward: workspace too small");
   if (q.n == 0) return OSSCAR_OK;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
@@ -427,6 +433,7 @@ extern "C" osscar_status osscar_gated_backward(const osscar_gated_desc* desc, co
   const osscar_gated_desc& q = *desc;
   Carve c(workspace_dev);
   const Buffers b = buffers(c, q, X_dev, Wg_dev, Wu_dev, 1, G_dev != nullptr);
+  if (!b.launchable()) return refuse_call(OSSCAR_EINVAL, TOO_LARGE);
   if (c.used > workspace_bytes || (c.used > 0 && !workspace_dev)) return refuse_call(OSSCAR_ENOMEM, "osscar_gated_backward: workspace too small");
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   const int f32 = q.dtype == OSSCAR_F32;

@@ -189,6 +189,10 @@ int64_t tiles(int64_t n, int64_t m) { return (n + S::BM - 1) / S::BM * ((m + S::
 Deal deal_of(int64_t n, int64_t d1, int64_t m) { return deal<Big, Small>(n, m, (d1 + STEP_BYTES - 1) / STEP_BYTES, 1); }
 bool few_rows(int64_t n) { return n <= 16; }      // (thin.h says why)
 bool bad_sizes(int64_t n, int64_t d1, int64_t m) { return !a_size(n, 0) || !a_size(m, 1) || d1 < 1 || d1 > OSSCAR_INT_MAX_DIM || tiles<Small>(n, m) > 0x3FFFFFFF; }
+bool launchable_product(int64_t n, int64_t d1, int64_t m) {
+  const thin::Deal d = thin::deal<OP_K, thin::I8>(n, m, d1);
+  return n == 0 || (few_rows(n) ? launchable(d.blocks, d.threads) : launchable(deal_of(n, d1, m).blocks, 256));
+}
 bool bad_digits(const void* q, int64_t ldq, int64_t d1) { return !q || (uintptr_t)q % 16 || ldq % 16 || ldq < d1 || ldq > MAX_LD_BYTES; }
 
 void quantise_rows(const void* X, int64_t n, int64_t d1, int64_t ldx, int f32, int8_t* Xq, int64_t ldq, float* scale, hipStream_t s) {
@@ -242,7 +246,7 @@ extern "C" osscar_status osscar_int_weights(const void* W_dev, int64_t d1, int64
 }
 
 extern "C" size_t osscar_int_workspace_bytes(int64_t n, int64_t d1, int64_t m) {
-  if (bad_sizes(n, d1, m)) return 0;
+  if (bad_sizes(n, d1, m) || !launchable_product(n, d1, m)) return 0;
   Carve c(nullptr);
   c.take((size_t)n * up16(d1));
   c.take((size_t)n * 4);
@@ -254,6 +258,7 @@ extern "C" osscar_status osscar_int_product(const void* X_dev, int64_t n, int64_
                                             int64_t ldq, const float* w_scale_dev, int64_t m, const float* bias_dev, void* Y_dev, int64_t ldy, int32_t y_dtype,
                                             void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
   if (bad_sizes(n, d1, m)) return refuse_call(OSSCAR_EINVAL, "osscar_int_product: n >= 0, m must be positive and 1 <= d1 <= OSSCAR_INT_MAX_DIM");
+  if (!launchable_product(n, d1, m)) return refuse_call(OSSCAR_EINVAL, "osscar_int_product: the product of the sizes is too large for one call");
   if ((!real_dtype(x_dtype) && x_dtype != OSSCAR_I8) || !real_dtype(y_dtype)) return refuse_call(OSSCAR_EINVAL, "osscar_int_product: unknown dtype");
   if (n == 0) return OSSCAR_OK;
   const bool given = x_dtype == OSSCAR_I8;

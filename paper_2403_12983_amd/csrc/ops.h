@@ -12,6 +12,8 @@ inline osscar_status launched() {
   return refuse_call(OSSCAR_EHIP, hipGetErrorString(e));
 }
 inline bool real_dtype(int32_t t) { return t == OSSCAR_F32 || t == OSSCAR_BF16; }
+// HIP cuts launches of 2^32 threads along a dimension off, without an error.
+inline bool launchable(int64_t blocks, int64_t threads) { return blocks * threads < (int64_t)1 << 32; }
 inline bool a_size(int64_t v, int64_t low) { return v >= low && v <= (int64_t)1 << 30; }
 
 // Pieces of a workspace, each at a 256-byte boundary.  With base = nullptr it only counts.

@@ -272,11 +272,11 @@ __device__ __forceinline__ void product(const Product<NB>& q, const Epi& epi) {
 }
 // How a product is dealt out: column blocks, wide or not, and parts of the contraction, enough for about two workgroups of four waves (OP_T) or half a
 // workgroup of eight (OP_K) per compute unit, each wave with at least two turns.
-struct Deal { unsigned blocks; int parts; bool wide; };
+struct Deal { unsigned blocks; int parts; bool wide; int threads; };
 template <int LAYOUT, int KIND>
 Deal deal(int64_t M, int64_t N, int64_t K) {
   typedef Wave<LAYOUT, KIND, 1, 1, false> W;
-  Deal d{(unsigned)((N + W::COLS - 1) / W::COLS), 1, LAYOUT == OP_K && KIND != BF16 && M > 1 && N >= WIDE_FROM};
+  Deal d{(unsigned)((N + W::COLS - 1) / W::COLS), 1, LAYOUT == OP_K && KIND != BF16 && M > 1 && N >= WIDE_FROM, W::WAVES * 64};
   if (d.wide) { d.blocks = (unsigned)((N + 31) / 32); return d; }
   const int64_t turns = (K + W::TURN - 1) / W::TURN, want = LAYOUT == OP_K ? 128 : 512, most = turns / (W::WAVES * 2);
   int64_t parts = want / d.blocks;

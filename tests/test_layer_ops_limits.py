@@ -1,0 +1,48 @@
+"""CPU-only checks of what sizes the layer operators take: what no launch or no address of a kernel reaches is refused before any GPU work."""
+import ctypes as C
+import os
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import paper_2403_12983_amd as pkg
+    if not os.path.exists(pkg.lib_path()):
+        from paper_2403_12983_amd import build
+        build.build()
+    return pkg.load_library()
+
+
+P = C.c_void_p(1 << 20)      # an address that no refused call may touch
+
+
+def _desc(n, d, f, dtype, rows_out):
+    from paper_2403_12983_amd.binding import _GatedDesc
+    return _GatedDesc(n, d, f, d, d if rows_out else f, f, dtype, 0, rows_out, 0)
+
+
+def _refused(lib, q, backward):
+    """of the workspace query and of the call"""
+    size = 1 << 50
+    if backward:
+        kept = (P, P) if backward == 1 else (None, None)
+        return (lib.osscar_gated_workspace_bytes(C.byref(q), backward) == 0 and
+                lib.osscar_gated_backward(C.byref(q), P, P, P, P, *kept, P, q.d, P, P, max(q.d, q.f), q.dtype, P, size, None) == 1)
+    return lib.osscar_gated_workspace_bytes(C.byref(q), 0) == 0 and lib.osscar_gated_forward(C.byref(q), P, P, P, P, None, None, P, size, None) == 1
+
+
+def test_products_of_more_threads_than_a_launch_takes_are_refused(lib):
+    # few rows: a workgroup of 512 threads per 16 columns (f x d, or 8-bit channels), one of 256 per 64 (float32, d x f)
+    for n in (1, 16):
+        assert _refused(lib, _desc(n, 9, 1 << 27, 1, 1), 0)
+        assert lib.osscar_gated_workspace_bytes(C.byref(_desc(n, 9, (1 << 27) - 16, 1, 1)), 0) > 0
+        assert _refused(lib, _desc(n, 9, 1 << 30, 0, 0), 0)
+        assert lib.osscar_gated_workspace_bytes(C.byref(_desc(n, 9, (1 << 30) - 64, 0, 0)), 0) > 0
+    for n, m in ((1, 1 << 27), (2, 1 << 28)):      # (two rows and more: 32 channels)
+        assert lib.osscar_int_workspace_bytes(n, 16, m) == 0 and lib.osscar_int_workspace_bytes(n, 16, m - 32) > 0
+        assert lib.osscar_int_product(P, n, 16, 16, 1, None, P, 16, P, m, None, P, m, 1, P, 1 << 50, None) == 1
+        assert b"too large" in lib.osscar_last_error(None)
+    # no rows: nothing to do, whatever the rest
+    assert lib.osscar_gated_forward(C.byref(_desc(0, 9, 1 << 27, 1, 1)), P, P, P, P, None, None, P, 1 << 50, None) == 0
+    assert lib.osscar_int_product(P, 0, 16, 16, 1, None, P, 16, P, 1 << 27, None, P, 1 << 27, 1, P, 1 << 50, None) == 0
