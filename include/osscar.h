@@ -328,7 +328,8 @@ osscar_status osscar_gram_static(const void* X_dev, int64_t n, int64_t ldx, int3
  * down projection's Gram, osscar_gram):
  *   g = X Wg,  u = X Wu,  H = act(g) * u  (element by element),   X n x d, Wg and Wu d x f, H n x f.
  * Sums are float32 (float32 operands: as three bf16 pieces each from 33 tokens on, which leaves the error of a
- * float32 product; an infinity there makes its row or column of the product NaN); H is rounded once. */
+ * float32 product; an infinity there makes its row or column of the product NaN); H is rounded once.  bf16 takes d up to 4194296 (backward: f too) and f up to
+ * 16777208, but for 16 rows or fewer of small or unaligned f x d weights, which have no such limit. */
 enum { OSSCAR_ACT_SILU = 0, OSSCAR_ACT_GELU = 1 /* 0.5 g (1 + erf(g / sqrt 2)) */, OSSCAR_ACT_GELU_TANH = 2, OSSCAR_ACT_RELU = 3 };
 typedef struct {
   int64_t n, d, f;    /* tokens (n = 0: nothing to do), inputs, neurons */

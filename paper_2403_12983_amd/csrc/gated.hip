@@ -7,6 +7,7 @@
 #include "split.h"
 #include "thin.h"
 #include "tile.h"
+#include <algorithm>
 
 using namespace osscar;
 using namespace osscar::tile;
@@ -334,6 +335,14 @@ Buffers buffers(Carve& c, const osscar_gated_desc& q, const void* X, const void*
   }
   return b;
 }
+// Whether the tiles reach all of every bf16 operand: rows as long as the copies and dg, du have them, along the contraction and across it
+bool addressable(const osscar_gated_desc& q, int backward, bool kept) {
+  if (q.dtype == OSSCAR_F32 || q.n == 0) return true;
+  const int64_t along = std::max(kept || few(q) ? 0 : q.d, backward ? q.f : 0);
+  const int64_t across = std::max(!q.rows_out && !kept && !few(q) ? q.f : 0, backward ? std::max(q.d, q.f) : 0);
+  return up8(along) * 2 <= MAX_K_BYTES && up8(across) * 2 <= MAX_T_BYTES;
+}
+const char TOO_LONG[] = "osscar_gated: rows of the bf16 operands are too long (d, and f of a backward pass: 4194296; f of a forward pass: 16777208)";
 int64_t up_tiles(int64_t v) { return (v + 63) / 64; }
 const char* bad_desc(const osscar_gated_desc* q) {
   if (!q) return "osscar_gated: NULL description";
@@ -394,7 +403,7 @@ void projections(const osscar_gated_desc& q, const Buffers& b, const void* X, co
 }  // namespace
 
 extern "C" size_t osscar_gated_workspace_bytes(const osscar_gated_desc* desc, int32_t backward) {
-  if (bad_desc(desc)) return 0;
+  if (bad_desc(desc) || !addressable(*desc, backward != 0, backward == 1)) return 0;
   Carve c(nullptr);
   if (!buffers(c, *desc, nullptr, nullptr, nullptr, backward != 0, backward == 1).launchable()) return 0;
   return c.used + 256;      // (never 0: that says that the description is invalid)
@@ -404,6 +413,7 @@ extern "C" osscar_status osscar_gated_forward(const osscar_gated_desc* desc, con
                                               float* G_dev, float* U_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
   const char* bad = bad_desc(desc);
   if (!bad) bad = bad_buffers(*desc, X_dev, Wg_dev, Wu_dev, H_dev, G_dev, U_dev, workspace_dev);
+  if (!bad && !addressable(*desc, 0, false)) bad = TOO_LONG;
   if (bad) return refuse_call(OSSCAR_EINVAL, bad);
   const osscar_gated_desc& q = *desc;
   Carve c(workspace_dev);
@@ -424,6 +434,7 @@ extern "C" osscar_status osscar_gated_backward(const osscar_gated_desc* desc, co
                                                int32_t dw_dtype, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
   const char* bad = bad_desc(desc);
   if (!bad) bad = bad_buffers(*desc, X_dev, Wg_dev, Wu_dev, dH_dev, G_dev, U_dev, workspace_dev);
+  if (!bad && !addressable(*desc, 1, G_dev != nullptr)) bad = TOO_LONG;
   if (!bad && (!real_dtype(dw_dtype) || (dWg_dev == nullptr) != (dWu_dev == nullptr))) bad = "osscar_gated_backward: unknown dtype, or one of dWg and dWu alone";
   if (!bad && ((dX_dev && lddx < desc->d) || (dWg_dev && lddw < (desc->rows_out ? desc->d : desc->f))))
     bad = "osscar_gated_backward: leading dimension below the row length";

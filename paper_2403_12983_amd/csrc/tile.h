@@ -28,7 +28,9 @@ typedef __attribute__((address_space(3))) void lds_void;
 enum { OP_K = 0, OP_T = 1 };
 constexpr int SEGS = 2;                         // the two products of dX
 constexpr int STEP_BYTES = 128;                 // contraction per stage and row: 64 bf16 or 128 int8, two matrix-core operands
-constexpr int64_t MAX_LD_BYTES = 1 << 22;       // 256 rows stay below the 2^30 bytes that an offset may take
+constexpr int64_t MAX_LD_BYTES = 1 << 22;       // of an operand in place: 256 rows stay below 2^30 bytes
+// of any operand: what a tile (OP_K, 256 rows) or a stage (OP_T, 64) spans stays below the 0x7FFFFFF0 bytes that stand for an offset past every end
+constexpr int64_t MAX_K_BYTES = 0x7FFFFFF0 / 256 / 16 * 16, MAX_T_BYTES = 0x7FFFFFF0 / 64 / 16 * 16;
 
 struct Operand {
   const char* p[SEGS];

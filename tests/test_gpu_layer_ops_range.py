@@ -27,6 +27,10 @@ def _randn(g, *shape, scale=1.0, dtype=torch.float32):
     return (torch.randn(*shape, generator=g, device=DEV) * scale).to(dtype)
 
 
+def _whole(g, low, high, *shape, dtype):
+    return torch.randint(low, high + 1, shape, generator=g, device=DEV).to(dtype)
+
+
 def _check_logprobs(osscar, L, t, top, scale=1.0):
     """logp, entropy, lse, alternatives and the gradient of all three.  A difference of scaled logits is off by 2 e = 2^-23 of its size, the sum of the exponentials and its
     logarithm by about 1e-6 together; the gradient by a few e times (1 + |log p|) of the terms it is made of, and half a unit of bf16's eight bits where it is
@@ -176,3 +180,29 @@ def test_int_rows_and_channels_beyond_what_a_launch_takes(osscar):
     one, s1 = osscar.osscar_int_weights(torch.ones(1, 1, device=DEV))
     Y = osscar.osscar_int_product(X, one, s1, out_dtype=torch.float32)
     assert ((Y - X).abs() <= 4 * 2.0 ** -24 * X.abs()).all()
+
+
+@pytest.mark.parametrize("rows", ["in", "out"])
+def test_gated_longest_bf16_rows(osscar, rows):
+    """rows of 4194296: the last row of a tile of 256 ends just below 2^31 bytes from its first.  Whole numbers, which have one right value."""
+    relu, K, g = osscar.OSSCAR_ACT_RELU, 4194296, _gen(6)
+    lay = lambda t: t.t().contiguous().t() if rows == "out" else t  # noqa: E731
+    X = torch.zeros(300, K, dtype=torch.bfloat16, device=DEV)
+    at = torch.cat([torch.arange(40), torch.arange(K - 40, K)]).to(DEV)      # both ends of every row
+    X[:, at] = _whole(g, -1, 1, 300, 80, dtype=torch.bfloat16)
+    Wg, Wu = (_whole(g, -1, 1, K, 8, dtype=torch.bfloat16) for _ in range(2))
+    x, wg, wu = X[:, at].double(), Wg[at].double(), Wu[at].double()
+    want = ((x @ wg).clamp_min(0) * (x @ wu)).to(torch.bfloat16)
+    assert torch.equal(osscar.osscar_gated_forward(X, lay(Wg), lay(Wu), relu), want)
+    del X
+    X = _whole(g, -1, 1, 300, 8, dtype=torch.bfloat16)
+    Wg, Wu = (_whole(g, -1, 1, 8, K, dtype=torch.bfloat16) for _ in range(2))
+    dH = torch.zeros(300, K, dtype=torch.bfloat16, device=DEV)
+    dH[:, at] = _whole(g, -2, 2, 300, 80, dtype=torch.bfloat16)
+    x, wg, wu, dh = X.double(), Wg[:, at].double(), Wu[:, at].double(), dH[:, at].double()
+    gate, up = x @ wg, x @ wu
+    dg, du = dh * up * (gate > 0), dh * gate.clamp_min(0)
+    dX, dWg, dWu = osscar.osscar_gated_backward(X, lay(Wg), lay(Wu), dH, relu, dw_dtype=torch.float32)
+    assert torch.equal(dX.double(), (dg @ wg.t().contiguous() + du @ wu.t().contiguous()).to(torch.bfloat16).double())
+    xt = x.t().contiguous()
+    assert torch.equal(dWg[:, at].double(), xt @ dg) and torch.equal(dWu[:, at].double(), xt @ du) and (dWg[:, 40:K - 40] == 0).all() and (dWu[:, 40:K - 40] == 0).all()

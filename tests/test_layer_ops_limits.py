@@ -46,3 +46,19 @@ def test_products_of_more_threads_than_a_launch_takes_are_refused(lib):
     # no rows: nothing to do, whatever the rest
     assert lib.osscar_gated_forward(C.byref(_desc(0, 9, 1 << 27, 1, 1)), P, P, P, P, None, None, P, 1 << 50, None) == 0
     assert lib.osscar_int_product(P, 0, 16, 16, 1, None, P, 16, P, 1 << 27, None, P, 1 << 27, 1, P, 1 << 50, None) == 0
+
+
+def test_rows_that_the_bf16_tiles_cannot_address_are_refused(lib):
+    long, longest = 4194296, 16777208      # a tile's 256 rows of `long`, a stage's 64 of `longest`, just below 2^31 bytes
+    query = lambda *a, backward=0: lib.osscar_gated_workspace_bytes(C.byref(_desc(*a)), backward)  # noqa: E731
+    for rows_out in (0, 1):
+        for n in (17, 300):
+            assert query(n, long, 8, 1, rows_out) > 0 and _refused(lib, _desc(n, long + 1, 8, 1, rows_out), 0) and _refused(lib, _desc(n, 1 << 25, 8, 1, rows_out), 0)
+            assert _refused(lib, _desc(n, long + 1, 8, 1, rows_out), 2) and query(n, long + 1, 8, 1, rows_out, backward=1) > 0 and _refused(lib, _desc(n, longest + 1, 8, 1, rows_out), 1)
+            for backward in (1, 2):
+                assert query(n, 8, long, 1, rows_out, backward=backward) > 0 and _refused(lib, _desc(n, 8, long + 1, 1, rows_out), backward)
+            # float32 has pointers of its own
+            assert query(n, 1 << 25, 8, 0, rows_out) > 0 and query(n, 8, 1 << 25, 0, rows_out, backward=2) > 0
+        assert _refused(lib, _desc(17, 8, longest + 1, 1, 0), 0) and query(17, 8, longest, 1, 0) > 0 and query(17, 8, 1 << 25, 1, 1) > 0
+    assert query(16, 1 << 25, 9, 1, 1) > 0 and query(16, 1 << 25, 9, 1, 0) == 0      # few rows of f x d weights do not go through tiles
+    assert query(0, 1 << 25, 8, 1, 0) > 0
