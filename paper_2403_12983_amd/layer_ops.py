@@ -111,10 +111,10 @@ def _gated(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, act: int) -> Tup
         _refuse("X, Wg and Wu are on one GPU")
     n, d = X.shape
     f = Wg.shape[1]
-    if Wg.stride() != Wu.stride():
-        _refuse("Wg and Wu lie in memory alike")
     rows_out = 1 if f > 1 and Wg.stride(1) != 1 else 0
     ldw = _ld(Wg.t() if rows_out else Wg, "Wg")
+    if Wg.stride() != Wu.stride() and _ld(Wu.t() if rows_out else Wu, "Wu") != ldw:      # (a dimension of one may have any stride)
+        _refuse("Wg and Wu lie in memory alike")
     xp, gp, up = X.data_ptr(), Wg.data_ptr(), Wu.data_ptr()
     return _GatedDesc(n, d, f, _ld(X, "X"), ldw, f, code, act, rows_out, 1 if (xp | gp | up) & 15 else 0), xp, gp, up
 

@@ -206,3 +206,20 @@ def test_gated_longest_bf16_rows(osscar, rows):
     assert torch.equal(dX.double(), (dg @ wg.t().contiguous() + du @ wu.t().contiguous()).to(torch.bfloat16).double())
     xt = x.t().contiguous()
     assert torch.equal(dWg[:, at].double(), xt @ dg) and torch.equal(dWu[:, at].double(), xt @ du) and (dWg[:, 40:K - 40] == 0).all() and (dWu[:, 40:K - 40] == 0).all()
+
+
+def test_gated_weights_whose_strides_differ_where_a_dimension_is_one(osscar):
+    """what the stride of a dimension of one says does not matter"""
+    g = _gen(2)
+    for dtype in (torch.bfloat16, torch.float32):
+        X = _randn(g, 5, 1, dtype=dtype)
+        both = _randn(g, 1, 48, dtype=dtype)
+        Wg, Wu = both[:, :24], torch.as_strided(both, (1, 24), (1, 1), 24)
+        assert torch.equal(osscar.osscar_gated_forward(X, Wg, Wu), osscar.osscar_gated_forward(X, Wg.clone(), Wu.clone()))
+        X, Wg, Wu = _randn(g, 5, 24, dtype=dtype), _randn(g, 24, 1, dtype=dtype), _randn(g, 1, 24, dtype=dtype).t()
+        assert Wg.stride() != torch.as_strided(Wu, (24, 1), (1, 24)).stride()
+        want = osscar.osscar_gated_forward(X, Wg, Wu.clone())
+        assert torch.equal(osscar.osscar_gated_forward(X, Wg, torch.as_strided(Wu, (24, 1), (1, 24))), want)
+        dH = _randn(g, 5, 1, dtype=dtype)
+        for a, b in zip(osscar.osscar_gated_backward(X, Wg, torch.as_strided(Wu, (24, 1), (1, 24)), dH), osscar.osscar_gated_backward(X, Wg, Wu.clone(), dH)):
+            assert torch.equal(a, b)
