@@ -231,6 +231,8 @@ def osscar_int_product(X: torch.Tensor, Wq: torch.Tensor, w_scale: torch.Tensor,
     bp = _vector(bias, m, torch.float32, "bias") if bias is not None else None
     xsp = _vector(x_scale, n, torch.float32, "x_scale") if x_scale is not None else None
     ldx, ldq = _ld(X, "X"), _ld(Wq, "Wq")
+    if m == 1 and ldq % 16 and Wq.untyped_storage().nbytes() - Wq.storage_offset() >= -(-d1 // 16) * 16:      # Wq[:, :d1] of one channel
+        ldq = -(-d1 // 16) * 16
     with context:
         Y = _EMPTY(n, m, dtype=out_dtype, device=device)
         size = lib.osscar_int_workspace_bytes(n, d1, m)

@@ -223,3 +223,17 @@ def test_gated_weights_whose_strides_differ_where_a_dimension_is_one(osscar):
         dH = _randn(g, 5, 1, dtype=dtype)
         for a, b in zip(osscar.osscar_gated_backward(X, Wg, torch.as_strided(Wu, (24, 1), (1, 24)), dH), osscar.osscar_gated_backward(X, Wg, Wu.clone(), dH)):
             assert torch.equal(a, b)
+
+
+def test_int_product_of_one_channel_without_its_padding(osscar):
+    """Wq[:, :d1] is taken for one channel as for several"""
+    g = _gen(3)
+    for n in (1, 5, 40):
+        X, W = _randn(g, n, 20), _randn(g, 20, 2)
+        Wq, ws = osscar.osscar_int_weights(W)
+        want = osscar.osscar_int_product(X, Wq[:, :20], ws, out_dtype=torch.float32)
+        one, s1 = osscar.osscar_int_weights(W[:, :1].contiguous())
+        assert torch.equal(osscar.osscar_int_product(X, one[:, :20], s1, out_dtype=torch.float32), want[:, :1])
+        assert torch.equal(osscar.osscar_int_product(X, Wq[1:, :20], ws[1:], out_dtype=torch.float32), want[:, 1:])
+        with pytest.raises(osscar.OsscarError):      # a tensor that ends there is no such view
+            osscar.osscar_int_product(X, torch.zeros(1, 20, dtype=torch.int8, device=DEV), s1)
