@@ -237,3 +237,57 @@ def test_int_product_of_one_channel_without_its_padding(osscar):
         assert torch.equal(osscar.osscar_int_product(X, Wq[1:, :20], ws[1:], out_dtype=torch.float32), want[:, 1:])
         with pytest.raises(osscar.OsscarError):      # a tensor that ends there is no such view
             osscar.osscar_int_product(X, torch.zeros(1, 20, dtype=torch.int8, device=DEV), s1)
+
+
+# sizes of every way that the products are dealt out in: large tiles, tiles past a full chip, parts of a contraction, many parts, with rows, columns and stages left over
+WHOLE = [(40, 96, 136), (300, 512, 777), (513, 65, 1030), (2100, 328, 3000), (2100, 333, 3001), (3600, 3600, 136), (3601, 1000, 137), (137, 3601, 2603), (136, 3600, 2600), (2300, 3000, 4100),
+         (2303, 1001, 1000), (1100, 2700, 1900), (150, 1500, 5000), (64, 3003, 4100)] + [(2048 + r, 520, 1024 + r) for r in range(1, 9)] + [(640 + 8 * r, 1024, 264) for r in range(1, 8)]
+
+
+@pytest.mark.parametrize("rows", ["in", "out"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,d,f", WHOLE)
+def test_gated_whole_numbers_are_exact(osscar, n, d, f, dtype, rows):
+    """X and the weights in {-1, 0, 1}, dH in {-2, ..., 2} and RELU: g and u are whole numbers up to 256, which bf16 holds, as it does dg and du; every sum is a whole number
+    below 2^24.  So G, U and the gradients have one right value each, rounded once where they are bf16: a single product left out, or counted twice, shows."""
+    g = _gen(n + f)
+    X = _whole(g, -1, 1, n, d, dtype=dtype)
+    Wg, Wu = (_whole(g, -1, 1, *((f, d) if rows == "out" else (d, f)), dtype=dtype) for _ in range(2))
+    if rows == "out":
+        Wg, Wu = Wg.t(), Wu.t()
+    dH = _whole(g, -2, 2, n, f, dtype=dtype)
+    dH[dH == 0] = 1
+    X64, Wg64, Wu64, dh = X.double(), Wg.double().contiguous(), Wu.double().contiguous(), dH.double()
+    g64, u64 = X64 @ Wg64, X64 @ Wu64
+    assert max(g64.abs().max().item(), u64.abs().max().item()) <= 256
+    relu = osscar.OSSCAR_ACT_RELU
+    H, G, Up = osscar.osscar_gated_forward(X, Wg, Wu, relu, save=True)
+    a = g64.clamp_min(0)
+    assert torch.equal(G.double(), g64) and torch.equal(Up.double(), u64) and torch.equal(H, (a * u64).to(dtype))
+    dg, du = dh * u64 * (g64 > 0), dh * a
+    dX64, dWg64, dWu64 = dg @ Wg64.t().contiguous() + du @ Wu64.t().contiguous(), X64.t().contiguous() @ dg, X64.t().contiguous() @ du
+    for kept in (True, False):
+        more = dict(G=G, U=Up) if kept else {}
+        for dw_dtype in (torch.float32, torch.bfloat16):
+            dX, dWg, dWu = osscar.osscar_gated_backward(X, Wg, Wu, dH, relu, dw_dtype=dw_dtype, **more)
+            assert torch.equal(dX, dX64.to(dtype)) and torch.equal(dWg, dWg64.to(dw_dtype)) and torch.equal(dWu, dWu64.to(dw_dtype))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,d,f", [(1, 2048, 4096), (24, 1365, 700), (150, 1500, 5000), (2100, 333, 3001), (2300, 2100, 2100)])
+def test_two_calls_give_the_same_bits(osscar, n, d, f, dtype):
+    g = _gen(n)
+    X, dH = _randn(g, n, d, dtype=dtype), _randn(g, n, f, dtype=dtype)
+    Wg, Wu = (_randn(g, d, f, scale=1 / math.sqrt(d), dtype=dtype) for _ in range(2))
+    Wq, ws = osscar.osscar_int_weights(_randn(g, d, f))
+    t = torch.randint(0, f, (n,), generator=g, device=DEV)
+
+    def all_of():
+        H, G, Up = osscar.osscar_gated_forward(X, Wg, Wu, save=True)
+        r = osscar.osscar_logprobs(H, t, 7)
+        return [H, G, Up, *osscar.osscar_gated_backward(X, Wg, Wu, dH, G=G, U=Up), *osscar.osscar_gated_backward(X, Wg, Wu, dH), osscar.osscar_int_product(X, Wq, ws), *r,
+                osscar.osscar_logprobs_backward(H, t, r.lse, torch.ones(n, device=DEV), entropy=r.entropy, dentropy=torch.ones(n, device=DEV))]
+    first = all_of()
+    for _ in range(3):
+        for a, b in zip(first, all_of()):
+            assert torch.equal(a, b)
