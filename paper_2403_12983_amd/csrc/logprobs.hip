@@ -19,7 +19,6 @@ constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.69314718055994531f;
 struct Stat { float m, S, A; };
 __device__ __forceinline__ bool plain(float m, float c2) { return fabsf(m) * c2 < 0x1p20f; }
 __device__ __forceinline__ float offset_of(float m, float c2) { return plain(m, c2) ? m * c2 : 0.f; }
-__device__ __forceinline__ float power_of(float l, float m, float c2) { return plain(m, c2) ? fmaf(l, c2, -(m * c2)) : (l - m) * c2; }
 // c2 m - m2: y = c2 (l - m) + this
 __device__ __forceinline__ float rounding_of(float m, float c2) { return plain(m, c2) ? fmaf(m, c2, -(m * c2)) : 0.f; }
 __device__ __forceinline__ void shift(Stat& s, float m, float c2) {      // the largest becomes m >= s.m: every y falls by d
@@ -41,11 +40,17 @@ __device__ __forceinline__ void join(Stat& s, Stat o, float c2) {
   s.A += o.A;
 }
 __device__ __forceinline__ float entropy_of(const Stat& s) { return s.S == 0.f ? 0.f : logf(s.S) + LN2 * (s.A / s.S); }
-__device__ __forceinline__ float logp_of(const Stat& s, float l, float c2) {
-  return s.S == 0.f ? -INFINITY : LN2 * power_of(l, s.m, c2) - logf(s.S);
-}
 // log sum exp(scale (l - m))
 __device__ __forceinline__ float log_sum_of(const Stat& s, float c2) { return s.S == 0.f ? -INFINITY : logf(s.S) - LN2 * rounding_of(s.m, c2); }
+// scale (l - m), where the difference may be no float though the result is one
+__device__ __forceinline__ float scaled(float l, float m, float scale) {
+  const float d = l - m;
+  return fabsf(d) < INFINITY ? scale * d : scale * l - scale * m;
+}
+// (not by way of c2: log2(e) times the lowest value, which masks are made of, is no float)
+__device__ __forceinline__ float logp_of(const Stat& s, float l, float scale, float c2) {
+  return s.S == 0.f ? -INFINITY : scaled(l, s.m, scale) - log_sum_of(s, c2);
+}
 
 // Order of alternatives: larger value first, then lower index; NaN above all, the two zeros equal.
 __device__ __forceinline__ uint64_t rank_of(float l, uint32_t v) {
@@ -114,7 +119,7 @@ __device__ __forceinline__ Given given(const Row& o, const void* logits, int f32
   return Given{t, t >= 0 && t < vocab ? logit(logits, f32, base + t) : NAN};
 }
 __device__ __forceinline__ void put_row(const Row& o, int64_t row, const Stat& s, Given g, float c2) {
-  o.logp[row] = g.t < 0 ? 0.f : (g.l == g.l ? logp_of(s, g.l, c2) : NAN);
+  o.logp[row] = g.t < 0 ? 0.f : (g.l == g.l ? logp_of(s, g.l, o.scale, c2) : NAN);
   if (o.entropy) o.entropy[row] = entropy_of(s);
   if (o.lse) { o.lse[2 * row] = s.m; o.lse[2 * row + 1] = log_sum_of(s, c2); }
 }
@@ -271,7 +276,7 @@ __global__ __launch_bounds__(T) void logprobs_kernel(const void* __restrict__ lo
       part_rank[(row * gridDim.y + blockIdx.y) * out.top + j] = r;
     } else {
       out.top_index[row * out.top + j] = index_of(r);
-      out.top_logp[row * out.top + j] = logp_of(s, logit_of(r), c2);
+      out.top_logp[row * out.top + j] = logp_of(s, logit_of(r), out.scale, c2);
     }
   };
   if (part_rank && tid >= k && tid < out.top) put(tid, 0);      // a part shorter than that (ranks of logits are above 0)
@@ -326,7 +331,7 @@ __global__ __launch_bounds__(T) void logprobs_join_kernel(const void* __restrict
   __syncthreads();
   choose(best, count, out.top, [&](int j, uint64_t r) {
     out.top_index[row * out.top + j] = index_of(r);
-    out.top_logp[row * out.top + j] = logp_of(s, logit_of(r), c2);
+    out.top_logp[row * out.top + j] = logp_of(s, logit_of(r), out.scale, c2);
   });
 }
 // Parts of a row: as many as give two workgroups per compute unit, each of at least a packet per thread, whose alternatives fit the join.

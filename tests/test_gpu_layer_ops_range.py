@@ -291,3 +291,23 @@ def test_two_calls_give_the_same_bits(osscar, n, d, f, dtype):
     for _ in range(3):
         for a, b in zip(first, all_of()):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,v", [(3, 70), (2, 8200), (600, 9000), (2, 131072)])
+def test_logprobs_of_targets_and_alternatives_masked_with_the_lowest_value(osscar, n, v, dtype):
+    """their log probability is the mask's value times the scale, as long as that is a float: not minus infinity"""
+    g = _gen(v)
+    low = torch.finfo(dtype).min
+    L = torch.full((n, v), low, dtype=dtype, device=DEV)
+    L[:, 2:7] = _randn(g, n, 5, scale=2.5, dtype=dtype)
+    t = torch.randint(7, v, (n,), generator=g, device=DEV)
+    for scale in (1.0, 0.75, 0.01, 4.0):
+        lp = torch.log_softmax(L.double() * scale, 1)
+        r = osscar.osscar_logprobs(L, t, 33, scale)
+        order = torch.sort(L.float(), dim=1, descending=True, stable=True).indices[:, :33]
+        assert torch.equal(r.top_index, order)
+        for got, want in ((r.logp, lp.gather(1, t[:, None])[:, 0]), (r.top_logp, lp.gather(1, order))):
+            fine = torch.isfinite(want.float())
+            assert torch.equal(torch.isfinite(got), fine) and ((got.double() - want)[fine].abs() <= 2e-6 * (1 + want[fine].abs() / 2)).all()
+            assert (got[~fine] == -math.inf).all()
