@@ -359,9 +359,9 @@ __global__ __launch_bounds__(T) void logprobs_backward_kernel(const void* logits
   const float dh = dentropy ? dentropy[row] : 0.f, H = dentropy ? entropy[row] : 0.f;
   float w = dl;
   for (int j = 0; j < top; j++) w += dtop[row * top + j];
-  const bool empty = lnS == -INFINITY;
+  const bool empty = lnS == -INFINITY, large = m > 1e30f;      // (only of such a maximum may a difference of logits be no float)
   auto grad = [&](float l, float own) {
-    const float lp = scale * (l - m) - lnS, p = __expf(lp);
+    const float lp = (large ? scaled(l, m, scale) : scale * (l - m)) - lnS, p = __expf(lp);
     const float x = -p * (w + (p == 0.f ? 0.f : dh * (lp + H)));      // (w of no number makes the whole row so)
     return empty ? 0.f : scale * (x + own);
   };

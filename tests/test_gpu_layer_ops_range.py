@@ -311,3 +311,25 @@ def test_logprobs_of_targets_and_alternatives_masked_with_the_lowest_value(ossca
             fine = torch.isfinite(want.float())
             assert torch.equal(torch.isfinite(got), fine) and ((got.double() - want)[fine].abs() <= 2e-6 * (1 + want[fine].abs() / 2)).all()
             assert (got[~fine] == -math.inf).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_logprobs_of_logits_whose_difference_is_no_float(osscar, dtype):
+    """logits from one end of the type to the other, at a scale that makes ordinary numbers of them; the gradient in units of the scale"""
+    g = _gen(31)
+    for n, v in ((3, 70), (2, 8200), (600, 9000), (2, 70000)):
+        L = (torch.rand(n, v, generator=g, device=DEV) * 2 - 1).mul_(3.3e38).to(dtype)
+        t = torch.randint(0, v, (n,), generator=g, device=DEV)
+        scale = 2.0 ** -125
+        lp = torch.log_softmax(L.double() * scale, 1)
+        r = osscar.osscar_logprobs(L, t, 5, scale)
+        want = lp.gather(1, t[:, None])[:, 0]
+        assert ((r.logp.double() - want).abs() <= 2e-6 * (1 + want.abs() / 2)).all()
+        entropy = -(lp * lp.exp()).sum(1)
+        assert ((r.entropy.double() - entropy).abs() <= 5e-6 * (1 + entropy)).all()
+        assert torch.equal(r.top_index, torch.sort(L.float(), dim=1, descending=True, stable=True).indices[:, :5])
+        unit = 2.0 ** 100
+        d = osscar.osscar_logprobs_backward(L, t, r.lse, torch.full((n,), unit, device=DEV), scale=scale)
+        p = lp.exp()
+        hot = torch.zeros_like(p).scatter_(1, t[:, None], 1.0)
+        assert ((d.double() / (unit * scale) - (hot - p)).abs() <= 8e-6 * (1 + lp.abs()) * (hot + p) + 2.0 ** -8 * (hot - p).abs() * (dtype == torch.bfloat16)).all()
