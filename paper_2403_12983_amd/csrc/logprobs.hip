@@ -458,6 +458,7 @@ extern "C" osscar_status osscar_logprobs_backward(const void* logits_dev, int64_
   if (!bad && (uintptr_t)dlogits_dev % (dtype == OSSCAR_F32 ? 4 : 2)) bad = "osscar_logprobs_backward: dlogits is not aligned to its elements";
   if (!bad && dlogits_dev == logits_dev && ldd != ld && n > 1) bad = "osscar_logprobs_backward: in place, both leading dimensions are the same";
   if (bad) return refuse_call(OSSCAR_EINVAL, bad);
+  if (n == 0) return OSSCAR_OK;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   const size_t es = dtype == OSSCAR_F32 ? 4 : 2;
   for (int64_t r = 0; r < n; r += 65535) {      // (the grid's second dimension ends there)

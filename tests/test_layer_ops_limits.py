@@ -62,3 +62,10 @@ def test_rows_that_the_bf16_tiles_cannot_address_are_refused(lib):
         assert _refused(lib, _desc(17, 8, longest + 1, 1, 0), 0) and query(17, 8, longest, 1, 0) > 0 and query(17, 8, 1 << 25, 1, 1) > 0
     assert query(16, 1 << 25, 9, 1, 1) > 0 and query(16, 1 << 25, 9, 1, 0) == 0      # few rows of f x d weights do not go through tiles
     assert query(0, 1 << 25, 8, 1, 0) > 0
+
+
+def test_calls_without_rows_do_not_touch_the_gpu(lib):
+    assert lib.osscar_logprobs(None, 0, 100, 100, 1, None, 1.0, 0, None, None, None, None, None, None, 0, None) == 0
+    assert lib.osscar_logprobs_backward(None, 0, 100, 100, 1, None, 1.0, None, None, None, None, 0, None, None, None, 100, None) == 0
+    assert lib.osscar_int_rows(None, 0, 16, 16, 1, None, 16, None, None) == 0
+    assert lib.osscar_gated_forward(C.byref(_desc(0, 16, 16, 1, 0)), None, P, P, None, None, None, None, 0, None) == 0
