@@ -377,7 +377,7 @@ osscar_status osscar_int_product(const void* X_dev, int64_t n, int64_t d1, int64
                                  void* workspace_dev, size_t workspace_bytes, void* hip_stream);
 
 /* What a model answers with, from its logits (n x vocab, leading dimension ld, the paper's perplexities are the exponential of the mean of -logp;
- * Section 5): with z = scale * logits and scale > 0,
+ * Section 5): with z = scale * logits and 0 < scale < 2.3e38,
  *   logp_i = z_{i,t_i} - lse_i,  entropy_i = -sum_v p_iv log p_iv,  lse_i = log sum_v exp z_iv,
  * and the `top` (<= OSSCAR_TOP_MAX, <= vocab) largest logits of each row, largest first, equal ones by index, NaN before all others.
  * targets_dev: n int64; negative: the row has no target, logp_i = 0; vocab or more: logp_i = NaN.

@@ -394,7 +394,7 @@ __global__ __launch_bounds__(T) void logprobs_backward_kernel(const void* logits
 const char* bad_logits(const void* logits, int64_t n, int64_t vocab, int64_t ld, int32_t dtype, const int64_t* targets, float scale, int32_t top) {
   if (!a_size(n, 0) || !a_size(vocab, 1)) return "osscar_logprobs: n >= 0 and vocab must be positive, none above 2^30";
   if (!real_dtype(dtype)) return "osscar_logprobs: unknown dtype";
-  if (!(scale > 0.f && scale < INFINITY)) return "osscar_logprobs: scale must be positive and finite";
+  if (!(scale > 0.f && scale * LOG2E < INFINITY)) return "osscar_logprobs: scale must be positive and below 2.3e38";
   if (top < 0 || top > OSSCAR_TOP_MAX || top > vocab) return "osscar_logprobs: top is at most OSSCAR_TOP_MAX and at most vocab";
   if (n > 0 && (!logits || !targets || ld < vocab)) return "osscar_logprobs: NULL pointer or leading dimension below the row length";
   if ((uintptr_t)logits % (dtype == OSSCAR_F32 ? 4 : 2)) return "osscar_logprobs: logits are not aligned to their elements";

@@ -333,3 +333,13 @@ def test_logprobs_of_logits_whose_difference_is_no_float(osscar, dtype):
         p = lp.exp()
         hot = torch.zeros_like(p).scatter_(1, t[:, None], 1.0)
         assert ((d.double() / (unit * scale) - (hot - p)).abs() <= 8e-6 * (1 + lp.abs()) * (hot + p) + 2.0 ** -8 * (hot - p).abs() * (dtype == torch.bfloat16)).all()
+
+
+def test_logprobs_at_the_largest_scale(osscar):
+    """one-hot rows, ties in halves"""
+    L = torch.tensor([[1.0, 2.0, -3.0, 0.5], [2.0, 2.0, 1.0, -1.0], [0.0, -1e-3, -1e30, -math.inf]], device=DEV)
+    t = torch.tensor([1, 0, 0], device=DEV)
+    r = osscar.osscar_logprobs(L, t, 2, 2.3e38)
+    half = math.log(0.5)
+    assert torch.allclose(r.logp, torch.tensor([0.0, half, 0.0], device=DEV), atol=1e-6) and torch.allclose(r.entropy, torch.tensor([0.0, -half, 0.0], device=DEV), atol=1e-6)
+    assert r.top_index.tolist() == [[1, 0], [0, 1], [0, 1]]

@@ -69,3 +69,10 @@ def test_calls_without_rows_do_not_touch_the_gpu(lib):
     assert lib.osscar_logprobs_backward(None, 0, 100, 100, 1, None, 1.0, None, None, None, None, 0, None, None, None, 100, None) == 0
     assert lib.osscar_int_rows(None, 0, 16, 16, 1, None, 16, None, None) == 0
     assert lib.osscar_gated_forward(C.byref(_desc(0, 16, 16, 1, 0)), None, P, P, None, None, None, None, 0, None) == 0
+
+
+def test_scales_whose_product_with_log2_e_is_no_float_are_refused(lib):
+    for scale, refused in ((2.4e38, True), (3.4e38, True), (2.3e38, False), (1e-45, False)):
+        # (without rows nothing is done with a scale that is taken)
+        assert lib.osscar_logprobs(P, 0, 100, 100, 1, P, scale, 0, P, P, P, None, None, None, 0, None) == int(refused)
+        assert lib.osscar_logprobs_backward(P, 0, 100, 100, 1, P, scale, P, P, None, None, 0, None, None, P, 100, None) == int(refused)
