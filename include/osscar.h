@@ -320,16 +320,16 @@ osscar_status osscar_gram_static(const void* X_dev, int64_t n, int64_t ldx, int3
  * hip_stream (a hipStream_t, NULL = default stream) and may be captured into a graph; no call waits for it, allocates or keeps
  * anything.  A workspace is device memory of the size that the query beside the call names, at a 256-byte boundary, with any
  * contents; two calls may use the same one if they are ordered.  Buffers of one call must not overlap unless said.  dtypes are
- * OSSCAR_F32 or OSSCAR_BF16 unless said.  No size may exceed 2^30, and a product's result no launch (16 rows or fewer: 2^27 columns, at least).  After a failure
+ * OSSCAR_F32 or OSSCAR_BF16 unless said.  No size may exceed 2^30, and no product what a launch takes (of 16 rows or fewer: 2^27 columns and more).  After a failure
  * osscar_last_error(NULL) describes it (per host thread).
  * ---------------------------------------------------------------------------------------------------------------------- */
 
 /* Gated feed-forward layer (the other common form of the layers whose neurons Section 3 prunes; its output is the X of the
  * down projection's Gram, osscar_gram):
  *   g = X Wg,  u = X Wu,  H = act(g) * u  (element by element),   X n x d, Wg and Wu d x f, H n x f.
- * Sums are float32 (float32 operands: as three bf16 pieces each from 33 tokens on, which leaves the error of a
- * float32 product; an infinity there makes its row or column of the product NaN); H is rounded once.  bf16 takes d up to 4194296 (backward: f too) and f up to
- * 16777208, but for 16 rows or fewer of small or unaligned f x d weights, which have no such limit. */
+ * Sums are float32; H is rounded once.  float32 operands of up to 16 tokens (32, where d f <= 2^25) are multiplied as they are; of more tokens, and in every product of
+ * the backward pass, as three bf16 pieces each, which leaves the error of a float32 product, but an infinity makes its row or column of the product NaN.
+ * bf16 takes d up to 4194296 (backward: f too) and f up to 16777208, but for 16 rows or fewer of small or unaligned f x d weights, which have no such limit. */
 enum { OSSCAR_ACT_SILU = 0, OSSCAR_ACT_GELU = 1 /* 0.5 g (1 + erf(g / sqrt 2)) */, OSSCAR_ACT_GELU_TANH = 2, OSSCAR_ACT_RELU = 3 };
 typedef struct {
   int64_t n, d, f;    /* tokens (n = 0: nothing to do), inputs, neurons */
@@ -342,7 +342,8 @@ typedef struct {
   int32_t unaligned;  /* nonzero: X, Wg or Wu may begin at any element; zero: at a 16-byte boundary (bf16) */
 } osscar_gated_desc;
 /* Workspace of a forward call (backward = 0), of a backward call with G and U (1) or without (2); 0 if the description is invalid.  A
- * forward call takes next to nothing, unless rows are copied: bf16 operands whose rows do not begin at 16-byte boundaries or are not a multiple of 8 long. */
+ * forward call takes: none, where its tiles fill the chip; where they leave part of it idle, the sums of the parts that a contraction is dealt out in (1 x 2048 x 4096 bf16 17 MB,
+ * float32 64 x 7168 x 14336 66 MB, 202 MB at most); and copies of bf16 operands whose rows do not begin at 16-byte boundaries or are not a multiple of 8 long. */
 size_t osscar_gated_workspace_bytes(const osscar_gated_desc* desc, int32_t backward);
 /* G_dev, U_dev (both or neither): dense n x f float32 outputs, g and u for osscar_gated_backward. */
 osscar_status osscar_gated_forward(const osscar_gated_desc* desc, const void* X_dev, const void* Wg_dev, const void* Wu_dev, void* H_dev,
