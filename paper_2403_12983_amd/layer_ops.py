@@ -4,7 +4,11 @@ log probabilities.  Argument marshalling only, as in binding.py: the outputs and
 
 Matrices are 2-D tensors on one GPU whose rows are contiguous; weights of a projection are d x f, and may lie in memory that way or as
 the transpose of a contiguous f x d tensor.  `stream` defaults to the current stream; tensors made on another stream are the caller's to
-order, as everywhere in torch."""
+order, as everywhere in torch.
+
+Nothing here is recorded by autograd: results never require a gradient, whatever the arguments do, and a loss.backward() that comes to one ends
+there.  The gradients of a call are those that its *_backward call returns; to have torch go on from a result, as H.requires_grad_() and
+osscar_gated_backward(..., H.grad) do, is the caller's."""
 from __future__ import annotations
 
 import contextlib

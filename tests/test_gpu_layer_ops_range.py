@@ -343,3 +343,25 @@ def test_logprobs_at_the_largest_scale(osscar):
     half = math.log(0.5)
     assert torch.allclose(r.logp, torch.tensor([0.0, half, 0.0], device=DEV), atol=1e-6) and torch.allclose(r.entropy, torch.tensor([0.0, -half, 0.0], device=DEV), atol=1e-6)
     assert r.top_index.tolist() == [[1, 0], [0, 1], [0, 1]]
+
+
+def test_results_are_constants_to_autograd(osscar):
+    """also of arguments that require a gradient; torch's part of a loss goes on from a result, the layer's part is the backward call's"""
+    g = _gen(8)
+    X, Wg, Wu = (_randn(g, *s).requires_grad_() for s in ((20, 48), (48, 64), (48, 64)))
+    Wd = _randn(g, 64, 90).requires_grad_()
+    t = torch.randint(0, 90, (20,), generator=g, device=DEV)
+    H, G, U = osscar.osscar_gated_forward(X, Wg, Wu, save=True)
+    assert not (H.requires_grad or G.requires_grad or U.requires_grad)
+    H.requires_grad_()
+    logits = H @ Wd
+    r = osscar.osscar_logprobs(logits, t)
+    assert not (r.logp.requires_grad or r.entropy.requires_grad)
+    logits.backward(osscar.osscar_logprobs_backward(logits, t, r.lse, torch.ones(20, device=DEV)))
+    assert Wd.grad is not None and Wg.grad is None
+    dX, dWg, dWu = osscar.osscar_gated_backward(X, Wg, Wu, H.grad, G=G, U=U)
+    x, wg, wu = (a.detach().double().cpu().requires_grad_() for a in (X, Wg, Wu))
+    h = torch.nn.functional.silu(x @ wg) * (x @ wu)
+    torch.log_softmax(h @ Wd.detach().double().cpu(), 1).gather(1, t.cpu()[:, None]).sum().backward()
+    for got, want in ((dX, x.grad), (dWg, wg.grad), (dWu, wu.grad)):
+        assert (got.double().cpu() - want).norm() <= 1e-5 * want.norm()
