@@ -1,8 +1,8 @@
 // Gated feed-forward: g = X Wg, u = X Wu, h = a(g) u with a one of SiLU, GELU (two forms), ReLU; its backward pass
 //     dg = dh u a'(g), du = dh a(g);   dX = dg Wg^T + du Wu^T, dWg = X^T dg, dWu = X^T du.
 // h is the X that the Gram of the layer's down projection takes.  Both projections are one product with the activation in its epilogue, both gradients of the
-// weights one launch,
-// dX one sum over both.  bf16, 16384 x 2048 x 8192 forward 0.88 ms (1250 TFLOP/s), 4096 x 7168 x 14336 forward with g and u kept and backward 4.0 ms (1260).
+// weights one launch, dX one sum over both.  bf16, 16384 x 2048 x 8192 forward 0.88 to 0.94 ms by machine (1170 to 1250 TFLOP/s), 4096 x 7168 x 14336 forward
+// with g and u kept and backward 4.0 to 4.3 ms (1170 to 1260).
 #include "ops.h"
 #include "split.h"
 #include "thin.h"
@@ -471,7 +471,7 @@ extern "C" osscar_status osscar_gated_backward(const osscar_gated_desc* desc, co
     const Operand wg[1] = {b.wg.operand()}, wu[1] = {b.wu.operand()};
     add_segment(p, dg, wg);
     add_segment(p, du, wu);
-      two.e[0] = PlainOut{dX_dev, lddx, f32};
+    two.e[0] = PlainOut{dX_dev, lddx, f32};
     if (q.rows_out) launch_product<OP_K, OP_T, Big1, Small1, Flat1>(two, 1, f32, b.dx, b.sums, s);
     else launch_product<OP_K, OP_K, Big1, Small1, Flat1>(two, 1, f32, b.dx, b.sums, s);
   }

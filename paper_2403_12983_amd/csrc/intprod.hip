@@ -1,6 +1,6 @@
-// Products in 8-bit integers with a scale per token and per output channel, and the quantisation of both sides: s_i = max_k |x_ik| / 127, q_ik = rint(x_ik / s_i),
-// y_ij = s_i w_j sum_k q_ik Q_jk (+ b_j), the sums exact in int32.  14336 x 7168 with given digits: one row 19 us (5.4 TB/s, thin.h), 64 rows 30 us, 8192 rows 0.65 ms
-// (2.6 POP/s, tile.h; the library's largest product 2.5).
+// Products in 8-bit integers with a scale per token and per output channel, and the quantisation of both sides: s_i = max_k |x_ik| / 127, q_ik = rint(x_ik /
+// s_i), y_ij = s_i w_j sum_k q_ik Q_jk (+ b_j), the sums exact in int32.  14336 x 7168 with given digits: one row 19 us (5.4 TB/s, thin.h), 64 rows 28 us, 8192
+// rows 0.66 ms (2.55 POP/s, tile.h; the library's largest product 2.5).
 #include "ops.h"
 #include "thin.h"
 #include "tile.h"
@@ -18,10 +18,9 @@ __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(
 
 typedef int8_t s8x8 __attribute__((ext_vector_type(8)));
 
-// One row by T threads: its digits, zeros from d1 to ldq, and its scale; sh: T / 64 words.  x (1 / s) is within 3 2^-24 127 = 2.3e-5 of the rounded quotient x / s,
-// so that
-// both have the same nearest integer unless one lies closer than that to a half; only there, and where 1 / s might be no normal number, is
-// divided (everywhere: 97 us for 8192 x 14336 bf16; so 91, 3.9 TB/s).
+// One row by T threads: its digits, zeros from d1 to ldq, and its scale; sh: T / 64 words.  x (1 / s) is within 3 2^-24 127 = 2.3e-5 of the rounded quotient x
+// / s, so that both have the same nearest integer unless one lies closer than that to a half; only there, and where 1 / s might be no normal number, is divided
+// (everywhere: 97 us for 8192 x 14336 bf16; so 91, 3.9 TB/s).
 template <int T>
 __device__ __forceinline__ float row_digits(const void* __restrict__ X, int64_t at, int f32, int d1, int8_t* __restrict__ q8, int ldq, uint32_t* sh) {
   uint32_t most = 0;
@@ -56,8 +55,8 @@ __device__ __forceinline__ float row_digits(const void* __restrict__ X, int64_t 
   }
   return s;
 }
-// One row per workgroup, read twice (the second time from cache).  Bound by reading X and writing Xq; few rows: by the latency of the steps, so that they get 1024
-// threads each.
+// One row per workgroup, read twice (the second time from cache).  Bound by reading X and writing Xq; few rows: by the latency of the steps, so that they get
+// 1024 threads each.  Weights m x d1 come here too, once per layer: 7168 rows of 14336 bf16 77 us (4.0 TB/s), float32 139 us.
 template <int T>
 __global__ __launch_bounds__(T) void int_rows_kernel(const void* __restrict__ X, int f32, int d1, int64_t ldx, int8_t* __restrict__ Xq, int64_t ldq,
                                                        float* __restrict__ scale) {
@@ -74,7 +73,8 @@ __global__ __launch_bounds__(256) void int_copy_kernel(const int8_t* __restrict_
     Xq[i] = k < d1 ? X[r * ldx + k] : (int8_t)0;
   }
 }
-// Columns of W (d1 x m): the maxima, 64 rows per workgroup and 256 columns, joined by an atomic maximum (the order does not matter)
+// Columns of W (d1 x m): the maxima, 64 rows per workgroup and 256 columns, joined by an atomic maximum (the order does not matter).  W is read twice, a number
+// per thread: 14336 x 7168 bf16 233 us for all four launches (2.2 TB/s), float32 310 us, once per layer.
 __global__ void int_zero_kernel(uint32_t* p, int n) {
   const int i = blockIdx.x * 256 + threadIdx.x;
   if (i < n) p[i] = 0u;
@@ -151,10 +151,9 @@ template <bool WIDE>
 __global__ __launch_bounds__((thin::Wave<OP_K, thin::I8, 1, 1, WIDE>::WAVES) * 64, 1) void int_thin_kernel(const thin::Product<1> p, const IntOut e) {
   thin::product<OP_K, thin::I8, 1, 1, WIDE>(p, e);
 }
-// The same for one row that is not digits yet: every workgroup makes them for itself, in LDS; scale: where the first one leaves the scale for a join.  Taken for rows of
-// up to TOKEN_DIM and no more than two workgroups per compute unit, where it costs less than a launch before (14336 x 7168 21.8 us and 24.5, 2048 x 2048 9.9 and
-// 13.2; 32768 x 4096
-// 39 and 35, 7168 x 14336 in 896 workgroups 25 and 23; two rows 26 and 23).
+// The same for one row that is not digits yet: every workgroup makes them for itself, in LDS; scale: where the first one leaves the scale for a join.  Taken
+// for rows of up to TOKEN_DIM and no more than two workgroups per compute unit, where it costs less than a launch before (14336 x 7168 21.8 us and 24.5, 2048 x
+// 2048 9.9 and 13.2; 32768 x 4096 39 and 35, 7168 x 14336 in 896 workgroups 25 and 23; two rows 26 and 23).
 constexpr int TOKEN_DIM = 16384, TOKEN_BLOCKS = 512;
 __global__ __launch_bounds__(512, 1) void int_token_kernel(const void* __restrict__ X, int f32, int ldq, float* __restrict__ scale, thin::Product<1> p, IntOut e) {
   static_assert(thin::Wave<OP_K, thin::I8, 1, 1, false>::WAVES == 8, "");

@@ -145,14 +145,14 @@ __device__ __forceinline__ void choose(const uint64_t* ranks, int n, int k, F pu
 }
 
 // A part of a row per workgroup (blockIdx.y of `parts`), read once: softmax statistics and the candidates for the alternatives.
-// The k largest logits lie in the k packets whose largest logit ranks highest (of equal ones the first packet).  After the first step, which holds the
-// lowest indices, the k-th largest of the threads' (groups of threads') maxima is a lower bound of the k-th packet's, and k packets of that step are not
-// below it.  They go into a list with their maxima, and so does every later packet above it (an equal one loses by its index): a few times k of
-// random logits, whatever the row's length; a step where no thread has one costs a comparison per 32 logits.  At the end the k best packets are
-// chosen by counting, read again, and the k best logits in them chosen likewise.  Where the list is too short (ever larger logits), or with NaN and infinity,
-// the part is read k times more.
-// Bound by reading the logits (4096 x 50304 bf16, five alternatives: 89 us, 4.6 TB/s; float32 6.0 TB/s); per logit about 10 slots of the vector unit, four of them
-// the exponential.
+// The k largest logits lie in the k packets whose largest logit ranks highest (of equal ones the first packet).  After the first step, which holds the lowest
+// indices, the k-th largest of the threads' (groups of threads') maxima is a lower bound of the k-th packet's, and k packets of that step are not below it.
+// They go into a list with their maxima, and so does every later packet above it (an equal one loses by its index): a few times k of random logits, whatever
+// the row's length; a step where no thread has one costs a comparison per 32 logits.  At the end the k best packets are chosen by counting, read again, and the
+// k best logits in them chosen likewise.  Where the list is too short (ever larger logits; a first step with a mask's value in all but fewer than k groups), or
+// with NaN and infinity, the part is read k times more.
+// Bound by reading the logits (4096 x 50304 bf16, five alternatives: 89 us, 4.6 TB/s; float32 6.0 TB/s); per logit about 10 slots of the vector unit, four of
+// them the exponential.
 template <bool F32>
 __global__ __launch_bounds__(T) void logprobs_kernel(const void* __restrict__ logits, int vocab, int64_t ld, int span, Row out, Stat* part_stat, uint64_t* part_rank) {
   __shared__ Stat st[T / 64];

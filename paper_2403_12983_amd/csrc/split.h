@@ -1,12 +1,11 @@
 // The products of tile.h for float32 operands: C[m][n] = sum over segments and k of A[m][k] B[n][k] to the error of a float32 product, on the bf16 matrix cores.
 //
-// x = x1 + x2 + x3 with bf16 pieces of 8 bits each, and the six products of weight 2^-16 and more are summed in float32, the smallest first: 2.5 PFLOP/s / 6 against
-// the 157 TFLOP/s of the float32 instruction.  A stage (32 of the contraction) goes from memory to registers, is cut there and written to LDS as pieces, so
-// that memory sees every operand as it is, at any alignment, and no pass over it is needed (pieces written out first: 22 bytes moved per weight
+// x = x1 + x2 + x3 with bf16 pieces of 8 bits each, and the six products of weight 2^-16 and more are summed in float32, the smallest first: 2.5 PFLOP/s / 6
+// against the 157 TFLOP/s of the float32 instruction.  A stage (32 of the contraction) goes from memory to registers, is cut there and written to LDS as
+// pieces, so that memory sees every operand as it is, at any alignment, and no pass over it is needed (pieces written out first: 22 bytes moved per weight
 // instead of 4, which 128 rows through 7168 x 14336 paid with half their speed).  One set of stage buffers, the next two stages in registers, two workgroups
-// per compute unit: while one cuts, the other multiplies.  4096 x 7168 x 14336: the pair of projections 8.9 ms (188 TFLOP/s; the library's float32 products 11.1),
-// the backward
-// pass 17.9 ms; operands whose rows begin at any 4 bytes (2048 x 1365 x 3001) 150 to 160 TFLOP/s.
+// per compute unit: while one cuts, the other multiplies.  4096 x 7168 x 14336: the pair of projections 8.9 ms (188 TFLOP/s; the library's float32 products
+// 11.1), the backward pass 17.9 ms; operands whose rows begin at any 4 bytes (2048 x 1365 x 3001) 150 to 160 TFLOP/s.
 #pragma once
 #include "ops.h"
 #include "tile.h"

@@ -2,15 +2,13 @@
 // so B goes from memory to registers and from there to the matrix core, past LDS: no barrier stands between a wave's loads, and any alignment will do.
 //
 // OP_K (a column's elements side by side): a workgroup takes 16 columns, its waves take the contraction in turns of four matrix-core operands.
-// OP_T (a row of B, one k, side by side; float32): a wave takes 64 columns.  The waves of a workgroup take the contraction in turns; where the column blocks do not
-// fill the chip, it is also cut into parts of a
-// workgroup each, whose sums a second launch adds in order.
+// OP_T (a row of B, one k, side by side; float32): a wave takes 64 columns.  The waves of a workgroup take the contraction in turns; where the column blocks do
+// not fill the chip, it is also cut into parts of a workgroup each, whose sums a second launch adds in order.
 // Taken where it beats the tiles, which read B as fast from 64 or 128 of their rows used (both sides measured): float32 up to 16 rows (the float32 instruction
-// has no pieces to make; 7168 x 14336, 16 rows 159 us, in tiles of 64 rows 220) and up to 32 of small matrices (2048 x 8192 40 to 44 us and 45 to 50, 1365 x 3001 f
-// x d 21 and 36;
-// 7168 x 14336 225 to 275 and 220), bf16 OP_K up to 16 rows of small matrices (2048 x 5461 13 us, tiles in two launches 15;
-// 7168 x 14336 82 and 76) and of those that tiles need copied (7161 x 14333, one row 143 and 240, 16 rows 205 and 243), int8 up to 16 rows (14336 x 7168 22 and 26;
-// 24 rows 27 and 27).
+// has no pieces to make; 7168 x 14336, 16 rows 159 us, in tiles of 64 rows 220) and up to 32 of small matrices (2048 x 8192 40 to 44 us and 45 to 50, 1365 x
+// 3001 f x d 21 and 36; 7168 x 14336 225 to 275 and 220), bf16 OP_K up to 16 rows of small matrices (2048 x 5461 13 us, tiles in two launches 15; 7168 x 14336
+// 82 and 76; nothing between was measured) and of those that tiles need copied (7161 x 14333, one row 143 and 240, 16 rows 205 and 243), int8 up to 16 rows
+// (14336 x 7168 22 and 26; 24 rows 27 and 27).
 #pragma once
 #include "ops.h"
 #include "tile.h"

@@ -7,12 +7,11 @@
 // pass over an operand is needed for any of the three products of a layer's forward and backward pass.
 // A segment is one pair of operands of the same shapes; two are summed for dX.
 //
-// Every packet is read through a buffer descriptor that ends where the operand ends, and a lane whose packet lies beyond the end of a
-// row gets an offset past that end: what is outside an operand reads as zero.  Rows and packets begin at 16-byte boundaries and the
-// contiguous length is a multiple of a packet; the callers copy operands of other alignments first (any alignment by way of registers, without the copy: half the rate
-// from 256 rows on).
-// Bound by the matrix cores and the chip's power (8192 x 8192 x 8192 on random operands: bf16 1470 to 1520 TFLOP/s in each order of the operands, the library 1200 to
-// 1620; the clock falls to 1.7 to 2.1 GHz); few rows, by reading B (16 x 7168 x 14336, both projections 77 us, 5.3 TB/s).
+// Every packet is read through a buffer descriptor that ends where the operand ends, and a lane whose packet lies beyond the end of a row gets an offset past
+// that end: what is outside an operand reads as zero.  Rows and packets begin at 16-byte boundaries and the contiguous length is a multiple of a packet; the
+// callers copy operands of other alignments first (any alignment by way of registers, without the copy: half the rate from 256 rows on).
+// Bound by the matrix cores and the chip's power (8192 x 8192 x 8192 on random operands: bf16 1470 to 1520 TFLOP/s in each order of the operands, the library
+// 1200 to 1620; the clock falls to 1.7 to 2.1 GHz); few rows, by reading B (16 x 7168 x 14336, both projections 77 us, 5.3 TB/s).
 #pragma once
 #include "ops.h"
 
@@ -37,7 +36,7 @@ struct Operand {
   int64_t ldb;               // bytes from one row to the next
   int rows, cols;            // stored rows, stored elements of a row
 };
-// element sizes and stages
+// whether an operand of elements of es bytes is read in place
 inline bool operand_fits(const void* p, int64_t ld, int64_t cols, int es) {
   return ((uintptr_t)p & 15) == 0 && (ld * es) % 16 == 0 && (cols * es) % 16 == 0 && ld * es <= MAX_LD_BYTES;
 }
@@ -417,12 +416,10 @@ __device__ __forceinline__ void join_tiles(const Product<S::NB>& q, const Epi& e
 }
 
 // How a product of `stages` stages is dealt out, one of `count` in a launch.  The chip takes 256 big tiles at a time or 512 small ones, a big one, four times a
-// small one,
-// in BIG times its time (8192 x 8192 x 8192 bf16: 1500 TFLOP/s and 1200).  Tiles past the last full 256 or 512 would keep part of the chip busy for as
-// long as all: their stages are dealt out in parts of at least `least` (eight; float32, whose stages take three times as long, three), so many that they fill it
-// once, twice or three times, where that makes up for
-// the launch that adds the sums and their way through memory (as long as about `launch` stages, and `sums` for a chip full of tiles).  The shape that takes less time
-// is taken.
+// small one, in BIG times its time (8192 x 8192 x 8192 bf16: 1500 TFLOP/s and 1200).  Tiles past the last full 256 or 512 would keep part of the chip busy for
+// as long as all: their stages are dealt out in parts of at least `least` (eight; float32, whose stages take three times as long, three), so many that they
+// fill it once, twice or three times, where that makes up for the launch that adds the sums and their way through memory (as long as about `launch` stages, and
+// `sums` for a chip full of tiles).  The shape that takes less time is taken.
 constexpr double BIG = 1.6;
 struct Plan { double time; int64_t whole, parts, blocks; };      // time: rounds of the chip
 inline Plan plan(int64_t tiles, int64_t slots, int64_t stages, int64_t least, double alone, double launch, double sums) {
@@ -455,8 +452,7 @@ Deal deal(int64_t M, int64_t N, int64_t stages, int count) {
   return b.time * BIG <= s.time ? deal_of_plan<SB>(BIG_TILE, big, b) : deal_of_plan<SS>(SMALL, small, s);
 }
 // float32 (split.h): flat tiles, 64 rows instead of 128 and twice the columns, more of which are cut per product.  7168 x 14336, 64 rows 340 us in tiles of 128
-// rows and 230 in flat
-// ones, 150 rows 700 and 560; tiles of either count (100 rows) 335 and 375.
+// rows and 230 in flat ones, 150 rows 700 and 560; tiles of either count (100 rows) 335 and 375.
 constexpr double FLAT_TIME = 1.1;
 template <class SF, class SS>
 Deal deal_split(int64_t M, int64_t N, int64_t stages, int count, bool flat_too) {
