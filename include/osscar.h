@@ -328,7 +328,8 @@ osscar_status osscar_gram_static(const void* X_dev, int64_t n, int64_t ldx, int3
  * down projection's Gram, osscar_gram):
  *   g = X Wg,  u = X Wu,  H = act(g) * u  (element by element),   X n x d, Wg and Wu d x f, H n x f.
  * Sums are float32; H is rounded once.  float32 operands of up to 16 tokens (32, where d f <= 2^25) are multiplied as they are; of more tokens, and in every product of
- * the backward pass, as three bf16 pieces each, which leaves the error of a float32 product, but an infinity makes its row or column of the product NaN.
+ * the backward pass, as three bf16 pieces each, which leaves the error of a float32 product, but an infinity makes its row or column of the product NaN, and operands
+ * below 1e-34 lose bits (relative error of the product 3e-6 at 1e-35, 3e-4 at 1e-37).
  * bf16 takes d up to 4194296 (backward: f too) and f up to 16777208, but for 16 rows or fewer of small or unaligned f x d weights, which have no such limit. */
 enum { OSSCAR_ACT_SILU = 0, OSSCAR_ACT_GELU = 1 /* 0.5 g (1 + erf(g / sqrt 2)) */, OSSCAR_ACT_GELU_TANH = 2, OSSCAR_ACT_RELU = 3 };
 typedef struct {

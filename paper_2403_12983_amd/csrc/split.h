@@ -22,7 +22,8 @@ using tile::v4s;
 
 constexpr int KS = 32;      // contraction of a stage: one matrix-core operand
 
-// Eight neighbouring values as pieces, each the nearest bf16 of what the ones before leave.  What bf16 cannot hold as a finite number goes into the first
+// Eight neighbouring values as pieces, each the nearest bf16 of what the ones before leave (of values below 1e-34 the last piece ends at bf16's smallest number,
+// 9e-41).  What bf16 cannot hold as a finite number goes into the first
 // piece alone, as it is (infinity, NaN) or cut off (the last float32 values).
 __device__ __forceinline__ void cut(const float (&x)[8], v4i (&p)[3]) {
   float most = fabsf(x[0]);
