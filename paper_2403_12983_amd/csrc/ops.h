@@ -36,6 +36,62 @@ typedef u16x8 u16x8_any __attribute__((aligned(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
 
+// Eight neighbouring elements of a row as they are in memory, so that few registers hold what is under way; zeros from the `most`-th on.
+template <bool F32> struct Eight;
+template <> struct Eight<false> {
+  typedef u16x8 type;
+  static __device__ __forceinline__ type load(const void* p, int64_t at, int64_t most = 8) {
+    const uint16_t* q = reinterpret_cast<const uint16_t*>(p) + at;
+    if (most >= 8) return *reinterpret_cast<const u16x8_any*>(q);
+    type w;
+#pragma unroll
+    for (int e = 0; e < 8; e++) { w[e] = 0; if (e < most) w[e] = q[e]; }
+    return w;
+  }
+  static __device__ __forceinline__ void values(const type& w, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[e] = bf16_value(w[e]);
+  }
+  static __device__ __forceinline__ void store(void* p, int64_t at, const float (&v)[8], int64_t most = 8) {
+    uint16_t* q = reinterpret_cast<uint16_t*>(p) + at;
+    u16x8 w;
+#pragma unroll
+    for (int e = 0; e < 8; e++) w[e] = bf16_nearest(v[e]);
+    if (most >= 8) { *reinterpret_cast<u16x8_any*>(q) = w; return; }
+#pragma unroll
+    for (int e = 0; e < 8; e++) if (e < most) q[e] = w[e];
+  }
+};
+template <> struct Eight<true> {
+  struct type { f32x4 a, b; };
+  static __device__ __forceinline__ type load(const void* p, int64_t at, int64_t most = 8) {
+    const float* q = reinterpret_cast<const float*>(p) + at;
+    if (most >= 8) return type{*reinterpret_cast<const f32x4_any*>(q), *reinterpret_cast<const f32x4_any*>(q + 4)};
+    type w;
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+      w.a[e] = w.b[e] = 0.f;
+      if (e < most) w.a[e] = q[e];
+      if (e + 4 < most) w.b[e] = q[e + 4];
+    }
+    return w;
+  }
+  static __device__ __forceinline__ void values(const type& w, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; e++) { v[e] = w.a[e]; v[e + 4] = w.b[e]; }
+  }
+  static __device__ __forceinline__ void store(void* p, int64_t at, const float (&v)[8], int64_t most = 8) {
+    float* q = reinterpret_cast<float*>(p) + at;
+    if (most >= 8) {
+      *reinterpret_cast<f32x4_any*>(q) = f32x4{v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<f32x4_any*>(q + 4) = f32x4{v[4], v[5], v[6], v[7]};
+      return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; e++) if (e < most) q[e] = v[e];
+  }
+};
+
 // C neighbouring values of a row, of which the ones before `most` exist
 template <int C>
 __device__ __forceinline__ void put_bf16(uint16_t* p, const float (&v)[C], int most) {
