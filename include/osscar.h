@@ -401,6 +401,62 @@ osscar_status osscar_logprobs_backward(const void* logits_dev, int64_t n, int64_
                                        const float* lse_dev, const float* dlogp_dev, const float* entropy_dev, const float* dentropy_dev, int32_t top,
                                        const int64_t* top_index_dev, const float* dtop_dev, void* dlogits_dev, int64_t ldd, void* hip_stream);
 
+/* Layer norm of the rows of X (n x d), in front of the projections that a pruned layer is made of:
+ *   mu = mean x,  r = 1 / sqrt(mean (x - mu)^2 + eps),  Y = (x - mu) r w + b.
+ * w_dev, b_dev: d of w_dtype; either may be NULL (1 and 0).  stats_dev: n x 2 float32 (may be NULL), mu and r of each row for osscar_layernorm_backward.  Sums are
+ * float32; a row whose squares sum to no float32 (values of 1e18 and beyond) or that holds an infinity or NaN is NaN.  Y_dev may be X_dev (ldy = ldx).  X and Y have
+ * one dtype; eps must be a positive float32. */
+osscar_status osscar_layernorm_forward(const void* X_dev, int64_t n, int64_t d, int64_t ldx, int32_t dtype, const void* w_dev, const void* b_dev, int32_t w_dtype, float eps,
+                                       void* Y_dev, int64_t ldy, float* stats_dev, void* hip_stream);
+/* Gradients, given dY (dtype as X): with h = (x - mu) r and g = dY w,  dX = r (g - mean g - h mean(g h)),  dw = sum over rows of dY h,  db = sum of dY.  dX_dev, dw_dev and
+ * db_dev: any may be NULL; dX_dev may be dY_dev or X_dev (of one leading dimension).  dw and db: dw_dtype, written, not added to, in an order that does not change from call
+ * to call.  A call that wants neither takes no workspace; osscar_layernorm_workspace_bytes is 0 if the sizes are invalid. */
+size_t osscar_layernorm_workspace_bytes(int64_t n, int64_t d);
+osscar_status osscar_layernorm_backward(const void* X_dev, int64_t n, int64_t d, int64_t ldx, int32_t dtype, const void* w_dev, int32_t w_dtype, const void* dY_dev, int64_t lddy,
+                                        const float* stats_dev, void* dX_dev, int64_t lddx, void* dw_dev, void* db_dev, int32_t dw_dtype, void* workspace_dev,
+                                        size_t workspace_bytes, void* hip_stream);
+
+/* AdamW, one step over many tensors: with t = step counted from 1, and float32 factors rounded once from float64, every operation below rounded by itself,
+ *   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) (g g),  p = p (1 - lr weight_decay) - lr / (1 - b1^t) (m / (sqrt v / sqrt(1 - b2^t) + eps)).
+ * A tensor is n contiguous elements of any shape (n = 0: nothing to do).  p: float32, or bf16, rounded to the nearest, with a float32 copy `master` that holds the
+ * parameters (p is then written, not read), or without.  Nothing may overlap, within a tensor or between tensors.
+ * bits 32: m and v are float32.  bits 8: m and v are codes of 8 bits, m_scale and v_scale a power of two (float32) for each OSSCAR_ADAMW_BLOCK elements of a tensor (the last block may be shorter):
+ *   m = m_scale * the 8-bit float e4m3 (sign, 4 bits of exponent with bias 7, 3 of mantissa, subnormal numbers);
+ *   sqrt v = v_scale * (c < 16 ? c : (16 + c % 16) 2^(c / 16 - 1)), c a byte: whole numbers to 32, then 16 steps an octave, to 31 * 2^14.
+ * The scales put the largest power of two of a block at 2^7 and 2^17 (never below 2^-126); numbers are rounded to the nearest code (halves to even), but a v above zero keeps a code above
+ * zero.  All codes and scales 0 is a state of zeros.  A state that is not finite makes its block's scale NaN, and so the whole block from the next step on.
+ * stochastic: codes, and bf16 parameters without a master, are rounded up with the probability that their part of a step is, so that changes smaller than a step (0.001 of v) are not lost
+ * on average: bits r of the hash h below are added to the float32 number under its last kept bit and the rest cut off; for m the low 20 of h, for sqrt v the high 19 of the
+ * low 32 of 0x9E3779B9 h, for p the high 16 of h (numbers below the smallest normal one first have it added).  h = mix(low 32 bits of i ^ mix(high 32 bits of i ^ mix(seed))), i the number of
+ * the element in the call, each tensor before it counting as whole blocks; mix(x): x = (x ^ x >> 16) * 0x9E3779B9, x = (x ^ x >> 15) * 0xB7E15163, x ^ x >> 16 in 32 bits.  A seed of its own for each step.
+ * lr_dev, step_dev (may be NULL): one float32, one int64 on the device that take the place of lr and step, for steps that are captured once and replayed.  grad_scale_dev (may be NULL): one float32 that
+ * every gradient is multiplied by first; if it is not finite the call changes nothing. */
+#define OSSCAR_ADAMW_BLOCK 256
+typedef struct {
+  int64_t n;
+  void* p;
+  float* master;               /* or NULL */
+  const void* g;
+  void *m, *v;
+  float *m_scale, *v_scale;    /* bits 8; else not looked at */
+  int32_t p_dtype, g_dtype;    /* OSSCAR_F32 or OSSCAR_BF16, each of its own */
+} osscar_adamw_tensor;
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay;
+  int64_t step;
+  const float* lr_dev;
+  const int64_t* step_dev;
+  const float* grad_scale_dev;
+  uint32_t seed;
+  int32_t stochastic;
+  int32_t bits;
+} osscar_adamw_desc;
+/* tensors: host array, read during the call. */
+osscar_status osscar_adamw(const osscar_adamw_tensor* tensors, int64_t count, const osscar_adamw_desc* desc, void* hip_stream);
+/* What 8-bit states stand for: m and sqrt v of each tensor in bf16, which holds them exactly, n elements at m_out[k] and root_out[k] (host arrays of device pointers).  Of the tensors n, m, v,
+ * m_scale and v_scale are looked at. */
+osscar_status osscar_adamw_values(const osscar_adamw_tensor* tensors, int64_t count, void* const* m_out, void* const* root_out, void* hip_stream);
+
 /* Description of the last failure: of a context, or (ctx == NULL) of the last failed call on this host thread that takes
  * no context. */
 const char* osscar_last_error(const osscar_ctx* ctx);

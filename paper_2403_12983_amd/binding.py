@@ -30,7 +30,9 @@ EXPORTED_SYMBOLS = ["osscar_workspace_bytes", "osscar_create", "osscar_destroy",
                     "osscar_gram_static", "osscar_last_error",
                     "osscar_gated_workspace_bytes", "osscar_gated_forward", "osscar_gated_backward",
                     "osscar_int_weights", "osscar_int_rows", "osscar_int_workspace_bytes", "osscar_int_product",
-                    "osscar_logprobs_workspace_bytes", "osscar_logprobs", "osscar_logprobs_backward"]
+                    "osscar_logprobs_workspace_bytes", "osscar_logprobs", "osscar_logprobs_backward",
+                    "osscar_layernorm_forward", "osscar_layernorm_workspace_bytes", "osscar_layernorm_backward",
+                    "osscar_adamw", "osscar_adamw_values"]
 
 
 class OsscarError(RuntimeError):
@@ -48,6 +50,16 @@ class _Desc(C.Structure):
 class _GatedDesc(C.Structure):
     _fields_ = [("n", C.c_int64), ("d", C.c_int64), ("f", C.c_int64), ("ldx", C.c_int64), ("ldw", C.c_int64), ("ldh", C.c_int64),
                 ("dtype", C.c_int32), ("act", C.c_int32), ("rows_out", C.c_int32), ("unaligned", C.c_int32)]
+
+
+class _AdamWTensor(C.Structure):
+    _fields_ = [("n", C.c_int64), ("p", C.c_void_p), ("master", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("p_dtype", C.c_int32), ("g_dtype", C.c_int32)]
+
+
+class _AdamWDesc(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double), ("step", C.c_int64),
+                ("lr_dev", C.c_void_p), ("step_dev", C.c_void_p), ("grad_scale_dev", C.c_void_p), ("seed", C.c_uint32), ("stochastic", C.c_int32), ("bits", C.c_int32)]
 
 
 class _SearchResult(C.Structure):
@@ -101,7 +113,7 @@ def load_library():
     lib.osscar_gram_static.argtypes = [vp, i64, i64, i32, vp, i64, i32, i64, i64, dbl, dbl, vp, vp, vp, vp]
     lib.osscar_debug_tile_schedule.restype = C.c_int32
     lib.osscar_debug_tile_schedule.argtypes = [i64, C.POINTER(i32), i32]
-    for name in ("osscar_gated_workspace_bytes", "osscar_int_workspace_bytes", "osscar_logprobs_workspace_bytes"):
+    for name in ("osscar_gated_workspace_bytes", "osscar_int_workspace_bytes", "osscar_logprobs_workspace_bytes", "osscar_layernorm_workspace_bytes"):
         getattr(lib, name).restype = C.c_size_t
     gd, f32 = C.POINTER(_GatedDesc), C.c_float
     lib.osscar_gated_workspace_bytes.argtypes = [gd, i32]
@@ -114,6 +126,11 @@ def load_library():
     lib.osscar_logprobs_workspace_bytes.argtypes = [i64, i64, i32]
     lib.osscar_logprobs.argtypes = [vp, i64, i64, i64, i32, vp, f32, i32, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
     lib.osscar_logprobs_backward.argtypes = [vp, i64, i64, i64, i32, vp, f32, vp, vp, vp, vp, i32, vp, vp, vp, i64, vp]
+    lib.osscar_layernorm_workspace_bytes.argtypes = [i64, i64]
+    lib.osscar_layernorm_forward.argtypes = [vp, i64, i64, i64, i32, vp, vp, i32, f32, vp, i64, vp, vp]
+    lib.osscar_layernorm_backward.argtypes = [vp, i64, i64, i64, i32, vp, i32, vp, i64, vp, vp, i64, vp, vp, i32, vp, C.c_size_t, vp]
+    lib.osscar_adamw.argtypes = [C.POINTER(_AdamWTensor), i64, C.POINTER(_AdamWDesc), vp]
+    lib.osscar_adamw_values.argtypes = [C.POINTER(_AdamWTensor), i64, C.POINTER(vp), C.POINTER(vp), vp]
     lib.osscar_last_error.restype = C.c_char_p
     lib.osscar_last_error.argtypes = [vp]
     for name in EXPORTED_SYMBOLS:

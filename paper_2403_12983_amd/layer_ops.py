@@ -13,11 +13,11 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
-from typing import NamedTuple, Optional, Tuple
+from typing import List, NamedTuple, Optional, Sequence, Tuple, Union
 
 import torch
 
-from .binding import OSSCAR_ACT_SILU, OSSCAR_BF16, OSSCAR_F32, OSSCAR_I8, OsscarError, _GatedDesc, load_library
+from .binding import OSSCAR_ACT_SILU, OSSCAR_BF16, OSSCAR_F32, OSSCAR_I8, OsscarError, _AdamWDesc, _AdamWTensor, _GatedDesc, load_library
 
 _CODES = {torch.float32: OSSCAR_F32, torch.bfloat16: OSSCAR_BF16}
 _EINVAL = 1
@@ -313,3 +313,226 @@ def osscar_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, lse: t
                                               handle)
     _done(lib, status)
     return out
+
+
+def _out(out: Optional[torch.Tensor], like: torch.Tensor, shape) -> torch.Tensor:
+    if out is None:
+        return _EMPTY(shape, dtype=like.dtype, device=like.device)
+    if out.shape != shape or out.dtype != like.dtype:
+        _refuse("out has another shape or dtype than the result")
+    return out
+
+
+def _gains(w: Optional[torch.Tensor], d: int, what: str) -> Tuple[Optional[int], Optional[int]]:
+    """(address, dtype) of a vector over the columns, or of none"""
+    return (None, None) if w is None else (_vector(w, d, w.dtype, what), _code(w, what))
+
+
+def osscar_layernorm_forward(X: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5, save: bool = False,
+                             out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Layer norm of the rows of X (n x d): (x - mean) / sqrt(var + eps) * weight + bias.  weight, bias: d, float32 or bfloat16 (both the same), or None.  save: returns
+    (Y, stats) with the mean and 1 / sqrt(var + eps) of each row that osscar_layernorm_backward takes, else Y.  out: where to put Y, `X` itself included."""
+    lib, index, handle, context = _begin(X, stream)
+    code, ldx = _code(X, "X"), _ld(X, "X")
+    n, d = X.shape
+    _on(index, weight=weight, bias=bias, out=out)
+    (wp, wc), (bp, bc) = _gains(weight, d, "weight"), _gains(bias, d, "bias")
+    if wc is not None and bc is not None and wc != bc:
+        _refuse("weight and bias have one dtype")
+    with context:
+        Y = _out(out, X, X.shape)
+        stats = _EMPTY(n, 2, dtype=torch.float32, device=X.device) if save else None
+        status = lib.osscar_layernorm_forward(X.data_ptr(), n, d, ldx, code, wp, bp, wc if wc is not None else bc if bc is not None else code, eps, Y.data_ptr(),
+                                              _ld(Y, "out"), stats.data_ptr() if save else None, handle)
+    _done(lib, status)
+    return (Y, stats) if save else Y
+
+
+def osscar_layernorm_backward(X: torch.Tensor, weight: Optional[torch.Tensor], dY: torch.Tensor, stats: torch.Tensor, need_x: bool = True, need_w: bool = True,
+                              dw_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """(dX, dweight, dbias) of osscar_layernorm_forward for the gradient dY of Y; None for what is not needed.  stats: from forward's save=True.  dw_dtype: float32 or bfloat16,
+    by default the weight's (without one: that of X).  out: where to put dX, `dY` or `X` itself included."""
+    lib, index, handle, context = _begin(X, stream)
+    code, ldx = _code(X, "X"), _ld(X, "X")
+    n, d = X.shape
+    if dY.shape != X.shape or dY.dtype != X.dtype:
+        _refuse("dY has the shape and dtype of X")
+    if stats.shape != (n, 2) or stats.dtype != torch.float32 or not stats.is_contiguous():
+        _refuse("stats must be the n x 2 float32 tensor of osscar_layernorm_forward")
+    _on(index, weight=weight, dY=dY, stats=stats, out=out)
+    wp, wc = _gains(weight, d, "weight")
+    wc = code if wc is None else wc
+    if dw_dtype is None:
+        dw_dtype = X.dtype if weight is None else weight.dtype
+    if dw_dtype not in _CODES:
+        _refuse(f"dw_dtype {dw_dtype} is neither float32 nor bfloat16")
+    if out is not None and not need_x:
+        _refuse("out goes with need_x")
+    with context:
+        dX = _out(out, X, X.shape) if need_x else None
+        dw = db = ws = None
+        size, wsp = 0, None
+        if need_w:
+            dw, db = _EMPTY(d, dtype=dw_dtype, device=X.device), _EMPTY(d, dtype=dw_dtype, device=X.device)
+            ws, wsp, size = _workspace(lib.osscar_layernorm_workspace_bytes(n, d), X.device)
+        status = lib.osscar_layernorm_backward(X.data_ptr(), n, d, ldx, code, wp, wc, dY.data_ptr(), _ld(dY, "dY"), stats.data_ptr(),
+                                               dX.data_ptr() if need_x else None, _ld(dX, "out") if need_x else d, dw.data_ptr() if need_w else None,
+                                               db.data_ptr() if need_w else None, _CODES[dw_dtype], wsp, size, handle)
+    _done(lib, status)
+    return dX, dw, db
+
+
+_BLOCK = 256
+
+
+def _place(t: torch.Tensor) -> Tuple[Tuple[int, ...], Tuple[int, ...]]:
+    """Shape, and strides where they say something."""
+    return tuple(t.shape), tuple(s for k, s in zip(t.shape, t.stride()) if k > 1)
+
+
+def _dense(t: torch.Tensor) -> bool:
+    """Whether the elements fill a piece of memory, in any order of the dimensions."""
+    at = 1
+    for stride, size in sorted((s, k) for s, k in zip(t.stride(), t.shape) if k > 1):
+        if stride != at:
+            return False
+        at *= size
+    return True
+
+
+class AdamWState(NamedTuple):
+    """The states of one parameter, in the order of its memory: float32 m and v; or in 8 bits codes of m (float8_e4m3fn) and of sqrt(v) (uint8), with a float32
+    scale for every 256 of them."""
+    m: torch.Tensor
+    v: torch.Tensor
+    m_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+
+
+class AdamWValues(NamedTuple):
+    """What 8-bit states stand for, in bfloat16 (exactly): m and the root of v, of the parameter's shape."""
+    m: torch.Tensor
+    root: torch.Tensor
+
+
+class AdamW:
+    """A list of parameters with their gradients and states, looked over once; osscar_adamw makes a step over all of them.
+
+    params: float32 or bfloat16 on one GPU, any shape, their elements side by side in memory (a transposed matrix will do).  grads: of the same shapes and layouts, float32 or
+    bfloat16; they may also be given, or given anew, at each step.  masters: a float32 copy for bfloat16 parameters, or None, as a list or None for all.  states: one AdamWState per
+    parameter, or None: zeros in `bits` bits.  The plan holds the tensors and writes to where they were when it was made; autograd does not see it."""
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Optional[Sequence[torch.Tensor]] = None, bits: Optional[int] = None,
+                 masters: Optional[Sequence[Optional[torch.Tensor]]] = None, states: Optional[Sequence[AdamWState]] = None):
+        self.params = list(params)
+        if not self.params:
+            _refuse("no parameters")
+        count = len(self.params)
+        self.masters = [None] * count if masters is None else list(masters)
+        if bits is None:
+            bits = 8 if states and states[0].m_scale is not None else 32
+        if bits not in (8, 32):
+            _refuse("states have 8 or 32 bits")
+        self.bits, self._device = bits, self.params[0].device
+        self._index = self.params[0].get_device()
+        self._lib = _begin(self.params[0], None)[0]
+        self._table = (_AdamWTensor * count)()
+        self._places = [_place(p) for p in self.params]
+        if len(self.masters) != count or (states is not None and len(states) != count):
+            _refuse("masters and states have one entry per parameter")
+        self.states: List[AdamWState] = []
+        written = set()
+        for k, (p, master) in enumerate(zip(self.params, self.masters)):
+            n = p.numel()
+            code = _code(p, f"parameter {k}")
+            if not _dense(p):
+                _refuse(f"the elements of parameter {k} are not side by side")
+            if master is not None and (p.dtype != torch.bfloat16 or master.dtype != torch.float32 or _place(master) != self._places[k]):
+                _refuse(f"master {k} must be float32, of the shape and layout of a bfloat16 parameter")
+            s = self._zeros(n) if states is None else AdamWState(*states[k])
+            blocks = -(-n // _BLOCK)
+            kinds = ((s.m, n, (torch.float32,)), (s.v, n, (torch.float32,))) if bits == 32 else (
+                (s.m, n, (torch.float8_e4m3fn, torch.uint8)), (s.v, n, (torch.uint8,)), (s.m_scale, blocks, (torch.float32,)), (s.v_scale, blocks, (torch.float32,)))
+            for t, size, dtypes in kinds:
+                if t is None or t.numel() != size or t.dtype not in dtypes or not t.is_contiguous():
+                    _refuse(f"state {k} is not of {bits} bits and parameter {k}'s size, side by side")
+            _on(self._index, **{f"parameter {k}": p, f"master {k}": master, f"state {k}": s.m, f"state {k}'s v": s.v, f"state {k}'s m_scale": s.m_scale, f"state {k}'s v_scale": s.v_scale})
+            for t in (p, master, *s):
+                if t is not None and t.numel() > 0:
+                    if t.data_ptr() in written:
+                        _refuse(f"parameter {k} or one of its states is listed twice")
+                    written.add(t.data_ptr())
+            self.states.append(s)
+            self._table[k] = _AdamWTensor(n, p.data_ptr(), None if master is None else master.data_ptr(), None, s.m.data_ptr(), s.v.data_ptr(),
+                                          s.m_scale.data_ptr() if bits == 8 else None, s.v_scale.data_ptr() if bits == 8 else None, code, 0)
+        self.grads: Optional[List[torch.Tensor]] = None
+        if grads is not None:
+            self._take(grads)
+
+    def _zeros(self, n: int) -> AdamWState:
+        if self.bits == 32:
+            return AdamWState(torch.zeros(n, dtype=torch.float32, device=self._device), torch.zeros(n, dtype=torch.float32, device=self._device))
+        blocks = -(-n // _BLOCK)
+        return AdamWState(torch.zeros(n, dtype=torch.uint8, device=self._device).view(torch.float8_e4m3fn), torch.zeros(n, dtype=torch.uint8, device=self._device),
+                          torch.zeros(blocks, dtype=torch.float32, device=self._device), torch.zeros(blocks, dtype=torch.float32, device=self._device))
+
+    def _take(self, grads: Sequence[torch.Tensor]):
+        grads = list(grads)
+        if len(grads) != len(self.params):
+            _refuse("one gradient per parameter")
+        for k, g in enumerate(grads):
+            _code(g, f"gradient {k}")
+            if _place(g) != self._places[k]:
+                _refuse(f"gradient {k} has another shape or layout than its parameter")
+            if g.get_device() != self._index:
+                _refuse(f"gradient {k} is on {g.device}, expected cuda:{self._index}")
+        for k, g in enumerate(grads):
+            self._table[k].g, self._table[k].g_dtype = g.data_ptr(), _CODES[g.dtype]
+        self.grads = grads
+
+    def _scalar(self, t: torch.Tensor, dtype: torch.dtype, what: str) -> int:
+        if t.dtype != dtype or t.numel() != 1 or t.get_device() != self._index:
+            _refuse(f"{what} must be one {dtype} on cuda:{self._index}")
+        return t.data_ptr()
+
+    def osscar_adamw(self, lr: Union[float, torch.Tensor], step: Union[int, torch.Tensor], beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
+                     grads: Optional[Sequence[torch.Tensor]] = None, grad_scale: Optional[torch.Tensor] = None, seed: Optional[int] = None,
+                     stream: Optional[torch.cuda.Stream] = None) -> None:
+        """One step of AdamW, in place.  step counts from 1; lr and step may be tensors of one element on the GPU (float32, int64), which a captured step reads anew at each replay.
+        grads: new gradients, kept for later steps.  grad_scale: one float32 on the GPU that the gradients are multiplied by; where it is not finite nothing
+        changes.  seed (32 bits, another for each step): 8-bit states, and bfloat16 parameters without a master, are rounded up by chance instead of to the nearest."""
+        if grads is not None:
+            self._take(grads)
+        if self.grads is None:
+            _refuse("no gradients were given")
+        lib, _, handle, context = _begin(self.params[0], stream)
+        desc = _AdamWDesc(0.0, beta1, beta2, eps, weight_decay, 1, None, None, None, 0, 0, self.bits)
+        if isinstance(lr, torch.Tensor):
+            desc.lr_dev = self._scalar(lr, torch.float32, "lr")
+        else:
+            desc.lr = lr
+        if isinstance(step, torch.Tensor):
+            desc.step_dev = self._scalar(step, torch.int64, "step")
+        else:
+            desc.step = step
+        if grad_scale is not None:
+            desc.grad_scale_dev = self._scalar(grad_scale, torch.float32, "grad_scale")
+        if seed is not None:
+            if not 0 <= seed < 1 << 32:
+                _refuse("seed has 32 bits")
+            desc.seed, desc.stochastic = seed, 1
+        with context:
+            status = lib.osscar_adamw(self._table, len(self.params), C.byref(desc), handle)
+        _done(lib, status)
+
+    def osscar_adamw_values(self, stream: Optional[torch.cuda.Stream] = None) -> List[AdamWValues]:
+        """What the 8-bit states stand for, one AdamWValues per parameter."""
+        if self.bits != 8:
+            _refuse("states of 32 bits are their own values")
+        lib, _, handle, context = _begin(self.params[0], stream)
+        with context:
+            values = [AdamWValues(torch.empty_like(p, dtype=torch.bfloat16, requires_grad=False), torch.empty_like(p, dtype=torch.bfloat16, requires_grad=False)) for p in self.params]
+            outs = C.c_void_p * len(values)
+            status = lib.osscar_adamw_values(self._table, len(values), outs(*(x.m.data_ptr() for x in values)), outs(*(x.root.data_ptr() for x in values)), handle)
+        _done(lib, status)
+        return values
