@@ -355,8 +355,10 @@ extern "C" osscar_status osscar_adamw(const osscar_adamw_tensor* tensors, int64_
   if (!bad && !d->lr_dev && !(d->lr >= 0 && (float)d->lr < INFINITY)) bad = "osscar_adamw: lr must not be negative";
   if (!bad && !d->step_dev && d->step < 1) bad = "osscar_adamw: steps count from 1";
   if (!bad && (((uintptr_t)d->lr_dev & 3) || ((uintptr_t)d->step_dev & 7) || ((uintptr_t)d->grad_scale_dev & 3))) bad = "osscar_adamw: a buffer is not aligned to its elements";
-  for (int64_t k = 0; !bad && k < count; k++) bad = bad_tensor(tensors[k], d->bits == 8, false);
+  bool any = false;
+  for (int64_t k = 0; !bad && k < count; k++) { bad = bad_tensor(tensors[k], d->bits == 8, false); any = any || tensors[k].n > 0; }
   if (bad) return refuse_call(OSSCAR_EINVAL, bad);
+  if (!any) return OSSCAR_OK;
   const Step s{d->lr, d->beta1, d->beta2, d->weight_decay, (float)d->eps, 1.f, d->step, d->lr_dev, d->grad_scale_dev, d->step_dev, d->seed, d->stochastic != 0};
   const Factors f = factors_of(s, d->lr_dev ? 0 : d->lr, d->step_dev ? 1 : d->step);
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
@@ -367,12 +369,15 @@ extern "C" osscar_status osscar_adamw(const osscar_adamw_tensor* tensors, int64_
 
 extern "C" osscar_status osscar_adamw_values(const osscar_adamw_tensor* tensors, int64_t count, void* const* m_out, void* const* root_out, void* hip_stream) {
   const char* bad = nullptr;
+  bool any = false;
   if (count < 0 || count > (int64_t)1 << 30 || (count > 0 && (!tensors || !m_out || !root_out))) bad = "osscar_adamw_values: NULL pointer or negative count";
   for (int64_t k = 0; !bad && k < count; k++) {
     bad = bad_tensor(tensors[k], true, true);
     if (!bad && tensors[k].n > 0 && (!m_out[k] || !root_out[k] || (((uintptr_t)m_out[k] | (uintptr_t)root_out[k]) & 1))) bad = "osscar_adamw_values: an output is missing or not aligned to its elements";
+    any = any || tensors[k].n > 0;
   }
   if (bad) return refuse_call(OSSCAR_EINVAL, bad);
+  if (!any) return OSSCAR_OK;
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
   static_assert(sizeof(Values) <= 4096, "a launch's arguments");
   in_launches<Values>(

@@ -429,6 +429,8 @@ class AdamW:
             _refuse("no parameters")
         count = len(self.params)
         self.masters = [None] * count if masters is None else list(masters)
+        if states is not None:
+            states = [AdamWState(*s) for s in states]
         if bits is None:
             bits = 8 if states and states[0].m_scale is not None else 32
         if bits not in (8, 32):
@@ -449,7 +451,7 @@ class AdamW:
                 _refuse(f"the elements of parameter {k} are not side by side")
             if master is not None and (p.dtype != torch.bfloat16 or master.dtype != torch.float32 or _place(master) != self._places[k]):
                 _refuse(f"master {k} must be float32, of the shape and layout of a bfloat16 parameter")
-            s = self._zeros(n) if states is None else AdamWState(*states[k])
+            s = self._zeros(n) if states is None else states[k]
             blocks = -(-n // _BLOCK)
             kinds = ((s.m, n, (torch.float32,)), (s.v, n, (torch.float32,))) if bits == 32 else (
                 (s.m, n, (torch.float8_e4m3fn, torch.uint8)), (s.v, n, (torch.uint8,)), (s.m_scale, blocks, (torch.float32,)), (s.v_scale, blocks, (torch.float32,)))

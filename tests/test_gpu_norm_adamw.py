@@ -1,0 +1,590 @@
+"""Layer norm and AdamW against plain float64 implementations of their definitions.
+
+Tolerances.  u = 2^-8 is the largest relative error of rounding to bf16, e = 2^-24 that of float32.  A float32 sum of K terms is off by a random walk of about e sqrt(K) of the sum of
+their sizes; walk(K) = e (4 + 2 sqrt(K)) is allowed, elementwise.  Layer norm: with c = x - mean and h = c r, both sums of a row (of c and of c^2) and the roundings of c, r and
+the products leave an error of h of walk(d) (|h| + 1) (h has unit size, and so has what the mean's error does to it); a mean rounded to float32 adds
+e |mean| r.  AdamW: each of m, v, p is a handful of float32 operations, counted beside the check; 8-bit codes have to be equal."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U, E = 2.0 ** -8, 2.0 ** -24
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def walk(K):
+    return E * (4 + 2 * math.sqrt(K))
+
+
+@pytest.fixture(scope="module")
+def osscar():
+    import paper_2403_12983_amd as pkg
+    pkg.load_library()
+    return pkg
+
+
+def _gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def _randn(g, *shape, scale=1.0, dtype=F32):
+    return (torch.randn(*shape, generator=g, device=DEV) * scale).to(dtype)
+
+
+def _within(got, want, tolerance, what):
+    got, want = got.double(), want.double()
+    assert got.shape == want.shape and torch.equal(torch.isfinite(got), torch.isfinite(want)), what
+    over = ((got - want).abs() - tolerance)
+    assert over.numel() == 0 or over.max().item() <= 0, (what, over.max().item(), (got - want).abs().max().item())
+
+
+# --------------------------------------------------------------------------------------------------
+# layer norm
+# --------------------------------------------------------------------------------------------------
+def _strided(t, pad, shift):
+    """The same values in rows `pad` elements apart from each other, beginning `shift` elements into their memory."""
+    n, d = t.shape
+    flat = torch.full((shift + n * (d + pad),), 7.0, dtype=t.dtype, device=t.device)
+    view = flat[shift:].view(n, d + pad)[:, :d]
+    view.copy_(t)
+    return view, flat
+
+
+def _norm64(X, w, b, eps):
+    x = X.double()
+    mean = x.mean(1, keepdim=True)
+    c = x - mean
+    r = 1 / torch.sqrt((c * c).mean(1, keepdim=True) + eps)
+    h = c * r
+    w = torch.ones(X.shape[1], dtype=torch.float64, device=DEV) if w is None else w.double()
+    return mean, r, h, w, h * w + (0 if b is None else b.double())
+
+
+def _check_norm(pkg, X, w, b, dY, eps=1e-5, **kw):
+    n, d = X.shape
+    rounding = U if X.dtype == BF16 else 0.0
+    mean, r, h, w64, y = _norm64(X, w, b, eps)
+    Y, stats = pkg.osscar_layernorm_forward(X, w, b, eps, save=True)
+    assert Y.dtype == X.dtype
+    _within(Y, y, walk(d) * (w64.abs() * (h.abs() + 1) + 2 * y.abs()) + rounding * y.abs(), "Y")
+    _within(stats[:, 0], mean[:, 0], walk(d) * (X.double().abs().mean(1) / 16 + (X.double() - mean).abs().mean(1)) + E * mean[:, 0].abs(), "mean")
+    _within(stats[:, 1], r[:, 0], walk(d) * r[:, 0], "r")
+    assert torch.equal(Y, pkg.osscar_layernorm_forward(X, w, b, eps))      # without keeping, the same bits
+    dy = dY.double()
+    g = dy * w64
+    m1, m2 = g.mean(1, keepdim=True), (g * h).mean(1, keepdim=True)
+    dx = r * (g - m1 - h * m2)
+    off = h.abs() + 1 + mean.abs() * r      # what an error of walk(d) of h goes by
+    size = r * (g.abs() + g.abs().mean(1, keepdim=True) + 2 * off * ((g * h).abs().mean(1, keepdim=True) + (g.abs() * off).mean(1, keepdim=True)))
+    got = pkg.osscar_layernorm_backward(X, w, dY, stats, **kw)
+    _within(got[0], dx, 2 * walk(d) * size + rounding * dx.abs(), "dX")
+    for x, want, s, name in ((got[1], (dy * h).sum(0), (dy.abs() * off).sum(0), "dw"), (got[2], dy.sum(0), dy.abs().sum(0), "db")):
+        _within(x, want, (walk(n) + walk(d)) * s + (U if x.dtype == BF16 else 0.0) * want.abs(), name)
+    return Y, stats, got
+
+
+NORMS = [(1, 1), (3, 2), (2, 7), (1, 8), (5, 9), (7, 63), (40, 64), (33, 257), (1, 2048), (9, 512), (1030, 513), (64, 1024), (17, 1365), (2100, 2048), (5, 2049), (12, 4096), (130, 5461),
+         (300, 7168), (3, 8193), (9, 14336), (2, 16384), (3, 16385), (2, 40001)]
+
+
+@pytest.mark.parametrize("dtype,w_dtype", [(BF16, BF16), (F32, F32), (BF16, F32), (F32, BF16)])
+@pytest.mark.parametrize("n,d", NORMS)
+def test_layernorm(osscar, n, d, dtype, w_dtype):
+    g = _gen(n * 7 + d)
+    X = (_randn(g, n, d) * torch.exp(0.5 * _randn(g, d)) + 0.5 * _randn(g, d)).to(dtype)
+    w, b = (1 + _randn(g, d, scale=0.2)).to(w_dtype), _randn(g, d, scale=0.2, dtype=w_dtype)
+    dY = _randn(g, n, d, dtype=dtype)
+    got = _check_norm(osscar, X, w, b, dY)[2]
+    assert got[0].dtype == dtype and got[1].dtype == w_dtype == got[2].dtype
+    again = osscar.osscar_layernorm_backward(X, w, dY, osscar.osscar_layernorm_forward(X, w, b, save=True)[1])
+    assert all(torch.equal(x, y) for x, y in zip(got, again))      # the same bits again
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,d", [(5, 3), (37, 200), (64, 1365), (20, 7161), (3, 20001)])
+def test_layernorm_strides_and_missing_parts(osscar, n, d, dtype):
+    g = _gen(d)
+    plain = _randn(g, n, d, dtype=dtype), _randn(g, n, d, dtype=dtype)
+    w, b = _randn(g, d, dtype=F32), _randn(g, d, dtype=F32)
+    Y0, stats0, got0 = _check_norm(osscar, plain[0], w, b, plain[1])
+    for pad, shift in ((0, 1), (3, 0), (5, 3), (8, 8)):
+        (X, fx), (dY, fy) = _strided(plain[0], pad, shift), _strided(plain[1], pad, shift)
+        out, fo = _strided(torch.zeros_like(X), pad, shift)
+        before = fo.clone()
+        Y, stats = osscar.osscar_layernorm_forward(X, w, b, save=True, out=out)
+        assert Y is out and torch.equal(Y, Y0) and torch.equal(stats, stats0)
+        before[shift:].view(n, d + pad)[:, :d] = Y0
+        assert torch.equal(fo, before)      # nothing beside the rows
+        out.zero_()
+        got = osscar.osscar_layernorm_backward(X, w, dY, stats, out=out)
+        assert got[0] is out and all(torch.equal(x, y) for x, y in zip(got, got0))
+        before[shift:].view(n, d + pad)[:, :d] = got0[0]
+        assert torch.equal(fo, before)
+        # in place
+        osscar.osscar_layernorm_forward(X, w, b, out=X)
+        assert torch.equal(X, Y0)
+        X.copy_(plain[0])
+        got = osscar.osscar_layernorm_backward(X, w, dY, stats, out=dY)
+        assert torch.equal(dY, got0[0]) and torch.equal(got[1], got0[1])
+        dY.copy_(plain[1])
+        osscar.osscar_layernorm_backward(X, w, dY, stats, out=X)
+        assert torch.equal(X, got0[0])
+    X, dY = plain
+    _check_norm(osscar, X, None, None, dY, dw_dtype=F32)
+    _check_norm(osscar, X, w, None, dY, eps=0.3)
+    _check_norm(osscar, X, None, b, dY)
+    stats = stats0
+    only = osscar.osscar_layernorm_backward(X, w, dY, stats, need_w=False)
+    assert only[1] is None and only[2] is None and torch.equal(only[0], got0[0])
+    only = osscar.osscar_layernorm_backward(X, w, dY, stats, need_x=False)
+    assert only[0] is None and torch.equal(only[1], got0[1]) and torch.equal(only[2], got0[2])
+
+
+@pytest.mark.parametrize("d", [6, 100, 1365, 9000, 17000])
+def test_layernorm_of_rows_far_from_zero_and_constant_rows(osscar, d):
+    g = _gen(d)
+    X = _randn(g, 6, d) + 1000
+    X[1] = 123.456
+    X[2] = 0
+    X[3] = 1e-20 * X[3]
+    X[4] = 1e15 * _randn(g, d)
+    Y, stats, _ = _check_norm(osscar, X, None, None, _randn(g, 6, d))
+    assert Y[2].abs().max() == 0 and Y[1].abs().max() < 1e-4 and stats[2].tolist() == pytest.approx([0, 1e5 ** 0.5])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [5, 300, 2048, 7168, 30000])
+def test_layernorm_keeps_what_is_not_finite_in_its_row(osscar, d, dtype):
+    g = _gen(d)
+    X, dY = _randn(g, 8, d, dtype=dtype), _randn(g, 8, d, dtype=dtype)
+    w = _randn(g, d, dtype=F32)
+    Y, stats = osscar.osscar_layernorm_forward(X, w, save=True)
+    dX = osscar.osscar_layernorm_backward(X, w, dY, stats, need_w=False)[0]
+    bad = X.clone()
+    bad[1, d // 2], bad[3, 0], bad[5] = math.inf, math.nan, 3e38
+    bad[6, d - 1] = -math.inf
+    Y2, stats2 = osscar.osscar_layernorm_forward(bad, w, save=True)
+    dX2 = osscar.osscar_layernorm_backward(bad, w, dY, stats2, need_w=False)[0]
+    for row in range(8):
+        if row in (1, 3, 6):
+            assert torch.isnan(Y2[row]).all() and torch.isnan(dX2[row]).all()
+        elif row != 5:
+            assert torch.equal(Y2[row], Y[row]) and torch.equal(dX2[row], dX[row])
+    dY[2, d // 3] = math.nan
+    dX3, dw, db = osscar.osscar_layernorm_backward(X, w, dY, stats)
+    assert torch.isnan(dX3[2]).all() and torch.equal(dX3[0], dX[0])
+    assert torch.isnan(dw).nonzero().flatten().tolist() == torch.isnan(db).nonzero().flatten().tolist() == [d // 3]
+
+
+def test_layernorm_without_rows_and_with_many(osscar):
+    w = torch.ones(300, device=DEV)
+    X = torch.empty(0, 300, device=DEV)
+    Y, stats = osscar.osscar_layernorm_forward(X, w, save=True)
+    assert Y.shape == (0, 300)
+    dX, dw, db = osscar.osscar_layernorm_backward(X, w, X, stats)
+    assert dX.shape == (0, 300) and dw.abs().max() == 0 and db.abs().max() == 0
+    g = _gen(1)
+    X, dY = _randn(g, 300000, 24, dtype=BF16), _randn(g, 300000, 24, dtype=BF16)
+    _check_norm(osscar, X, torch.ones(24, device=DEV), None, dY)
+
+
+def test_layernorm_gradient_against_differences(osscar):
+    """f(t) = sum dY norm(X + t V): the slope from dX, and from f itself at two points (error of the third order, t^2, and float32's of Y over t)."""
+    g = _gen(5)
+    n, d = 12, 700
+    X, V, dY, w = _randn(g, n, d), _randn(g, n, d), _randn(g, n, d), 1 + _randn(g, d, scale=0.2)
+    _, stats = osscar.osscar_layernorm_forward(X, w, save=True)
+    dX = osscar.osscar_layernorm_backward(X, w, dY, stats)[0]
+    t = 2.0 ** -6
+    f = [(dY.double() * osscar.osscar_layernorm_forward(X + s * V, w).double()).sum() for s in (t, -t)]
+    slope = ((f[0] - f[1]) / (2 * t)).item()
+    # third derivatives of a normalised row are below 20 of |V|^3 / size^3, with |V| = size = 1; f is a random sum of n d terms
+    assert abs((dX.double() * V.double()).sum().item() - slope) <= math.sqrt(n * d) * (20 * t * t / 6 + 4 * walk(d) / t)
+
+
+def test_layernorm_captured_and_on_another_stream(osscar):
+    g = _gen(9)
+    X, dY, w = _randn(g, 500, 1365, dtype=BF16), _randn(g, 500, 1365, dtype=BF16), _randn(g, 1365)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    Y, stats = osscar.osscar_layernorm_forward(X, w, save=True, stream=side)
+    got = osscar.osscar_layernorm_backward(X, w, dY, stats, stream=side)
+    side.synchronize()
+    want = osscar.osscar_layernorm_backward(X, w, dY, osscar.osscar_layernorm_forward(X, w, save=True)[1])
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        Yg, sg = osscar.osscar_layernorm_forward(X, w, save=True)
+        gg = osscar.osscar_layernorm_backward(X, w, dY, sg)
+    for k in range(3):
+        X.copy_(_randn(g, 500, 1365, dtype=BF16))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = osscar.osscar_layernorm_backward(X, w, dY, osscar.osscar_layernorm_forward(X, w, save=True)[1])
+        assert all(torch.equal(x, y) for x, y in zip(gg, want))
+
+
+def test_layernorm_refusals(osscar):
+    X, w = torch.zeros(4, 16, device=DEV), torch.zeros(16, device=DEV)
+    stats = torch.zeros(4, 2, device=DEV)
+    bad = [lambda: osscar.osscar_layernorm_forward(X.half()), lambda: osscar.osscar_layernorm_forward(X[0]), lambda: osscar.osscar_layernorm_forward(X.t()),
+           lambda: osscar.osscar_layernorm_forward(X, w[:8]), lambda: osscar.osscar_layernorm_forward(X, w, w.bfloat16()), lambda: osscar.osscar_layernorm_forward(X, w.cpu()),
+           lambda: osscar.osscar_layernorm_forward(X, eps=0.0), lambda: osscar.osscar_layernorm_forward(X, eps=math.nan), lambda: osscar.osscar_layernorm_forward(X, eps=1e-60),
+           lambda: osscar.osscar_layernorm_forward(X, out=X[:3]), lambda: osscar.osscar_layernorm_forward(X, out=X.bfloat16()), lambda: osscar.osscar_layernorm_forward(X[:0].expand(4, 0)),
+           lambda: osscar.osscar_layernorm_backward(X, w, X.bfloat16(), stats), lambda: osscar.osscar_layernorm_backward(X, w, X[:3], stats),
+           lambda: osscar.osscar_layernorm_backward(X, w, X, stats[:3]), lambda: osscar.osscar_layernorm_backward(X, w, X, stats.double()),
+           lambda: osscar.osscar_layernorm_backward(X, w, X, stats, dw_dtype=torch.half), lambda: osscar.osscar_layernorm_backward(X, w, X, stats, need_x=False, out=X)]
+    for k, call in enumerate(bad):
+        with pytest.raises((osscar.OsscarError, RuntimeError)) as e:
+            call()
+        if k != 11:
+            assert isinstance(e.value, osscar.OsscarError) and e.value.status == 1, k
+
+
+# --------------------------------------------------------------------------------------------------
+# AdamW
+# --------------------------------------------------------------------------------------------------
+LR, B1, B2, EPS, WD = 3e-3, 0.9, 0.999, 1e-6, 0.05
+
+
+def _factors(lr, step, b1, b2, wd):
+    return [np.float32(x) for x in (b1, 1 - b1, b2, 1 - b2, 1 - lr * wd, lr / (1 - b1 ** step), 1 / math.sqrt(1 - b2 ** step))]
+
+
+def _step32(p, g, m, v, step, lr=LR, b1=B1, b2=B2, eps=EPS, wd=WD):
+    """The definition in float32, each operation rounded by itself (numpy)."""
+    f1, c1, f2, c2, decay, a, c = _factors(lr, step, b1, b2, wd)
+    m = m * f1 + g * c1
+    v = v * f2 + (g * g) * c2
+    root = np.sqrt(v)
+    return p * decay - a * (m / (root * c + np.float32(eps))), m, v, root
+
+
+E4M3 = np.array([(s * (a % 8) * 2.0 ** -9 if a < 8 else s * (8 + a % 8) * 2.0 ** (a // 8 - 10)) if a < 127 else math.nan for s in (1, -1) for a in range(128)])
+ROOTS = np.array([c if c < 16 else (16 + c % 16) * 2.0 ** (c // 16 - 1) for c in range(256)])
+
+
+def _power(x):
+    return 2.0 ** (np.floor(np.log2(x)) if x > 0 else -126)
+
+
+def _codes(x, table, top, keep):
+    """The nearest of table's numbers (ascending, not negative) to |x| / scale, of two as near the even one, block by block; keep: above zero stays there."""
+    codes, scales = np.zeros(x.size, np.int64), np.zeros(-(-x.size // 256))
+    for b in range(scales.size):
+        y = np.abs(x[b * 256:(b + 1) * 256]).astype(np.float64)
+        scales[b] = max(_power(y.max()) / 2.0 ** top, 2.0 ** -126)
+        z = y / scales[b]
+        hi = np.clip(np.searchsorted(table, z), 1, table.size - 1)
+        lo = hi - 1
+        d = (table[hi] - z) - (z - table[lo])
+        c = np.where(d < 0, hi, np.where(d > 0, lo, np.where(lo % 2 == 0, lo, hi)))
+        codes[b * 256:(b + 1) * 256] = np.where(keep & (y > 0), np.maximum(c, 1), c)
+    return codes, scales
+
+
+def _np(t):
+    return t.detach().float().cpu().numpy()
+
+
+def _tensors(g, shapes, p_dtype, g_dtype):
+    return [_randn(g, *s, scale=0.3, dtype=p_dtype) for s in shapes], [(_randn(g, *s) * torch.exp(3 * _randn(g, *s)) * 1e-2).to(g_dtype) for s in shapes]
+
+
+SHAPES = [(1,), (7,), (8,), (255,), (256,), (257,), (2047,), (2048,), (2049,), (5, 1365), (64, 300), (3, 5, 7), (0,), (20001,)]
+
+
+@pytest.mark.parametrize("g_dtype", [F32, BF16])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "master"])
+def test_adamw_32(osscar, kind, g_dtype):
+    g = _gen(3)
+    params, grads = _tensors(g, SHAPES, F32 if kind == "f32" else BF16, g_dtype)
+    masters = [p.float() + _randn(g, *p.shape, scale=1e-4) for p in params] if kind == "master" else None
+    plan = osscar.AdamW(params, grads, masters=masters)
+    kept = masters if masters else params
+    want = [(_np(p).ravel(), np.zeros(p.numel(), np.float32), np.zeros(p.numel(), np.float32)) for p in kept]
+    exact = [tuple(x.astype(np.float64) for x in w) for w in want]
+    for step in (1, 2, 3):
+        plan.osscar_adamw(LR, step, B1, B2, EPS, WD)
+        for k, (p, s) in enumerate(zip(kept, plan.states)):
+            gr = _np(grads[k]).ravel()
+            np_, m, v, _ = _step32(want[k][0], gr, *want[k][1:], step)
+            if p.dtype == BF16:
+                np_ = _np(torch.from_numpy(np_).to(BF16))
+            # the definition to the bit
+            assert np.array_equal(_np(p).ravel(), np_) and np.array_equal(_np(s.m), m) and np.array_equal(_np(s.v), v), (k, step)
+            if masters:
+                assert torch.equal(params[k], p.to(BF16))
+            # and in 64 bits, from the same state: factors, products and sums are rounded once each (m 4, v 5 roundings of positive terms; the root half of v's and
+            # its own, the denominator two, the quotient and the product one each: 10 of the step; p three)
+            x = [a.astype(np.float64) for a in want[k]]
+            g64 = gr.astype(np.float64)
+            m64, v64 = B1 * x[1] + (1 - B1) * g64, B2 * x[2] + (1 - B2) * g64 ** 2
+            den = np.sqrt(v64 / (1 - B2 ** step)) + EPS
+            up = LR / (1 - B1 ** step) * m64 / den
+            p64 = x[0] * (1 - LR * WD) - up
+            mass = B1 * np.abs(x[1]) + (1 - B1) * np.abs(g64)
+            tiny = 1e-44      # steps of the smallest numbers, under which squares of gradients fall
+            assert np.all(np.abs(m - m64) <= 4 * E * mass + tiny) and np.all(np.abs(v - v64) <= 5 * E * v64 + tiny)
+            off = 3 * E * np.abs(x[0]) + 10 * E * np.abs(up) + LR / (1 - B1 ** step) * 4 * E * mass / den
+            assert np.all(np.abs(_np(p).ravel() - p64) <= off * 1.01 + (U * np.abs(p64) if p.dtype == BF16 else 0))
+            want[k] = (np_, m, v)
+    del exact
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "master"])
+def test_adamw_8_bits_to_the_nearest(osscar, kind):
+    g = _gen(4)
+    params, grads = _tensors(g, SHAPES, F32 if kind == "f32" else BF16, F32)
+    masters = [p.float() for p in params] if kind == "master" else None
+    plan = osscar.AdamW(params, grads, bits=8, masters=masters)
+    kept = masters if masters else params
+    state = [(_np(p).ravel(), np.zeros(p.numel(), np.float32), np.zeros(p.numel(), np.float32)) for p in kept]
+    for step in (1, 2, 3, 4):
+        plan.osscar_adamw(LR, step, B1, B2, EPS, WD)
+        values = plan.osscar_adamw_values()
+        for k, (p, s, x) in enumerate(zip(kept, plan.states, values)):
+            np_, m, v, root = _step32(state[k][0], _np(grads[k]).ravel(), *state[k][1:], step)
+            if p.dtype == BF16:
+                np_ = _np(torch.from_numpy(np_).to(BF16))
+            assert np.array_equal(_np(p).ravel(), np_)
+            cm, sm = _codes(m, E4M3[:127], 7, False)
+            cv, sv = _codes(root, ROOTS, 17, True)
+            codes = s.m.view(torch.uint8).cpu().numpy()
+            assert np.array_equal(codes & 127, cm) and np.array_equal(codes >> 7, np.signbit(m)) and np.array_equal(s.v.cpu().numpy(), cv), (k, step)
+            assert np.array_equal(_np(s.m_scale), sm) and np.array_equal(_np(s.v_scale), sv)
+            blocks = np.arange(m.size) // 256
+            vm, vr = E4M3[codes] * sm[blocks], ROOTS[cv] * sv[blocks]
+            assert x.m.shape == p.shape and x.m.dtype == BF16 and np.array_equal(_np(x.m).ravel(), vm) and np.array_equal(_np(x.root).ravel(), vr)      # exactly, in bf16
+            vr = vr.astype(np.float32)
+            state[k] = (np_, vm.astype(np.float32), vr * vr)
+            # half a step off at most: e4m3 2^-4 of the number or half of 2^-9 scales, the root 2^-5 or half a scale (a whole one where it stays above zero)
+            assert np.all(np.abs(vm - m) <= np.maximum(2.0 ** -4 * np.abs(m), 2.0 ** -10 * sm[blocks]))
+            assert np.all(np.abs(vr - root) <= np.maximum(2.0 ** -5 * root, np.where(root < sv[blocks] / 2, 1.0, 0.5) * sv[blocks]))
+
+
+def _mix(x):
+    x = ((x ^ (x >> 16)) * 0x9E3779B9) & 0xFFFFFFFF
+    x = ((x ^ (x >> 15)) * 0xB7E15163) & 0xFFFFFFFF
+    return x ^ (x >> 16)
+
+
+def test_adamw_rounded_by_chance(osscar):
+    g = _gen(6)
+    shapes = [(300,), (17, 33), (1,), (5000,)]
+    params, grads = _tensors(g, shapes, BF16, BF16)
+    plan = osscar.AdamW(params, grads, bits=8)
+    before = [_np(p).ravel() for p in params]
+    seed = 0xFFFFFFF1
+    plan.osscar_adamw(LR, 1, B1, B2, EPS, WD, seed=seed)
+    first = 0
+    for k, p in enumerate(params):
+        n = p.numel()
+        zero = np.zeros(n, np.float32)
+        np_, m, _, root = _step32(before[k], _np(grads[k]).ravel(), zero, zero, 1)
+        i = np.arange(first, first + n, dtype=np.uint64)
+        h = _mix((i & 0xFFFFFFFF) ^ _mix((i >> 32) ^ np.uint64(_mix(seed))))
+        first += -(-n // 256) * 256
+        # p: 16 bits of chance over the 16 that are cut off
+        bits = np_.view(np.uint32).astype(np.uint64)
+        assert np.array_equal(_np(p).ravel().view(np.uint32), (((bits + (h >> 16)) >> 16) << 16).astype(np.uint32)), k
+        s = plan.states[k]
+        for x, code, scale, table, part in ((np.abs(m), s.m.view(torch.uint8).cpu().numpy() & 127, _np(s.m_scale), E4M3[:127], (h & 0xFFFFF) / 2.0 ** 20),
+                                            (root, s.v.cpu().numpy(), _np(s.v_scale), ROOTS, (((h * 0x9E3779B9) & 0xFFFFFFFF) >> 13) / 2.0 ** 19)):
+            z = x.astype(np.float64) / scale[np.arange(n) // 256]
+            lo = np.clip(np.searchsorted(table, z, side="right") - 1, 0, table.size - 2)
+            up = (z - table[lo]) / (table[lo + 1] - table[lo]) + part >= 1
+            want = lo + up
+            if table is ROOTS:
+                want = np.where(x > 0, np.maximum(want, 1), want)
+            # below the normal numbers a sum is rounded to float32 before: where the chance is that near, either will do
+            near = np.abs((z - table[lo]) / (table[lo + 1] - table[lo]) + part - 1) < 2.0 ** -18
+            assert np.all((code == want) | near) and near.mean() < 0.01, k
+
+
+def test_adamw_by_chance_follows_what_nearest_loses(osscar):
+    """v of gradients of one size, from a v that is a quarter of theirs: 0.001 of the difference a step is less than half of a code's step, and is lost to the nearest."""
+    n, steps = 4096, 600
+    ends = {}
+    for way in ("nearest", "chance"):
+        p, gr = torch.zeros(n, device=DEV), torch.full((n,), 2e-2, device=DEV)
+        gr[::2] = -2e-2
+        state = osscar.AdamWState(torch.zeros(n, dtype=torch.uint8, device=DEV), torch.full((n,), 14 * 16, dtype=torch.uint8, device=DEV), torch.zeros(16, device=DEV),
+                                  torch.full((16,), 1e-2 / 2 ** 17, device=DEV))
+        plan = osscar.AdamW([p], [gr], states=[state])
+        for t in range(1, steps + 1):
+            plan.osscar_adamw(1e-3, t, seed=t if way == "chance" else None)
+        ends[way] = plan.osscar_adamw_values()[0].root.double().mean().item()
+    want = math.sqrt(4e-4 + (1e-4 - 4e-4) * B2 ** steps)
+    # the mean of 4096 walks whose step is 1/32 of the value: at the end each is off by less than its 0.1; and a root's rounding lifts its square by (step^2 / 12) a step,
+    # which 0.001 of the square takes back: (1/32)^2 / 12 / 0.002 / 2 < 0.03
+    assert abs(ends["chance"] - want) < 0.05 * want
+    assert abs(ends["nearest"] - 1e-2) < 0.04 * 1e-2      # to the nearest it has not moved
+
+
+def test_adamw_many_tensors_of_several_kinds(osscar):
+    g = _gen(8)
+    shapes = [(k % 13 + 1, k % 7 + 1) for k in range(400)]
+    params = [_randn(g, *s, dtype=(F32, BF16, BF16)[k % 3]) for k, s in enumerate(shapes)]
+    grads = [_randn(g, *s, dtype=(F32, BF16)[k % 2]) for k, s in enumerate(shapes)]
+    masters = [p.float() if k % 3 == 1 else None for k, p in enumerate(params)]
+    for bits in (32, 8):
+        together = [p.clone() for p in params]
+        plan = osscar.AdamW(together, grads, bits=bits, masters=[None if x is None else x.clone() for x in masters])
+        plan.osscar_adamw(LR, 5, B1, B2, EPS, WD)
+        for k, p in enumerate(params):
+            alone = p.clone()
+            one = osscar.AdamW([alone], [grads[k]], bits=bits, masters=[None if masters[k] is None else masters[k].clone()])
+            one.osscar_adamw(LR, 5, B1, B2, EPS, WD)
+            assert torch.equal(alone, together[k]) and all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(one.states[0], plan.states[k]) if a is not None)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_adamw_views_of_any_alignment_and_layout(osscar, bits):
+    g = _gen(10)
+    for shift in (1, 3, 8):
+        for n in (5, 300, 4099):
+            store = [torch.full((n + 32,), 3.0, device=DEV) for _ in range(2)] + [torch.full((n + 32,), 3.0, device=DEV, dtype=BF16) for _ in range(2)]
+            views = [s[shift:shift + n] for s in store]
+            for v in views:
+                v.copy_(_randn(g, n))
+            clean = [v.clone() for v in views]
+            states = [osscar.AdamW([v], bits=bits).states[0] for v in (views[0], views[2])]
+            shifted, raws = [], []
+            for s in states:
+                parts = []
+                for t in s[:2]:
+                    raw = torch.full((n + 32,), 77, dtype=torch.uint8 if bits == 8 else F32, device=DEV)
+                    raws.append(raw)
+                    parts.append(raw[shift:shift + n].view(t.dtype))
+                    parts[-1].copy_(t)
+                shifted.append(osscar.AdamWState(*parts, *s[2:]))
+            osscar.AdamW([views[0], views[2]], [views[1], views[3]], states=shifted, bits=bits).osscar_adamw(LR, 1)
+            ref = osscar.AdamW([clean[0], clean[2]], [clean[1], clean[3]], bits=bits)
+            ref.osscar_adamw(LR, 1)
+            for v, c, s in zip(views, clean, store):
+                assert torch.equal(v, c) and (s[:shift] == 3).all() and (s[shift + n:] == 3).all()
+            for a, b in zip(shifted, ref.states):
+                assert all(torch.equal(x.contiguous().view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a[:2], b[:2]))
+            assert all((raw[:shift] == 77).all() and (raw[shift + n:] == 77).all() for raw in raws)
+    # a transposed matrix, as the gated layer's weights may be; its gradient lies alike
+    W = _randn(g, 40, 70).t()
+    G = _randn(g, 40, 70).t()
+    flat, gflat = W.t().contiguous().clone(), G.t().contiguous().clone()
+    osscar.AdamW([W], [G], bits=bits).osscar_adamw(LR, 1)
+    osscar.AdamW([flat], [gflat], bits=bits).osscar_adamw(LR, 1)
+    assert torch.equal(W.t(), flat)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_adamw_captured_with_rate_and_step_on_the_device(osscar, bits):
+    g = _gen(11)
+    shapes = [(300,), (64, 65), (5000,)]
+    params, grads = _tensors(g, shapes, F32, F32)
+    host = osscar.AdamW([p.clone() for p in params], [x.clone() for x in grads], bits=bits)
+    plan = osscar.AdamW(params, grads, bits=bits)
+    lr, step, scale = torch.tensor(1e-3, device=DEV), torch.zeros(1, dtype=torch.int64, device=DEV), torch.tensor([0.5], device=DEV)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step.add_(1)
+        plan.osscar_adamw(lr, step, grad_scale=scale)
+    for t in range(1, 5):
+        lr.fill_(1e-3 / t)
+        scale.fill_(0.5 * t)
+        graph.replay()
+        torch.cuda.synchronize()
+        host.osscar_adamw(float(np.float32(1e-3 / t)), t, grad_scale=scale)
+        for a, b in zip(params, host.params):
+            assert torch.equal(a, b), t
+        for a, b in zip(plan.states, host.states):
+            assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a, b) if x is not None)
+        for x, y in zip(grads, host.grads):
+            x.normal_(generator=g)
+            y.copy_(x)
+    # a scale that is not finite: nothing changes
+    for bad in (math.nan, math.inf, -math.inf):
+        before = [p.clone() for p in params] + [x.view(torch.uint8).clone() for s in plan.states for x in s if x is not None]
+        plan.osscar_adamw(1e-3, 5, grad_scale=torch.tensor(bad, device=DEV))
+        after = params + [x.view(torch.uint8) for s in plan.states for x in s if x is not None]
+        assert all(torch.equal(x, y) for x, y in zip(before, after))
+    # late steps: the powers of beta are nothing
+    for t in (10 ** 6, 2 ** 40):
+        host.osscar_adamw(1e-3, t)
+        plan.osscar_adamw(torch.tensor(1e-3, device=DEV), torch.tensor(t, device=DEV))
+
+
+def test_adamw_gradients_that_are_not_finite(osscar):
+    for bits in (8, 32):
+        p, gr = torch.ones(700, device=DEV), torch.ones(700, device=DEV)
+        gr[300], gr[301], gr[5] = math.nan, math.inf, 1e30      # (the last one's square is none of float32)
+        plan = osscar.AdamW([p], [gr], bits=bits)
+        plan.osscar_adamw(1e-2, 1)
+        assert torch.isnan(p).nonzero().flatten().tolist() == [300, 301]
+        s = plan.states[0]
+        if bits == 8:
+            assert torch.isnan(s.m_scale).tolist() == [False, True, False] and torch.isnan(s.v_scale).tolist() == [True, True, False]
+            assert torch.isfinite(plan.osscar_adamw_values()[0].m[:256]).all() and torch.isnan(plan.osscar_adamw_values()[0].root[:512]).all()
+        gr.fill_(1.0)
+        plan.osscar_adamw(1e-2, 2)
+        left = torch.isfinite(p)
+        assert left[512:].all() and (left[:256].any().item() if bits == 32 else not left[:512].any().item())
+
+
+def test_adamw_zero_gradients_and_blocks(osscar):
+    p = _randn(_gen(1), 1000)
+    plan = osscar.AdamW([p], [torch.zeros(1000, device=DEV)], bits=8)
+    want = p * np.float32(1 - 1e-2 * 0.1)
+    plan.osscar_adamw(1e-2, 1, weight_decay=0.1)
+    assert torch.equal(p, want) and not plan.states[0].m.view(torch.uint8).any() and not plan.states[0].v.any()
+    # numbers at the low end of float32: scales stay normal numbers
+    gr = torch.full((1000,), 1e-36, device=DEV)
+    plan.osscar_adamw(1e-2, 2, grads=[gr])
+    assert (plan.states[0].m_scale == 2.0 ** -126).all() and torch.isfinite(p).all()
+
+
+def test_adamw_on_another_stream(osscar):
+    g = _gen(2)
+    p, gr = _randn(g, 100000), _randn(g, 100000)
+    q = p.clone()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    a, b = osscar.AdamW([p], [gr], bits=8), osscar.AdamW([q], [gr], bits=8)
+    torch.cuda.synchronize()
+    a.osscar_adamw(LR, 1, stream=side)
+    va = a.osscar_adamw_values(stream=side)
+    side.synchronize()
+    b.osscar_adamw(LR, 1)
+    vb = b.osscar_adamw_values()
+    assert torch.equal(p, q) and torch.equal(va[0].m, vb[0].m) and torch.equal(va[0].root, vb[0].root)
+
+
+def test_adamw_refusals(osscar):
+    p, gr = torch.zeros(8, 16, device=DEV), torch.zeros(8, 16, device=DEV)
+    A = osscar.AdamW
+    s32, s8 = A([p]).states, A([p], bits=8).states
+    assert A([p], states=s8).bits == 8
+    plan = A([p], [gr])
+    bad = [lambda: A([]), lambda: A([p.half()]), lambda: A([p[:, :8]]), lambda: A([p.cpu()]), lambda: A([p], [gr, gr]), lambda: A([p], [gr.t()]), lambda: A([p], [gr[:4]]),
+           lambda: A([p], [gr.half()]), lambda: A([p], [gr.cpu()]), lambda: A([p, p]), lambda: A([p, p.view(-1)]), lambda: A([p], masters=[p.clone()]),
+           lambda: A([p.bfloat16()], masters=[p.bfloat16()]), lambda: A([p.bfloat16()], masters=[p[:4].clone()]), lambda: A([p], masters=[]), lambda: A([p], bits=16),
+           lambda: A([p], states=s32 + s32), lambda: A([p], states=s8, bits=32), lambda: A([p], states=s32, bits=8), lambda: A([p], states=[(s32[0].m[:5], s32[0].v)]),
+           lambda: A([p], states=[(s32[0].m, s32[0].m)]), lambda: A([p], states=[(s8[0].m, s8[0].v, s8[0].m_scale, s8[0].v_scale[:0])]), lambda: A([p]).osscar_adamw(LR, 1),
+           lambda: plan.osscar_adamw(LR, 0), lambda: plan.osscar_adamw(-1.0, 1), lambda: plan.osscar_adamw(math.nan, 1), lambda: plan.osscar_adamw(LR, 1, beta1=1.0),
+           lambda: plan.osscar_adamw(LR, 1, beta2=-0.1), lambda: plan.osscar_adamw(LR, 1, beta2=math.nan), lambda: plan.osscar_adamw(LR, 1, eps=0.0), lambda: plan.osscar_adamw(LR, 1, eps=math.inf),
+           lambda: plan.osscar_adamw(LR, 1, weight_decay=-1.0), lambda: plan.osscar_adamw(LR, 1, seed=-1), lambda: plan.osscar_adamw(LR, 1, seed=1 << 32),
+           lambda: plan.osscar_adamw(torch.tensor(LR), 1), lambda: plan.osscar_adamw(torch.tensor(LR, device=DEV, dtype=torch.double), 1),
+           lambda: plan.osscar_adamw(LR, torch.tensor(1, device=DEV, dtype=torch.int32)), lambda: plan.osscar_adamw(LR, 1, grad_scale=torch.ones(2, device=DEV)),
+           lambda: plan.osscar_adamw_values()]
+    for k, call in enumerate(bad):
+        with pytest.raises(osscar.OsscarError) as e:
+            call()
+        assert e.value.status == 1, k
+    assert not p.any()      # nothing was written
