@@ -416,6 +416,39 @@ osscar_status osscar_layernorm_backward(const void* X_dev, int64_t n, int64_t d,
                                         const float* stats_dev, void* dX_dev, int64_t lddx, void* dw_dev, void* db_dev, int32_t dw_dtype, void* workspace_dev,
                                         size_t workspace_bytes, void* hip_stream);
 
+/* Low-rank adapters of many requests beside a shared projection (one that osscar_int_product serves, or any other), each row with its own:
+ *   T_i = A_e x_i,  y_i = base_i + s_e B_e^T T_i,   e = index_i,   X n x d, Y and base n x m, T n x rank.
+ * A is count x rank x d and B count x rank x m in memory: a component's numbers side by side in both (B of a layer m x rank is stored transposed, once).  index: n int64; a row with a
+ * negative one has no adapter (y = base), one with `count` or more is NaN.  Without an index every row has the first adapter.  scale: count float32 (NULL: 1).  ranks: count int32 (NULL: all of
+ * `rank`), the components of each adapter that count, from the first on; the others are not read.  base may be NULL (zeros) or Y itself.  Products of bf16 are summed in float32, T is float32 and goes
+ * into the second product as two bf16 pieces (16 bits; an infinity there makes its row NaN), y is rounded once.  Rows of one adapter next to each other are fastest: 32 neighbouring rows
+ * are read once for each adapter that they have. */
+#define OSSCAR_ADAPTERS_MAX 4096
+#define OSSCAR_ADAPTER_MAX_RANK 1024
+typedef struct {
+  int64_t n, d, m;            /* rows (n = 0: nothing to do; at most 2^22), inputs, outputs */
+  int64_t ldx;                /* leading dimension of X */
+  int64_t lda, next_a;        /* elements from one component of A to the next, from one adapter to the next */
+  int64_t ldb, next_b;        /* the same of B */
+  int32_t count, rank;        /* at most OSSCAR_ADAPTERS_MAX, OSSCAR_ADAPTER_MAX_RANK */
+  int32_t dtype;              /* of X, A, B, base, Y, dY, dX */
+  int32_t index;              /* nonzero: the calls are given an index */
+} osscar_adapters_desc;
+/* Workspace of a forward call (backward = 0) or of a backward call (1); 0 if the description is invalid. */
+size_t osscar_adapters_workspace_bytes(const osscar_adapters_desc* desc, int32_t backward);
+/* T_dev: dense n x rank float32 output for osscar_adapters_backward (zeros where there is no adapter or component), or NULL. */
+osscar_status osscar_adapters_forward(const osscar_adapters_desc* desc, const void* X_dev, const void* A_dev, const void* B_dev, const int64_t* index_dev,
+                                      const float* scale_dev, const int32_t* ranks_dev, const void* base_dev, int64_t ldbase, void* Y_dev, int64_t ldy, float* T_dev,
+                                      void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+/* Gradients, given dY (n x m, leading dimension lddy):  dT_i = s_e B_e dY_i,  dX_i = base_i + A_e^T dT_i,  dA_e = sum of dT_i x_i^T and dB_e = s_e sum of T_i dY_i^T over the rows of
+ * e.  T_dev: what forward left there, or NULL: computed again.  base_dev: n x d, leading dimension ldbase, NULL (zeros) or dX itself (the gradient that came through the
+ * shared projection).  dX_dev may be NULL, dA_dev and dB_dev too (both or neither): dense, of the shapes of A and B, dw_dtype, written, not added to, zeros for adapters and components without
+ * rows, in an order that does not change from call to call.  A row whose index is `count` or more has dX of NaN and no part in dA and dB. */
+osscar_status osscar_adapters_backward(const osscar_adapters_desc* desc, const void* X_dev, const void* A_dev, const void* B_dev, const int64_t* index_dev,
+                                       const float* scale_dev, const int32_t* ranks_dev, const void* dY_dev, int64_t lddy, const float* T_dev, const void* base_dev, int64_t ldbase,
+                                       void* dX_dev, int64_t lddx, void* dA_dev, void* dB_dev, int32_t dw_dtype, void* workspace_dev, size_t workspace_bytes,
+                                       void* hip_stream);
+
 /* AdamW, one step over many tensors: with t = step counted from 1, and float32 factors rounded once from float64, every operation below rounded by itself,
  *   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) (g g),  p = p (1 - lr weight_decay) - lr / (1 - b1^t) (m / (sqrt v / sqrt(1 - b2^t) + eps)).
  * A tensor is n contiguous elements of any shape (n = 0: nothing to do).  p: float32, or bf16, rounded to the nearest, with a float32 copy `master` that holds the

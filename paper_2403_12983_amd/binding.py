@@ -32,6 +32,7 @@ EXPORTED_SYMBOLS = ["osscar_workspace_bytes", "osscar_create", "osscar_destroy",
                     "osscar_int_weights", "osscar_int_rows", "osscar_int_workspace_bytes", "osscar_int_product",
                     "osscar_logprobs_workspace_bytes", "osscar_logprobs", "osscar_logprobs_backward",
                     "osscar_layernorm_forward", "osscar_layernorm_workspace_bytes", "osscar_layernorm_backward",
+                    "osscar_adapters_workspace_bytes", "osscar_adapters_forward", "osscar_adapters_backward",
                     "osscar_adamw", "osscar_adamw_values"]
 
 
@@ -50,6 +51,11 @@ class _Desc(C.Structure):
 class _GatedDesc(C.Structure):
     _fields_ = [("n", C.c_int64), ("d", C.c_int64), ("f", C.c_int64), ("ldx", C.c_int64), ("ldw", C.c_int64), ("ldh", C.c_int64),
                 ("dtype", C.c_int32), ("act", C.c_int32), ("rows_out", C.c_int32), ("unaligned", C.c_int32)]
+
+
+class _AdaptersDesc(C.Structure):
+    _fields_ = [("n", C.c_int64), ("d", C.c_int64), ("m", C.c_int64), ("ldx", C.c_int64), ("lda", C.c_int64), ("next_a", C.c_int64), ("ldb", C.c_int64),
+                ("next_b", C.c_int64), ("count", C.c_int32), ("rank", C.c_int32), ("dtype", C.c_int32), ("index", C.c_int32)]
 
 
 class _AdamWTensor(C.Structure):
@@ -113,7 +119,8 @@ def load_library():
     lib.osscar_gram_static.argtypes = [vp, i64, i64, i32, vp, i64, i32, i64, i64, dbl, dbl, vp, vp, vp, vp]
     lib.osscar_debug_tile_schedule.restype = C.c_int32
     lib.osscar_debug_tile_schedule.argtypes = [i64, C.POINTER(i32), i32]
-    for name in ("osscar_gated_workspace_bytes", "osscar_int_workspace_bytes", "osscar_logprobs_workspace_bytes", "osscar_layernorm_workspace_bytes"):
+    for name in ("osscar_gated_workspace_bytes", "osscar_int_workspace_bytes", "osscar_logprobs_workspace_bytes", "osscar_layernorm_workspace_bytes",
+                 "osscar_adapters_workspace_bytes"):
         getattr(lib, name).restype = C.c_size_t
     gd, f32 = C.POINTER(_GatedDesc), C.c_float
     lib.osscar_gated_workspace_bytes.argtypes = [gd, i32]
@@ -129,6 +136,10 @@ def load_library():
     lib.osscar_layernorm_workspace_bytes.argtypes = [i64, i64]
     lib.osscar_layernorm_forward.argtypes = [vp, i64, i64, i64, i32, vp, vp, i32, f32, vp, i64, vp, vp]
     lib.osscar_layernorm_backward.argtypes = [vp, i64, i64, i64, i32, vp, i32, vp, i64, vp, vp, i64, vp, vp, i32, vp, C.c_size_t, vp]
+    ad = C.POINTER(_AdaptersDesc)
+    lib.osscar_adapters_workspace_bytes.argtypes = [ad, i32]
+    lib.osscar_adapters_forward.argtypes = [ad, vp, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, C.c_size_t, vp]
+    lib.osscar_adapters_backward.argtypes = [ad, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp, i64, vp, i64, vp, vp, i32, vp, C.c_size_t, vp]
     lib.osscar_adamw.argtypes = [C.POINTER(_AdamWTensor), i64, C.POINTER(_AdamWDesc), vp]
     lib.osscar_adamw_values.argtypes = [C.POINTER(_AdamWTensor), i64, C.POINTER(vp), C.POINTER(vp), vp]
     lib.osscar_last_error.restype = C.c_char_p

@@ -1,0 +1,780 @@
+// Low-rank adapters of many requests beside a shared projection: y_i = base_i + s_e B_e^T (A_e x_i) with e the adapter of row i, and the gradients.
+// A (count x rank x d) and B (count x rank x m) both hold a component's numbers side by side, so that three kernels do it all:
+//   contract  T[i][j] = sum_k Z[i][k] V_e[j][k]        (T from X and A; dT from dY and B)
+//   expand    Y[i][c] = base[i][c] + sum_j T[i][j] V_e[j][c]      (y from T and B; dX from dT and A)
+//   outer     dV_e[j][c] = sum over the rows i of e of T[i][j] Z[i][c]      (dA from dT and X; dB from T and dY)
+// Rows go through in tiles as they lie; a tile is taken once for each adapter in it (one or two where the rows of a request lie together), each time with the
+// results of that adapter's rows kept.  All are bound by reading and writing Z, base and Y, or A and B where rows are few: 2 rank operations for each of their elements.
+#include "ops.h"
+#include <algorithm>
+
+using namespace osscar;
+
+namespace {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+
+// Which adapter each row has, and what it says of itself.  index NULL: every row has the first.
+struct Pick {
+  const int64_t* index;
+  const float* scale;
+  const int32_t* ranks;
+  int count, rank;
+  __device__ __forceinline__ int of(int64_t row) const {      // -1: none; -2: there is no such adapter
+    if (!index) return 0;
+    const int64_t e = index[row];
+    return e < 0 ? -1 : e < count ? (int)e : -2;
+  }
+  __device__ __forceinline__ float scale_of(int e) const { return scale ? scale[e] : 1.f; }
+  __device__ __forceinline__ int rank_of(int e) const { return ranks ? min(max(ranks[e], 0), rank) : rank; }
+};
+// f(e, which rows of the tile) for each adapter that some of the lanes' rows have, every `slots`-th of them.
+template <class F>
+__device__ __forceinline__ void each_adapter(int mine, int slot, int slots, F f) {
+  uint64_t left = __ballot(mine >= 0);
+  for (int k = 0; left; k++) {
+    const int e = __builtin_amdgcn_readlane(mine, __ffsll((unsigned long long)left) - 1);
+    const uint64_t rows = __ballot(mine == e);
+    left &= ~rows;
+    if (k % slots == slot) f(e, rows);
+  }
+}
+
+struct Mat { const void* p; int64_t ld; };                  // rows of elements
+struct Adapters { const void* p; int64_t ld, next; };       // of one component, of one adapter
+
+// 16 bytes of a row and the matrix instruction that contracts them: lane (i, g) = (lane % 16, lane / 16) holds elements g E .. g E + E - 1 of row i.
+template <bool F32> struct Num;
+template <> struct Num<false> {
+  static constexpr int E = 8, STEP = 32, ES = 2;
+  static __device__ __forceinline__ v4f mma(u32x4 a, u32x4 b, v4f c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+  }
+};
+template <> struct Num<true> {
+  static constexpr int E = 4, STEP = 16, ES = 4;
+  static __device__ __forceinline__ v4f mma(u32x4 a, u32x4 b, v4f c) {
+#pragma unroll
+    for (int e = 0; e < 4; e++) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
+    return c;
+  }
+};
+template <bool F32>
+__device__ __forceinline__ u32x4 packet(const char* row, int k) { return *reinterpret_cast<const u32x4_any*>(row + (int64_t)k * Num<F32>::ES); }
+template <bool F32>
+__device__ __forceinline__ u32x4 packet_some(const char* row, int k, int K) {      // zeros from K on
+  if constexpr (F32) {
+    const uint32_t* p = reinterpret_cast<const uint32_t*>(row) + k;
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 4; e++) { w[e] = 0; if (k + e < K) w[e] = p[e]; }
+    return w;
+  } else {
+    const uint16_t* p = reinterpret_cast<const uint16_t*>(row) + k;
+    u16x8 w;
+#pragma unroll
+    for (int e = 0; e < 8; e++) { w[e] = 0; if (k + e < K) w[e] = p[e]; }
+    return __builtin_bit_cast(u32x4, w);
+  }
+}
+
+// --------------------------------------------------------------------------------------------------
+// contract
+// --------------------------------------------------------------------------------------------------
+// A workgroup takes 16 RT rows and 16 CT components; its waves take the contraction in turns, parts of it are a workgroup's each (their sums are added where T is
+// read).  Operands go from memory to registers; the next turn's are on their way while one is multiplied.
+struct Contract {
+  Mat z;
+  Adapters v;
+  int64_t n;
+  int K, parts, slots, scaled;      // scaled: times the adapter's scale
+  float* t;                         // [part][n][rank]
+};
+constexpr int CW = 8;      // waves
+template <bool F32, int RT, int CT>
+__global__ __launch_bounds__(CW * 64) void contract_kernel(Contract q, Pick pick) {
+  typedef Num<F32> N;
+  constexpr int U = F32 ? 2 : RT * CT >= 4 ? 2 : 4, TURN = U * N::STEP, ROWS = RT * 16, COLS = CT * 16;
+  __shared__ float sums[CW / 2][ROWS * (COLS + 1)];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
+  const int64_t tiles = (q.n + ROWS - 1) / ROWS, row0 = (blockIdx.x % tiles) * ROWS;
+  const int slot = (int)(blockIdx.x / tiles), part = blockIdx.y, j0 = blockIdx.z * COLS;
+  const int have = (int)std::min<int64_t>(ROWS, q.n - row0);
+  const int mine = lane < have ? pick.of(row0 + lane) : -1;
+  float* t = q.t + (int64_t)part * q.n * pick.rank;
+  if (slot == 0) {      // rows without an adapter
+    const uint64_t none = __ballot(mine < 0);
+    for (int k = threadIdx.x; k < have * COLS; k += CW * 64) {
+      const int r = k / COLS, j = j0 + k % COLS;
+      if ((none >> r & 1) && j < pick.rank) t[(row0 + r) * pick.rank + j] = 0.f;
+    }
+  }
+  each_adapter(mine, slot, q.slots, [&](int e, uint64_t rows) {
+    const int rank = pick.rank_of(e), first = __ffsll((unsigned long long)rows) - 1;
+    const char *zr[RT], *vr[CT];
+#pragma unroll
+    for (int r = 0; r < RT; r++) {      // (rows of other adapters: one of this one's again, not used)
+      const int at = rows >> (r * 16 + i) & 1 ? r * 16 + i : first;
+      zr[r] = reinterpret_cast<const char*>(q.z.p) + (row0 + at) * q.z.ld * N::ES;
+    }
+#pragma unroll
+    for (int c = 0; c < CT; c++) vr[c] = reinterpret_cast<const char*>(q.v.p) + (e * q.v.next + (int64_t)std::max(0, std::min(j0 + c * 16 + i, rank - 1)) * q.v.ld) * N::ES;
+    struct Regs { u32x4 z[RT][U], v[CT][U]; };
+    auto load = [&](int k0, Regs& w) {
+      if (k0 + TURN <= q.K) {
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+          const int k = k0 + u * N::STEP + g * N::E;
+#pragma unroll
+          for (int r = 0; r < RT; r++) w.z[r][u] = packet<F32>(zr[r], k);
+#pragma unroll
+          for (int c = 0; c < CT; c++) w.v[c][u] = packet<F32>(vr[c], k);
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+          const int k = k0 + u * N::STEP + g * N::E;
+#pragma unroll
+          for (int r = 0; r < RT; r++) w.z[r][u] = packet_some<F32>(zr[r], k, q.K);
+#pragma unroll
+          for (int c = 0; c < CT; c++) w.v[c][u] = packet_some<F32>(vr[c], k, q.K);
+        }
+      }
+    };
+    v4f acc[RT][CT];
+#pragma unroll
+    for (int r = 0; r < RT; r++)
+#pragma unroll
+      for (int c = 0; c < CT; c++) acc[r][c] = v4f{0, 0, 0, 0};
+    auto multiply = [&](const Regs& w) {
+#pragma unroll
+      for (int u = 0; u < U; u++)
+#pragma unroll
+        for (int r = 0; r < RT; r++)
+#pragma unroll
+          for (int c = 0; c < CT; c++) acc[r][c] = N::mma(w.z[r][u], w.v[c][u], acc[r][c]);
+    };
+    const int turns = (q.K + TURN - 1) / TURN, per = (turns + q.parts - 1) / q.parts;
+    const int begin = part * per + wave, end = std::min(turns, (part + 1) * per);
+    if (j0 < rank && begin < end) {
+      Regs x[2];
+      load(begin * TURN, x[0]);
+      for (int k = begin; k < end; k += 2 * CW) {
+        if (k + CW < end) load((k + CW) * TURN, x[1]);
+        multiply(x[0]);
+        if (k + CW >= end) break;
+        if (k + 2 * CW < end) load((k + 2 * CW) * TURN, x[0]);
+        multiply(x[1]);
+      }
+    }
+    // the waves' sums, added in a fixed order
+    auto each = [&](auto f) {
+#pragma unroll
+      for (int r = 0; r < RT; r++)
+#pragma unroll
+        for (int c = 0; c < CT; c++)
+#pragma unroll
+          for (int d = 0; d < 4; d++) acc[r][c][d] = f((r * 16 + g * 4 + d) * (COLS + 1) + c * 16 + i, acc[r][c][d]);
+    };
+#pragma unroll
+    for (int half = CW / 2; half > 0; half /= 2) {
+      __syncthreads();
+      if (wave >= half && wave < 2 * half) each([&](int at, float s) { return sums[wave - half][at] = s; });
+      __syncthreads();
+      if (wave < half) each([&](int at, float s) { return s + sums[wave][at]; });
+    }
+    if (wave == 0) {
+      const float s = q.scaled ? pick.scale_of(e) : 1.f;
+#pragma unroll
+      for (int r = 0; r < RT; r++)
+#pragma unroll
+        for (int d = 0; d < 4; d++) {
+          const int row = r * 16 + g * 4 + d;
+          if (rows >> row & 1) {
+#pragma unroll
+            for (int c = 0; c < CT; c++) {
+              const int j = j0 + c * 16 + i;
+              if (j < pick.rank) t[(row0 + row) * pick.rank + j] = j < rank ? acc[r][c][d] * s : 0.f;
+            }
+          }
+        }
+    }
+  });
+}
+
+// --------------------------------------------------------------------------------------------------
+// expand
+// --------------------------------------------------------------------------------------------------
+// float32 factors of a bf16 product go in as two pieces of bf16 each (16 bits: what is left out is 2^-16 of a term at most, the rounding of a bf16 result 2^-8 of its), or three (24 bits).
+template <int PIECES>
+__device__ __forceinline__ void pieces(const float (&x)[8], u32x4 (&p)[PIECES]) {
+  float left[8];
+#pragma unroll
+  for (int e = 0; e < 8; e++) left[e] = x[e];
+#pragma unroll
+  for (int k = 0; k < PIECES; k++) {
+    v8bf w;
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      w[e] = (__bf16)left[e];
+      left[e] -= (float)w[e];
+    }
+    p[k] = __builtin_bit_cast(u32x4, w);
+  }
+}
+// Eight rows of eight bf16 columns, turned: operand t holds column t of all eight.
+__device__ __forceinline__ void turned(const u16x8 (&w)[8], u32x4 (&p)[8]) {
+#pragma unroll
+  for (int t = 0; t < 8; t++) {
+    u16x8 c;
+#pragma unroll
+    for (int e = 0; e < 8; e++) c[e] = w[e][t];
+    p[t] = __builtin_bit_cast(u32x4, c);
+  }
+}
+
+struct Expand {
+  const float* t;      // [part][n][rank]
+  int parts, slots, scaled;
+  Adapters v;
+  Mat base;            // (p may be NULL, or y)
+  int64_t n;
+  int C;
+  void* y;
+  int64_t ldy;
+  float* t_out;        // the parts' sum, or NULL
+};
+constexpr int EW = 4, ECOLS = 128;      // waves, columns of each
+// A wave takes 16 RT rows and 128 columns: lane (i, g) reads eight columns c0 + 8 i .. of eight components 8 g .. and turns them in its registers, so that the instruction for tile t
+// has columns c0 + 8 i + t; the results of a lane are then eight neighbouring columns of four rows.
+template <bool F32, int RT>
+__global__ __launch_bounds__(EW * 64) void expand_kernel(Expand q, Pick pick) {
+  typedef Eight<F32> E8;
+  constexpr int ROWS = RT * 16, STEP = F32 ? 16 : 32, E = F32 ? 4 : 8;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
+  const int blocks = (q.C + EW * ECOLS - 1) / (EW * ECOLS);
+  const int64_t row0 = (int64_t)(blockIdx.x / blocks) * ROWS;
+  const int c0 = (blockIdx.x % blocks) * (EW * ECOLS) + wave * ECOLS, slot = blockIdx.y, c = c0 + i * 8;
+  if (c0 >= q.C && !(q.t_out && c0 == 0)) return;
+  const int have = (int)std::min<int64_t>(ROWS, q.n - row0), most = q.C - c;
+  const int mine = lane < have ? pick.of(row0 + lane) : -1;
+  const bool whole = c0 + ECOLS <= q.C;
+  const size_t es = F32 ? 4 : 2;
+  if (slot == 0) {      // rows without an adapter
+    uint64_t none = __ballot(mine < 0 && lane < have), wrong = __ballot(mine == -2);
+    if (q.t_out && c0 == 0)
+      for (int k = lane; k < have * pick.rank; k += 64)
+        if (none >> (k / pick.rank) & 1) q.t_out[row0 * pick.rank + k] = 0.f;
+    if (q.y == q.base.p) none = wrong;
+    while (none) {
+      const int r = __ffsll((unsigned long long)none) - 1;
+      none &= none - 1;
+      if (g == 0 && most > 0) {
+        float y[8];
+        if (q.base.p) E8::values(E8::load(q.base.p, (row0 + r) * q.base.ld + c, most), y);
+#pragma unroll
+        for (int t = 0; t < 8; t++) y[t] = wrong >> r & 1 ? NAN : q.base.p ? y[t] : 0.f;
+        E8::store(q.y, (row0 + r) * q.ldy + c, y, most);
+      }
+    }
+  }
+  each_adapter(mine, slot, q.slots, [&](int e, uint64_t rows) {
+    const int rank = pick.rank_of(e);
+    const float s = q.scaled ? pick.scale_of(e) : 1.f;
+    const char* v = reinterpret_cast<const char*>(q.v.p) + e * q.v.next * es;
+    typename E8::type base[RT][4];
+    if (q.base.p) {
+#pragma unroll
+      for (int r = 0; r < RT; r++)
+#pragma unroll
+        for (int d = 0; d < 4; d++) {
+          const int row = r * 16 + g * 4 + d;
+          if (rows >> row & 1) base[r][d] = whole ? E8::load(q.base.p, (row0 + row) * q.base.ld + c) : E8::load(q.base.p, (row0 + row) * q.base.ld + c, most);
+        }
+    }
+    v4f acc[RT][8];
+#pragma unroll
+    for (int r = 0; r < RT; r++)
+#pragma unroll
+      for (int t = 0; t < 8; t++) acc[r][t] = v4f{0, 0, 0, 0};
+    for (int j0 = 0; j0 < rank; j0 += STEP) {
+      const int j = j0 + g * E;
+      // this lane's components of V and of T
+      typename E8::type w[E];
+#pragma unroll
+      for (int k = 0; k < E; k++) {
+        const int64_t at = (int64_t)std::min(j + k, rank - 1) * q.v.ld + c;
+        w[k] = whole ? E8::load(v, at) : E8::load(v, at, most);
+        if (j + k >= rank) w[k] = E8::load(v, 0, 0);      // (zeros)
+      }
+      float x[RT][E];
+#pragma unroll
+      for (int r = 0; r < RT; r++) {
+        const int at = rows >> (r * 16 + i) & 1 ? r * 16 + i : -1;
+#pragma unroll
+        for (int k = 0; k < E; k++) x[r][k] = 0.f;
+        if (at >= 0) {
+          for (int p = 0; p < q.parts; p++) {
+            const float* t = q.t + ((int64_t)p * q.n + row0 + at) * pick.rank + j;
+#pragma unroll
+            for (int k = 0; k < E; k++)
+              if (j + k < rank) x[r][k] += t[k];
+          }
+          if (q.t_out && c0 == 0) {
+#pragma unroll
+            for (int k = 0; k < E; k++)
+              if (j + k < rank) q.t_out[(row0 + at) * pick.rank + j + k] = x[r][k];
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < E; k++) x[r][k] *= s;
+      }
+      if constexpr (F32) {
+#pragma unroll
+        for (int k = 0; k < E; k++) {
+          float col[8];
+          E8::values(w[k], col);
+#pragma unroll
+          for (int r = 0; r < RT; r++)
+#pragma unroll
+            for (int t = 0; t < 8; t++) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[r][k], col[t], acc[r][t], 0, 0, 0);
+        }
+      } else {
+        u32x4 cols[8];
+        turned(w, cols);
+#pragma unroll
+        for (int r = 0; r < RT; r++) {
+          u32x4 p[2];
+          pieces<2>(x[r], p);
+#pragma unroll
+          for (int t = 0; t < 8; t++) acc[r][t] = Num<false>::mma(p[1], cols[t], Num<false>::mma(p[0], cols[t], acc[r][t]));
+        }
+      }
+    }
+    if (q.t_out && c0 == 0) {      // components past the adapter's rank
+      for (int r = 0; r < have; r++)
+        if (rows >> r & 1)
+          for (int j = rank + lane; j < pick.rank; j += 64) q.t_out[(row0 + r) * pick.rank + j] = 0.f;
+    }
+#pragma unroll
+    for (int r = 0; r < RT; r++)
+#pragma unroll
+      for (int d = 0; d < 4; d++) {
+        const int row = r * 16 + g * 4 + d;
+        if (rows >> row & 1) {
+          float y[8];
+          if (q.base.p) E8::values(base[r][d], y);
+#pragma unroll
+          for (int t = 0; t < 8; t++) y[t] = q.base.p ? y[t] + acc[r][t][d] : acc[r][t][d];
+          if (whole) E8::store(q.y, (row0 + row) * q.ldy + c, y);
+          else E8::store(q.y, (row0 + row) * q.ldy + c, y, most);
+        }
+      }
+  });
+}
+
+// --------------------------------------------------------------------------------------------------
+// outer
+// --------------------------------------------------------------------------------------------------
+// The rows in the order of their adapters, and pieces of at most CHUNK rows of one adapter.
+constexpr int CHUNK = 512;
+struct Chunk { int e, begin, end, number; };      // number: of its adapter's
+struct Plan {
+  const int* order;            // (NULL: as they lie)
+  const Chunk* chunks;
+  const int* first;            // count + 1: an adapter's first chunk
+  int64_t n;
+  int total;                   // order NULL: how many
+  __device__ __forceinline__ Chunk at(int c) const {
+    if (!order) return Chunk{0, (int)((int64_t)c * CHUNK), (int)std::min<int64_t>(n, ((int64_t)c + 1) * CHUNK), c};
+    return chunks[c];
+  }
+  __device__ __forceinline__ int chunks_of(int e) const { return order ? first[e + 1] - first[e] : e == 0 ? total : 0; }
+  __device__ __forceinline__ int first_of(int e) const { return order ? first[e] : 0; }
+  __device__ __forceinline__ int all(int count) const { return order ? first[count] : total; }
+};
+// One workgroup; waves take the rows in spans, in order, so that an adapter's rows keep theirs.  Each wave counts its span by adapter; after sums over waves
+// and adapters it goes over the span again, 64 rows at a time, and gives rows of one adapter their places together.
+constexpr int PLAN_WORDS = 32768;      // of LDS: counts by wave and adapter
+static_assert(OSSCAR_ADAPTERS_MAX * 2 <= PLAN_WORDS, "");
+__global__ __launch_bounds__(1024) void plan_kernel(Pick pick, int n, int waves, int* order, Chunk* chunks, int* first) {
+  __shared__ uint32_t counts[PLAN_WORDS];
+  __shared__ uint32_t wave_rows[16], wave_chunks[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, count = pick.count;
+  for (int k = threadIdx.x; k < waves * count; k += 1024) counts[k] = 0;
+  __syncthreads();
+  const int span = ((n + waves - 1) / waves + 63) / 64 * 64;
+  const int64_t begin = (int64_t)wave * span, end = std::min<int64_t>(n, begin + span);
+  if (wave < waves)
+    for (int64_t r = begin + lane; r < end; r += 64) {
+      const int e = pick.of(r);
+      if (e >= 0) atomicAdd(&counts[wave * count + e], 1u);      // (whole numbers: any order)
+    }
+  __syncthreads();
+  // places of adapters, `each` of them a thread: rows before, chunks before
+  const int each = (count + 1023) / 1024;
+  uint32_t rows = 0, parts = 0;
+  for (int k = 0; k < each; k++) {
+    const int e = threadIdx.x * each + k;
+    if (e >= count) break;
+    uint32_t s = 0;
+    for (int w = 0; w < waves; w++) s += counts[w * count + e];
+    rows += s;
+    parts += (s + CHUNK - 1) / CHUNK;
+  }
+  uint32_t rows_to = rows, parts_to = parts;      // sums up to this thread, itself included
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t a = __shfl_up(rows_to, o, 64), b = __shfl_up(parts_to, o, 64);
+    if (lane >= o) { rows_to += a; parts_to += b; }
+  }
+  if (lane == 63) { wave_rows[wave] = rows_to; wave_chunks[wave] = parts_to; }
+  __syncthreads();
+  uint32_t at = rows_to - rows, chunk = parts_to - parts;
+  for (int w = 0; w < wave; w++) { at += wave_rows[w]; chunk += wave_chunks[w]; }
+  for (int k = 0; k < each; k++) {
+    const int e = threadIdx.x * each + k;
+    if (e >= count) break;
+    first[e] = (int)chunk;
+    const uint32_t from = at;
+    for (int w = 0; w < waves; w++) {
+      const uint32_t s = counts[w * count + e];
+      counts[w * count + e] = at;
+      at += s;
+    }
+    for (uint32_t b = from, m = 0; b < at; b += CHUNK, m++) chunks[chunk++] = Chunk{e, (int)b, (int)std::min(at, b + (uint32_t)CHUNK), (int)m};
+    if (e == count - 1) first[count] = (int)chunk;
+  }
+  __syncthreads();
+  if (wave >= waves) return;
+  for (int64_t r0 = begin; r0 < end; r0 += 64) {
+    const int mine = r0 + lane < end ? pick.of(r0 + lane) : -1;
+    each_adapter(mine, 0, 1, [&](int e, uint64_t rows) {
+      const uint32_t base = counts[wave * count + e];      // (this wave's own word)
+      if (mine == e) order[base + __popcll(rows & ((1ull << lane) - 1))] = (int)(r0 + lane);
+      if (lane == 0) counts[wave * count + e] = base + __popcll(rows);
+      __builtin_amdgcn_wave_barrier();
+    });
+  }
+}
+
+// A workgroup takes 16 CT components and 128 columns of a chunk; its waves take the rows in turns.  The columns of eight rows are turned in a lane's registers as in
+// expand; T's numbers of eight rows come as they are wanted, one component a lane.
+struct Outer {
+  const float* t;      // [n][rank]
+  Mat z;
+  int C, scaled;
+  float* part;         // [chunk][rank][C]
+};
+constexpr int OW = 4;
+template <bool F32, int CT, int PIECES>
+__global__ __launch_bounds__(OW * 64) void outer_kernel(Outer q, Plan plan, Pick pick) {
+  typedef Eight<F32> E8;
+  constexpr int STEP = F32 ? 16 : 32, E = F32 ? 4 : 8, COLS = 128;
+  __shared__ float sums[OW / 2][CT * 16 * COLS];
+  const int chunk = blockIdx.y;
+  if (chunk >= plan.all(pick.count)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
+  const int c0 = blockIdx.x * COLS, c = c0 + i * 8, most = q.C - c, j0 = blockIdx.z * CT * 16;
+  const bool whole = c0 + COLS <= q.C;
+  const Chunk h = plan.at(chunk);
+  const float s = q.scaled ? pick.scale_of(h.e) : 1.f;
+  v4f acc[CT][8];
+#pragma unroll
+  for (int a = 0; a < CT; a++)
+#pragma unroll
+    for (int t = 0; t < 8; t++) acc[a][t] = v4f{0, 0, 0, 0};
+  for (int b = h.begin + wave * STEP; b < h.end; b += OW * STEP) {
+    typename E8::type w[E];
+    float x[CT][E];
+#pragma unroll
+    for (int k = 0; k < E; k++) {
+      const int at = b + g * E + k;
+      const bool in = at < h.end;
+      const int64_t row = in ? (plan.order ? plan.order[at] : at) : 0;
+      w[k] = E8::load(q.z.p, row * q.z.ld + c, in ? (whole ? 8 : most) : 0);
+#pragma unroll
+      for (int a = 0; a < CT; a++) {
+        const int j = j0 + a * 16 + i;
+        x[a][k] = in && j < pick.rank ? q.t[row * pick.rank + j] * s : 0.f;
+      }
+    }
+    if constexpr (F32) {
+#pragma unroll
+      for (int k = 0; k < E; k++) {
+        float col[8];
+        E8::values(w[k], col);
+#pragma unroll
+        for (int a = 0; a < CT; a++)
+#pragma unroll
+          for (int t = 0; t < 8; t++) acc[a][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[a][k], col[t], acc[a][t], 0, 0, 0);
+      }
+    } else {
+      u32x4 cols[8];
+      turned(w, cols);
+#pragma unroll
+      for (int a = 0; a < CT; a++) {
+        u32x4 p[PIECES];
+        pieces<PIECES>(x[a], p);
+#pragma unroll
+        for (int k = PIECES - 1; k >= 0; k--)
+#pragma unroll
+          for (int t = 0; t < 8; t++) acc[a][t] = Num<false>::mma(p[k], cols[t], acc[a][t]);
+      }
+    }
+  }
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int a = 0; a < CT; a++)
+#pragma unroll
+      for (int t = 0; t < 8; t++)
+#pragma unroll
+        for (int d = 0; d < 4; d++) acc[a][t][d] = f(((a * 8 + t) * 4 + d) * 64 + lane, acc[a][t][d]);
+  };
+#pragma unroll
+  for (int half = OW / 2; half > 0; half /= 2) {
+    __syncthreads();
+    if (wave >= half && wave < 2 * half) each([&](int at, float v) { return sums[wave - half][at] = v; });
+    __syncthreads();
+    if (wave < half) each([&](int at, float v) { return v + sums[wave][at]; });
+  }
+  if (wave > 0 || most <= 0) return;
+#pragma unroll
+  for (int a = 0; a < CT; a++)
+#pragma unroll
+    for (int d = 0; d < 4; d++) {
+      const int j = j0 + a * 16 + g * 4 + d;
+      if (j < pick.rank) {
+        float v[8];
+#pragma unroll
+        for (int t = 0; t < 8; t++) v[t] = acc[a][t][d];
+        put_f32(q.part + ((int64_t)chunk * pick.rank + j) * q.C + c, v, most);
+      }
+    }
+}
+// The chunks' sums of an adapter's component, added in order; zeros for what has no rows.
+__global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ part, Plan plan, Pick pick, int C, void* out, int f32) {
+  const int64_t rows = (int64_t)pick.count * pick.rank;
+  for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
+    const int e = (int)(row / pick.rank), j = (int)(row % pick.rank), first = plan.first_of(e), chunks = j < pick.rank_of(e) ? plan.chunks_of(e) : 0;
+    const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
+    if (c >= C) return;
+    float s[8] = {};
+    for (int k = 0; k < chunks; k++) {
+      float v[8];
+      get_values(part, ((int64_t)(first + k) * pick.rank + j) * C + c, 1, v, C - c);
+#pragma unroll
+      for (int t = 0; t < 8; t++) s[t] += v[t];
+    }
+    if (f32) put_f32(reinterpret_cast<float*>(out) + row * C + c, s, C - c);
+    else put_bf16(reinterpret_cast<uint16_t*>(out) + row * C + c, s, C - c);
+  }
+}
+
+// --------------------------------------------------------------------------------------------------
+// host
+// --------------------------------------------------------------------------------------------------
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Row tiles of 16 in a workgroup, and how its work is dealt out: parts of the contraction and slots of adapters to fill the chip where rows are few.
+struct Deal { int rt, ct, parts, slots; int64_t tiles; };
+Deal deal(int64_t n, int64_t K, int count, int rank, bool f32, bool index) {
+  Deal d;
+  d.rt = n <= 16 ? 1 : 2;
+  d.ct = rank <= 16 ? 1 : rank <= 32 ? 2 : 4;
+  d.tiles = up(n, 16 * d.rt);
+  d.slots = index ? (int)std::max<int64_t>(1, std::min<int64_t>({256 / d.tiles, 16 * d.rt, n, count})) : 1;
+  const int64_t turns = up(K, f32 ? 32 : d.rt * d.ct >= 4 ? 64 : 128), blocks = d.tiles * d.slots * up(rank, 16 * d.ct);
+  d.parts = (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(blocks, 1), up(turns, CW), 8}));
+  return d;
+}
+
+template <bool F32>
+void contract(const Contract& all, const Pick& pick, const Deal& d, hipStream_t s) {
+  const dim3 grid((unsigned)(d.tiles * d.slots), (unsigned)d.parts, (unsigned)up(pick.rank, 16 * d.ct)), block(CW * 64);
+  if (d.rt == 1) {
+    if (d.ct == 1) hipLaunchKernelGGL((contract_kernel<F32, 1, 1>), grid, block, 0, s, all, pick);
+    else if (d.ct == 2) hipLaunchKernelGGL((contract_kernel<F32, 1, 2>), grid, block, 0, s, all, pick);
+    else hipLaunchKernelGGL((contract_kernel<F32, 1, 4>), grid, block, 0, s, all, pick);
+  } else {
+    if (d.ct == 1) hipLaunchKernelGGL((contract_kernel<F32, 2, 1>), grid, block, 0, s, all, pick);
+    else if (d.ct == 2) hipLaunchKernelGGL((contract_kernel<F32, 2, 2>), grid, block, 0, s, all, pick);
+    else hipLaunchKernelGGL((contract_kernel<F32, 2, 4>), grid, block, 0, s, all, pick);
+  }
+}
+template <bool F32>
+void expand(const Expand& q, const Pick& pick, hipStream_t s) {
+  const int rt = q.n <= 16 ? 1 : 2;
+  const int64_t tiles = up(q.n, 16 * rt), blocks = up(q.C, EW * ECOLS);
+  Expand a = q;
+  a.slots = pick.index ? (int)std::max<int64_t>(1, std::min<int64_t>({1024 / (tiles * blocks), 16 * rt, q.n, pick.count})) : 1;
+  const dim3 grid((unsigned)(tiles * blocks), (unsigned)a.slots), block(EW * 64);
+  if (rt == 1) hipLaunchKernelGGL((expand_kernel<F32, 1>), grid, block, 0, s, a, pick);
+  else hipLaunchKernelGGL((expand_kernel<F32, 2>), grid, block, 0, s, a, pick);
+}
+template <bool F32, int PIECES>
+void outer(const Outer& q, const Plan& plan, const Pick& pick, int64_t chunks, hipStream_t s) {
+  const int ct = pick.rank <= 16 ? 1 : pick.rank <= 32 ? 2 : 4;
+  const dim3 grid((unsigned)up(q.C, 128), (unsigned)chunks, (unsigned)up(pick.rank, 16 * ct)), block(OW * 64);
+  if (ct == 1) hipLaunchKernelGGL((outer_kernel<F32, 1, PIECES>), grid, block, 0, s, q, plan, pick);
+  else if (ct == 2) hipLaunchKernelGGL((outer_kernel<F32, 2, PIECES>), grid, block, 0, s, q, plan, pick);
+  else hipLaunchKernelGGL((outer_kernel<F32, 4, PIECES>), grid, block, 0, s, q, plan, pick);
+}
+void outer_of(const Outer& q, const Plan& plan, const Pick& pick, int64_t chunks, bool f32, int32_t out_dtype, void* out, hipStream_t s) {
+  if (chunks > 0) {
+    if (f32) outer<true, 1>(q, plan, pick, chunks, s);
+    else if (out_dtype == OSSCAR_F32) outer<false, 3>(q, plan, pick, chunks, s);
+    else outer<false, 2>(q, plan, pick, chunks, s);
+  }
+  const int64_t rows = (int64_t)pick.count * pick.rank;
+  hipLaunchKernelGGL(join_kernel, dim3((unsigned)up(q.C, 2048), (unsigned)std::min<int64_t>(rows, 65535)), dim3(256), 0, s, q.part, plan, pick, q.C, out, out_dtype == OSSCAR_F32);
+}
+
+int64_t chunks_of(const osscar_adapters_desc& d, bool index) { return index ? up(d.n, CHUNK) + std::min<int64_t>(d.n, d.count) : up(d.n, CHUNK); }
+
+const char* bad_desc(const osscar_adapters_desc* d) {
+  if (!d) return "osscar_adapters: NULL description";
+  if (!a_size(d->n, 0) || !a_size(d->d, 1) || !a_size(d->m, 1)) return "osscar_adapters: n >= 0, d and m must be positive, none above 2^30";
+  if (d->count < 1 || d->count > OSSCAR_ADAPTERS_MAX) return "osscar_adapters: 1 to OSSCAR_ADAPTERS_MAX adapters";
+  if (d->rank < 1 || d->rank > OSSCAR_ADAPTER_MAX_RANK) return "osscar_adapters: ranks are 1 to OSSCAR_ADAPTER_MAX_RANK";
+  if (!real_dtype(d->dtype)) return "osscar_adapters: unknown dtype";
+  if (d->ldx < d->d || d->lda < d->d || d->ldb < d->m) return "osscar_adapters: leading dimension below the row length";
+  if (d->next_a < 0 || d->next_b < 0) return "osscar_adapters: negative stride of adapters";
+  // (of the launches' grids, which one row tile times the column blocks fill)
+  if (d->n > (int64_t)1 << 22) return "osscar_adapters: more than 2^22 rows in one call";
+  if (up(d->n, 16) * up(std::max(d->d, d->m), EW * ECOLS) >= (int64_t)1 << 23) return "osscar_adapters: too large";
+  return nullptr;
+}
+bool misaligned(const void* p, int32_t dtype) { return (uintptr_t)p % (dtype == OSSCAR_F32 ? 4 : 2) != 0; }
+size_t t_bytes(const osscar_adapters_desc& d, int parts) { return (size_t)parts * d.n * d.rank * 4; }
+
+}  // namespace
+
+extern "C" size_t osscar_adapters_workspace_bytes(const osscar_adapters_desc* d, int32_t backward) {
+  if (bad_desc(d)) return 0;
+  Carve c(nullptr);
+  if (d->n == 0 && !backward) return 256;
+  const bool f32 = d->dtype == OSSCAR_F32;
+  if (!backward) {
+    c.take(t_bytes(*d, deal(std::max<int64_t>(d->n, 1), d->d, d->count, d->rank, f32, d->index != 0).parts));
+  } else {
+    c.take(t_bytes(*d, deal(std::max<int64_t>(d->n, 1), d->m, d->count, d->rank, f32, d->index != 0).parts));      // dT in parts
+    c.take(t_bytes(*d, 1));                                                      // dT
+    c.take(t_bytes(*d, 1));                                                      // T, where it is not given
+    const int64_t chunks = chunks_of(*d, d->index != 0);
+    if (d->index) {
+      c.take((size_t)d->n * 4);
+      c.take((size_t)chunks * sizeof(Chunk));
+      c.take((size_t)(d->count + 1) * 4);
+    }
+    c.take((size_t)chunks * d->rank * std::max(d->d, d->m) * 4);
+  }
+  return c.used + 256;
+}
+
+extern "C" osscar_status osscar_adapters_forward(const osscar_adapters_desc* d, const void* X_dev, const void* A_dev, const void* B_dev, const int64_t* index_dev,
+                                                 const float* scale_dev, const int32_t* ranks_dev, const void* base_dev, int64_t ldbase, void* Y_dev, int64_t ldy, float* T_dev,
+                                                 void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  const char* bad = bad_desc(d);
+  if (!bad && (ldy < d->m || (base_dev && ldbase < d->m))) bad = "osscar_adapters_forward: leading dimension below the row length";
+  if (!bad && d->n > 0 && (d->index != 0) != (index_dev != nullptr)) bad = "osscar_adapters_forward: the description says whether there is an index";
+  if (!bad && (!A_dev || !B_dev || (d->n > 0 && (!X_dev || !Y_dev)))) bad = "osscar_adapters_forward: NULL pointer";
+  if (!bad && (misaligned(X_dev, d->dtype) || misaligned(A_dev, d->dtype) || misaligned(B_dev, d->dtype) || misaligned(base_dev, d->dtype) || misaligned(Y_dev, d->dtype) ||
+               misaligned(T_dev, OSSCAR_F32) || misaligned(scale_dev, OSSCAR_F32) || misaligned(ranks_dev, OSSCAR_F32) || ((uintptr_t)index_dev & 7)))
+    bad = "osscar_adapters_forward: a buffer is not aligned to its elements";
+  if (!bad && base_dev && base_dev == Y_dev && ldbase != ldy && d->n > 1) bad = "osscar_adapters_forward: in place, both leading dimensions are the same";
+  if (!bad && ((uintptr_t)workspace_dev & 255)) bad = "osscar_adapters_forward: the workspace must begin at a 256-byte boundary";
+  if (bad) return refuse_call(OSSCAR_EINVAL, bad);
+  if (d->n == 0) return OSSCAR_OK;
+  hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
+  const bool f32 = d->dtype == OSSCAR_F32;
+  const Pick pick{index_dev, scale_dev, ranks_dev, d->count, d->rank};
+  const Deal deal1 = deal(d->n, d->d, d->count, d->rank, f32, d->index != 0);
+  Carve c(workspace_dev);
+  float* t = reinterpret_cast<float*>(c.take(t_bytes(*d, deal1.parts)));
+  if (!workspace_dev || c.used > workspace_bytes) return refuse_call(OSSCAR_ENOMEM, "osscar_adapters_forward: workspace too small");
+  const bool direct = T_dev && deal1.parts == 1;
+  if (direct) t = T_dev;
+  const Contract k{Mat{X_dev, d->ldx}, Adapters{A_dev, d->lda, d->next_a}, d->n, (int)d->d, deal1.parts, deal1.slots, 0, t};
+  const Expand x{t, deal1.parts, 1, 1, Adapters{B_dev, d->ldb, d->next_b}, Mat{base_dev, ldbase}, d->n, (int)d->m, Y_dev, ldy, direct ? nullptr : T_dev};
+  if (f32) {
+    contract<true>(k, pick, deal1, s);
+    expand<true>(x, pick, s);
+  } else {
+    contract<false>(k, pick, deal1, s);
+    expand<false>(x, pick, s);
+  }
+  return launched();
+}
+
+extern "C" osscar_status osscar_adapters_backward(const osscar_adapters_desc* d, const void* X_dev, const void* A_dev, const void* B_dev, const int64_t* index_dev,
+                                                  const float* scale_dev, const int32_t* ranks_dev, const void* dY_dev, int64_t lddy, const float* T_dev, const void* base_dev,
+                                                  int64_t ldbase, void* dX_dev, int64_t lddx, void* dA_dev, void* dB_dev, int32_t dw_dtype, void* workspace_dev,
+                                                  size_t workspace_bytes, void* hip_stream) {
+  const char* bad = bad_desc(d);
+  const bool grads = dA_dev || dB_dev;
+  if (!bad && (lddy < d->m || (dX_dev && lddx < d->d) || (base_dev && ldbase < d->d))) bad = "osscar_adapters_backward: leading dimension below the row length";
+  if (!bad && d->n > 0 && (d->index != 0) != (index_dev != nullptr)) bad = "osscar_adapters_backward: the description says whether there is an index";
+  if (!bad && (!A_dev || !B_dev || (d->n > 0 && (!X_dev || !dY_dev)))) bad = "osscar_adapters_backward: NULL pointer";
+  if (!bad && (!dA_dev != !dB_dev)) bad = "osscar_adapters_backward: dA and dB are given together or not at all";
+  if (!bad && base_dev && !dX_dev) bad = "osscar_adapters_backward: base goes with dX";
+  if (!bad && grads && !real_dtype(dw_dtype)) bad = "osscar_adapters_backward: unknown dtype";
+  if (!bad && (misaligned(X_dev, d->dtype) || misaligned(A_dev, d->dtype) || misaligned(B_dev, d->dtype) || misaligned(base_dev, d->dtype) || misaligned(dY_dev, d->dtype) ||
+               misaligned(dX_dev, d->dtype) || misaligned(T_dev, OSSCAR_F32) || misaligned(scale_dev, OSSCAR_F32) || misaligned(ranks_dev, OSSCAR_F32) || ((uintptr_t)index_dev & 7) ||
+               (grads && (misaligned(dA_dev, dw_dtype) || misaligned(dB_dev, dw_dtype)))))
+    bad = "osscar_adapters_backward: a buffer is not aligned to its elements";
+  if (!bad && base_dev && base_dev == dX_dev && ldbase != lddx && d->n > 1) bad = "osscar_adapters_backward: in place, both leading dimensions are the same";
+  if (!bad && ((uintptr_t)workspace_dev & 255)) bad = "osscar_adapters_backward: the workspace must begin at a 256-byte boundary";
+  if (bad) return refuse_call(OSSCAR_EINVAL, bad);
+  if ((!grads && !dX_dev) || (d->n == 0 && !grads)) return OSSCAR_OK;
+  hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
+  const bool f32 = d->dtype == OSSCAR_F32, index = d->index != 0;
+  const Pick pick{index_dev, scale_dev, ranks_dev, d->count, d->rank};
+  const int64_t chunks = chunks_of(*d, index);
+  Deal dy = deal(std::max<int64_t>(d->n, 1), d->m, d->count, d->rank, f32, index), dx = deal(std::max<int64_t>(d->n, 1), d->d, d->count, d->rank, f32, index);
+  Carve c(workspace_dev);
+  float* dt_parts = reinterpret_cast<float*>(c.take(t_bytes(*d, dy.parts)));
+  float* dt = reinterpret_cast<float*>(c.take(t_bytes(*d, 1)));
+  float* t = reinterpret_cast<float*>(c.take(t_bytes(*d, 1)));
+  int* order = nullptr;
+  Chunk* table = nullptr;
+  int* first = nullptr;
+  if (index) {
+    order = reinterpret_cast<int*>(c.take((size_t)d->n * 4));
+    table = reinterpret_cast<Chunk*>(c.take((size_t)chunks * sizeof(Chunk)));
+    first = reinterpret_cast<int*>(c.take((size_t)(d->count + 1) * 4));
+  }
+  float* part = reinterpret_cast<float*>(c.take((size_t)chunks * d->rank * std::max(d->d, d->m) * 4));
+  if (c.used > 0 && (!workspace_dev || c.used > workspace_bytes)) return refuse_call(OSSCAR_ENOMEM, "osscar_adapters_backward: workspace too small");
+  if (d->n > 0) {
+    if (!dX_dev) dy.parts = 1;      // (the parts are added where dX is made)
+    if (dy.parts == 1) dt_parts = dt;
+    const Contract k{Mat{dY_dev, lddy}, Adapters{B_dev, d->ldb, d->next_b}, d->n, (int)d->m, dy.parts, dy.slots, 1, dt_parts};
+    if (f32) contract<true>(k, pick, dy, s);
+    else contract<false>(k, pick, dy, s);
+    if (dX_dev) {
+      const Expand x{dt_parts, dy.parts, 1, 0, Adapters{A_dev, d->lda, d->next_a}, Mat{base_dev, ldbase}, d->n, (int)d->d, dX_dev, lddx, dy.parts > 1 ? dt : nullptr};
+      if (f32) expand<true>(x, pick, s);
+      else expand<false>(x, pick, s);
+    }
+    if (!grads) return launched();
+    if (!T_dev) {
+      dx.parts = 1;
+      const Contract k2{Mat{X_dev, d->ldx}, Adapters{A_dev, d->lda, d->next_a}, d->n, (int)d->d, 1, dx.slots, 0, t};
+      if (f32) contract<true>(k2, pick, dx, s);
+      else contract<false>(k2, pick, dx, s);
+      T_dev = t;
+    }
+    if (index) {
+      const int waves = (int)std::min<int64_t>({16, PLAN_WORDS / d->count, up(d->n, 64)});
+      hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(1024), 0, s, pick, (int)d->n, waves, order, table, first);
+    }
+  }
+  const bool listed = index && d->n > 0;
+  const Plan plan{listed ? order : nullptr, table, first, d->n, listed ? 0 : (int)chunks};
+  const int64_t some = d->n > 0 ? chunks : 0;
+  outer_of(Outer{dt, Mat{X_dev, d->ldx}, (int)d->d, 0, part}, plan, pick, some, f32, dw_dtype, dA_dev, s);
+  outer_of(Outer{T_dev, Mat{dY_dev, lddy}, (int)d->m, 1, part}, plan, pick, some, f32, dw_dtype, dB_dev, s);
+  return launched();
+}

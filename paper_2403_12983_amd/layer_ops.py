@@ -17,7 +17,7 @@ from typing import List, NamedTuple, Optional, Sequence, Tuple, Union
 
 import torch
 
-from .binding import OSSCAR_ACT_SILU, OSSCAR_BF16, OSSCAR_F32, OSSCAR_I8, OsscarError, _AdamWDesc, _AdamWTensor, _GatedDesc, load_library
+from .binding import OSSCAR_ACT_SILU, OSSCAR_BF16, OSSCAR_F32, OSSCAR_I8, OsscarError, _AdamWDesc, _AdamWTensor, _AdaptersDesc, _GatedDesc, load_library
 
 _CODES = {torch.float32: OSSCAR_F32, torch.bfloat16: OSSCAR_BF16}
 _EINVAL = 1
@@ -50,7 +50,7 @@ def _ld(t: torch.Tensor, what: str) -> int:
     return s0
 
 
-def _on(index: int, **tensors: Optional[torch.Tensor]):
+def _on(index: int, /, **tensors: Optional[torch.Tensor]):
     for name, t in tensors.items():
         if t is not None and t.get_device() != index:
             _refuse(f"{name} is on {t.device}, expected cuda:{index}")
@@ -380,6 +380,93 @@ def osscar_layernorm_backward(X: torch.Tensor, weight: Optional[torch.Tensor], d
                                                db.data_ptr() if need_w else None, _CODES[dw_dtype], wsp, size, handle)
     _done(lib, status)
     return dX, dw, db
+
+
+def _components(t: torch.Tensor, what: str) -> Tuple[int, int]:
+    """(from one component to the next, from one adapter to the next) of adapters x components x width"""
+    if t.dim() != 3:
+        _refuse(f"{what} is adapters x rank x width")
+    count, rank, width = t.shape
+    if width > 1 and t.stride(2) != 1:
+        _refuse(f"the components of {what} must be contiguous")
+    ld = t.stride(1) if rank > 1 else width
+    if ld < width:
+        _refuse(f"the components of {what} overlap")
+    return max(ld, 1), t.stride(0) if count > 1 else 0
+
+
+def _adapters(X, A, B, index, scale, ranks, at: int):
+    """(description, addresses of X, A, B, index, scale, ranks)"""
+    code = _code(X, "X")
+    if A.dtype != X.dtype or B.dtype != X.dtype:
+        _refuse("X, A and B have one dtype")
+    ldx, (lda, next_a), (ldb, next_b) = _ld(X, "X"), _components(A, "A"), _components(B, "B")
+    n, d = X.shape
+    if A.shape[:2] != B.shape[:2] or A.shape[2] != d:
+        _refuse("A is adapters x rank x d, B adapters x rank x m")
+    _on(at, A=A, B=B, index=index, scale=scale, ranks=ranks)
+    count, rank = A.shape[:2]
+    ip = None if index is None else _vector(index, n, torch.int64, "index")
+    sp = None if scale is None else _vector(scale, count, torch.float32, "scale")
+    rp = None if ranks is None else _vector(ranks, count, torch.int32, "ranks")
+    return _AdaptersDesc(n, d, B.shape[2], ldx, lda, next_a, ldb, next_b, count, rank, code, 0 if index is None else 1), (X.data_ptr(), A.data_ptr(), B.data_ptr(), ip, sp, rp)
+
+
+def osscar_adapters_forward(X: torch.Tensor, A: torch.Tensor, B: torch.Tensor, index: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                            ranks: Optional[torch.Tensor] = None, base: Optional[torch.Tensor] = None, save: bool = False, out: Optional[torch.Tensor] = None,
+                            stream: Optional[torch.cuda.Stream] = None):
+    """Row i of Y is base_i + scale_e (X_i A_e^T) B_e with e = index[i]: low-rank adapters beside a projection whose output is `base` (n x m; None: zeros).  X: n x d, A: adapters x rank x d,
+    B: adapters x rank x m, one dtype.  index: int64, negative where a row has none; None: all rows have the first.  scale: float32 per adapter.  ranks: int32 per adapter, how
+    many of its components count.  out: where to put Y, `base` itself included.  save: returns (Y, T) with the n x rank float32 products X_i A_e^T, else Y."""
+    lib, at, handle, context = _begin(X, stream)
+    desc, (xp, ap, bp, ip, sp, rp) = _adapters(X, A, B, index, scale, ranks, at)
+    n, m = desc.n, desc.m
+    if base is not None and (base.shape != (n, m) or base.dtype != X.dtype):
+        _refuse("base is n x m, of the dtype of X")
+    _on(at, base=base, out=out)
+    with context:
+        Y = _out(out, X, (n, m))
+        T = _EMPTY(n, desc.rank, dtype=torch.float32, device=X.device) if save else None
+        ws, wp, size = _workspace(lib.osscar_adapters_workspace_bytes(C.byref(desc), 0), X.device)
+        status = lib.osscar_adapters_forward(C.byref(desc), xp, ap, bp, ip, sp, rp, None if base is None else base.data_ptr(), m if base is None else _ld(base, "base"),
+                                             Y.data_ptr(), _ld(Y, "out"), T.data_ptr() if save else None, wp, size, handle)
+    _done(lib, status)
+    return (Y, T) if save else Y
+
+
+def osscar_adapters_backward(X: torch.Tensor, A: torch.Tensor, B: torch.Tensor, dY: torch.Tensor, T: Optional[torch.Tensor] = None, index: Optional[torch.Tensor] = None,
+                             scale: Optional[torch.Tensor] = None, ranks: Optional[torch.Tensor] = None, base: Optional[torch.Tensor] = None, need_x: bool = True,
+                             need_w: bool = True, dw_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """(dX, dA, dB) of osscar_adapters_forward for the gradient dY of Y; None for what is not needed.  T: from forward's save=True (else it is computed again).  base: n x d, what
+    dX is added to, as the gradient that came through the projection (None: zeros).  out: where to put dX, `base` itself included.  dw_dtype: float32 or
+    bfloat16, by default the adapters'."""
+    lib, at, handle, context = _begin(X, stream)
+    desc, (xp, ap, bp, ip, sp, rp) = _adapters(X, A, B, index, scale, ranks, at)
+    n, d, m, device = desc.n, desc.d, desc.m, X.device
+    if dY.shape != (n, m) or dY.dtype != X.dtype:
+        _refuse("dY is n x m, of the dtype of X")
+    if base is not None and (base.shape != (n, d) or base.dtype != X.dtype):
+        _refuse("base is n x d, of the dtype of X")
+    if T is not None and (T.shape != (n, desc.rank) or T.dtype != torch.float32 or not T.is_contiguous()):
+        _refuse("T must be the n x rank float32 tensor of osscar_adapters_forward")
+    if not need_x and (base is not None or out is not None):
+        _refuse("base and out go with need_x")
+    dw_dtype = X.dtype if dw_dtype is None else dw_dtype
+    if dw_dtype not in _CODES:
+        _refuse(f"dw_dtype {dw_dtype} is neither float32 nor bfloat16")
+    _on(at, dY=dY, T=T, base=base, out=out)
+    with context:
+        dX = _out(out, X, (n, d)) if need_x else None
+        dA = dB = None
+        if need_w:
+            dA, dB = _EMPTY(A.shape, dtype=dw_dtype, device=device), _EMPTY(B.shape, dtype=dw_dtype, device=device)
+        ws, wp, size = _workspace(lib.osscar_adapters_workspace_bytes(C.byref(desc), 1), device)
+        status = lib.osscar_adapters_backward(C.byref(desc), xp, ap, bp, ip, sp, rp, dY.data_ptr(), _ld(dY, "dY"), None if T is None else T.data_ptr(),
+                                              None if base is None else base.data_ptr(), d if base is None else _ld(base, "base"), dX.data_ptr() if need_x else None,
+                                              _ld(dX, "out") if need_x else d, dA.data_ptr() if need_w else None, dB.data_ptr() if need_w else None, _CODES[dw_dtype], wp, size,
+                                              handle)
+    _done(lib, status)
+    return dX, dA, dB
 
 
 _BLOCK = 256
