@@ -97,7 +97,7 @@ constexpr int CW = 8;      // waves
 template <bool F32, int RT, int CT>
 __global__ __launch_bounds__(CW * 64) void contract_kernel(Contract q, Pick pick) {
   typedef Num<F32> N;
-  constexpr int U = F32 ? 2 : RT * CT >= 4 ? 2 : 4, TURN = U * N::STEP, ROWS = RT * 16, COLS = CT * 16;
+  constexpr int U = F32 ? 2 : RT * CT > 4 ? 2 : 4, TURN = U * N::STEP, ROWS = RT * 16, COLS = CT * 16;
   __shared__ float sums[CW / 2][ROWS * (COLS + 1)];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
   const int64_t tiles = (q.n + ROWS - 1) / ROWS, row0 = (blockIdx.x % tiles) * ROWS;
@@ -238,7 +238,7 @@ __device__ __forceinline__ void turned(const u16x8 (&w)[8], u32x4 (&p)[8]) {
 
 struct Expand {
   const float* t;      // [part][n][rank]
-  int parts, slots, scaled;
+  int parts, slots, scaled, subs;
   Adapters v;
   Mat base;            // (p may be NULL, or y)
   int64_t n;
@@ -248,24 +248,92 @@ struct Expand {
   float* t_out;        // the parts' sum, or NULL
 };
 constexpr int EW = 4, ECOLS = 128;      // waves, columns of each
-// A wave takes 16 RT rows and 128 columns: lane (i, g) reads eight columns c0 + 8 i .. of eight components 8 g .. and turns them in its registers, so that the instruction for tile t
-// has columns c0 + 8 i + t; the results of a lane are then eight neighbouring columns of four rows.
-template <bool F32, int RT>
-__global__ __launch_bounds__(EW * 64) void expand_kernel(Expand q, Pick pick) {
+// The components j .. of eight columns from c, as the matrix instruction takes them; zeros from `rank` on.
+template <bool F32> struct Columns;
+template <> struct Columns<false> {
+  static constexpr int STEP = 32, E = 8;
+  u32x4 w[8];      // column c + t of eight components
+  __device__ __forceinline__ void load(const char* v, int64_t ld, int j, int rank, int c, bool whole, int most) {
+    u16x8 x[E];
+#pragma unroll
+    for (int k = 0; k < E; k++) {
+      const int64_t at = (int64_t)std::min(j + k, rank - 1) * ld + c;
+      x[k] = whole ? Eight<false>::load(v, at) : Eight<false>::load(v, at, most);
+    }
+#pragma unroll
+    for (int k = 0; k < E; k++)
+      if (j + k >= rank) x[k] = u16x8{};
+    turned(x, w);
+  }
+  __device__ __forceinline__ void multiply(const float (&x)[E], v4f (&acc)[8]) const {
+    u32x4 p[2];
+    pieces<2>(x, p);
+#pragma unroll
+    for (int k = 1; k >= 0; k--)
+#pragma unroll
+      for (int t = 0; t < 8; t++) acc[t] = Num<false>::mma(p[k], w[t], acc[t]);
+  }
+};
+template <> struct Columns<true> {
+  static constexpr int STEP = 16, E = 4;
+  float w[E][8];
+  __device__ __forceinline__ void load(const char* v, int64_t ld, int j, int rank, int c, bool whole, int most) {
+    Eight<true>::type x[E];
+#pragma unroll
+    for (int k = 0; k < E; k++) {
+      const int64_t at = (int64_t)std::min(j + k, rank - 1) * ld + c;
+      x[k] = whole ? Eight<true>::load(v, at) : Eight<true>::load(v, at, most);
+    }
+#pragma unroll
+    for (int k = 0; k < E; k++) {
+      Eight<true>::values(x[k], w[k]);
+#pragma unroll
+      for (int t = 0; t < 8; t++) w[k][t] = j + k < rank ? w[k][t] : 0.f;
+    }
+  }
+  __device__ __forceinline__ void multiply(const float (&x)[E], v4f (&acc)[8]) const {
+#pragma unroll
+    for (int k = 0; k < E; k++)
+#pragma unroll
+      for (int t = 0; t < 8; t++) acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[k], w[k][t], acc[t], 0, 0, 0);
+  }
+};
+// E numbers of a row of T, from its j-th of `rank`
+template <int E>
+__device__ __forceinline__ void t_values(const float* t, int j, int rank, float (&x)[E]) {
+  if (j + E <= rank) {
+#pragma unroll
+    for (int k = 0; k < E; k += 4) {
+      const f32x4 w = *reinterpret_cast<const f32x4_any*>(t + j + k);
+#pragma unroll
+      for (int e = 0; e < 4; e++) x[k + e] = w[e];
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < E; k++) { x[k] = 0.f; if (j + k < rank) x[k] = t[j + k]; }
+  }
+}
+// A wave takes 128 columns of up to 64 rows, 16 at a time: lane (i, g) reads eight columns c0 + 8 i .. of components 8 g .. and turns them in its registers, so that
+// the instruction for tile t has columns c0 + 8 i + t; the results of a lane are then eight neighbouring columns of four rows.  The columns stay in registers for all rows of their
+// adapter (KS steps of components; 0: more than that, read again for each 16 rows), the next 16 rows' base and T are on their way while those before are multiplied.
+template <bool F32, int KS>
+__global__ __launch_bounds__(EW * 64, 2) void expand_kernel(Expand q, Pick pick) {
   typedef Eight<F32> E8;
-  constexpr int ROWS = RT * 16, STEP = F32 ? 16 : 32, E = F32 ? 4 : 8;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
+  typedef Columns<F32> Cols;
+  constexpr int STEP = Cols::STEP, E = Cols::E, HELD = KS > 0 ? KS : 1;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4, rows_a_tile = q.subs * 16;
   const int blocks = (q.C + EW * ECOLS - 1) / (EW * ECOLS);
-  const int64_t row0 = (int64_t)(blockIdx.x / blocks) * ROWS;
+  const int64_t row0 = (int64_t)(blockIdx.x / blocks) * rows_a_tile;
   const int c0 = (blockIdx.x % blocks) * (EW * ECOLS) + wave * ECOLS, slot = blockIdx.y, c = c0 + i * 8;
-  if (c0 >= q.C && !(q.t_out && c0 == 0)) return;
-  const int have = (int)std::min<int64_t>(ROWS, q.n - row0), most = q.C - c;
+  if (c0 >= q.C) return;
+  const int have = (int)std::min<int64_t>(rows_a_tile, q.n - row0), most = q.C - c;
   const int mine = lane < have ? pick.of(row0 + lane) : -1;
-  const bool whole = c0 + ECOLS <= q.C;
-  const size_t es = F32 ? 4 : 2;
+  const bool whole = c0 + ECOLS <= q.C, keeps = q.t_out && c0 == 0;
+  constexpr size_t ES = F32 ? 4 : 2;
   if (slot == 0) {      // rows without an adapter
-    uint64_t none = __ballot(mine < 0 && lane < have), wrong = __ballot(mine == -2);
-    if (q.t_out && c0 == 0)
+    uint64_t none = __ballot(mine < 0 && lane < have);
+    const uint64_t wrong = __ballot(mine == -2);
+    if (keeps)
       for (int k = lane; k < have * pick.rank; k += 64)
         if (none >> (k / pick.rank) & 1) q.t_out[row0 * pick.rank + k] = 0.f;
     if (q.y == q.base.p) none = wrong;
@@ -284,112 +352,113 @@ __global__ __launch_bounds__(EW * 64) void expand_kernel(Expand q, Pick pick) {
   each_adapter(mine, slot, q.slots, [&](int e, uint64_t rows) {
     const int rank = pick.rank_of(e);
     const float s = q.scaled ? pick.scale_of(e) : 1.f;
-    const char* v = reinterpret_cast<const char*>(q.v.p) + e * q.v.next * es;
-    typename E8::type base[RT][4];
-    if (q.base.p) {
-#pragma unroll
-      for (int r = 0; r < RT; r++)
+    const char* v = reinterpret_cast<const char*>(q.v.p) + e * q.v.next * ES;
+    struct Rows16 { typename E8::type base[4]; float x[HELD][E]; };
+    auto next = [&](int sub) {      // the first from there on with rows of this adapter
+      while (sub < q.subs && !(rows >> (sub * 16) & 0xFFFF)) sub++;
+      return sub;
+    };
+    auto fetch = [&](int sub, Rows16& w) {
+      if (q.base.p) {
 #pragma unroll
         for (int d = 0; d < 4; d++) {
-          const int row = r * 16 + g * 4 + d;
-          if (rows >> row & 1) base[r][d] = whole ? E8::load(q.base.p, (row0 + row) * q.base.ld + c) : E8::load(q.base.p, (row0 + row) * q.base.ld + c, most);
+          const int row = sub * 16 + g * 4 + d;
+          if (rows >> row & 1) w.base[d] = whole ? E8::load(q.base.p, (row0 + row) * q.base.ld + c) : E8::load(q.base.p, (row0 + row) * q.base.ld + c, most);
         }
+      }
+      const int row = sub * 16 + i;
+#pragma unroll
+      for (int k = 0; k < KS; k++) {
+#pragma unroll
+        for (int x = 0; x < E; x++) w.x[k][x] = 0.f;
+        if (rows >> row & 1) t_values<E>(q.t + (row0 + row) * pick.rank, k * STEP + g * E, pick.rank, w.x[k]);
+      }
+    };
+    // T of a row: the other parts, kept where that is asked for, components past the rank left out, scaled
+    auto finish = [&](int sub, int j, float (&x)[E]) {
+      const int row = sub * 16 + i;
+      if (rows >> row & 1) {
+#pragma unroll 4
+        for (int p = 1; p < q.parts; p++) {
+          float more[E];
+          t_values<E>(q.t + ((int64_t)p * q.n + row0 + row) * pick.rank, j, pick.rank, more);
+#pragma unroll
+          for (int k = 0; k < E; k++) x[k] += more[k];
+        }
+        if (keeps) {
+#pragma unroll
+          for (int k = 0; k < E; k++)
+            if (j + k < pick.rank) q.t_out[(row0 + row) * pick.rank + j + k] = x[k];
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < E; k++) x[k] = j + k < rank ? x[k] * s : 0.f;
+    };
+    Rows16 now, then;
+    int sub = next(0);
+    fetch(sub, now);
+    Cols cols[HELD];
+    if (rank > 0) {
+#pragma unroll
+      for (int k = 0; k < KS; k++) cols[k].load(v, q.v.ld, k * STEP + g * E, rank, c, whole, most);
     }
-    v4f acc[RT][8];
+    while (sub < q.subs) {
+      const int after = next(sub + 1);
+      if (after < q.subs) fetch(after, then);
+      v4f acc[8];
 #pragma unroll
-    for (int r = 0; r < RT; r++)
+      for (int t = 0; t < 8; t++) acc[t] = v4f{0, 0, 0, 0};
+      if constexpr (KS > 0) {
 #pragma unroll
-      for (int t = 0; t < 8; t++) acc[r][t] = v4f{0, 0, 0, 0};
-    for (int j0 = 0; j0 < rank; j0 += STEP) {
-      const int j = j0 + g * E;
-      // this lane's components of V and of T
-      typename E8::type w[E];
-#pragma unroll
-      for (int k = 0; k < E; k++) {
-        const int64_t at = (int64_t)std::min(j + k, rank - 1) * q.v.ld + c;
-        w[k] = whole ? E8::load(v, at) : E8::load(v, at, most);
-        if (j + k >= rank) w[k] = E8::load(v, 0, 0);      // (zeros)
-      }
-      float x[RT][E];
-#pragma unroll
-      for (int r = 0; r < RT; r++) {
-        const int at = rows >> (r * 16 + i) & 1 ? r * 16 + i : -1;
-#pragma unroll
-        for (int k = 0; k < E; k++) x[r][k] = 0.f;
-        if (at >= 0) {
-          for (int p = 0; p < q.parts; p++) {
-            const float* t = q.t + ((int64_t)p * q.n + row0 + at) * pick.rank + j;
-#pragma unroll
-            for (int k = 0; k < E; k++)
-              if (j + k < rank) x[r][k] += t[k];
-          }
-          if (q.t_out && c0 == 0) {
-#pragma unroll
-            for (int k = 0; k < E; k++)
-              if (j + k < rank) q.t_out[(row0 + at) * pick.rank + j + k] = x[r][k];
-          }
-        }
-#pragma unroll
-        for (int k = 0; k < E; k++) x[r][k] *= s;
-      }
-      if constexpr (F32) {
-#pragma unroll
-        for (int k = 0; k < E; k++) {
-          float col[8];
-          E8::values(w[k], col);
-#pragma unroll
-          for (int r = 0; r < RT; r++)
-#pragma unroll
-            for (int t = 0; t < 8; t++) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[r][k], col[t], acc[r][t], 0, 0, 0);
+        for (int k = 0; k < KS; k++) {
+          finish(sub, k * STEP + g * E, now.x[k]);
+          if (k * STEP < rank) cols[k].multiply(now.x[k], acc);
         }
       } else {
-        u32x4 cols[8];
-        turned(w, cols);
+        const int row = sub * 16 + i;
+        for (int j0 = 0; j0 < (keeps ? pick.rank : rank); j0 += STEP) {
+          float x[E];
 #pragma unroll
-        for (int r = 0; r < RT; r++) {
-          u32x4 p[2];
-          pieces<2>(x[r], p);
-#pragma unroll
-          for (int t = 0; t < 8; t++) acc[r][t] = Num<false>::mma(p[1], cols[t], Num<false>::mma(p[0], cols[t], acc[r][t]));
+          for (int k = 0; k < E; k++) x[k] = 0.f;
+          if (rows >> row & 1) t_values<E>(q.t + (row0 + row) * pick.rank, j0 + g * E, pick.rank, x);
+          finish(sub, j0 + g * E, x);
+          if (j0 < rank) {
+            cols[0].load(v, q.v.ld, j0 + g * E, rank, c, whole, most);
+            cols[0].multiply(x, acc);
+          }
         }
       }
-    }
-    if (q.t_out && c0 == 0) {      // components past the adapter's rank
-      for (int r = 0; r < have; r++)
-        if (rows >> r & 1)
-          for (int j = rank + lane; j < pick.rank; j += 64) q.t_out[(row0 + r) * pick.rank + j] = 0.f;
-    }
-#pragma unroll
-    for (int r = 0; r < RT; r++)
 #pragma unroll
       for (int d = 0; d < 4; d++) {
-        const int row = r * 16 + g * 4 + d;
+        const int row = sub * 16 + g * 4 + d;
         if (rows >> row & 1) {
           float y[8];
-          if (q.base.p) E8::values(base[r][d], y);
+          if (q.base.p) E8::values(now.base[d], y);
 #pragma unroll
-          for (int t = 0; t < 8; t++) y[t] = q.base.p ? y[t] + acc[r][t][d] : acc[r][t][d];
+          for (int t = 0; t < 8; t++) y[t] = q.base.p ? y[t] + acc[t][d] : acc[t][d];
           if (whole) E8::store(q.y, (row0 + row) * q.ldy + c, y);
           else E8::store(q.y, (row0 + row) * q.ldy + c, y, most);
         }
       }
+      now = then;
+      sub = after;
+    }
   });
 }
 
 // --------------------------------------------------------------------------------------------------
 // outer
 // --------------------------------------------------------------------------------------------------
-// The rows in the order of their adapters, and pieces of at most CHUNK rows of one adapter.
-constexpr int CHUNK = 512;
-struct Chunk { int e, begin, end, number; };      // number: of its adapter's
+// The rows in the order of their adapters, and pieces of at most `chunk` rows of one adapter.
+struct Chunk { int e, begin, end; };
 struct Plan {
   const int* order;            // (NULL: as they lie)
   const Chunk* chunks;
   const int* first;            // count + 1: an adapter's first chunk
   int64_t n;
-  int total;                   // order NULL: how many
+  int total, chunk;            // order NULL: how many; rows of one at most
   __device__ __forceinline__ Chunk at(int c) const {
-    if (!order) return Chunk{0, (int)((int64_t)c * CHUNK), (int)std::min<int64_t>(n, ((int64_t)c + 1) * CHUNK), c};
+    if (!order) return Chunk{0, c * chunk, (int)min(n, ((int64_t)c + 1) * chunk)};
     return chunks[c];
   }
   __device__ __forceinline__ int chunks_of(int e) const { return order ? first[e + 1] - first[e] : e == 0 ? total : 0; }
@@ -400,7 +469,7 @@ struct Plan {
 // and adapters it goes over the span again, 64 rows at a time, and gives rows of one adapter their places together.
 constexpr int PLAN_WORDS = 32768;      // of LDS: counts by wave and adapter
 static_assert(OSSCAR_ADAPTERS_MAX * 2 <= PLAN_WORDS, "");
-__global__ __launch_bounds__(1024) void plan_kernel(Pick pick, int n, int waves, int* order, Chunk* chunks, int* first) {
+__global__ __launch_bounds__(1024) void plan_kernel(Pick pick, int n, int waves, uint32_t rows_a_chunk, int* order, Chunk* chunks, int* first) {
   __shared__ uint32_t counts[PLAN_WORDS];
   __shared__ uint32_t wave_rows[16], wave_chunks[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, count = pick.count;
@@ -423,7 +492,7 @@ __global__ __launch_bounds__(1024) void plan_kernel(Pick pick, int n, int waves,
     uint32_t s = 0;
     for (int w = 0; w < waves; w++) s += counts[w * count + e];
     rows += s;
-    parts += (s + CHUNK - 1) / CHUNK;
+    parts += (s + rows_a_chunk - 1) / rows_a_chunk;
   }
   uint32_t rows_to = rows, parts_to = parts;      // sums up to this thread, itself included
   for (int o = 1; o < 64; o <<= 1) {
@@ -444,7 +513,7 @@ __global__ __launch_bounds__(1024) void plan_kernel(Pick pick, int n, int waves,
       counts[w * count + e] = at;
       at += s;
     }
-    for (uint32_t b = from, m = 0; b < at; b += CHUNK, m++) chunks[chunk++] = Chunk{e, (int)b, (int)std::min(at, b + (uint32_t)CHUNK), (int)m};
+    for (uint32_t b = from; b < at; b += rows_a_chunk) chunks[chunk++] = Chunk{e, (int)b, (int)min(at, b + rows_a_chunk)};
     if (e == count - 1) first[count] = (int)chunk;
   }
   __syncthreads();
@@ -460,99 +529,154 @@ __global__ __launch_bounds__(1024) void plan_kernel(Pick pick, int n, int waves,
   }
 }
 
-// A workgroup takes 16 CT components and 128 columns of a chunk; its waves take the rows in turns.  The columns of eight rows are turned in a lane's registers as in
-// expand; T's numbers of eight rows come as they are wanted, one component a lane.
+// A workgroup takes 16 CT components and 128 columns of a chunk, 32 columns a wave.  Rows go through LDS, STAGE of them at a time (the next ones on their way in registers while
+// one stage is multiplied): Z as it is, T cut into its pieces once for all waves.  The contraction runs across the rows of both, so bf16 operands come through the transposing
+// read of four 16-bit elements, float32 ones word by word.
 struct Outer {
   const float* t;      // [n][rank]
   Mat z;
   int C, scaled;
   float* part;         // [chunk][rank][C]
 };
-constexpr int OW = 4;
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4s lds_v4s;
+constexpr int OW = 4, OCOLS = 128;
+template <bool F32, int CT, int PIECES> struct Stage;
+template <int CT, int PIECES>
+struct Stage<false, CT, PIECES> {
+  static constexpr int ROWS = 64, ZROW = OCOLS * 2, TROW = CT * 32 + 16, ZBYTES = ROWS * ZROW, BYTES = ZBYTES + PIECES * ROWS * TROW;
+  // packets of a row change places, so that the four rows that sixteen lanes read at once meet other banks
+  static __device__ __forceinline__ int swizzle(int row) { return ((row & 3) | ((row >> 3) & 1) << 2) << 1; }
+  static __device__ __forceinline__ void put_z(char* lds, int row, int packet, const u16x8& w) {
+    *reinterpret_cast<u16x8*>(lds + row * ZROW + ((packet ^ swizzle(row)) * 16)) = w;
+  }
+  static __device__ __forceinline__ void put_t(char* lds, int row, int j, const float (&x)[4]) {
+    float left[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+    for (int p = 0; p < PIECES; p++) {
+      typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
+      v4bf w;
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        w[e] = (__bf16)left[e];
+        left[e] -= (float)w[e];
+      }
+      *reinterpret_cast<v4bf*>(lds + ZBYTES + (p * ROWS + row) * TROW + j * 2) = w;
+    }
+  }
+  static __device__ __forceinline__ u32x4 turned_read(const char* q, int below) {
+    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)q), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(q + below));
+    return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+  // sixteen lanes read four rows of four quads of neighbouring elements each and get a column of them
+  static __device__ __forceinline__ void multiply(const char* lds, int wave, int lane, v4f (&acc)[CT][2]) {
+    const int i = lane & 15, g = lane >> 4, k = g * 8 + (i >> 2), q = i & 3;
+#pragma unroll
+    for (int half = 0; half < ROWS / 32; half++) {
+      u32x4 z[2];
+#pragma unroll
+      for (int t = 0; t < 2; t++) {
+        const int row = half * 32 + k, col = wave * 32 + t * 16 + q * 4;
+        z[t] = turned_read(lds + row * ZROW + (((col >> 3) ^ swizzle(row)) * 16) + ((col >> 2) & 1) * 8, 4 * ZROW);      // (rows + 4: the same swizzle)
+      }
+#pragma unroll
+      for (int a = 0; a < CT; a++)
+#pragma unroll
+        for (int p = PIECES - 1; p >= 0; p--) {
+          const u32x4 w = turned_read(lds + ZBYTES + (p * ROWS + half * 32 + k) * TROW + a * 32 + q * 8, 4 * TROW);
+#pragma unroll
+          for (int t = 0; t < 2; t++) acc[a][t] = Num<false>::mma(w, z[t], acc[a][t]);
+        }
+    }
+  }
+};
+template <int CT, int PIECES>
+struct Stage<true, CT, PIECES> {
+  static constexpr int ROWS = 32, ZROW = (OCOLS + 16) * 4, TROW = (CT == 1 ? 16 : CT * 16 + 16) * 4, ZBYTES = ROWS * ZROW, BYTES = ZBYTES + ROWS * TROW;      // (four rows meet other banks)
+  static __device__ __forceinline__ void put_z(char* lds, int row, int packet, const Eight<true>::type& w) {
+    f32x4* q = reinterpret_cast<f32x4*>(lds + row * ZROW + packet * 32);
+    q[0] = w.a;
+    q[1] = w.b;
+  }
+  static __device__ __forceinline__ void put_t(char* lds, int row, int j, const float (&x)[4]) {
+    *reinterpret_cast<f32x4*>(lds + ZBYTES + row * TROW + j * 4) = f32x4{x[0], x[1], x[2], x[3]};
+  }
+  static __device__ __forceinline__ void multiply(const char* lds, int wave, int lane, v4f (&acc)[CT][2]) {
+    const int i = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int k = 0; k < ROWS; k += 4) {
+      float z[2];
+#pragma unroll
+      for (int t = 0; t < 2; t++) z[t] = *reinterpret_cast<const float*>(lds + (k + g) * ZROW + (wave * 32 + t * 16 + i) * 4);
+#pragma unroll
+      for (int a = 0; a < CT; a++) {
+        const float w = *reinterpret_cast<const float*>(lds + ZBYTES + (k + g) * TROW + (a * 16 + i) * 4);
+#pragma unroll
+        for (int t = 0; t < 2; t++) acc[a][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(w, z[t], acc[a][t], 0, 0, 0);
+      }
+    }
+  }
+};
 template <bool F32, int CT, int PIECES>
 __global__ __launch_bounds__(OW * 64) void outer_kernel(Outer q, Plan plan, Pick pick) {
   typedef Eight<F32> E8;
-  constexpr int STEP = F32 ? 16 : 32, E = F32 ? 4 : 8, COLS = 128;
-  __shared__ float sums[OW / 2][CT * 16 * COLS];
+  typedef Stage<F32, CT, PIECES> S;
+  constexpr int NZ = S::ROWS * (OCOLS / 8) / (OW * 64), TPR = OW * 64 / S::ROWS, NT = CT * 16 / (TPR * 4) > 0 ? CT * 16 / (TPR * 4) : 1;      // packets of Z, quads of T a thread
+  __shared__ __align__(16) char lds[2][S::BYTES];
   const int chunk = blockIdx.y;
   if (chunk >= plan.all(pick.count)) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
-  const int c0 = blockIdx.x * COLS, c = c0 + i * 8, most = q.C - c, j0 = blockIdx.z * CT * 16;
-  const bool whole = c0 + COLS <= q.C;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c0 = blockIdx.x * OCOLS, j0 = blockIdx.z * CT * 16;
+  const bool whole = c0 + OCOLS <= q.C;
   const Chunk h = plan.at(chunk);
   const float s = q.scaled ? pick.scale_of(h.e) : 1.f;
-  v4f acc[CT][8];
+  typename E8::type z[NZ];
+  float t[NT][4];
+  const int zc = tid % (OCOLS / 8), zr = tid / (OCOLS / 8), tr = tid / TPR, tq = tid % TPR;
+  auto fetch = [&](int b) {
 #pragma unroll
-  for (int a = 0; a < CT; a++)
-#pragma unroll
-    for (int t = 0; t < 8; t++) acc[a][t] = v4f{0, 0, 0, 0};
-  for (int b = h.begin + wave * STEP; b < h.end; b += OW * STEP) {
-    typename E8::type w[E];
-    float x[CT][E];
-#pragma unroll
-    for (int k = 0; k < E; k++) {
-      const int at = b + g * E + k;
-      const bool in = at < h.end;
-      const int64_t row = in ? (plan.order ? plan.order[at] : at) : 0;
-      w[k] = E8::load(q.z.p, row * q.z.ld + c, in ? (whole ? 8 : most) : 0);
-#pragma unroll
-      for (int a = 0; a < CT; a++) {
-        const int j = j0 + a * 16 + i;
-        x[a][k] = in && j < pick.rank ? q.t[row * pick.rank + j] * s : 0.f;
-      }
+    for (int k = 0; k < NZ; k++) {
+      const int at = b + zr + k * (OW * 64 / (OCOLS / 8)), c = c0 + zc * 8;
+      const int64_t row = plan.order ? plan.order[min(at, h.end - 1)] : min(at, h.end - 1);
+      z[k] = whole ? E8::load(q.z.p, row * q.z.ld + c) : E8::load(q.z.p, row * q.z.ld + c, q.C - c);
+      if (at >= h.end) z[k] = typename E8::type{};
     }
-    if constexpr (F32) {
+    const int at = b + tr;
+    const float* from = q.t + (int64_t)(plan.order ? plan.order[min(at, h.end - 1)] : min(at, h.end - 1)) * pick.rank;
 #pragma unroll
-      for (int k = 0; k < E; k++) {
-        float col[8];
-        E8::values(w[k], col);
+    for (int k = 0; k < NT; k++) {
+      const int j = j0 + (tq + k * TPR) * 4;
+      t_values<4>(from, j, pick.rank, t[k]);
 #pragma unroll
-        for (int a = 0; a < CT; a++)
-#pragma unroll
-          for (int t = 0; t < 8; t++) acc[a][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[a][k], col[t], acc[a][t], 0, 0, 0);
-      }
-    } else {
-      u32x4 cols[8];
-      turned(w, cols);
-#pragma unroll
-      for (int a = 0; a < CT; a++) {
-        u32x4 p[PIECES];
-        pieces<PIECES>(x[a], p);
-#pragma unroll
-        for (int k = PIECES - 1; k >= 0; k--)
-#pragma unroll
-          for (int t = 0; t < 8; t++) acc[a][t] = Num<false>::mma(p[k], cols[t], acc[a][t]);
-      }
+      for (int e = 0; e < 4; e++) t[k][e] = at < h.end ? t[k][e] * s : 0.f;
     }
-  }
-  auto each = [&](auto f) {
-#pragma unroll
-    for (int a = 0; a < CT; a++)
-#pragma unroll
-      for (int t = 0; t < 8; t++)
-#pragma unroll
-        for (int d = 0; d < 4; d++) acc[a][t][d] = f(((a * 8 + t) * 4 + d) * 64 + lane, acc[a][t][d]);
   };
-#pragma unroll
-  for (int half = OW / 2; half > 0; half /= 2) {
-    __syncthreads();
-    if (wave >= half && wave < 2 * half) each([&](int at, float v) { return sums[wave - half][at] = v; });
-    __syncthreads();
-    if (wave < half) each([&](int at, float v) { return v + sums[wave][at]; });
-  }
-  if (wave > 0 || most <= 0) return;
+  v4f acc[CT][2];
 #pragma unroll
   for (int a = 0; a < CT; a++)
 #pragma unroll
-    for (int d = 0; d < 4; d++) {
-      const int j = j0 + a * 16 + g * 4 + d;
-      if (j < pick.rank) {
-        float v[8];
+    for (int c = 0; c < 2; c++) acc[a][c] = v4f{0, 0, 0, 0};
+  fetch(h.begin);
+  int buffer = 0;
+  for (int b = h.begin; b < h.end; b += S::ROWS, buffer ^= 1) {      // (one barrier a stage: who is past it has left the other buffer)
 #pragma unroll
-        for (int t = 0; t < 8; t++) v[t] = acc[a][t][d];
-        put_f32(q.part + ((int64_t)chunk * pick.rank + j) * q.C + c, v, most);
+    for (int k = 0; k < NZ; k++) S::put_z(lds[buffer], zr + k * (OW * 64 / (OCOLS / 8)), zc, z[k]);
+#pragma unroll
+    for (int k = 0; k < NT; k++)
+      if ((tq + k * TPR) * 4 < CT * 16) S::put_t(lds[buffer], tr, (tq + k * TPR) * 4, t[k]);
+    __syncthreads();
+    if (b + S::ROWS < h.end) fetch(b + S::ROWS);
+    S::multiply(lds[buffer], wave, lane, acc);
+  }
+#pragma unroll
+  for (int a = 0; a < CT; a++)
+#pragma unroll
+    for (int c = 0; c < 2; c++)
+#pragma unroll
+      for (int d = 0; d < 4; d++) {
+        const int j = j0 + a * 16 + (lane >> 4) * 4 + d, col = c0 + wave * 32 + c * 16 + (lane & 15);
+        if (j < pick.rank && col < q.C) q.part[((int64_t)chunk * pick.rank + j) * q.C + col] = acc[a][c][d];
       }
-    }
 }
 // The chunks' sums of an adapter's component, added in order; zeros for what has no rows.
 __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ part, Plan plan, Pick pick, int C, void* out, int f32) {
@@ -585,7 +709,7 @@ Deal deal(int64_t n, int64_t K, int count, int rank, bool f32, bool index) {
   d.ct = rank <= 16 ? 1 : rank <= 32 ? 2 : 4;
   d.tiles = up(n, 16 * d.rt);
   d.slots = index ? (int)std::max<int64_t>(1, std::min<int64_t>({256 / d.tiles, 16 * d.rt, n, count})) : 1;
-  const int64_t turns = up(K, f32 ? 32 : d.rt * d.ct >= 4 ? 64 : 128), blocks = d.tiles * d.slots * up(rank, 16 * d.ct);
+  const int64_t turns = up(K, f32 ? 32 : d.rt * d.ct > 4 ? 64 : 128), blocks = d.tiles * d.slots * up(rank, 16 * d.ct);
   d.parts = (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(blocks, 1), up(turns, CW), 8}));
   return d;
 }
@@ -605,18 +729,21 @@ void contract(const Contract& all, const Pick& pick, const Deal& d, hipStream_t 
 }
 template <bool F32>
 void expand(const Expand& q, const Pick& pick, hipStream_t s) {
-  const int rt = q.n <= 16 ? 1 : 2;
-  const int64_t tiles = up(q.n, 16 * rt), blocks = up(q.C, EW * ECOLS);
+  const int64_t blocks = up(q.C, EW * ECOLS);
   Expand a = q;
-  a.slots = pick.index ? (int)std::max<int64_t>(1, std::min<int64_t>({1024 / (tiles * blocks), 16 * rt, q.n, pick.count})) : 1;
+  a.subs = 4;
+  while (a.subs > 1 && (up(q.n, a.subs * 16) * blocks < 1024 || q.n <= a.subs * 8)) a.subs /= 2;
+  const int64_t tiles = up(q.n, 16 * a.subs);
+  a.slots = pick.index ? (int)std::max<int64_t>(1, std::min<int64_t>({4096 / (tiles * blocks), 16 * a.subs, q.n, pick.count})) : 1;
   const dim3 grid((unsigned)(tiles * blocks), (unsigned)a.slots), block(EW * 64);
-  if (rt == 1) hipLaunchKernelGGL((expand_kernel<F32, 1>), grid, block, 0, s, a, pick);
-  else hipLaunchKernelGGL((expand_kernel<F32, 2>), grid, block, 0, s, a, pick);
+  if (pick.rank <= Columns<F32>::STEP) hipLaunchKernelGGL((expand_kernel<F32, 1>), grid, block, 0, s, a, pick);
+  else if (pick.rank <= 2 * Columns<F32>::STEP) hipLaunchKernelGGL((expand_kernel<F32, 2>), grid, block, 0, s, a, pick);
+  else hipLaunchKernelGGL((expand_kernel<F32, 0>), grid, block, 0, s, a, pick);
 }
 template <bool F32, int PIECES>
 void outer(const Outer& q, const Plan& plan, const Pick& pick, int64_t chunks, hipStream_t s) {
   const int ct = pick.rank <= 16 ? 1 : pick.rank <= 32 ? 2 : 4;
-  const dim3 grid((unsigned)up(q.C, 128), (unsigned)chunks, (unsigned)up(pick.rank, 16 * ct)), block(OW * 64);
+  const dim3 grid((unsigned)up(q.C, OCOLS), (unsigned)chunks, (unsigned)up(pick.rank, 16 * ct)), block(OW * 64);
   if (ct == 1) hipLaunchKernelGGL((outer_kernel<F32, 1, PIECES>), grid, block, 0, s, q, plan, pick);
   else if (ct == 2) hipLaunchKernelGGL((outer_kernel<F32, 2, PIECES>), grid, block, 0, s, q, plan, pick);
   else hipLaunchKernelGGL((outer_kernel<F32, 4, PIECES>), grid, block, 0, s, q, plan, pick);
@@ -631,7 +758,13 @@ void outer_of(const Outer& q, const Plan& plan, const Pick& pick, int64_t chunks
   hipLaunchKernelGGL(join_kernel, dim3((unsigned)up(q.C, 2048), (unsigned)std::min<int64_t>(rows, 65535)), dim3(256), 0, s, q.part, plan, pick, q.C, out, out_dtype == OSSCAR_F32);
 }
 
-int64_t chunks_of(const osscar_adapters_desc& d, bool index) { return index ? up(d.n, CHUNK) + std::min<int64_t>(d.n, d.count) : up(d.n, CHUNK); }
+// Rows of a chunk: as many as leave two workgroups per compute unit, 128 to 512 (their sums are written and read again: 4 rank bytes per 2 rows of bf16).
+int chunk_of(const osscar_adapters_desc& d) {
+  int chunk = 512;
+  while (chunk > 128 && up(d.n, chunk) * up(std::min(d.d, d.m), OCOLS) * up(d.rank, 64) < 512) chunk /= 2;
+  return chunk;
+}
+int64_t chunks_of(const osscar_adapters_desc& d) { return up(d.n, chunk_of(d)) + (d.index ? std::min<int64_t>(d.n, d.count) : 0); }
 
 const char* bad_desc(const osscar_adapters_desc* d) {
   if (!d) return "osscar_adapters: NULL description";
@@ -662,7 +795,7 @@ extern "C" size_t osscar_adapters_workspace_bytes(const osscar_adapters_desc* d,
     c.take(t_bytes(*d, deal(std::max<int64_t>(d->n, 1), d->m, d->count, d->rank, f32, d->index != 0).parts));      // dT in parts
     c.take(t_bytes(*d, 1));                                                      // dT
     c.take(t_bytes(*d, 1));                                                      // T, where it is not given
-    const int64_t chunks = chunks_of(*d, d->index != 0);
+    const int64_t chunks = chunks_of(*d);
     if (d->index) {
       c.take((size_t)d->n * 4);
       c.take((size_t)chunks * sizeof(Chunk));
@@ -697,7 +830,7 @@ extern "C" osscar_status osscar_adapters_forward(const osscar_adapters_desc* d, 
   const bool direct = T_dev && deal1.parts == 1;
   if (direct) t = T_dev;
   const Contract k{Mat{X_dev, d->ldx}, Adapters{A_dev, d->lda, d->next_a}, d->n, (int)d->d, deal1.parts, deal1.slots, 0, t};
-  const Expand x{t, deal1.parts, 1, 1, Adapters{B_dev, d->ldb, d->next_b}, Mat{base_dev, ldbase}, d->n, (int)d->m, Y_dev, ldy, direct ? nullptr : T_dev};
+  const Expand x{t, deal1.parts, 1, 1, 1, Adapters{B_dev, d->ldb, d->next_b}, Mat{base_dev, ldbase}, d->n, (int)d->m, Y_dev, ldy, direct ? nullptr : T_dev};
   if (f32) {
     contract<true>(k, pick, deal1, s);
     expand<true>(x, pick, s);
@@ -731,7 +864,7 @@ extern "C" osscar_status osscar_adapters_backward(const osscar_adapters_desc* d,
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   const bool f32 = d->dtype == OSSCAR_F32, index = d->index != 0;
   const Pick pick{index_dev, scale_dev, ranks_dev, d->count, d->rank};
-  const int64_t chunks = chunks_of(*d, index);
+  const int64_t chunks = chunks_of(*d);
   Deal dy = deal(std::max<int64_t>(d->n, 1), d->m, d->count, d->rank, f32, index), dx = deal(std::max<int64_t>(d->n, 1), d->d, d->count, d->rank, f32, index);
   Carve c(workspace_dev);
   float* dt_parts = reinterpret_cast<float*>(c.take(t_bytes(*d, dy.parts)));
@@ -754,7 +887,7 @@ extern "C" osscar_status osscar_adapters_backward(const osscar_adapters_desc* d,
     if (f32) contract<true>(k, pick, dy, s);
     else contract<false>(k, pick, dy, s);
     if (dX_dev) {
-      const Expand x{dt_parts, dy.parts, 1, 0, Adapters{A_dev, d->lda, d->next_a}, Mat{base_dev, ldbase}, d->n, (int)d->d, dX_dev, lddx, dy.parts > 1 ? dt : nullptr};
+      const Expand x{dt_parts, dy.parts, 1, 0, 1, Adapters{A_dev, d->lda, d->next_a}, Mat{base_dev, ldbase}, d->n, (int)d->d, dX_dev, lddx, dy.parts > 1 ? dt : nullptr};
       if (f32) expand<true>(x, pick, s);
       else expand<false>(x, pick, s);
     }
@@ -768,11 +901,11 @@ extern "C" osscar_status osscar_adapters_backward(const osscar_adapters_desc* d,
     }
     if (index) {
       const int waves = (int)std::min<int64_t>({16, PLAN_WORDS / d->count, up(d->n, 64)});
-      hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(1024), 0, s, pick, (int)d->n, waves, order, table, first);
+      hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(1024), 0, s, pick, (int)d->n, waves, (uint32_t)chunk_of(*d), order, table, first);
     }
   }
   const bool listed = index && d->n > 0;
-  const Plan plan{listed ? order : nullptr, table, first, d->n, listed ? 0 : (int)chunks};
+  const Plan plan{listed ? order : nullptr, table, first, d->n, listed ? 0 : (int)chunks, chunk_of(*d)};
   const int64_t some = d->n > 0 ? chunks : 0;
   outer_of(Outer{dt, Mat{X_dev, d->ldx}, (int)d->d, 0, part}, plan, pick, some, f32, dw_dtype, dA_dev, s);
   outer_of(Outer{T_dev, Mat{dY_dev, lddy}, (int)d->m, 1, part}, plan, pick, some, f32, dw_dtype, dB_dev, s);
