@@ -85,7 +85,8 @@ __device__ __forceinline__ u32x4 packet_some(const char* row, int k, int K) {   
 // contract
 // --------------------------------------------------------------------------------------------------
 // A workgroup takes 16 RT rows and 16 CT components; its waves take the contraction in turns, parts of it are a workgroup's each (their sums are added where T is
-// read).  Operands go from memory to registers; the next turn's are on their way while one is multiplied.
+// read).  Operands go from memory to registers, the next turn's while one is multiplied.  The instruction wants 64 bytes of each of 16 rows in a packet of its lanes, which memory
+// answers in requests of 64 bytes: rows of Z are fetched 128 or 256 bytes at a time and change lanes through LDS, a piece of it for every wave (8192 x 14336, rank 32: 83 us without, 72 with).
 struct Contract {
   Mat z;
   Adapters v;
@@ -94,11 +95,15 @@ struct Contract {
   float* t;                         // [part][n][rank]
 };
 constexpr int CW = 8;      // waves
+constexpr int turn_of(bool f32, int rt, int ct) { return f32 || rt * ct > 4 ? 2 : 4; }      // instructions' worth of a row in a turn
 template <bool F32, int RT, int CT>
 __global__ __launch_bounds__(CW * 64) void contract_kernel(Contract q, Pick pick) {
   typedef Num<F32> N;
-  constexpr int U = F32 ? 2 : RT * CT > 4 ? 2 : 4, TURN = U * N::STEP, ROWS = RT * 16, COLS = CT * 16;
-  __shared__ float sums[CW / 2][ROWS * (COLS + 1)];
+  constexpr int U = turn_of(F32, RT, CT), TURN = U * N::STEP, ROWS = RT * 16, COLS = CT * 16;
+  constexpr int NC = U * 4, PER = 64 / NC, ROW = NC * 16;      // packets of a row in a turn, rows of one load, bytes of a row
+  constexpr int SUMS = CW / 2 * ROWS * (COLS + 1) * 4, TURNS = CW * ROWS * ROW;
+  __shared__ __align__(16) char lds[SUMS > TURNS ? SUMS : TURNS];
+  float(*sums)[ROWS * (COLS + 1)] = reinterpret_cast<float(*)[ROWS * (COLS + 1)]>(lds);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
   const int64_t tiles = (q.n + ROWS - 1) / ROWS, row0 = (blockIdx.x % tiles) * ROWS;
   const int slot = (int)(blockIdx.x / tiles), part = blockIdx.y, j0 = blockIdx.z * COLS;
@@ -114,12 +119,16 @@ __global__ __launch_bounds__(CW * 64) void contract_kernel(Contract q, Pick pick
   }
   each_adapter(mine, slot, q.slots, [&](int e, uint64_t rows) {
     const int rank = pick.rank_of(e), first = __ffsll((unsigned long long)rows) - 1;
-    const char *zr[RT], *vr[CT];
+    const char *zr[RT][U], *vr[CT];
 #pragma unroll
-    for (int r = 0; r < RT; r++) {      // (rows of other adapters: one of this one's again, not used)
-      const int at = rows >> (r * 16 + i) & 1 ? r * 16 + i : first;
-      zr[r] = reinterpret_cast<const char*>(q.z.p) + (row0 + at) * q.z.ld * N::ES;
-    }
+    for (int r = 0; r < RT; r++)
+#pragma unroll
+      for (int u = 0; u < U; u++) {      // (rows of other adapters: one of this one's again, not used)
+        const int row = r * 16 + u * PER + lane / NC, at = rows >> row & 1 ? row : first;
+        zr[r][u] = reinterpret_cast<const char*>(q.z.p) + (row0 + at) * q.z.ld * N::ES;
+      }
+    const int zk = lane % NC * N::E;
+    char* mine_lds = lds + wave * ROWS * ROW;
 #pragma unroll
     for (int c = 0; c < CT; c++) vr[c] = reinterpret_cast<const char*>(q.v.p) + (e * q.v.next + (int64_t)std::max(0, std::min(j0 + c * 16 + i, rank - 1)) * q.v.ld) * N::ES;
     struct Regs { u32x4 z[RT][U], v[CT][U]; };
@@ -129,7 +138,7 @@ __global__ __launch_bounds__(CW * 64) void contract_kernel(Contract q, Pick pick
         for (int u = 0; u < U; u++) {
           const int k = k0 + u * N::STEP + g * N::E;
 #pragma unroll
-          for (int r = 0; r < RT; r++) w.z[r][u] = packet<F32>(zr[r], k);
+          for (int r = 0; r < RT; r++) w.z[r][u] = packet<F32>(zr[r][u], k0 + zk);
 #pragma unroll
           for (int c = 0; c < CT; c++) w.v[c][u] = packet<F32>(vr[c], k);
         }
@@ -138,7 +147,7 @@ __global__ __launch_bounds__(CW * 64) void contract_kernel(Contract q, Pick pick
         for (int u = 0; u < U; u++) {
           const int k = k0 + u * N::STEP + g * N::E;
 #pragma unroll
-          for (int r = 0; r < RT; r++) w.z[r][u] = packet_some<F32>(zr[r], k, q.K);
+          for (int r = 0; r < RT; r++) w.z[r][u] = packet_some<F32>(zr[r][u], k0 + zk, q.K);
 #pragma unroll
           for (int c = 0; c < CT; c++) w.v[c][u] = packet_some<F32>(vr[c], k, q.K);
         }
@@ -149,13 +158,24 @@ __global__ __launch_bounds__(CW * 64) void contract_kernel(Contract q, Pick pick
     for (int r = 0; r < RT; r++)
 #pragma unroll
       for (int c = 0; c < CT; c++) acc[r][c] = v4f{0, 0, 0, 0};
-    auto multiply = [&](const Regs& w) {
+    auto multiply = [&](const Regs& w) {      // (packets of a row change places, so that the lanes of one access meet the banks evenly)
+#pragma unroll
+      for (int r = 0; r < RT; r++)
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+          const int row = u * PER + lane / NC;
+          *reinterpret_cast<u32x4*>(mine_lds + (r * 16 + row) * ROW + ((lane % NC) ^ (row & (NC - 1))) * 16) = w.z[r][u];
+        }
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int u = 0; u < U; u++)
 #pragma unroll
-        for (int r = 0; r < RT; r++)
+        for (int r = 0; r < RT; r++) {
+          const u32x4 z = *reinterpret_cast<const u32x4*>(mine_lds + (r * 16 + i) * ROW + ((u * 4 + g) ^ (i & (NC - 1))) * 16);
 #pragma unroll
-          for (int c = 0; c < CT; c++) acc[r][c] = N::mma(w.z[r][u], w.v[c][u], acc[r][c]);
+          for (int c = 0; c < CT; c++) acc[r][c] = N::mma(z, w.v[c][u], acc[r][c]);
+        }
+      __builtin_amdgcn_wave_barrier();
     };
     const int turns = (q.K + TURN - 1) / TURN, per = (turns + q.parts - 1) / q.parts;
     const int begin = part * per + wave, end = std::min(turns, (part + 1) * per);
@@ -617,16 +637,19 @@ struct Stage<true, CT, PIECES> {
     }
   }
 };
+struct Outers { Outer a, b; int blocks_a; };      // dA and dB in one launch: that many column blocks are of dA
 template <bool F32, int CT, int PIECES>
-__global__ __launch_bounds__(OW * 64) void outer_kernel(Outer q, Plan plan, Pick pick) {
+__global__ __launch_bounds__(OW * 64) void outer_kernel(Outers both, Plan plan, Pick pick) {
   typedef Eight<F32> E8;
   typedef Stage<F32, CT, PIECES> S;
   constexpr int NZ = S::ROWS * (OCOLS / 8) / (OW * 64), TPR = OW * 64 / S::ROWS, NT = CT * 16 / (TPR * 4) > 0 ? CT * 16 / (TPR * 4) : 1;      // packets of Z, quads of T a thread
-  __shared__ __align__(16) char lds[2][S::BYTES];
+  __shared__ __align__(16) char lds[S::BYTES];
   const int chunk = blockIdx.y;
   if (chunk >= plan.all(pick.count)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int c0 = blockIdx.x * OCOLS, j0 = blockIdx.z * CT * 16;
+  const bool first = (int)blockIdx.x < both.blocks_a;
+  const Outer q = first ? both.a : both.b;
+  const int c0 = ((int)blockIdx.x - (first ? 0 : both.blocks_a)) * OCOLS, j0 = blockIdx.z * CT * 16;
   const bool whole = c0 + OCOLS <= q.C;
   const Chunk h = plan.at(chunk);
   const float s = q.scaled ? pick.scale_of(h.e) : 1.f;
@@ -657,16 +680,16 @@ __global__ __launch_bounds__(OW * 64) void outer_kernel(Outer q, Plan plan, Pick
 #pragma unroll
     for (int c = 0; c < 2; c++) acc[a][c] = v4f{0, 0, 0, 0};
   fetch(h.begin);
-  int buffer = 0;
-  for (int b = h.begin; b < h.end; b += S::ROWS, buffer ^= 1) {      // (one barrier a stage: who is past it has left the other buffer)
+  for (int b = h.begin; b < h.end; b += S::ROWS) {      // (two buffers and one barrier a stage leave fewer workgroups on a compute unit: 62 and 92 us instead of 39 and 74)
 #pragma unroll
-    for (int k = 0; k < NZ; k++) S::put_z(lds[buffer], zr + k * (OW * 64 / (OCOLS / 8)), zc, z[k]);
+    for (int k = 0; k < NZ; k++) S::put_z(lds, zr + k * (OW * 64 / (OCOLS / 8)), zc, z[k]);
 #pragma unroll
     for (int k = 0; k < NT; k++)
-      if ((tq + k * TPR) * 4 < CT * 16) S::put_t(lds[buffer], tr, (tq + k * TPR) * 4, t[k]);
+      if ((tq + k * TPR) * 4 < CT * 16) S::put_t(lds, tr, (tq + k * TPR) * 4, t[k]);
     __syncthreads();
     if (b + S::ROWS < h.end) fetch(b + S::ROWS);
-    S::multiply(lds[buffer], wave, lane, acc);
+    S::multiply(lds, wave, lane, acc);
+    __syncthreads();
   }
 #pragma unroll
   for (int a = 0; a < CT; a++)
@@ -679,21 +702,29 @@ __global__ __launch_bounds__(OW * 64) void outer_kernel(Outer q, Plan plan, Pick
       }
 }
 // The chunks' sums of an adapter's component, added in order; zeros for what has no rows.
-__global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ part, Plan plan, Pick pick, int C, void* out, int f32) {
+struct Join { const float* part; int C; void* out; };
+__global__ __launch_bounds__(256) void join_kernel(Join a, Join b, int blocks_a, Plan plan, Pick pick, int f32) {
   const int64_t rows = (int64_t)pick.count * pick.rank;
+  const bool first_half = (int)blockIdx.x < blocks_a;
+  const Join q = first_half ? a : b;
+  const int c = (((int)blockIdx.x - (first_half ? 0 : blocks_a)) * 256 + threadIdx.x) * 4;
+  if (c >= q.C) return;
   for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
     const int e = (int)(row / pick.rank), j = (int)(row % pick.rank), first = plan.first_of(e), chunks = j < pick.rank_of(e) ? plan.chunks_of(e) : 0;
-    const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
-    if (c >= C) return;
-    float s[8] = {};
+    float s[4] = {};
+#pragma unroll 4
     for (int k = 0; k < chunks; k++) {
-      float v[8];
-      get_values(part, ((int64_t)(first + k) * pick.rank + j) * C + c, 1, v, C - c);
+      float v[4];
+      t_values<4>(q.part + ((int64_t)(first + k) * pick.rank + j) * q.C, c, q.C, v);
 #pragma unroll
-      for (int t = 0; t < 8; t++) s[t] += v[t];
+      for (int t = 0; t < 4; t++) s[t] += v[t];
     }
-    if (f32) put_f32(reinterpret_cast<float*>(out) + row * C + c, s, C - c);
-    else put_bf16(reinterpret_cast<uint16_t*>(out) + row * C + c, s, C - c);
+#pragma unroll
+    for (int t = 0; t < 4; t++)
+      if (c + t < q.C) {
+        if (f32) reinterpret_cast<float*>(q.out)[row * q.C + c + t] = s[t];
+        else reinterpret_cast<uint16_t*>(q.out)[row * q.C + c + t] = bf16_nearest(s[t]);
+      }
   }
 }
 
@@ -705,12 +736,12 @@ int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 struct Deal { int rt, ct, parts, slots; int64_t tiles; };
 Deal deal(int64_t n, int64_t K, int count, int rank, bool f32, bool index) {
   Deal d;
-  d.rt = n <= 16 ? 1 : 2;
+  d.rt = n <= 16 ? 1 : 2;      // (64 rows, whose sums and operands do not fit the registers: 75 us instead of 73 at rank 32, 62 instead of 28 at rank 64)
   d.ct = rank <= 16 ? 1 : rank <= 32 ? 2 : 4;
   d.tiles = up(n, 16 * d.rt);
   d.slots = index ? (int)std::max<int64_t>(1, std::min<int64_t>({256 / d.tiles, 16 * d.rt, n, count})) : 1;
-  const int64_t turns = up(K, f32 ? 32 : d.rt * d.ct > 4 ? 64 : 128), blocks = d.tiles * d.slots * up(rank, 16 * d.ct);
-  d.parts = (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(blocks, 1), up(turns, CW), 8}));
+  const int64_t turns = up(K, turn_of(f32, d.rt, d.ct) * (f32 ? 16 : 32)), blocks = d.tiles * d.slots * up(rank, 16 * d.ct);
+  d.parts = (int)std::max<int64_t>(1, std::min<int64_t>({256 / std::max<int64_t>(blocks, 1), up(turns, CW), 8}));
   return d;
 }
 
@@ -741,21 +772,12 @@ void expand(const Expand& q, const Pick& pick, hipStream_t s) {
   else hipLaunchKernelGGL((expand_kernel<F32, 0>), grid, block, 0, s, a, pick);
 }
 template <bool F32, int PIECES>
-void outer(const Outer& q, const Plan& plan, const Pick& pick, int64_t chunks, hipStream_t s) {
+void outer(const Outers& q, const Plan& plan, const Pick& pick, int64_t chunks, hipStream_t s) {
   const int ct = pick.rank <= 16 ? 1 : pick.rank <= 32 ? 2 : 4;
-  const dim3 grid((unsigned)up(q.C, OCOLS), (unsigned)chunks, (unsigned)up(pick.rank, 16 * ct)), block(OW * 64);
+  const dim3 grid((unsigned)(q.blocks_a + up(q.b.C, OCOLS)), (unsigned)chunks, (unsigned)up(pick.rank, 16 * ct)), block(OW * 64);
   if (ct == 1) hipLaunchKernelGGL((outer_kernel<F32, 1, PIECES>), grid, block, 0, s, q, plan, pick);
   else if (ct == 2) hipLaunchKernelGGL((outer_kernel<F32, 2, PIECES>), grid, block, 0, s, q, plan, pick);
   else hipLaunchKernelGGL((outer_kernel<F32, 4, PIECES>), grid, block, 0, s, q, plan, pick);
-}
-void outer_of(const Outer& q, const Plan& plan, const Pick& pick, int64_t chunks, bool f32, int32_t out_dtype, void* out, hipStream_t s) {
-  if (chunks > 0) {
-    if (f32) outer<true, 1>(q, plan, pick, chunks, s);
-    else if (out_dtype == OSSCAR_F32) outer<false, 3>(q, plan, pick, chunks, s);
-    else outer<false, 2>(q, plan, pick, chunks, s);
-  }
-  const int64_t rows = (int64_t)pick.count * pick.rank;
-  hipLaunchKernelGGL(join_kernel, dim3((unsigned)up(q.C, 2048), (unsigned)std::min<int64_t>(rows, 65535)), dim3(256), 0, s, q.part, plan, pick, q.C, out, out_dtype == OSSCAR_F32);
 }
 
 // Rows of a chunk: as many as leave two workgroups per compute unit, 128 to 512 (their sums are written and read again: 4 rank bytes per 2 rows of bf16).
@@ -801,7 +823,8 @@ extern "C" size_t osscar_adapters_workspace_bytes(const osscar_adapters_desc* d,
       c.take((size_t)chunks * sizeof(Chunk));
       c.take((size_t)(d->count + 1) * 4);
     }
-    c.take((size_t)chunks * d->rank * std::max(d->d, d->m) * 4);
+    c.take((size_t)chunks * d->rank * d->d * 4);
+    c.take((size_t)chunks * d->rank * d->m * 4);
   }
   return c.used + 256;
 }
@@ -878,7 +901,8 @@ extern "C" osscar_status osscar_adapters_backward(const osscar_adapters_desc* d,
     table = reinterpret_cast<Chunk*>(c.take((size_t)chunks * sizeof(Chunk)));
     first = reinterpret_cast<int*>(c.take((size_t)(d->count + 1) * 4));
   }
-  float* part = reinterpret_cast<float*>(c.take((size_t)chunks * d->rank * std::max(d->d, d->m) * 4));
+  float* part_a = reinterpret_cast<float*>(c.take((size_t)chunks * d->rank * d->d * 4));
+  float* part_b = reinterpret_cast<float*>(c.take((size_t)chunks * d->rank * d->m * 4));
   if (c.used > 0 && (!workspace_dev || c.used > workspace_bytes)) return refuse_call(OSSCAR_ENOMEM, "osscar_adapters_backward: workspace too small");
   if (d->n > 0) {
     if (!dX_dev) dy.parts = 1;      // (the parts are added where dX is made)
@@ -906,8 +930,14 @@ extern "C" osscar_status osscar_adapters_backward(const osscar_adapters_desc* d,
   }
   const bool listed = index && d->n > 0;
   const Plan plan{listed ? order : nullptr, table, first, d->n, listed ? 0 : (int)chunks, chunk_of(*d)};
-  const int64_t some = d->n > 0 ? chunks : 0;
-  outer_of(Outer{dt, Mat{X_dev, d->ldx}, (int)d->d, 0, part}, plan, pick, some, f32, dw_dtype, dA_dev, s);
-  outer_of(Outer{T_dev, Mat{dY_dev, lddy}, (int)d->m, 1, part}, plan, pick, some, f32, dw_dtype, dB_dev, s);
+  const Outers both{Outer{dt, Mat{X_dev, d->ldx}, (int)d->d, 0, part_a}, Outer{T_dev, Mat{dY_dev, lddy}, (int)d->m, 1, part_b}, (int)up(d->d, OCOLS)};
+  if (d->n > 0) {
+    if (f32) outer<true, 1>(both, plan, pick, chunks, s);
+    else if (dw_dtype == OSSCAR_F32) outer<false, 3>(both, plan, pick, chunks, s);
+    else outer<false, 2>(both, plan, pick, chunks, s);
+  }
+  const int blocks_a = (int)up(d->d, 1024);
+  hipLaunchKernelGGL(join_kernel, dim3((unsigned)(blocks_a + up(d->m, 1024)), (unsigned)std::min<int64_t>((int64_t)d->count * d->rank, 65535)), dim3(256), 0, s,
+                     Join{part_a, (int)d->d, dA_dev}, Join{part_b, (int)d->m, dB_dev}, blocks_a, plan, pick, dw_dtype == OSSCAR_F32);
   return launched();
 }
