@@ -7,6 +7,7 @@
 // results of that adapter's rows kept.  All are bound by reading and writing Z, base and Y, or A and B where rows are few: 2 rank operations for each of their elements.
 #include "ops.h"
 #include <algorithm>
+#include <type_traits>
 
 using namespace osscar;
 
@@ -87,6 +88,7 @@ __device__ __forceinline__ u32x4 packet_some(const char* row, int k, int K) {   
 // A workgroup takes 16 RT rows and 16 CT components; its waves take the contraction in turns, parts of it are a workgroup's each (their sums are added where T is
 // read).  Operands go from memory to registers, the next turn's while one is multiplied.  The instruction wants 64 bytes of each of 16 rows in a packet of its lanes, which memory
 // answers in requests of 64 bytes: rows of Z are fetched 128 or 256 bytes at a time and change lanes through LDS, a piece of it for every wave (8192 x 14336, rank 32: 83 us without, 72 with).
+constexpr int FW = 4;      // waves of the kernel for few rows
 struct Contract {
   Mat z;
   Adapters v;
@@ -110,7 +112,7 @@ __global__ __launch_bounds__(CW * 64) void contract_kernel(Contract q, Pick pick
   const int have = (int)std::min<int64_t>(ROWS, q.n - row0);
   const int mine = lane < have ? pick.of(row0 + lane) : -1;
   float* t = q.t + (int64_t)part * q.n * pick.rank;
-  if (slot == 0) {      // rows without an adapter
+  if (slot == q.slots - 1) {      // rows without an adapter (by the slot that is likeliest to have none itself)
     const uint64_t none = __ballot(mine < 0);
     for (int k = threadIdx.x; k < have * COLS; k += CW * 64) {
       const int r = k / COLS, j = j0 + k % COLS;
@@ -267,7 +269,7 @@ struct Expand {
   int64_t ldy;
   float* t_out;        // the parts' sum, or NULL
 };
-constexpr int EW = 4, ECOLS = 128;      // waves, columns of each
+constexpr int EW = 4, ECOLS = 128, PARTS_MOST = 4;      // waves, columns of each; parts of T
 // The components j .. of eight columns from c, as the matrix instruction takes them; zeros from `rank` on.
 template <bool F32> struct Columns;
 template <> struct Columns<false> {
@@ -336,7 +338,7 @@ __device__ __forceinline__ void t_values(const float* t, int j, int rank, float 
 // A wave takes 128 columns of up to 64 rows, 16 at a time: lane (i, g) reads eight columns c0 + 8 i .. of components 8 g .. and turns them in its registers, so that
 // the instruction for tile t has columns c0 + 8 i + t; the results of a lane are then eight neighbouring columns of four rows.  The columns stay in registers for all rows of their
 // adapter (KS steps of components; 0: more than that, read again for each 16 rows), the next 16 rows' base and T are on their way while those before are multiplied.
-template <bool F32, int KS>
+template <bool F32, int KS, bool PARTS>
 __global__ __launch_bounds__(EW * 64, 2) void expand_kernel(Expand q, Pick pick) {
   typedef Eight<F32> E8;
   typedef Columns<F32> Cols;
@@ -350,17 +352,18 @@ __global__ __launch_bounds__(EW * 64, 2) void expand_kernel(Expand q, Pick pick)
   const int mine = lane < have ? pick.of(row0 + lane) : -1;
   const bool whole = c0 + ECOLS <= q.C, keeps = q.t_out && c0 == 0;
   constexpr size_t ES = F32 ? 4 : 2;
-  if (slot == 0) {      // rows without an adapter
+  if (slot == q.slots - 1) {      // rows without an adapter (by the slot that is likeliest to have none itself)
     uint64_t none = __ballot(mine < 0 && lane < have);
     const uint64_t wrong = __ballot(mine == -2);
     if (keeps)
       for (int k = lane; k < have * pick.rank; k += 64)
         if (none >> (k / pick.rank) & 1) q.t_out[row0 * pick.rank + k] = 0.f;
     if (q.y == q.base.p) none = wrong;
-    while (none) {
-      const int r = __ffsll((unsigned long long)none) - 1;
-      none &= none - 1;
-      if (g == 0 && most > 0) {
+    while (none) {      // four at a time, one for each group of lanes
+      int r = -1;
+      for (int k = 0; k < 4 && none; k++, none &= none - 1)
+        if (g == k) r = __ffsll((unsigned long long)none) - 1;
+      if (r >= 0 && most > 0) {
         float y[8];
         if (q.base.p) E8::values(E8::load(q.base.p, (row0 + r) * q.base.ld + c, most), y);
 #pragma unroll
@@ -398,12 +401,14 @@ __global__ __launch_bounds__(EW * 64, 2) void expand_kernel(Expand q, Pick pick)
     auto finish = [&](int sub, int j, float (&x)[E]) {
       const int row = sub * 16 + i;
       if (rows >> row & 1) {
-#pragma unroll 4
-        for (int p = 1; p < q.parts; p++) {
-          float more[E];
-          t_values<E>(q.t + ((int64_t)p * q.n + row0 + row) * pick.rank, j, pick.rank, more);
+        if constexpr (PARTS) {      // (all on their way together: few rows wait for each load)
+          float more[PARTS_MOST - 1][E];
 #pragma unroll
-          for (int k = 0; k < E; k++) x[k] += more[k];
+          for (int p = 1; p < PARTS_MOST; p++) t_values<E>(q.t + ((int64_t)std::min(p, q.parts - 1) * q.n + row0 + row) * pick.rank, j, pick.rank, more[p - 1]);
+#pragma unroll
+          for (int p = 1; p < PARTS_MOST; p++)
+#pragma unroll
+            for (int k = 0; k < E; k++) x[k] += p < q.parts ? more[p - 1][k] : 0.f;
         }
         if (keeps) {
 #pragma unroll
@@ -464,6 +469,134 @@ __global__ __launch_bounds__(EW * 64, 2) void expand_kernel(Expand q, Pick pick)
       sub = after;
     }
   });
+}
+
+// Few rows wait for one load after the other; these two kernels have few of them in a row, and read V once per row.  16 rows of any of 32 adapters of rank 16, 7168 x 14336: 10 us for both
+// (12 MB, 2.5 us at the rate of a copy), 9.4 with one row: two launches of 4 us, most of it waiting for index, operands and T one behind the other.
+// A workgroup takes 16 components of one row and a part of the contraction, a wave 512 numbers of it at a time.
+template <bool F32>
+__global__ __launch_bounds__(FW * 64) void contract_few_kernel(Contract q, Pick pick) {
+  typedef Eight<F32> E8;
+  constexpr size_t ES = F32 ? 4 : 2;
+  constexpr int SPAN = 512;
+  __shared__ float sums[FW][16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = blockIdx.x, j0 = blockIdx.z * 16;
+  const int64_t row = blockIdx.y;
+  const int e = pick.of(row), rank = e < 0 ? 0 : pick.rank_of(e);
+  const float s = e >= 0 && q.scaled ? pick.scale_of(e) : 1.f;
+  float acc[16];
+#pragma unroll
+  for (int j = 0; j < 16; j++) acc[j] = 0.f;
+  if (j0 < rank) {
+    const char* v = reinterpret_cast<const char*>(q.v.p) + (e * q.v.next + (int64_t)j0 * q.v.ld) * ES;
+    for (int b = (part * FW + wave) * SPAN; b < q.K; b += q.parts * FW * SPAN) {
+      const int k = b + lane * 8, most = q.K - k;
+      typename E8::type z, w[16];
+      if (b + SPAN <= q.K) {
+        z = E8::load(q.z.p, row * q.z.ld + k);
+#pragma unroll
+        for (int j = 0; j < 16; j++) w[j] = E8::load(v, std::min(j, rank - 1 - j0) * q.v.ld + k);
+      } else {
+        z = E8::load(q.z.p, row * q.z.ld + k, most);
+#pragma unroll
+        for (int j = 0; j < 16; j++) w[j] = E8::load(v, std::min(j, rank - 1 - j0) * q.v.ld + k, most);
+      }
+      float x[8];
+      E8::values(z, x);
+#pragma unroll
+      for (int j = 0; j < 16; j++) {
+        float y[8];
+        E8::values(w[j], y);
+#pragma unroll
+        for (int d = 0; d < 8; d++) acc[j] = fmaf(x[d], y[d], acc[j]);
+      }
+    }
+  }
+  // sums over the lanes: in each step a lane keeps half of its numbers and gets its partner's share of them
+#pragma unroll
+  for (int half = 8; half > 0; half /= 2) {
+    const int o = half * 4;      // partners 32, 16, 8, 4 lanes away
+    const bool upper = lane & o;
+#pragma unroll
+    for (int j = 0; j < half; j++) {
+      const float mine = upper ? acc[j + half] : acc[j], other = upper ? acc[j] : acc[j + half];
+      acc[j] = mine + __shfl_xor(other, o, 64);
+    }
+  }
+  acc[0] += __shfl_xor(acc[0], 2, 64);
+  acc[0] += __shfl_xor(acc[0], 1, 64);
+  if ((lane & 3) == 0) sums[wave][lane >> 2] = acc[0];
+  __syncthreads();
+  const int j = j0 + threadIdx.x;
+  if (threadIdx.x < 16 && j < pick.rank) {
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < FW; w++) t += sums[w][threadIdx.x];
+    q.t[((int64_t)part * q.n + row) * pick.rank + j] = j < rank ? t * s : 0.f;
+  }
+}
+// A workgroup takes 512 columns of one row, its waves (one for each 16 components, up to four) the components in turns; a component's number goes to all lanes as a scalar.
+template <bool F32>
+__global__ __launch_bounds__(256) void expand_few_kernel(Expand q, Pick pick) {
+  typedef Eight<F32> E8;
+  constexpr size_t ES = F32 ? 4 : 2;
+  __shared__ __align__(16) float sums[3][64][8];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, c = (blockIdx.x * 64 + lane) * 8, most = q.C - c;
+  const bool whole = ((int)blockIdx.x + 1) * 512 <= q.C;
+  const int64_t row = blockIdx.y;
+  const int e = pick.of(row);
+  typename E8::type base{};
+  if (q.base.p && wave == 0) base = E8::load(q.base.p, row * q.base.ld + c, most);
+  const int rank = e < 0 ? 0 : pick.rank_of(e);
+  const float s = e >= 0 && q.scaled ? pick.scale_of(e) : 1.f;
+  const char* v = reinterpret_cast<const char*>(q.v.p) + std::max(e, 0) * q.v.next * ES;
+  float y[8];
+#pragma unroll
+  for (int t = 0; t < 8; t++) y[t] = 0.f;
+  for (int j0 = wave * 16; j0 < pick.rank; j0 += waves * 16) {
+    const int j = j0 + (lane & 15);
+    float t = 0.f, part[PARTS_MOST];
+    typename E8::type w[16];
+    if (j0 < rank) {
+#pragma unroll
+      for (int k = 0; k < 16; k++) w[k] = whole ? E8::load(v, std::min(j0 + k, rank - 1) * q.v.ld + c) : E8::load(v, std::min(j0 + k, rank - 1) * q.v.ld + c, most);
+#pragma unroll
+      for (int p = 0; p < PARTS_MOST; p++) part[p] = q.t[((int64_t)std::min(p, q.parts - 1) * q.n + row) * pick.rank + std::min(j, rank - 1)];
+#pragma unroll
+      for (int p = 0; p < PARTS_MOST; p++) t += p < q.parts && j < rank ? part[p] : 0.f;
+    }
+    if (q.t_out && blockIdx.x == 0 && lane < 16 && j < pick.rank) q.t_out[row * pick.rank + j] = t;
+    if (j0 >= rank) continue;
+    t *= s;
+#pragma unroll
+    for (int k = 0; k < 16; k++) {
+      if (j0 + k < rank) {
+        float x[8];
+        E8::values(w[k], x);
+        const float a = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(t), k));
+#pragma unroll
+        for (int d = 0; d < 8; d++) y[d] = fmaf(a, x[d], y[d]);
+      }
+    }
+  }
+  if (waves > 1) {
+    if (wave > 0) {
+#pragma unroll
+      for (int d = 0; d < 8; d++) sums[wave - 1][lane][d] = y[d];
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    for (int w = 1; w < waves; w++) {
+#pragma unroll
+      for (int d = 0; d < 8; d++) y[d] += sums[w - 1][lane][d];
+    }
+  }
+  if (most <= 0 || (e == -1 && q.y == q.base.p)) return;
+  float x[8];
+  E8::values(base, x);
+#pragma unroll
+  for (int t = 0; t < 8; t++) y[t] = e == -2 ? NAN : q.base.p ? x[t] + y[t] : y[t];
+  E8::store(q.y, row * q.ldy + c, y, most);
 }
 
 // --------------------------------------------------------------------------------------------------
@@ -732,21 +865,29 @@ __global__ __launch_bounds__(256) void join_kernel(Join a, Join b, int blocks_a,
 // host
 // --------------------------------------------------------------------------------------------------
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Rows that go through the kernels for few.  7168 x 14336 bf16, forward, these and the tiles: rows of 32 adapters, rank 16: 16 rows 10 and 13 us, 64 rows 12 and 25, 256 rows 24 and 52 (rank 64: 128 rows
+// 50 and 74); of two adapters, sorted: 128 rows 14 and 18 (rank 64: 35 and 35), 256 rows 21 and 24; without an index 64 rows 11 and 13 (20 and 23), 128 rows 14 and 14 (34 and 23).
+int64_t few_of(bool index) { return index ? 256 : 64; }
 // Row tiles of 16 in a workgroup, and how its work is dealt out: parts of the contraction and slots of adapters to fill the chip where rows are few.
 struct Deal { int rt, ct, parts, slots; int64_t tiles; };
 Deal deal(int64_t n, int64_t K, int count, int rank, bool f32, bool index) {
   Deal d;
+  if (n <= few_of(index)) return Deal{0, 0, (int)std::min<int64_t>(PARTS_MOST, up(K, FW * 512)), 1, n};
   d.rt = n <= 16 ? 1 : 2;      // (64 rows, whose sums and operands do not fit the registers: 75 us instead of 73 at rank 32, 62 instead of 28 at rank 64)
   d.ct = rank <= 16 ? 1 : rank <= 32 ? 2 : 4;
   d.tiles = up(n, 16 * d.rt);
   d.slots = index ? (int)std::max<int64_t>(1, std::min<int64_t>({256 / d.tiles, 16 * d.rt, n, count})) : 1;
   const int64_t turns = up(K, turn_of(f32, d.rt, d.ct) * (f32 ? 16 : 32)), blocks = d.tiles * d.slots * up(rank, 16 * d.ct);
-  d.parts = (int)std::max<int64_t>(1, std::min<int64_t>({256 / std::max<int64_t>(blocks, 1), up(turns, CW), 8}));
+  d.parts = (int)std::max<int64_t>(1, std::min<int64_t>({256 / std::max<int64_t>(blocks, 1), up(turns, 2 * CW), PARTS_MOST}));
   return d;
 }
 
 template <bool F32>
 void contract(const Contract& all, const Pick& pick, const Deal& d, hipStream_t s) {
+  if (d.rt == 0) {
+    hipLaunchKernelGGL(contract_few_kernel<F32>, dim3((unsigned)all.parts, (unsigned)all.n, (unsigned)up(pick.rank, 16)), dim3(FW * 64), 0, s, all, pick);
+    return;
+  }
   const dim3 grid((unsigned)(d.tiles * d.slots), (unsigned)d.parts, (unsigned)up(pick.rank, 16 * d.ct)), block(CW * 64);
   if (d.rt == 1) {
     if (d.ct == 1) hipLaunchKernelGGL((contract_kernel<F32, 1, 1>), grid, block, 0, s, all, pick);
@@ -760,16 +901,25 @@ void contract(const Contract& all, const Pick& pick, const Deal& d, hipStream_t 
 }
 template <bool F32>
 void expand(const Expand& q, const Pick& pick, hipStream_t s) {
+  if (q.n <= few_of(pick.index != nullptr)) {
+    hipLaunchKernelGGL(expand_few_kernel<F32>, dim3((unsigned)up(q.C, 512), (unsigned)q.n), dim3((unsigned)(64 * std::min<int64_t>(4, up(pick.rank, 16)))), 0, s, q, pick);
+    return;
+  }
   const int64_t blocks = up(q.C, EW * ECOLS);
   Expand a = q;
   a.subs = 4;
-  while (a.subs > 1 && (up(q.n, a.subs * 16) * blocks < 1024 || q.n <= a.subs * 8)) a.subs /= 2;
+  while (a.subs > 1 && (up(q.n, a.subs * 16) * blocks < 512 || q.n <= a.subs * 8)) a.subs /= 2;
   const int64_t tiles = up(q.n, 16 * a.subs);
   a.slots = pick.index ? (int)std::max<int64_t>(1, std::min<int64_t>({4096 / (tiles * blocks), 16 * a.subs, q.n, pick.count})) : 1;
   const dim3 grid((unsigned)(tiles * blocks), (unsigned)a.slots), block(EW * 64);
-  if (pick.rank <= Columns<F32>::STEP) hipLaunchKernelGGL((expand_kernel<F32, 1>), grid, block, 0, s, a, pick);
-  else if (pick.rank <= 2 * Columns<F32>::STEP) hipLaunchKernelGGL((expand_kernel<F32, 2>), grid, block, 0, s, a, pick);
-  else hipLaunchKernelGGL((expand_kernel<F32, 0>), grid, block, 0, s, a, pick);
+  auto go = [&](auto parts) {
+    constexpr bool PARTS = decltype(parts)::value;
+    if (pick.rank <= Columns<F32>::STEP) hipLaunchKernelGGL((expand_kernel<F32, 1, PARTS>), grid, block, 0, s, a, pick);
+    else if (pick.rank <= 2 * Columns<F32>::STEP) hipLaunchKernelGGL((expand_kernel<F32, 2, PARTS>), grid, block, 0, s, a, pick);
+    else hipLaunchKernelGGL((expand_kernel<F32, 0, PARTS>), grid, block, 0, s, a, pick);
+  };
+  if (a.parts > 1) go(std::true_type{});
+  else go(std::false_type{});
 }
 template <bool F32, int PIECES>
 void outer(const Outers& q, const Plan& plan, const Pick& pick, int64_t chunks, hipStream_t s) {

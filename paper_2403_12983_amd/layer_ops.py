@@ -57,9 +57,15 @@ def _on(index: int, /, **tensors: Optional[torch.Tensor]):
 
 
 def _vector(t: torch.Tensor, n: int, dtype: torch.dtype, what: str) -> int:
-    if t.dim() != 1 or t.shape[0] != n or t.dtype != dtype or (n > 1 and t.stride(0) != 1):
+    if t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous():
         _refuse(f"{what} must be a contiguous {dtype} vector of {n}")
     return t.data_ptr()
+
+
+def _vector_on(index: int, t: torch.Tensor, n: int, dtype: torch.dtype, what: str) -> int:
+    if t.get_device() != index:
+        _refuse(f"{what} is on {t.device}, expected cuda:{index}")
+    return _vector(t, n, dtype, what)
 
 
 def _begin(t: torch.Tensor, stream: Optional[torch.cuda.Stream]):
@@ -323,9 +329,9 @@ def _out(out: Optional[torch.Tensor], like: torch.Tensor, shape) -> torch.Tensor
     return out
 
 
-def _gains(w: Optional[torch.Tensor], d: int, what: str) -> Tuple[Optional[int], Optional[int]]:
+def _gains(index: int, w: Optional[torch.Tensor], d: int, what: str) -> Tuple[Optional[int], Optional[int]]:
     """(address, dtype) of a vector over the columns, or of none"""
-    return (None, None) if w is None else (_vector(w, d, w.dtype, what), _code(w, what))
+    return (None, None) if w is None else (_vector_on(index, w, d, w.dtype, what), _code(w, what))
 
 
 def osscar_layernorm_forward(X: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5, save: bool = False,
@@ -335,8 +341,9 @@ def osscar_layernorm_forward(X: torch.Tensor, weight: Optional[torch.Tensor] = N
     lib, index, handle, context = _begin(X, stream)
     code, ldx = _code(X, "X"), _ld(X, "X")
     n, d = X.shape
-    _on(index, weight=weight, bias=bias, out=out)
-    (wp, wc), (bp, bc) = _gains(weight, d, "weight"), _gains(bias, d, "bias")
+    if out is not None:
+        _on(index, out=out)
+    (wp, wc), (bp, bc) = _gains(index, weight, d, "weight"), _gains(index, bias, d, "bias")
     if wc is not None and bc is not None and wc != bc:
         _refuse("weight and bias have one dtype")
     with context:
@@ -359,8 +366,8 @@ def osscar_layernorm_backward(X: torch.Tensor, weight: Optional[torch.Tensor], d
         _refuse("dY has the shape and dtype of X")
     if stats.shape != (n, 2) or stats.dtype != torch.float32 or not stats.is_contiguous():
         _refuse("stats must be the n x 2 float32 tensor of osscar_layernorm_forward")
-    _on(index, weight=weight, dY=dY, stats=stats, out=out)
-    wp, wc = _gains(weight, d, "weight")
+    _on(index, dY=dY, stats=stats, out=out)
+    wp, wc = _gains(index, weight, d, "weight")
     wc = code if wc is None else wc
     if dw_dtype is None:
         dw_dtype = X.dtype if weight is None else weight.dtype
@@ -382,34 +389,37 @@ def osscar_layernorm_backward(X: torch.Tensor, weight: Optional[torch.Tensor], d
     return dX, dw, db
 
 
-def _components(t: torch.Tensor, what: str) -> Tuple[int, int]:
+def _components(t: torch.Tensor, count: int, rank: int, width: int, what: str) -> Tuple[int, int]:
     """(from one component to the next, from one adapter to the next) of adapters x components x width"""
-    if t.dim() != 3:
-        _refuse(f"{what} is adapters x rank x width")
-    count, rank, width = t.shape
-    if width > 1 and t.stride(2) != 1:
+    after, ld, one = t.stride()
+    if one != 1 and width > 1:
         _refuse(f"the components of {what} must be contiguous")
-    ld = t.stride(1) if rank > 1 else width
+    if rank <= 1:
+        ld = width
     if ld < width:
         _refuse(f"the components of {what} overlap")
-    return max(ld, 1), t.stride(0) if count > 1 else 0
+    return ld or 1, after if count > 1 else 0
 
 
 def _adapters(X, A, B, index, scale, ranks, at: int):
     """(description, addresses of X, A, B, index, scale, ranks)"""
-    code = _code(X, "X")
+    code, ldx = _code(X, "X"), _ld(X, "X")
     if A.dtype != X.dtype or B.dtype != X.dtype:
         _refuse("X, A and B have one dtype")
-    ldx, (lda, next_a), (ldb, next_b) = _ld(X, "X"), _components(A, "A"), _components(B, "B")
     n, d = X.shape
-    if A.shape[:2] != B.shape[:2] or A.shape[2] != d:
+    if A.dim() != 3 or B.dim() != 3:
+        _refuse("A and B are adapters x rank x width")
+    (count, rank, width), (b_count, b_rank, m) = A.shape, B.shape
+    if width != d or b_count != count or b_rank != rank:
         _refuse("A is adapters x rank x d, B adapters x rank x m")
-    _on(at, A=A, B=B, index=index, scale=scale, ranks=ranks)
-    count, rank = A.shape[:2]
-    ip = None if index is None else _vector(index, n, torch.int64, "index")
-    sp = None if scale is None else _vector(scale, count, torch.float32, "scale")
-    rp = None if ranks is None else _vector(ranks, count, torch.int32, "ranks")
-    return _AdaptersDesc(n, d, B.shape[2], ldx, lda, next_a, ldb, next_b, count, rank, code, 0 if index is None else 1), (X.data_ptr(), A.data_ptr(), B.data_ptr(), ip, sp, rp)
+    if A.get_device() != at or B.get_device() != at:
+        _on(at, A=A, B=B)
+    lda, next_a = _components(A, count, rank, d, "A")
+    ldb, next_b = _components(B, count, rank, m, "B")
+    ip = None if index is None else _vector_on(at, index, n, torch.int64, "index")
+    sp = None if scale is None else _vector_on(at, scale, count, torch.float32, "scale")
+    rp = None if ranks is None else _vector_on(at, ranks, count, torch.int32, "ranks")
+    return _AdaptersDesc(n, d, m, ldx, lda, next_a, ldb, next_b, count, rank, code, 0 if index is None else 1), (X.data_ptr(), A.data_ptr(), B.data_ptr(), ip, sp, rp)
 
 
 def osscar_adapters_forward(X: torch.Tensor, A: torch.Tensor, B: torch.Tensor, index: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
@@ -423,7 +433,8 @@ def osscar_adapters_forward(X: torch.Tensor, A: torch.Tensor, B: torch.Tensor, i
     n, m = desc.n, desc.m
     if base is not None and (base.shape != (n, m) or base.dtype != X.dtype):
         _refuse("base is n x m, of the dtype of X")
-    _on(at, base=base, out=out)
+    if base is not None or out is not None:
+        _on(at, base=base, out=out)
     with context:
         Y = _out(out, X, (n, m))
         T = _EMPTY(n, desc.rank, dtype=torch.float32, device=X.device) if save else None
