@@ -12,21 +12,22 @@ namespace {
 constexpr int BLOCK = OSSCAR_ADAMW_BLOCK;
 static_assert(BLOCK == 256, "32 threads of eight elements");
 constexpr int T = 256, CHUNK = T * 8;      // elements of a workgroup
-constexpr int TABLE_BYTES = 3600;          // of the kernel's arguments (4096 at most)
+constexpr int TABLE_BYTES = 3860;          // of the kernel's arguments (4096 at most)
 
 // The tensors of a launch, passed by value: nothing has to be copied to the device before, and a captured launch keeps its own.
-template <bool SMALL, bool MASTER>
+// NUMBERED: elements are rounded by chance, which goes by their number.
+template <bool SMALL, bool MASTER, bool NUMBERED>
 struct Table {
-  static constexpr int MOST = TABLE_BYTES / (6 * 8 + 4 + (SMALL ? 16 : 0) + (MASTER ? 8 : 0));
+  static constexpr int MOST = TABLE_BYTES / (5 * 8 + (NUMBERED ? 8 : 0) + (SMALL ? 16 : 0) + (MASTER ? 8 : 0));
   void* p[MOST];
   const void* g[MOST];
   void* m[MOST];
   void* v[MOST];
-  int64_t n[MOST];
-  int64_t first[MOST];               // number of the tensor's first block in the call
+  int64_t first[NUMBERED ? MOST : 1];      // number of the tensor's first block in the call
   float* m_scale[SMALL ? MOST : 1];
   float* v_scale[SMALL ? MOST : 1];
   float* master[MASTER ? MOST : 1];
+  uint32_t n[MOST];                  // (at most 2^30)
   uint32_t begin[MOST];              // its first workgroup
   int count;
 };
@@ -58,37 +59,65 @@ __device__ __forceinline__ uint32_t mix(uint32_t x) {
   x = (x ^ x >> 15) * 0xB7E15163u;
   return x ^ x >> 16;
 }
-// The bits of z > 0 without its last BITS: to the nearest, halves to even, or up by chance.
-template <int BITS>
-__device__ __forceinline__ uint32_t keep(float z, bool random, uint32_t h) {
+// The bits of z > 0 without its last BITS: to the nearest, halves to even, or (RANDOM) up by chance.
+template <int BITS, bool RANDOM>
+__device__ __forceinline__ uint32_t keep(float z, uint32_t h) {
   const uint32_t u = __float_as_uint(z);
-  return (u + (random ? h : (1u << (BITS - 1)) - 1 + (u >> BITS & 1))) >> BITS;
+  return (u + (RANDOM ? h : (1u << (BITS - 1)) - 1 + (u >> BITS & 1))) >> BITS;
 }
-struct Unit { float scale, inverse; bool number; };
-// The power of two 2^BELOW under the largest power of two in `most` >= 0.
+struct Unit { float scale, inverse; };
+// The power of two that is 2^BELOW under the largest power of two in `most` >= 0; NaN and zero for what is not finite.
 template <int BELOW>
 __device__ __forceinline__ Unit unit_of(float most) {
   const int e = __float_as_int(most) >> 23, at = max(e - BELOW, 1);
-  return e == 255 ? Unit{NAN, 0.f, false} : Unit{__int_as_float(at << 23), __int_as_float((254 - at) << 23), true};
+  return e == 255 ? Unit{NAN, 0.f} : Unit{__int_as_float(at << 23), __int_as_float((254 - at) << 23)};
 }
-// m: sign, four bits of exponent, three of mantissa (the 8-bit float e4m3), 256 at most.  Below 2^-6 a sum with it has the step of its smallest normal numbers.
-__device__ __forceinline__ uint32_t code_m(float y, bool random, uint32_t h) {
-  const float a = fabsf(y);
-  const bool low = a < 0x1p-6f;
-  return (keep<20>(low ? a + 0x1p-6f : a, random, h & 0xFFFFF) - (low ? 121 * 8 : 120 * 8)) | (__float_as_uint(y) >> 24 & 128);
+typedef float v2f __attribute__((ext_vector_type(2)));
+// m: sign, four bits of exponent, three of mantissa (the 8-bit float e4m3, which the machine converts), 256 at most.  Rounded by chance: below 2^-6 a sum with it has the step of its smallest
+// normal numbers.
+template <bool RANDOM>
+__device__ __forceinline__ uint32_t codes_m(const float (&y)[4], const uint32_t* h) {
+  if constexpr (RANDOM) {
+    uint32_t c[4];
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+      const bool low = fabsf(y[e]) < 0x1p-6f;
+      const uint32_t k = keep<20, true>(fabsf(y[e]) + (low ? 0x1p-6f : 0.f), h[e] & 0xFFFFF) - (low ? 121 * 8 : 120 * 8);
+      c[e] = k | (__float_as_uint(y[e]) >> 24 & 128);
+    }
+    return c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
+  } else {
+    int c = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], c, true);
+  }
 }
-__device__ __forceinline__ float value_m(uint32_t c) {
-  const uint32_t a = c & 127;
-  const float x = a < 8 ? a * 0x1p-9f : __uint_as_float((a + 120 * 8) << 20);
-  return __uint_as_float((a == 127 ? 0x7FC00000u : __float_as_uint(x)) | (c & 128) << 24);
+__device__ __forceinline__ void values_m(uint32_t c, float (&m)[4]) {
+  const v2f a = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
+  m[0] = a[0];
+  m[1] = a[1];
+  m[2] = b[0];
+  m[3] = b[1];
 }
 // sqrt v: four bits of exponent, four of mantissa, whole numbers below 32; what is above zero stays there, so that no m is divided by a lost v.
-__device__ __forceinline__ uint32_t code_root(float y, bool some, bool random, uint32_t h) {
-  const bool low = y < 16.f;
-  const uint32_t c = keep<19>(low ? y + 16.f : y, random, (h * 0x9E3779B9u) >> 13) - (low ? 131 * 16 : 130 * 16);
-  return some && c == 0 ? 1 : c;
+template <bool RANDOM>
+__device__ __forceinline__ uint32_t codes_root(const float (&y)[4], const float (&root)[4], const uint32_t* h) {
+  uint32_t c[4];
+#pragma unroll
+  for (int e = 0; e < 4; e++) {
+    const bool low = y[e] < 16.f;
+    c[e] = keep<19, RANDOM>(y[e] + (low ? 16.f : 0.f), RANDOM ? (h[e] * 0x9E3779B9u) >> 13 : 0u) - (low ? 131 * 16 : 130 * 16);
+    c[e] = max(c[e], root[e] > 0.f ? 1u : 0u);
+  }
+  return c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
 }
-__device__ __forceinline__ float value_root(uint32_t c) { return c < 16 ? (float)c : __uint_as_float((c + 130 * 16) << 19); }
+__device__ __forceinline__ void values_root(uint32_t c, float (&r)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; e++) {
+    const uint32_t k = c >> (8 * e) & 255;
+    const bool low = k < 16;
+    r[e] = __uint_as_float((k + (low ? 131 * 16 : 130 * 16)) << 19) - (low ? 16.f : 0.f);
+  }
+}
 
 __device__ __forceinline__ float largest_of_32(float x) {      // NaN where one is: the largest of the bits of what is not negative
   uint32_t u = __float_as_uint(x);
@@ -96,22 +125,26 @@ __device__ __forceinline__ float largest_of_32(float x) {      // NaN where one 
   for (int o = 16; o > 0; o >>= 1) { const uint32_t w = __shfl_xor(u, o, 32); u = w > u ? w : u; }
   return __uint_as_float(u);
 }
-typedef uint8_t u8x8 __attribute__((ext_vector_type(8)));
-typedef u8x8 u8x8_any __attribute__((aligned(1)));
-__device__ __forceinline__ u8x8 load_codes(const void* p, int64_t at, int64_t most) {
+// Eight codes, four in a word
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(1)));
+__device__ __forceinline__ u32x2 load_codes(const void* p, int64_t at, int64_t most) {
   const uint8_t* q = reinterpret_cast<const uint8_t*>(p) + at;
-  if (most >= 8) return *reinterpret_cast<const u8x8_any*>(q);
-  u8x8 w;
+  if (most >= 8) return *reinterpret_cast<const u32x2_any*>(q);
+  u32x2 w{0, 0};
 #pragma unroll
-  for (int e = 0; e < 8; e++) { w[e] = 0; if (e < most) w[e] = q[e]; }
+  for (int e = 0; e < 8; e++) if (e < most) w[e / 4] |= (uint32_t)q[e] << (8 * (e % 4));
   return w;
 }
-__device__ __forceinline__ void store_codes(void* p, int64_t at, const u8x8& w, int64_t most) {
+__device__ __forceinline__ void store_codes(void* p, int64_t at, const u32x2& w, int64_t most) {
   uint8_t* q = reinterpret_cast<uint8_t*>(p) + at;
-  if (most >= 8) { *reinterpret_cast<u8x8_any*>(q) = w; return; }
+  if (most >= 8) { *reinterpret_cast<u32x2_any*>(q) = w; return; }
 #pragma unroll
-  for (int e = 0; e < 8; e++) if (e < most) q[e] = w[e];
+  for (int e = 0; e < 8; e++) if (e < most) q[e] = (uint8_t)(w[e / 4] >> (8 * (e % 4)));
 }
+template <class F>
+__device__ __forceinline__ void in_fours(F f) { f(0); f(1); }
+
 // The tensor of this workgroup: how many of them begin at or before it.
 template <class Tab>
 __device__ __forceinline__ int tensor_of(const Tab& t, uint32_t block) {
@@ -123,35 +156,40 @@ __device__ __forceinline__ int tensor_of(const Tab& t, uint32_t block) {
   return __builtin_amdgcn_readfirstlane(i - 1);
 }
 
-// One pass over a chunk of one tensor, eight elements a thread.  Bound by reading and writing parameters and states.
-template <bool P32, bool G32, bool MASTER, bool SMALL>
-__global__ __launch_bounds__(T) void adamw_kernel(const Table<SMALL, MASTER> tab, const Step s, Factors f) {
+// One pass over a chunk of one tensor, eight elements a thread.  Bound by reading and writing parameters and states; in 8 bits the vector units are as busy.
+template <bool P32, bool G32, bool MASTER, bool SMALL, bool RANDOM>
+__global__ __launch_bounds__(T) void adamw_kernel(const Table<SMALL, MASTER, RANDOM> tab, const Step s, Factors f) {
+  constexpr bool CODED_P = RANDOM && !P32 && !MASTER;      // bf16 parameters rounded by chance
   const int i = tensor_of(tab, blockIdx.x);
   const int64_t n = tab.n[i], at = (int64_t)(blockIdx.x - tab.begin[i]) * CHUNK + threadIdx.x * 8, most = n - at;
   const bool mine = most > 0;
   typedef Eight<P32 || MASTER> EP;
   typedef Eight<G32> EG;
-  typename EP::type rp;
-  typename EG::type rg;
-  typename Eight<true>::type rm, rv;
-  u8x8 cm, cv;
+  typename EP::type rp{};
+  typename EG::type rg{};
+  typename Eight<true>::type rm{}, rv{};
+  u32x2 cm{0, 0}, cv{0, 0};
   float ms = 0.f, vs = 0.f;
   void* kept;
   if constexpr (MASTER) kept = tab.master[i];
   else kept = tab.p[i];
-  if (mine) {
-    rp = EP::load(kept, at, most);
-    rg = EG::load(tab.g[i], at, most);
+  const void* grad = tab.g[i];
+  void *am = tab.m[i], *av = tab.v[i];
+  auto fetch = [&](int64_t all) {
+    rp = EP::load(kept, at, all);
+    rg = EG::load(grad, at, all);
     if constexpr (SMALL) {
-      cm = load_codes(tab.m[i], at, most);
-      cv = load_codes(tab.v[i], at, most);
+      cm = load_codes(am, at, all);
+      cv = load_codes(av, at, all);
       ms = tab.m_scale[i][at / BLOCK];
       vs = tab.v_scale[i][at / BLOCK];
     } else {
-      rm = Eight<true>::load(tab.m[i], at, most);
-      rv = Eight<true>::load(tab.v[i], at, most);
+      rm = Eight<true>::load(am, at, all);
+      rv = Eight<true>::load(av, at, all);
     }
-  }
+  };
+  if (most >= 8) fetch(8);
+  else if (mine) fetch(most);
   if (s.t_dev || s.lr_dev) f = factors_of(s, s.lr_dev ? (double)*s.lr_dev : s.lr, s.t_dev ? *s.t_dev : s.t);
   float gs = 1.f;
   if (s.scale_dev) {
@@ -159,83 +197,90 @@ __global__ __launch_bounds__(T) void adamw_kernel(const Table<SMALL, MASTER> tab
     if (!(fabsf(gs) < INFINITY)) return;      // the step is left out
   }
   float p[8], g[8], m[8], v[8], root[8];
-  if (mine) {
-    EP::values(rp, p);
-    EG::values(rg, g);
-    if constexpr (!SMALL) {
-      Eight<true>::values(rm, m);
-      Eight<true>::values(rv, v);
-    }
+  EP::values(rp, p);
+  EG::values(rg, g);
+  if constexpr (SMALL) {
+    in_fours([&](int k) {
+      float x[4], r[4];
+      values_m(cm[k], x);
+      values_root(cv[k], r);
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        m[4 * k + e] = x[e] * ms;
+        r[e] *= vs;
+        v[4 * k + e] = r[e] * r[e];
+      }
+    });
+  } else {
+    Eight<true>::values(rm, m);
+    Eight<true>::values(rv, v);
   }
 #pragma unroll
   for (int e = 0; e < 8; e++) {
-    if (!mine) { p[e] = g[e] = m[e] = v[e] = 0.f; }
-    else if constexpr (SMALL) {
-      m[e] = value_m(cm[e]) * ms;
-      v[e] = value_root(cv[e]) * vs;
-      v[e] = v[e] * v[e];
-    }
     if (s.scale_dev) g[e] = g[e] * gs;
     m[e] = m[e] * f.b1 + g[e] * f.c1;
     v[e] = v[e] * f.b2 + (g[e] * g[e]) * f.c2;
     root[e] = sqrtf(v[e]);
     p[e] = p[e] * f.decay - f.step * (m[e] / (root[e] * f.root + s.eps));
   }
-  uint32_t h[8];
-  const bool random = s.random != 0;
-  if (random) {
+  uint32_t h[8] = {};
+  if constexpr (SMALL ? RANDOM : CODED_P) {
     const uint64_t number = (uint64_t)tab.first[i] * BLOCK + (uint64_t)at;      // of the element in the call; eight of them have one high half
     const uint32_t key = mix((uint32_t)(number >> 32) ^ mix(s.seed));
 #pragma unroll
     for (int e = 0; e < 8; e++) h[e] = mix(((uint32_t)number + e) ^ key);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; e++) h[e] = 0;
   }
-  if (mine) {
-    EP::store(kept, at, p, most);
-    if constexpr (!P32 && !MASTER) {
-      if (random) {      // up by chance, as its part of a step is; again over what was rounded to the nearest
-        uint16_t* q = reinterpret_cast<uint16_t*>(kept) + at;
-        u16x8 w;
+  Unit um, ur;
+  if constexpr (SMALL) {
+    uint32_t mm = 0, mr = 0;
 #pragma unroll
-        for (int e = 0; e < 8; e++) w[e] = fabsf(p[e]) < INFINITY ? (uint16_t)((__float_as_uint(p[e]) + (h[e] >> 16)) >> 16) : bf16_nearest(p[e]);
-        if (most >= 8) *reinterpret_cast<u16x8_any*>(q) = w;
-        else {
-#pragma unroll
-          for (int e = 0; e < 8; e++) if (e < most) q[e] = w[e];
-        }
-      }
+    for (int e = 0; e < 8; e++) {      // (as bits, so that a NaN is the largest; what is past the end is zero, as its gradient was)
+      mm = max(mm, __float_as_uint(m[e]) & 0x7FFFFFFFu);
+      mr = max(mr, __float_as_uint(root[e]) & 0x7FFFFFFFu);
     }
-    if constexpr (MASTER) Eight<false>::store(tab.p[i], at, p, most);
+    um = unit_of<7>(largest_of_32(__uint_as_float(mm)));
+    ur = unit_of<17>(largest_of_32(__uint_as_float(mr)));
+    in_fours([&](int k) {
+      float y[4], z[4], r[4];
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        y[e] = m[4 * k + e] * um.inverse;
+        r[e] = root[4 * k + e];
+        z[e] = r[e] * ur.inverse;
+      }
+      cm[k] = um.inverse > 0.f ? codes_m<RANDOM>(y, h + 4 * k) : 0u;
+      cv[k] = ur.inverse > 0.f ? codes_root<RANDOM>(z, r, h + 4 * k) : 0u;
+    });
   }
-  if constexpr (!SMALL) {
-    if (mine) {
-      Eight<true>::store(tab.m[i], at, m, most);
-      Eight<true>::store(tab.v[i], at, v, most);
-    }
-  } else {
-    float mm = 0.f, mr = 0.f;
+  auto store = [&](int64_t all) {
+    if constexpr (CODED_P) {      // up by chance, as its part of a step is
+      u16x8 w;
 #pragma unroll
-    for (int e = 0; e < 8; e++) {      // (as bits, so that a NaN is the largest)
-      mm = __uint_as_float(max(__float_as_uint(mm), e < most ? __float_as_uint(m[e]) & 0x7FFFFFFFu : 0u));
-      mr = __uint_as_float(max(__float_as_uint(mr), e < most ? __float_as_uint(root[e]) & 0x7FFFFFFFu : 0u));
-    }
-    const Unit um = unit_of<7>(largest_of_32(mm)), ur = unit_of<17>(largest_of_32(mr));
-    if (mine) {
+      for (int e = 0; e < 8; e++) w[e] = fabsf(p[e]) < INFINITY ? (uint16_t)((__float_as_uint(p[e]) + (h[e] >> 16)) >> 16) : bf16_nearest(p[e]);
+      uint16_t* q = reinterpret_cast<uint16_t*>(kept) + at;
+      if (all >= 8) *reinterpret_cast<u16x8_any*>(q) = w;
+      else {
 #pragma unroll
-      for (int e = 0; e < 8; e++) {
-        cm[e] = um.number ? (uint8_t)code_m(m[e] * um.inverse, random, h[e]) : (uint8_t)0;
-        cv[e] = ur.number ? (uint8_t)code_root(root[e] * ur.inverse, root[e] > 0.f, random, h[e]) : (uint8_t)0;
+        for (int e = 0; e < 8; e++) if (e < all) q[e] = w[e];
       }
-      store_codes(tab.m[i], at, cm, most);
-      store_codes(tab.v[i], at, cv, most);
+    } else {
+      EP::store(kept, at, p, all);
+    }
+    if constexpr (MASTER) Eight<false>::store(tab.p[i], at, p, all);
+    if constexpr (SMALL) {
+      store_codes(am, at, cm, all);
+      store_codes(av, at, cv, all);
       if ((threadIdx.x & 31) == 0) {
         tab.m_scale[i][at / BLOCK] = um.scale;
         tab.v_scale[i][at / BLOCK] = ur.scale;
       }
+    } else {
+      Eight<true>::store(am, at, m, all);
+      Eight<true>::store(av, at, v, all);
     }
-  }
+  };
+  if (most >= 8) store(8);
+  else if (mine) store(most);
 }
 
 // What 8-bit states stand for, in bf16, which holds them exactly.
@@ -252,14 +297,19 @@ __global__ __launch_bounds__(T) void values_kernel(const Values tab) {
   const int i = tensor_of(tab, blockIdx.x);
   const int64_t n = tab.n[i], at = (int64_t)(blockIdx.x - tab.begin[i]) * CHUNK + threadIdx.x * 8, most = n - at;
   if (most <= 0) return;
-  const u8x8 cm = load_codes(tab.m[i], at, most), cv = load_codes(tab.v[i], at, most);
+  const u32x2 cm = load_codes(tab.m[i], at, most), cv = load_codes(tab.v[i], at, most);
   const float ms = tab.m_scale[i][at / BLOCK], vs = tab.v_scale[i][at / BLOCK];
   float m[8], r[8];
+  in_fours([&](int k) {
+    float x[4], y[4];
+    values_m(cm[k], x);
+    values_root(cv[k], y);
 #pragma unroll
-  for (int e = 0; e < 8; e++) {
-    m[e] = value_m(cm[e]) * ms;
-    r[e] = value_root(cv[e]) * vs;
-  }
+    for (int e = 0; e < 4; e++) {
+      m[4 * k + e] = x[e] * ms;
+      r[4 * k + e] = y[e] * vs;
+    }
+  });
   Eight<false>::store(tab.m_out[i], at, m, most);
   Eight<false>::store(tab.root_out[i], at, r, most);
 }
@@ -296,35 +346,39 @@ int kind_of(const osscar_adamw_tensor& t) { return (t.master ? 2 : t.p_dtype == 
 bool is_kind(const osscar_adamw_tensor& t, int which) { return kind_of(t) == which; }
 bool any_kind(const osscar_adamw_tensor&, int) { return true; }
 
-template <bool P32, bool G32, bool MASTER, bool SMALL>
+template <bool P32, bool G32, bool MASTER, bool SMALL, bool RANDOM>
 void steps(const osscar_adamw_tensor* t, int64_t count, const Step& s, const Factors& f, hipStream_t stream) {
-  typedef Table<SMALL, MASTER> Tab;
-  static_assert(sizeof(Tab) + sizeof(Step) + sizeof(Factors) <= 4096, "a launch's arguments");
-  in_launches<Tab>(
-      count, t, is_kind, (MASTER ? 2 : P32 ? 0 : 1) * 2 + (G32 ? 1 : 0),
-      [](Tab& tab, int at, const osscar_adamw_tensor& x, int64_t number) {
-        tab.p[at] = x.p;
-        tab.g[at] = x.g;
-        tab.m[at] = x.m;
-        tab.v[at] = x.v;
-        tab.n[at] = x.n;
-        tab.first[at] = number;
-        if constexpr (SMALL) { tab.m_scale[at] = x.m_scale; tab.v_scale[at] = x.v_scale; }
-        if constexpr (MASTER) tab.master[at] = x.master;
-      },
-      [&](const Tab& tab, unsigned blocks) { hipLaunchKernelGGL((adamw_kernel<P32, G32, MASTER, SMALL>), dim3(blocks), dim3(T), 0, stream, tab, s, f); });
+  if constexpr (RANDOM && !SMALL && (P32 || MASTER)) {      // (nothing is rounded to fewer bits but copies of masters)
+    steps<P32, G32, MASTER, SMALL, false>(t, count, s, f, stream);
+  } else {
+    typedef Table<SMALL, MASTER, RANDOM> Tab;
+    static_assert(sizeof(Tab) + sizeof(Step) + sizeof(Factors) <= 4096, "a launch's arguments");
+    in_launches<Tab>(
+        count, t, is_kind, (MASTER ? 2 : P32 ? 0 : 1) * 2 + (G32 ? 1 : 0),
+        [](Tab& tab, int at, const osscar_adamw_tensor& x, int64_t number) {
+          tab.p[at] = x.p;
+          tab.g[at] = x.g;
+          tab.m[at] = x.m;
+          tab.v[at] = x.v;
+          tab.n[at] = (uint32_t)x.n;
+          if constexpr (RANDOM) tab.first[at] = number;
+          if constexpr (SMALL) { tab.m_scale[at] = x.m_scale; tab.v_scale[at] = x.v_scale; }
+          if constexpr (MASTER) tab.master[at] = x.master;
+        },
+        [&](const Tab& tab, unsigned blocks) { hipLaunchKernelGGL((adamw_kernel<P32, G32, MASTER, SMALL, RANDOM>), dim3(blocks), dim3(T), 0, stream, tab, s, f); });
+  }
 }
-template <bool SMALL>
+template <bool SMALL, bool RANDOM>
 void steps_of(const osscar_adamw_tensor* t, int64_t count, const Step& s, const Factors& f, hipStream_t stream) {
   bool seen[6] = {};
   for (int64_t k = 0; k < count; k++)
     if (t[k].n > 0) seen[kind_of(t[k])] = true;
-  if (seen[0]) steps<true, false, false, SMALL>(t, count, s, f, stream);
-  if (seen[1]) steps<true, true, false, SMALL>(t, count, s, f, stream);
-  if (seen[2]) steps<false, false, false, SMALL>(t, count, s, f, stream);
-  if (seen[3]) steps<false, true, false, SMALL>(t, count, s, f, stream);
-  if (seen[4]) steps<false, false, true, SMALL>(t, count, s, f, stream);
-  if (seen[5]) steps<false, true, true, SMALL>(t, count, s, f, stream);
+  if (seen[0]) steps<true, false, false, SMALL, RANDOM>(t, count, s, f, stream);
+  if (seen[1]) steps<true, true, false, SMALL, RANDOM>(t, count, s, f, stream);
+  if (seen[2]) steps<false, false, false, SMALL, RANDOM>(t, count, s, f, stream);
+  if (seen[3]) steps<false, true, false, SMALL, RANDOM>(t, count, s, f, stream);
+  if (seen[4]) steps<false, false, true, SMALL, RANDOM>(t, count, s, f, stream);
+  if (seen[5]) steps<false, true, true, SMALL, RANDOM>(t, count, s, f, stream);
 }
 
 const char* bad_tensor(const osscar_adamw_tensor& t, bool small, bool values) {
@@ -362,8 +416,10 @@ extern "C" osscar_status osscar_adamw(const osscar_adamw_tensor* tensors, int64_
   const Step s{d->lr, d->beta1, d->beta2, d->weight_decay, (float)d->eps, 1.f, d->step, d->lr_dev, d->grad_scale_dev, d->step_dev, d->seed, d->stochastic != 0};
   const Factors f = factors_of(s, d->lr_dev ? 0 : d->lr, d->step_dev ? 1 : d->step);
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
-  if (d->bits == 8) steps_of<true>(tensors, count, s, f, stream);
-  else steps_of<false>(tensors, count, s, f, stream);
+  if (d->bits == 8 && s.random) steps_of<true, true>(tensors, count, s, f, stream);
+  else if (d->bits == 8) steps_of<true, false>(tensors, count, s, f, stream);
+  else if (s.random) steps_of<false, true>(tensors, count, s, f, stream);
+  else steps_of<false, false>(tensors, count, s, f, stream);
   return launched();
 }
 
