@@ -461,8 +461,9 @@ osscar_status osscar_adapters_backward(const osscar_adapters_desc* desc, const v
  * stochastic: codes, and bf16 parameters without a master, are rounded up with the probability that their part of a step is, so that changes smaller than a step (0.001 of v) are not lost
  * on average: bits r of the hash h below are added to the float32 number under its last kept bit and the rest cut off; for m the low 20 of h, for sqrt v the high 19 of the
  * low 32 of 0x9E3779B9 h, for p the high 16 of h (numbers below the smallest normal one first have it added).  h = mix(low 32 bits of i ^ mix(high 32 bits of i ^ mix(seed))), i the number of
- * the element in the call, each tensor before it counting as whole blocks; mix(x): x = (x ^ x >> 16) * 0x9E3779B9, x = (x ^ x >> 15) * 0xB7E15163, x ^ x >> 16 in 32 bits.  A seed of its own for each step.
- * lr_dev, step_dev (may be NULL): one float32, one int64 on the device that take the place of lr and step, for steps that are captured once and replayed.  grad_scale_dev (may be NULL): one float32 that
+ * the element in the call, each tensor before it counting as whole blocks; mix(x): x = (x ^ x >> 16) * 0x9E3779B9, x = (x ^ x >> 15) * 0xB7E15163, x ^ x >> 16 in 32 bits.  A seed of its own for each step;
+ * with step_dev the low 32 bits of the step are added to it, so that each replay of a captured step has one.
+ * lr_dev, step_dev (may be NULL): one float32, one int64 on the device that take the place of lr and step (below 1: 1), for steps that are captured once and replayed.  grad_scale_dev (may be NULL): one float32 that
  * every gradient is multiplied by first; if it is not finite the call changes nothing. */
 #define OSSCAR_ADAMW_BLOCK 256
 typedef struct {

@@ -190,7 +190,8 @@ __global__ __launch_bounds__(T) void adamw_kernel(const Table<SMALL, MASTER, RAN
   };
   if (most >= 8) fetch(8);
   else if (mine) fetch(most);
-  if (s.t_dev || s.lr_dev) f = factors_of(s, s.lr_dev ? (double)*s.lr_dev : s.lr, s.t_dev ? *s.t_dev : s.t);
+  const int64_t t = s.t_dev ? max(*s.t_dev, (int64_t)1) : s.t;
+  if (s.t_dev || s.lr_dev) f = factors_of(s, s.lr_dev ? (double)*s.lr_dev : s.lr, t);
   float gs = 1.f;
   if (s.scale_dev) {
     gs = *s.scale_dev;
@@ -226,7 +227,7 @@ __global__ __launch_bounds__(T) void adamw_kernel(const Table<SMALL, MASTER, RAN
   uint32_t h[8] = {};
   if constexpr (SMALL ? RANDOM : CODED_P) {
     const uint64_t number = (uint64_t)tab.first[i] * BLOCK + (uint64_t)at;      // of the element in the call; eight of them have one high half
-    const uint32_t key = mix((uint32_t)(number >> 32) ^ mix(s.seed));
+    const uint32_t key = mix((uint32_t)(number >> 32) ^ mix(s.seed + (s.t_dev ? (uint32_t)t : 0u)));
 #pragma unroll
     for (int e = 0; e < 8; e++) h[e] = mix(((uint32_t)number + e) ^ key);
   }

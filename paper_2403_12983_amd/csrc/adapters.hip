@@ -930,9 +930,10 @@ void outer(const Outers& q, const Plan& plan, const Pick& pick, int64_t chunks, 
   else hipLaunchKernelGGL((outer_kernel<F32, 4, PIECES>), grid, block, 0, s, q, plan, pick);
 }
 
-// Rows of a chunk: as many as leave two workgroups per compute unit, 128 to 512 (their sums are written and read again: 4 rank bytes per 2 rows of bf16).
+// Rows of a chunk: as many as leave two workgroups per compute unit, 128 to 512, and no more than 64 chunks of many rows (their sums are written and read again: as much as 2 rank
+// rows of bf16 each).
 int chunk_of(const osscar_adapters_desc& d) {
-  int chunk = 512;
+  int chunk = (int)std::max<int64_t>(512, up(up(d.n, 64), 64) * 64);
   while (chunk > 128 && up(d.n, chunk) * up(std::min(d.d, d.m), OCOLS) * up(d.rank, 64) < 512) chunk /= 2;
   return chunk;
 }

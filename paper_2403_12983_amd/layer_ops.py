@@ -541,7 +541,7 @@ class AdamW:
         if len(self.masters) != count or (states is not None and len(states) != count):
             _refuse("masters and states have one entry per parameter")
         self.states: List[AdamWState] = []
-        written = set()
+        written = []      # (address, end, parameter) of what a step writes
         for k, (p, master) in enumerate(zip(self.params, self.masters)):
             n = p.numel()
             code = _code(p, f"parameter {k}")
@@ -559,12 +559,14 @@ class AdamW:
             _on(self._index, **{f"parameter {k}": p, f"master {k}": master, f"state {k}": s.m, f"state {k}'s v": s.v, f"state {k}'s m_scale": s.m_scale, f"state {k}'s v_scale": s.v_scale})
             for t in (p, master, *s):
                 if t is not None and t.numel() > 0:
-                    if t.data_ptr() in written:
-                        _refuse(f"parameter {k} or one of its states is listed twice")
-                    written.add(t.data_ptr())
+                    written.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), k))
             self.states.append(s)
             self._table[k] = _AdamWTensor(n, p.data_ptr(), None if master is None else master.data_ptr(), None, s.m.data_ptr(), s.v.data_ptr(),
                                           s.m_scale.data_ptr() if bits == 8 else None, s.v_scale.data_ptr() if bits == 8 else None, code, 0)
+        written.sort()
+        for (_, end, a), (start, _, b) in zip(written, written[1:]):
+            if start < end:
+                _refuse(f"parameters {a} and {b} or their states share memory")
         self.grads: Optional[List[torch.Tensor]] = None
         if grads is not None:
             self._take(grads)
@@ -600,7 +602,8 @@ class AdamW:
                      stream: Optional[torch.cuda.Stream] = None) -> None:
         """One step of AdamW, in place.  step counts from 1; lr and step may be tensors of one element on the GPU (float32, int64), which a captured step reads anew at each replay.
         grads: new gradients, kept for later steps.  grad_scale: one float32 on the GPU that the gradients are multiplied by; where it is not finite nothing
-        changes.  seed (32 bits, another for each step): 8-bit states, and bfloat16 parameters without a master, are rounded up by chance instead of to the nearest."""
+        changes.  seed (32 bits, another for each step; a step on the GPU is added to it): 8-bit states, and bfloat16 parameters without a master, are rounded up by chance instead of
+        to the nearest."""
         if grads is not None:
             self._take(grads)
         if self.grads is None:

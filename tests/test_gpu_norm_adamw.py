@@ -515,6 +515,29 @@ def test_adamw_captured_with_rate_and_step_on_the_device(osscar, bits):
         plan.osscar_adamw(1e-3, 5, grad_scale=torch.tensor(bad, device=DEV))
         after = params + [x.view(torch.uint8) for s in plan.states for x in s if x is not None]
         assert all(torch.equal(x, y) for x, y in zip(before, after))
+    # by chance: the step is added to the seed, so that each replay has its own
+    if bits == 8:
+        host = osscar.AdamW([p.clone() for p in params], [x.clone() for x in grads], bits=bits)
+        plan = osscar.AdamW(params, grads, bits=bits)
+        step.zero_()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step.add_(1)
+            plan.osscar_adamw(1e-3, step, seed=(1 << 32) - 2)
+        for t in range(1, 4):
+            graph.replay()
+            torch.cuda.synchronize()
+            host.osscar_adamw(1e-3, t, seed=((1 << 32) - 2 + t) % (1 << 32))
+            for a, b in zip(plan.states, host.states):
+                assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a, b)), t
+    # a step below 1 counts as the first
+    ends = []
+    for t in (-5, 0, 1):
+        q = params[1].clone()
+        osscar.AdamW([q], [grads[1]], bits=bits).osscar_adamw(1e-3, torch.tensor(t, device=DEV))
+        ends.append(q)
+    assert torch.equal(ends[0], ends[2]) and torch.equal(ends[1], ends[2])
     # late steps: the powers of beta are nothing
     for t in (10 ** 6, 2 ** 40):
         host.osscar_adamw(1e-3, t)
@@ -573,7 +596,7 @@ def test_adamw_refusals(osscar):
     assert A([p], states=s8).bits == 8
     plan = A([p], [gr])
     bad = [lambda: A([]), lambda: A([p.half()]), lambda: A([p[:, :8]]), lambda: A([p.cpu()]), lambda: A([p], [gr, gr]), lambda: A([p], [gr.t()]), lambda: A([p], [gr[:4]]),
-           lambda: A([p], [gr.half()]), lambda: A([p], [gr.cpu()]), lambda: A([p, p]), lambda: A([p, p.view(-1)]), lambda: A([p], masters=[p.clone()]),
+           lambda: A([p], [gr.half()]), lambda: A([p], [gr.cpu()]), lambda: A([p, p]), lambda: A([p, p.view(-1)]), lambda: A([p, p.view(-1)[100:]]), lambda: A([p], masters=[p.clone()]),
            lambda: A([p.bfloat16()], masters=[p.bfloat16()]), lambda: A([p.bfloat16()], masters=[p[:4].clone()]), lambda: A([p], masters=[]), lambda: A([p], bits=16),
            lambda: A([p], states=s32 + s32), lambda: A([p], states=s8, bits=32), lambda: A([p], states=s32, bits=8), lambda: A([p], states=[(s32[0].m[:5], s32[0].v)]),
            lambda: A([p], states=[(s32[0].m, s32[0].m)]), lambda: A([p], states=[(s8[0].m, s8[0].v, s8[0].m_scale, s8[0].v_scale[:0])]), lambda: A([p]).osscar_adamw(LR, 1),
