@@ -910,7 +910,7 @@ void expand(const Expand& q, const Pick& pick, hipStream_t s) {
   a.subs = 4;
   while (a.subs > 1 && (up(q.n, a.subs * 16) * blocks < 512 || q.n <= a.subs * 8)) a.subs /= 2;
   const int64_t tiles = up(q.n, 16 * a.subs);
-  a.slots = pick.index ? (int)std::max<int64_t>(1, std::min<int64_t>({4096 / (tiles * blocks), 16 * a.subs, q.n, pick.count})) : 1;
+  a.slots = pick.index ? (int)std::max<int64_t>(1, std::min<int64_t>({2048 / (tiles * blocks), 16 * a.subs, q.n, pick.count})) : 1;
   const dim3 grid((unsigned)(tiles * blocks), (unsigned)a.slots), block(EW * 64);
   auto go = [&](auto parts) {
     constexpr bool PARTS = decltype(parts)::value;
