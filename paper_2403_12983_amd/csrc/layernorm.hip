@@ -28,7 +28,7 @@ struct Place {
 template <int TPR, int GROUPS>
 __device__ __forceinline__ void sum2(float& a, float& b, float2* sh, int sub, int tid) {      // over the TPR threads of a row; sh: GROUPS x TPR / 64
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) { a += __shfl_xor(a, o, 64); b += __shfl_xor(b, o, 64); }
+  for (int o = (TPR < 64 ? TPR : 64) / 2; o > 0; o >>= 1) { a += __shfl_xor(a, o, 64); b += __shfl_xor(b, o, 64); }
   if constexpr (TPR > 64) {
     constexpr int W = TPR / 64;
     __syncthreads();
@@ -53,7 +53,8 @@ __device__ __forceinline__ void affine_values(const void* p, int f32, int at, in
   }
 }
 
-// Forward.  Bound by reading X and writing Y.
+// Forward.  Bound by reading X and writing Y: bf16 16384 x 2048 25 us (5.4 TB/s), 8192 x 7168 45 us (5.2), 100000 x 64 7 us (3.5), 4096 x 14336 60 us (3.9; one workgroup of 1024
+// threads a compute unit; without the next row and the gains in registers 64); rows of 1365 or 5461, at any two bytes, 3.7 to 4.3 TB/s; float32 4.2 to 6.3.
 template <bool F32, int TPR, int PK, int GROUPS>
 __global__ __launch_bounds__(TPR* GROUPS) void forward_kernel(const void* X, Rows q, Affine p, void* Y, float* stats) {
   __shared__ float2 sh[GROUPS * TPR / 64];
@@ -120,21 +121,25 @@ __global__ __launch_bounds__(TPR* GROUPS) void forward_kernel(const void* X, Row
 
 // Backward: with h = (x - mean) rstd and g = dy w,  dx = rstd (g - mean g - h mean(g h)),  dw = sum over rows of dy h,  db = sum of dy.
 // A thread has the same columns in every row that it takes, so the sums over rows stay in its registers; a workgroup's rows are added in order through LDS and go
-// to `part` ([workgroup][dw, db][d]), which a second launch adds in order.  Bound by reading X and dY and writing dX.
+// to `part` ([workgroup][dw, db][d]), which a second launch adds in order.  Bound by reading X and dY and writing dX: bf16, both launches, 16384 x 2048 38 us (5.3 TB/s), 8192 x 7168 74
+// us (4.7), 100000 x 64 14 us (2.7), 4096 x 14336 100 us (3.5; with the next row and the gain in registers 158); float32 4.1 to 5.6.  512 workgroups, with twice the parts: 80 us of 74.
 template <bool F32, int TPR, int PK, int GROUPS>
 __global__ __launch_bounds__(TPR* GROUPS) void backward_kernel(const void* X, const void* dY, Rows q, int64_t lddy, int64_t lddx, const void* weight, int w_f32,
                                                                const float* __restrict__ stats, void* dX, float* part) {
   __shared__ float2 sh[GROUPS * TPR / 64];
-  __shared__ float cols[GROUPS > 1 ? 2 * TPR * PK * 8 : 1];
+  // Rows of fewer threads than a wave's are added within it first
+  constexpr int SUBS = TPR < 64 ? 64 / TPR : 1, PARTS_IN = GROUPS / SUBS;
+  constexpr bool HOLD = TPR < 1024;      // the gain stays in registers, and so does the next row; of 1024 threads each has 128 of them
+  __shared__ float cols[PARTS_IN > 1 ? 2 * TPR * PK * 8 : 1];
   const int sub = threadIdx.x / TPR, tid = threadIdx.x % TPR;
   const float inv = 1.f / q.d;
   typedef Eight<F32> E8;
   typedef Place<TPR> At;
-  float w[PK][8], aw[PK][8], ab[PK][8];
+  float w[HOLD ? PK : 1][8], aw[PK][8], ab[PK][8];
 #pragma unroll
   for (int k = 0; k < PK; k++) {
     const At at(k, tid, q.d);
-    affine_values(weight, w_f32, at.at, at.at + 8, w[k], 1.f);
+    if constexpr (HOLD) affine_values(weight, w_f32, at.at, at.at + 8, w[k], 1.f);
 #pragma unroll
     for (int e = 0; e < 8; e++) aw[k][e] = ab[k][e] = 0.f;
   }
@@ -150,9 +155,10 @@ __global__ __launch_bounds__(TPR* GROUPS) void backward_kernel(const void* X, co
     }
   };
   int64_t row = (int64_t)blockIdx.x * GROUPS + sub;
-  if (row < q.n) fetch(row);
+  if (HOLD && row < q.n) fetch(row);
   for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < q.n; first += step, row += step) {
     const bool mine = row < q.n;
+    if (!HOLD && mine) fetch(row);
     float h[PK][8], g[PK][8], s = 0.f, s2 = 0.f;
     const float mean = st.x, rstd = st.y;
 #pragma unroll
@@ -160,6 +166,7 @@ __global__ __launch_bounds__(TPR* GROUPS) void backward_kernel(const void* X, co
       const At at(k, tid, q.d);
       E8::values(rx[k], h[k]);
       E8::values(ry[k], g[k]);
+      if constexpr (!HOLD) affine_values(weight, w_f32, at.at, at.at + 8, w[0], 1.f);
 #pragma unroll
       for (int e = 0; e < 8; e++) {
         h[k][e] = (h[k][e] - mean) * rstd;
@@ -167,12 +174,12 @@ __global__ __launch_bounds__(TPR* GROUPS) void backward_kernel(const void* X, co
           aw[k][e] = fmaf(g[k][e], h[k][e], aw[k][e]);
           ab[k][e] += g[k][e];
         }
-        g[k][e] *= w[k][e];
+        g[k][e] *= w[HOLD ? k : 0][e];
         s += e >= at.skip ? g[k][e] : 0.f;
         s2 += e >= at.skip ? g[k][e] * h[k][e] : 0.f;
       }
     }
-    if (row + step < q.n) fetch(row + step);
+    if (HOLD && row + step < q.n) fetch(row + step);
     if (!dX) continue;
     sum2<TPR, GROUPS>(s, s2, sh, sub, tid);
     if (mine) {
@@ -189,9 +196,18 @@ __global__ __launch_bounds__(TPR* GROUPS) void backward_kernel(const void* X, co
     }
   }
   if (!part) return;
-  if constexpr (GROUPS > 1) {
-    for (int k0 = 0; k0 < GROUPS - 1; k0++) {
-      if (sub == k0) {
+  if constexpr (SUBS > 1) {
+#pragma unroll
+    for (int o = TPR; o < 64; o <<= 1)
+#pragma unroll
+      for (int k = 0; k < PK; k++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) { aw[k][e] += __shfl_xor(aw[k][e], o, 64); ab[k][e] += __shfl_xor(ab[k][e], o, 64); }
+  }
+  const bool speaks = sub % SUBS == 0;      // for its wave's rows
+  if constexpr (PARTS_IN > 1) {
+    for (int k0 = 0; k0 < PARTS_IN - 1; k0++) {
+      if (sub / SUBS == k0 && speaks) {
 #pragma unroll
         for (int k = 0; k < PK; k++)
 #pragma unroll
@@ -203,7 +219,7 @@ __global__ __launch_bounds__(TPR* GROUPS) void backward_kernel(const void* X, co
       }
       __syncthreads();
     }
-    if (sub != GROUPS - 1) return;
+    if (sub / SUBS != PARTS_IN - 1 || !speaks) return;
 #pragma unroll
     for (int k = 0; k < PK; k++)
 #pragma unroll
@@ -333,7 +349,7 @@ __global__ __launch_bounds__(256) void long_columns_kernel(const void* X, const 
   put_f32(out + q.d, ab, most);
 }
 
-// The parts of dw and db added: 64 columns per workgroup, an eighth of the parts per thread, in order.
+// The parts of dw and db added: 64 columns per workgroup, an eighth of the parts per thread, in order (256 parts of 7168: 4.8 us).
 __global__ __launch_bounds__(512) void join_columns_kernel(const float* __restrict__ part, int parts, int64_t d, void* dw, void* db, int f32) {
   __shared__ float sh[8][64];
   const int slice = threadIdx.x >> 6, per = (parts + 7) / 8, last = min(parts, (slice + 1) * per);
@@ -359,7 +375,7 @@ __global__ __launch_bounds__(512) void join_columns_kernel(const float* __restri
 }
 
 constexpr int FORWARD_BLOCKS = 2048, PARTS = 256;
-int groups_of(int64_t d) { return d <= 1024 ? 8 : d <= 2048 ? 4 : d <= 4096 ? 2 : 1; }      // rows that a workgroup of the backward pass takes together
+int groups_of(int64_t d) { return d <= 64 ? 64 : d <= 128 ? 32 : d <= 256 ? 16 : d <= 1024 ? 8 : d <= 2048 ? 4 : d <= 4096 ? 2 : 1; }      // rows that a workgroup of the backward pass takes together
 int parts_of(int64_t n, int64_t d) {
   const int64_t blocks = (n + groups_of(d) - 1) / groups_of(d);
   return (int)(blocks < 1 ? 1 : blocks > PARTS ? PARTS : blocks);
@@ -374,6 +390,9 @@ template <bool F32>
 void forward_of(const void* X, const Rows& q, const Affine& p, void* Y, float* stats, hipStream_t s) {
   if (q.d < 8 || q.d > LONGEST)
     hipLaunchKernelGGL(long_forward_kernel<F32>, dim3((unsigned)(q.n < FORWARD_BLOCKS ? q.n : FORWARD_BLOCKS)), dim3(1024), 0, s, X, q, p, Y, stats);
+  else if (q.d <= 64) forward<F32, 8, 1, 32>(X, q, p, Y, stats, s);
+  else if (q.d <= 128) forward<F32, 16, 1, 16>(X, q, p, Y, stats, s);
+  else if (q.d <= 256) forward<F32, 32, 1, 8>(X, q, p, Y, stats, s);
   else if (q.d <= 512) forward<F32, 64, 1, 4>(X, q, p, Y, stats, s);
   else if (q.d <= 1024) forward<F32, 64, 2, 4>(X, q, p, Y, stats, s);
   else if (q.d <= 2048) forward<F32, 128, 2, 2>(X, q, p, Y, stats, s);
@@ -394,7 +413,10 @@ void backward_of(const Back& a, hipStream_t s) {
     if (a.part) hipLaunchKernelGGL(long_columns_kernel<F32>, dim3((unsigned)((d + 2047) / 2048), (unsigned)a.parts), dim3(256), 0, s, a.X, a.dY, a.q, a.lddy, a.stats, a.part);
     if (a.dX) hipLaunchKernelGGL(long_backward_kernel<F32>, dim3((unsigned)(a.q.n < FORWARD_BLOCKS ? a.q.n : FORWARD_BLOCKS)), dim3(1024), 0, s, a.X, a.dY, a.q, a.lddy, a.lddx,
                                  a.w, a.w_f32, a.stats, a.dX);
-  } else if (d <= 512) backward<F32, 64, 1, 8>(a, s);
+  } else if (d <= 64) backward<F32, 8, 1, 64>(a, s);
+  else if (d <= 128) backward<F32, 16, 1, 32>(a, s);
+  else if (d <= 256) backward<F32, 32, 1, 16>(a, s);
+  else if (d <= 512) backward<F32, 64, 1, 8>(a, s);
   else if (d <= 1024) backward<F32, 64, 2, 8>(a, s);
   else if (d <= 2048) backward<F32, 128, 2, 4>(a, s);
   else if (d <= 4096) backward<F32, 256, 2, 2>(a, s);
