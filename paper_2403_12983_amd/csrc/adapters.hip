@@ -97,11 +97,12 @@ struct Contract {
   float* t;                         // [part][n][rank]
 };
 constexpr int CW = 8;      // waves
-constexpr int turn_of(bool f32, int rt, int ct) { return f32 || rt * ct > 4 ? 2 : 4; }      // instructions' worth of a row in a turn
-template <bool F32, int RT, int CT>
+constexpr int RT = 2;      // row tiles of 16 in a workgroup (with four, half as many reads of V, it takes as long: 75 us instead of 74 at rank 32; with rank 64 they do not fit the registers)
+constexpr int turn_of(bool f32, int ct) { return f32 || RT * ct > 4 ? 2 : 4; }      // instructions' worth of a row in a turn
+template <bool F32, int CT>
 __global__ __launch_bounds__(CW * 64) void contract_kernel(Contract q, Pick pick) {
   typedef Num<F32> N;
-  constexpr int U = turn_of(F32, RT, CT), TURN = U * N::STEP, ROWS = RT * 16, COLS = CT * 16;
+  constexpr int U = turn_of(F32, CT), TURN = U * N::STEP, ROWS = RT * 16, COLS = CT * 16;
   constexpr int NC = U * 4, PER = 64 / NC, ROW = NC * 16;      // packets of a row in a turn, rows of one load, bytes of a row
   constexpr int SUMS = CW / 2 * ROWS * (COLS + 1) * 4, TURNS = CW * ROWS * ROW;
   __shared__ __align__(16) char lds[SUMS > TURNS ? SUMS : TURNS];
@@ -869,35 +870,26 @@ int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // 50 and 74); of two adapters, sorted: 128 rows 14 and 18 (rank 64: 35 and 35), 256 rows 21 and 24; without an index 64 rows 11 and 13 (20 and 23), 128 rows 14 and 14 (34 and 23).
 int64_t few_of(bool index) { return index ? 256 : 64; }
 // Row tiles of 16 in a workgroup, and how its work is dealt out: parts of the contraction and slots of adapters to fill the chip where rows are few.
-struct Deal { int rt, ct, parts, slots; int64_t tiles; };
+struct Deal { bool few; int ct, parts, slots; int64_t tiles; };
 Deal deal(int64_t n, int64_t K, int count, int rank, bool f32, bool index) {
-  Deal d;
-  if (n <= few_of(index)) return Deal{0, 0, (int)std::min<int64_t>(PARTS_MOST, up(K, FW * 512)), 1, n};
-  d.rt = n <= 16 ? 1 : 2;      // (64 rows, whose sums and operands do not fit the registers: 75 us instead of 73 at rank 32, 62 instead of 28 at rank 64)
-  d.ct = rank <= 16 ? 1 : rank <= 32 ? 2 : 4;
-  d.tiles = up(n, 16 * d.rt);
-  d.slots = index ? (int)std::max<int64_t>(1, std::min<int64_t>({256 / d.tiles, 16 * d.rt, n, count})) : 1;
-  const int64_t turns = up(K, turn_of(f32, d.rt, d.ct) * (f32 ? 16 : 32)), blocks = d.tiles * d.slots * up(rank, 16 * d.ct);
-  d.parts = (int)std::max<int64_t>(1, std::min<int64_t>({256 / std::max<int64_t>(blocks, 1), up(turns, 2 * CW), PARTS_MOST}));
+  if (n <= few_of(index)) return Deal{true, 0, (int)std::min<int64_t>(PARTS_MOST, up(K, FW * 512)), 1, n};
+  Deal d{false, rank <= 16 ? 1 : rank <= 32 ? 2 : 4, 1, 1, up(n, 16 * RT)};
+  if (index) d.slots = (int)std::max<int64_t>(1, std::min<int64_t>({256 / d.tiles, 16 * RT, count}));
+  const int64_t turns = up(K, turn_of(f32, d.ct) * (f32 ? 16 : 32)), blocks = d.tiles * d.slots * up(rank, 16 * d.ct);
+  d.parts = (int)std::max<int64_t>(1, std::min<int64_t>({256 / blocks, up(turns, 2 * CW), PARTS_MOST}));
   return d;
 }
 
 template <bool F32>
 void contract(const Contract& all, const Pick& pick, const Deal& d, hipStream_t s) {
-  if (d.rt == 0) {
+  if (d.few) {
     hipLaunchKernelGGL(contract_few_kernel<F32>, dim3((unsigned)all.parts, (unsigned)all.n, (unsigned)up(pick.rank, 16)), dim3(FW * 64), 0, s, all, pick);
     return;
   }
-  const dim3 grid((unsigned)(d.tiles * d.slots), (unsigned)d.parts, (unsigned)up(pick.rank, 16 * d.ct)), block(CW * 64);
-  if (d.rt == 1) {
-    if (d.ct == 1) hipLaunchKernelGGL((contract_kernel<F32, 1, 1>), grid, block, 0, s, all, pick);
-    else if (d.ct == 2) hipLaunchKernelGGL((contract_kernel<F32, 1, 2>), grid, block, 0, s, all, pick);
-    else hipLaunchKernelGGL((contract_kernel<F32, 1, 4>), grid, block, 0, s, all, pick);
-  } else {
-    if (d.ct == 1) hipLaunchKernelGGL((contract_kernel<F32, 2, 1>), grid, block, 0, s, all, pick);
-    else if (d.ct == 2) hipLaunchKernelGGL((contract_kernel<F32, 2, 2>), grid, block, 0, s, all, pick);
-    else hipLaunchKernelGGL((contract_kernel<F32, 2, 4>), grid, block, 0, s, all, pick);
-  }
+  const dim3 grid((unsigned)(d.tiles * d.slots), (unsigned)all.parts, (unsigned)up(pick.rank, 16 * d.ct)), block(CW * 64);
+  if (d.ct == 1) hipLaunchKernelGGL((contract_kernel<F32, 1>), grid, block, 0, s, all, pick);
+  else if (d.ct == 2) hipLaunchKernelGGL((contract_kernel<F32, 2>), grid, block, 0, s, all, pick);
+  else hipLaunchKernelGGL((contract_kernel<F32, 4>), grid, block, 0, s, all, pick);
 }
 template <bool F32>
 void expand(const Expand& q, const Pick& pick, hipStream_t s) {
@@ -908,7 +900,7 @@ void expand(const Expand& q, const Pick& pick, hipStream_t s) {
   const int64_t blocks = up(q.C, EW * ECOLS);
   Expand a = q;
   a.subs = 4;
-  while (a.subs > 1 && (up(q.n, a.subs * 16) * blocks < 512 || q.n <= a.subs * 8)) a.subs /= 2;
+  while (a.subs > 1 && up(q.n, a.subs * 16) * blocks < 512) a.subs /= 2;
   const int64_t tiles = up(q.n, 16 * a.subs);
   a.slots = pick.index ? (int)std::max<int64_t>(1, std::min<int64_t>({2048 / (tiles * blocks), 16 * a.subs, q.n, pick.count})) : 1;
   const dim3 grid((unsigned)(tiles * blocks), (unsigned)a.slots), block(EW * 64);

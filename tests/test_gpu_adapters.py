@@ -104,7 +104,7 @@ def _check(pkg, X, dY, A, B, more, base=None, dbase=None, dw_dtype=None, T_kept=
 
 
 SIZES = [(1, 1, 1, 1, 1), (1, 2048, 300, 4, 16), (3, 7, 9, 2, 3), (2, 64, 130, 3, 8), (16, 300, 520, 32, 16), (17, 136, 77, 5, 17), (31, 33, 640, 3, 4), (33, 513, 129, 40, 12), (64, 128, 256, 7, 32),
-         (70, 1365, 200, 3, 33), (200, 512, 1030, 90, 5), (300, 257, 128, 2, 64), (513, 130, 300, 6, 65), (777, 96, 1365, 3, 12), (1500, 520, 136, 2, 130), (2100, 40, 48, 300, 2)]
+         (70, 1365, 200, 3, 33), (200, 512, 1030, 90, 5), (300, 257, 128, 2, 64), (513, 130, 300, 6, 65), (777, 96, 1365, 3, 12), (1500, 520, 136, 2, 130), (2100, 40, 48, 300, 2), (65, 600, 520, 2, 16), (256, 520, 640, 20, 20), (257, 520, 640, 20, 20), (2, 9000, 70, 2, 100)]
 
 
 @pytest.mark.parametrize("order", ["one", "runs", "mixed"])
