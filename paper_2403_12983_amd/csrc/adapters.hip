@@ -209,6 +209,7 @@ __global__ __launch_bounds__(CW * 64) void contract_kernel(Contract q, Pick pick
       __syncthreads();
       if (wave < half) each([&](int at, float s) { return s + sums[wave][at]; });
     }
+    __syncthreads();      // (the next adapter's operands take the same place)
     if (wave == 0) {
       const float s = q.scaled ? pick.scale_of(e) : 1.f;
 #pragma unroll
