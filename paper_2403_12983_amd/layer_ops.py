@@ -1,5 +1,5 @@
-"""The calls of include/osscar.h that run, serve, score and train on a pruned layer: gated feed-forward, 8-bit integer products,
-log probabilities.  Argument marshalling only, as in binding.py: the outputs and the workspace are torch tensors made here (on
+"""The calls of include/osscar.h that run, serve, score, repair and train on a pruned layer: gated feed-forward, 8-bit integer products,
+log probabilities, layer norm, low-rank adapters, AdamW.  Argument marshalling only, as in binding.py: the outputs and the workspace are torch tensors made here (on
 `stream`), everything is computed by the library, and no call waits for the GPU.
 
 Matrices are 2-D tensors on one GPU whose rows are contiguous; weights of a projection are d x f, and may lie in memory that way or as
