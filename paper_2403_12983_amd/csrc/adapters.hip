@@ -65,21 +65,28 @@ template <> struct Num<true> {
 };
 template <bool F32>
 __device__ __forceinline__ u32x4 packet(const char* row, int k) { return *reinterpret_cast<const u32x4_any*>(row + (int64_t)k * Num<F32>::ES); }
+// The same where the row ends: zeros from K on; read from a packet before the end on and moved to their places, but for rows of fewer elements
 template <bool F32>
-__device__ __forceinline__ u32x4 packet_some(const char* row, int k, int K) {      // zeros from K on
+__device__ __forceinline__ u32x4 packet_some(const char* row, int k, int K) {
+  constexpr int E = Num<F32>::E;
+  u32x4 x;
+  if (K >= E) {
+    const int at = min(k, K - E), s = k - at;
+    x = packet<F32>(row, at);
+    const int words = F32 ? s : s >> 1;
+    if (words & 2) x = u32x4{x[2], x[3], 0, 0};
+    if (words & 1) x = u32x4{x[1], x[2], x[3], 0};
+    if (!F32 && (s & 1)) x = u32x4{x[0] >> 16 | x[1] << 16, x[1] >> 16 | x[2] << 16, x[2] >> 16 | x[3] << 16, x[3] >> 16};
+    return s >= E ? u32x4{0, 0, 0, 0} : x;
+  }
   if constexpr (F32) {
     const uint32_t* p = reinterpret_cast<const uint32_t*>(row) + k;
-    u32x4 w;
 #pragma unroll
-    for (int e = 0; e < 4; e++) { w[e] = 0; if (k + e < K) w[e] = p[e]; }
-    return w;
+    for (int e = 0; e < 4; e++) { x[e] = 0; if (k + e < K) x[e] = p[e]; }
   } else {
-    const uint16_t* p = reinterpret_cast<const uint16_t*>(row) + k;
-    u16x8 w;
-#pragma unroll
-    for (int e = 0; e < 8; e++) { w[e] = 0; if (k + e < K) w[e] = p[e]; }
-    return __builtin_bit_cast(u32x4, w);
+    x = __builtin_bit_cast(u32x4, Eight<false>::load(row, k, K - k));
   }
+  return x;
 }
 
 // --------------------------------------------------------------------------------------------------
@@ -277,12 +284,12 @@ template <bool F32> struct Columns;
 template <> struct Columns<false> {
   static constexpr int STEP = 32, E = 8;
   u32x4 w[8];      // column c + t of eight components
-  __device__ __forceinline__ void load(const char* v, int64_t ld, int j, int rank, int c, bool whole, int most) {
+  __device__ __forceinline__ void load(const char* v, int64_t ld, int j, int rank, int c, bool whole, int C) {
     u16x8 x[E];
 #pragma unroll
     for (int k = 0; k < E; k++) {
-      const int64_t at = (int64_t)std::min(j + k, rank - 1) * ld + c;
-      x[k] = whole ? Eight<false>::load(v, at) : Eight<false>::load(v, at, most);
+      const int64_t row = (int64_t)std::min(j + k, rank - 1) * ld;
+      x[k] = whole ? Eight<false>::load(v, row + c) : edge_load<false>(v, row, c, C);
     }
 #pragma unroll
     for (int k = 0; k < E; k++)
@@ -301,12 +308,12 @@ template <> struct Columns<false> {
 template <> struct Columns<true> {
   static constexpr int STEP = 16, E = 4;
   float w[E][8];
-  __device__ __forceinline__ void load(const char* v, int64_t ld, int j, int rank, int c, bool whole, int most) {
+  __device__ __forceinline__ void load(const char* v, int64_t ld, int j, int rank, int c, bool whole, int C) {
     Eight<true>::type x[E];
 #pragma unroll
     for (int k = 0; k < E; k++) {
-      const int64_t at = (int64_t)std::min(j + k, rank - 1) * ld + c;
-      x[k] = whole ? Eight<true>::load(v, at) : Eight<true>::load(v, at, most);
+      const int64_t row = (int64_t)std::min(j + k, rank - 1) * ld;
+      x[k] = whole ? Eight<true>::load(v, row + c) : edge_load<true>(v, row, c, C);
     }
 #pragma unroll
     for (int k = 0; k < E; k++) {
@@ -389,7 +396,7 @@ __global__ __launch_bounds__(EW * 64, 2) void expand_kernel(Expand q, Pick pick)
 #pragma unroll
         for (int d = 0; d < 4; d++) {
           const int row = sub * 16 + g * 4 + d;
-          if (rows >> row & 1) w.base[d] = whole ? E8::load(q.base.p, (row0 + row) * q.base.ld + c) : E8::load(q.base.p, (row0 + row) * q.base.ld + c, most);
+          if (rows >> row & 1) w.base[d] = whole ? E8::load(q.base.p, (row0 + row) * q.base.ld + c) : edge_load<F32>(q.base.p, (row0 + row) * q.base.ld, c, q.C);
         }
       }
       const int row = sub * 16 + i;
@@ -428,7 +435,7 @@ __global__ __launch_bounds__(EW * 64, 2) void expand_kernel(Expand q, Pick pick)
     Cols cols[HELD];
     if (rank > 0) {
 #pragma unroll
-      for (int k = 0; k < KS; k++) cols[k].load(v, q.v.ld, k * STEP + g * E, rank, c, whole, most);
+      for (int k = 0; k < KS; k++) cols[k].load(v, q.v.ld, k * STEP + g * E, rank, c, whole, q.C);
     }
     while (sub < q.subs) {
       const int after = next(sub + 1);
@@ -451,7 +458,7 @@ __global__ __launch_bounds__(EW * 64, 2) void expand_kernel(Expand q, Pick pick)
           if (rows >> row & 1) t_values<E>(q.t + (row0 + row) * pick.rank, j0 + g * E, pick.rank, x);
           finish(sub, j0 + g * E, x);
           if (j0 < rank) {
-            cols[0].load(v, q.v.ld, j0 + g * E, rank, c, whole, most);
+            cols[0].load(v, q.v.ld, j0 + g * E, rank, c, whole, q.C);
             cols[0].multiply(x, acc);
           }
         }
@@ -549,7 +556,7 @@ __global__ __launch_bounds__(256) void expand_few_kernel(Expand q, Pick pick) {
   const int64_t row = blockIdx.y;
   const int e = pick.of(row);
   typename E8::type base{};
-  if (q.base.p && wave == 0) base = E8::load(q.base.p, row * q.base.ld + c, most);
+  if (q.base.p && wave == 0) base = whole ? E8::load(q.base.p, row * q.base.ld + c) : edge_load<F32>(q.base.p, row * q.base.ld, c, q.C);
   const int rank = e < 0 ? 0 : pick.rank_of(e);
   const float s = e >= 0 && q.scaled ? pick.scale_of(e) : 1.f;
   const char* v = reinterpret_cast<const char*>(q.v.p) + std::max(e, 0) * q.v.next * ES;
@@ -562,7 +569,7 @@ __global__ __launch_bounds__(256) void expand_few_kernel(Expand q, Pick pick) {
     typename E8::type w[16];
     if (j0 < rank) {
 #pragma unroll
-      for (int k = 0; k < 16; k++) w[k] = whole ? E8::load(v, std::min(j0 + k, rank - 1) * q.v.ld + c) : E8::load(v, std::min(j0 + k, rank - 1) * q.v.ld + c, most);
+      for (int k = 0; k < 16; k++) w[k] = whole ? E8::load(v, std::min(j0 + k, rank - 1) * q.v.ld + c) : edge_load<F32>(v, std::min(j0 + k, rank - 1) * q.v.ld, c, q.C);
 #pragma unroll
       for (int p = 0; p < PARTS_MOST; p++) part[p] = q.t[((int64_t)std::min(p, q.parts - 1) * q.n + row) * pick.rank + std::min(j, rank - 1)];
 #pragma unroll
@@ -798,7 +805,7 @@ __global__ __launch_bounds__(OW * 64) void outer_kernel(Outers both, Plan plan, 
     for (int k = 0; k < NZ; k++) {
       const int at = b + zr + k * (OW * 64 / (OCOLS / 8)), c = c0 + zc * 8;
       const int64_t row = plan.order ? plan.order[min(at, h.end - 1)] : min(at, h.end - 1);
-      z[k] = whole ? E8::load(q.z.p, row * q.z.ld + c) : E8::load(q.z.p, row * q.z.ld + c, q.C - c);
+      z[k] = whole ? E8::load(q.z.p, row * q.z.ld + c) : edge_load<F32>(q.z.p, row * q.z.ld, c, q.C);
       if (at >= h.end) z[k] = typename E8::type{};
     }
     const int at = b + tr;

@@ -92,6 +92,31 @@ template <> struct Eight<true> {
   }
 };
 
+// Eight elements of a row from its c-th, in the wave that the row ends in, without a branch for each of them (what is past the end is anything): bf16 from eight before the end on and
+// moved to their places, float32 (where that is 24 moves) one by one, the last one again past the end.  A row of fewer than eight bf16 is read one by one.
+template <bool F32>
+__device__ __forceinline__ typename Eight<F32>::type edge_load(const void* p, int64_t row_at, int c, int C) {
+  if constexpr (F32) {
+    const float* q = reinterpret_cast<const float*>(p) + row_at;
+    typename Eight<true>::type w;
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+      w.a[e] = q[min(c + e, C - 1)];
+      w.b[e] = q[min(c + e + 4, C - 1)];
+    }
+    return w;
+  } else {
+    if (C < 8) return Eight<false>::load(p, row_at + c, C - c);
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    const int at = min(c, C - 8), s = c - at;
+    u32x4 x = __builtin_bit_cast(u32x4, Eight<false>::load(p, row_at + at));
+    if (s & 4) x = u32x4{x[2], x[3], x[3], x[3]};
+    if (s & 2) x = u32x4{x[1], x[2], x[3], x[3]};
+    if (s & 1) x = u32x4{x[0] >> 16 | x[1] << 16, x[1] >> 16 | x[2] << 16, x[2] >> 16 | x[3] << 16, x[3] >> 16};
+    return __builtin_bit_cast(u16x8, x);
+  }
+}
+
 // C neighbouring values of a row, of which the ones before `most` exist
 template <int C>
 __device__ __forceinline__ void put_bf16(uint16_t* p, const float (&v)[C], int most) {
