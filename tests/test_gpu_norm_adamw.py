@@ -90,7 +90,7 @@ def _check_norm(pkg, X, w, b, dY, eps=1e-5, **kw):
 
 
 NORMS = [(1, 1), (3, 2), (2, 7), (1, 8), (5, 9), (7, 63), (40, 64), (33, 257), (1, 2048), (9, 512), (1030, 513), (64, 1024), (17, 1365), (2100, 2048), (5, 2049), (12, 4096), (130, 5461),
-         (300, 7168), (3, 8193), (9, 14336), (2, 16384), (3, 16385), (2, 40001), (700, 64), (333, 65), (1000, 100), (257, 128), (600, 130), (129, 255), (77, 256)]
+         (300, 7168), (3, 8193), (9, 14336), (2, 16384), (3, 16385), (2, 40001), (700, 64), (333, 65), (1000, 100), (257, 128), (600, 130), (129, 255), (77, 256), (21, 1536), (300, 1537), (19, 2500), (7, 4999), (600, 6144), (9, 7169), (5, 9001), (11, 11008), (530, 12289), (4, 14337)]
 
 
 @pytest.mark.parametrize("dtype,w_dtype", [(BF16, BF16), (F32, F32), (BF16, F32), (F32, BF16)])
