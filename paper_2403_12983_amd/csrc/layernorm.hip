@@ -2,6 +2,9 @@
 #include "ops.h"
 #include <float.h>
 
+// Products and sums are rounded each, but where fmaf says otherwise: the mean that is kept has to be the one that was taken off (a row of one value is then zero in the backward pass too).
+#pragma clang fp contract(off)
+
 using namespace osscar;
 
 namespace {
@@ -176,7 +179,7 @@ __global__ __launch_bounds__(TPR* GROUPS) void backward_kernel(const void* X, co
         }
         g[k][e] *= w[HOLD ? k : 0][e];
         s += e >= at.skip ? g[k][e] : 0.f;
-        s2 += e >= at.skip ? g[k][e] * h[k][e] : 0.f;
+        s2 = e >= at.skip ? fmaf(g[k][e], h[k][e], s2) : s2;
       }
     }
     if (HOLD && row + step < q.n) fetch(row + step);
@@ -190,7 +193,7 @@ __global__ __launch_bounds__(TPR* GROUPS) void backward_kernel(const void* X, co
         const At at(k, tid, q.d);
         float dx[8];
 #pragma unroll
-        for (int e = 0; e < 8; e++) dx[e] = rstd * (g[k][e] - s - h[k][e] * s2);
+        for (int e = 0; e < 8; e++) dx[e] = rstd * fmaf(-h[k][e], s2, g[k][e] - s);
         if (at.in) E8::store(dX, row * lddx + at.at, dx);
       }
     }
@@ -324,7 +327,7 @@ __global__ __launch_bounds__(1024) void long_backward_kernel(const void* X, cons
     s2 *= inv;
     each([&](int at) {
 #pragma unroll
-      for (int e = 0; e < 8; e++) g[e] = rstd * (g[e] - s - h[e] * s2);
+      for (int e = 0; e < 8; e++) g[e] = rstd * fmaf(-h[e], s2, g[e] - s);
       E8::store(dX, row * lddx + at, g, q.d - at);
     });
   }

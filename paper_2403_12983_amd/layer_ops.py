@@ -485,11 +485,14 @@ _BLOCK = 256
 
 def _place(t: torch.Tensor) -> Tuple[Tuple[int, ...], Tuple[int, ...]]:
     """Shape, and strides where they say something."""
-    return tuple(t.shape), tuple(s for k, s in zip(t.shape, t.stride()) if k > 1)
+    shape, stride = t.shape, t.stride()
+    return shape, stride if 1 not in shape else tuple(s for k, s in zip(shape, stride) if k > 1)
 
 
 def _dense(t: torch.Tensor) -> bool:
     """Whether the elements fill a piece of memory, in any order of the dimensions."""
+    if t.is_contiguous():
+        return True
     at = 1
     for stride, size in sorted((s, k) for s, k in zip(t.stride(), t.shape) if k > 1):
         if stride != at:
@@ -544,7 +547,9 @@ class AdamW:
         written = []      # (address, end, parameter) of what a step writes
         for k, (p, master) in enumerate(zip(self.params, self.masters)):
             n = p.numel()
-            code = _code(p, f"parameter {k}")
+            code = _CODES.get(p.dtype)
+            if code is None:
+                _refuse(f"parameter {k} is neither float32 nor bfloat16")
             if not _dense(p):
                 _refuse(f"the elements of parameter {k} are not side by side")
             if master is not None and (p.dtype != torch.bfloat16 or master.dtype != torch.float32 or _place(master) != self._places[k]):
@@ -556,10 +561,15 @@ class AdamW:
             for t, size, dtypes in kinds:
                 if t is None or t.numel() != size or t.dtype not in dtypes or not t.is_contiguous():
                     _refuse(f"state {k} is not of {bits} bits and parameter {k}'s size, side by side")
-            _on(self._index, **{f"parameter {k}": p, f"master {k}": master, f"state {k}": s.m, f"state {k}'s v": s.v, f"state {k}'s m_scale": s.m_scale, f"state {k}'s v_scale": s.v_scale})
             for t in (p, master, *s):
-                if t is not None and t.numel() > 0:
-                    written.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), k))
+                if t is None:
+                    continue
+                if t.get_device() != self._index:
+                    _refuse(f"parameter {k}, its master or its state is on {t.device}, expected cuda:{self._index}")
+                size = t.numel()
+                if size > 0:
+                    at = t.data_ptr()
+                    written.append((at, at + size * t.element_size(), k))
             self.states.append(s)
             self._table[k] = _AdamWTensor(n, p.data_ptr(), None if master is None else master.data_ptr(), None, s.m.data_ptr(), s.v.data_ptr(),
                                           s.m_scale.data_ptr() if bits == 8 else None, s.v_scale.data_ptr() if bits == 8 else None, code, 0)
@@ -583,13 +593,14 @@ class AdamW:
         if len(grads) != len(self.params):
             _refuse("one gradient per parameter")
         for k, g in enumerate(grads):
-            _code(g, f"gradient {k}")
+            if g.dtype not in _CODES:
+                _refuse(f"gradient {k} is neither float32 nor bfloat16")
             if _place(g) != self._places[k]:
                 _refuse(f"gradient {k} has another shape or layout than its parameter")
             if g.get_device() != self._index:
                 _refuse(f"gradient {k} is on {g.device}, expected cuda:{self._index}")
-        for k, g in enumerate(grads):
-            self._table[k].g, self._table[k].g_dtype = g.data_ptr(), _CODES[g.dtype]
+        for row, g in zip(self._table, grads):
+            row.g, row.g_dtype = g.data_ptr(), _CODES[g.dtype]
         self.grads = grads
 
     def _scalar(self, t: torch.Tensor, dtype: torch.dtype, what: str) -> int:

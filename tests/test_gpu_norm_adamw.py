@@ -156,6 +156,11 @@ def test_layernorm_of_rows_far_from_zero_and_constant_rows(osscar, d):
     X[4] = 1e15 * _randn(g, d)
     Y, stats, _ = _check_norm(osscar, X, None, None, _randn(g, 6, d))
     assert Y[2].abs().max() == 0 and Y[1].abs().max() < 1e-4 and stats[2].tolist() == pytest.approx([0, 1e5 ** 0.5])
+    # rows of one value: the kept mean is that value, and they have no part in the gain's gradient
+    X = torch.tensor([1.0, 123.456, -7e-5, 3e8], device=DEV)[:, None].expand(4, d).contiguous()
+    Y, stats = osscar.osscar_layernorm_forward(X, save=True)
+    assert torch.equal(stats[:, 0], X[:, 0]) and not Y.any()
+    assert not osscar.osscar_layernorm_backward(X, None, _randn(g, 4, d), stats)[1].any()
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
