@@ -94,7 +94,7 @@ __device__ __forceinline__ u32x4 packet_some(const char* row, int k, int K) {
 // --------------------------------------------------------------------------------------------------
 // A workgroup takes 16 RT rows and 16 CT components; its waves take the contraction in turns, parts of it are a workgroup's each (their sums are added where T is
 // read).  Operands go from memory to registers, the next turn's while one is multiplied.  The instruction wants 64 bytes of each of 16 rows in a packet of its lanes, which memory
-// answers in requests of 64 bytes: rows of Z are fetched 128 or 256 bytes at a time and change lanes through LDS, a piece of it for every wave (8192 x 14336, rank 32: 83 us without, 72 with).
+// answers in requests of 64 bytes: rows of Z are fetched 128 bytes at a time and change lanes through LDS, a piece of it for every wave (8192 x 14336, rank 32: 83 us without, 72 with).
 constexpr int FW = 4;      // waves of the kernel for few rows
 struct Contract {
   Mat z;
@@ -105,11 +105,11 @@ struct Contract {
 };
 constexpr int CW = 8;      // waves
 constexpr int RT = 2;      // row tiles of 16 in a workgroup (with four, half as many reads of V, it takes as long: 75 us instead of 74 at rank 32; with rank 64 they do not fit the registers)
-constexpr int turn_of(bool f32, int ct) { return f32 || RT * ct > 4 ? 2 : 4; }      // instructions' worth of a row in a turn
+constexpr int U = 2;       // instructions' worth of a row in a turn (four, rows 256 bytes at a time: with bf16 and two column tiles 24 registers too many, 6000 x 2048 x 8192 rank 32 forward 52 us instead of 48; with one no difference)
 template <bool F32, int CT>
 __global__ __launch_bounds__(CW * 64) void contract_kernel(Contract q, Pick pick) {
   typedef Num<F32> N;
-  constexpr int U = turn_of(F32, CT), TURN = U * N::STEP, ROWS = RT * 16, COLS = CT * 16;
+  constexpr int TURN = U * N::STEP, ROWS = RT * 16, COLS = CT * 16;
   constexpr int NC = U * 4, PER = 64 / NC, ROW = NC * 16;      // packets of a row in a turn, rows of one load, bytes of a row
   constexpr int SUMS = CW / 2 * ROWS * (COLS + 1) * 4, TURNS = CW * ROWS * ROW;
   __shared__ __align__(16) char lds[SUMS > TURNS ? SUMS : TURNS];
@@ -346,10 +346,12 @@ __device__ __forceinline__ void t_values(const float* t, int j, int rank, float 
 }
 // A wave takes 128 columns of up to 64 rows, 16 at a time: lane (i, g) reads eight columns c0 + 8 i .. of components 8 g .. and turns them in its registers, so that
 // the instruction for tile t has columns c0 + 8 i + t; the results of a lane are then eight neighbouring columns of four rows.  The columns stay in registers for all rows of their
-// adapter (KS steps of components; 0: more than that, read again for each 16 rows), the next 16 rows' base and T are on their way while those before are multiplied.
+// adapter (KS steps of components; 0: more than that, read again for each 16 rows), the next 16 rows' base and T are on their way while those before are multiplied (AHEAD).
+// Float32 of up to 16 components without AHEAD takes 165 registers instead of 192, so that a third wave fits: better where a workgroup has one or two tiles of 16 rows (777 rows of three adapters,
+// 1365 x 5461, rank 12: 28.6 us instead of 32.3 forward, 2000 41.7 instead of 44.7), worse with four (6000 sorted rows 97.6 instead of 91.7); bf16 gains nothing by it.
 // 8192 x 14336 bf16, rank 32: 90 us (base and y 470 MB, 5.2 TB/s; 16 and 32 rows at a time without that: 193); 6000 x 8192, rank 64: 52 us (3.8 TB/s).
-template <bool F32, int KS, bool PARTS>
-__global__ __launch_bounds__(EW * 64, 2) void expand_kernel(Expand q, Pick pick) {
+template <bool F32, int KS, bool PARTS, bool AHEAD>
+__global__ __launch_bounds__(EW * 64, AHEAD ? 2 : 3) void expand_kernel(Expand q, Pick pick) {
   typedef Eight<F32> E8;
   typedef Columns<F32> Cols;
   constexpr int STEP = Cols::STEP, E = Cols::E, HELD = KS > 0 ? KS : 1;
@@ -439,7 +441,7 @@ __global__ __launch_bounds__(EW * 64, 2) void expand_kernel(Expand q, Pick pick)
     }
     while (sub < q.subs) {
       const int after = next(sub + 1);
-      if (after < q.subs) fetch(after, then);
+      if (AHEAD && after < q.subs) fetch(after, then);
       v4f acc[8];
 #pragma unroll
       for (int t = 0; t < 8; t++) acc[t] = v4f{0, 0, 0, 0};
@@ -475,7 +477,8 @@ __global__ __launch_bounds__(EW * 64, 2) void expand_kernel(Expand q, Pick pick)
           else E8::store(q.y, (row0 + row) * q.ldy + c, y, most);
         }
       }
-      now = then;
+      if (AHEAD) now = then;
+      else if (after < q.subs) fetch(after, now);
       sub = after;
     }
   });
@@ -885,7 +888,7 @@ Deal deal(int64_t n, int64_t K, int count, int rank, bool f32, bool index) {
   if (n <= few_of(index)) return Deal{true, 0, (int)std::min<int64_t>(PARTS_MOST, up(K, FW * 512)), 1, n};
   Deal d{false, rank <= 16 ? 1 : rank <= 32 ? 2 : 4, 1, 1, up(n, 16 * RT)};
   if (index) d.slots = (int)std::max<int64_t>(1, std::min<int64_t>({256 / d.tiles, 16 * RT, count}));
-  const int64_t turns = up(K, turn_of(f32, d.ct) * (f32 ? 16 : 32)), blocks = d.tiles * d.slots * up(rank, 16 * d.ct);
+  const int64_t turns = up(K, U * (f32 ? 16 : 32)), blocks = d.tiles * d.slots * up(rank, 16 * d.ct);
   d.parts = (int)std::max<int64_t>(1, std::min<int64_t>({256 / blocks, up(turns, 2 * CW), PARTS_MOST}));
   return d;
 }
@@ -916,9 +919,11 @@ void expand(const Expand& q, const Pick& pick, hipStream_t s) {
   const dim3 grid((unsigned)(tiles * blocks), (unsigned)a.slots), block(EW * 64);
   auto go = [&](auto parts) {
     constexpr bool PARTS = decltype(parts)::value;
-    if (pick.rank <= Columns<F32>::STEP) hipLaunchKernelGGL((expand_kernel<F32, 1, PARTS>), grid, block, 0, s, a, pick);
-    else if (pick.rank <= 2 * Columns<F32>::STEP) hipLaunchKernelGGL((expand_kernel<F32, 2, PARTS>), grid, block, 0, s, a, pick);
-    else hipLaunchKernelGGL((expand_kernel<F32, 0, PARTS>), grid, block, 0, s, a, pick);
+    if (pick.rank <= Columns<F32>::STEP) {
+      if (F32 && a.subs < 4) hipLaunchKernelGGL((expand_kernel<F32, 1, PARTS, !F32>), grid, block, 0, s, a, pick);
+      else hipLaunchKernelGGL((expand_kernel<F32, 1, PARTS, true>), grid, block, 0, s, a, pick);
+    } else if (pick.rank <= 2 * Columns<F32>::STEP) hipLaunchKernelGGL((expand_kernel<F32, 2, PARTS, true>), grid, block, 0, s, a, pick);
+    else hipLaunchKernelGGL((expand_kernel<F32, 0, PARTS, true>), grid, block, 0, s, a, pick);
   };
   if (a.parts > 1) go(std::true_type{});
   else go(std::false_type{});
