@@ -24,6 +24,7 @@ struct Pick {
   const float* scale;
   const int32_t* ranks;
   int count, rank;
+  const int2* order;      // which row, of which adapter, lies at which place of the tiles (NULL: as they are)
   __device__ __forceinline__ int of(int64_t row) const {      // -1: none; -2: there is no such adapter
     if (!index) return 0;
     const int64_t e = index[row];
@@ -106,7 +107,7 @@ struct Contract {
 constexpr int CW = 8;      // waves
 constexpr int RT = 2;      // row tiles of 16 in a workgroup (with four, half as many reads of V, it takes as long: 75 us instead of 74 at rank 32; with rank 64 they do not fit the registers)
 constexpr int U = 2;       // instructions' worth of a row in a turn (four, rows 256 bytes at a time: with bf16 and two column tiles 24 registers too many, 6000 x 2048 x 8192 rank 32 forward 52 us instead of 48; with one no difference)
-template <bool F32, int CT>
+template <bool F32, int CT, bool SORTED>
 __global__ __launch_bounds__(CW * 64) void contract_kernel(Contract q, Pick pick) {
   typedef Num<F32> N;
   constexpr int TURN = U * N::STEP, ROWS = RT * 16, COLS = CT * 16;
@@ -118,13 +119,16 @@ __global__ __launch_bounds__(CW * 64) void contract_kernel(Contract q, Pick pick
   const int64_t tiles = (q.n + ROWS - 1) / ROWS, row0 = (blockIdx.x % tiles) * ROWS;
   const int slot = (int)(blockIdx.x / tiles), part = blockIdx.y, j0 = blockIdx.z * COLS;
   const int have = (int)std::min<int64_t>(ROWS, q.n - row0);
-  const int mine = lane < have ? pick.of(row0 + lane) : -1;
+  const int2 at = SORTED && lane < have ? pick.order[row0 + lane] : int2{0, -1};
+  const int line = at.x;
+  auto row_of = [&](int r) -> int64_t { return SORTED ? __shfl(line, r, 64) : row0 + r; };      // (by all lanes)
+  const int mine = SORTED ? at.y : lane < have ? pick.of(row0 + lane) : -1;
   float* t = q.t + (int64_t)part * q.n * pick.rank;
   if (slot == q.slots - 1) {      // rows without an adapter (by the slot that is likeliest to have none itself)
     const uint64_t none = __ballot(mine < 0);
     for (int k = threadIdx.x; k < have * COLS; k += CW * 64) {
       const int r = k / COLS, j = j0 + k % COLS;
-      if ((none >> r & 1) && j < pick.rank) t[(row0 + r) * pick.rank + j] = 0.f;
+      if ((none >> r & 1) && j < pick.rank) t[(SORTED ? pick.order[row0 + r].x : row0 + r) * pick.rank + j] = 0.f;
     }
   }
   each_adapter(mine, slot, q.slots, [&](int e, uint64_t rows) {
@@ -135,7 +139,7 @@ __global__ __launch_bounds__(CW * 64) void contract_kernel(Contract q, Pick pick
 #pragma unroll
       for (int u = 0; u < U; u++) {      // (rows of other adapters: one of this one's again, not used)
         const int row = r * 16 + u * PER + lane / NC, at = rows >> row & 1 ? row : first;
-        zr[r][u] = reinterpret_cast<const char*>(q.z.p) + (row0 + at) * q.z.ld * N::ES;
+        zr[r][u] = reinterpret_cast<const char*>(q.z.p) + row_of(at) * q.z.ld * N::ES;
       }
     const int zk = lane % NC * N::E;
     char* mine_lds = lds + wave * ROWS * ROW;
@@ -224,11 +228,12 @@ __global__ __launch_bounds__(CW * 64) void contract_kernel(Contract q, Pick pick
 #pragma unroll
         for (int d = 0; d < 4; d++) {
           const int row = r * 16 + g * 4 + d;
+          const int64_t to = row_of(row);
           if (rows >> row & 1) {
 #pragma unroll
             for (int c = 0; c < CT; c++) {
               const int j = j0 + c * 16 + i;
-              if (j < pick.rank) t[(row0 + row) * pick.rank + j] = j < rank ? acc[r][c][d] * s : 0.f;
+              if (j < pick.rank) t[to * pick.rank + j] = j < rank ? acc[r][c][d] * s : 0.f;
             }
           }
         }
@@ -350,7 +355,7 @@ __device__ __forceinline__ void t_values(const float* t, int j, int rank, float 
 // Float32 of up to 16 components without AHEAD takes 165 registers instead of 192, so that a third wave fits: better where a workgroup has one or two tiles of 16 rows (777 rows of three adapters,
 // 1365 x 5461, rank 12: 28.6 us instead of 32.3 forward, 2000 41.7 instead of 44.7), worse with four (6000 sorted rows 97.6 instead of 91.7); bf16 gains nothing by it.
 // 8192 x 14336 bf16, rank 32: 90 us (base and y 470 MB, 5.2 TB/s; 16 and 32 rows at a time without that: 193); 6000 x 8192, rank 64: 52 us (3.8 TB/s).
-template <bool F32, int KS, bool PARTS, bool AHEAD>
+template <bool F32, int KS, bool PARTS, bool AHEAD, bool SORTED>
 __global__ __launch_bounds__(EW * 64, AHEAD ? 2 : 3) void expand_kernel(Expand q, Pick pick) {
   typedef Eight<F32> E8;
   typedef Columns<F32> Cols;
@@ -361,7 +366,11 @@ __global__ __launch_bounds__(EW * 64, AHEAD ? 2 : 3) void expand_kernel(Expand q
   const int c0 = (blockIdx.x % blocks) * (EW * ECOLS) + wave * ECOLS, slot = blockIdx.y, c = c0 + i * 8;
   if (c0 >= q.C) return;
   const int have = (int)std::min<int64_t>(rows_a_tile, q.n - row0), most = q.C - c;
-  const int mine = lane < have ? pick.of(row0 + lane) : -1;
+  const int2 at = SORTED && lane < have ? pick.order[row0 + lane] : int2{0, -1};
+  const int line = at.x;
+  auto row_of = [&](int r) -> int64_t { return SORTED ? __shfl(line, r, 64) : row0 + r; };      // (by all lanes)
+  auto line_of = [&](int r) -> int64_t { return SORTED ? pick.order[row0 + r].x : row0 + r; };    // (by any)
+  const int mine = SORTED ? at.y : lane < have ? pick.of(row0 + lane) : -1;
   const bool whole = c0 + ECOLS <= q.C, keeps = q.t_out && c0 == 0;
   constexpr size_t ES = F32 ? 4 : 2;
   if (slot == q.slots - 1) {      // rows without an adapter (by the slot that is likeliest to have none itself)
@@ -369,18 +378,19 @@ __global__ __launch_bounds__(EW * 64, AHEAD ? 2 : 3) void expand_kernel(Expand q
     const uint64_t wrong = __ballot(mine == -2);
     if (keeps)
       for (int k = lane; k < have * pick.rank; k += 64)
-        if (none >> (k / pick.rank) & 1) q.t_out[row0 * pick.rank + k] = 0.f;
+        if (none >> (k / pick.rank) & 1) q.t_out[line_of(k / pick.rank) * pick.rank + k % pick.rank] = 0.f;
     if (q.y == q.base.p) none = wrong;
     while (none) {      // four at a time, one for each group of lanes
       int r = -1;
       for (int k = 0; k < 4 && none; k++, none &= none - 1)
         if (g == k) r = __ffsll((unsigned long long)none) - 1;
       if (r >= 0 && most > 0) {
+        const int64_t row = line_of(r);
         float y[8];
-        if (q.base.p) E8::values(E8::load(q.base.p, (row0 + r) * q.base.ld + c, most), y);
+        if (q.base.p) E8::values(E8::load(q.base.p, row * q.base.ld + c, most), y);
 #pragma unroll
         for (int t = 0; t < 8; t++) y[t] = wrong >> r & 1 ? NAN : q.base.p ? y[t] : 0.f;
-        E8::store(q.y, (row0 + r) * q.ldy + c, y, most);
+        E8::store(q.y, row * q.ldy + c, y, most);
       }
     }
   }
@@ -398,25 +408,28 @@ __global__ __launch_bounds__(EW * 64, AHEAD ? 2 : 3) void expand_kernel(Expand q
 #pragma unroll
         for (int d = 0; d < 4; d++) {
           const int row = sub * 16 + g * 4 + d;
-          if (rows >> row & 1) w.base[d] = whole ? E8::load(q.base.p, (row0 + row) * q.base.ld + c) : edge_load<F32>(q.base.p, (row0 + row) * q.base.ld, c, q.C);
+          const int64_t from = row_of(row);
+          if (rows >> row & 1) w.base[d] = whole ? E8::load(q.base.p, from * q.base.ld + c) : edge_load<F32>(q.base.p, from * q.base.ld, c, q.C);
         }
       }
       const int row = sub * 16 + i;
+      const int64_t from = row_of(row);
 #pragma unroll
       for (int k = 0; k < KS; k++) {
 #pragma unroll
         for (int x = 0; x < E; x++) w.x[k][x] = 0.f;
-        if (rows >> row & 1) t_values<E>(q.t + (row0 + row) * pick.rank, k * STEP + g * E, pick.rank, w.x[k]);
+        if (rows >> row & 1) t_values<E>(q.t + from * pick.rank, k * STEP + g * E, pick.rank, w.x[k]);
       }
     };
     // T of a row: the other parts, kept where that is asked for, components past the rank left out, scaled
     auto finish = [&](int sub, int j, float (&x)[E]) {
       const int row = sub * 16 + i;
+      const int64_t from = row_of(row);
       if (rows >> row & 1) {
         if constexpr (PARTS) {      // (all on their way together: few rows wait for each load)
           float more[PARTS_MOST - 1][E];
 #pragma unroll
-          for (int p = 1; p < PARTS_MOST; p++) t_values<E>(q.t + ((int64_t)std::min(p, q.parts - 1) * q.n + row0 + row) * pick.rank, j, pick.rank, more[p - 1]);
+          for (int p = 1; p < PARTS_MOST; p++) t_values<E>(q.t + ((int64_t)std::min(p, q.parts - 1) * q.n + from) * pick.rank, j, pick.rank, more[p - 1]);
 #pragma unroll
           for (int p = 1; p < PARTS_MOST; p++)
 #pragma unroll
@@ -425,7 +438,7 @@ __global__ __launch_bounds__(EW * 64, AHEAD ? 2 : 3) void expand_kernel(Expand q
         if (keeps) {
 #pragma unroll
           for (int k = 0; k < E; k++)
-            if (j + k < pick.rank) q.t_out[(row0 + row) * pick.rank + j + k] = x[k];
+            if (j + k < pick.rank) q.t_out[from * pick.rank + j + k] = x[k];
         }
       }
 #pragma unroll
@@ -453,11 +466,12 @@ __global__ __launch_bounds__(EW * 64, AHEAD ? 2 : 3) void expand_kernel(Expand q
         }
       } else {
         const int row = sub * 16 + i;
+        const int64_t from = row_of(row);
         for (int j0 = 0; j0 < (keeps ? pick.rank : rank); j0 += STEP) {
           float x[E];
 #pragma unroll
           for (int k = 0; k < E; k++) x[k] = 0.f;
-          if (rows >> row & 1) t_values<E>(q.t + (row0 + row) * pick.rank, j0 + g * E, pick.rank, x);
+          if (rows >> row & 1) t_values<E>(q.t + from * pick.rank, j0 + g * E, pick.rank, x);
           finish(sub, j0 + g * E, x);
           if (j0 < rank) {
             cols[0].load(v, q.v.ld, j0 + g * E, rank, c, whole, q.C);
@@ -468,13 +482,14 @@ __global__ __launch_bounds__(EW * 64, AHEAD ? 2 : 3) void expand_kernel(Expand q
 #pragma unroll
       for (int d = 0; d < 4; d++) {
         const int row = sub * 16 + g * 4 + d;
+        const int64_t to = row_of(row);
         if (rows >> row & 1) {
           float y[8];
           if (q.base.p) E8::values(now.base[d], y);
 #pragma unroll
           for (int t = 0; t < 8; t++) y[t] = q.base.p ? y[t] + acc[t][d] : acc[t][d];
-          if (whole) E8::store(q.y, (row0 + row) * q.ldy + c, y);
-          else E8::store(q.y, (row0 + row) * q.ldy + c, y, most);
+          if (whole) E8::store(q.y, to * q.ldy + c, y);
+          else E8::store(q.y, to * q.ldy + c, y, most);
         }
       }
       if (AHEAD) now = then;
@@ -632,22 +647,39 @@ struct Plan {
   __device__ __forceinline__ int all(int count) const { return order ? first[count] : total; }
 };
 // One workgroup; waves take the rows in spans, in order, so that an adapter's rows keep theirs.  Each wave counts its span by adapter; after sums over waves
-// and adapters it goes over the span again, 64 rows at a time, and gives rows of one adapter their places together.  777 rows of 3 adapters 4 us.
+// and adapters it goes over the span again, 64 rows at a time, and gives rows of one adapter their places together.  Rows without one come last (in `places` alone).  A lane finds the
+// others with its adapter by the bits of the number: with a turn for each adapter, and sums in LDS by atomics, 16384 rows of 1000 adapters took 89 us more.  777 rows of 3 adapters 4 us.
 constexpr int PLAN_WORDS = 32768;      // of LDS: counts by wave and adapter
 static_assert(OSSCAR_ADAPTERS_MAX * 2 <= PLAN_WORDS, "");
-__global__ __launch_bounds__(1024) void plan_kernel(Pick pick, int n, int waves, uint32_t rows_a_chunk, int* order, Chunk* chunks, int* first) {
+__global__ __launch_bounds__(1024) void plan_kernel(Pick pick, int n, int waves, uint32_t rows_a_chunk, int2* places, int* order, Chunk* chunks, int* first) {
   __shared__ uint32_t counts[PLAN_WORDS];
-  __shared__ uint32_t wave_rows[16], wave_chunks[16];
+  __shared__ uint32_t wave_rows[16], wave_chunks[16], wave_none[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, count = pick.count;
   for (int k = threadIdx.x; k < waves * count; k += 1024) counts[k] = 0;
   __syncthreads();
   const int span = ((n + waves - 1) / waves + 63) / 64 * 64;
   const int64_t begin = (int64_t)wave * span, end = std::min<int64_t>(n, begin + span);
-  if (wave < waves)
-    for (int64_t r = begin + lane; r < end; r += 64) {
-      const int e = pick.of(r);
-      if (e >= 0) atomicAdd(&counts[wave * count + e], 1u);      // (whole numbers: any order)
+  const int bits = 32 - __clz(count);
+  auto same = [&](int mine) {      // the lanes whose rows have this one's adapter (one bit of its number after the other; -1 and -2 are none)
+    uint64_t rows = __ballot(mine >= 0);
+    for (int b = 0; b < bits; b++) {
+      const uint64_t set = __ballot(mine >> b & 1);
+      rows &= mine >> b & 1 ? set : ~set;
     }
+    return rows;
+  };
+  const uint64_t below = (1ull << lane) - 1;
+  uint32_t none = 0;
+  if (wave < waves)
+    for (int64_t r0 = begin; r0 < end; r0 += 64) {
+      const int mine = r0 + lane < end ? pick.of(r0 + lane) : -1;
+      const uint64_t rows = same(mine);
+      if (mine >= 0 && !(rows & below)) counts[wave * count + mine] += __popcll(rows);      // (this wave's own word)
+      if (mine < 0 && r0 + lane < end) none++;
+      __builtin_amdgcn_wave_barrier();
+    }
+  for (int o = 32; o > 0; o >>= 1) none += __shfl_xor(none, o, 64);
+  if (lane == 0) wave_none[wave] = none;
   __syncthreads();
   // places of adapters, `each` of them a thread: rows before, chunks before
   const int each = (count + 1023) / 1024;
@@ -672,26 +704,34 @@ __global__ __launch_bounds__(1024) void plan_kernel(Pick pick, int n, int waves,
   for (int k = 0; k < each; k++) {
     const int e = threadIdx.x * each + k;
     if (e >= count) break;
-    first[e] = (int)chunk;
+    if (first) first[e] = (int)chunk;
     const uint32_t from = at;
     for (int w = 0; w < waves; w++) {
       const uint32_t s = counts[w * count + e];
       counts[w * count + e] = at;
       at += s;
     }
-    for (uint32_t b = from; b < at; b += rows_a_chunk) chunks[chunk++] = Chunk{e, (int)b, (int)min(at, b + rows_a_chunk)};
-    if (e == count - 1) first[count] = (int)chunk;
+    for (uint32_t b = from; first && b < at; b += rows_a_chunk) chunks[chunk++] = Chunk{e, (int)b, (int)min(at, b + rows_a_chunk)};
+    if (first && e == count - 1) first[count] = (int)chunk;
   }
   __syncthreads();
   if (wave >= waves) return;
+  uint32_t last = 0;      // rows without an adapter lie behind all others
+  for (int w = 0; w < 16; w++) last += wave_rows[w] + (w < wave ? wave_none[w] : 0);
   for (int64_t r0 = begin; r0 < end; r0 += 64) {
     const int mine = r0 + lane < end ? pick.of(r0 + lane) : -1;
-    each_adapter(mine, 0, 1, [&](int e, uint64_t rows) {
-      const uint32_t base = counts[wave * count + e];      // (this wave's own word)
-      if (mine == e) order[base + __popcll(rows & ((1ull << lane) - 1))] = (int)(r0 + lane);
-      if (lane == 0) counts[wave * count + e] = base + __popcll(rows);
-      __builtin_amdgcn_wave_barrier();
-    });
+    const uint64_t without = __ballot(mine < 0 && r0 + lane < end), rows = same(mine);
+    if (places && (without >> lane & 1)) places[last + __popcll(without & below)] = int2{(int)(r0 + lane), mine};
+    last += __popcll(without);
+    const uint32_t base = mine >= 0 ? counts[wave * count + mine] : 0;
+    __builtin_amdgcn_wave_barrier();
+    if (mine >= 0) {
+      const uint32_t to = base + __popcll(rows & below);
+      if (places) places[to] = int2{(int)(r0 + lane), mine};
+      if (order) order[to] = (int)(r0 + lane);
+      if (!(rows & below)) counts[wave * count + mine] = base + __popcll(rows);
+    }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -882,12 +922,19 @@ int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Rows that go through the kernels for few.  7168 x 14336 bf16, forward, these and the tiles: rows of 32 adapters, rank 16: 16 rows 10 and 13 us, 64 rows 12 and 25, 256 rows 24 and 52 (rank 64: 128 rows
 // 50 and 74); of two adapters, sorted: 128 rows 14 and 18 (rank 64: 35 and 35), 256 rows 21 and 24; without an index 64 rows 11 and 13 (20 and 23), 128 rows 14 and 14 (34 and 23).
 int64_t few_of(bool index) { return index ? 256 : 64; }
+// Rows of many adapters are put in their order first, by a launch of one workgroup: where they are mixed, a tile has most adapters among its rows and is taken once for each; where they
+// lie together already, that launch is lost.  bf16, forward, rank 16, as they lie and in order: 6000 rows, 2048 x 8192, mixed of 3 adapters 86 and 60 us, of 8 172 and 63, of 32 359 and 68; in runs
+// of 2 49 and 60, of 8 51 and 63.  777 rows, 1365 x 5461, mixed of 8 42 and 28, in runs 23 and 28; 300 rows, 2048 x 2048, of 8, mixed or not, 13 and 18.  The gradients of A and B need the order
+// in any case, so that their pass goes by it whenever there are more than few rows.
+constexpr int SORT_FROM = 8, SORT_ROWS = 512;
+bool sorts(int64_t n, int count, bool index) { return index && n >= SORT_ROWS && count >= SORT_FROM; }
+static_assert(SORT_ROWS > 256, "");      // (more than few)
 // Row tiles of 16 in a workgroup, and how its work is dealt out: parts of the contraction and slots of adapters to fill the chip where rows are few.
 struct Deal { bool few; int ct, parts, slots; int64_t tiles; };
-Deal deal(int64_t n, int64_t K, int count, int rank, bool f32, bool index) {
+Deal deal(int64_t n, int64_t K, int count, int rank, bool f32, bool index, bool sorted) {
   if (n <= few_of(index)) return Deal{true, 0, (int)std::min<int64_t>(PARTS_MOST, up(K, FW * 512)), 1, n};
   Deal d{false, rank <= 16 ? 1 : rank <= 32 ? 2 : 4, 1, 1, up(n, 16 * RT)};
-  if (index) d.slots = (int)std::max<int64_t>(1, std::min<int64_t>({256 / d.tiles, 16 * RT, count}));
+  if (index) d.slots = (int)std::max<int64_t>(1, std::min<int64_t>({256 / d.tiles, 16 * RT, count, sorted ? up(d.tiles + count, d.tiles) : count}));
   const int64_t turns = up(K, U * (f32 ? 16 : 32)), blocks = d.tiles * d.slots * up(rank, 16 * d.ct);
   d.parts = (int)std::max<int64_t>(1, std::min<int64_t>({256 / blocks, up(turns, 2 * CW), PARTS_MOST}));
   return d;
@@ -900,9 +947,18 @@ void contract(const Contract& all, const Pick& pick, const Deal& d, hipStream_t 
     return;
   }
   const dim3 grid((unsigned)(d.tiles * d.slots), (unsigned)all.parts, (unsigned)up(pick.rank, 16 * d.ct)), block(CW * 64);
-  if (d.ct == 1) hipLaunchKernelGGL((contract_kernel<F32, 1>), grid, block, 0, s, all, pick);
-  else if (d.ct == 2) hipLaunchKernelGGL((contract_kernel<F32, 2>), grid, block, 0, s, all, pick);
-  else hipLaunchKernelGGL((contract_kernel<F32, 4>), grid, block, 0, s, all, pick);
+  auto go = [&](auto sorted) {
+    constexpr bool SORTED = decltype(sorted)::value;
+    if (d.ct == 1) hipLaunchKernelGGL((contract_kernel<F32, 1, SORTED>), grid, block, 0, s, all, pick);
+    else if (d.ct == 2) hipLaunchKernelGGL((contract_kernel<F32, 2, SORTED>), grid, block, 0, s, all, pick);
+    else hipLaunchKernelGGL((contract_kernel<F32, 4, SORTED>), grid, block, 0, s, all, pick);
+  };
+  if (pick.order) go(std::true_type{});
+  else go(std::false_type{});
+}
+void order_rows(const Pick& pick, int64_t n, int rows_a_chunk, int2* places, int* order, Chunk* chunks, int* first, hipStream_t s) {
+  const int waves = (int)std::min<int64_t>({16, PLAN_WORDS / pick.count, up(n, 64)});
+  hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(1024), 0, s, pick, (int)n, waves, (uint32_t)rows_a_chunk, places, order, chunks, first);
 }
 template <bool F32>
 void expand(const Expand& q, const Pick& pick, hipStream_t s) {
@@ -915,18 +971,18 @@ void expand(const Expand& q, const Pick& pick, hipStream_t s) {
   a.subs = 4;
   while (a.subs > 1 && up(q.n, a.subs * 16) * blocks < 512) a.subs /= 2;
   const int64_t tiles = up(q.n, 16 * a.subs);
-  a.slots = pick.index ? (int)std::max<int64_t>(1, std::min<int64_t>({2048 / (tiles * blocks), 16 * a.subs, q.n, pick.count})) : 1;
+  a.slots = pick.index ? (int)std::max<int64_t>(1, std::min<int64_t>({2048 / (tiles * blocks), 16 * a.subs, q.n, pick.order ? up(tiles + pick.count, tiles) : pick.count})) : 1;
   const dim3 grid((unsigned)(tiles * blocks), (unsigned)a.slots), block(EW * 64);
-  auto go = [&](auto parts) {
-    constexpr bool PARTS = decltype(parts)::value;
+  auto go = [&](auto parts, auto sorted) {
+    constexpr bool PARTS = decltype(parts)::value, SORTED = decltype(sorted)::value;
     if (pick.rank <= Columns<F32>::STEP) {
-      if (F32 && a.subs < 4) hipLaunchKernelGGL((expand_kernel<F32, 1, PARTS, !F32>), grid, block, 0, s, a, pick);
-      else hipLaunchKernelGGL((expand_kernel<F32, 1, PARTS, true>), grid, block, 0, s, a, pick);
-    } else if (pick.rank <= 2 * Columns<F32>::STEP) hipLaunchKernelGGL((expand_kernel<F32, 2, PARTS, true>), grid, block, 0, s, a, pick);
-    else hipLaunchKernelGGL((expand_kernel<F32, 0, PARTS, true>), grid, block, 0, s, a, pick);
+      if (F32 && a.subs < 4) hipLaunchKernelGGL((expand_kernel<F32, 1, PARTS, !F32, SORTED>), grid, block, 0, s, a, pick);
+      else hipLaunchKernelGGL((expand_kernel<F32, 1, PARTS, true, SORTED>), grid, block, 0, s, a, pick);
+    } else if (pick.rank <= 2 * Columns<F32>::STEP) hipLaunchKernelGGL((expand_kernel<F32, 2, PARTS, true, SORTED>), grid, block, 0, s, a, pick);
+    else hipLaunchKernelGGL((expand_kernel<F32, 0, PARTS, true, SORTED>), grid, block, 0, s, a, pick);
   };
-  if (a.parts > 1) go(std::true_type{});
-  else go(std::false_type{});
+  if (a.parts > 1) pick.order ? go(std::true_type{}, std::true_type{}) : go(std::true_type{}, std::false_type{});
+  else pick.order ? go(std::false_type{}, std::true_type{}) : go(std::false_type{}, std::false_type{});
 }
 template <bool F32, int PIECES>
 void outer(const Outers& q, const Plan& plan, const Pick& pick, int64_t chunks, hipStream_t s) {
@@ -970,13 +1026,16 @@ extern "C" size_t osscar_adapters_workspace_bytes(const osscar_adapters_desc* d,
   if (d->n == 0 && !backward) return 256;
   const bool f32 = d->dtype == OSSCAR_F32;
   if (!backward) {
-    c.take(t_bytes(*d, deal(std::max<int64_t>(d->n, 1), d->d, d->count, d->rank, f32, d->index != 0).parts));
+    const bool sorted = sorts(d->n, d->count, d->index != 0);
+    c.take(t_bytes(*d, deal(std::max<int64_t>(d->n, 1), d->d, d->count, d->rank, f32, d->index != 0, sorted).parts));
+    if (sorted) c.take((size_t)d->n * 8);
   } else {
-    c.take(t_bytes(*d, deal(std::max<int64_t>(d->n, 1), d->m, d->count, d->rank, f32, d->index != 0).parts));      // dT in parts
+    c.take(t_bytes(*d, deal(std::max<int64_t>(d->n, 1), d->m, d->count, d->rank, f32, d->index != 0, d->index != 0).parts));      // dT in parts
     c.take(t_bytes(*d, 1));                                                      // dT
     c.take(t_bytes(*d, 1));                                                      // T, where it is not given
     const int64_t chunks = chunks_of(*d);
     if (d->index) {
+      c.take((size_t)d->n * 8);
       c.take((size_t)d->n * 4);
       c.take((size_t)chunks * sizeof(Chunk));
       c.take((size_t)(d->count + 1) * 4);
@@ -1003,15 +1062,18 @@ extern "C" osscar_status osscar_adapters_forward(const osscar_adapters_desc* d, 
   if (d->n == 0) return OSSCAR_OK;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   const bool f32 = d->dtype == OSSCAR_F32;
-  const Pick pick{index_dev, scale_dev, ranks_dev, d->count, d->rank};
-  const Deal deal1 = deal(d->n, d->d, d->count, d->rank, f32, d->index != 0);
+  const bool sorted = sorts(d->n, d->count, d->index != 0);
+  const Deal deal1 = deal(d->n, d->d, d->count, d->rank, f32, d->index != 0, sorted);
   Carve c(workspace_dev);
   float* t = reinterpret_cast<float*>(c.take(t_bytes(*d, deal1.parts)));
+  int2* places = sorted ? reinterpret_cast<int2*>(c.take((size_t)d->n * 8)) : nullptr;
+  const Pick pick{index_dev, scale_dev, ranks_dev, d->count, d->rank, places};
   if (!workspace_dev || c.used > workspace_bytes) return refuse_call(OSSCAR_ENOMEM, "osscar_adapters_forward: workspace too small");
   const bool direct = T_dev && deal1.parts == 1;
   if (direct) t = T_dev;
   const Contract k{Mat{X_dev, d->ldx}, Adapters{A_dev, d->lda, d->next_a}, d->n, (int)d->d, deal1.parts, deal1.slots, 0, t};
   const Expand x{t, deal1.parts, 1, 1, 1, Adapters{B_dev, d->ldb, d->next_b}, Mat{base_dev, ldbase}, d->n, (int)d->m, Y_dev, ldy, direct ? nullptr : T_dev};
+  if (sorted) order_rows(pick, d->n, 1, places, nullptr, nullptr, nullptr, s);
   if (f32) {
     contract<true>(k, pick, deal1, s);
     expand<true>(x, pick, s);
@@ -1044,17 +1106,19 @@ extern "C" osscar_status osscar_adapters_backward(const osscar_adapters_desc* d,
   if ((!grads && !dX_dev) || (d->n == 0 && !grads)) return OSSCAR_OK;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   const bool f32 = d->dtype == OSSCAR_F32, index = d->index != 0;
-  const Pick pick{index_dev, scale_dev, ranks_dev, d->count, d->rank};
   const int64_t chunks = chunks_of(*d);
-  Deal dy = deal(std::max<int64_t>(d->n, 1), d->m, d->count, d->rank, f32, index), dx = deal(std::max<int64_t>(d->n, 1), d->d, d->count, d->rank, f32, index);
+  const bool sorted = index && d->n > few_of(true) && (grads || sorts(d->n, d->count, true));      // (the gradients of A and B need the order in any case)
+  Deal dy = deal(std::max<int64_t>(d->n, 1), d->m, d->count, d->rank, f32, index, sorted), dx = deal(std::max<int64_t>(d->n, 1), d->d, d->count, d->rank, f32, index, sorted);
   Carve c(workspace_dev);
   float* dt_parts = reinterpret_cast<float*>(c.take(t_bytes(*d, dy.parts)));
   float* dt = reinterpret_cast<float*>(c.take(t_bytes(*d, 1)));
   float* t = reinterpret_cast<float*>(c.take(t_bytes(*d, 1)));
+  int2* places = nullptr;
   int* order = nullptr;
   Chunk* table = nullptr;
   int* first = nullptr;
   if (index) {
+    places = reinterpret_cast<int2*>(c.take((size_t)d->n * 8));
     order = reinterpret_cast<int*>(c.take((size_t)d->n * 4));
     table = reinterpret_cast<Chunk*>(c.take((size_t)chunks * sizeof(Chunk)));
     first = reinterpret_cast<int*>(c.take((size_t)(d->count + 1) * 4));
@@ -1062,7 +1126,9 @@ extern "C" osscar_status osscar_adapters_backward(const osscar_adapters_desc* d,
   float* part_a = reinterpret_cast<float*>(c.take((size_t)chunks * d->rank * d->d * 4));
   float* part_b = reinterpret_cast<float*>(c.take((size_t)chunks * d->rank * d->m * 4));
   if (c.used > 0 && (!workspace_dev || c.used > workspace_bytes)) return refuse_call(OSSCAR_ENOMEM, "osscar_adapters_backward: workspace too small");
+  const Pick pick{index_dev, scale_dev, ranks_dev, d->count, d->rank, sorted ? places : nullptr};
   if (d->n > 0) {
+    if (index && (grads || sorted)) order_rows(pick, d->n, chunk_of(*d), sorted ? places : nullptr, order, table, first, s);
     if (!dX_dev) dy.parts = 1;      // (the parts are added where dX is made)
     if (dy.parts == 1) dt_parts = dt;
     const Contract k{Mat{dY_dev, lddy}, Adapters{B_dev, d->ldb, d->next_b}, d->n, (int)d->m, dy.parts, dy.slots, 1, dt_parts};
@@ -1080,10 +1146,6 @@ extern "C" osscar_status osscar_adapters_backward(const osscar_adapters_desc* d,
       if (f32) contract<true>(k2, pick, dx, s);
       else contract<false>(k2, pick, dx, s);
       T_dev = t;
-    }
-    if (index) {
-      const int waves = (int)std::min<int64_t>({16, PLAN_WORDS / d->count, up(d->n, 64)});
-      hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(1024), 0, s, pick, (int)d->n, waves, (uint32_t)chunk_of(*d), order, table, first);
     }
   }
   const bool listed = index && d->n > 0;

@@ -325,6 +325,82 @@ def test_adapters_captured_and_on_another_stream(osscar):
         torch.cuda.synchronize()
 
 
+# rows of many adapters are put in their order: sizes at both sides of that, most tiles with several adapters, more adapters than rows
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,d,m,count,r", [(511, 130, 264, 8, 12), (512, 130, 264, 8, 12), (512, 97, 300, 7, 16), (640, 2100, 391, 9, 33), (1100, 130, 1030, 40, 20), (700, 64, 72, 4096, 2), (3333, 264, 200, 17, 70)])
+def test_adapters_rows_put_in_order(osscar, n, d, m, count, r, dtype):
+    g = _gen(n + count)
+    X, dY, A, B, more = _case(g, n, d, m, count, r, dtype, "mixed", ragged=True)
+    base, dbase = _randn(g, n, m, dtype=dtype), _randn(g, n, d, dtype=dtype)
+    Y, T, got = _check(osscar, X, dY, A, B, more, base, dbase)
+    # a row's result does not know where it lies, nor its neighbours'
+    at = torch.randperm(n, generator=g, device=DEV)
+    moved = dict(more, index=more["index"][at].contiguous())
+    Y2, T2 = osscar.osscar_adapters_forward(X[at].contiguous(), A, B, base=base[at].contiguous(), save=True, **moved)
+    dX2 = osscar.osscar_adapters_backward(X[at].contiguous(), A, B, dY[at].contiguous(), T=T2, base=dbase[at].contiguous(), **moved)[0]
+    assert torch.equal(Y2, Y[at]) and torch.equal(T2, T[at]) and torch.equal(dX2, got[0][at])
+    # in place
+    out = base.clone()
+    osscar.osscar_adapters_forward(X, A, B, base=out, out=out, **more)
+    assert torch.equal(out, Y)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_adapters_rows_put_in_order_without_adapters_and_with_wrong_ones(osscar, dtype):
+    g = _gen(15)
+    n, d, m, count, r = 900, 200, 300, 12, 8
+    X, dY, A, B, more = _case(g, n, d, m, count, r, dtype, "mixed")
+    base, dbase = _randn(g, n, m, dtype=dtype), _randn(g, n, d, dtype=dtype)
+    good = osscar.osscar_adapters_forward(X, A, B, base=base, **more)
+    index = more["index"].clone()
+    wrong = [0, 40, 64, 513, 899]
+    index[wrong] = torch.tensor([count, 1 << 40, count + 1, 15, 1 << 32], device=DEV)
+    index[700:790] = torch.tensor([-1, -5, -(1 << 40)], device=DEV).repeat(30)
+    rest = torch.tensor([k for k in range(n) if k not in wrong and not 700 <= k < 790], device=DEV)
+    for out, dout in ((None, None), (base.clone(), dbase.clone())):
+        use = dict(more, index=index)
+        Y, T = osscar.osscar_adapters_forward(X, A, B, base=base if out is None else out, out=out, save=True, **use)
+        dX, dA, dB = osscar.osscar_adapters_backward(X, A, B, dY, T=T, base=dbase if dout is None else dout, out=dout, **use)
+        assert torch.isnan(Y[wrong]).all() and torch.isnan(dX[wrong]).all() and not T[wrong].any()
+        assert torch.equal(Y[700:790], base[700:790]) and torch.equal(dX[700:790], dbase[700:790]) and not T[700:790].any()
+        assert torch.equal(Y[rest], good[rest]) and torch.isfinite(dX[rest]).all() and torch.isfinite(dA).all() and torch.isfinite(dB).all()
+    none = dict(more, index=torch.full((n,), -1, device=DEV))
+    Y, T = osscar.osscar_adapters_forward(X, A, B, save=True, **none)
+    dX, dA, dB = osscar.osscar_adapters_backward(X, A, B, dY, T=T, **none)
+    assert not Y.any() and not T.any() and not dX.any() and not dA.any() and not dB.any()
+    X, A = X.clone(), A.clone()      # what is not finite stays with its rows
+    X[5] = math.nan
+    A[3] = math.inf
+    clean = [k for k in rest.tolist() if k != 5 and index[k] != 3]
+    assert torch.equal(osscar.osscar_adapters_forward(X, A, B, base=base, **dict(more, index=index))[clean], good[clean])
+
+
+def test_adapters_rows_put_in_order_in_graphs(osscar):
+    g = _gen(16)
+    X, dY, A, B, more = _case(g, 600, 400, 264, 20, 16, BF16, "mixed")
+
+    def both():
+        Y, T = osscar.osscar_adapters_forward(X, A, B, save=True, **more)
+        return (Y, T) + tuple(osscar.osscar_adapters_backward(X, A, B, dY, T=T, **more))
+
+    both()
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = both()
+        graphs.append((graph, out))
+    for k in range(5):
+        X.copy_(_randn(g, 600, 400, dtype=BF16))
+        more["index"].copy_(torch.randint(-1, (22, 3, 20)[k % 3], (600,), generator=g, device=DEV))
+        graph, out = graphs[k % 2]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(torch.nan_to_num(x), torch.nan_to_num(y)) and torch.equal(torch.isnan(x), torch.isnan(y)) for x, y in zip(out, both()))
+        torch.cuda.synchronize()
+
+
 def test_adapters_refusals(osscar):
     X, dY, base = torch.zeros(4, 16, device=DEV), torch.zeros(4, 24, device=DEV), torch.zeros(4, 24, device=DEV)
     A, B = torch.zeros(2, 3, 16, device=DEV), torch.zeros(2, 3, 24, device=DEV)
