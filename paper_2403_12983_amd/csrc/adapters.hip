@@ -648,7 +648,8 @@ struct Plan {
 };
 // One workgroup; waves take the rows in spans, in order, so that an adapter's rows keep theirs.  Each wave counts its span by adapter; after sums over waves
 // and adapters it goes over the span again, 64 rows at a time, and gives rows of one adapter their places together.  Rows without one come last (in `places` alone).  A lane finds the
-// others with its adapter by the bits of the number: with a turn for each adapter, and sums in LDS by atomics, 16384 rows of 1000 adapters took 89 us more.  777 rows of 3 adapters 4 us.
+// others with its adapter by the bits of the number: with a turn for each adapter, and sums in LDS by atomics, 16384 rows of 1000 adapters took 89 us more.  One compute unit, bound by its vector instructions: 6000 rows in runs of 8 adapters 9 us, 16384 16 (12 and 24 without the shortcut for 64 rows of one adapter
+// and with the masks made twice); 777 rows of 3 adapters 4 us.
 constexpr int PLAN_WORDS = 32768;      // of LDS: counts by wave and adapter
 static_assert(OSSCAR_ADAPTERS_MAX * 2 <= PLAN_WORDS, "");
 __global__ __launch_bounds__(1024) void plan_kernel(Pick pick, int n, int waves, uint32_t rows_a_chunk, int2* places, int* order, Chunk* chunks, int* first) {
@@ -662,6 +663,7 @@ __global__ __launch_bounds__(1024) void plan_kernel(Pick pick, int n, int waves,
   const int bits = 32 - __clz(count);
   auto same = [&](int mine) {      // the lanes whose rows have this one's adapter (one bit of its number after the other; -1 and -2 are none)
     uint64_t rows = __ballot(mine >= 0);
+    if (!__ballot(mine != __builtin_amdgcn_readfirstlane(mine))) return rows;      // (in runs most often: all the same)
     for (int b = 0; b < bits; b++) {
       const uint64_t set = __ballot(mine >> b & 1);
       rows &= mine >> b & 1 ? set : ~set;
@@ -669,14 +671,30 @@ __global__ __launch_bounds__(1024) void plan_kernel(Pick pick, int n, int waves,
     return rows;
   };
   const uint64_t below = (1ull << lane) - 1;
+  constexpr int AT_ONCE = 8;      // times 64 rows, of which the reads are on their way together; those that a wave begins with stay for the second time
+  auto read = [&](int64_t r0, int (&mine)[AT_ONCE]) {
+#pragma unroll
+    for (int b = 0; b < AT_ONCE; b++) mine[b] = pick.of(std::min<int64_t>(r0 + b * 64 + lane, n - 1));
+  };
   uint32_t none = 0;
+  int kept[AT_ONCE];
+  uint64_t kept_rows[AT_ONCE];
+  read(begin, kept);
   if (wave < waves)
-    for (int64_t r0 = begin; r0 < end; r0 += 64) {
-      const int mine = r0 + lane < end ? pick.of(r0 + lane) : -1;
-      const uint64_t rows = same(mine);
-      if (mine >= 0 && !(rows & below)) counts[wave * count + mine] += __popcll(rows);      // (this wave's own word)
-      if (mine < 0 && r0 + lane < end) none++;
-      __builtin_amdgcn_wave_barrier();
+    for (int64_t r0 = begin; r0 < end; r0 += AT_ONCE * 64) {
+      int some[AT_ONCE];
+      if (r0 > begin) read(r0, some);
+#pragma unroll
+      for (int b = 0; b < AT_ONCE; b++) {
+        if (r0 + b * 64 >= end) break;
+        const bool is = r0 + b * 64 + lane < end;
+        const int mine = !is ? -1 : r0 > begin ? some[b] : kept[b];
+        const uint64_t rows = same(mine);
+        if (r0 == begin) kept_rows[b] = rows;
+        if (mine >= 0 && !(rows & below)) counts[wave * count + mine] += __popcll(rows);      // (this wave's own word)
+        if (mine < 0 && is) none++;
+        __builtin_amdgcn_wave_barrier();
+      }
     }
   for (int o = 32; o > 0; o >>= 1) none += __shfl_xor(none, o, 64);
   if (lane == 0) wave_none[wave] = none;
@@ -718,20 +736,27 @@ __global__ __launch_bounds__(1024) void plan_kernel(Pick pick, int n, int waves,
   if (wave >= waves) return;
   uint32_t last = 0;      // rows without an adapter lie behind all others
   for (int w = 0; w < 16; w++) last += wave_rows[w] + (w < wave ? wave_none[w] : 0);
-  for (int64_t r0 = begin; r0 < end; r0 += 64) {
-    const int mine = r0 + lane < end ? pick.of(r0 + lane) : -1;
-    const uint64_t without = __ballot(mine < 0 && r0 + lane < end), rows = same(mine);
-    if (places && (without >> lane & 1)) places[last + __popcll(without & below)] = int2{(int)(r0 + lane), mine};
-    last += __popcll(without);
-    const uint32_t base = mine >= 0 ? counts[wave * count + mine] : 0;
-    __builtin_amdgcn_wave_barrier();
-    if (mine >= 0) {
-      const uint32_t to = base + __popcll(rows & below);
-      if (places) places[to] = int2{(int)(r0 + lane), mine};
-      if (order) order[to] = (int)(r0 + lane);
-      if (!(rows & below)) counts[wave * count + mine] = base + __popcll(rows);
+  for (int64_t r0 = begin; r0 < end; r0 += AT_ONCE * 64) {
+    int some[AT_ONCE];
+    if (r0 > begin) read(r0, some);
+#pragma unroll
+    for (int b = 0; b < AT_ONCE; b++) {
+      const int64_t r = r0 + b * 64 + lane;
+      if (r0 + b * 64 >= end) break;
+      const int mine = r >= end ? -1 : r0 > begin ? some[b] : kept[b];
+      const uint64_t without = __ballot(mine < 0 && r < end), rows = r0 > begin ? same(mine) : kept_rows[b];
+      if (places && (without >> lane & 1)) places[last + __popcll(without & below)] = int2{(int)r, mine};
+      last += __popcll(without);
+      const uint32_t base = mine >= 0 ? counts[wave * count + mine] : 0;
+      __builtin_amdgcn_wave_barrier();
+      if (mine >= 0) {
+        const uint32_t to = base + __popcll(rows & below);
+        if (places) places[to] = int2{(int)r, mine};
+        if (order) order[to] = (int)r;
+        if (!(rows & below)) counts[wave * count + mine] = base + __popcll(rows);
+      }
+      __builtin_amdgcn_wave_barrier();
     }
-    __builtin_amdgcn_wave_barrier();
   }
 }
 
