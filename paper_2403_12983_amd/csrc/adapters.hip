@@ -948,8 +948,8 @@ int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // 50 and 74); of two adapters, sorted: 128 rows 14 and 18 (rank 64: 35 and 35), 256 rows 21 and 24; without an index 64 rows 11 and 13 (20 and 23), 128 rows 14 and 14 (34 and 23).
 int64_t few_of(bool index) { return index ? 256 : 64; }
 // Rows of many adapters are put in their order first, by a launch of one workgroup: where they are mixed, a tile has most adapters among its rows and is taken once for each; where they
-// lie together already, that launch is lost.  bf16, forward, rank 16, as they lie and in order: 6000 rows, 2048 x 8192, mixed of 3 adapters 86 and 60 us, of 8 172 and 63, of 32 359 and 68; in runs
-// of 2 49 and 60, of 8 51 and 63.  777 rows, 1365 x 5461, mixed of 8 42 and 28, in runs 23 and 28; 300 rows, 2048 x 2048, of 8, mixed or not, 13 and 18.  The gradients of A and B need the order
+// lie together already, that launch is lost.  bf16, forward, rank 16, as they lie and in order: 6000 rows, 2048 x 8192, mixed of 3 adapters 86 and 59 us, of 8 172 and 63, of 32 359 and 66; in runs
+// of 2 49 and 59, of 8 51 and 61.  777 rows, 1365 x 5461, mixed of 8 42 and 28, in runs 23 and 28; 300 rows, 2048 x 2048, of 8, mixed or not, 13 and 18.  The gradients of A and B need the order
 // in any case, so that their pass goes by it whenever there are more than few rows.
 constexpr int SORT_FROM = 8, SORT_ROWS = 512;
 bool sorts(int64_t n, int count, bool index) { return index && n >= SORT_ROWS && count >= SORT_FROM; }
