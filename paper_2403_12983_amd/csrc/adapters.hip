@@ -649,7 +649,7 @@ struct Plan {
 // One workgroup; waves take the rows in spans, in order, so that an adapter's rows keep theirs.  Each wave counts its span by adapter; after sums over waves
 // and adapters it goes over the span again, 64 rows at a time, and gives rows of one adapter their places together.  Rows without one come last (in `places` alone).  A lane finds the
 // others with its adapter by the bits of the number: with a turn for each adapter, and sums in LDS by atomics, 16384 rows of 1000 adapters took 89 us more.  One compute unit, bound by its vector instructions: 6000 rows in runs of 8 adapters 9 us, 16384 16 (12 and 24 without the shortcut for 64 rows of one adapter
-// and with the masks made twice); 777 rows of 3 adapters 4 us.
+// and with the masks made twice); 777 rows of 3 mixed adapters 6 us.
 constexpr int PLAN_WORDS = 32768;      // of LDS: counts by wave and adapter
 static_assert(OSSCAR_ADAPTERS_MAX * 2 <= PLAN_WORDS, "");
 __global__ __launch_bounds__(1024) void plan_kernel(Pick pick, int n, int waves, uint32_t rows_a_chunk, int2* places, int* order, Chunk* chunks, int* first) {
