@@ -77,6 +77,7 @@ def lib_path() -> str:
 
 
 _LIB = None
+_TENSORS = None
 
 
 def load_library():
@@ -149,6 +150,18 @@ def load_library():
             getattr(lib, name).restype = C.c_int
     _LIB = lib
     return lib
+
+
+def load_tensors():
+    """The module that reads lists of tensors (csrc/tensors.cpp); built with the library."""
+    global _TENSORS
+    if _TENSORS is None:
+        try:
+            from . import _tensors
+        except ImportError as e:
+            raise FileNotFoundError("_tensors.so is missing or of another torch: build it with `python -m paper_2403_12983_amd.build` (or __graft_entry__.build())") from e
+        _TENSORS = _tensors
+    return _TENSORS
 
 
 def _dtype_code(t: torch.dtype) -> int:

@@ -1,17 +1,27 @@
-"""Builds libosscar.so (HIP, gfx950) in-tree with hipcc.  Run as a module or call build()."""
+"""Builds libosscar.so (HIP, gfx950) in-tree with hipcc, and the module that reads lists of tensors for the binding (host C++ on torch's headers).  Run as a module or call build()."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libosscar.so")
+TENSORS = os.path.join(HERE, "_tensors.so")
 SOURCES = ["gemm.hip", "gemm64.hip", "i8gemm.hip", "gram.hip", "tableau.hip", "lazy.hip", "swap.hip", "swaprun.hip", "api.hip", "noalloc.hip",
            "gated.hip", "intprod.hip", "logprobs.hip", "layernorm.hip", "adapters.hip", "adamw.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-result", "-Wno-unused-value"]
+
+
+def _tensors_command():
+    import torch
+    root = os.path.dirname(os.path.abspath(torch.__file__))
+    return [os.environ.get("CXX", "g++"), "-O2", "-fPIC", "-shared", "-std=c++17", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            *(f"-I{d}" for d in (os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"])),
+            os.path.join(CSRC, "tensors.cpp"), "-o", TENSORS, f"-L{os.path.join(root, 'lib')}", "-lc10", "-ltorch_cpu", "-ltorch_python"]
 
 
 def build(verbose: bool = False) -> str:
@@ -25,10 +35,12 @@ def build(verbose: bool = False) -> str:
             print(" ".join(cmd), flush=True)
         procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
         objs.append(obj)
+    cmd = _tensors_command()
+    procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     for cmd, pr in procs:
         out, _ = pr.communicate()
         if pr.returncode != 0:
-            raise RuntimeError("hipcc failed: %s\n%s" % (" ".join(cmd), out))
+            raise RuntimeError("compiler failed: %s\n%s" % (" ".join(cmd), out))
         if verbose:
             sys.stdout.write("\n".join(l for l in out.splitlines() if "packed-fp32-ops" not in l))
     cmd = [hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", *objs, "-o", LIB]

@@ -13,11 +13,12 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import math
 from typing import List, NamedTuple, Optional, Sequence, Tuple, Union
 
 import torch
 
-from .binding import OSSCAR_ACT_SILU, OSSCAR_BF16, OSSCAR_F32, OSSCAR_I8, OsscarError, _AdamWDesc, _AdamWTensor, _AdaptersDesc, _GatedDesc, load_library
+from .binding import OSSCAR_ACT_SILU, OSSCAR_BF16, OSSCAR_F32, OSSCAR_I8, OsscarError, _AdamWDesc, _AdamWTensor, _AdaptersDesc, _GatedDesc, load_library, load_tensors
 
 _CODES = {torch.float32: OSSCAR_F32, torch.bfloat16: OSSCAR_BF16}
 _EINVAL = 1
@@ -483,31 +484,17 @@ def osscar_adapters_backward(X: torch.Tensor, A: torch.Tensor, B: torch.Tensor, 
 _BLOCK = 256
 
 
-def _place(t: torch.Tensor) -> Tuple[Tuple[int, ...], Tuple[int, ...]]:
-    """Shape, and strides where they say something."""
-    shape, stride = t.shape, t.stride()
-    return shape, stride if 1 not in shape else tuple(s for k, s in zip(shape, stride) if k > 1)
-
-
-def _dense(t: torch.Tensor) -> bool:
-    """Whether the elements fill a piece of memory, in any order of the dimensions."""
-    if t.is_contiguous():
-        return True
-    at = 1
-    for stride, size in sorted((s, k) for s, k in zip(t.stride(), t.shape) if k > 1):
-        if stride != at:
-            return False
-        at *= size
-    return True
-
-
-class AdamWState(NamedTuple):
-    """The states of one parameter, in the order of its memory: float32 m and v; or in 8 bits codes of m (float8_e4m3fn) and of sqrt(v) (uint8), with a float32
-    scale for every 256 of them."""
+class _StateTensors(NamedTuple):
     m: torch.Tensor
     v: torch.Tensor
     m_scale: Optional[torch.Tensor] = None
     v_scale: Optional[torch.Tensor] = None
+
+
+class AdamWState(_StateTensors):
+    """The states of one parameter, in the order of its memory: float32 m and v; or in 8 bits codes of m (float8_e4m3fn) and of sqrt(v) (uint8), with a float32
+    scale for every 256 of them.  place: shape and strides of the parameter that 8-bit states were last stepped with."""
+    place: Optional[Tuple[Tuple[int, ...], Tuple[int, ...]]] = None
 
 
 class AdamWValues(NamedTuple):
@@ -516,137 +503,135 @@ class AdamWValues(NamedTuple):
     root: torch.Tensor
 
 
-class AdamW:
-    """A list of parameters with their gradients and states, looked over once; osscar_adamw makes a step over all of them.
+def _listed(tensors):
+    return tensors if tensors is None or type(tensors) is list else list(tensors)
+
+
+def _rows(params: Optional[list], grads: Optional[list], masters: Optional[list], states: list, bits: int, index: int):
+    """The table of osscar_adamw, of tensors as they are now: an address is read at each call, so that none is used after its memory went elsewhere."""
+    table = (_AdamWTensor * len(states))()
+    why = load_tensors().adamw_rows(C.addressof(table), params, grads, masters, states, bits, index)
+    if why is not None:
+        _refuse(why)
+    return table
+
+
+def _bits(states: list) -> int:
+    return 8 if states[0][2] is not None else 32
+
+
+def _scalar(t: torch.Tensor, dtype: torch.dtype, what: str, index: int) -> int:
+    if t.dtype != dtype or t.numel() != 1 or t.get_device() != index:
+        _refuse(f"{what} must be one {dtype} on cuda:{index}")
+    return t.data_ptr()
+
+
+def _adamw(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], states: Sequence[AdamWState], lr: Union[float, torch.Tensor], step: Union[int, torch.Tensor], beta1: float = 0.9,
+                 beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01, masters: Optional[Sequence[Optional[torch.Tensor]]] = None, grad_scale: Optional[torch.Tensor] = None,
+                 seed: Optional[int] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """One step of AdamW over a list of parameters, in place; autograd does not see it.
 
     params: float32 or bfloat16 on one GPU, any shape, their elements side by side in memory (a transposed matrix will do).  grads: of the same shapes and layouts, float32 or
-    bfloat16; they may also be given, or given anew, at each step.  masters: a float32 copy for bfloat16 parameters, or None, as a list or None for all.  states: one AdamWState per
-    parameter, or None: zeros in `bits` bits.  The plan holds the tensors and writes to where they were when it was made; autograd does not see it."""
+    bfloat16.  states: one AdamWState per parameter, all of 32 or all of 8 bits (AdamW(params, bits=8).states makes zeros).  masters: a float32 copy for bfloat16 parameters, or None, as a
+    list or None for all.  step counts from 1; lr and step may be tensors of one element on the GPU (float32, int64), which a captured step reads anew at each replay; the tensors of
+    the lists it reads and writes where they were when it was captured.  grad_scale: one float32 on the GPU that the gradients are multiplied by; where it is not finite nothing
+    changes.  seed (32 bits, another for each step; a step on the GPU is added to it): 8-bit states, and bfloat16 parameters without a master, are rounded up by chance instead of
+    to the nearest."""
+    params, grads, masters, states = _listed(params), _listed(grads), _listed(masters), _listed(states)
+    if not params or len(states) != len(params):
+        _refuse("states have one entry per parameter, and there is one parameter at least")
+    if grads is None:
+        _refuse("no gradients were given")
+    lib, index, handle, context = _begin(params[0], stream)
+    bits = _bits(states)
+    table = _rows(params, grads, masters, states, bits, index)
+    desc = _AdamWDesc(0.0, beta1, beta2, eps, weight_decay, 1, None, None, None, 0, 0, bits)
+    if isinstance(lr, torch.Tensor):
+        desc.lr_dev = _scalar(lr, torch.float32, "lr", index)
+    else:
+        desc.lr = lr
+    if isinstance(step, torch.Tensor):
+        desc.step_dev = _scalar(step, torch.int64, "step", index)
+    else:
+        desc.step = step
+    if grad_scale is not None:
+        desc.grad_scale_dev = _scalar(grad_scale, torch.float32, "grad_scale", index)
+    if seed is not None:
+        if not 0 <= seed < 1 << 32:
+            _refuse("seed has 32 bits")
+        desc.seed, desc.stochastic = seed, 1
+    with context:
+        status = lib.osscar_adamw(table, len(params), C.byref(desc), handle)
+    _done(lib, status)
+
+
+def _adamw_values(states: Sequence[AdamWState], stream: Optional[torch.cuda.Stream] = None) -> List[AdamWValues]:
+    """What 8-bit states stand for, one AdamWValues each, of the shape and layout of the parameter that the state was last stepped with (one that was not: a vector)."""
+    states = _listed(states)
+    if not states:
+        _refuse("no states")
+    if _bits(states) != 8:
+        _refuse("states of 32 bits are their own values")
+    device = states[0][0].device
+    lib, index, handle, context = _begin(states[0][0], stream)
+    table = _rows(None, None, None, states, 8, index)
+    with context:
+        values = []
+        for row, s in zip(table, states):
+            place = getattr(s, "place", None)
+            if place is None or math.prod(place[0]) != row.n:
+                place = (row.n,), (1,)
+            values.append(AdamWValues(*(torch.empty_strided(*place, dtype=torch.bfloat16, device=device) for _ in range(2))))
+        outs = C.c_void_p * len(values)
+        status = lib.osscar_adamw_values(table, len(values), outs(*(x.m.data_ptr() for x in values)), outs(*(x.root.data_ptr() for x in values)), handle)
+    _done(lib, status)
+    return values
+
+
+class AdamW:
+    """The lists of osscar_adamw kept together: parameters, masters, states, and the gradients that were given last.
+
+    params, grads, masters: as osscar_adamw takes them; grads may also be given, or given anew, at each step.  states: one AdamWState per parameter, or None: zeros in `bits` bits.  Each step looks
+    at the tensors again: one that was moved, as by `p.data = ...`, is stepped where it is now, and one that no longer goes with its state, master or gradient is refused."""
 
     def __init__(self, params: Sequence[torch.Tensor], grads: Optional[Sequence[torch.Tensor]] = None, bits: Optional[int] = None,
                  masters: Optional[Sequence[Optional[torch.Tensor]]] = None, states: Optional[Sequence[AdamWState]] = None):
         self.params = list(params)
         if not self.params:
             _refuse("no parameters")
-        count = len(self.params)
-        self.masters = [None] * count if masters is None else list(masters)
+        self.masters = [None] * len(self.params) if masters is None else list(masters)
         if states is not None:
-            states = [AdamWState(*s) for s in states]
+            states = [s if isinstance(s, AdamWState) else AdamWState(*s) for s in states]
+            if len(states) != len(self.params):
+                _refuse("states have one entry per parameter")
         if bits is None:
             bits = 8 if states and states[0].m_scale is not None else 32
         if bits not in (8, 32):
             _refuse("states have 8 or 32 bits")
-        self.bits, self._device = bits, self.params[0].device
-        self._index = self.params[0].get_device()
-        self._lib = _begin(self.params[0], None)[0]
-        self._table = (_AdamWTensor * count)()
-        self._places = [_place(p) for p in self.params]
-        if len(self.masters) != count or (states is not None and len(states) != count):
-            _refuse("masters and states have one entry per parameter")
-        self.states: List[AdamWState] = []
-        written = []      # (address, end, parameter) of what a step writes
-        for k, (p, master) in enumerate(zip(self.params, self.masters)):
-            n = p.numel()
-            code = _CODES.get(p.dtype)
-            if code is None:
-                _refuse(f"parameter {k} is neither float32 nor bfloat16")
-            if not _dense(p):
-                _refuse(f"the elements of parameter {k} are not side by side")
-            if master is not None and (p.dtype != torch.bfloat16 or master.dtype != torch.float32 or _place(master) != self._places[k]):
-                _refuse(f"master {k} must be float32, of the shape and layout of a bfloat16 parameter")
-            s = self._zeros(n) if states is None else states[k]
-            blocks = -(-n // _BLOCK)
-            kinds = ((s.m, n, (torch.float32,)), (s.v, n, (torch.float32,))) if bits == 32 else (
-                (s.m, n, (torch.float8_e4m3fn, torch.uint8)), (s.v, n, (torch.uint8,)), (s.m_scale, blocks, (torch.float32,)), (s.v_scale, blocks, (torch.float32,)))
-            for t, size, dtypes in kinds:
-                if t is None or t.numel() != size or t.dtype not in dtypes or not t.is_contiguous():
-                    _refuse(f"state {k} is not of {bits} bits and parameter {k}'s size, side by side")
-            for t in (p, master, *s):
-                if t is None:
-                    continue
-                if t.get_device() != self._index:
-                    _refuse(f"parameter {k}, its master or its state is on {t.device}, expected cuda:{self._index}")
-                size = t.numel()
-                if size > 0:
-                    at = t.data_ptr()
-                    written.append((at, at + size * t.element_size(), k))
-            self.states.append(s)
-            self._table[k] = _AdamWTensor(n, p.data_ptr(), None if master is None else master.data_ptr(), None, s.m.data_ptr(), s.v.data_ptr(),
-                                          s.m_scale.data_ptr() if bits == 8 else None, s.v_scale.data_ptr() if bits == 8 else None, code, 0)
-        written.sort()
-        for (_, end, a), (start, _, b) in zip(written, written[1:]):
-            if start < end:
-                _refuse(f"parameters {a} and {b} or their states share memory")
-        self.grads: Optional[List[torch.Tensor]] = None
-        if grads is not None:
-            self._take(grads)
+        self.bits = bits
+        index = _begin(self.params[0], None)[1]
+        self.states: List[AdamWState] = [self._zeros(p) for p in self.params] if states is None else states
+        self.grads: Optional[List[torch.Tensor]] = None if grads is None else list(grads)
+        _rows(self.params, self.grads, self.masters, self.states, bits, index)
 
-    def _zeros(self, n: int) -> AdamWState:
+    def _zeros(self, p: torch.Tensor) -> AdamWState:
+        n, device = p.numel(), self.params[0].device
         if self.bits == 32:
-            return AdamWState(torch.zeros(n, dtype=torch.float32, device=self._device), torch.zeros(n, dtype=torch.float32, device=self._device))
+            return AdamWState(torch.zeros(n, dtype=torch.float32, device=device), torch.zeros(n, dtype=torch.float32, device=device))
         blocks = -(-n // _BLOCK)
-        return AdamWState(torch.zeros(n, dtype=torch.uint8, device=self._device).view(torch.float8_e4m3fn), torch.zeros(n, dtype=torch.uint8, device=self._device),
-                          torch.zeros(blocks, dtype=torch.float32, device=self._device), torch.zeros(blocks, dtype=torch.float32, device=self._device))
-
-    def _take(self, grads: Sequence[torch.Tensor]):
-        grads = list(grads)
-        if len(grads) != len(self.params):
-            _refuse("one gradient per parameter")
-        for k, g in enumerate(grads):
-            if g.dtype not in _CODES:
-                _refuse(f"gradient {k} is neither float32 nor bfloat16")
-            if _place(g) != self._places[k]:
-                _refuse(f"gradient {k} has another shape or layout than its parameter")
-            if g.get_device() != self._index:
-                _refuse(f"gradient {k} is on {g.device}, expected cuda:{self._index}")
-        for row, g in zip(self._table, grads):
-            row.g, row.g_dtype = g.data_ptr(), _CODES[g.dtype]
-        self.grads = grads
-
-    def _scalar(self, t: torch.Tensor, dtype: torch.dtype, what: str) -> int:
-        if t.dtype != dtype or t.numel() != 1 or t.get_device() != self._index:
-            _refuse(f"{what} must be one {dtype} on cuda:{self._index}")
-        return t.data_ptr()
+        return AdamWState(torch.zeros(n, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn), torch.zeros(n, dtype=torch.uint8, device=device),
+                          torch.zeros(blocks, dtype=torch.float32, device=device), torch.zeros(blocks, dtype=torch.float32, device=device))
 
     def osscar_adamw(self, lr: Union[float, torch.Tensor], step: Union[int, torch.Tensor], beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
                      grads: Optional[Sequence[torch.Tensor]] = None, grad_scale: Optional[torch.Tensor] = None, seed: Optional[int] = None,
                      stream: Optional[torch.cuda.Stream] = None) -> None:
-        """One step of AdamW, in place.  step counts from 1; lr and step may be tensors of one element on the GPU (float32, int64), which a captured step reads anew at each replay.
-        grads: new gradients, kept for later steps.  grad_scale: one float32 on the GPU that the gradients are multiplied by; where it is not finite nothing
-        changes.  seed (32 bits, another for each step; a step on the GPU is added to it): 8-bit states, and bfloat16 parameters without a master, are rounded up by chance instead of
-        to the nearest."""
-        if grads is not None:
-            self._take(grads)
-        if self.grads is None:
-            _refuse("no gradients were given")
-        lib, _, handle, context = _begin(self.params[0], stream)
-        desc = _AdamWDesc(0.0, beta1, beta2, eps, weight_decay, 1, None, None, None, 0, 0, self.bits)
-        if isinstance(lr, torch.Tensor):
-            desc.lr_dev = self._scalar(lr, torch.float32, "lr")
-        else:
-            desc.lr = lr
-        if isinstance(step, torch.Tensor):
-            desc.step_dev = self._scalar(step, torch.int64, "step")
-        else:
-            desc.step = step
-        if grad_scale is not None:
-            desc.grad_scale_dev = self._scalar(grad_scale, torch.float32, "grad_scale")
-        if seed is not None:
-            if not 0 <= seed < 1 << 32:
-                _refuse("seed has 32 bits")
-            desc.seed, desc.stochastic = seed, 1
-        with context:
-            status = lib.osscar_adamw(self._table, len(self.params), C.byref(desc), handle)
-        _done(lib, status)
+        """One step, in place.  grads: new gradients, kept for later steps."""
+        grads = self.grads if grads is None else list(grads)
+        _adamw(self.params, grads, self.states, lr, step, beta1, beta2, eps, weight_decay, self.masters, grad_scale, seed, stream)
+        self.grads = grads
 
     def osscar_adamw_values(self, stream: Optional[torch.cuda.Stream] = None) -> List[AdamWValues]:
-        """What the 8-bit states stand for, one AdamWValues per parameter."""
-        if self.bits != 8:
-            _refuse("states of 32 bits are their own values")
-        lib, _, handle, context = _begin(self.params[0], stream)
-        with context:
-            values = [AdamWValues(torch.empty_like(p, dtype=torch.bfloat16, requires_grad=False), torch.empty_like(p, dtype=torch.bfloat16, requires_grad=False)) for p in self.params]
-            outs = C.c_void_p * len(values)
-            status = lib.osscar_adamw_values(self._table, len(values), outs(*(x.m.data_ptr() for x in values)), outs(*(x.root.data_ptr() for x in values)), handle)
-        _done(lib, status)
-        return values
+        """What the 8-bit states stand for, one AdamWValues per parameter, of its shape."""
+        index = _begin(self.params[0], None)[1]
+        _rows(self.params, None, self.masters, self.states, self.bits, index)      # (a parameter that no longer goes with its state is refused)
+        return _adamw_values(self.states, stream)
