@@ -526,7 +526,7 @@ def _scalar(t: torch.Tensor, dtype: torch.dtype, what: str, index: int) -> int:
     return t.data_ptr()
 
 
-def _adamw(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], states: Sequence[AdamWState], lr: Union[float, torch.Tensor], step: Union[int, torch.Tensor], beta1: float = 0.9,
+def osscar_adamw(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], states: Sequence[AdamWState], lr: Union[float, torch.Tensor], step: Union[int, torch.Tensor], beta1: float = 0.9,
                  beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01, masters: Optional[Sequence[Optional[torch.Tensor]]] = None, grad_scale: Optional[torch.Tensor] = None,
                  seed: Optional[int] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """One step of AdamW over a list of parameters, in place; autograd does not see it.
@@ -565,7 +565,7 @@ def _adamw(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], states
     _done(lib, status)
 
 
-def _adamw_values(states: Sequence[AdamWState], stream: Optional[torch.cuda.Stream] = None) -> List[AdamWValues]:
+def osscar_adamw_values(states: Sequence[AdamWState], stream: Optional[torch.cuda.Stream] = None) -> List[AdamWValues]:
     """What 8-bit states stand for, one AdamWValues each, of the shape and layout of the parameter that the state was last stepped with (one that was not: a vector)."""
     states = _listed(states)
     if not states:
@@ -625,13 +625,13 @@ class AdamW:
     def osscar_adamw(self, lr: Union[float, torch.Tensor], step: Union[int, torch.Tensor], beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
                      grads: Optional[Sequence[torch.Tensor]] = None, grad_scale: Optional[torch.Tensor] = None, seed: Optional[int] = None,
                      stream: Optional[torch.cuda.Stream] = None) -> None:
-        """One step, in place.  grads: new gradients, kept for later steps."""
+        """osscar_adamw over the lists.  grads: new gradients, kept for later steps."""
         grads = self.grads if grads is None else list(grads)
-        _adamw(self.params, grads, self.states, lr, step, beta1, beta2, eps, weight_decay, self.masters, grad_scale, seed, stream)
+        osscar_adamw(self.params, grads, self.states, lr, step, beta1, beta2, eps, weight_decay, self.masters, grad_scale, seed, stream)
         self.grads = grads
 
     def osscar_adamw_values(self, stream: Optional[torch.cuda.Stream] = None) -> List[AdamWValues]:
         """What the 8-bit states stand for, one AdamWValues per parameter, of its shape."""
         index = _begin(self.params[0], None)[1]
         _rows(self.params, None, self.masters, self.states, self.bits, index)      # (a parameter that no longer goes with its state is refused)
-        return _adamw_values(self.states, stream)
+        return osscar_adamw_values(self.states, stream)

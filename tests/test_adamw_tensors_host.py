@@ -103,3 +103,32 @@ def test_what_is_no_list_of_tensors_is_refused(library):
                  lambda: pkg.AdamW([torch.zeros(4, 4).to_sparse()]), lambda: pkg.AdamW([p], [torch.zeros(4).to_sparse()])):
         with pytest.raises((pkg.OsscarError, AttributeError)):
             call()
+
+
+def test_the_call_without_a_list_kept(library):
+    params, grads = [torch.zeros(300), torch.zeros(20, 30).t(), torch.zeros(5, dtype=BF16)], [torch.zeros(300), torch.zeros(20, 30).t(), torch.zeros(5, dtype=BF16)]
+    masters = [None, None, torch.zeros(5)]
+    for bits in (8, 32):
+        states = pkg.AdamW(params, bits=bits).states
+        fresh = [pkg.AdamWState(*s) for s in states]      # the same memory
+        pkg.osscar_adamw(params, grads, fresh, 1e-3, 1, masters=masters)
+        assert library.rows == _rows(params, grads, masters, states)
+        pkg.osscar_adamw(tuple(params), tuple(grads), tuple(states), 1e-3, 1)
+        assert library.rows == _rows(params, grads, [None] * 3, states)
+        if bits == 8:
+            values = pkg.osscar_adamw_values(fresh)
+            assert [(x.m.shape, x.m.stride(), x.root.stride(), x.m.dtype) for x in values] == [(p.shape, p.stride(), p.stride(), BF16) for p in params]
+            assert [x.m.shape for x in pkg.osscar_adamw_values([pkg.AdamWState(*s) for s in states])] == [(300,), (600,), (5,)]
+            pkg.osscar_adamw([torch.zeros(600)], [torch.zeros(600)], fresh[1:2], 1e-3, 1)
+            assert pkg.osscar_adamw_values(fresh[1:2])[0].root.shape == (600,)
+    s32, s8 = pkg.AdamW(params).states, pkg.AdamW(params, bits=8).states
+    library.rows = None
+    for call in (lambda: pkg.osscar_adamw([], [], [], 1e-3, 1), lambda: pkg.osscar_adamw(params, grads[:2], s32, 1e-3, 1), lambda: pkg.osscar_adamw(params, grads, s32[:2], 1e-3, 1),
+                 lambda: pkg.osscar_adamw(params, None, s32, 1e-3, 1), lambda: pkg.osscar_adamw(params, grads, s32, 1e-3, 1, masters=masters[:2]), lambda: pkg.osscar_adamw(params, grads, s8[:1] + s32[1:], 1e-3, 1),
+                 lambda: pkg.osscar_adamw(params, grads, s32[:2] + s8[2:], 1e-3, 1), lambda: pkg.osscar_adamw([params[0]] * 2, [grads[0]] * 2, [s32[0], pkg.AdamWState(*(t.clone() for t in s32[0][:2]))], 1e-3, 1),
+                 lambda: pkg.osscar_adamw(params, grads, s32, torch.tensor(1e-3, dtype=torch.double), 1), lambda: pkg.osscar_adamw(params, grads, s32, 1e-3, torch.tensor(1, dtype=torch.int32)),
+                 lambda: pkg.osscar_adamw(params, grads, s32, 1e-3, 1, seed=1 << 32), lambda: pkg.osscar_adamw(params, grads, s32, 1e-3, 1, grad_scale=torch.ones(2)),
+                 lambda: pkg.osscar_adamw_values(s32), lambda: pkg.osscar_adamw_values([]), lambda: pkg.osscar_adamw_values(s8[:1] + s32[1:])):
+        with pytest.raises(pkg.OsscarError) as e:
+            call()
+        assert e.value.status == 1 and library.rows is None
