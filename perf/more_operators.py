@@ -196,9 +196,6 @@ def prepare(case, seed):
         state["states"] = [(state["m"][a:a + c], state["v"][a:a + c],
                             None if case["bits"] == 32 else state["m_scale"][a // _BLOCK:a // _BLOCK + k], None if case["bits"] == 32 else state["v_scale"][a // _BLOCK:a // _BLOCK + k])
                            for a, c, k in zip(starts, flat, blocks)]
-        if own:      # what a training program makes once for its tensors: the list of them, looked over
-            import paper_2403_12983_amd as osscar
-            state["plan"] = osscar.AdamW(state["params"], state["grads"], masters=state["masters"], states=[osscar.AdamWState(*x) for x in state["states"]])
     return state
 
 
@@ -232,15 +229,16 @@ def _adapters_own(state, case):
 
 
 def _adamw_own(state, case):
-    plan = state["plan"]
-    plan.osscar_adamw(_LR, _STEP, _B1, _B2, _ADAM_EPS, _WD, seed=_STEP if case["stochastic"] else None)
+    import paper_2403_12983_amd as osscar
+    states = [osscar.AdamWState(*s) for s in state["states"]]
+    osscar.osscar_adamw(state["params"], state["grads"], states, _LR, _STEP, _B1, _B2, _ADAM_EPS, _WD, masters=state["masters"], seed=_STEP if case["stochastic"] else None)
     out = {"param": state["param"]}
     if state["master"] is not None:
         out["master"] = state["master"]
     if case["bits"] == 32:
         out.update(m=state["m"], v=state["v"])
     else:
-        values = plan.osscar_adamw_values()
+        values = osscar.osscar_adamw_values(states)
         out.update(m=[x.m for x in values], root=[x.root for x in values])
     return out
 
