@@ -442,7 +442,8 @@ osscar_status osscar_adapters_forward(const osscar_adapters_desc* desc, const vo
                                       void* workspace_dev, size_t workspace_bytes, void* hip_stream);
 /* Gradients, given dY (n x m, leading dimension lddy):  dT_i = s_e B_e dY_i,  dX_i = base_i + A_e^T dT_i,  dA_e = sum of dT_i x_i^T and dB_e = s_e sum of T_i dY_i^T over the rows of
  * e.  T_dev: what forward left there, or NULL: computed again.  base_dev: n x d, leading dimension ldbase, NULL (zeros) or dX itself (the gradient that came through the
- * shared projection).  dX_dev may be NULL, dA_dev and dB_dev too (both or neither): dense, of the shapes of A and B, dw_dtype, written, not added to, zeros for adapters and components without
+ * shared projection).  dX_dev may be NULL, or dY_dev or X_dev, which are read first (and base too: around a square projection they may be one).  dA_dev and dB_dev may be NULL (both or
+ * neither): dense, of the shapes of A and B, dw_dtype, written, not added to, zeros for adapters and components without
  * rows, in an order that does not change from call to call.  A row whose index is `count` or more has dX of NaN and no part in dA and dB. */
 osscar_status osscar_adapters_backward(const osscar_adapters_desc* desc, const void* X_dev, const void* A_dev, const void* B_dev, const int64_t* index_dev,
                                        const float* scale_dev, const int32_t* ranks_dev, const void* dY_dev, int64_t lddy, const float* T_dev, const void* base_dev, int64_t ldbase,

@@ -627,6 +627,15 @@ __global__ __launch_bounds__(256) void expand_few_kernel(Expand q, Pick pick) {
   E8::store(q.y, row * q.ldy + c, y, most);
 }
 
+// T's parts added, in the order that expand adds them in: where dX takes the place of dY or X, the outer products come before it and want T whole (n rank numbers, a few us at most).
+__global__ __launch_bounds__(256) void add_parts_kernel(const float* part, int parts, int64_t size, float* t) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= size) return;
+  float s = part[i];
+  for (int p = 1; p < parts; p++) s += part[p * size + i];
+  t[i] = s;
+}
+
 // --------------------------------------------------------------------------------------------------
 // outer
 // --------------------------------------------------------------------------------------------------
@@ -1041,6 +1050,11 @@ const char* bad_desc(const osscar_adapters_desc* d) {
   return nullptr;
 }
 bool misaligned(const void* p, int32_t dtype) { return (uintptr_t)p % (dtype == OSSCAR_F32 ? 4 : 2) != 0; }
+// Whether rows of one matrix reach into the memory of another's (n > 0 rows)
+bool meet(const void* a, int64_t lda, int64_t d, const void* b, int64_t ldb, int64_t m, int64_t n, int32_t dtype) {
+  const uintptr_t size = dtype == OSSCAR_F32 ? 4 : 2, p = (uintptr_t)a, q = (uintptr_t)b;
+  return p < q + ((n - 1) * ldb + m) * size && q < p + ((n - 1) * lda + d) * size;
+}
 size_t t_bytes(const osscar_adapters_desc& d, int parts) { return (size_t)parts * d.n * d.rank * 4; }
 
 }  // namespace
@@ -1152,6 +1166,13 @@ extern "C" osscar_status osscar_adapters_backward(const osscar_adapters_desc* d,
   float* part_b = reinterpret_cast<float*>(c.take((size_t)chunks * d->rank * d->m * 4));
   if (c.used > 0 && (!workspace_dev || c.used > workspace_bytes)) return refuse_call(OSSCAR_ENOMEM, "osscar_adapters_backward: workspace too small");
   const Pick pick{index_dev, scale_dev, ranks_dev, d->count, d->rank, sorted ? places : nullptr};
+  // The outer products read X and dY: where dX takes the place of one of them, it comes behind
+  const bool late = grads && dX_dev && d->n > 0 && (meet(dX_dev, lddx, d->d, dY_dev, lddy, d->m, d->n, d->dtype) || meet(dX_dev, lddx, d->d, X_dev, d->ldx, d->d, d->n, d->dtype));
+  auto make_dx = [&] {
+    const Expand x{dt_parts, dy.parts, 1, 0, 1, Adapters{A_dev, d->lda, d->next_a}, Mat{base_dev, ldbase}, d->n, (int)d->d, dX_dev, lddx, dy.parts > 1 ? dt : nullptr};
+    if (f32) expand<true>(x, pick, s);
+    else expand<false>(x, pick, s);
+  };
   if (d->n > 0) {
     if (index && (grads || sorted)) order_rows(pick, d->n, chunk_of(*d), sorted ? places : nullptr, order, table, first, s);
     if (!dX_dev) dy.parts = 1;      // (the parts are added where dX is made)
@@ -1159,11 +1180,13 @@ extern "C" osscar_status osscar_adapters_backward(const osscar_adapters_desc* d,
     const Contract k{Mat{dY_dev, lddy}, Adapters{B_dev, d->ldb, d->next_b}, d->n, (int)d->m, dy.parts, dy.slots, 1, dt_parts};
     if (f32) contract<true>(k, pick, dy, s);
     else contract<false>(k, pick, dy, s);
-    if (dX_dev) {
-      const Expand x{dt_parts, dy.parts, 1, 0, 1, Adapters{A_dev, d->lda, d->next_a}, Mat{base_dev, ldbase}, d->n, (int)d->d, dX_dev, lddx, dy.parts > 1 ? dt : nullptr};
-      if (f32) expand<true>(x, pick, s);
-      else expand<false>(x, pick, s);
+    if (late && dy.parts > 1) {      // (few rows: 2^12 at most)
+      const int64_t size = d->n * d->rank;
+      hipLaunchKernelGGL(add_parts_kernel, dim3((unsigned)up(size, 256)), dim3(256), 0, s, dt_parts, dy.parts, size, dt);
+      dt_parts = dt;
+      dy.parts = 1;
     }
+    if (dX_dev && !late) make_dx();
     if (!grads) return launched();
     if (!T_dev) {
       dx.parts = 1;
@@ -1181,6 +1204,7 @@ extern "C" osscar_status osscar_adapters_backward(const osscar_adapters_desc* d,
     else if (dw_dtype == OSSCAR_F32) outer<false, 3>(both, plan, pick, chunks, s);
     else outer<false, 2>(both, plan, pick, chunks, s);
   }
+  if (late) make_dx();
   const int blocks_a = (int)up(d->d, 1024);
   hipLaunchKernelGGL(join_kernel, dim3((unsigned)(blocks_a + up(d->m, 1024)), (unsigned)std::min<int64_t>((int64_t)d->count * d->rank, 65535)), dim3(256), 0, s,
                      Join{part_a, (int)d->d, dA_dev}, Join{part_b, (int)d->m, dB_dev}, blocks_a, plan, pick, dw_dtype == OSSCAR_F32);

@@ -450,7 +450,7 @@ def osscar_adapters_backward(X: torch.Tensor, A: torch.Tensor, B: torch.Tensor, 
                              scale: Optional[torch.Tensor] = None, ranks: Optional[torch.Tensor] = None, base: Optional[torch.Tensor] = None, need_x: bool = True,
                              need_w: bool = True, dw_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """(dX, dA, dB) of osscar_adapters_forward for the gradient dY of Y; None for what is not needed.  T: from forward's save=True (else it is computed again).  base: n x d, what
-    dX is added to, as the gradient that came through the projection (None: zeros).  out: where to put dX, `base` itself included.  dw_dtype: float32 or
+    dX is added to, as the gradient that came through the projection (None: zeros).  out: where to put dX, `base`, `dY` or `X` itself included.  dw_dtype: float32 or
     bfloat16, by default the adapters'."""
     lib, at, handle, context = _begin(X, stream)
     desc, (xp, ap, bp, ip, sp, rp) = _adapters(X, A, B, index, scale, ranks, at)
