@@ -1057,6 +1057,27 @@ bool meet(const void* a, int64_t lda, int64_t d, const void* b, int64_t ldb, int
 }
 size_t t_bytes(const osscar_adapters_desc& d, int parts) { return (size_t)parts * d.n * d.rank * 4; }
 
+// (the gradients of A and B need the order in any case)
+bool sorts_backward(const osscar_adapters_desc& d, bool grads) { return d.index && d.n > few_of(true) && (grads || sorts(d.n, d.count, true)); }
+struct BackwardSpace { float *dt_parts, *dt, *t; int2* places; int* order; Chunk* table; int* first; float *part_a, *part_b; };
+BackwardSpace backward_space(Carve& c, const osscar_adapters_desc& d, bool grads, int parts) {
+  BackwardSpace w{};
+  w.dt_parts = reinterpret_cast<float*>(c.take(t_bytes(d, parts)));
+  if (sorts_backward(d, grads)) w.places = reinterpret_cast<int2*>(c.take((size_t)d.n * 8));
+  if (!grads) return w;
+  const int64_t chunks = chunks_of(d);
+  w.dt = reinterpret_cast<float*>(c.take(t_bytes(d, 1)));
+  w.t = reinterpret_cast<float*>(c.take(t_bytes(d, 1)));      // where T is not given
+  if (d.index) {
+    w.order = reinterpret_cast<int*>(c.take((size_t)d.n * 4));
+    w.table = reinterpret_cast<Chunk*>(c.take((size_t)chunks * sizeof(Chunk)));
+    w.first = reinterpret_cast<int*>(c.take((size_t)(d.count + 1) * 4));
+  }
+  w.part_a = reinterpret_cast<float*>(c.take((size_t)chunks * d.rank * d.d * 4));
+  w.part_b = reinterpret_cast<float*>(c.take((size_t)chunks * d.rank * d.m * 4));
+  return w;
+}
+
 }  // namespace
 
 extern "C" size_t osscar_adapters_workspace_bytes(const osscar_adapters_desc* d, int32_t backward) {
@@ -1069,18 +1090,8 @@ extern "C" size_t osscar_adapters_workspace_bytes(const osscar_adapters_desc* d,
     c.take(t_bytes(*d, deal(std::max<int64_t>(d->n, 1), d->d, d->count, d->rank, f32, d->index != 0, sorted).parts));
     if (sorted) c.take((size_t)d->n * 8);
   } else {
-    c.take(t_bytes(*d, deal(std::max<int64_t>(d->n, 1), d->m, d->count, d->rank, f32, d->index != 0, d->index != 0).parts));      // dT in parts
-    c.take(t_bytes(*d, 1));                                                      // dT
-    c.take(t_bytes(*d, 1));                                                      // T, where it is not given
-    const int64_t chunks = chunks_of(*d);
-    if (d->index) {
-      c.take((size_t)d->n * 8);
-      c.take((size_t)d->n * 4);
-      c.take((size_t)chunks * sizeof(Chunk));
-      c.take((size_t)(d->count + 1) * 4);
-    }
-    c.take((size_t)chunks * d->rank * d->d * 4);
-    c.take((size_t)chunks * d->rank * d->m * 4);
+    const bool grads = backward != 2;
+    backward_space(c, *d, grads, deal(std::max<int64_t>(d->n, 1), d->m, d->count, d->rank, f32, d->index != 0, sorts_backward(*d, grads)).parts);
   }
   return c.used + 256;
 }
@@ -1146,26 +1157,13 @@ extern "C" osscar_status osscar_adapters_backward(const osscar_adapters_desc* d,
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   const bool f32 = d->dtype == OSSCAR_F32, index = d->index != 0;
   const int64_t chunks = chunks_of(*d);
-  const bool sorted = index && d->n > few_of(true) && (grads || sorts(d->n, d->count, true));      // (the gradients of A and B need the order in any case)
+  const bool sorted = sorts_backward(*d, grads);
   Deal dy = deal(std::max<int64_t>(d->n, 1), d->m, d->count, d->rank, f32, index, sorted), dx = deal(std::max<int64_t>(d->n, 1), d->d, d->count, d->rank, f32, index, sorted);
   Carve c(workspace_dev);
-  float* dt_parts = reinterpret_cast<float*>(c.take(t_bytes(*d, dy.parts)));
-  float* dt = reinterpret_cast<float*>(c.take(t_bytes(*d, 1)));
-  float* t = reinterpret_cast<float*>(c.take(t_bytes(*d, 1)));
-  int2* places = nullptr;
-  int* order = nullptr;
-  Chunk* table = nullptr;
-  int* first = nullptr;
-  if (index) {
-    places = reinterpret_cast<int2*>(c.take((size_t)d->n * 8));
-    order = reinterpret_cast<int*>(c.take((size_t)d->n * 4));
-    table = reinterpret_cast<Chunk*>(c.take((size_t)chunks * sizeof(Chunk)));
-    first = reinterpret_cast<int*>(c.take((size_t)(d->count + 1) * 4));
-  }
-  float* part_a = reinterpret_cast<float*>(c.take((size_t)chunks * d->rank * d->d * 4));
-  float* part_b = reinterpret_cast<float*>(c.take((size_t)chunks * d->rank * d->m * 4));
+  const BackwardSpace w = backward_space(c, *d, grads, dy.parts);
   if (c.used > 0 && (!workspace_dev || c.used > workspace_bytes)) return refuse_call(OSSCAR_ENOMEM, "osscar_adapters_backward: workspace too small");
-  const Pick pick{index_dev, scale_dev, ranks_dev, d->count, d->rank, sorted ? places : nullptr};
+  float *dt_parts = w.dt_parts, *const dt = w.dt;      // (dt, whole, is wanted by the outer products alone)
+  const Pick pick{index_dev, scale_dev, ranks_dev, d->count, d->rank, w.places};
   // The outer products read X and dY: where dX takes the place of one of them, it comes behind
   const bool late = grads && dX_dev && d->n > 0 && (meet(dX_dev, lddx, d->d, dY_dev, lddy, d->m, d->n, d->dtype) || meet(dX_dev, lddx, d->d, X_dev, d->ldx, d->d, d->n, d->dtype));
   auto make_dx = [&] {
@@ -1174,9 +1172,9 @@ extern "C" osscar_status osscar_adapters_backward(const osscar_adapters_desc* d,
     else expand<false>(x, pick, s);
   };
   if (d->n > 0) {
-    if (index && (grads || sorted)) order_rows(pick, d->n, chunk_of(*d), sorted ? places : nullptr, order, table, first, s);
+    if (index && (grads || sorted)) order_rows(pick, d->n, chunk_of(*d), w.places, w.order, w.table, w.first, s);
     if (!dX_dev) dy.parts = 1;      // (the parts are added where dX is made)
-    if (dy.parts == 1) dt_parts = dt;
+    if (dy.parts == 1 && grads) dt_parts = dt;
     const Contract k{Mat{dY_dev, lddy}, Adapters{B_dev, d->ldb, d->next_b}, d->n, (int)d->m, dy.parts, dy.slots, 1, dt_parts};
     if (f32) contract<true>(k, pick, dy, s);
     else contract<false>(k, pick, dy, s);
@@ -1190,15 +1188,15 @@ extern "C" osscar_status osscar_adapters_backward(const osscar_adapters_desc* d,
     if (!grads) return launched();
     if (!T_dev) {
       dx.parts = 1;
-      const Contract k2{Mat{X_dev, d->ldx}, Adapters{A_dev, d->lda, d->next_a}, d->n, (int)d->d, 1, dx.slots, 0, t};
+      const Contract k2{Mat{X_dev, d->ldx}, Adapters{A_dev, d->lda, d->next_a}, d->n, (int)d->d, 1, dx.slots, 0, w.t};
       if (f32) contract<true>(k2, pick, dx, s);
       else contract<false>(k2, pick, dx, s);
-      T_dev = t;
+      T_dev = w.t;
     }
   }
   const bool listed = index && d->n > 0;
-  const Plan plan{listed ? order : nullptr, table, first, d->n, listed ? 0 : (int)chunks, chunk_of(*d)};
-  const Outers both{Outer{dt, Mat{X_dev, d->ldx}, (int)d->d, 0, part_a}, Outer{T_dev, Mat{dY_dev, lddy}, (int)d->m, 1, part_b}, (int)up(d->d, OCOLS)};
+  const Plan plan{listed ? w.order : nullptr, w.table, w.first, d->n, listed ? 0 : (int)chunks, chunk_of(*d)};
+  const Outers both{Outer{dt, Mat{X_dev, d->ldx}, (int)d->d, 0, w.part_a}, Outer{T_dev, Mat{dY_dev, lddy}, (int)d->m, 1, w.part_b}, (int)up(d->d, OCOLS)};
   if (d->n > 0) {
     if (f32) outer<true, 1>(both, plan, pick, chunks, s);
     else if (dw_dtype == OSSCAR_F32) outer<false, 3>(both, plan, pick, chunks, s);
@@ -1207,6 +1205,6 @@ extern "C" osscar_status osscar_adapters_backward(const osscar_adapters_desc* d,
   if (late) make_dx();
   const int blocks_a = (int)up(d->d, 1024);
   hipLaunchKernelGGL(join_kernel, dim3((unsigned)(blocks_a + up(d->m, 1024)), (unsigned)std::min<int64_t>((int64_t)d->count * d->rank, 65535)), dim3(256), 0, s,
-                     Join{part_a, (int)d->d, dA_dev}, Join{part_b, (int)d->m, dB_dev}, blocks_a, plan, pick, dw_dtype == OSSCAR_F32);
+                     Join{w.part_a, (int)d->d, dA_dev}, Join{w.part_b, (int)d->m, dB_dev}, blocks_a, plan, pick, dw_dtype == OSSCAR_F32);
   return launched();
 }

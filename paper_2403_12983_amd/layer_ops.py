@@ -472,7 +472,7 @@ def osscar_adapters_backward(X: torch.Tensor, A: torch.Tensor, B: torch.Tensor, 
         dA = dB = None
         if need_w:
             dA, dB = _EMPTY(A.shape, dtype=dw_dtype, device=device), _EMPTY(B.shape, dtype=dw_dtype, device=device)
-        ws, wp, size = _workspace(lib.osscar_adapters_workspace_bytes(C.byref(desc), 1), device)
+        ws, wp, size = _workspace(lib.osscar_adapters_workspace_bytes(C.byref(desc), 1 if need_w else 2), device)
         status = lib.osscar_adapters_backward(C.byref(desc), xp, ap, bp, ip, sp, rp, dY.data_ptr(), _ld(dY, "dY"), None if T is None else T.data_ptr(),
                                               None if base is None else base.data_ptr(), d if base is None else _ld(base, "base"), dX.data_ptr() if need_x else None,
                                               _ld(dX, "out") if need_x else d, dA.data_ptr() if need_w else None, dB.data_ptr() if need_w else None, _CODES[dw_dtype], wp, size,

@@ -75,3 +75,14 @@ def test_the_binding_refuses_tensors_that_are_not_on_a_gpu():
         with pytest.raises(pkg.OsscarError) as e:
             call()
         assert e.value.status == 1
+
+
+def test_a_call_without_gradients_of_the_weights_takes_no_space_for_them(lib):
+    """Their partial sums alone (one for each adapter and component at least, of both widths) are 22 GB here."""
+    wide = dict(d=7168, ldx=7168, lda=7168, m=14336, ldb=14336, rank=64)
+    for n, count, index in ((16384, 4096, 1), (4096, 1024, 1), (300, 3, 1), (16, 32, 1), (8192, 1, 0)):
+        d = _desc(n=n, count=count, index=index, **wide)
+        full, less = (lib.osscar_adapters_workspace_bytes(C.byref(d), k) for k in (1, 2))
+        assert full > min(n, count) * 64 * (7168 + 14336) * 4 and less <= 4 * n * 64 * 4 + 8 * n + 1024      # T in four parts at most, the order of the rows
+        calls = dict(ldy=14336, ldb=7168, ldx=7168, i=P if index else None)
+        assert _backward(lib, d, dA=None, dB=None, size=less - 257, **calls) == 2 and _backward(lib, d, size=less, **calls) == 2
