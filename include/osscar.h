@@ -434,7 +434,8 @@ typedef struct {
   int32_t dtype;              /* of X, A, B, base, Y, dY, dX */
   int32_t index;              /* nonzero: the calls are given an index */
 } osscar_adapters_desc;
-/* Workspace of a forward call (backward = 0), of a backward call (1), or of one without dA and dB (2); 0 if the description is invalid. */
+/* Workspace of a forward call (backward = 0), of a backward call (1), or of one without dA and dB (2); 0 if the description is invalid (for 1: also if
+ * d and m have 2^24 blocks of 128 columns together). */
 size_t osscar_adapters_workspace_bytes(const osscar_adapters_desc* desc, int32_t backward);
 /* T_dev: dense n x rank float32 output for osscar_adapters_backward (zeros where there is no adapter or component), or NULL. */
 osscar_status osscar_adapters_forward(const osscar_adapters_desc* desc, const void* X_dev, const void* A_dev, const void* B_dev, const int64_t* index_dev,

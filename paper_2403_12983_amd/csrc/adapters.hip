@@ -1049,6 +1049,10 @@ const char* bad_desc(const osscar_adapters_desc* d) {
   if (up(d->n, 16) * up(std::max(d->d, d->m), EW * ECOLS) >= (int64_t)1 << 23) return "osscar_adapters: too large";
   return nullptr;
 }
+// (of the outer products' launch, which has the column blocks of both widths in one row of its grid)
+const char* bad_gradients(const osscar_adapters_desc& d) {
+  return launchable(up(d.d, OCOLS) + up(d.m, OCOLS), OW * 64) ? nullptr : "osscar_adapters_backward: d and m are too large together for dA and dB";
+}
 bool misaligned(const void* p, int32_t dtype) { return (uintptr_t)p % (dtype == OSSCAR_F32 ? 4 : 2) != 0; }
 // Whether rows of one matrix reach into the memory of another's (n > 0 rows)
 bool meet(const void* a, int64_t lda, int64_t d, const void* b, int64_t ldb, int64_t m, int64_t n, int32_t dtype) {
@@ -1091,6 +1095,7 @@ extern "C" size_t osscar_adapters_workspace_bytes(const osscar_adapters_desc* d,
     if (sorted) c.take((size_t)d->n * 8);
   } else {
     const bool grads = backward != 2;
+    if (grads && bad_gradients(*d)) return 0;
     backward_space(c, *d, grads, deal(std::max<int64_t>(d->n, 1), d->m, d->count, d->rank, f32, d->index != 0, sorts_backward(*d, grads)).parts);
   }
   return c.used + 256;
@@ -1146,6 +1151,7 @@ extern "C" osscar_status osscar_adapters_backward(const osscar_adapters_desc* d,
   if (!bad && (!dA_dev != !dB_dev)) bad = "osscar_adapters_backward: dA and dB are given together or not at all";
   if (!bad && base_dev && !dX_dev) bad = "osscar_adapters_backward: base goes with dX";
   if (!bad && grads && !real_dtype(dw_dtype)) bad = "osscar_adapters_backward: unknown dtype";
+  if (!bad && grads) bad = bad_gradients(*d);
   if (!bad && (misaligned(X_dev, d->dtype) || misaligned(A_dev, d->dtype) || misaligned(B_dev, d->dtype) || misaligned(base_dev, d->dtype) || misaligned(dY_dev, d->dtype) ||
                misaligned(dX_dev, d->dtype) || misaligned(T_dev, OSSCAR_F32) || misaligned(scale_dev, OSSCAR_F32) || misaligned(ranks_dev, OSSCAR_F32) || ((uintptr_t)index_dev & 7) ||
                (grads && (misaligned(dA_dev, dw_dtype) || misaligned(dB_dev, dw_dtype)))))

@@ -86,3 +86,16 @@ def test_a_call_without_gradients_of_the_weights_takes_no_space_for_them(lib):
         assert full > min(n, count) * 64 * (7168 + 14336) * 4 and less <= 4 * n * 64 * 4 + 8 * n + 1024      # T in four parts at most, the order of the rows
         calls = dict(ldy=14336, ldb=7168, ldx=7168, i=P if index else None)
         assert _backward(lib, d, dA=None, dB=None, size=less - 257, **calls) == 2 and _backward(lib, d, size=less, **calls) == 2
+
+
+def test_gradients_wider_than_a_launch_are_refused(lib):
+    """Column blocks of 128 of both widths, 256 threads each: 2^32 threads of one launch, which HIP would cut off without an error."""
+    big = 1 << 30
+    for rank in (1, 64):
+        wide = dict(n=1, d=big, ldx=big, lda=big, m=big, ldb=big, rank=rank, count=1, index=0, next_a=0, next_b=0)
+        d = _desc(**wide)
+        assert lib.osscar_adapters_workspace_bytes(C.byref(d), 1) == 0
+        assert _backward(lib, d, i=None, ldy=big, ldb=big, ldx=big) == 1 and b"osscar_adapters_backward" in lib.osscar_last_error(None)
+        # a block less, and calls without them
+        assert lib.osscar_adapters_workspace_bytes(C.byref(_desc(**{**wide, "m": big - 128})), 1) > 0
+        assert lib.osscar_adapters_workspace_bytes(C.byref(d), 0) > 0 and lib.osscar_adapters_workspace_bytes(C.byref(d), 2) > 0
