@@ -489,8 +489,8 @@ typedef struct {
 } osscar_adamw_desc;
 /* tensors: host array, read during the call. */
 osscar_status osscar_adamw(const osscar_adamw_tensor* tensors, int64_t count, const osscar_adamw_desc* desc, void* hip_stream);
-/* What 8-bit states stand for: m and sqrt v of each tensor in bf16, which holds them exactly, n elements at m_out[k] and root_out[k] (host arrays of device pointers).  Of the tensors n, m, v,
- * m_scale and v_scale are looked at. */
+/* What 8-bit states stand for: m and sqrt v of each tensor in bf16, which holds them exactly but for m of scales below 2^-124 (m reaches 2^-9 scales, bf16's steps end at 2^-133:
+ * rounded to the nearest of them, halves to even); n elements at m_out[k] and root_out[k] (host arrays of device pointers).  Of the tensors n, m, v, m_scale and v_scale are looked at. */
 osscar_status osscar_adamw_values(const osscar_adamw_tensor* tensors, int64_t count, void* const* m_out, void* const* root_out, void* hip_stream);
 
 /* Description of the last failure: of a context, or (ctx == NULL) of the last failed call on this host thread that takes

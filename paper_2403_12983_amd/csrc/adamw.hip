@@ -285,7 +285,7 @@ __global__ __launch_bounds__(T) void adamw_kernel(const Table<SMALL, MASTER, RAN
   else if (mine) store(most);
 }
 
-// What 8-bit states stand for, in bf16, which holds them exactly: 308 M 334 us, 5.5 TB/s.
+// What 8-bit states stand for, in bf16, which holds them exactly but for m of scales below 2^-124 (3 bits above steps of 2^-135): 308 M 334 us, 5.5 TB/s.
 struct Values {
   static constexpr int MOST = TABLE_BYTES / (7 * 8 + 4);
   const void *m[MOST], *v[MOST];

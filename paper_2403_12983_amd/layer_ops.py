@@ -498,7 +498,7 @@ class AdamWState(_StateTensors):
 
 
 class AdamWValues(NamedTuple):
-    """What 8-bit states stand for, in bfloat16 (exactly): m and the root of v, of the parameter's shape."""
+    """What 8-bit states stand for, in bfloat16 (exactly, but for m of scales below 2^-124, which bfloat16 has fewer bits for): m and the root of v, of the parameter's shape."""
     m: torch.Tensor
     root: torch.Tensor
 

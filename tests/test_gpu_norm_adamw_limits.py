@@ -65,3 +65,22 @@ def test_a_late_step_has_no_correction(osscar):
     f = np.float32
     m, v = g * f(1 - 0.9), (g * g) * f(1 - 0.999)
     assert np.array_equal(p.cpu().numpy(), x * f(1 - 1e-3 * 0.1) - f(1e-3) * (m / (np.sqrt(v) * f(1) + f(1e-8))))
+
+
+def test_values_of_the_smallest_states(osscar):
+    """m reaches 2^-9 scales: bf16 has steps of 2^-133, so that scales below 2^-124 leave m rounded to them (to the nearest, halves to even), and all others exact."""
+    codes = torch.tensor([c for c in range(256) if c & 127 != 127] + [0, 0], dtype=torch.uint8, device=DEV)
+    table = np.array([(-1.0 if c >> 7 else 1.0) * ((c & 7) * 2.0 ** -9 if c & 127 < 8 else (8 + (c & 7)) * 2.0 ** ((c & 127) // 8 - 10)) for c in codes.tolist()])
+    roots = np.array([c if c < 16 else (16 + c % 16) * 2.0 ** (c // 16 - 1) for c in range(256)], dtype=np.float64)
+    all_codes = torch.arange(256, device=DEV).to(torch.uint8)
+    scales = [2.0 ** -k for k in (126, 125, 124, 123, 100)]
+    scale = torch.tensor(scales, device=DEV)
+    state = osscar.AdamWState(codes.repeat(5), all_codes.repeat(5), scale, scale.clone())
+    got = osscar.osscar_adamw_values([state])[0]
+    for k, s in enumerate(scales):
+        m, root = (x[k * 256:(k + 1) * 256].double().cpu().numpy() for x in (got.m, got.root))
+        want = table * s
+        assert np.array_equal(root, roots * s)
+        step = 2.0 ** -133
+        rounded = np.where(np.abs(want) < 2.0 ** -126, np.rint(want / step) * step, want)
+        assert np.array_equal(m, rounded) and np.array_equal(rounded, want) == (s >= 2.0 ** -124)
