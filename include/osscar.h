@@ -422,7 +422,7 @@ osscar_status osscar_layernorm_backward(const void* X_dev, int64_t n, int64_t d,
  * negative one has no adapter (y = base), one with `count` or more is NaN.  Without an index every row has the first adapter.  scale: count float32 (NULL: 1).  ranks: count int32 (NULL: all of
  * `rank`), the components of each adapter that count, from the first on; the others are not read.  base may be NULL (zeros) or Y itself.  Products of bf16 are summed in float32, T is float32 and goes
  * into the second product as two bf16 pieces (16 bits; an infinity there makes its row NaN), y is rounded once.  Rows of one adapter next to each other are fastest: 32 neighbouring rows
- * are read once for each adapter that they have. */
+ * are read once for each adapter that they have; from 512 rows and 8 adapters on (backward with dA and dB: from 257 rows on) the rows are put in that order first. */
 #define OSSCAR_ADAPTERS_MAX 4096
 #define OSSCAR_ADAPTER_MAX_RANK 1024
 typedef struct {

@@ -33,7 +33,7 @@ struct Table {
 };
 struct Step {
   double lr, b1, b2, wd;
-  float eps, grad_scale;
+  float eps;
   int64_t t;
   const float *lr_dev, *scale_dev;
   const int64_t* t_dev;
@@ -415,7 +415,7 @@ extern "C" osscar_status osscar_adamw(const osscar_adamw_tensor* tensors, int64_
   for (int64_t k = 0; !bad && k < count; k++) { bad = bad_tensor(tensors[k], d->bits == 8, false); any = any || tensors[k].n > 0; }
   if (bad) return refuse_call(OSSCAR_EINVAL, bad);
   if (!any) return OSSCAR_OK;
-  const Step s{d->lr, d->beta1, d->beta2, d->weight_decay, (float)d->eps, 1.f, d->step, d->lr_dev, d->grad_scale_dev, d->step_dev, d->seed, d->stochastic != 0};
+  const Step s{d->lr, d->beta1, d->beta2, d->weight_decay, (float)d->eps, d->step, d->lr_dev, d->grad_scale_dev, d->step_dev, d->seed, d->stochastic != 0};
   const Factors f = factors_of(s, d->lr_dev ? 0 : d->lr, d->step_dev ? 1 : d->step);
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
   if (d->bits == 8 && s.random) steps_of<true, true>(tensors, count, s, f, stream);

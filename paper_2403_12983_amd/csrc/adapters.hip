@@ -3,8 +3,9 @@
 //   contract  T[i][j] = sum_k Z[i][k] V_e[j][k]        (T from X and A; dT from dY and B)
 //   expand    Y[i][c] = base[i][c] + sum_j T[i][j] V_e[j][c]      (y from T and B; dX from dT and A)
 //   outer     dV_e[j][c] = sum over the rows i of e of T[i][j] Z[i][c]      (dA from dT and X; dB from T and dY)
-// Rows go through in tiles as they lie; a tile is taken once for each adapter in it (one or two where the rows of a request lie together), each time with the
-// results of that adapter's rows kept.  All are bound by reading and writing Z, base and Y, or A and B where rows are few: 2 rank operations for each of their elements.
+// Rows go through in tiles, a tile once for each adapter in it, each time with the results of that adapter's rows kept: as they lie, or in the order of their adapters (places alone, no row is moved) from 8
+// adapters and 512 rows on, and wherever dA and dB are made of more than 256 rows.  Up to 64 rows (256 with an index) take kernels that read V once per row instead.  All are bound by reading and writing Z, base
+// and Y, or A and B where rows are few: 2 rank operations for each of their elements.
 #include "ops.h"
 #include <algorithm>
 #include <type_traits>
@@ -657,7 +658,7 @@ struct Plan {
 };
 // One workgroup; waves take the rows in spans, in order, so that an adapter's rows keep theirs.  Each wave counts its span by adapter; after sums over waves
 // and adapters it goes over the span again, 64 rows at a time, and gives rows of one adapter their places together.  Rows without one come last (in `places` alone).  A lane finds the
-// others with its adapter by the bits of the number: with a turn for each adapter, and sums in LDS by atomics, 16384 rows of 1000 adapters took 89 us more.  One compute unit, bound by its vector instructions: 6000 rows in runs of 8 adapters 9 us, 16384 16 (12 and 24 without the shortcut for 64 rows of one adapter
+// others with its adapter by the bits of the number: with a turn for each adapter, and sums in LDS by atomics, 16384 rows of 1000 adapters took 89 us more.  One compute unit, bound by its vector instructions at about 1 ns a row from there on: 6000 rows in runs of 8 adapters 9 us, 16384 16 (12 and 24 without the shortcut for 64 rows of one adapter
 // and with the masks made twice); 777 rows of 3 mixed adapters 6 us.
 constexpr int PLAN_WORDS = 32768;      // of LDS: counts by wave and adapter
 static_assert(OSSCAR_ADAPTERS_MAX * 2 <= PLAN_WORDS, "");
@@ -1027,8 +1028,8 @@ void outer(const Outers& q, const Plan& plan, const Pick& pick, int64_t chunks, 
   else hipLaunchKernelGGL((outer_kernel<F32, 4, PIECES>), grid, block, 0, s, q, plan, pick);
 }
 
-// Rows of a chunk: as many as leave two workgroups per compute unit, 128 to 512, and no more than 64 chunks of many rows (their sums are written and read again: as much as 2 rank
-// rows of bf16 each).
+// Rows of a chunk: 512, of many rows as many as leave 64 chunks (their sums are written and read again: as much as 2 rank rows of bf16 each), and half of that again and again, down to 65, while the
+// narrower width's workgroups are fewer than 512.  So a narrow width has up to 1023 chunks: 2^20 rows of 256 x 14336, rank 64, have 256 of them, 956 MB of sums.
 int chunk_of(const osscar_adapters_desc& d) {
   int chunk = (int)std::max<int64_t>(512, up(up(d.n, 64), 64) * 64);
   while (chunk > 128 && up(d.n, chunk) * up(std::min(d.d, d.m), OCOLS) * up(d.rank, 64) < 512) chunk /= 2;

@@ -126,6 +126,7 @@ __global__ __launch_bounds__(TPR* GROUPS) void forward_kernel(const void* X, Row
 // A thread has the same columns in every row that it takes, so the sums over rows stay in its registers; a workgroup's rows are added in order through LDS and go
 // to `part` ([workgroup][dw, db][d]), which a second launch adds in order.  Bound by reading X and dY and writing dX: bf16, both launches, 16384 x 2048 38 us (5.3 TB/s), 8192 x 7168 74
 // us (4.7), 100000 x 64 14 us (2.7), 4096 x 14336 100 us (3.5; with the next row and the gain in registers 158); float32 4.1 to 5.6.  512 workgroups, with twice the parts: 80 us of 74.
+// A few registers do not fit and are kept in memory: 4 of 640 and 12 of 768 threads in float32, 4 of 1024 in both types.
 template <bool F32, int TPR, int PK, int GROUPS>
 __global__ __launch_bounds__(TPR* GROUPS) void backward_kernel(const void* X, const void* dY, Rows q, int64_t lddy, int64_t lddx, const void* weight, int w_f32,
                                                                const float* __restrict__ stats, void* dX, float* part) {

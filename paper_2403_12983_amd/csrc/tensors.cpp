@@ -1,6 +1,6 @@
 // Python module _tensors: looks over the lists of tensors of an AdamW step and writes down where they are, for osscar_adamw.  A step over hundreds of small tensors takes tens of
-// microseconds on the GPU; a property of a tensor read in Python takes 35 to 70 ns and a step needs about 12 of each parameter (192 of them: 0.2 ms), here a few ns.  So every step can look
-// again, and nothing is kept by address from one to the next.
+// microseconds on the GPU; a property of a tensor read in Python takes 35 to 70 ns and a step needs about 20 of each parameter and its states.  Here a call over 192 parameters takes 12 us of the host,
+// under the 28 that its kernels take, with the gradients of the step before or new ones: so every step can look again, and nothing is kept by address from one to the next.
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ATen.h>
 #include <algorithm>
