@@ -517,7 +517,8 @@ def _rows(params: Optional[list], grads: Optional[list], masters: Optional[list]
 
 
 def _bits(states: list) -> int:
-    return 8 if states[0][2] is not None else 32
+    first = states[0]
+    return 8 if isinstance(first, tuple) and len(first) == 4 and first[2] is not None else 32
 
 
 def _scalar(t: torch.Tensor, dtype: torch.dtype, what: str, index: int) -> int:
@@ -538,7 +539,7 @@ def osscar_adamw(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], 
     changes.  seed (32 bits, another for each step; a step on the GPU is added to it): 8-bit states, and bfloat16 parameters without a master, are rounded up by chance instead of
     to the nearest."""
     params, grads, masters, states = _listed(params), _listed(grads), _listed(masters), _listed(states)
-    if not params or len(states) != len(params):
+    if not params or not states or len(states) != len(params):
         _refuse("states have one entry per parameter, and there is one parameter at least")
     if grads is None:
         _refuse("no gradients were given")

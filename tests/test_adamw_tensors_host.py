@@ -132,3 +132,26 @@ def test_the_call_without_a_list_kept(library):
         with pytest.raises(pkg.OsscarError) as e:
             call()
         assert e.value.status == 1 and library.rows is None
+
+
+def test_states_that_are_none_are_refused(library):
+    p = [torch.zeros(4)]
+    for states in (None, [], [None], [3], [(torch.zeros(4), torch.zeros(4))], [[torch.zeros(4), torch.zeros(4), None, None]], [(None, None, None, None)]):
+        for call in (lambda: pkg.osscar_adamw(p, p, states, 1e-3, 1), lambda: pkg.osscar_adamw_values(states)):
+            with pytest.raises(pkg.OsscarError) as e:
+                call()
+            assert e.value.status == 1 and not library.rows
+    pkg.osscar_adamw(p, [torch.zeros(4)], [(torch.zeros(4), torch.zeros(4), None, None)], 1e-3, 1)      # a plain tuple of all four will do
+    assert len(library.rows) == 1
+
+
+def test_the_module_has_no_substitute(monkeypatch):
+    import sys
+
+    from paper_2403_12983_amd import binding
+    assert pkg.load_tensors().adamw_rows
+    monkeypatch.setattr(binding, "_TENSORS", None)
+    monkeypatch.delattr(pkg, "_tensors", raising=False)
+    monkeypatch.setitem(sys.modules, "paper_2403_12983_amd._tensors", None)
+    with pytest.raises(FileNotFoundError, match="paper_2403_12983_amd.build"):
+        binding.load_tensors()
